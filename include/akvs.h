@@ -127,6 +127,34 @@ typedef struct akvs_reuse_out {
                               value leaves room for the tokens a decode step appends */
 } akvs_reuse_out;
 
+/* A batch of requests that go on from one shared context (akvs_shared_attention,
+ * akvs_attention_weights). Rows are new tokens, packed request by request; every row sees all
+ * keys of the shared prefix, and of its request's own keys those up to its own: the rows of a
+ * request are its last ones, so row i of its n sees own keys 0 .. own_len - n + i. */
+typedef struct akvs_shared_cfg {
+  int32_t n_req;        /* B >= 1                                                            */
+  int32_t n_rows;       /* rows that q, out and lse hold, >= 0                               */
+  int32_t rows_max;     /* the most rows of one request, >= 1                                */
+  int32_t prefix_len;   /* shared keys P, >= 0 (0: none)                                     */
+  int32_t own_rows;     /* rows per request of k_own / v_own, >= 0 (0: none)                 */
+  const int32_t *row_start; /* device [B + 1], from 0, ascending, <= n_rows: request b has rows
+                               row_start[b] .. row_start[b + 1] - 1, at most rows_max of them.
+                               NULL: every request has rows_max (n_rows = B * rows_max)        */
+  const int32_t *own_len;   /* device [B]: own keys, 0 .. own_rows (NULL where own_rows = 0)  */
+} akvs_shared_cfg;
+
+/* What akvs_evict_cache keeps. A sequence is what has a cache of its own: a layer, a request. */
+typedef struct akvs_evict_cfg {
+  int32_t n_seq;        /* S >= 1                                                            */
+  int32_t n_keys;       /* keys per sequence (of `weights`), >= 0                            */
+  int32_t src_rows;     /* rows per sequence of k / v, >= n_keys (0: n_keys)                 */
+  int32_t n_keep;       /* keys kept per sequence and KV head, >= 1                          */
+  int32_t dst_rows;     /* rows per sequence of k_out / v_out, >= n_keep (0: n_keep)         */
+  int32_t n_first, n_recent; /* always kept: the first and the last keys (n_first + n_recent
+                                <= n_keep)                                                   */
+  const int32_t *lens;  /* device [S]: keys of each sequence, 0 .. n_keys (NULL: n_keys)     */
+} akvs_evict_cfg;
+
 /* ---- library information ---------------------------------------------------- */
 int32_t akvs_version(void);
 const char *akvs_status_string(akvs_status s);
@@ -379,6 +407,81 @@ akvs_status akvs_decode_step_noalloc(const int32_t *token, int32_t n_past, const
                                      const void *w_out, const akvs_model_cfg *m, void *k_cache,
                                      void *v_cache, int32_t cache_rows, float *logits,
                                      int32_t *next_token, hipStream_t stream);
+
+/* ---- a batch over one shared context -----------------------------------------------------
+ * Serving steps of several requests that continue from the same corrected caches: the new
+ * tokens' queries and keys are normalised per head and rotated, their keys and values join
+ * their requests' own caches, every row attends to the shared prefix and to its request's own
+ * keys, the weight that each cached key received is summed, and the keys of least weight are
+ * evicted. One layer per call (akvs_evict_cache: any number of sequences). */
+
+/* Per-head RMS norms of queries and keys with the rotary map, for decoders that normalise
+ * both per head (Sec. 4.1 evaluates Qwen3): x = x rsqrt(mean(x^2) + rms_eps) * norm over hd,
+ * then the rotation at positions[r]; one rounding, at the end. Values are copied.
+ * q: [n_rows][Hq][hd], k, v: [n_rows][Hkv][hd], model dtype, row r at r * ldq / ldk / ldv
+ * elements (a packed projection output, or dense tensors; each ld * element size a multiple
+ * of 16 bytes); q_norm, k_norm: [hd] model dtype, NULL: that side is not normalised;
+ * positions: device [n_rows], each < rope_rows; kv_rows: device [n_rows] row of k_out / v_out
+ * that takes row r (one outside [0, n_kv_rows), e.g. -1, is written nowhere; rows must be
+ * distinct), NULL: row r, n_kv_rows >= n_rows then. q_out: [n_rows][Hq][hd]; k_out, v_out:
+ * [n_kv_rows][Hkv][hd]; rows that no token names stay as they were. q_out may be q where
+ * ldq = Hq * hd (k_out k and v_out v likewise, without kv_rows); no other overlap. v and v_out
+ * may both be NULL. Errors: EINVAL (negative sizes, null or misaligned pointers, strides
+ * shorter than a row or not of 16 bytes, n_kv_rows < n_rows without kv_rows), EHIP. */
+akvs_status akvs_qk_norm_rope(const void *q, int64_t ldq, const void *k, int64_t ldk,
+                              const void *v, int64_t ldv, int32_t n_rows,
+                              const int32_t *positions, const void *q_norm, const void *k_norm,
+                              const akvs_model_cfg *m, const float *rope, int32_t rope_rows,
+                              const int32_t *kv_rows, int32_t n_kv_rows, void *q_out,
+                              void *k_out, void *v_out, hipStream_t stream);
+
+/* Workspace bytes of akvs_shared_attention and akvs_attention_weights over this batch; 0 for
+ * an invalid one, or where neither needs any. */
+size_t akvs_shared_workspace_size(const akvs_model_cfg *m, const akvs_shared_cfg *c);
+
+/* Attention of a batch's rows over the shared prefix and each request's own keys, scores
+ * q.k/sqrt(hd), softmax over both together, in fp32; the prefix is read once for all requests.
+ * q: [n_rows][Hq][hd]; k_prefix, v_prefix: [P][Hkv][hd] (e.g. one layer of a reuse prefill's
+ * k_corr / v_corr); k_own, v_own: [B][own_rows][Hkv][hd]; out: [n_rows][Hq][hd]; all model
+ * dtype. lse (device [n_rows][Hq] fp32, may be NULL): natural log of the row's sum of
+ * exp(score). A row that sees no key gets out 0 and lse -inf. Keys past a row's last one are
+ * never part of its result, whatever they hold; rows from row_start[B] on stay as they were.
+ * Errors: EINVAL / ESHAPE / ENOSPACE, EHIP. */
+akvs_status akvs_shared_attention(const void *q, const akvs_shared_cfg *c, const void *k_prefix,
+                                  const void *v_prefix, const void *k_own, const void *v_own,
+                                  const akvs_model_cfg *m, void *out, float *lse, void *ws,
+                                  size_t ws_bytes, hipStream_t stream);
+
+/* Attention weight that each key received from a batch's rows, summed over the rows that see
+ * it and the Hq/Hkv query heads of its KV head, added to what it had:
+ * w[j] = w_prev[j] + sum_r sum_h exp(q.k_j/sqrt(hd) - lse[r][h]), fp32 sums in a fixed order.
+ * q, lse: as akvs_shared_attention took and left them; w_prefix, w_prefix_prev: device
+ * [Hkv][P] fp32; w_own, w_own_prev: [B][Hkv][own_rows] fp32 (keys past own_len keep what they
+ * had). A w_*_prev may be its w_* itself, or NULL (0). w_prefix or w_own may be NULL: that
+ * side is not formed. A row with lse = -inf gives nothing. */
+akvs_status akvs_attention_weights(const void *q, const float *lse, const akvs_shared_cfg *c,
+                                   const void *k_prefix, const void *k_own,
+                                   const akvs_model_cfg *m, const float *w_prefix_prev,
+                                   float *w_prefix, const float *w_own_prev, float *w_own,
+                                   void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* Workspace bytes of akvs_evict_cache (needed where `keep` is NULL); 0 if invalid. */
+size_t akvs_evict_workspace_size(const akvs_model_cfg *m, const akvs_evict_cfg *c);
+
+/* Eviction by accumulated weight: per sequence of n keys and per KV head, the first n_first
+ * and the last n_recent keys and of the others those of largest weight (equal ones: the lower
+ * index; a NaN counts as the smallest) are kept, min(n, n_keep) in all, in their order; keys
+ * and values move to rows 0.. of k_out / v_out as they are (keys keep their rotation).
+ * k, v: [S][src_rows][Hkv][hd] model dtype; weights: [S][Hkv][n_keys] fp32; keep (device
+ * [S][Hkv][n_keep], may be NULL): indices of the kept keys, -1 past the last; k_out, v_out:
+ * [S][dst_rows][Hkv][hd], rows past the kept ones stay as they were, no overlap with k or v;
+ * k, v, k_out, v_out may all be NULL (selection alone); weights_out (device
+ * [S][Hkv][dst_rows] fp32, may be NULL, not `weights`): the kept keys' weights, then 0;
+ * lens_out (device [S], may be NULL, may be lens): keys kept. */
+akvs_status akvs_evict_cache(const void *k, const void *v, const float *weights,
+                             const akvs_evict_cfg *c, const akvs_model_cfg *m, int32_t *keep,
+                             void *k_out, void *v_out, float *weights_out, int32_t *lens_out,
+                             void *ws, size_t ws_bytes, hipStream_t stream);
 
 /* ---- kernel timing -------------------------------------------------------------------
  * akvs_profile_enable(mask): for every kernel class whose bit (1 << class) is set in

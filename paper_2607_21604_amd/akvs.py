@@ -74,8 +74,23 @@ class ReuseOut(ctypes.Structure):
                 ("rows", ctypes.c_void_p), ("n_rows", ctypes.c_void_p), ("kv_rows", ctypes.c_int32)]
 
 
+class SharedCfg(ctypes.Structure):
+    _fields_ = [("n_req", ctypes.c_int32), ("n_rows", ctypes.c_int32),
+                ("rows_max", ctypes.c_int32), ("prefix_len", ctypes.c_int32),
+                ("own_rows", ctypes.c_int32), ("row_start", ctypes.c_void_p),
+                ("own_len", ctypes.c_void_p)]
+
+
+class EvictCfg(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_int32), ("n_keys", ctypes.c_int32),
+                ("src_rows", ctypes.c_int32), ("n_keep", ctypes.c_int32),
+                ("dst_rows", ctypes.c_int32), ("n_first", ctypes.c_int32),
+                ("n_recent", ctypes.c_int32), ("lens", ctypes.c_void_p)]
+
+
 _P = ctypes.c_void_p
 _I = ctypes.c_int32
+_L = ctypes.c_int64
 _SIGS = {
     "akvs_version": (_I, []),
     "akvs_status_string": (ctypes.c_char_p, [_I]),
@@ -120,6 +135,19 @@ _SIGS = {
                               _P, _P, _I, _P, _P, _P, ctypes.c_size_t, _P]),
     "akvs_decode_step_noalloc": (_I, [_P, _I, _P, ctypes.POINTER(LayerW), _P, _P,
                                       ctypes.POINTER(ModelCfg), _P, _P, _I, _P, _P, _P]),
+    "akvs_qk_norm_rope": (_I, [_P, _L, _P, _L, _P, _L, _I, _P, _P, _P, ctypes.POINTER(ModelCfg), _P,
+                               _I, _P, _I, _P, _P, _P, _P]),
+    "akvs_shared_workspace_size": (ctypes.c_size_t, [ctypes.POINTER(ModelCfg),
+                                                     ctypes.POINTER(SharedCfg)]),
+    "akvs_shared_attention": (_I, [_P, ctypes.POINTER(SharedCfg), _P, _P, _P, _P,
+                                   ctypes.POINTER(ModelCfg), _P, _P, _P, ctypes.c_size_t, _P]),
+    "akvs_attention_weights": (_I, [_P, _P, ctypes.POINTER(SharedCfg), _P, _P,
+                                    ctypes.POINTER(ModelCfg), _P, _P, _P, _P, _P, ctypes.c_size_t,
+                                    _P]),
+    "akvs_evict_workspace_size": (ctypes.c_size_t, [ctypes.POINTER(ModelCfg),
+                                                    ctypes.POINTER(EvictCfg)]),
+    "akvs_evict_cache": (_I, [_P, _P, _P, ctypes.POINTER(EvictCfg), ctypes.POINTER(ModelCfg), _P,
+                              _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     "akvs_profile_enable": (_I, [_I]),
     "akvs_profile_read": (_I, [_I, ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_double)]),
     "akvs_mfma_busy_loop": (_I, [_I, _I, _P, _P]),
@@ -157,6 +185,26 @@ def ptr(t: Optional[torch.Tensor]):
     if not t.is_contiguous():
         raise ValueError("tensor arguments must be contiguous")
     return t.data_ptr()
+
+
+def int_ptr(t: Optional[torch.Tensor], least: int):
+    """Pointer of a descriptor's int32 table of at least `least` entries (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.numel() < least:
+        raise ValueError(f"need an int32 tensor of at least {least} entries")
+    return ptr(t)
+
+
+def rows_ptr(t: torch.Tensor):
+    """(pointer, elements between rows) of rows that are dense but may lie apart, as the
+    columns of a packed projection output do."""
+    n, width = t.shape[0], 1
+    for size, step in zip(t.shape[:0:-1], t.stride()[:0:-1]):
+        if size != 1 and step != width:
+            raise ValueError("each row must be contiguous")
+        width *= size
+    return t.data_ptr(), t.stride(0) if n > 1 else width
 
 
 # The current stream's handle without building a torch.cuda.Stream object for it (3.1 us a
@@ -213,6 +261,24 @@ def cache_struct(k, v, k_meta=None, v_meta=None, dtype: Optional[int] = None) ->
         dtype = dtype_code(k)
     c = Cache(ptr(k), ptr(v), ptr(k_meta), ptr(v_meta), dtype)
     c._keep = (k, v, k_meta, v_meta)
+    return c
+
+
+def shared_cfg(n_req, n_rows, rows_max, prefix_len, own_rows=0, row_start=None,
+               own_len=None) -> SharedCfg:
+    """A batch over a shared prefix; it holds references to its device tensors."""
+    c = SharedCfg(int(n_req), int(n_rows), int(rows_max), int(prefix_len), int(own_rows),
+                  int_ptr(row_start, n_req + 1), int_ptr(own_len, n_req))
+    c._keep = (row_start, own_len)
+    return c
+
+
+def evict_cfg(n_seq, n_keys, n_keep, n_first=0, n_recent=0, src_rows=0, dst_rows=0,
+              lens=None) -> EvictCfg:
+    """What an eviction keeps; it holds a reference to lens (device int32 [n_seq])."""
+    c = EvictCfg(int(n_seq), int(n_keys), int(src_rows), int(n_keep), int(dst_rows), int(n_first),
+                 int(n_recent), int_ptr(lens, n_seq))
+    c._keep = lens
     return c
 
 
@@ -398,6 +464,52 @@ def akvs_decode_step_noalloc(token, n_past, embed, layers: ctypes.Array, final_n
                                            ptr(k_cache), ptr(v_cache), int(cache_rows),
                                            ptr(logits), ptr(next_token), stream_handle(stream)),
            "akvs_decode_step_noalloc")
+
+
+def akvs_qk_norm_rope(q, k, v, n_rows, positions, q_norm, k_norm, m: ModelCfg, rope, rope_rows,
+                      kv_rows, n_kv_rows, q_out, k_out, v_out, stream=None):
+    """q, k, v: rows that may lie apart (views of a packed projection output)."""
+    (pq, ldq), (pk, ldk), (pv, ldv) = rows_ptr(q), rows_ptr(k), (
+        rows_ptr(v) if v is not None else (None, 0))
+    _check(load().akvs_qk_norm_rope(pq, ldq, pk, ldk, pv, ldv, n_rows, ptr(positions), ptr(q_norm),
+                                    ptr(k_norm), ctypes.byref(m), ptr(rope), rope_rows,
+                                    ptr(kv_rows), n_kv_rows, ptr(q_out), ptr(k_out), ptr(v_out),
+                                    stream_handle(stream)), "akvs_qk_norm_rope")
+
+
+def akvs_shared_workspace_size(m: ModelCfg, cfg: SharedCfg) -> int:
+    return load().akvs_shared_workspace_size(ctypes.byref(m), ctypes.byref(cfg))
+
+
+def akvs_shared_attention(q, cfg: SharedCfg, k_prefix, v_prefix, k_own, v_own, m: ModelCfg, out,
+                          lse=None, ws=None, stream=None):
+    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check(load().akvs_shared_attention(ptr(q), ctypes.byref(cfg), ptr(k_prefix), ptr(v_prefix),
+                                        ptr(k_own), ptr(v_own), ctypes.byref(m), ptr(out),
+                                        ptr(lse), ptr(ws), nbytes, stream_handle(stream)),
+           "akvs_shared_attention")
+
+
+def akvs_attention_weights(q, lse, cfg: SharedCfg, k_prefix, k_own, m: ModelCfg, w_prefix_prev,
+                           w_prefix, w_own_prev, w_own, ws=None, stream=None):
+    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check(load().akvs_attention_weights(ptr(q), ptr(lse), ctypes.byref(cfg), ptr(k_prefix),
+                                         ptr(k_own), ctypes.byref(m), ptr(w_prefix_prev),
+                                         ptr(w_prefix), ptr(w_own_prev), ptr(w_own), ptr(ws),
+                                         nbytes, stream_handle(stream)), "akvs_attention_weights")
+
+
+def akvs_evict_workspace_size(m: ModelCfg, cfg: EvictCfg) -> int:
+    return load().akvs_evict_workspace_size(ctypes.byref(m), ctypes.byref(cfg))
+
+
+def akvs_evict_cache(k, v, weights, cfg: EvictCfg, m: ModelCfg, keep, k_out, v_out, weights_out,
+                     lens_out, ws=None, stream=None):
+    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check(load().akvs_evict_cache(ptr(k), ptr(v), ptr(weights), ctypes.byref(cfg),
+                                   ctypes.byref(m), ptr(keep), ptr(k_out), ptr(v_out),
+                                   ptr(weights_out), ptr(lens_out), ptr(ws), nbytes,
+                                   stream_handle(stream)), "akvs_evict_cache")
 
 
 def akvs_profile_enable(class_mask: int):

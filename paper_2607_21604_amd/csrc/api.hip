@@ -1645,3 +1645,186 @@ akvs_status akvs_decode_step_noalloc(const int32_t *token, int32_t n_past, const
 }
 
 }  // extern "C"
+
+// ---- a batch over one shared context -------------------------------------------------------
+
+static akvs_status check_shared(const akvs_model_cfg *m, const akvs_shared_cfg *c,
+                                SharedBatch *s) {
+  akvs_status st = check_model(m);
+  if (st) return st;
+  REQUIRE(c, AKVS_EINVAL, "shared cfg is NULL");
+  REQUIRE(c->n_req >= 1 && c->n_req <= (1 << 20), AKVS_EINVAL, "n_req %d outside [1, 2^20]",
+          c->n_req);
+  REQUIRE(c->n_rows >= 0 && c->rows_max >= 1 && c->prefix_len >= 0 && c->own_rows >= 0,
+          AKVS_EINVAL, "need n_rows, prefix_len, own_rows >= 0 and rows_max >= 1");
+  REQUIRE(c->n_rows < (1 << 24) && c->prefix_len < (1 << 28) &&
+              (long long)c->n_req * c->own_rows < (1LL << 31) && c->own_rows < (1 << 28) &&
+              (long long)c->n_rows * m->n_q_heads < (1LL << 30),
+          AKVS_ESHAPE, "batch too large");
+  REQUIRE(c->row_start || (long long)c->n_req * c->rows_max == c->n_rows, AKVS_ESHAPE,
+          "without row_start every request has rows_max rows: n_rows %d is not %d * %d", c->n_rows,
+          c->n_req, c->rows_max);
+  REQUIRE(c->own_len || c->own_rows == 0, AKVS_EINVAL, "own_rows %d needs own_len", c->own_rows);
+  *s = {c->n_req,    c->n_rows,    c->rows_max, c->prefix_len,
+        c->own_rows, c->row_start, c->own_len};
+  return AKVS_OK;
+}
+
+extern "C" {
+
+akvs_status akvs_qk_norm_rope(const void *q, int64_t ldq, const void *k, int64_t ldk,
+                              const void *v, int64_t ldv, int32_t n_rows,
+                              const int32_t *positions, const void *q_norm, const void *k_norm,
+                              const akvs_model_cfg *m, const float *rope, int32_t rope_rows,
+                              const int32_t *kv_rows, int32_t n_kv_rows, void *q_out,
+                              void *k_out, void *v_out, hipStream_t stream) {
+  akvs_status st = check_model(m);
+  if (st) return st;
+  const long long hqw = m->n_q_heads * m->head_dim, kvw = m->n_kv_heads * m->head_dim;
+  const long long es = (long long)es_of(m->dtype);
+  REQUIRE(n_rows >= 0 && n_kv_rows >= 0 && rope_rows >= 1, AKVS_EINVAL,
+          "need n_rows, n_kv_rows >= 0 and rope_rows >= 1");
+  REQUIRE((long long)n_rows * (hqw + 2 * kvw) < (1LL << 40), AKVS_ESHAPE, "too large");
+  REQUIRE(kv_rows || n_kv_rows >= n_rows, AKVS_EINVAL,
+          "n_kv_rows %d < n_rows %d without kv_rows", n_kv_rows, n_rows);
+  REQUIRE(q && k && positions && rope && q_out && k_out, AKVS_EINVAL, "NULL argument");
+  REQUIRE((v == nullptr) == (v_out == nullptr), AKVS_EINVAL, "v and v_out go together");
+  REQUIRE(aligned16(q) && aligned16(k) && aligned16(v) && aligned16(q_norm) &&
+              aligned16(k_norm) && aligned16(rope) && aligned16(q_out) && aligned16(k_out) &&
+              aligned16(v_out),
+          AKVS_EINVAL, "misaligned argument");
+  REQUIRE(ldq >= hqw && ldk >= kvw && (!v || ldv >= kvw), AKVS_EINVAL,
+          "row strides shorter than a row");
+  REQUIRE(ldq < (1LL << 31) && ldk < (1LL << 31) && ldv < (1LL << 31), AKVS_ESHAPE,
+          "row strides too large");
+  REQUIRE(ldq * es % 16 == 0 && ldk * es % 16 == 0 && (!v || ldv * es % 16 == 0), AKVS_EINVAL,
+          "row strides must be multiples of 16 bytes");
+  const QkNorm a{q,           k,      v,      ldq,          ldk,
+                 ldv,         n_rows, m->n_q_heads, m->n_kv_heads, m->head_dim,
+                 positions,   q_norm, k_norm, m->rms_eps,   rope,
+                 rope_rows,   kv_rows, n_kv_rows, q_out,    k_out,
+                 v_out};
+  LAUNCH(AKVS_K_NORM, launch_qk_norm_rope(a, m->dtype, stream));
+  return AKVS_OK;
+}
+
+size_t akvs_shared_workspace_size(const akvs_model_cfg *m, const akvs_shared_cfg *c) {
+  SharedBatch s;
+  if (check_shared(m, c, &s) != AKVS_OK) return 0;
+  return 0;
+}
+
+akvs_status akvs_shared_attention(const void *q, const akvs_shared_cfg *c, const void *k_prefix,
+                                  const void *v_prefix, const void *k_own, const void *v_own,
+                                  const akvs_model_cfg *m, void *out, float *lse, void *ws,
+                                  size_t ws_bytes, hipStream_t stream) {
+  SharedBatch s;
+  akvs_status st = check_shared(m, c, &s);
+  if (st) return st;
+  REQUIRE((q && out) || s.n_rows == 0, AKVS_EINVAL, "NULL argument");
+  REQUIRE((k_prefix && v_prefix) || s.prefix_len == 0, AKVS_EINVAL, "prefix keys or values NULL");
+  REQUIRE((k_own && v_own) || s.own_rows == 0, AKVS_EINVAL, "own keys or values NULL");
+  REQUIRE(aligned16(q) && aligned16(k_prefix) && aligned16(v_prefix) && aligned16(k_own) &&
+              aligned16(v_own) && aligned16(out) && aligned16(lse) && aligned16(ws),
+          AKVS_EINVAL, "misaligned argument");
+  LAUNCH(AKVS_K_ATTENTION,
+         launch_shared_attention(s, q, k_prefix, v_prefix, k_own, v_own, m->n_q_heads,
+                                 m->n_kv_heads, m->head_dim, m->dtype, out, lse, stream));
+  return AKVS_OK;
+}
+
+akvs_status akvs_attention_weights(const void *q, const float *lse, const akvs_shared_cfg *c,
+                                   const void *k_prefix, const void *k_own,
+                                   const akvs_model_cfg *m, const float *w_prefix_prev,
+                                   float *w_prefix, const float *w_own_prev, float *w_own,
+                                   void *ws, size_t ws_bytes, hipStream_t stream) {
+  SharedBatch s;
+  akvs_status st = check_shared(m, c, &s);
+  if (st) return st;
+  REQUIRE((q && lse) || s.n_rows == 0, AKVS_EINVAL, "NULL argument");
+  REQUIRE(w_prefix || w_own, AKVS_EINVAL, "neither w_prefix nor w_own is given");
+  REQUIRE(k_prefix || s.prefix_len == 0 || !w_prefix, AKVS_EINVAL, "k_prefix is NULL");
+  REQUIRE(k_own || s.own_rows == 0 || !w_own, AKVS_EINVAL, "k_own is NULL");
+  REQUIRE(aligned16(q) && aligned16(lse) && aligned16(k_prefix) && aligned16(k_own) &&
+              aligned16(w_prefix_prev) && aligned16(w_prefix) && aligned16(w_own_prev) &&
+              aligned16(w_own) && aligned16(ws),
+          AKVS_EINVAL, "misaligned argument");
+  LAUNCH(AKVS_K_ATTENTION,
+         launch_attention_weights(s, q, lse, k_prefix, k_own, m->n_q_heads, m->n_kv_heads,
+                                  m->head_dim, m->dtype, w_prefix_prev, w_prefix, w_own_prev,
+                                  w_own, stream));
+  return AKVS_OK;
+}
+
+}  // extern "C"
+
+static akvs_status check_evict(const akvs_model_cfg *m, const akvs_evict_cfg *c, EvictArgs *a) {
+  akvs_status st = check_model(m);
+  if (st) return st;
+  REQUIRE(c, AKVS_EINVAL, "evict cfg is NULL");
+  REQUIRE(c->n_seq >= 1 && c->n_keys >= 0 && c->n_keep >= 1 && c->n_first >= 0 && c->n_recent >= 0,
+          AKVS_EINVAL, "need n_seq, n_keep >= 1 and n_keys, n_first, n_recent >= 0");
+  REQUIRE((long long)c->n_first + c->n_recent <= c->n_keep, AKVS_EINVAL,
+          "n_first + n_recent above n_keep %d", c->n_keep);
+  REQUIRE(c->src_rows == 0 || c->src_rows >= c->n_keys, AKVS_ESHAPE, "src_rows %d < n_keys %d",
+          c->src_rows, c->n_keys);
+  REQUIRE(c->dst_rows == 0 || c->dst_rows >= c->n_keep, AKVS_ESHAPE, "dst_rows %d < n_keep %d",
+          c->dst_rows, c->n_keep);
+  *a = {c->n_seq,   c->n_keys,  c->src_rows ? c->src_rows : c->n_keys,
+        c->n_keep,  c->dst_rows ? c->dst_rows : c->n_keep,
+        c->n_first, c->n_recent, c->lens};
+  REQUIRE(a->n_seq <= (1 << 16) && a->src_rows < (1 << 28) && a->dst_rows < (1 << 28) &&
+              (long long)a->n_seq * a->n_keep * m->n_kv_heads < (1LL << 31),
+          AKVS_ESHAPE, "too large");
+  return AKVS_OK;
+}
+
+static bool overlap(const void *a, size_t na, const void *b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
+
+extern "C" {
+
+size_t akvs_evict_workspace_size(const akvs_model_cfg *m, const akvs_evict_cfg *c) {
+  EvictArgs a;
+  if (check_evict(m, c, &a) != AKVS_OK) return 0;
+  return align256((size_t)a.n_seq * m->n_kv_heads * a.n_keep * sizeof(int32_t));
+}
+
+akvs_status akvs_evict_cache(const void *k, const void *v, const float *weights,
+                             const akvs_evict_cfg *c, const akvs_model_cfg *m, int32_t *keep,
+                             void *k_out, void *v_out, float *weights_out, int32_t *lens_out,
+                             void *ws, size_t ws_bytes, hipStream_t stream) {
+  EvictArgs a;
+  akvs_status st = check_evict(m, c, &a);
+  if (st) return st;
+  REQUIRE(weights || a.n_keys == 0, AKVS_EINVAL, "weights are NULL");
+  REQUIRE((k && v && k_out && v_out) || (!k && !v && !k_out && !v_out), AKVS_EINVAL,
+          "k, v, k_out and v_out go together");
+  REQUIRE(aligned16(k) && aligned16(v) && aligned16(weights) && aligned16(keep) &&
+              aligned16(k_out) && aligned16(v_out) && aligned16(weights_out) && aligned16(ws),
+          AKVS_EINVAL, "misaligned argument");
+  const size_t row = (size_t)m->n_kv_heads * m->head_dim * es_of(m->dtype);
+  const size_t from = a.n_seq * (size_t)a.src_rows * row, to = a.n_seq * (size_t)a.dst_rows * row;
+  REQUIRE(!k || (!overlap(k, from, k_out, to) && !overlap(k, from, v_out, to) &&
+                 !overlap(v, from, k_out, to) && !overlap(v, from, v_out, to) &&
+                 !overlap(k_out, to, v_out, to)),
+          AKVS_EINVAL, "k_out / v_out overlap k, v or each other");
+  REQUIRE(!weights_out ||
+              !overlap(weights, (size_t)a.n_seq * m->n_kv_heads * a.n_keys * 4, weights_out,
+                       (size_t)a.n_seq * m->n_kv_heads * a.dst_rows * 4),
+          AKVS_EINVAL, "weights_out overlaps weights");
+  const size_t need = akvs_evict_workspace_size(m, c);
+  REQUIRE(keep || (ws && ws_bytes >= need), AKVS_ENOSPACE, "workspace %zu < %zu bytes", ws_bytes,
+          need);
+  if (!keep) keep = reinterpret_cast<int32_t *>(ws);
+  LAUNCH(AKVS_K_SELECT,
+         launch_evict_select(weights, a, m->n_kv_heads, keep, weights_out, stream));
+  LAUNCH(AKVS_K_OTHER, launch_evict_gather(k, v, a, m->n_kv_heads,
+                                           (int)(m->head_dim * es_of(m->dtype)), keep, k_out,
+                                           v_out, lens_out, stream));
+  return AKVS_OK;
+}
+
+}  // extern "C"

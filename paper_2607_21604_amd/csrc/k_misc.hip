@@ -1,4 +1,5 @@
-// Small bandwidth kernels: rotary table, embedding gather, RMSNorm, row gather.
+// Small bandwidth kernels: rotary table, embedding gather, RMSNorm, row gather, norms and
+// rotation of query and key heads.
 #include "kernels.h"
 
 namespace akvs {
@@ -310,6 +311,88 @@ __global__ __launch_bounds__(256) void k_mfma_busy_loop(float *out, int iters) {
 hipError_t launch_mfma_busy_loop(int n_blocks, int iters, float *out, hipStream_t s) {
   if (n_blocks <= 0) return hipSuccess;
   hipLaunchKernelGGL(k_mfma_busy_loop, dim3(n_blocks), dim3(256), 0, s, out, iters);
+  return hipGetLastError();
+}
+
+// Norms and rotation of query and key heads. A head is one task of hd / 16 neighbouring lanes,
+// each with 8 elements of its lower half and their rotary partners of the upper half, so the
+// pair turns in a lane and only the sum of squares crosses lanes. A value head is a copy.
+template <typename TS, int LPH>
+__global__ __launch_bounds__(256) void k_qk_norm_rope(QkNorm a) {
+  constexpr int half = LPH * 8, hd = 2 * half;
+  const int heads = a.hq + a.hkv * (a.v ? 2 : 1);
+  const long long gid = (long long)blockIdx.x * 256 + threadIdx.x;
+  const long long task = gid / LPH;
+  const int e0 = (int)(gid % LPH) * 8;
+  const long long r = task / heads;
+  if (r >= a.n_rows) return;  // (whole groups of LPH lanes)
+  int h = (int)(task - r * heads);
+  const TS *src;
+  TS *dst;
+  const TS *gain = nullptr;
+  bool turn = true, write = true;
+  if (h < a.hq) {
+    src = reinterpret_cast<const TS *>(a.q) + r * a.ldq + h * hd;
+    dst = reinterpret_cast<TS *>(a.q_out) + (r * a.hq + h) * hd;
+    gain = reinterpret_cast<const TS *>(a.q_gain);
+  } else {
+    h -= a.hq;
+    const int to = a.kv_rows ? a.kv_rows[r] : (int)r;
+    write = to >= 0 && to < a.n_kv_rows;
+    turn = h < a.hkv;
+    if (!turn) h -= a.hkv;
+    src = reinterpret_cast<const TS *>(turn ? a.k : a.v) + r * (turn ? a.ldk : a.ldv) + h * hd;
+    dst = reinterpret_cast<TS *>(turn ? a.k_out : a.v_out) + ((size_t)max(to, 0) * a.hkv + h) * hd;
+    if (turn) gain = reinterpret_cast<const TS *>(a.k_gain);
+  }
+  float lo[8], hi[8];
+  load8(src + e0, lo);
+  load8(src + e0 + half, hi);
+  if (turn) {
+    const int p = min(max(a.pos[r], 0), a.rope_rows - 1);
+    float cs[16];
+    const float *rope = a.rope + ((size_t)p * half + e0) * 2;
+    load8(rope, *reinterpret_cast<float(*)[8]>(cs));
+    load8(rope + 8, *reinterpret_cast<float(*)[8]>(cs + 8));
+    if (gain) {
+      float gl[8], gh[8], ss = 0.f;
+      load8(gain + e0, gl);
+      load8(gain + e0 + half, gh);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss = fmaf(lo[i], lo[i], fmaf(hi[i], hi[i], ss));
+#pragma unroll
+      for (int o = 1; o < LPH; o <<= 1) ss += __shfl_xor(ss, o, 64);
+      const float rs = 1.0f / sqrtf(ss * (1.0f / hd) + a.eps);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        lo[i] *= rs * gl[i];
+        hi[i] *= rs * gh[i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float x = lo[i], y = hi[i], c = cs[2 * i], s = cs[2 * i + 1];
+      lo[i] = x * c - y * s;
+      hi[i] = y * c + x * s;
+    }
+  }
+  if (!write) return;
+  store8(dst + e0, lo);
+  store8(dst + e0 + half, hi);
+}
+
+hipError_t launch_qk_norm_rope(const QkNorm &a, int dtype, hipStream_t s) {
+  const int heads = a.hq + a.hkv * (a.v ? 2 : 1), lph = a.hd / 16;
+  const long long threads = (long long)a.n_rows * heads * lph;
+  if (threads == 0) return hipSuccess;
+  const dim3 g((unsigned)((threads + 255) / 256)), b(256);
+  if (dtype == AKVS_BF16) {
+    if (lph == 8) hipLaunchKernelGGL((k_qk_norm_rope<bf16_t, 8>), g, b, 0, s, a);
+    else hipLaunchKernelGGL((k_qk_norm_rope<bf16_t, 4>), g, b, 0, s, a);
+  } else {
+    if (lph == 8) hipLaunchKernelGGL((k_qk_norm_rope<float, 8>), g, b, 0, s, a);
+    else hipLaunchKernelGGL((k_qk_norm_rope<float, 4>), g, b, 0, s, a);
+  }
   return hipGetLastError();
 }
 

@@ -54,6 +54,23 @@ hipError_t launch_copy_ints_at(const int32_t *src, int cap, const int32_t *n_dev
                                const int32_t *dst_base, hipStream_t s);
 // dst[0] = src[0] on the device.
 hipError_t launch_copy_int(const int32_t *src, int32_t *dst, hipStream_t s);
+// Per-head RMS norms (a null gain: none) and rotation of queries and keys, values copied; key
+// and value rows go to row kv_rows[r] (nullptr: r) of k_out / v_out where that is one of
+// n_kv_rows.
+struct QkNorm {
+  const void *q, *k, *v;
+  long long ldq, ldk, ldv;  // elements between rows
+  int n_rows, hq, hkv, hd;
+  const int32_t *pos;
+  const void *q_gain, *k_gain;
+  float eps;
+  const float *rope;
+  int rope_rows;
+  const int32_t *kv_rows;
+  int n_kv_rows;
+  void *q_out, *k_out, *v_out;
+};
+hipError_t launch_qk_norm_rope(const QkNorm &a, int dtype, hipStream_t s);
 // ---- k_reuse.hip --------------------------------------------------------------------
 hipError_t launch_divergence(const void *k_fresh, const void *v_fresh, int fresh_dtype,
                              CacheLayer cache, int n_tokens, int hkv, int hd,
@@ -185,6 +202,31 @@ int attn_splits(int rows, int hq, int hkv, int n_keys);
 int attn_part_splits(int rows, int hq, int hkv, int hd, int n_keys, bool lean = false);
 int attn_split_keys(int n_keys, int n_splits);
 
+// ---- k_shared.hip ---------------------------------------------------------------------
+// A batch over one shared context (akvs_shared_cfg).
+struct SharedBatch {
+  int n_req, n_rows, rows_max, prefix_len, own_rows;
+  const int32_t *row_start, *own_len;
+};
+hipError_t launch_shared_attention(const SharedBatch &s, const void *q, const void *kp,
+                                   const void *vp, const void *ko, const void *vo, int hq,
+                                   int hkv, int hd, int dtype, void *out, float *lse,
+                                   hipStream_t st);
+hipError_t launch_attention_weights(const SharedBatch &s, const void *q, const float *lse,
+                                    const void *kp, const void *ko, int hq, int hkv, int hd,
+                                    int dtype, const float *wp_prev, float *wp,
+                                    const float *wo_prev, float *wo, hipStream_t st);
+// ---- k_evict.hip ----------------------------------------------------------------------
+struct EvictArgs {
+  int n_seq, n_keys, src_rows, n_keep, dst_rows, n_first, n_recent;
+  const int32_t *lens;
+};
+hipError_t launch_evict_select(const float *weights, const EvictArgs &a, int hkv, int32_t *keep,
+                               float *w_out, hipStream_t s);
+// Kept rows of k and v (k null: none) and, with lens_out, the kept lengths.
+hipError_t launch_evict_gather(const void *k, const void *v, const EvictArgs &a, int hkv,
+                               int row_bytes, const int32_t *keep, void *k_out, void *v_out,
+                               int32_t *lens_out, hipStream_t s);
 // ---- k_decode.hip -------------------------------------------------------------------
 // Matrix-vector products of one token, y = W x (W [N][K], K a multiple of 8), item i of
 // a launch = one pair of rows, with these epilogues:

@@ -1,0 +1,620 @@
+"""Operators over one shared context against their definitions in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_21604_amd import akvs
+from tests import shared_ref as ref
+from tests.gpu_util import DEV
+from tests.libutil import ensure_built
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    return ensure_built()
+
+
+def model(hq, hkv, hd, dt):
+    return akvs.ModelCfg(1, 256, hq, hkv, hd, 256, 64, 1e4, 1e-6,
+                         akvs.AKVS_F32 if dt == F32 else akvs.AKVS_BF16)
+
+
+def randn(seed, *shape, dt=F32, std=1.0):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return (torch.randn(shape, generator=g) * std).to(dt).to(DEV)
+
+
+def ints(x):
+    return torch.tensor(np.asarray(x), dtype=torch.int32, device=DEV)
+
+
+def starts(rows):
+    return [0] + list(np.cumsum(rows))
+
+
+class Batch:
+    """A batch's tensors on the GPU; own keys past each length hold NaN."""
+
+    def __init__(self, hq, hkv, hd, dt, prefix, rows, own_len, own_rows=None, seed=0, spare=0,
+                 q_std=2.0):
+        self.hq, self.hkv, self.hd, self.dt = hq, hkv, hd, dt
+        self.m = model(hq, hkv, hd, dt)
+        self.rows, self.own_len, self.B = list(rows), list(own_len), len(rows)
+        self.start = starts(rows)
+        self.n = self.start[-1]
+        self.P, self.cap = prefix, max(own_len) if own_rows is None else own_rows
+        self.q = randn(seed + 1, self.n + spare, hq, hd, dt=dt, std=q_std)
+        self.kp, self.vp = (randn(seed + i, prefix, hkv, hd, dt=dt) for i in (2, 3))
+        self.ko, self.vo = (randn(seed + i, self.B, self.cap, hkv, hd, dt=dt) for i in (4, 5))
+        for b, n in enumerate(own_len):
+            self.ko[b, n:] = math.nan
+            self.vo[b, n:] = math.nan
+        self.out = torch.full((self.n + spare, hq, hd), 7.0, dtype=dt, device=DEV)
+        self.lse = torch.full((self.n + spare, hq), 7.0, dtype=F32, device=DEV)
+
+    def cfg(self, uniform=False):
+        return akvs.shared_cfg(self.B, self.q.shape[0], max(1, max(self.rows)), self.P, self.cap,
+                               None if uniform else ints(self.start), ints(self.own_len))
+
+    def ws(self, cfg):
+        n = akvs.akvs_shared_workspace_size(self.m, cfg)
+        return torch.full((n,), 255, dtype=torch.uint8, device=DEV) if n else None
+
+    def attend(self, uniform=False, **kw):
+        c = self.cfg(uniform)
+        akvs.akvs_shared_attention(self.q, c, self.kp, self.vp, self.ko, self.vo, self.m, self.out,
+                                   self.lse, self.ws(c), **kw)
+        return self.out, self.lse
+
+    def expect(self):
+        return ref.attention(self.q[:self.n], self.kp, self.vp, self.ko, self.vo, self.start,
+                             self.own_len)
+
+    def check(self):
+        out, lse, mass, reach = self.expect()
+        got, gl = self.out[:self.n].double().cpu(), self.lse[:self.n].double().cpu()
+        keys = self.P + self.cap
+        none = torch.isinf(lse)
+        assert torch.equal(torch.isinf(gl), none)
+        tol = ref.lse_bound(lse, reach, self.hd, keys)
+        assert bool(((gl - lse).abs() <= tol)[~none].all()), float(((gl - lse).abs() - tol)[~none].max())
+        tol = ref.out_bound(out, mass, reach, self.hd, keys, self.dt)
+        err = (got - out).abs()
+        assert bool((err <= tol).all()), float((err - tol).max())
+        assert bool((self.out[self.n:] == 7).all()) and bool((self.lse[self.n:] == 7).all())
+
+
+GEOMS = [(24, 8, 128, BF), (28, 4, 128, BF), (40, 8, 128, BF), (6, 2, 64, BF), (3, 3, 64, BF),
+         (40, 1, 64, BF), (17, 1, 128, BF), (4, 4, 64, F32), (28, 4, 128, F32), (18, 1, 64, F32)]
+
+
+@pytest.mark.parametrize("hq,hkv,hd,dt", GEOMS)
+@pytest.mark.parametrize("prefix", [0, 1, 33, 64, 257])
+def test_decode_batch(hq, hkv, hd, dt, prefix):
+    """One row per request, own caches from one key to past a tile's end."""
+    b = Batch(hq, hkv, hd, dt, prefix, [1] * 5, [1, 2, 31, 64, 70], seed=prefix)
+    b.attend(uniform=True)
+    b.check()
+
+
+@pytest.mark.parametrize("hq,hkv,hd,dt", GEOMS)
+def test_ragged_rows(hq, hkv, hd, dt):
+    """Requests without rows, with more rows than own keys (the first see none of them), of one
+    row, and rows behind the last request that stay as they were."""
+    b = Batch(hq, hkv, hd, dt, 70, [3, 0, 5, 1, 17], [3, 40, 2, 0, 50], seed=11, spare=3)
+    b.attend()
+    b.check()
+
+
+@pytest.mark.parametrize("hq,hkv,hd,dt", [(24, 8, 128, BF), (6, 2, 64, BF), (4, 2, 128, F32)])
+def test_rows_that_see_no_key(hq, hkv, hd, dt):
+    """No prefix and no own keys: out 0, lse -inf; the other rows as ever."""
+    b = Batch(hq, hkv, hd, dt, 0, [2, 3, 1], [0, 1, 9], own_rows=12, seed=21)
+    b.attend()
+    b.check()
+    assert bool((b.out[:4] == 0).all()) and bool((b.lse[:4] == -math.inf).all())
+
+
+@pytest.mark.parametrize("hq,hkv,hd,dt", [(24, 8, 128, BF), (6, 2, 64, BF), (4, 2, 128, F32)])
+def test_prefix_alone(hq, hkv, hd, dt):
+    """No own caches at all."""
+    b = Batch(hq, hkv, hd, dt, 130, [4], [0], seed=25)
+    c = akvs.shared_cfg(1, 4, 4, 130)
+    akvs.akvs_shared_attention(b.q, c, b.kp, b.vp, None, None, b.m, b.out, b.lse, b.ws(c))
+    b.check()
+
+
+@pytest.mark.parametrize("hq,hkv,hd,dt,prefix,rows", [
+    (28, 4, 128, BF, 2500, [1] * 16), (40, 8, 128, BF, 1100, [1] * 3),
+    (24, 8, 128, BF, 900, [9, 40, 64]), (6, 2, 64, BF, 3000, [1, 7]),
+    (28, 4, 128, F32, 1500, [1, 5]), (24, 8, 128, BF, 5000, [1])])
+def test_long_prefix(hq, hkv, hd, dt, prefix, rows):
+    """Key ranges that are split, over few and many rows."""
+    b = Batch(hq, hkv, hd, dt, prefix, rows, [r + 5 * i for i, r in enumerate(rows)], seed=31)
+    b.attend()
+    b.check()
+
+
+@pytest.mark.parametrize("hq,hkv,hd,dt", [(24, 8, 128, BF), (6, 2, 64, BF), (4, 2, 128, F32)])
+def test_long_own_caches(hq, hkv, hd, dt):
+    """Own caches much longer than the prefix, one of them almost empty."""
+    b = Batch(hq, hkv, hd, dt, 10, [1, 2, 1, 4], [900, 1, 2000, 1203], own_rows=2100, seed=41)
+    b.attend()
+    b.check()
+
+
+@pytest.mark.parametrize("hq,hkv,hd,dt", [(24, 8, 128, BF), (6, 2, 64, BF), (4, 2, 128, F32)])
+def test_large_scores(hq, hkv, hd, dt):
+    """Scores of several hundred: the running maximum rises by large steps, most probabilities
+    underflow."""
+    b = Batch(hq, hkv, hd, dt, 300, [1, 3], [40, 3], seed=51, q_std=60.0)
+    b.attend()
+    b.check()
+
+
+@pytest.mark.parametrize("hq,hkv,hd,dt", [(24, 8, 128, BF), (6, 2, 64, BF), (4, 2, 128, F32)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_hidden_values_that_are_not_finite(hq, hkv, hd, dt, bad):
+    """A key and a value that the last row of a request alone sees are not finite: the rows
+    before it are as if they were not there, the last one is not finite, other requests'
+    rows are untouched. (Keys of +-inf: the scores are infinite or NaN.)"""
+    def batch():
+        return Batch(hq, hkv, hd, dt, 40, [4, 2, 1], [20, 30, 5], seed=61)
+    b = batch()
+    b.attend()
+    b.check()
+    clean = b.out.clone(), b.lse.clone()
+    c = batch()
+    c.vo[0, 19, :, 5] = bad
+    c.attend()
+    assert torch.equal(c.out[:3], clean[0][:3]) and torch.equal(c.out[4:], clean[0][4:])
+    assert torch.equal(c.lse, clean[1])
+    assert not bool(torch.isfinite(c.out[3, :, 5].float()).any())
+    assert torch.equal(c.out[3, :, 6:], clean[0][3, :, 6:])
+    c = batch()
+    c.ko[0, 19] = bad
+    c.attend()
+    assert torch.equal(c.out[:3], clean[0][:3]) and torch.equal(c.out[4:], clean[0][4:])
+    assert torch.equal(c.lse[:3], clean[1][:3])
+    assert bool(torch.isnan(c.out[3].float()).all())
+
+
+@pytest.mark.parametrize("hq,hkv,hd,dt", [(24, 8, 128, BF), (4, 2, 128, F32)])
+def test_nan_rows_stay_their_own(hq, hkv, hd, dt):
+    """A row whose query is NaN, next to rows that are not."""
+    b = Batch(hq, hkv, hd, dt, 200, [1, 3, 1], [4, 9, 70], seed=71)
+    b.attend()
+    clean = b.out.clone(), b.lse.clone()
+    b.q[2] = math.nan
+    b.attend()
+    keep = [0, 1, 3, 4]
+    assert torch.equal(b.out[keep], clean[0][keep]) and torch.equal(b.lse[keep], clean[1][keep])
+    assert bool(torch.isnan(b.out[2].float()).all()) and bool(torch.isnan(b.lse[2]).all())
+
+
+def test_values_on_the_device_out_of_range():
+    """Lengths outside their buffers leave other requests' rows what they are; row starts outside
+    theirs (where two requests claim row 0, so that no row's result is defined) write nothing
+    behind the buffers."""
+    b = Batch(24, 8, 128, BF, 50, [1, 1, 1, 1], [5, 6, 7, 8], seed=81)
+    b.attend(uniform=True)
+    clean = b.out.clone()
+    guard = torch.full((b.n + 8, 24, 128), 3.0, dtype=BF, device=DEV)
+    b.out = guard[:b.n]
+    c = akvs.shared_cfg(4, 4, 1, 50, 8, None, ints([5, 600, -7, 8]))
+    akvs.akvs_shared_attention(b.q, c, b.kp, b.vp, b.ko, b.vo, b.m, b.out, b.lse, b.ws(c))
+    assert torch.equal(b.out[[0, 3]], clean[[0, 3]])
+    c = akvs.shared_cfg(4, 4, 2, 50, 8, ints([0, 1, -5, 1 << 30, 1 << 30]), ints([5, 6, 7, 8]))
+    akvs.akvs_shared_attention(b.q, c, b.kp, b.vp, b.ko, b.vo, b.m, b.out, b.lse, b.ws(c))
+    assert bool((guard[b.n:] == 3).all())
+
+
+def test_long_cache_offsets_past_32_bits():
+    """A prefix of 2.2 million keys (4.5 GB of keys, as many of values): the last ones count."""
+    P, hkv, hd = 2_200_003, 8, 128
+    k = torch.zeros((P, hkv, hd), dtype=BF, device=DEV)
+    v = torch.zeros_like(k)
+    q = torch.zeros((1, 16, hd), dtype=BF, device=DEV)
+    q[..., 0] = 64.0
+    k[P - 1, :, 0] = 16.0  # score 64 * 16 / sqrt(128) = 90 above all others
+    v[P - 1] = randn(91, hkv, hd, dt=BF)
+    m = model(16, hkv, hd, BF)
+    c = akvs.shared_cfg(1, 1, 1, P)
+    n = akvs.akvs_shared_workspace_size(m, c)
+    ws = torch.empty(max(n, 256), dtype=torch.uint8, device=DEV)
+    out = torch.empty_like(q)
+    lse = torch.empty((1, 16), device=DEV)
+    akvs.akvs_shared_attention(q, c, k, v, None, None, m, out, lse, ws)
+    assert torch.equal(out[0].view(8, 2, hd), v[P - 1][:, None].expand(8, 2, hd))
+    w = torch.empty((hkv, P), device=DEV)
+    akvs.akvs_attention_weights(q, lse, c, k, None, m, None, w, None, None, ws)
+    assert bool(((w[:, P - 1] - 2).abs() < 1e-4).all()) and float(w[:, :P - 1].max()) < 1e-30
+
+
+def test_deterministic_streams_and_graphs():
+    """The same bits twice, on another stream, and from a graph replayed between eager work,
+    also after its inputs changed in place."""
+    b = Batch(28, 4, 128, BF, 1000, [1] * 6, [9, 1, 40, 8, 100, 128], seed=95)
+    c = b.cfg(True)
+    ws = b.ws(c)
+    w, wo = (torch.zeros(s, device=DEV) for s in ((4, 1000), (6, 4, 128)))
+
+    def run(out, lse, w, wo, stream=None):
+        akvs.akvs_shared_attention(b.q, c, b.kp, b.vp, b.ko, b.vo, b.m, out, lse, ws,
+                                   stream=stream)
+        akvs.akvs_attention_weights(b.q, lse, c, b.kp, b.ko, b.m, None, w, None, wo, ws,
+                                    stream=stream)
+    bufs = b.out, b.lse, w, wo
+    run(*bufs)
+    torch.cuda.synchronize()
+    first = [t.clone() for t in bufs]
+    run(*bufs)
+    assert all(torch.equal(x, y) for x, y in zip(first, bufs))
+    s = torch.cuda.Stream()
+    for t in bufs:
+        t.zero_()
+    torch.cuda.synchronize()
+    run(*bufs, stream=s)
+    s.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(first, bufs))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(*bufs)
+    other = randn(96, *b.q.shape, dt=BF)
+    for step in range(4):
+        for t in bufs:
+            t.zero_()
+        if step == 2:
+            b.q.copy_(other)
+            run(*bufs)
+            torch.cuda.synchronize()
+            first = [t.clone() for t in bufs]
+            for t in bufs:
+                t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(first, bufs)), step
+    b.check()
+
+
+# ---- weights ------------------------------------------------------------------------------
+
+def weigh(b, prev=True, seed=0):
+    c = b.cfg()
+    wp = randn(seed + 7, b.hkv, b.P).square()
+    wo = randn(seed + 8, b.B, b.hkv, b.cap).square()
+    p0, o0 = wp.clone(), wo.clone()
+    akvs.akvs_attention_weights(b.q, b.lse, c, b.kp, b.ko, b.m, wp if prev else None, wp,
+                                wo if prev else None, wo, b.ws(c))
+    ep, eo, fp, fo = ref.weights(b.q[:b.n], b.lse[:b.n], b.kp, b.ko, b.start, b.own_len, b.cap)
+    if prev:
+        ep, eo = ep + p0.double().cpu(), eo + o0.double().cpu()
+    terms = b.n * (b.hq // b.hkv)
+    for got, want, far in ((wp, ep, fp), (wo, eo, fo)):
+        err = (got.double().cpu() - want).abs()
+        tol = ref.weights_bound(want, far, b.hd, terms)
+        assert bool((err <= tol).all()), float((err - tol).max())
+    return wp, wo
+
+
+@pytest.mark.parametrize("hq,hkv,hd,dt", GEOMS)
+@pytest.mark.parametrize("prev", [True, False])
+def test_weights(hq, hkv, hd, dt, prev):
+    b = Batch(hq, hkv, hd, dt, 131, [3, 0, 5, 1, 17], [3, 40, 2, 0, 50], seed=101, spare=2)
+    b.attend()
+    b.lse[b.n:] = 0.0  # rows behind the last request give nothing
+    weigh(b, prev, 101)
+
+
+@pytest.mark.parametrize("hq,hkv,hd,dt,prefix,rows,own", [
+    (24, 8, 128, BF, 700, [60, 70, 3], [80, 70, 400]), (28, 4, 128, BF, 2100, [1] * 20, [7] * 20),
+    (4, 2, 64, F32, 300, [50, 1], [60, 1]), (6, 2, 64, BF, 5, [130], [300]),
+    (24, 8, 128, BF, 0, [2], [33])])
+def test_weights_of_many_rows(hq, hkv, hd, dt, prefix, rows, own):
+    b = Batch(hq, hkv, hd, dt, prefix, rows, own, seed=111)
+    b.attend()
+    wp, wo = weigh(b, False, 111)
+    # every row's probabilities add up to one, each query head's
+    total = float(wp.double().sum() + wo.double().sum())
+    assert abs(total - b.n * hq) < 1e-4 * b.n * hq
+
+
+def test_weights_of_rows_that_see_no_key():
+    b = Batch(24, 8, 128, BF, 0, [2, 3, 1], [0, 1, 9], own_rows=12, seed=121)
+    b.attend()
+    c = b.cfg()
+    wo = torch.empty((3, 8, 12), device=DEV)
+    akvs.akvs_attention_weights(b.q, b.lse, c, None, b.ko, b.m, None, None, None, wo, b.ws(c))
+    assert bool((wo[0] == 0).all()) and bool(torch.isfinite(wo).all())
+    assert abs(float(wo[1].sum()) - 24) < 1e-3 and abs(float(wo[2].sum()) - 24) < 1e-3
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_weights_of_keys_that_are_not_finite(dt):
+    """A hidden key of NaN (behind a request's last row) gives nothing and keeps what it had; a
+    NaN query spoils every key of its KV head that its row sees and none else."""
+    b = Batch(4, 2, 128, dt, 70, [3, 1], [9, 4], own_rows=16, seed=131)
+    b.attend()
+    weigh(b, True, 131)  # (own keys past the lengths are NaN)
+    b.q[0, 0] = math.nan
+    c = b.cfg()
+    wp, wo = torch.empty((2, 70), device=DEV), torch.empty((2, 2, 16), device=DEV)
+    akvs.akvs_attention_weights(b.q, b.lse, c, b.kp, b.ko, b.m, None, wp, None, wo, b.ws(c))
+    assert bool(torch.isnan(wp[0]).all()) and bool(torch.isfinite(wp[1]).all())
+    assert bool(torch.isnan(wo[0, 0, :7]).all()) and bool(torch.isfinite(wo[0, 0, 7:]).all())
+    assert bool(torch.isfinite(wo[0, 1]).all()) and bool(torch.isfinite(wo[1]).all())
+
+
+# ---- norms and rotation ----------------------------------------------------------------------
+
+def rope(n, hd):
+    t = torch.empty((n, hd // 2, 2), dtype=F32, device=DEV)
+    akvs.akvs_rope_table(n, hd, 1e4, t)
+    return t
+
+
+def close_rotated(got, want, mags, dt):
+    """One rounding to the storage type; 32-bit sums of hd squares and ten more operations on
+    terms of the size `mags`."""
+    tol = (torch.finfo(dt).eps / 2) * want.abs() + (128 + 16) * 2.0 ** -24 * mags * 1.01 + 1e-30
+    err = (got.double().cpu() - want).abs()
+    assert bool((err <= tol).all()), float((err - tol).max())
+
+
+@pytest.mark.parametrize("hq,hkv,hd,dt", GEOMS)
+@pytest.mark.parametrize("rows", [1, 7, 130])
+def test_qk_norm_rope_packed(hq, hkv, hd, dt, rows):
+    """Views of a packed projection, cache rows in any order, some written nowhere."""
+    m, tab = model(hq, hkv, hd, dt), rope(500, hd)
+    qkv = randn(rows, rows, (hq + 2 * hkv) * hd, dt=dt, std=3.0)
+    a, b = hq * hd, (hq + hkv) * hd
+    gq, gk = randn(1, hd, dt=dt), randn(2, hd, dt=dt)
+    rng = np.random.default_rng(rows)
+    pos = rng.integers(0, 500, rows)
+    slots = rng.permutation(rows + 20)[:rows]
+    slots[rows // 2] = -1 if rows > 1 else slots[rows // 2]
+    if rows > 5:
+        slots[0] = rows + 20
+    qo = torch.full((rows, hq, hd), 5.0, dtype=dt, device=DEV)
+    ko = torch.full((rows + 20, hkv, hd), 5.0, dtype=dt, device=DEV)
+    vo = ko.clone()
+    akvs.akvs_qk_norm_rope(qkv[:, :a], qkv[:, a:b], qkv[:, b:], rows, ints(pos), gq, gk, m, tab,
+                           500, ints(slots), rows + 20, qo, ko, vo)
+    cs = tab.cpu()[pos]
+    x = qkv.cpu().view(rows, hq + 2 * hkv, hd)
+    want, mags = ref.norm_rope(x[:, :hq], gq, cs[..., 0], cs[..., 1], 1e-6)
+    close_rotated(qo, want, mags, dt)
+    want, mags = ref.norm_rope(x[:, hq:hq + hkv], gk, cs[..., 0], cs[..., 1], 1e-6)
+    ok = [i for i in range(rows) if 0 <= slots[i] < rows + 20]
+    at = slots[ok]
+    close_rotated(ko[at], want[ok], mags[ok], dt)
+    assert torch.equal(vo[at].cpu(), x[ok, hq + hkv:])
+    rest = np.setdiff1d(np.arange(rows + 20), at)
+    assert bool((ko[rest] == 5).all()) and bool((vo[rest] == 5).all())
+
+
+@pytest.mark.parametrize("hq,hkv,hd,dt", [(24, 8, 128, BF), (6, 2, 64, BF), (4, 2, 128, F32)])
+def test_qk_norm_rope_in_place_without_norms_or_values(hq, hkv, hd, dt):
+    m, tab, n = model(hq, hkv, hd, dt), rope(40, hd), 9
+    q, k = randn(1, n, hq, hd, dt=dt), randn(2, n, hkv, hd, dt=dt)
+    q0, k0 = q.clone(), k.clone()
+    pos = np.arange(n) * 4 % 40
+    gk = randn(3, hd, dt=dt)
+    akvs.akvs_qk_norm_rope(q, k, None, n, ints(pos), None, gk, m, tab, 40, None, n, q, k, None)
+    cs = tab.cpu()[pos]
+    for got, x, g in ((q, q0, None), (k, k0, gk)):
+        want, mags = ref.norm_rope(x, g, cs[..., 0], cs[..., 1], 1e-6)
+        close_rotated(got, want, mags, dt)
+
+
+def test_qk_norm_rope_extremes():
+    """Rows of zeros (0 / sqrt(eps)), of one large element, of the smallest and largest
+    magnitudes whose squares stay in range, and NaN that stays in its head."""
+    hq, hkv, hd, n = 4, 2, 128, 6
+    m, tab = model(hq, hkv, hd, F32), rope(8, hd)
+    q, k = torch.zeros((n, hq, hd), device=DEV), torch.zeros((n, hkv, hd), device=DEV)
+    q[1, :, 3] = 1e4
+    q[2] = randn(5, hq, hd) * 1e-12
+    q[3] = randn(6, hq, hd) * 1e17
+    q[4] = randn(7, hq, hd)
+    k[:] = randn(8, n, hkv, hd)
+    k[4, 1, 60] = math.nan
+    g = randn(9, hd)
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    akvs.akvs_qk_norm_rope(q, k, None, n, ints(np.arange(n)), g, g, m, tab, 8, None, n, qo, ko, None)
+    cs = tab.cpu()[np.arange(n)]
+    want, mags = ref.norm_rope(q, g, cs[..., 0], cs[..., 1], 1e-6)
+    close_rotated(qo, want, mags, F32)
+    assert bool((qo[0] == 0).all())
+    assert bool(torch.isnan(ko[4, 1]).all())
+    ko[4, 1] = 0
+    assert bool(torch.isfinite(ko).all())
+
+
+# ---- eviction -------------------------------------------------------------------------------
+
+class Evict:
+    def __init__(self, hkv, hd, dt, seqs, keys, keep, first=0, recent=0, src=0, dst=0, lens=None,
+                 weights=None, seed=0):
+        self.m = model(hkv, hkv, hd, dt)
+        self.hkv, self.S, self.n, self.keep_n = hkv, seqs, keys, keep
+        self.first, self.recent, self.dst = first, recent, dst or keep
+        self.lens = lens
+        self.k, self.v = (randn(seed + i, seqs, src or keys, hkv, hd, dt=dt) for i in (1, 2))
+        self.w = randn(seed + 3, seqs, hkv, keys).square() if weights is None else weights.to(DEV)
+        self.dlens = None if lens is None else ints(lens)
+        self.cfg = akvs.evict_cfg(seqs, keys, keep, first, recent, src, dst, self.dlens)
+        self.keep = torch.full((seqs, hkv, keep), -9, dtype=torch.int32, device=DEV)
+        self.ko = torch.full((seqs, self.dst, hkv, hd), 3.0, dtype=dt, device=DEV)
+        self.vo = self.ko.clone()
+        self.wo = torch.full((seqs, hkv, self.dst), -9.0, device=DEV)
+        self.lo = torch.full((seqs,), -9, dtype=torch.int32, device=DEV)
+
+    def run(self, **kw):
+        akvs.akvs_evict_cache(self.k, self.v, self.w, self.cfg, self.m, self.keep, self.ko, self.vo,
+                              self.wo, self.lo, **kw)
+        return self
+
+    def check(self):
+        w = self.w.cpu().numpy()
+        for s in range(self.S):
+            n = self.n if self.lens is None else self.lens[s]
+            kept = min(n, self.keep_n)
+            assert int(self.lo[s]) == kept
+            for h in range(self.hkv):
+                want = ref.evict([float(x) for x in w[s, h, :n]], n, self.keep_n, self.first,
+                                 self.recent)
+                assert self.keep[s, h].tolist() == want + [-1] * (self.keep_n - kept), (s, h)
+                i = torch.tensor(want, dtype=torch.long, device=DEV)
+                assert torch.equal(self.ko[s, :kept, h], self.k[s, i, h])
+                assert torch.equal(self.vo[s, :kept, h], self.v[s, i, h])
+                got = self.wo[s, h].view(torch.int32)
+                assert torch.equal(got[:kept], self.w[s, h, i].view(torch.int32))
+                assert bool((self.wo[s, h, kept:] == 0).all())
+            assert bool((self.ko[s, kept:] == 3).all()) and bool((self.vo[s, kept:] == 3).all())
+
+
+@pytest.mark.parametrize("hkv,hd,dt", [(8, 128, BF), (3, 64, BF), (2, 64, F32), (4, 128, F32)])
+@pytest.mark.parametrize("keys,keep,first,recent", [
+    (1, 1, 0, 0), (2, 1, 0, 0), (65, 64, 0, 0), (300, 17, 4, 9), (300, 13, 4, 9), (130, 130, 1, 1),
+    (90, 200, 3, 5), (1500, 512, 0, 64), (4097, 1024, 4, 128)])
+def test_evict(hkv, hd, dt, keys, keep, first, recent):
+    Evict(hkv, hd, dt, 2, keys, keep, first, recent, seed=keys).run().check()
+
+
+def test_evict_ragged_and_roomy_buffers():
+    """Lengths of 0, 1, fewer and more than are kept, one past its buffer (clamped), rows to
+    spare on both sides; lens_out over lens."""
+    lens = [0, 1, 49, 50, 51, 300, 299]
+    e = Evict(2, 64, BF, 7, 300, 50, 2, 10, src=310, dst=60, lens=lens, seed=3)
+    e.run().check()
+    e.lo = e.dlens
+    e.run().check()
+
+
+def test_evict_equal_and_unusual_weights():
+    """Equal weights keep the lower indices; NaN counts least, below -inf; zeros of both signs
+    are equal; the highest bits decide as well as the lowest."""
+    g = np.random.default_rng(5)
+    n = 700
+    w = np.stack([
+        np.zeros(n), g.integers(0, 3, n).astype(float), np.where(g.random(n) < 0.5, -0.0, 0.0),
+        np.where(g.random(n) < 0.9, np.nan, g.random(n)), np.full(n, np.nan),
+        np.where(g.random(n) < 0.7, -np.inf, np.inf), -g.random(n),
+        1.0 + g.integers(0, 40, n) * 2.0 ** -23]).astype(np.float32)
+    w[5, ::7] = np.nan
+    for keep in (1, 100, 350, 699):
+        Evict(8, 64, BF, 1, n, keep, weights=torch.from_numpy(w)[None], seed=keep).run().check()
+
+
+def test_evict_long_sequence():
+    e = Evict(2, 64, BF, 1, 70001, 9000, 4, 700, seed=13)
+    e.w[0, 1] = (e.w[0, 1] * 4).floor()  # few distinct values
+    e.run()
+    w = e.w.cpu().numpy()
+    for h in range(2):
+        mid = np.arange(4, 70001 - 700)
+        best = mid[np.argsort(-w[0, h, mid], kind="stable")[:9000 - 704]]
+        want = np.concatenate((np.arange(4), np.sort(best), np.arange(70001 - 700, 70001)))
+        assert np.array_equal(e.keep[0, h].cpu().numpy(), want)
+        assert torch.equal(e.ko[0, :, h], e.k[0, torch.from_numpy(want).to(DEV), h])
+
+
+def test_evict_outputs_left_out():
+    """Selection alone; the kept indices in the workspace."""
+    e = Evict(4, 128, BF, 3, 500, 90, 4, 20, seed=17)
+    e.run().check()
+    keep, ko, vo = e.keep.clone(), e.ko.clone(), e.vo.clone()
+    e.keep.fill_(-9)
+    e.lo.fill_(-9)
+    akvs.akvs_evict_cache(None, None, e.w, e.cfg, e.m, e.keep, None, None, None, e.lo)
+    assert torch.equal(e.keep, keep) and e.lo.tolist() == [90] * 3
+    ws = torch.empty(akvs.akvs_evict_workspace_size(e.m, e.cfg), dtype=torch.uint8, device=DEV)
+    e.ko.zero_()
+    e.vo.zero_()
+    akvs.akvs_evict_cache(e.k, e.v, e.w, e.cfg, e.m, None, e.ko, e.vo, None, None, ws)
+    assert torch.equal(e.ko, ko) and torch.equal(e.vo, vo)
+
+
+def test_evict_from_a_graph():
+    e = Evict(4, 128, BF, 2, 600, 100, 4, 20, seed=19)
+    e.run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        e.run()
+    for seed in (1, 2, 3):
+        e.w.copy_(randn(seed, *e.w.shape).square())
+        e.ko.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        e.check()
+
+
+# ---- together ---------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("hq,hkv,hd,dt", [(28, 4, 128, BF), (4, 2, 64, F32)])
+def test_decoding_over_a_context_that_is_cut(hq, hkv, hd, dt):
+    """Steps of a batch over one context: norms and rotation into the own caches, attention,
+    weights; after some the context and the own caches are cut and the batch goes on. Every
+    step's outputs against the definitions on what the caches hold."""
+    m, P, B, cap = model(hq, hkv, hd, dt), 200, 3, 24
+    tab = rope(400, hd)
+    kp, vp = randn(1, P, hkv, hd, dt=dt), randn(2, P, hkv, hd, dt=dt)
+    ko = torch.zeros((B, cap, hkv, hd), dtype=dt, device=DEV)
+    vo = torch.zeros_like(ko)
+    lens = torch.tensor([0, 3, 7], dtype=torch.int32, device=DEV)
+    ko.copy_(randn(3, *ko.shape, dt=dt))
+    vo.copy_(randn(4, *vo.shape, dt=dt))
+    wp, wo = torch.zeros((hkv, P), device=DEV), torch.zeros((B, hkv, cap), device=DEV)
+    gq, gk = randn(5, hd, dt=dt), randn(6, hd, dt=dt)
+    tokens = lens + 200  # positions go on counting whatever is evicted
+    slot0 = torch.arange(B, dtype=torch.int32, device=DEV) * cap
+    for step in range(12):
+        x = randn(20 + step, B, hq + 2 * hkv, hd, dt=dt)
+        q, out = torch.empty((2, B, hq, hd), dtype=dt, device=DEV)
+        lse = torch.empty((B, hq), device=DEV)
+        akvs.akvs_qk_norm_rope(x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:], B, tokens, gq, gk, m,
+                               tab, 400, slot0 + lens, B * cap, q, ko.view(B * cap, hkv, hd),
+                               vo.view(B * cap, hkv, hd))
+        tokens += 1
+        lens += 1
+        c = akvs.shared_cfg(B, B, 1, P, cap, None, lens)
+        n = akvs.akvs_shared_workspace_size(m, c)
+        ws = torch.empty(max(n, 256), dtype=torch.uint8, device=DEV)
+        akvs.akvs_shared_attention(q, c, kp, vp, ko, vo, m, out, lse, ws)
+        p0, o0 = wp.double().cpu(), wo.double().cpu()
+        akvs.akvs_attention_weights(q, lse, c, kp, ko, m, wp, wp, wo, wo, ws)
+        ln, st = lens.tolist(), starts([1] * B)
+        eo, el, mass, reach = ref.attention(q, kp, vp, ko, vo, st, ln)
+        assert bool(((out.double().cpu() - eo).abs() <= ref.out_bound(eo, mass, reach, hd, P + cap, dt)).all())
+        assert bool(((lse.double().cpu() - el).abs() <= ref.lse_bound(el, reach, hd, P + cap)).all())
+        ep, eo, fp, fo = ref.weights(q, lse, kp, ko, st, ln, cap)
+        for got, had, add, far in ((wp, p0, ep, fp), (wo, o0, eo, fo)):
+            tol = ref.weights_bound(had + add, far, hd, hq // hkv * B)
+            assert bool(((got.double().cpu() - had - add).abs() <= tol).all())
+        if step % 5 == 4:  # the context to 60 %, the own caches to 8 keys, the last 3 for sure
+            keep = P * 3 // 5
+            e = akvs.evict_cfg(1, P, keep, 4, 16)
+            k2, v2 = torch.empty((2, keep, hkv, hd), dtype=dt, device=DEV)
+            idx = torch.empty((hkv, keep), dtype=torch.int32, device=DEV)
+            w2 = torch.empty((hkv, keep), device=DEV)
+            akvs.akvs_evict_cache(kp, vp, wp, e, m, idx, k2, v2, w2, None)
+            for h in range(hkv):
+                want = ref.evict(wp[h].tolist(), P, keep, 4, 16)
+                assert idx[h].tolist() == want and torch.equal(k2[:, h], kp[want, h])
+                assert torch.equal(v2[:, h], vp[want, h])
+            kp, vp, wp, P = k2, v2, w2, keep
+            e = akvs.evict_cfg(B, cap, 8, 0, 3, dst_rows=cap, lens=lens)
+            k2, v2, w2 = torch.zeros_like(ko), torch.zeros_like(vo), torch.empty_like(wo)
+            idx = torch.empty((B, hkv, 8), dtype=torch.int32, device=DEV)
+            akvs.akvs_evict_cache(ko, vo, wo, e, m, idx, k2, v2, w2, lens)
+            assert lens.tolist() == [min(x, 8) for x in ln]
+            ko, vo, wo = k2, v2, w2

@@ -1,0 +1,177 @@
+"""Operators over a shared context: what they refuse, without a GPU."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2607_21604_amd import akvs
+from tests.libutil import ensure_built
+
+A = 4096  # an aligned address that nothing reads: every call here is refused
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return ensure_built()
+
+
+def model(hq=24, hkv=8, hd=128, dtype=akvs.AKVS_BF16):
+    return akvs.ModelCfg(1, 256, hq, hkv, hd, 256, 64, 1e4, 1e-6, dtype)
+
+
+def shared(**kw):
+    d = dict(n_req=4, n_rows=4, rows_max=1, prefix_len=100, own_rows=16, row_start=None, own_len=A)
+    d.update(kw)
+    return akvs.SharedCfg(*d.values())
+
+
+SHARED = [
+    (dict(n_req=0), akvs.AKVS_EINVAL), (dict(n_rows=-1), akvs.AKVS_EINVAL),
+    (dict(rows_max=0), akvs.AKVS_EINVAL), (dict(prefix_len=-1), akvs.AKVS_EINVAL),
+    (dict(own_rows=-1), akvs.AKVS_EINVAL), (dict(own_len=None), akvs.AKVS_EINVAL),
+    (dict(n_rows=5), akvs.AKVS_ESHAPE), (dict(rows_max=2), akvs.AKVS_ESHAPE),
+    (dict(prefix_len=1 << 28), akvs.AKVS_ESHAPE),
+    (dict(n_req=1 << 10, n_rows=1 << 10, own_rows=1 << 22), akvs.AKVS_ESHAPE),
+    (dict(n_rows=1 << 24, row_start=A), akvs.AKVS_ESHAPE),
+]
+
+
+@pytest.mark.parametrize("kw,status", SHARED)
+def test_invalid_batches(lib, kw, status):
+    m, c = model(), shared(**kw)
+    assert akvs.akvs_shared_workspace_size(m, c) == 0
+    assert lib.akvs_shared_attention(A, ctypes.byref(c), A, A, A, A, ctypes.byref(m), A, A, A,
+                                     1 << 40, None) == status
+    assert lib.akvs_attention_weights(A, A, ctypes.byref(c), A, A, ctypes.byref(m), A, A, A, A, A,
+                                      1 << 40, None) == status
+
+
+def test_invalid_models(lib):
+    c, e = shared(), akvs.evict_cfg(2, 100, 10)
+    for m, status in ((model(hd=96), akvs.AKVS_EUNSUPPORTED), (model(hq=20), akvs.AKVS_ESHAPE),
+                      (model(dtype=akvs.AKVS_U4G64), akvs.AKVS_EDTYPE)):
+        r = ctypes.byref(m)
+        assert lib.akvs_shared_attention(A, ctypes.byref(c), A, A, A, A, r, A, A, A, 1 << 40,
+                                         None) == status
+        assert lib.akvs_attention_weights(A, A, ctypes.byref(c), A, A, r, A, A, A, A, A, 1 << 40,
+                                          None) == status
+        assert lib.akvs_evict_cache(A, A, A, ctypes.byref(e), r, A, A, A, A, A, A, 1 << 40,
+                                    None) == status
+        assert lib.akvs_qk_norm_rope(A, 4096, A, 4096, A, 4096, 4, A, A, A, r, A, 10, None, 4, A, A,
+                                     A, None) == status
+        assert akvs.akvs_shared_workspace_size(m, c) == 0
+        assert akvs.akvs_evict_workspace_size(m, e) == 0
+
+
+def test_null_and_misaligned_pointers(lib):
+    m, c = model(), shared()
+    args = [A, ctypes.byref(c), A, A, A, A, ctypes.byref(m), A, A, A, 1 << 40, None]
+    for i in (0, 1, 2, 3, 4, 5, 6, 7):
+        bad = list(args)
+        bad[i] = None
+        assert lib.akvs_shared_attention(*bad) == akvs.AKVS_EINVAL, i
+    for i in (0, 2, 3, 4, 5, 7, 8, 9):
+        bad = list(args)
+        bad[i] = A + 8
+        assert lib.akvs_shared_attention(*bad) == akvs.AKVS_EINVAL, i
+    args = [A, A, ctypes.byref(c), A, A, ctypes.byref(m), A, A, A, A, A, 1 << 40, None]
+    for i in (0, 1, 2, 3, 4, 5):
+        bad = list(args)
+        bad[i] = None
+        assert lib.akvs_attention_weights(*bad) == akvs.AKVS_EINVAL, i
+    for i in (0, 1, 3, 4, 6, 7, 8, 9, 10):
+        bad = list(args)
+        bad[i] = A + 4
+        assert lib.akvs_attention_weights(*bad) == akvs.AKVS_EINVAL, i
+    bad = list(args)
+    bad[7] = bad[9] = None
+    assert lib.akvs_attention_weights(*bad) == akvs.AKVS_EINVAL
+
+
+def test_workspace(lib):
+    for kw in (dict(), dict(prefix_len=8000), dict(own_rows=3000), dict(n_req=64, n_rows=64)):
+        m, c = model(), shared(**kw)
+        need = akvs.akvs_shared_workspace_size(m, c)
+        if need == 0:
+            continue
+        assert lib.akvs_shared_attention(A, ctypes.byref(c), A, A, A, A, ctypes.byref(m), A, A, A,
+                                         need - 1, None) == akvs.AKVS_ENOSPACE
+        assert lib.akvs_shared_attention(A, ctypes.byref(c), A, A, A, A, ctypes.byref(m), A, A, None,
+                                         need, None) == akvs.AKVS_ENOSPACE
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(n_seq=0), akvs.AKVS_EINVAL), (dict(n_keys=-1), akvs.AKVS_EINVAL),
+    (dict(n_keep=0), akvs.AKVS_EINVAL), (dict(n_first=-1), akvs.AKVS_EINVAL),
+    (dict(n_recent=-1), akvs.AKVS_EINVAL), (dict(n_first=6, n_recent=5), akvs.AKVS_EINVAL),
+    (dict(src_rows=99), akvs.AKVS_ESHAPE), (dict(dst_rows=9), akvs.AKVS_ESHAPE),
+    (dict(n_seq=1 << 17), akvs.AKVS_ESHAPE), (dict(n_first=1 << 30, n_recent=1 << 30), akvs.AKVS_EINVAL)])
+def test_invalid_evictions(lib, kw, status):
+    d = dict(n_seq=2, n_keys=100, src_rows=0, n_keep=10, dst_rows=0, n_first=0, n_recent=0, lens=None)
+    d.update(kw)
+    m, c = model(), akvs.EvictCfg(*d.values())
+    assert akvs.akvs_evict_workspace_size(m, c) == 0
+    assert lib.akvs_evict_cache(A, A, A, ctypes.byref(c), ctypes.byref(m), A, A, A, A, A, A, 1 << 40,
+                                None) == status
+
+
+def test_eviction_buffers(lib):
+    """Missing and misaligned buffers, a short workspace, and outputs over inputs."""
+    m, c = model(2, 2, 64), akvs.evict_cfg(2, 100, 10)
+    row = 2 * 64 * 2
+    k, v, ko, vo = 1 << 20, 2 << 20, 3 << 20, 4 << 20
+    call = lambda *a: lib.akvs_evict_cache(*a[:3], ctypes.byref(c), ctypes.byref(m), *a[3:], None)  # noqa: E731
+    ok = [k, v, 5 << 20, 6 << 20, ko, vo, 7 << 20, 8 << 20, A, 1 << 30]
+    for i in (0, 1, 2, 4, 5):  # k, v, weights, k_out, v_out missing one by one
+        bad = list(ok)
+        bad[i] = None
+        assert call(*bad) == akvs.AKVS_EINVAL, i
+    for i in (0, 1, 2, 3, 4, 5, 6, 8):
+        bad = list(ok)
+        bad[i] += 4
+        assert call(*bad) == akvs.AKVS_EINVAL, i
+    need = akvs.akvs_evict_workspace_size(m, c)
+    bad = list(ok)
+    bad[3], bad[9] = None, need - 1
+    assert call(*bad) == akvs.AKVS_ENOSPACE
+    bad[8], bad[9] = None, need
+    assert call(*bad) == akvs.AKVS_ENOSPACE
+    for i, at in ((4, k), (4, v + 2 * 100 * row - 16), (5, k - 2 * 10 * row + 16), (5, ko), (6, 5 << 20)):
+        bad = list(ok)
+        bad[i] = at
+        assert call(*bad) == akvs.AKVS_EINVAL, (i, at)
+        assert b"overlap" in lib.akvs_last_error()
+
+
+def test_norm_arguments(lib):
+    m = model()
+    ok = [A, 24 * 128, A, 8 * 128, A, 8 * 128, 4, A, A, A, ctypes.byref(m), A, 10, None, 4, A, A, A,
+          None]
+    for i in (0, 2, 4, 7, 10, 11, 15, 16, 17):
+        bad = list(ok)
+        bad[i] = None
+        assert lib.akvs_qk_norm_rope(*bad) == akvs.AKVS_EINVAL, i
+    for i in (0, 2, 4, 8, 9, 11, 15, 16, 17):
+        bad = list(ok)
+        bad[i] = A + 8
+        assert lib.akvs_qk_norm_rope(*bad) == akvs.AKVS_EINVAL, i
+    for i, x in ((1, 24 * 128 - 8), (3, 1016), (5, 0), (1, 24 * 128 + 4), (3, 1028), (6, -1), (12, 0),
+                 (14, 3), (14, -1)):
+        bad = list(ok)
+        bad[i] = x
+        assert lib.akvs_qk_norm_rope(*bad) == akvs.AKVS_EINVAL, (i, x)
+
+
+def test_binding_refuses_wrong_tables_and_rows():
+    with pytest.raises(ValueError):
+        akvs.shared_cfg(4, 4, 1, 10, 8, None, torch.zeros(3, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        akvs.shared_cfg(4, 4, 1, 10, 8, torch.zeros(5, dtype=torch.int64), torch.zeros(4, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        akvs.evict_cfg(4, 10, 5, lens=torch.zeros(2, dtype=torch.int32))
+    x = torch.zeros(6, 8, 16)
+    assert akvs.rows_ptr(x[:, 2:4])[1] == 128 and akvs.rows_ptr(x[:1, 2:4])[1] == 32
+    with pytest.raises(ValueError):
+        akvs.rows_ptr(x[:, :, :8])
+    with pytest.raises(ValueError):
+        akvs.rows_ptr(x.transpose(0, 1))
