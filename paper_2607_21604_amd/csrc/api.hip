@@ -1711,7 +1711,8 @@ akvs_status akvs_qk_norm_rope(const void *q, int64_t ldq, const void *k, int64_t
 size_t akvs_shared_workspace_size(const akvs_model_cfg *m, const akvs_shared_cfg *c) {
   SharedBatch s;
   if (check_shared(m, c, &s) != AKVS_OK) return 0;
-  return 0;
+  return align256(sizeof(float) *
+                  shared_part_floats(s, m->n_q_heads, m->n_kv_heads, m->head_dim, m->dtype));
 }
 
 akvs_status akvs_shared_attention(const void *q, const akvs_shared_cfg *c, const void *k_prefix,
@@ -1727,9 +1728,13 @@ akvs_status akvs_shared_attention(const void *q, const akvs_shared_cfg *c, const
   REQUIRE(aligned16(q) && aligned16(k_prefix) && aligned16(v_prefix) && aligned16(k_own) &&
               aligned16(v_own) && aligned16(out) && aligned16(lse) && aligned16(ws),
           AKVS_EINVAL, "misaligned argument");
+  const size_t need = akvs_shared_workspace_size(m, c);
+  REQUIRE(need == 0 || (ws && ws_bytes >= need), AKVS_ENOSPACE, "workspace %zu < %zu bytes",
+          ws_bytes, need);
   LAUNCH(AKVS_K_ATTENTION,
          launch_shared_attention(s, q, k_prefix, v_prefix, k_own, v_own, m->n_q_heads,
-                                 m->n_kv_heads, m->head_dim, m->dtype, out, lse, stream));
+                                 m->n_kv_heads, m->head_dim, m->dtype, out, lse,
+                                 reinterpret_cast<float *>(ws), stream));
   return AKVS_OK;
 }
 

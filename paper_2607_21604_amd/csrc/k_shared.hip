@@ -1,13 +1,22 @@
 // Attention of a batch over one shared context, and the weights that its keys received.
+//
+// Both treat the (row, query head) pairs that read one KV head as rows of one matrix: 16
+// decoding requests of 5 heads per KV head are 80 rows against the shared keys, which are then
+// read once, through LDS, for all of them. The prefix is cut into splits and a request's own
+// keys into chunks; each is a work item of its own, all items run in one launch and leave
+// (output, maximum, sum) partials that a second launch merges.
+#include <algorithm>
+
 #include "kernels.h"
 
 namespace akvs {
 
-// Rows of request b: [r0, r1). Values of row_start are clamped into the buffers.
+// Rows of request b: [r0, r1), at most rows_max. Values of row_start are clamped into the
+// buffers.
 __device__ __forceinline__ void shared_rows(const SharedBatch &s, int b, int &r0, int &r1) {
   if (s.row_start) {
     r0 = min(max(s.row_start[b], 0), s.n_rows);
-    r1 = min(max(s.row_start[b + 1], r0), s.n_rows);
+    r1 = min(max(s.row_start[b + 1], r0), min(s.n_rows, r0 + s.rows_max));
   } else {
     r0 = b * s.rows_max;
     r1 = r0 + s.rows_max;
@@ -15,6 +24,363 @@ __device__ __forceinline__ void shared_rows(const SharedBatch &s, int b, int &r0
 }
 __device__ __forceinline__ int shared_live(const SharedBatch &s) {
   return s.row_start ? min(max(s.row_start[s.n_req], 0), s.n_rows) : s.n_rows;
+}
+
+// Work items of one call. Blocks [0, prefix_blocks): (split, pair tile, KV head), KV heads
+// innermost, so that the blocks streaming one head's keys share an XCD's L2; then (request,
+// chunk, pair tile, KV head) of the own keys.
+struct SharedPlan {
+  int p_groups, p_tiles, splits, split_keys, prefix_blocks;  // groups: 32-pair groups of a tile
+  int o_groups, o_tiles, chunks, chunk_keys;
+  int slots;  // partials per (row, head): splits + chunks
+};
+constexpr int SH_TILE = 64;  // keys of an LDS tile
+
+// The item that a block serves: pairs v0 .. of rows [r0, r1), keys [k0, k1) of (K, V) rows from
+// `base`. own = -1: prefix (every row sees all of it), else the request's own keys.
+struct SharedItem {
+  int kvh, r0, r1, v0, groups, k0, k1, slot, own;
+  size_t base;
+};
+__device__ __forceinline__ bool shared_item(const SharedBatch &s, const SharedPlan &p, int hkv,
+                                            int G, SharedItem &it) {
+  int id = blockIdx.x;
+  const bool prefix = id < p.prefix_blocks;
+  if (!prefix) id -= p.prefix_blocks;
+  it.kvh = id % hkv;
+  id /= hkv;
+  if (prefix) {
+    const int tile = id % p.p_tiles, split = id / p.p_tiles;
+    it.groups = p.p_groups;
+    it.v0 = tile * 32 * it.groups;
+    it.r0 = 0;
+    it.r1 = shared_live(s);
+    it.k0 = split * p.split_keys;
+    it.k1 = min(s.prefix_len, it.k0 + p.split_keys);
+    it.slot = split;
+    it.own = -1;
+    it.base = 0;
+  } else {
+    const int tile = id % p.o_tiles;
+    id /= p.o_tiles;
+    const int chunk = id % p.chunks, b = id / p.chunks;
+    it.groups = p.o_groups;
+    it.v0 = tile * 32 * it.groups;
+    shared_rows(s, b, it.r0, it.r1);
+    it.own = min(max(s.own_len[b], 0), s.own_rows);
+    it.k0 = chunk * p.chunk_keys;
+    it.k1 = min(it.own, it.k0 + p.chunk_keys);
+    it.slot = p.splits + chunk;
+    it.base = (size_t)b * s.own_rows;
+  }
+  return it.v0 < (it.r1 - it.r0) * G;
+}
+// Keys that row r (of the item's rows) sees.
+__device__ __forceinline__ int shared_seen(const SharedItem &it, int r) {
+  if (it.own < 0) return it.k1;
+  return min(max(it.own - (it.r1 - r) + 1, 0), it.k1);
+}
+
+__device__ __forceinline__ bool odd_bf16(uint32_t lo16) { return (lo16 & 0x7f80u) == 0x7f80u; }
+
+// bf16. Block = 4 waves over a tile of 32 * groups pairs (groups 1, 2 or 4) and one key range.
+// Keys stream through LDS in tiles of 64, loaded into registers a tile ahead; a wave takes 32
+// pairs and 32 or 64 of the tile's keys: with 4 groups each wave has a group, with 2 two waves
+// share a group's keys, with 1 two of the waves only load. Scores are formed transposed,
+// S^T = K Q^T (MFMA 32x32x16): lane l holds 16 scores of pair l % 32, which is the operand
+// layout of O^T = V^T P^T; V^T comes from row-major rows by the transposing LDS read. Softmax
+// statistics and outputs are fp32; the probabilities are rounded to bf16 for the second
+// product (the matrix cores' type), their sum is not.
+template <int HD>
+__global__ __launch_bounds__(256, 2) void k_shared_bf16(
+    SharedBatch s, SharedPlan p, const bf16_t *__restrict__ Q, const bf16_t *__restrict__ Kp,
+    const bf16_t *__restrict__ Vp, const bf16_t *__restrict__ Ko, const bf16_t *__restrict__ Vo,
+    int hq, int hkv, float scale_log2, bf16_t *__restrict__ out, float *__restrict__ lse,
+    float *__restrict__ part_o, float2 *__restrict__ part_ml) {
+  constexpr int KS = HD / 16, DB = HD / 32, CPK = HD / 8;
+  constexpr int KST = HD + 8, VST = HD + 32;       // row strides: fragment reads on all banks
+  constexpr int NCH = SH_TILE * CPK / 256;         // 16-byte chunks of K (and V) per thread
+  constexpr int KB = SH_TILE * KST, VB = SH_TILE * VST;
+  __shared__ __attribute__((aligned(16))) bf16_t s_kv[2 * (KB + VB)];
+  __shared__ int s_odd;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hi = lane >> 5;
+  const int G = hq / hkv;
+  SharedItem it;
+  if (!shared_item(s, p, hkv, G, it)) return;
+  const bf16_t *K = it.own < 0 ? Kp : Ko, *V = it.own < 0 ? Vp : Vo;
+  // this wave's pairs and its share of a tile's two 32-key halves
+  const int group = it.groups == 4 ? wave : it.groups == 2 ? wave >> 1 : 0;
+  const bool works = it.groups > 1 || wave < 2;
+  const int st0 = it.groups == 4 ? 0 : wave & 1, st_step = it.groups == 4 ? 1 : 2;
+  const int n_pairs = (it.r1 - it.r0) * G;
+  const int v = it.v0 + group * 32 + (lane & 31);
+  const bool valid = v < n_pairs;
+  const int r = it.r0 + (valid ? v : it.v0) / G, head = it.kvh * G + (valid ? v : it.v0) % G;
+  const int seen = valid ? shared_seen(it, r) : 0;
+  // what the tile's last and first rows see: keys past the one are not read, keys up to the
+  // other need no mask
+  const int last = min(n_pairs, it.v0 + 32 * it.groups) - 1;
+  const int k1 = shared_seen(it, it.r0 + last / G), all_see = shared_seen(it, it.r0 + it.v0 / G);
+  const size_t prow = ((size_t)it.slot * s.n_rows + r) * hq + head;
+  const int nkt = k1 > it.k0 ? (k1 - it.k0 + SH_TILE - 1) / SH_TILE : 0;
+  const bool writes = valid && (it.groups == 4 || (works && (wave & 1) == 0));
+  if (nkt == 0 && p.slots > 1) {
+    if (writes && hi == 0) part_ml[prow] = make_float2(-INFINITY, 0.f);
+    return;
+  }
+
+  bf16x8_t qf[KS];
+  {
+    const bf16_t *q = Q + ((size_t)r * hq + head) * HD + hi * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8_t *>(q + ks * 16);
+  }
+  f32x16_t o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;  // (l_run: of this lane's half of the keys)
+
+  u32x4_t kreg[NCH], vreg[NCH];
+  auto load = [&](int key0) __attribute__((always_inline)) {  // keys past k1 re-read the last
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int c = tid + 256 * i, kr = c / CPK, e0 = (c % CPK) * 8;
+      const size_t at = ((it.base + min(key0 + kr, k1 - 1)) * hkv + it.kvh) * HD + e0;
+      kreg[i] = *reinterpret_cast<const u32x4_t *>(K + at);
+      vreg[i] = *reinterpret_cast<const u32x4_t *>(V + at);
+    }
+  };
+  // Values that some pair of the tile must not see take part with probability 0, and 0 * inf is
+  // NaN: where such a value is not finite, 0 goes to LDS, and the pairs that do see it get it
+  // added at the end.
+  auto store = [&](int key0, int buf) __attribute__((always_inline)) {
+    bf16_t *ks = s_kv + buf * (KB + VB), *vs = ks + KB;
+    const bool some_hidden = key0 + SH_TILE > all_see;
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int c = tid + 256 * i, kr = c / CPK, e0 = (c % CPK) * 8;
+      if (some_hidden && key0 + kr >= all_see) {
+        bool odd = false;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t w = vreg[i][j];
+          const bool a = odd_bf16(w), b = odd_bf16(w >> 16);
+          odd |= a | b;
+          vreg[i][j] = w & (a ? 0xffff0000u : 0xffffffffu) & (b ? 0xffffu : 0xffffffffu);
+        }
+        if (odd) s_odd = 1;
+      }
+      *reinterpret_cast<u32x4_t *>(ks + kr * KST + e0) = kreg[i];
+      *reinterpret_cast<u32x4_t *>(vs + kr * VST + e0) = vreg[i];
+    }
+  };
+  if (tid == 0) s_odd = 0;
+  if (nkt) load(it.k0);
+  __syncthreads();
+  if (nkt) store(it.k0, 0);
+  __syncthreads();
+  for (int kt = 0; kt < nkt; ++kt) {
+    const int key0 = it.k0 + kt * SH_TILE;
+    const bool more = kt + 1 < nkt;
+    if (more) load(key0 + SH_TILE);
+    const bf16_t *ks_ = s_kv + (kt & 1) * (KB + VB), *vs_ = ks_ + KB;
+    for (int st = works ? st0 : 2; st < 2; st += st_step) {
+      const int sk0 = key0 + st * 32;
+      if (sk0 >= k1) break;
+      // S^T block: score i is key sk0 + (i / 4) * 8 + hi * 4 + i % 4 of this lane's pair
+      f32x16_t sc;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+      const bf16_t *krow = ks_ + (st * 32 + (lane & 31)) * KST + hi * 8;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            *reinterpret_cast<const bf16x8_t *>(krow + ks * 16), qf[ks], sc, 0, 0, 0);
+      // V^T operand of step t, dims db * 32 + lane % 32: its 8 slots are keys 16 t + 4 hi + 0..3
+      // and the same + 8 of the block
+      bf16x8_t vf[2][DB];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          typedef short v4s __attribute__((ext_vector_type(4)));
+          const bf16_t *vb = vs_ + (st * 32 + 16 * t + 4 * hi + ((lane & 15) >> 2)) * VST +
+                             db * 32 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+          const v4s x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) v4s *)(vb));
+          const v4s x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) v4s *)(vb + 8 * VST));
+          __builtin_memcpy(&vf[t][db], &x0, 8);
+          __builtin_memcpy(reinterpret_cast<char *>(&vf[t][db]) + 8, &x1, 8);
+        }
+      if (sk0 + 32 > all_see) {
+        const int lim = seen - (sk0 + hi * 4);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if ((i >> 2) * 8 + (i & 3) >= lim) sc[i] = -INFINITY;
+      }
+      float mx = sc[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[i]);
+      // the running maximum rises only when some score exceeds it by more than 2^8
+      if (__ballot(mx * scale_log2 > m_run + 8.f)) {
+        const float mp = fmaxf(mx, __shfl_xor(mx, 32, 64)) * scale_log2;
+        const float m_new = fmaxf(m_run, mp);
+        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[db] *= alpha;
+        l_run *= alpha;
+        m_run = m_new;
+      }
+      const float m_off = m_run == -INFINITY ? 0.f : m_run;  // (no key yet: every p is 0)
+      float pv[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        pv[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], scale_log2, -m_off));
+        l_run += pv[i];
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        uint32_t pw[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) pw[j] = pack_bf2(pv[8 * t + 2 * j], pv[8 * t + 2 * j + 1]);
+        bf16x8_t pb;
+        __builtin_memcpy(&pb, pw, 16);
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[t][db], pb, o[db], 0, 0, 0);
+      }
+    }
+    if (more) store(key0 + SH_TILE, (kt + 1) & 1);
+    __syncthreads();
+  }
+  float l = l_run + __shfl_xor(l_run, 32, 64);
+  if (it.groups < 4) {  // the two waves of a group: the odd one hands over through LDS
+    float *x = reinterpret_cast<float *>(s_kv) + group * (HD / 2 + 2) * 64 + lane;
+    if (works && (wave & 1)) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[(db * 16 + i) * 64] = o[db][i];
+      x[HD / 2 * 64] = m_run;
+      x[(HD / 2 + 1) * 64] = l;
+    }
+    __syncthreads();
+    if (!works || (wave & 1)) return;
+    const float m2 = x[HD / 2 * 64], l2 = x[(HD / 2 + 1) * 64];
+    const float mm = fmaxf(m_run, m2), off = mm == -INFINITY ? 0.f : mm;
+    // a half without a key has m = -inf, l = 0 and o = 0; one of NaN scores l = NaN
+    const float a = __builtin_amdgcn_exp2f(m_run - off), b = __builtin_amdgcn_exp2f(m2 - off);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[db][i] = a * o[db][i] + b * x[(db * 16 + i) * 64];
+    l = a * l + b * l2;
+    m_run = mm;
+  }
+  if (!valid) return;
+  if (s_odd) {  // values left out above that this pair sees
+    for (int k = max(it.k0, all_see); k < seen; ++k) {
+      const bf16_t *vr = V + ((it.base + k) * hkv + it.kvh) * HD + hi * 4;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const uint2 w = *reinterpret_cast<const uint2 *>(vr + db * 32 + q4 * 8);
+          const uint32_t x[4] = {w.x & 0xffffu, w.x >> 16, w.y & 0xffffu, w.y >> 16};
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (odd_bf16(x[j])) o[db][4 * q4 + j] += __uint_as_float(x[j] << 16);
+        }
+    }
+  }
+  // o[db][i] is dim db * 32 + (i / 4) * 8 + hi * 4 + i % 4 of the pair
+  if (p.slots > 1) {
+    float *po = part_o + prow * HD + hi * 4;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4)
+        store4(po + db * 32 + q4 * 8, o[db][4 * q4], o[db][4 * q4 + 1], o[db][4 * q4 + 2],
+               o[db][4 * q4 + 3]);
+    if (hi == 0) part_ml[prow] = make_float2(m_run, l);
+    return;
+  }
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  bf16_t *orow = out + ((size_t)r * hq + head) * HD + hi * 4;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4)
+      store4(orow + db * 32 + q4 * 8, o[db][4 * q4] * inv, o[db][4 * q4 + 1] * inv,
+             o[db][4 * q4 + 2] * inv, o[db][4 * q4 + 3] * inv);
+  if (lse && hi == 0)
+    lse[(size_t)r * hq + head] =
+        l == 0.f ? -INFINITY : (m_run == -INFINITY ? 0.f : m_run * 0.6931471805599453f) + logf(l);
+}
+
+// out = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s over a pair's slots, M = max m_s. A slot
+// without a key holds m = -inf, l = 0 (its output was not written and is not read); one of NaN
+// scores holds l = NaN. A block serves 256 / (per * GROUPS) pairs: `per` threads of 8 dims,
+// GROUPS of them taking the slots in turn, added in order through LDS.
+template <typename TS, int GROUPS>
+__global__ __launch_bounds__(256) void k_shared_merge(SharedBatch s, int slots, int hq, int hd,
+                                                      const float *__restrict__ part_o,
+                                                      const float2 *__restrict__ part_ml,
+                                                      TS *__restrict__ out,
+                                                      float *__restrict__ lse) {
+  __shared__ float s_a[GROUPS > 1 ? 256 * 9 : 1], s_m[GROUPS > 1 ? 256 : 1];
+  const int per = hd >> 3, team = per * GROUPS, tid = threadIdx.x;
+  const int e0 = (tid % per) * 8, g = tid % team / per;
+  const long long item = (long long)blockIdx.x * (256 / team) + tid / team;
+  const bool live = item < (long long)shared_live(s) * hq;
+  const size_t stride = (size_t)s.n_rows * hq;
+  float m = -INFINITY, l = 0.f, a[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a[i] = 0.f;
+  if (live) {
+    for (int u = g; u < slots; u += GROUPS) {
+      const float2 ml = part_ml[u * stride + item];
+      if (ml.y == 0.f) continue;
+      float x[8];
+      load8(part_o + (u * stride + item) * hd + e0, x);
+      const float m_new = fmaxf(m, ml.x), off = m_new == -INFINITY ? 0.f : m_new;
+      const float wa = exp2f(m - off), wb = exp2f(ml.x - off);
+      l = wa * l + wb * ml.y;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) a[i] = wa * a[i] + wb * x[i];
+      m = m_new;
+    }
+  }
+  if (GROUPS > 1) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s_a[tid * 9 + i] = a[i];
+    s_a[tid * 9 + 8] = l;
+    s_m[tid] = m;
+    __syncthreads();
+    if (g != 0 || !live) return;
+    for (int q = 1; q < GROUPS; ++q) {
+      const int o = tid + q * per;
+      const float m2 = s_m[o], l2 = s_a[o * 9 + 8];
+      if (l2 == 0.f) continue;
+      const float m_new = fmaxf(m, m2), off = m_new == -INFINITY ? 0.f : m_new;
+      const float wa = exp2f(m - off), wb = exp2f(m2 - off);
+      l = wa * l + wb * l2;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) a[i] = wa * a[i] + wb * s_a[o * 9 + i];
+      m = m_new;
+    }
+  } else if (!live) {
+    return;
+  }
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a[i] *= inv;
+  store8(out + item * hd + e0, a);
+  if (lse && e0 == 0)
+    lse[item] = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m * 0.6931471805599453f) + logf(l);
 }
 
 // A wave per (row, query head): a lane per key for the scores, a lane per dim (or two) for the
@@ -145,25 +511,89 @@ __global__ __launch_bounds__(256) void k_attn_weights(SharedBatch s, const TS *_
   w[j] = (prev ? prev[j] : 0.f) + sum;
 }
 
-template <typename TS>
-static hipError_t shared_attention(const SharedBatch &s, const void *q, const void *kp,
-                                   const void *vp, const void *ko, const void *vo, int hq,
-                                   int hkv, int hd, void *out, float *lse, hipStream_t st) {
-  auto p = [](const void *x) { return reinterpret_cast<const TS *>(x); };
-  hipLaunchKernelGGL(k_shared_attn<TS>, dim3((unsigned)((size_t)s.n_rows * hq)), dim3(64), 0, st, s,
-                     p(q), p(kp), p(vp), p(ko), p(vo), hq, hkv, hd,
-                     1.4426950408889634f / sqrtf((float)hd), reinterpret_cast<TS *>(out), lse);
+// Items of a call (bf16).
+static SharedPlan shared_plan(const SharedBatch &s, int hq, int hkv, int cus) {
+  SharedPlan p{};
+  const int G = hq / hkv;
+  auto groups = [](long long pairs) { return pairs > 64 ? 4 : pairs > 32 ? 2 : 1; };
+  auto tiles = [](long long pairs, int g) { return (int)((pairs + 32 * g - 1) / (32 * g)); };
+  const long long pp = (long long)s.n_rows * G, op = (long long)s.rows_max * G;
+  p.p_groups = groups(pp);
+  p.p_tiles = tiles(pp, p.p_groups);
+  p.o_groups = groups(op);
+  p.o_tiles = tiles(op, p.o_groups);
+  const int slots = 2 * cus;
+  auto cut = [&](long long items, int keys, int *pieces, int *piece_keys) {
+    const int kt = (keys + SH_TILE - 1) / SH_TILE;
+    long long want = items ? std::max(1LL, slots / items) : 1;
+    want = std::min<long long>(want, std::max(1, kt / 2));
+    const int per = kt ? (int)((kt + want - 1) / want) : 1;
+    *piece_keys = per * SH_TILE;
+    *pieces = (kt + per - 1) / per;
+  };
+  cut((long long)p.p_tiles * hkv, s.prefix_len, &p.splits, &p.split_keys);
+  cut((long long)s.n_req * p.o_tiles * hkv, s.own_rows, &p.chunks, &p.chunk_keys);
+  p.prefix_blocks = p.splits * p.p_tiles * hkv;
+  p.slots = p.splits + p.chunks;
+  return p;
+}
+
+size_t shared_part_floats(const SharedBatch &s, int hq, int hkv, int hd, int dtype) {
+  if (dtype != AKVS_BF16 || s.n_rows == 0) return 0;
+  const SharedPlan p = shared_plan(s, hq, hkv, gemm_cu_count());
+  return p.slots > 1 ? (size_t)p.slots * s.n_rows * hq * (hd + 2) : 0;
+}
+
+template <int HD>
+static hipError_t shared_bf16(const SharedBatch &s, const void *q, const void *kp, const void *vp,
+                              const void *ko, const void *vo, int hq, int hkv, void *out,
+                              float *lse, float *part, hipStream_t st) {
+  auto b = [](const void *x) { return reinterpret_cast<const bf16_t *>(x); };
+  bf16_t *O = reinterpret_cast<bf16_t *>(out);
+  SharedPlan p = shared_plan(s, hq, hkv, gemm_cu_count());
+  const size_t n = (size_t)p.slots * s.n_rows * hq;
+  float2 *ml = reinterpret_cast<float2 *>(part + n * HD);
+  size_t blocks = p.prefix_blocks + (size_t)s.n_req * p.chunks * p.o_tiles * hkv;
+  if (blocks == 0) {  // no key at all: one item without keys writes the rows' zeros
+    p.splits = p.slots = 1;
+    p.prefix_blocks = p.p_tiles * hkv;
+    blocks = p.prefix_blocks;
+  }
+  hipLaunchKernelGGL(k_shared_bf16<HD>, dim3((unsigned)blocks), dim3(256), 0, st, s, p, b(q), b(kp),
+                     b(vp), b(ko), b(vo), hq, hkv, 1.4426950408889634f / sqrtf((float)HD), O, lse,
+                     part, ml);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.slots <= 1) return e;
+  const size_t items = (size_t)s.n_rows * hq;
+  const int teams = 256 / (HD / 8);
+#define AKVS_MERGE(G_)                                                                          \
+  hipLaunchKernelGGL((k_shared_merge<bf16_t, G_>), dim3((unsigned)((items * G_ + teams - 1) / teams)), \
+                     dim3(256), 0, st, s, p.slots, hq, HD, part, ml, O, lse)
+  if (p.slots >= 12) AKVS_MERGE(16);
+  else if (p.slots >= 4) AKVS_MERGE(4);
+  else AKVS_MERGE(1);
+#undef AKVS_MERGE
+  return hipGetLastError();
+}
+
+static hipError_t shared_f32(const SharedBatch &s, const void *q, const void *kp, const void *vp,
+                             const void *ko, const void *vo, int hq, int hkv, int hd, void *out,
+                             float *lse, hipStream_t st) {
+  auto p = [](const void *x) { return reinterpret_cast<const float *>(x); };
+  hipLaunchKernelGGL(k_shared_attn<float>, dim3((unsigned)((size_t)s.n_rows * hq)), dim3(64), 0, st,
+                     s, p(q), p(kp), p(vp), p(ko), p(vo), hq, hkv, hd,
+                     1.4426950408889634f / sqrtf((float)hd), reinterpret_cast<float *>(out), lse);
   return hipGetLastError();
 }
 
 hipError_t launch_shared_attention(const SharedBatch &s, const void *q, const void *kp,
                                    const void *vp, const void *ko, const void *vo, int hq,
-                                   int hkv, int hd, int dtype, void *out, float *lse,
+                                   int hkv, int hd, int dtype, void *out, float *lse, float *part,
                                    hipStream_t st) {
   if (s.n_rows == 0) return hipSuccess;
-  return dtype == AKVS_BF16
-             ? shared_attention<bf16_t>(s, q, kp, vp, ko, vo, hq, hkv, hd, out, lse, st)
-             : shared_attention<float>(s, q, kp, vp, ko, vo, hq, hkv, hd, out, lse, st);
+  if (dtype != AKVS_BF16) return shared_f32(s, q, kp, vp, ko, vo, hq, hkv, hd, out, lse, st);
+  return hd == 128 ? shared_bf16<128>(s, q, kp, vp, ko, vo, hq, hkv, out, lse, part, st)
+                   : shared_bf16<64>(s, q, kp, vp, ko, vo, hq, hkv, out, lse, part, st);
 }
 
 template <typename TS>

@@ -210,8 +210,10 @@ struct SharedBatch {
 };
 hipError_t launch_shared_attention(const SharedBatch &s, const void *q, const void *kp,
                                    const void *vp, const void *ko, const void *vo, int hq,
-                                   int hkv, int hd, int dtype, void *out, float *lse,
+                                   int hkv, int hd, int dtype, void *out, float *lse, float *part,
                                    hipStream_t st);
+// floats of `part` (partials of key splits) that launch_shared_attention needs
+size_t shared_part_floats(const SharedBatch &s, int hq, int hkv, int hd, int dtype);
 hipError_t launch_attention_weights(const SharedBatch &s, const void *q, const float *lse,
                                     const void *kp, const void *ko, int hq, int hkv, int hd,
                                     int dtype, const float *wp_prev, float *wp,
