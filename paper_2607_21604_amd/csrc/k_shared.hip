@@ -450,65 +450,156 @@ __global__ __launch_bounds__(64) void k_shared_attn(SharedBatch s, const TS *__r
     lse[(size_t)r * hq + h] = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) * 0.6931471805599453f + logf(l);
 }
 
-// A thread per key of one KV head; blocks past the prefix's serve a request's own keys.
+// ---- the weights that keys received ----------------------------------------------------
+// Scores again, S = Q K^T, on the matrix cores (bf16: 32x32x16, fp32: 16x16x4), with pairs as
+// rows and keys as columns, so that a lane holds scores of one key: p = exp(s - lse) is summed
+// over pairs inside the lane, and a key's sum never leaves its column. A wave keeps a tile of
+// keys in registers and walks the pair tiles, the next tile's queries in flight; where keys
+// are few, `walkers` waves of a block share a key tile's pairs and are added in order.
 template <typename TS>
-__global__ __launch_bounds__(256) void k_attn_weights(SharedBatch s, const TS *__restrict__ Q,
+struct WeightTile;
+template <>
+struct WeightTile<bf16_t> {  // 32 pairs x 32 keys; C value i of a lane: row pair(i)
+  static constexpr int PAIRS = 32, KEYS = 32, NC = 16, VE = 8;
+  typedef f32x16_t Acc;
+  __device__ static int pair(int i, int sub) { return (i >> 2) * 8 + sub * 4 + (i & 3); }
+  __device__ static Acc mma(u32x4_t q, u32x4_t k, Acc c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, q),
+                                                   __builtin_bit_cast(bf16x8_t, k), c, 0, 0, 0);
+  }
+};
+template <>
+struct WeightTile<float> {  // 16 x 16
+  static constexpr int PAIRS = 16, KEYS = 16, NC = 4, VE = 4;
+  typedef f32x4_t Acc;
+  __device__ static int pair(int i, int sub) { return sub * 4 + i; }
+  __device__ static Acc mma(u32x4_t q, u32x4_t k, Acc c) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(q[e]), __uint_as_float(k[e]), c, 0,
+                                               0, 0);
+    return c;
+  }
+};
+
+// Blocks [0, prefix_blocks): (key block, KV head), then (request, key block, KV head) of the own
+// keys; a block's 4 waves are 4 / walkers key tiles by `walkers` waves each.
+struct WeightPlan {
+  int p_walkers, prefix_blocks, o_walkers, own_blocks;
+};
+
+template <typename TS, int HD>
+__global__ __launch_bounds__(256) void k_attn_weights(SharedBatch s, WeightPlan p,
+                                                      const TS *__restrict__ Q,
                                                       const float *__restrict__ lse,
                                                       const TS *__restrict__ Kp,
                                                       const TS *__restrict__ Ko, int hq, int hkv,
-                                                      int hd, float scale, int prefix_blocks,
-                                                      int own_blocks, const float *wp_prev,
+                                                      float scale_log2, const float *wp_prev,
                                                       float *wp, const float *wo_prev,
                                                       float *wo) {
-  const int kvh = blockIdx.y, G = hq / hkv;
-  int blk = blockIdx.x, r0 = 0, r1, n, n_all, own = 0;
+  typedef WeightTile<TS> W;
+  constexpr int C = HD / 16;
+  __shared__ float s_lse[4][W::PAIRS];
+  __shared__ int s_seen[4][W::PAIRS];
+  __shared__ float s_sum[4][W::KEYS];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, G = hq / hkv;
+  const int li = lane % W::KEYS, sub = lane / W::KEYS;  // this lane's pair / key, and its part
+  int id = blockIdx.x, r0 = 0, r1, n, n_all, own = 0, walkers;
   const TS *K;
   const float *prev;
   float *w;
-  const bool prefix = blk < prefix_blocks;
+  const bool prefix = id < p.prefix_blocks;
+  if (!prefix) id -= p.prefix_blocks;
+  const int kvh = id % hkv;
+  id /= hkv;
   if (prefix) {
     r1 = shared_live(s);
     n = n_all = s.prefix_len;
     K = Kp;
     prev = wp_prev ? wp_prev + (size_t)kvh * n : nullptr;
     w = wp + (size_t)kvh * n;
+    walkers = p.p_walkers;
   } else {
-    blk -= prefix_blocks;
-    const int b = blk / own_blocks;
-    blk -= b * own_blocks;
+    const int b = id / p.own_blocks;
+    id -= b * p.own_blocks;
     shared_rows(s, b, r0, r1);
     n = own = min(max(s.own_len[b], 0), s.own_rows);
     n_all = s.own_rows;
-    K = Ko + (size_t)b * s.own_rows * hkv * hd;
+    K = Ko + (size_t)b * s.own_rows * hkv * HD;
     const size_t o = ((size_t)b * hkv + kvh) * n_all;
     prev = wo_prev ? wo_prev + o : nullptr;
     w = wo + o;
+    walkers = p.o_walkers;
   }
-  const int j = blk * 256 + threadIdx.x;
-  if (j >= n_all) return;
+  const int j0 = (id * (4 / walkers) + wave / walkers) * W::KEYS, j = j0 + li;
+  const int n_pairs = (r1 - r0) * G;
+  const int step = walkers * W::PAIRS;
   float sum = 0.f;
-  if (j < n) {
-    const TS *k = K + ((size_t)j * hkv + kvh) * hd;
-    for (int r = r0; r < r1; ++r) {
-      if (!prefix && j > own - (r1 - r0) + (r - r0)) continue;
-      for (int g = 0; g < G; ++g) {
-        const int h = kvh * G + g;
-        const float ls = lse[(size_t)r * hq + h];
-        if (ls == -INFINITY) continue;
-        const TS *q = Q + ((size_t)r * hq + h) * hd;
-        float sc = 0.f;
-        for (int d = 0; d < hd; d += 8) {
-          float a[8], c[8];
-          load8(q + d, a);
-          load8(k + d, c);
+  int v0 = wave % walkers * W::PAIRS;
+  if (j0 < n && v0 < n_pairs) {
+    u32x4_t kf[C], qa[C], qb[C];
+    const TS *k = K + ((size_t)min(j, n - 1) * hkv + kvh) * HD + sub * W::VE;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) sc = fmaf(a[i], c[i], sc);
-        }
-        sum += expf(sc * scale - ls);
+    for (int c = 0; c < C; ++c) kf[c] = *reinterpret_cast<const u32x4_t *>(k + c * 16);
+    // the lane's pair of the tile from `at`: its query fragment, its lse (times log2 e) and how
+    // many keys it sees (0: no pair, or a row without keys)
+    auto load = [&](int at, u32x4_t (&q)[C], float &ls, int &seen) __attribute__((always_inline)) {
+      const int v = min(at + li, n_pairs - 1), r = r0 + v / G, h = kvh * G + v % G;
+      const TS *x = Q + ((size_t)r * hq + h) * HD + sub * W::VE;
+#pragma unroll
+      for (int c = 0; c < C; ++c) q[c] = *reinterpret_cast<const u32x4_t *>(x + c * 16);
+      ls = lse[(size_t)r * hq + h];
+      seen = at + li >= n_pairs || ls == -INFINITY ? 0 : prefix ? n : min(max(own - (r1 - r) + 1, 0), n);
+      ls *= 1.4426950408889634f;
+    };
+    auto weigh = [&](const u32x4_t (&q)[C], float ls, int seen) __attribute__((always_inline)) {
+      if (sub == 0) {
+        s_lse[wave][li] = ls;
+        s_seen[wave][li] = seen;
       }
+      typename W::Acc c;
+#pragma unroll
+      for (int i = 0; i < W::NC; ++i) c[i] = 0.f;
+#pragma unroll
+      for (int e = 0; e < C; ++e) c = W::mma(q[e], kf[e], c);
+      // (a wave's LDS accesses stay in order)
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      const bool masked = __ballot(seen < min(j0 + W::KEYS, n)) != 0;
+      float add = 0.f;
+#pragma unroll
+      for (int i = 0; i < W::NC; ++i) {
+        const int m = W::pair(i, sub);
+        const float e = __builtin_amdgcn_exp2f(fmaf(c[i], scale_log2, -s_lse[wave][m]));
+        add += masked && j >= s_seen[wave][m] ? 0.f : e;
+      }
+      sum += add;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    };
+    float la, lb;
+    int sa, sb;
+    load(v0, qa, la, sa);
+    while (true) {
+      if (v0 + step < n_pairs) load(v0 + step, qb, lb, sb);
+      weigh(qa, la, sa);
+      v0 += step;
+      if (v0 >= n_pairs) break;
+      if (v0 + step < n_pairs) load(v0 + step, qa, la, sa);
+      weigh(qb, lb, sb);
+      v0 += step;
+      if (v0 >= n_pairs) break;
     }
+#pragma unroll
+    for (int o = W::KEYS; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
   }
-  w[j] = (prev ? prev[j] : 0.f) + sum;
+  if (walkers > 1) {
+    if (sub == 0) s_sum[wave][li] = sum;
+    __syncthreads();
+    if (wave % walkers) return;
+    for (int q = 1; q < walkers; ++q) sum += s_sum[wave + q][li];
+  }
+  if (sub == 0 && j < n_all) w[j] = (prev ? prev[j] : 0.f) + (j < n ? sum : 0.f);
 }
 
 // Items of a call (bf16).
@@ -601,13 +692,31 @@ static hipError_t attention_weights(const SharedBatch &s, const void *q, const f
                                     const void *kp, const void *ko, int hq, int hkv, int hd,
                                     const float *wp_prev, float *wp, const float *wo_prev,
                                     float *wo, hipStream_t st) {
-  const int pb = wp ? (s.prefix_len + 255) / 256 : 0, ob = wo ? (s.own_rows + 255) / 256 : 0;
-  const size_t blocks = pb + (size_t)s.n_req * ob;
+  typedef WeightTile<TS> W;
+  const int G = hq / hkv, waves = 8 * gemm_cu_count();  // two per SIMD
+  // waves that share a key tile: more of them while the keys alone do not fill the chip
+  auto share = [&](long long tiles, long long pairs) {
+    int n = 1;
+    while (n < 4 && tiles * n < waves && pairs > W::PAIRS * n) n *= 2;
+    return n;
+  };
+  const long long pt = wp ? (s.prefix_len + W::KEYS - 1) / W::KEYS : 0;
+  const long long ot = wo ? (s.own_rows + W::KEYS - 1) / W::KEYS : 0;
+  WeightPlan p;
+  p.p_walkers = share(pt * hkv, (long long)s.n_rows * G);
+  p.o_walkers = share(ot * s.n_req * hkv, (long long)s.rows_max * G);
+  p.prefix_blocks = (int)((pt * p.p_walkers + 3) / 4) * hkv;
+  p.own_blocks = (int)((ot * p.o_walkers + 3) / 4);
+  const size_t blocks = p.prefix_blocks + (size_t)s.n_req * p.own_blocks * hkv;
   if (blocks == 0) return hipSuccess;
-  hipLaunchKernelGGL(k_attn_weights<TS>, dim3((unsigned)blocks, hkv), dim3(256), 0, st, s,
-                     reinterpret_cast<const TS *>(q), lse, reinterpret_cast<const TS *>(kp),
-                     reinterpret_cast<const TS *>(ko), hq, hkv, hd, 1.0f / sqrtf((float)hd), pb,
-                     ob, wp_prev, wp, wo_prev, wo);
+  const float scale = 1.4426950408889634f / sqrtf((float)hd);
+  auto x = [](const void *a) { return reinterpret_cast<const TS *>(a); };
+#define AKVS_WEIGHTS(HD_)                                                                      \
+  hipLaunchKernelGGL((k_attn_weights<TS, HD_>), dim3((unsigned)blocks), dim3(256), 0, st, s, p, \
+                     x(q), lse, x(kp), x(ko), hq, hkv, scale, wp_prev, wp, wo_prev, wo)
+  if (hd == 128) AKVS_WEIGHTS(128);
+  else AKVS_WEIGHTS(64);
+#undef AKVS_WEIGHTS
   return hipGetLastError();
 }
 
