@@ -1711,8 +1711,10 @@ akvs_status akvs_qk_norm_rope(const void *q, int64_t ldq, const void *k, int64_t
 size_t akvs_shared_workspace_size(const akvs_model_cfg *m, const akvs_shared_cfg *c) {
   SharedBatch s;
   if (check_shared(m, c, &s) != AKVS_OK) return 0;
-  return align256(sizeof(float) *
-                  shared_part_floats(s, m->n_q_heads, m->n_kv_heads, m->head_dim, m->dtype));
+  return align256(
+      sizeof(float) *
+      std::max(shared_part_floats(s, m->n_q_heads, m->n_kv_heads, m->head_dim, m->dtype),
+               weight_part_floats(s, m->n_q_heads, m->n_kv_heads, m->dtype)));
 }
 
 akvs_status akvs_shared_attention(const void *q, const akvs_shared_cfg *c, const void *k_prefix,
@@ -1754,10 +1756,13 @@ akvs_status akvs_attention_weights(const void *q, const float *lse, const akvs_s
               aligned16(w_prefix_prev) && aligned16(w_prefix) && aligned16(w_own_prev) &&
               aligned16(w_own) && aligned16(ws),
           AKVS_EINVAL, "misaligned argument");
+  const size_t need = akvs_shared_workspace_size(m, c);
+  REQUIRE(need == 0 || (ws && ws_bytes >= need), AKVS_ENOSPACE, "workspace %zu < %zu bytes",
+          ws_bytes, need);
   LAUNCH(AKVS_K_ATTENTION,
          launch_attention_weights(s, q, lse, k_prefix, k_own, m->n_q_heads, m->n_kv_heads,
                                   m->head_dim, m->dtype, w_prefix_prev, w_prefix, w_own_prev,
-                                  w_own, stream));
+                                  w_own, reinterpret_cast<float *>(ws), stream));
   return AKVS_OK;
 }
 

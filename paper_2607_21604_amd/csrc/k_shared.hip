@@ -454,13 +454,15 @@ __global__ __launch_bounds__(64) void k_shared_attn(SharedBatch s, const TS *__r
 // Scores again, S = Q K^T, on the matrix cores (bf16: 32x32x16, fp32: 16x16x4), with pairs as
 // rows and keys as columns, so that a lane holds scores of one key: p = exp(s - lse) is summed
 // over pairs inside the lane, and a key's sum never leaves its column. A wave keeps a tile of
-// keys in registers and walks the pair tiles, the next tile's queries in flight; where keys
-// are few, `walkers` waves of a block share a key tile's pairs and are added in order.
+// keys in registers; the pair tiles pass through LDS for the block's four waves, the next one
+// in flight. (Each wave fetching the queries itself was bound by that: 32 rows of 256 bytes
+// are 32 cache lines an instruction; 1070 rows over 4516 keys of 24/8 heads took 162 us.)
+typedef __attribute__((ext_vector_type(4))) int i32x4_t;
 template <typename TS>
 struct WeightTile;
 template <>
 struct WeightTile<bf16_t> {  // 32 pairs x 32 keys; C value i of a lane: row pair(i)
-  static constexpr int PAIRS = 32, KEYS = 32, NC = 16, VE = 8;
+  static constexpr int PAIRS = 32, KEYS = 32, NC = 16;
   typedef f32x16_t Acc;
   __device__ static int pair(int i, int sub) { return (i >> 2) * 8 + sub * 4 + (i & 3); }
   __device__ static Acc mma(u32x4_t q, u32x4_t k, Acc c) {
@@ -470,7 +472,7 @@ struct WeightTile<bf16_t> {  // 32 pairs x 32 keys; C value i of a lane: row pai
 };
 template <>
 struct WeightTile<float> {  // 16 x 16
-  static constexpr int PAIRS = 16, KEYS = 16, NC = 4, VE = 4;
+  static constexpr int PAIRS = 16, KEYS = 16, NC = 4;
   typedef f32x4_t Acc;
   __device__ static int pair(int i, int sub) { return sub * 4 + i; }
   __device__ static Acc mma(u32x4_t q, u32x4_t k, Acc c) {
@@ -482,10 +484,11 @@ struct WeightTile<float> {  // 16 x 16
   }
 };
 
-// Blocks [0, prefix_blocks): (key block, KV head), then (request, key block, KV head) of the own
-// keys; a block's 4 waves are 4 / walkers key tiles by `walkers` waves each.
+// Blocks [0, prefix_blocks): (part, key block, KV head), part: a share of the pair tiles, whose
+// sums go to a buffer of their own where there are several; then (request, key block, KV head)
+// of the own keys.
 struct WeightPlan {
-  int p_walkers, prefix_blocks, o_walkers, own_blocks;
+  int parts, part_pairs, key_blocks, prefix_blocks, own_blocks;
 };
 
 template <typename TS, int HD>
@@ -498,13 +501,17 @@ __global__ __launch_bounds__(256) void k_attn_weights(SharedBatch s, WeightPlan 
                                                       float *wp, const float *wo_prev,
                                                       float *wo) {
   typedef WeightTile<TS> W;
-  constexpr int C = HD / 16;
-  __shared__ float s_lse[4][W::PAIRS];
-  __shared__ int s_seen[4][W::PAIRS];
-  __shared__ float s_sum[4][W::KEYS];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, G = hq / hkv;
-  const int li = lane % W::KEYS, sub = lane / W::KEYS;  // this lane's pair / key, and its part
-  int id = blockIdx.x, r0 = 0, r1, n, n_all, own = 0, walkers;
+  constexpr int NSUB = 64 / W::KEYS;               // lanes that share a row or column
+  constexpr int ROW = HD * sizeof(TS), CPR = ROW / 16, C = CPR / NSUB;
+  constexpr int STRIDE = ROW + 16;                 // fragment reads on all banks
+  constexpr int NCH = W::PAIRS * CPR / 256;        // 16-byte chunks of a tile per thread
+  __shared__ __attribute__((aligned(16))) char s_q[2][W::PAIRS * STRIDE];
+  __shared__ __attribute__((aligned(16))) float s_lse[2][W::PAIRS];
+  __shared__ __attribute__((aligned(16))) int s_seen[2][W::PAIRS];
+  __shared__ int s_masked[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, G = hq / hkv;
+  const int li = lane % W::KEYS, sub = lane / W::KEYS;  // this lane's row / column, and its part
+  int id = blockIdx.x, r0 = 0, r1, n, n_all, own = 0, kb, v0 = 0, n_pairs;
   const TS *K;
   const float *prev;
   float *w;
@@ -513,15 +520,18 @@ __global__ __launch_bounds__(256) void k_attn_weights(SharedBatch s, WeightPlan 
   const int kvh = id % hkv;
   id /= hkv;
   if (prefix) {
+    kb = id % p.key_blocks;
+    const int part = id / p.key_blocks;
     r1 = shared_live(s);
     n = n_all = s.prefix_len;
     K = Kp;
     prev = wp_prev ? wp_prev + (size_t)kvh * n : nullptr;
-    w = wp + (size_t)kvh * n;
-    walkers = p.p_walkers;
+    w = wp + ((size_t)part * hkv + kvh) * n;
+    v0 = part * p.part_pairs;
+    n_pairs = min(r1 * G, v0 + p.part_pairs);
   } else {
     const int b = id / p.own_blocks;
-    id -= b * p.own_blocks;
+    kb = id - b * p.own_blocks;
     shared_rows(s, b, r0, r1);
     n = own = min(max(s.own_len[b], 0), s.own_rows);
     n_all = s.own_rows;
@@ -529,77 +539,101 @@ __global__ __launch_bounds__(256) void k_attn_weights(SharedBatch s, WeightPlan 
     const size_t o = ((size_t)b * hkv + kvh) * n_all;
     prev = wo_prev ? wo_prev + o : nullptr;
     w = wo + o;
-    walkers = p.o_walkers;
+    n_pairs = (r1 - r0) * G;
   }
-  const int j0 = (id * (4 / walkers) + wave / walkers) * W::KEYS, j = j0 + li;
-  const int n_pairs = (r1 - r0) * G;
-  const int step = walkers * W::PAIRS;
+  const int j0 = kb * 4 * W::KEYS, j = j0 + wave * W::KEYS + li;
   float sum = 0.f;
-  int v0 = wave % walkers * W::PAIRS;
   if (j0 < n && v0 < n_pairs) {
-    u32x4_t kf[C], qa[C], qb[C];
-    const TS *k = K + ((size_t)min(j, n - 1) * hkv + kvh) * HD + sub * W::VE;
+    u32x4_t kf[C], qreg[NCH];
+    {
+      const char *k = reinterpret_cast<const char *>(K + ((size_t)min(j, n - 1) * hkv + kvh) * HD);
 #pragma unroll
-    for (int c = 0; c < C; ++c) kf[c] = *reinterpret_cast<const u32x4_t *>(k + c * 16);
-    // the lane's pair of the tile from `at`: its query fragment, its lse (times log2 e) and how
-    // many keys it sees (0: no pair, or a row without keys)
-    auto load = [&](int at, u32x4_t (&q)[C], float &ls, int &seen) __attribute__((always_inline)) {
-      const int v = min(at + li, n_pairs - 1), r = r0 + v / G, h = kvh * G + v % G;
-      const TS *x = Q + ((size_t)r * hq + h) * HD + sub * W::VE;
+      for (int c = 0; c < C; ++c)
+        kf[c] = *reinterpret_cast<const u32x4_t *>(k + (c * NSUB + sub) * 16);
+    }
+    // one tile of queries; the first threads have a pair's lse and how many keys it sees (0: no
+    // pair, or a row without keys)
+    float ls = 0.f;
+    int seen = 0;
+    auto load = [&](int at) __attribute__((always_inline)) {
 #pragma unroll
-      for (int c = 0; c < C; ++c) q[c] = *reinterpret_cast<const u32x4_t *>(x + c * 16);
-      ls = lse[(size_t)r * hq + h];
-      seen = at + li >= n_pairs || ls == -INFINITY ? 0 : prefix ? n : min(max(own - (r1 - r) + 1, 0), n);
-      ls *= 1.4426950408889634f;
-    };
-    auto weigh = [&](const u32x4_t (&q)[C], float ls, int seen) __attribute__((always_inline)) {
-      if (sub == 0) {
-        s_lse[wave][li] = ls;
-        s_seen[wave][li] = seen;
+      for (int i = 0; i < NCH; ++i) {
+        const int c = tid + 256 * i, v = min(at + c / CPR, n_pairs - 1), r = r0 + v / G;
+        const TS *x = Q + ((size_t)r * hq + kvh * G + v % G) * HD;
+        qreg[i] = *reinterpret_cast<const u32x4_t *>(reinterpret_cast<const char *>(x) +
+                                                     c % CPR * 16);
       }
+      if (tid < W::PAIRS) {
+        const int v = min(at + tid, n_pairs - 1), r = r0 + v / G;
+        ls = lse[(size_t)r * hq + kvh * G + v % G];
+        seen = at + tid >= n_pairs ? 0 : prefix ? n : min(max(own - (r1 - r) + 1, 0), n);
+      }
+    };
+    auto store = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        const int c = tid + 256 * i;
+        *reinterpret_cast<u32x4_t *>(&s_q[buf][c / CPR * STRIDE + c % CPR * 16]) = qreg[i];
+      }
+      if (tid < W::PAIRS) {
+        if (ls == -INFINITY) seen = 0;
+        s_lse[buf][tid] = ls * 1.4426950408889634f;
+        s_seen[buf][tid] = seen;
+        const bool any = __ballot(seen < min(j0 + 4 * W::KEYS, n)) != 0;
+        if (tid == 0) s_masked[buf] = any;
+      }
+    };
+    load(v0);
+    store(0);
+    __syncthreads();
+    for (int buf = 0; v0 < n_pairs; v0 += W::PAIRS, buf ^= 1) {
+      const bool more = v0 + W::PAIRS < n_pairs;
+      if (more) load(v0 + W::PAIRS);
       typename W::Acc c;
 #pragma unroll
       for (int i = 0; i < W::NC; ++i) c[i] = 0.f;
+      const char *q = &s_q[buf][li * STRIDE + sub * 16];
 #pragma unroll
-      for (int e = 0; e < C; ++e) c = W::mma(q[e], kf[e], c);
-      // (a wave's LDS accesses stay in order)
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      const bool masked = __ballot(seen < min(j0 + W::KEYS, n)) != 0;
-      float add = 0.f;
+      for (int e = 0; e < C; ++e)
+        c = W::mma(*reinterpret_cast<const u32x4_t *>(q + e * NSUB * 16), kf[e], c);
+      float x[W::NC];
 #pragma unroll
-      for (int i = 0; i < W::NC; ++i) {
-        const int m = W::pair(i, sub);
-        const float e = __builtin_amdgcn_exp2f(fmaf(c[i], scale_log2, -s_lse[wave][m]));
-        add += masked && j >= s_seen[wave][m] ? 0.f : e;
+      for (int i = 0; i < W::NC / 4; ++i) {
+        const f32x4_t off = *reinterpret_cast<const f32x4_t *>(&s_lse[buf][W::pair(4 * i, sub)]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          x[4 * i + e] = __builtin_amdgcn_exp2f(fmaf(c[4 * i + e], scale_log2, -off[e]));
       }
-      sum += add;
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-    };
-    float la, lb;
-    int sa, sb;
-    load(v0, qa, la, sa);
-    while (true) {
-      if (v0 + step < n_pairs) load(v0 + step, qb, lb, sb);
-      weigh(qa, la, sa);
-      v0 += step;
-      if (v0 >= n_pairs) break;
-      if (v0 + step < n_pairs) load(v0 + step, qa, la, sa);
-      weigh(qb, lb, sb);
-      v0 += step;
-      if (v0 >= n_pairs) break;
+      if (s_masked[buf]) {
+#pragma unroll
+        for (int i = 0; i < W::NC / 4; ++i) {
+          const i32x4_t end = *reinterpret_cast<const i32x4_t *>(&s_seen[buf][W::pair(4 * i, sub)]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[4 * i + e] = j < end[e] ? x[4 * i + e] : 0.f;
+        }
+      }
+#pragma unroll
+      for (int o = W::NC / 2; o > 0; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < o; ++i) x[i] += x[i + o];
+      sum += x[0];
+      if (more) store(buf ^ 1);
+      __syncthreads();
     }
 #pragma unroll
     for (int o = W::KEYS; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
   }
-  if (walkers > 1) {
-    if (sub == 0) s_sum[wave][li] = sum;
-    __syncthreads();
-    if (wave % walkers) return;
-    for (int q = 1; q < walkers; ++q) sum += s_sum[wave + q][li];
-  }
   if (sub == 0 && j < n_all) w[j] = (prev ? prev[j] : 0.f) + (j < n ? sum : 0.f);
+}
+
+// w = prev + the parts' sums in order.
+__global__ __launch_bounds__(256) void k_weight_parts(const float *__restrict__ part, int parts,
+                                                      size_t n, const float *prev, float *w) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  float sum = part[i];
+  for (int q = 1; q < parts; ++q) sum += part[q * n + i];
+  w[i] = (prev ? prev[i] : 0.f) + sum;
 }
 
 // Items of a call (bf16).
@@ -687,47 +721,66 @@ hipError_t launch_shared_attention(const SharedBatch &s, const void *q, const vo
                    : shared_bf16<64>(s, q, kp, vp, ko, vo, hq, hkv, out, lse, part, st);
 }
 
+// The pairs go in parts while the keys alone do not make four blocks a compute unit (a block's
+// four waves wait for LDS and exponentials in turn), at least four tiles each.
+template <typename TS>
+static WeightPlan weight_plan(const SharedBatch &s, int hq, int hkv, bool prefix, bool own) {
+  typedef WeightTile<TS> W;
+  WeightPlan p;
+  p.key_blocks = prefix ? (s.prefix_len + 4 * W::KEYS - 1) / (4 * W::KEYS) : 0;
+  p.own_blocks = own ? (s.own_rows + 4 * W::KEYS - 1) / (4 * W::KEYS) : 0;
+  const int tiles = (int)(((long long)s.n_rows * (hq / hkv) + W::PAIRS - 1) / W::PAIRS);
+  const long long blocks = std::max(1LL, (long long)p.key_blocks * hkv);
+  long long parts = std::max(1LL, 4LL * gemm_cu_count() / blocks);
+  parts = std::min<long long>(parts, std::max(1, tiles / 4));
+  const int per = tiles ? (int)((tiles + parts - 1) / parts) : 1;
+  p.parts = tiles ? (tiles + per - 1) / per : 1;
+  p.part_pairs = per * W::PAIRS;
+  p.prefix_blocks = p.parts * p.key_blocks * hkv;
+  return p;
+}
+
+size_t weight_part_floats(const SharedBatch &s, int hq, int hkv, int dtype) {
+  const WeightPlan p = dtype == AKVS_BF16 ? weight_plan<bf16_t>(s, hq, hkv, true, true)
+                                          : weight_plan<float>(s, hq, hkv, true, true);
+  return p.parts > 1 ? (size_t)p.parts * hkv * s.prefix_len : 0;
+}
+
 template <typename TS>
 static hipError_t attention_weights(const SharedBatch &s, const void *q, const float *lse,
                                     const void *kp, const void *ko, int hq, int hkv, int hd,
                                     const float *wp_prev, float *wp, const float *wo_prev,
-                                    float *wo, hipStream_t st) {
-  typedef WeightTile<TS> W;
-  const int G = hq / hkv, waves = 8 * gemm_cu_count();  // two per SIMD
-  // waves that share a key tile: more of them while the keys alone do not fill the chip
-  auto share = [&](long long tiles, long long pairs) {
-    int n = 1;
-    while (n < 4 && tiles * n < waves && pairs > W::PAIRS * n) n *= 2;
-    return n;
-  };
-  const long long pt = wp ? (s.prefix_len + W::KEYS - 1) / W::KEYS : 0;
-  const long long ot = wo ? (s.own_rows + W::KEYS - 1) / W::KEYS : 0;
-  WeightPlan p;
-  p.p_walkers = share(pt * hkv, (long long)s.n_rows * G);
-  p.o_walkers = share(ot * s.n_req * hkv, (long long)s.rows_max * G);
-  p.prefix_blocks = (int)((pt * p.p_walkers + 3) / 4) * hkv;
-  p.own_blocks = (int)((ot * p.o_walkers + 3) / 4);
+                                    float *wo, float *part, hipStream_t st) {
+  const WeightPlan p = weight_plan<TS>(s, hq, hkv, wp != nullptr, wo != nullptr);
   const size_t blocks = p.prefix_blocks + (size_t)s.n_req * p.own_blocks * hkv;
   if (blocks == 0) return hipSuccess;
+  const bool split = p.parts > 1 && p.prefix_blocks > 0;
   const float scale = 1.4426950408889634f / sqrtf((float)hd);
   auto x = [](const void *a) { return reinterpret_cast<const TS *>(a); };
 #define AKVS_WEIGHTS(HD_)                                                                      \
   hipLaunchKernelGGL((k_attn_weights<TS, HD_>), dim3((unsigned)blocks), dim3(256), 0, st, s, p, \
-                     x(q), lse, x(kp), x(ko), hq, hkv, scale, wp_prev, wp, wo_prev, wo)
+                     x(q), lse, x(kp), x(ko), hq, hkv, scale, split ? nullptr : wp_prev,        \
+                     split ? part : wp, wo_prev, wo)
   if (hd == 128) AKVS_WEIGHTS(128);
   else AKVS_WEIGHTS(64);
 #undef AKVS_WEIGHTS
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !split) return e;
+  const size_t n = (size_t)hkv * s.prefix_len;
+  hipLaunchKernelGGL(k_weight_parts, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, part,
+                     p.parts, n, wp_prev, wp);
   return hipGetLastError();
 }
 
 hipError_t launch_attention_weights(const SharedBatch &s, const void *q, const float *lse,
                                     const void *kp, const void *ko, int hq, int hkv, int hd,
                                     int dtype, const float *wp_prev, float *wp,
-                                    const float *wo_prev, float *wo, hipStream_t st) {
+                                    const float *wo_prev, float *wo, float *part,
+                                    hipStream_t st) {
   return dtype == AKVS_BF16 ? attention_weights<bf16_t>(s, q, lse, kp, ko, hq, hkv, hd, wp_prev, wp,
-                                                        wo_prev, wo, st)
+                                                        wo_prev, wo, part, st)
                             : attention_weights<float>(s, q, lse, kp, ko, hq, hkv, hd, wp_prev, wp,
-                                                       wo_prev, wo, st);
+                                                       wo_prev, wo, part, st);
 }
 
 }  // namespace akvs

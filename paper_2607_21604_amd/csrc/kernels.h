@@ -217,7 +217,10 @@ size_t shared_part_floats(const SharedBatch &s, int hq, int hkv, int hd, int dty
 hipError_t launch_attention_weights(const SharedBatch &s, const void *q, const float *lse,
                                     const void *kp, const void *ko, int hq, int hkv, int hd,
                                     int dtype, const float *wp_prev, float *wp,
-                                    const float *wo_prev, float *wo, hipStream_t st);
+                                    const float *wo_prev, float *wo, float *part,
+                                    hipStream_t st);
+// floats of `part` (sums of shares of the rows) that launch_attention_weights needs
+size_t weight_part_floats(const SharedBatch &s, int hq, int hkv, int dtype);
 // ---- k_evict.hip ----------------------------------------------------------------------
 struct EvictArgs {
   int n_seq, n_keys, src_rows, n_keep, dst_rows, n_first, n_recent;
