@@ -488,10 +488,11 @@ struct WeightTile<float> {  // 16 x 16
 // sums go to a buffer of their own where there are several; then (request, key block, KV head)
 // of the own keys.
 struct WeightPlan {
-  int parts, part_pairs, key_blocks, prefix_blocks, own_blocks;
+  int nk, parts, part_pairs, key_blocks, prefix_blocks, own_blocks;
 };
 
-template <typename TS, int HD>
+// NK: key tiles of a wave. Two halve the LDS reads of a pair tile, which bound long walks.
+template <typename TS, int HD, int NK>
 __global__ __launch_bounds__(256) void k_attn_weights(SharedBatch s, WeightPlan p,
                                                       const TS *__restrict__ Q,
                                                       const float *__restrict__ lse,
@@ -541,89 +542,144 @@ __global__ __launch_bounds__(256) void k_attn_weights(SharedBatch s, WeightPlan 
     w = wo + o;
     n_pairs = (r1 - r0) * G;
   }
-  const int j0 = kb * 4 * W::KEYS, j = j0 + wave * W::KEYS + li;
-  float sum = 0.f;
+  constexpr int KEYS = NK * W::KEYS;  // of a wave
+  const int j0 = kb * 4 * KEYS, j = j0 + wave * KEYS + li;
+  float sum[NK];
+#pragma unroll
+  for (int u = 0; u < NK; ++u) sum[u] = 0.f;
   if (j0 < n && v0 < n_pairs) {
-    u32x4_t kf[C], qreg[NCH];
-    {
-      const char *k = reinterpret_cast<const char *>(K + ((size_t)min(j, n - 1) * hkv + kvh) * HD);
+    u32x4_t kf[NK][C];
+#pragma unroll
+    for (int u = 0; u < NK; ++u) {
+      const char *k = reinterpret_cast<const char *>(
+          K + ((size_t)min(j + u * W::KEYS, n - 1) * hkv + kvh) * HD);
 #pragma unroll
       for (int c = 0; c < C; ++c)
-        kf[c] = *reinterpret_cast<const u32x4_t *>(k + (c * NSUB + sub) * 16);
+        kf[u][c] = *reinterpret_cast<const u32x4_t *>(k + (c * NSUB + sub) * 16);
     }
-    // one tile of queries; the first threads have a pair's lse and how many keys it sees (0: no
-    // pair, or a row without keys)
-    float ls = 0.f;
-    int seen = 0;
-    auto load = [&](int at) __attribute__((always_inline)) {
+    // This thread's chunks of a tile belong to pairs that are PAIRS apart from one tile to the
+    // next: their places (in query heads) are carried along, without a division per tile. The
+    // first threads have a pair's lse and how many keys it sees (0: no pair, or a row without
+    // keys).
+    const int dr = W::PAIRS / G, dg = W::PAIRS % G, last = (r1 - 1) * hq + kvh * G + G - 1;
+    struct Pair {
+      int g, at;  // head of the KV head's G, place in [n_rows][hq]
+    };
+    auto pair_at = [&](int v) { return Pair{v % G, (r0 + v / G) * hq + kvh * G + v % G}; };
+    auto next = [&](Pair &x) __attribute__((always_inline)) {
+      const bool wrap = x.g + dg >= G;
+      x.g += wrap ? dg - G : dg;
+      x.at += dr * hq + dg + (wrap ? hq - G : 0);
+    };
+    Pair mine[NCH], first = pair_at(v0 + tid % W::PAIRS);
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) mine[i] = pair_at(v0 + (tid + 256 * i) / CPR);
+    int row = r0 + (v0 + tid % W::PAIRS) / G;  // of `first`
+    struct Tile {
+      u32x4_t q[NCH];
+      float ls;
+      int seen;
+    };
+    auto load = [&](Tile &x) __attribute__((always_inline)) {  // (past the end: the last pair)
 #pragma unroll
       for (int i = 0; i < NCH; ++i) {
-        const int c = tid + 256 * i, v = min(at + c / CPR, n_pairs - 1), r = r0 + v / G;
-        const TS *x = Q + ((size_t)r * hq + kvh * G + v % G) * HD;
-        qreg[i] = *reinterpret_cast<const u32x4_t *>(reinterpret_cast<const char *>(x) +
-                                                     c % CPR * 16);
+        const char *a = reinterpret_cast<const char *>(Q + (size_t)min(mine[i].at, last) * HD);
+        x.q[i] = *reinterpret_cast<const u32x4_t *>(a + (tid + 256 * i) % CPR * 16);
+        next(mine[i]);
       }
-      if (tid < W::PAIRS) {
-        const int v = min(at + tid, n_pairs - 1), r = r0 + v / G;
-        ls = lse[(size_t)r * hq + kvh * G + v % G];
-        seen = at + tid >= n_pairs ? 0 : prefix ? n : min(max(own - (r1 - r) + 1, 0), n);
-      }
+      x.ls = lse[min(first.at, last)];
+      x.seen = row >= r1 ? 0 : prefix ? n : min(max(own - (r1 - row) + 1, 0), n);
+      row += dr + (first.g + dg >= G);
+      next(first);
     };
-    auto store = [&](int buf) __attribute__((always_inline)) {
+    auto store = [&](const Tile &x, int buf) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < NCH; ++i) {
         const int c = tid + 256 * i;
-        *reinterpret_cast<u32x4_t *>(&s_q[buf][c / CPR * STRIDE + c % CPR * 16]) = qreg[i];
+        *reinterpret_cast<u32x4_t *>(&s_q[buf][c / CPR * STRIDE + c % CPR * 16]) = x.q[i];
       }
       if (tid < W::PAIRS) {
-        if (ls == -INFINITY) seen = 0;
-        s_lse[buf][tid] = ls * 1.4426950408889634f;
+        const int seen = x.ls == -INFINITY ? 0 : x.seen;
+        s_lse[buf][tid] = x.ls * 1.4426950408889634f;
         s_seen[buf][tid] = seen;
-        const bool any = __ballot(seen < min(j0 + 4 * W::KEYS, n)) != 0;
+        const bool any = __ballot(seen < min(j0 + 4 * KEYS, n)) != 0;
         if (tid == 0) s_masked[buf] = any;
       }
     };
-    load(v0);
-    store(0);
-    __syncthreads();
-    for (int buf = 0; v0 < n_pairs; v0 += W::PAIRS, buf ^= 1) {
-      const bool more = v0 + W::PAIRS < n_pairs;
-      if (more) load(v0 + W::PAIRS);
-      typename W::Acc c;
+    auto weigh = [&](int buf) __attribute__((always_inline)) {
+      typename W::Acc c[NK];
 #pragma unroll
-      for (int i = 0; i < W::NC; ++i) c[i] = 0.f;
+      for (int u = 0; u < NK; ++u)
+#pragma unroll
+        for (int i = 0; i < W::NC; ++i) c[u][i] = 0.f;
       const char *q = &s_q[buf][li * STRIDE + sub * 16];
 #pragma unroll
-      for (int e = 0; e < C; ++e)
-        c = W::mma(*reinterpret_cast<const u32x4_t *>(q + e * NSUB * 16), kf[e], c);
-      float x[W::NC];
+      for (int e = 0; e < C; ++e) {
+        const u32x4_t x = *reinterpret_cast<const u32x4_t *>(q + e * NSUB * 16);
+#pragma unroll
+        for (int u = 0; u < NK; ++u) c[u] = W::mma(x, kf[u][e], c[u]);
+      }
+      float x[NK][W::NC];
 #pragma unroll
       for (int i = 0; i < W::NC / 4; ++i) {
         const f32x4_t off = *reinterpret_cast<const f32x4_t *>(&s_lse[buf][W::pair(4 * i, sub)]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          x[4 * i + e] = __builtin_amdgcn_exp2f(fmaf(c[4 * i + e], scale_log2, -off[e]));
+        for (int u = 0; u < NK; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            x[u][4 * i + e] =
+                __builtin_amdgcn_exp2f(fmaf(c[u][4 * i + e], scale_log2, -off[e]));
       }
       if (s_masked[buf]) {
 #pragma unroll
         for (int i = 0; i < W::NC / 4; ++i) {
           const i32x4_t end = *reinterpret_cast<const i32x4_t *>(&s_seen[buf][W::pair(4 * i, sub)]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[4 * i + e] = j < end[e] ? x[4 * i + e] : 0.f;
+          for (int u = 0; u < NK; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              x[u][4 * i + e] = j + u * W::KEYS < end[e] ? x[u][4 * i + e] : 0.f;
         }
       }
 #pragma unroll
-      for (int o = W::NC / 2; o > 0; o >>= 1)
+      for (int u = 0; u < NK; ++u) {
 #pragma unroll
-        for (int i = 0; i < o; ++i) x[i] += x[i + o];
-      sum += x[0];
-      if (more) store(buf ^ 1);
+        for (int o = W::NC / 2; o > 0; o >>= 1)
+#pragma unroll
+          for (int i = 0; i < o; ++i) x[u][i] += x[u][i + o];
+        sum[u] += x[u][0];
+      }
+    };
+    // Loads run two tiles ahead, in registers, and are made whether or not there is a tile: a
+    // block alone on its compute unit is else bound by their latency (2 requests of 98 rows
+    // over 506 keys of 40/8 heads: see the figures below).
+    Tile a, b;
+    load(a);
+    load(b);
+    store(a, 0);
+    __syncthreads();
+    while (true) {
+      load(a);
+      weigh(0);
+      v0 += W::PAIRS;
+      if (v0 >= n_pairs) break;
+      store(b, 1);
+      __syncthreads();
+      load(b);
+      weigh(1);
+      v0 += W::PAIRS;
+      if (v0 >= n_pairs) break;
+      store(a, 0);
       __syncthreads();
     }
-#pragma unroll
-    for (int o = W::KEYS; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
   }
-  if (sub == 0 && j < n_all) w[j] = (prev ? prev[j] : 0.f) + (j < n ? sum : 0.f);
+#pragma unroll
+  for (int u = 0; u < NK; ++u) {
+#pragma unroll
+    for (int o = W::KEYS; o < 64; o <<= 1) sum[u] += __shfl_xor(sum[u], o, 64);
+    const int k = j + u * W::KEYS;
+    if (sub == 0 && k < n_all) w[k] = (prev ? prev[k] : 0.f) + (k < n ? sum[u] : 0.f);
+  }
 }
 
 // w = prev + the parts' sums in order.
@@ -721,17 +777,24 @@ hipError_t launch_shared_attention(const SharedBatch &s, const void *q, const vo
                    : shared_bf16<64>(s, q, kp, vp, ko, vo, hq, hkv, out, lse, part, st);
 }
 
-// The pairs go in parts while the keys alone do not make four blocks a compute unit (a block's
-// four waves wait for LDS and exponentials in turn), at least four tiles each.
+// Two key tiles a wave share a pair tile's staging and LDS reads, but a block then takes 192
+// registers (two a compute unit) and 256 keys: taken where the prefix makes two such blocks a
+// unit by parts of eight tiles (1070 rows over 4516 keys of 24/8 heads: 58 us with one, 49 with
+// two; 195 rows over 506 keys of 40/8 heads: 19 and 25). The pairs go in parts while the keys
+// alone do not fill the units, at least four tiles each.
 template <typename TS>
 static WeightPlan weight_plan(const SharedBatch &s, int hq, int hkv, bool prefix, bool own) {
   typedef WeightTile<TS> W;
   WeightPlan p;
-  p.key_blocks = prefix ? (s.prefix_len + 4 * W::KEYS - 1) / (4 * W::KEYS) : 0;
-  p.own_blocks = own ? (s.own_rows + 4 * W::KEYS - 1) / (4 * W::KEYS) : 0;
+  const int cus = gemm_cu_count();
   const int tiles = (int)(((long long)s.n_rows * (hq / hkv) + W::PAIRS - 1) / W::PAIRS);
+  const long long wide = (s.prefix_len + 8 * W::KEYS - 1) / (8 * W::KEYS);
+  p.nk = wide * hkv * (tiles / 8) >= 2 * cus ? 2 : 1;
+  const int keys = 4 * W::KEYS * p.nk;
+  p.key_blocks = prefix ? (s.prefix_len + keys - 1) / keys : 0;
+  p.own_blocks = own ? (s.own_rows + keys - 1) / keys : 0;
   const long long blocks = std::max(1LL, (long long)p.key_blocks * hkv);
-  long long parts = std::max(1LL, 4LL * gemm_cu_count() / blocks);
+  long long parts = std::max(1LL, (p.nk == 2 ? 2LL : 4LL) * cus / blocks);
   parts = std::min<long long>(parts, std::max(1, tiles / 4));
   const int per = tiles ? (int)((tiles + parts - 1) / parts) : 1;
   p.parts = tiles ? (tiles + per - 1) / per : 1;
@@ -757,12 +820,15 @@ static hipError_t attention_weights(const SharedBatch &s, const void *q, const f
   const bool split = p.parts > 1 && p.prefix_blocks > 0;
   const float scale = 1.4426950408889634f / sqrtf((float)hd);
   auto x = [](const void *a) { return reinterpret_cast<const TS *>(a); };
-#define AKVS_WEIGHTS(HD_)                                                                      \
-  hipLaunchKernelGGL((k_attn_weights<TS, HD_>), dim3((unsigned)blocks), dim3(256), 0, st, s, p, \
+#define AKVS_WEIGHTS(HD_, NK_)                                                                 \
+  hipLaunchKernelGGL((k_attn_weights<TS, HD_, NK_>), dim3((unsigned)blocks), dim3(256), 0, st, s, p, \
                      x(q), lse, x(kp), x(ko), hq, hkv, scale, split ? nullptr : wp_prev,        \
                      split ? part : wp, wo_prev, wo)
-  if (hd == 128) AKVS_WEIGHTS(128);
-  else AKVS_WEIGHTS(64);
+  if (hd == 128) {
+    if (p.nk == 2) AKVS_WEIGHTS(128, 2); else AKVS_WEIGHTS(128, 1);
+  } else {
+    if (p.nk == 2) AKVS_WEIGHTS(64, 2); else AKVS_WEIGHTS(64, 1);
+  }
 #undef AKVS_WEIGHTS
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !split) return e;
