@@ -199,12 +199,13 @@ def int_ptr(t: Optional[torch.Tensor], least: int):
 def rows_ptr(t: torch.Tensor):
     """(pointer, elements between rows) of rows that are dense but may lie apart, as the
     columns of a packed projection output do."""
-    n, width = t.shape[0], 1
-    for size, step in zip(t.shape[:0:-1], t.stride()[:0:-1]):
-        if size != 1 and step != width:
+    shape, stride = t.shape, t.stride()
+    width = 1
+    for i in range(len(shape) - 1, 0, -1):
+        if stride[i] != width and shape[i] != 1:
             raise ValueError("each row must be contiguous")
-        width *= size
-    return t.data_ptr(), t.stride(0) if n > 1 else width
+        width *= shape[i]
+    return t.data_ptr(), stride[0] if shape[0] > 1 else width
 
 
 # The current stream's handle without building a torch.cuda.Stream object for it (3.1 us a

@@ -30,16 +30,16 @@ __device__ __forceinline__ int shared_live(const SharedBatch &s) {
 // innermost, so that the blocks streaming one head's keys share an XCD's L2; then (request,
 // chunk, pair tile, KV head) of the own keys.
 struct SharedPlan {
-  int p_groups, p_tiles, splits, split_keys, prefix_blocks;  // groups: 32-pair groups of a tile
-  int o_groups, o_tiles, chunks, chunk_keys;
+  int p_pairs, p_tiles, splits, split_keys, prefix_blocks;  // pairs of a tile, tiles, ..
+  int o_pairs, o_tiles, chunks, chunk_keys;
   int slots;  // partials per (row, head): splits + chunks
 };
 constexpr int SH_TILE = 64;  // keys of an LDS tile
 
-// The item that a block serves: pairs v0 .. of rows [r0, r1), keys [k0, k1) of (K, V) rows from
+// The item that a block serves: `pairs` pairs from v0 of rows [r0, r1), keys [k0, k1) of (K, V) rows from
 // `base`. own = -1: prefix (every row sees all of it), else the request's own keys.
 struct SharedItem {
-  int kvh, r0, r1, v0, groups, k0, k1, slot, own;
+  int kvh, r0, r1, v0, pairs, k0, k1, slot, own;
   size_t base;
 };
 __device__ __forceinline__ bool shared_item(const SharedBatch &s, const SharedPlan &p, int hkv,
@@ -51,8 +51,8 @@ __device__ __forceinline__ bool shared_item(const SharedBatch &s, const SharedPl
   id /= hkv;
   if (prefix) {
     const int tile = id % p.p_tiles, split = id / p.p_tiles;
-    it.groups = p.p_groups;
-    it.v0 = tile * 32 * it.groups;
+    it.pairs = p.p_pairs;
+    it.v0 = tile * it.pairs;
     it.r0 = 0;
     it.r1 = shared_live(s);
     it.k0 = split * p.split_keys;
@@ -64,8 +64,8 @@ __device__ __forceinline__ bool shared_item(const SharedBatch &s, const SharedPl
     const int tile = id % p.o_tiles;
     id /= p.o_tiles;
     const int chunk = id % p.chunks, b = id / p.chunks;
-    it.groups = p.o_groups;
-    it.v0 = tile * 32 * it.groups;
+    it.pairs = p.o_pairs;
+    it.v0 = tile * it.pairs;
     shared_rows(s, b, it.r0, it.r1);
     it.own = min(max(s.own_len[b], 0), s.own_rows);
     it.k0 = chunk * p.chunk_keys;
@@ -109,9 +109,10 @@ __global__ __launch_bounds__(256, 2) void k_shared_bf16(
   if (!shared_item(s, p, hkv, G, it)) return;
   const bf16_t *K = it.own < 0 ? Kp : Ko, *V = it.own < 0 ? Vp : Vo;
   // this wave's pairs and its share of a tile's two 32-key halves
-  const int group = it.groups == 4 ? wave : it.groups == 2 ? wave >> 1 : 0;
-  const bool works = it.groups > 1 || wave < 2;
-  const int st0 = it.groups == 4 ? 0 : wave & 1, st_step = it.groups == 4 ? 1 : 2;
+  const int groups = it.pairs >> 5;
+  const int group = groups == 4 ? wave : groups == 2 ? wave >> 1 : 0;
+  const bool works = groups > 1 || wave < 2;
+  const int st0 = groups == 4 ? 0 : wave & 1, st_step = groups == 4 ? 1 : 2;
   const int n_pairs = (it.r1 - it.r0) * G;
   const int v = it.v0 + group * 32 + (lane & 31);
   const bool valid = v < n_pairs;
@@ -119,11 +120,11 @@ __global__ __launch_bounds__(256, 2) void k_shared_bf16(
   const int seen = valid ? shared_seen(it, r) : 0;
   // what the tile's last and first rows see: keys past the one are not read, keys up to the
   // other need no mask
-  const int last = min(n_pairs, it.v0 + 32 * it.groups) - 1;
+  const int last = min(n_pairs, it.v0 + it.pairs) - 1;
   const int k1 = shared_seen(it, it.r0 + last / G), all_see = shared_seen(it, it.r0 + it.v0 / G);
   const size_t prow = ((size_t)it.slot * s.n_rows + r) * hq + head;
   const int nkt = k1 > it.k0 ? (k1 - it.k0 + SH_TILE - 1) / SH_TILE : 0;
-  const bool writes = valid && (it.groups == 4 || (works && (wave & 1) == 0));
+  const bool writes = valid && (groups == 4 || (works && (wave & 1) == 0));
   if (nkt == 0 && p.slots > 1) {
     if (writes && hi == 0) part_ml[prow] = make_float2(-INFINITY, 0.f);
     return;
@@ -257,7 +258,7 @@ __global__ __launch_bounds__(256, 2) void k_shared_bf16(
     __syncthreads();
   }
   float l = l_run + __shfl_xor(l_run, 32, 64);
-  if (it.groups < 4) {  // the two waves of a group: the odd one hands over through LDS
+  if (groups < 4) {  // the two waves of a group: the odd one hands over through LDS
     float *x = reinterpret_cast<float *>(s_kv) + group * (HD / 2 + 2) * 64 + lane;
     if (works && (wave & 1)) {
 #pragma unroll
@@ -383,71 +384,185 @@ __global__ __launch_bounds__(256) void k_shared_merge(SharedBatch s, int slots, 
     lse[item] = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m * 0.6931471805599453f) + logf(l);
 }
 
-// A wave per (row, query head): a lane per key for the scores, a lane per dim (or two) for the
-// values.
-template <typename TS>
-__global__ __launch_bounds__(64) void k_shared_attn(SharedBatch s, const TS *__restrict__ Q,
-                                                    const TS *__restrict__ Kp,
-                                                    const TS *__restrict__ Vp,
-                                                    const TS *__restrict__ Ko,
-                                                    const TS *__restrict__ Vo, int hq, int hkv,
-                                                    int hd, float scale_log2,
-                                                    TS *__restrict__ out, float *lse) {
-  const int lane = threadIdx.x, r = blockIdx.x / hq, h = blockIdx.x % hq, kvh = h / (hq / hkv);
-  if (r >= shared_live(s)) return;
-  int b = 0;
-  if (s.row_start) {
-    int lo = 0, hi = s.n_req - 1;  // the last request that starts at or before r
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (s.row_start[mid] <= r) lo = mid;
-      else hi = mid - 1;
-    }
-    b = lo;
-  } else {
-    b = r / s.rows_max;
+__device__ __forceinline__ bool odd_f32(float x) {
+  return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u;
+}
+
+// fp32, on v_mfma_f32_16x16x4_f32. Block = 16 pairs; its waves take the 16-key tiles of the
+// item's range in turn, each with its own maximum, sum and output, merged through LDS in wave
+// order at the end, so that the loop has no barrier; keys and values come straight to
+// registers, a tile ahead. Scores are formed transposed: lane l holds the scores of pair l % 16
+// at keys 4 (l / 16) + 0..3 of the tile, the operand layout of O^T = V^T P^T as it is; row
+// l % 16 of V^T block c stands for dim (l % 16) * C + c, so that a lane's values are contiguous.
+template <int HD>
+__global__ __launch_bounds__(256, 2) void k_shared_f32(
+    SharedBatch s, SharedPlan p, const float *__restrict__ Q, const float *__restrict__ Kp,
+    const float *__restrict__ Vp, const float *__restrict__ Ko, const float *__restrict__ Vo,
+    int hq, int hkv, float scale_log2, float *__restrict__ out, float *__restrict__ lse,
+    float *__restrict__ part_o, float2 *__restrict__ part_ml) {
+  constexpr int C = HD / 16, NW = 4;
+  __shared__ float s_o[NW][HD][17];
+  __shared__ float s_m[NW][16], s_l[NW][16];
+  __shared__ int s_odd;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int lr = lane & 15, lg = lane >> 4, G = hq / hkv;
+  SharedItem it;
+  if (!shared_item(s, p, hkv, G, it)) return;
+  const float *K = it.own < 0 ? Kp : Ko, *V = it.own < 0 ? Vp : Vo;
+  const int n_pairs = (it.r1 - it.r0) * G, v = it.v0 + lr;
+  const bool valid = v < n_pairs;
+  const int r = it.r0 + (valid ? v : it.v0) / G, head = it.kvh * G + (valid ? v : it.v0) % G;
+  const int seen = valid ? shared_seen(it, r) : 0;
+  const int last = min(n_pairs, it.v0 + 16) - 1;
+  const int k1 = shared_seen(it, it.r0 + last / G), all_see = shared_seen(it, it.r0 + it.v0 / G);
+  if (k1 <= it.k0 && p.slots > 1) {
+    if (tid < 16 && valid)
+      part_ml[((size_t)it.slot * s.n_rows + r) * hq + head] = make_float2(-INFINITY, 0.f);
+    return;
   }
-  int r0, r1;
-  shared_rows(s, b, r0, r1);
-  const int own = s.own_rows ? min(max(s.own_len[b], 0), s.own_rows) : 0;
-  const int seen = min(max(own - (r1 - r0) + (r - r0) + 1, 0), own);
-  const TS *q = Q + ((size_t)r * hq + h) * hd;
-  float m = -INFINITY, l = 0.f, o[2] = {0.f, 0.f};
-  for (int part = 0; part < 2; ++part) {
-    const int n = part ? seen : s.prefix_len;
-    const size_t base = part ? (size_t)b * s.own_rows : 0;
-    const TS *K = part ? Ko : Kp, *V = part ? Vo : Vp;
-    for (int k0 = 0; k0 < n; k0 += 64) {
-      const int k = min(k0 + lane, n - 1);
-      float sc = 0.f;
-      for (int d = 0; d < hd; d += 8) {
-        float a[8], c[8];
-        load8(q + d, a);
-        load8(K + ((base + k) * hkv + kvh) * hd + d, c);
+  if (tid == 0) s_odd = 0;
+  __syncthreads();
+  f32x4_t qf[C], o[C];
+  {
+    const float *q = Q + ((size_t)r * hq + head) * HD + lg * 4;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sc = fmaf(a[i], c[i], sc);
+    for (int c = 0; c < C; ++c) qf[c] = *reinterpret_cast<const f32x4_t *>(q + 16 * c);
+  }
+  const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int c = 0; c < C; ++c) o[c] = zero;
+  float m = -INFINITY, l = 0.f;  // of pair lr (l: this lane's quarter of the keys)
+  struct Tile {
+    f32x4_t k[C];
+    float v[4][C];
+  };
+  auto fetch = [&](Tile &t, int key0) __attribute__((always_inline)) {  // past k1: the last key
+    const float *k = K + ((it.base + min(key0 + lr, k1 - 1)) * hkv + it.kvh) * HD + lg * 4;
+#pragma unroll
+    for (int c = 0; c < C; ++c) t.k[c] = *reinterpret_cast<const f32x4_t *>(k + 16 * c);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float *x =
+          V + ((it.base + min(key0 + lg * 4 + e, k1 - 1)) * hkv + it.kvh) * HD + lr * C;
+#pragma unroll
+      for (int c = 0; c < C; c += 4)
+        *reinterpret_cast<f32x4_t *>(&t.v[e][c]) = *reinterpret_cast<const f32x4_t *>(x + c);
+    }
+  };
+  auto attend = [&](Tile &t, int key0) __attribute__((always_inline)) {
+    f32x4_t s0 = zero, s1 = zero;  // two chains of dependent MFMAs
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(t.k[c][e], qf[c][e], s0, 0, 0, 0);
+        s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(t.k[c][e + 1], qf[c][e + 1], s1, 0, 0, 0);
       }
-      sc = k0 + lane < n ? sc * scale_log2 : -INFINITY;
-      const float m_new = fmaxf(m, wave_max(sc)), off = m_new == -INFINITY ? 0.f : m_new;
-      const float p = exp2f(sc - off), alpha = exp2f(m - off);
-      m = m_new;
-      l = l * alpha + wave_sum(p);
-      o[0] *= alpha;
-      o[1] *= alpha;
-      for (int e = 0; e < 64 && k0 + e < n; ++e) {
-        const float pe = __shfl(p, e, 64);
-        const TS *v = V + ((base + k0 + e) * hkv + kvh) * hd;
-        o[0] = fmaf(pe, load1(v + lane), o[0]);
-        if (hd > 64) o[1] = fmaf(pe, load1(v + 64 + lane), o[1]);
-      }
+    f32x4_t x = s0 + s1;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      x[e] = key0 + lg * 4 + e < seen ? x[e] * scale_log2 : -INFINITY;
+    if (key0 + 16 > all_see) {  // a hidden value that is not finite must not meet p = 0
+      bool odd = false;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (key0 + lg * 4 + e >= all_see) {
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+            if (odd_f32(t.v[e][c])) {
+              odd = true;
+              t.v[e][c] = 0.f;
+            }
+        }
+      if (odd) s_odd = 1;
+    }
+    float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float m_new = fmaxf(m, mx);
+    const float off = m_new == -INFINITY ? 0.f : m_new;  // no key yet: every p is 0
+    const float alpha = __builtin_amdgcn_exp2f(m - off);
+    f32x4_t q;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) q[e] = __builtin_amdgcn_exp2f(x[e] - off);
+    l = l * alpha + ((q[0] + q[1]) + (q[2] + q[3]));
+    m = m_new;
+#pragma unroll
+    for (int c = 0; c < C; ++c) o[c] *= alpha;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.v[e][c], q[e], o[c], 0, 0, 0);
+  };
+  constexpr int STEP = NW * 16;
+  int key0 = it.k0 + wave * 16;
+  if (key0 < k1) {
+    Tile t0, t1;
+    fetch(t0, key0);
+    while (true) {  // the next tile (the last key where there is none) is in flight meanwhile
+      fetch(t1, key0 + STEP);
+      attend(t0, key0);
+      key0 += STEP;
+      if (key0 >= k1) break;
+      fetch(t0, key0 + STEP);
+      attend(t1, key0);
+      key0 += STEP;
+      if (key0 >= k1) break;
     }
   }
-  const float inv = l == 0.f ? 0.f : 1.0f / l;
-  TS *dst = out + ((size_t)r * hq + h) * hd;
-  store1(dst + lane, o[0] * inv);
-  if (hd > 64) store1(dst + 64 + lane, o[1] * inv);
-  if (lse && lane == 0)
-    lse[(size_t)r * hq + h] = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) * 0.6931471805599453f + logf(l);
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  // o[c][e] is dim (4 lg + e) C + c of pair lr
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s_o[wave][(4 * lg + e) * C + c][lr] = o[c][e];
+  if (lg == 0) {
+    s_m[wave][lr] = m;
+    s_l[wave][lr] = l;
+  }
+  __syncthreads();
+  for (int i = wave; i < 16 && it.v0 + i < n_pairs; i += NW) {  // a wave per pair, lanes on dims
+    const int vi = it.v0 + i, ri = it.r0 + vi / G, hi = it.kvh * G + vi % G;
+    float mm = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) mm = fmaxf(mm, s_m[w][i]);
+    float so[HD / 64] = {}, sl = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      // a wave without a key of the pair has l = 0 (m = -inf is also what NaN scores leave, with
+      // a sum of NaN)
+      const float lw = s_l[w][i], a = __builtin_amdgcn_exp2f(s_m[w][i] - mm);
+      if (lw == 0.f) continue;
+      sl = fmaf(mm == -INFINITY ? 1.f : a, lw, sl);
+#pragma unroll
+      for (int c = 0; c < HD / 64; ++c) so[c] = fmaf(a, s_o[w][64 * c + lane][i], so[c]);
+    }
+    if (s_odd) {  // values left out above that this pair sees
+      const int end = shared_seen(it, ri);
+      for (int k = max(it.k0, all_see); k < end; ++k) {
+        const float *x = V + ((it.base + k) * hkv + it.kvh) * HD + lane;
+#pragma unroll
+        for (int c = 0; c < HD / 64; ++c)
+          if (odd_f32(x[64 * c])) so[c] += x[64 * c];
+      }
+    }
+    const size_t row = (size_t)ri * hq + hi;
+    if (p.slots > 1) {
+      const size_t prow = (size_t)it.slot * s.n_rows * hq + row;
+#pragma unroll
+      for (int c = 0; c < HD / 64; ++c) part_o[prow * HD + 64 * c + lane] = so[c];
+      if (lane == 0) part_ml[prow] = make_float2(mm, sl);
+    } else {
+      const float inv = sl == 0.f ? 0.f : 1.0f / sl;
+#pragma unroll
+      for (int c = 0; c < HD / 64; ++c) out[row * HD + 64 * c + lane] = so[c] * inv;
+      if (lse && lane == 0)
+        lse[row] =
+            sl == 0.f ? -INFINITY : (mm == -INFINITY ? 0.f : mm * 0.6931471805599453f) + logf(sl);
+    }
+  }
 }
 
 // ---- the weights that keys received ----------------------------------------------------
@@ -692,21 +807,24 @@ __global__ __launch_bounds__(256) void k_weight_parts(const float *__restrict__ 
   w[i] = (prev ? prev[i] : 0.f) + sum;
 }
 
-// Items of a call (bf16).
-static SharedPlan shared_plan(const SharedBatch &s, int hq, int hkv, int cus) {
+// Items of a call. bf16 tiles have 32, 64 or 128 pairs (see k_shared_bf16), fp32 ones 16. Each
+// side's key ranges are cut into pieces until there are two blocks a compute unit, pieces of
+// two key tiles (fp32: of two tiles for each wave) at least.
+static SharedPlan shared_plan(const SharedBatch &s, int hq, int hkv, int dtype) {
   SharedPlan p{};
-  const int G = hq / hkv;
-  auto groups = [](long long pairs) { return pairs > 64 ? 4 : pairs > 32 ? 2 : 1; };
-  auto tiles = [](long long pairs, int g) { return (int)((pairs + 32 * g - 1) / (32 * g)); };
+  const int G = hq / hkv, blocks = 2 * gemm_cu_count();
+  const bool bf = dtype == AKVS_BF16;
+  auto tile_pairs = [&](long long pairs) {
+    return !bf ? 16 : pairs > 64 ? 128 : pairs > 32 ? 64 : 32;
+  };
   const long long pp = (long long)s.n_rows * G, op = (long long)s.rows_max * G;
-  p.p_groups = groups(pp);
-  p.p_tiles = tiles(pp, p.p_groups);
-  p.o_groups = groups(op);
-  p.o_tiles = tiles(op, p.o_groups);
-  const int slots = 2 * cus;
+  p.p_pairs = tile_pairs(pp);
+  p.p_tiles = (int)((pp + p.p_pairs - 1) / p.p_pairs);
+  p.o_pairs = tile_pairs(op);
+  p.o_tiles = (int)((op + p.o_pairs - 1) / p.o_pairs);
   auto cut = [&](long long items, int keys, int *pieces, int *piece_keys) {
     const int kt = (keys + SH_TILE - 1) / SH_TILE;
-    long long want = items ? std::max(1LL, slots / items) : 1;
+    long long want = items ? std::max(1LL, blocks / items) : 1;
     want = std::min<long long>(want, std::max(1, kt / 2));
     const int per = kt ? (int)((kt + want - 1) / want) : 1;
     *piece_keys = per * SH_TILE;
@@ -720,50 +838,45 @@ static SharedPlan shared_plan(const SharedBatch &s, int hq, int hkv, int cus) {
 }
 
 size_t shared_part_floats(const SharedBatch &s, int hq, int hkv, int hd, int dtype) {
-  if (dtype != AKVS_BF16 || s.n_rows == 0) return 0;
-  const SharedPlan p = shared_plan(s, hq, hkv, gemm_cu_count());
+  if (s.n_rows == 0) return 0;
+  const SharedPlan p = shared_plan(s, hq, hkv, dtype);
   return p.slots > 1 ? (size_t)p.slots * s.n_rows * hq * (hd + 2) : 0;
 }
 
-template <int HD>
-static hipError_t shared_bf16(const SharedBatch &s, const void *q, const void *kp, const void *vp,
-                              const void *ko, const void *vo, int hq, int hkv, void *out,
-                              float *lse, float *part, hipStream_t st) {
-  auto b = [](const void *x) { return reinterpret_cast<const bf16_t *>(x); };
-  bf16_t *O = reinterpret_cast<bf16_t *>(out);
-  SharedPlan p = shared_plan(s, hq, hkv, gemm_cu_count());
-  const size_t n = (size_t)p.slots * s.n_rows * hq;
-  float2 *ml = reinterpret_cast<float2 *>(part + n * HD);
+template <typename TS, int HD>
+static hipError_t shared_attention(const SharedBatch &s, const void *q, const void *kp,
+                                   const void *vp, const void *ko, const void *vo, int hq,
+                                   int hkv, int dtype, void *out, float *lse, float *part,
+                                   hipStream_t st) {
+  auto x = [](const void *a) { return reinterpret_cast<const TS *>(a); };
+  TS *O = reinterpret_cast<TS *>(out);
+  SharedPlan p = shared_plan(s, hq, hkv, dtype);
+  const size_t items = (size_t)s.n_rows * hq;
+  float2 *ml = reinterpret_cast<float2 *>(part + p.slots * items * HD);
   size_t blocks = p.prefix_blocks + (size_t)s.n_req * p.chunks * p.o_tiles * hkv;
   if (blocks == 0) {  // no key at all: one item without keys writes the rows' zeros
     p.splits = p.slots = 1;
     p.prefix_blocks = p.p_tiles * hkv;
     blocks = p.prefix_blocks;
   }
-  hipLaunchKernelGGL(k_shared_bf16<HD>, dim3((unsigned)blocks), dim3(256), 0, st, s, p, b(q), b(kp),
-                     b(vp), b(ko), b(vo), hq, hkv, 1.4426950408889634f / sqrtf((float)HD), O, lse,
-                     part, ml);
+  const dim3 g((unsigned)blocks), b(256);
+  const float scale = 1.4426950408889634f / sqrtf((float)HD);
+  if constexpr (sizeof(TS) == 2)
+    hipLaunchKernelGGL(k_shared_bf16<HD>, g, b, 0, st, s, p, x(q), x(kp), x(vp), x(ko), x(vo), hq,
+                       hkv, scale, O, lse, part, ml);
+  else
+    hipLaunchKernelGGL(k_shared_f32<HD>, g, b, 0, st, s, p, x(q), x(kp), x(vp), x(ko), x(vo), hq,
+                       hkv, scale, O, lse, part, ml);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.slots <= 1) return e;
-  const size_t items = (size_t)s.n_rows * hq;
   const int teams = 256 / (HD / 8);
-#define AKVS_MERGE(G_)                                                                          \
-  hipLaunchKernelGGL((k_shared_merge<bf16_t, G_>), dim3((unsigned)((items * G_ + teams - 1) / teams)), \
-                     dim3(256), 0, st, s, p.slots, hq, HD, part, ml, O, lse)
+#define AKVS_MERGE(G_)                                                                         \
+  hipLaunchKernelGGL((k_shared_merge<TS, G_>), dim3((unsigned)((items * G_ + teams - 1) / teams)), \
+                     b, 0, st, s, p.slots, hq, HD, part, ml, O, lse)
   if (p.slots >= 12) AKVS_MERGE(16);
   else if (p.slots >= 4) AKVS_MERGE(4);
   else AKVS_MERGE(1);
 #undef AKVS_MERGE
-  return hipGetLastError();
-}
-
-static hipError_t shared_f32(const SharedBatch &s, const void *q, const void *kp, const void *vp,
-                             const void *ko, const void *vo, int hq, int hkv, int hd, void *out,
-                             float *lse, hipStream_t st) {
-  auto p = [](const void *x) { return reinterpret_cast<const float *>(x); };
-  hipLaunchKernelGGL(k_shared_attn<float>, dim3((unsigned)((size_t)s.n_rows * hq)), dim3(64), 0, st,
-                     s, p(q), p(kp), p(vp), p(ko), p(vo), hq, hkv, hd,
-                     1.4426950408889634f / sqrtf((float)hd), reinterpret_cast<float *>(out), lse);
   return hipGetLastError();
 }
 
@@ -772,9 +885,11 @@ hipError_t launch_shared_attention(const SharedBatch &s, const void *q, const vo
                                    int hkv, int hd, int dtype, void *out, float *lse, float *part,
                                    hipStream_t st) {
   if (s.n_rows == 0) return hipSuccess;
-  if (dtype != AKVS_BF16) return shared_f32(s, q, kp, vp, ko, vo, hq, hkv, hd, out, lse, st);
-  return hd == 128 ? shared_bf16<128>(s, q, kp, vp, ko, vo, hq, hkv, out, lse, part, st)
-                   : shared_bf16<64>(s, q, kp, vp, ko, vo, hq, hkv, out, lse, part, st);
+#define AKVS_SHARED(TS_, HD_) \
+  shared_attention<TS_, HD_>(s, q, kp, vp, ko, vo, hq, hkv, dtype, out, lse, part, st)
+  if (dtype == AKVS_BF16) return hd == 128 ? AKVS_SHARED(bf16_t, 128) : AKVS_SHARED(bf16_t, 64);
+  return hd == 128 ? AKVS_SHARED(float, 128) : AKVS_SHARED(float, 64);
+#undef AKVS_SHARED
 }
 
 // Two key tiles a wave share a pair tile's staging and LDS reads, but a block then takes 192
