@@ -1783,7 +1783,7 @@ static akvs_status check_evict(const akvs_model_cfg *m, const akvs_evict_cfg *c,
   *a = {c->n_seq,   c->n_keys,  c->src_rows ? c->src_rows : c->n_keys,
         c->n_keep,  c->dst_rows ? c->dst_rows : c->n_keep,
         c->n_first, c->n_recent, c->lens};
-  REQUIRE(a->n_seq <= (1 << 16) && a->src_rows < (1 << 28) && a->dst_rows < (1 << 28) &&
+  REQUIRE(a->n_seq < (1 << 16) && a->src_rows < (1 << 28) && a->dst_rows < (1 << 28) &&
               (long long)a->n_seq * a->n_keep * m->n_kv_heads < (1LL << 31),
           AKVS_ESHAPE, "too large");
   return AKVS_OK;

@@ -12,17 +12,23 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Block = one KV head of one sequence. The kept weights' smallest key T is found eight bits at
-// a time from a histogram of the candidates that agree with T so far; then wave w lists the
-// kept keys of its 1/16 of the sequence in order. Of the keys equal to T the first are kept.
-constexpr int EV_T = 1024, EV_W = EV_T / 64;
-__global__ __launch_bounds__(EV_T) void k_evict_select(const float *__restrict__ weights,
-                                                       EvictArgs a, int hkv,
-                                                       int32_t *__restrict__ keep,
-                                                       float *__restrict__ w_out) {
-  __shared__ int hist[256];
-  __shared__ int s_pick[2];
-  __shared__ int s_gt[EV_W], s_eq[EV_W];
+// Block = one KV head of one sequence, NW waves; wave w has the keys [w * per, (w + 1) * per), in
+// registers where a lane's are at most R (R = 0: read again from cache in each pass). The
+// smallest kept candidate T is found a digit at a time (11, 11 and 10 bits): a histogram in LDS
+// of the candidates that agree with T so far, its counts summed from the top by all threads, and
+// the bin in which the count reaches what is wanted. Then each wave lists its kept keys in
+// order; of the keys equal to T the first are kept. Bound by its dozen barriers and the LDS
+// round trips between them.
+constexpr int EV_BINS = 2048;
+template <int NW, int R>
+__global__ __launch_bounds__(NW * 64) void k_evict_select(const float *__restrict__ weights,
+                                                          EvictArgs a, int hkv,
+                                                          int32_t *__restrict__ keep,
+                                                          float *__restrict__ w_out) {
+  constexpr int T_ = NW * 64, PER_T = EV_BINS / T_;
+  __shared__ int hist[EV_BINS];
+  __shared__ int s_wave[NW], s_pick[2];
+  __shared__ int s_gt[NW], s_eq[NW];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int seq = blockIdx.x / hkv;
   const float *w = weights + (size_t)blockIdx.x * a.n_keys;
@@ -31,50 +37,92 @@ __global__ __launch_bounds__(EV_T) void k_evict_select(const float *__restrict__
   const int n = a.lens ? min(max(a.lens[seq], 0), a.n_keys) : a.n_keys;
   const int kept = min(n, a.n_keep);
   const bool all = n <= a.n_keep;
-  // candidates [c0, c1): every key where all are kept, none of them then
+  // candidates [c0, c1), of which `want` are kept; the keys beside them are kept
   const int c0 = a.n_first, c1 = n - a.n_recent, want = a.n_keep - a.n_first - a.n_recent;
+  const int steps = (n + T_ - 1) / T_, b0 = wave * steps * 64, b1 = min(b0 + steps * 64, n);
+  float reg[R ? R : 1];
+  if (R) {
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+      if (i < steps) reg[i] = w[min(b0 + i * 64 + lane, max(n - 1, 0))];
+  }
+  // f(step, key index, weight) over this wave's keys (indices from b1 on: none)
+  auto each = [&](auto &&f) __attribute__((always_inline)) {
+    if (R) {
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        if (i < steps) f(b0 + i * 64 + lane, reg[i]);
+    } else {
+      for (int i = 0; i < steps; ++i) {
+        const int j = b0 + i * 64 + lane;
+        f(j, w[min(j, n - 1)]);
+      }
+    }
+  };
   uint32_t T = 0;
   int eq_take = 0;
   if (!all && want > 0) {
     int left = want;  // how many of the candidates that agree with T are kept
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (t < 256) hist[t] = 0;
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+      const int bits = pass == 2 ? 10 : 11;
+#pragma unroll
+      for (int i = 0; i < PER_T; ++i) hist[t + i * T_] = 0;
       __syncthreads();
-      for (int j = c0 + t; j < c1; j += EV_T) {
-        const uint32_t u = weight_key(w[j]);
-        if (shift == 24 || (u >> (shift + 8)) == (T >> (shift + 8)))
-          atomicAdd(&hist[(u >> shift) & 255], 1);
+      each([&](int j, float x) {
+        const uint32_t u = weight_key(x);
+        // (a shift by 32 is none: the first pass takes all)
+        const bool agree = pass == 0 || (u >> (shift + bits)) == (T >> (shift + bits));
+        if (j >= c0 && j < min(c1, b1) && agree)
+          atomicAdd(&hist[(u >> shift) & ((1u << bits) - 1)], 1);
+      });
+      __syncthreads();
+      // thread t has the bins below EV_BINS - t * PER_T, the highest first
+      int h[PER_T], mine = 0;
+#pragma unroll
+      for (int i = 0; i < PER_T; ++i) {
+        h[i] = hist[EV_BINS - 1 - (t * PER_T + i)];
+        mine += h[i];
       }
+      int upto = mine;  // the counts of this wave's threads up to this one
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int x = __shfl_up(upto, o, 64);
+        if (lane >= o) upto += x;
+      }
+      if (lane == 63) s_wave[wave] = upto;
       __syncthreads();
-      if (t == 0) {
-        int above = 0, d = 255;
-        while (d > 0 && above + hist[d] < left) above += hist[d--];
-        s_pick[0] = d;
-        s_pick[1] = above;
+      int above = upto - mine;
+      for (int v = 0; v < wave; ++v) above += s_wave[v];
+#pragma unroll
+      for (int i = 0; i < PER_T; ++i) {
+        if (above < left && above + h[i] >= left) {  // (one bin of one thread)
+          s_pick[0] = EV_BINS - 1 - (t * PER_T + i);
+          s_pick[1] = above;
+        }
+        above += h[i];
       }
       __syncthreads();
       T |= (uint32_t)s_pick[0] << shift;
       left -= s_pick[1];
-      __syncthreads();
     }
     eq_take = left;
   }
-  // [b0, b1): this wave's keys, in order
-  const int per = ((n + EV_W - 1) / EV_W + 63) / 64 * 64;
-  const int b0 = min(wave * per, n), b1 = min(b0 + per, n);
-  auto sort_of = [&](int j) {  // 2: kept, 1: equal to T, 0: evicted
+  // 2: kept, 1: equal to T, 0: evicted
+  auto sort_of = [&](int j, float x) {
     if (j >= b1) return 0;
     if (all || j < c0 || j >= c1) return 2;
     if (want <= 0) return 0;
-    const uint32_t u = weight_key(w[j]);
+    const uint32_t u = weight_key(x);
     return u > T ? 2 : u == T ? 1 : 0;
   };
   int gt = 0, eq = 0;
-  for (int j0 = b0; j0 < b1; j0 += 64) {
-    const int k = sort_of(j0 + lane);
+  each([&](int j, float x) {
+    const int k = sort_of(j, x);
     gt += __popcll(__ballot(k == 2));
     eq += __popcll(__ballot(k == 1));
-  }
+  });
   if (lane == 0) {
     s_gt[wave] = gt;
     s_eq[wave] = eq;
@@ -86,54 +134,83 @@ __global__ __launch_bounds__(EV_T) void k_evict_select(const float *__restrict__
     eqs += s_eq[v];
   }
   const unsigned long long below = (1ull << lane) - 1;
-  for (int j0 = b0; j0 < b1; j0 += 64) {
-    const int k = sort_of(j0 + lane);
+  each([&](int j, float x) {
+    const int k = sort_of(j, x);
     const unsigned long long e = __ballot(k == 1);
     const bool take = k == 2 || (k == 1 && eqs + __popcll(e & below) < eq_take);
     const unsigned long long m = __ballot(take);
     if (take) {
       const int i = at + __popcll(m & below);
-      keep[i] = j0 + lane;
-      if (w_out) w_out[i] = w[j0 + lane];
+      keep[i] = j;
+      if (w_out) w_out[i] = x;
     }
     at += __popcll(m);
     eqs += __popcll(e);
-  }
-  for (int i = kept + t; i < a.n_keep; i += EV_T) keep[i] = -1;
+  });
+  for (int i = kept + t; i < a.n_keep; i += T_) keep[i] = -1;
   if (w_out)
-    for (int i = kept + t; i < a.dst_rows; i += EV_T) w_out[i] = 0.f;
+    for (int i = kept + t; i < a.dst_rows; i += T_) w_out[i] = 0.f;
 }
 
-// A thread moves 16 bytes of a kept key's row and of its value's.
-__global__ __launch_bounds__(256) void k_evict_gather(const char *__restrict__ k,
-                                                      const char *__restrict__ v, EvictArgs a,
+// Rows of kept keys and their values: a thread moves 16 bytes of each of EV_U rows, all indices
+// and then all loads requested at once (index, row and store are a chain of three round trips).
+// Blocks (row group, sequence).
+constexpr int EV_U = 4;
+__global__ __launch_bounds__(256) void k_evict_gather(const u32x4_t *__restrict__ k,
+                                                      const u32x4_t *__restrict__ v, EvictArgs a,
                                                       int hkv, int row16,
                                                       const int32_t *__restrict__ keep,
-                                                      char *__restrict__ k_out,
-                                                      char *__restrict__ v_out, int32_t *lens_out) {
-  const long long gid = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (lens_out && gid < a.n_seq) {
-    const int n = a.lens ? min(max(a.lens[gid], 0), a.n_keys) : a.n_keys;
-    lens_out[gid] = min(n, a.n_keep);
+                                                      u32x4_t *__restrict__ k_out,
+                                                      u32x4_t *__restrict__ v_out,
+                                                      int32_t *lens_out) {
+  const int seq = blockIdx.y;
+  if (lens_out && blockIdx.x == 0 && threadIdx.x == 0) {
+    const int n = a.lens ? min(max(a.lens[seq], 0), a.n_keys) : a.n_keys;
+    lens_out[seq] = min(n, a.n_keep);
   }
   if (!k) return;
-  const long long row = gid / row16;  // (sequence, kept row, head)
-  const int c = (int)(gid - row * row16);
-  const long long si = row / hkv;
-  const int h = (int)(row - si * hkv), seq = (int)(si / a.n_keep), i = (int)(si % a.n_keep);
-  if (seq >= a.n_seq) return;
-  const int j = keep[((size_t)seq * hkv + h) * a.n_keep + i];
-  if (j < 0 || j >= a.n_keys) return;
-  const size_t src = (((size_t)seq * a.src_rows + j) * hkv + h) * row16 + c;
-  const size_t dst = (((size_t)seq * a.dst_rows + i) * hkv + h) * row16 + c;
-  reinterpret_cast<uint4 *>(k_out)[dst] = reinterpret_cast<const uint4 *>(k)[src];
-  reinterpret_cast<uint4 *>(v_out)[dst] = reinterpret_cast<const uint4 *>(v)[src];
+  const unsigned width = hkv * row16;  // 16-byte chunks of a token's row
+  const unsigned id = blockIdx.x * 256 + threadIdx.x;
+  const unsigned rows = (a.n_keep + EV_U - 1) / EV_U;  // this thread's rows are `rows` apart
+  const unsigned i0 = id / width, ch = id - i0 * width;
+  if (i0 >= rows) return;
+  keep += ((size_t)seq * hkv + ch / row16) * a.n_keep;
+  int j[EV_U];
+#pragma unroll
+  for (int u = 0; u < EV_U; ++u) {
+    const unsigned i = i0 + u * rows;
+    j[u] = i < (unsigned)a.n_keep ? keep[i] : -1;
+    if (j[u] >= a.n_keys) j[u] = -1;
+  }
+  const size_t src = (size_t)seq * a.src_rows, dst = (size_t)seq * a.dst_rows;
+  u32x4_t x[EV_U], y[EV_U];
+#pragma unroll
+  for (int u = 0; u < EV_U; ++u)
+    if (j[u] >= 0) {
+      x[u] = k[(src + j[u]) * width + ch];
+      y[u] = v[(src + j[u]) * width + ch];
+    }
+#pragma unroll
+  for (int u = 0; u < EV_U; ++u)
+    if (j[u] >= 0) {
+      k_out[(dst + i0 + u * rows) * width + ch] = x[u];
+      v_out[(dst + i0 + u * rows) * width + ch] = y[u];
+    }
 }
 
+// Few keys: four waves (barriers of 4 waves cost less than of 16, and short sequences have few
+// keys a lane either way).
 hipError_t launch_evict_select(const float *weights, const EvictArgs &a, int hkv, int32_t *keep,
                                float *w_out, hipStream_t s) {
-  hipLaunchKernelGGL(k_evict_select, dim3((unsigned)(a.n_seq * hkv)), dim3(EV_T), 0, s, weights, a,
-                     hkv, keep, w_out);
+  const dim3 g((unsigned)(a.n_seq * hkv));
+#define AKVS_SELECT(NW_, R_)                                                                  \
+  hipLaunchKernelGGL((k_evict_select<NW_, R_>), g, dim3(NW_ * 64), 0, s, weights, a, hkv, keep, \
+                     w_out)
+  if (a.n_keys <= 2048) AKVS_SELECT(4, 8);
+  else if (a.n_keys <= 8192) AKVS_SELECT(16, 8);
+  else if (a.n_keys <= 32768) AKVS_SELECT(16, 32);
+  else AKVS_SELECT(16, 0);
+#undef AKVS_SELECT
   return hipGetLastError();
 }
 
@@ -142,12 +219,11 @@ hipError_t launch_evict_gather(const void *k, const void *v, const EvictArgs &a,
                                int32_t *lens_out, hipStream_t s) {
   if (!k && !lens_out) return hipSuccess;
   const int row16 = row_bytes / 16;
-  long long threads = k ? (long long)a.n_seq * a.n_keep * hkv * row16 : a.n_seq;
-  if (lens_out && threads < a.n_seq) threads = a.n_seq;
-  hipLaunchKernelGGL(k_evict_gather, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s,
-                     reinterpret_cast<const char *>(k), reinterpret_cast<const char *>(v), a, hkv,
-                     row16, keep, reinterpret_cast<char *>(k_out), reinterpret_cast<char *>(v_out),
-                     lens_out);
+  const long long threads = k ? (long long)((a.n_keep + EV_U - 1) / EV_U) * hkv * row16 : 1;
+  hipLaunchKernelGGL(k_evict_gather, dim3((unsigned)((threads + 255) / 256), a.n_seq), dim3(256), 0,
+                     s, reinterpret_cast<const u32x4_t *>(k), reinterpret_cast<const u32x4_t *>(v), a,
+                     hkv, row16, keep, reinterpret_cast<u32x4_t *>(k_out),
+                     reinterpret_cast<u32x4_t *>(v_out), lens_out);
   return hipGetLastError();
 }
 

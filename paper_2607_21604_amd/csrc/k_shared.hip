@@ -6,6 +6,7 @@
 // keys into chunks; each is a work item of its own, all items run in one launch and leave
 // (output, maximum, sum) partials that a second launch merges.
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.h"
 
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(256, 2) void k_shared_bf16(
     SharedBatch s, SharedPlan p, const bf16_t *__restrict__ Q, const bf16_t *__restrict__ Kp,
     const bf16_t *__restrict__ Vp, const bf16_t *__restrict__ Ko, const bf16_t *__restrict__ Vo,
     int hq, int hkv, float scale_log2, bf16_t *__restrict__ out, float *__restrict__ lse,
-    float *__restrict__ part_o, float2 *__restrict__ part_ml) {
+    _Float16 *__restrict__ part_o, float4 *__restrict__ part_ml) {
   constexpr int KS = HD / 16, DB = HD / 32, CPK = HD / 8;
   constexpr int KST = HD + 8, VST = HD + 32;       // row strides: fragment reads on all banks
   constexpr int NCH = SH_TILE * CPK / 256;         // 16-byte chunks of K (and V) per thread
@@ -126,7 +127,7 @@ __global__ __launch_bounds__(256, 2) void k_shared_bf16(
   const int nkt = k1 > it.k0 ? (k1 - it.k0 + SH_TILE - 1) / SH_TILE : 0;
   const bool writes = valid && (groups == 4 || (works && (wave & 1) == 0));
   if (nkt == 0 && p.slots > 1) {
-    if (writes && hi == 0) part_ml[prow] = make_float2(-INFINITY, 0.f);
+    if (writes && hi == 0) part_ml[prow] = make_float4(-INFINITY, 0.f, 1.f, 0.f);
     return;
   }
 
@@ -299,14 +300,29 @@ __global__ __launch_bounds__(256, 2) void k_shared_bf16(
   }
   // o[db][i] is dim db * 32 + (i / 4) * 8 + hi * 4 + i % 4 of the pair
   if (p.slots > 1) {
-    float *po = part_o + prow * HD + hi * 4;
+    float big = 0.f;  // the pair's largest finite value
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4)
-        store4(po + db * 32 + q4 * 8, o[db][4 * q4], o[db][4 * q4 + 1], o[db][4 * q4 + 2],
-               o[db][4 * q4 + 3]);
-    if (hi == 0) part_ml[prow] = make_float2(m_run, l);
+      for (int i = 0; i < 16; ++i) {
+        const float x = fabsf(o[db][i]);
+        big = x < INFINITY ? fmaxf(big, x) : big;
+      }
+    big = fmaxf(big, __shfl_xor(big, 32, 64));
+    const int e = max(__builtin_amdgcn_frexp_expf(big), -100) - 15;
+    const float down = ldexpf(1.f, -e);
+    _Float16 *po = part_o + prow * HD + hi * 4;
+    typedef _Float16 f16x4_t __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        f16x4_t x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = (_Float16)(o[db][4 * q4 + j] * down);
+        *reinterpret_cast<f16x4_t *>(po + db * 32 + q4 * 8) = x;
+      }
+    if (hi == 0) part_ml[prow] = make_float4(m_run, l, ldexpf(1.f, e), 0.f);
     return;
   }
   const float inv = l == 0.f ? 0.f : 1.0f / l;
@@ -323,65 +339,142 @@ __global__ __launch_bounds__(256, 2) void k_shared_bf16(
 }
 
 // out = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s over a pair's slots, M = max m_s. A slot
-// without a key holds m = -inf, l = 0 (its output was not written and is not read); one of NaN
-// scores holds l = NaN. A block serves 256 / (per * GROUPS) pairs: `per` threads of 8 dims,
-// GROUPS of them taking the slots in turn, added in order through LDS.
-template <typename TS, int GROUPS>
-__global__ __launch_bounds__(256) void k_shared_merge(SharedBatch s, int slots, int hq, int hd,
-                                                      const float *__restrict__ part_o,
-                                                      const float2 *__restrict__ part_ml,
-                                                      TS *__restrict__ out,
-                                                      float *__restrict__ lse) {
-  __shared__ float s_a[GROUPS > 1 ? 256 * 9 : 1], s_m[GROUPS > 1 ? 256 : 1];
-  const int per = hd >> 3, team = per * GROUPS, tid = threadIdx.x;
-  const int e0 = (tid % per) * 8, g = tid % team / per;
-  const long long item = (long long)blockIdx.x * (256 / team) + tid / team;
-  const bool live = item < (long long)shared_live(s) * hq;
+// holds (m, l, f) and its output over f: fp32 values with f = 1, or fp16 with f a power of two
+// that brings the largest to [2^14, 2^15). fp16 carries 11 bits of a slot's large values, three
+// more than the bf16 result keeps, at half the traffic of fp32. A slot without a key holds
+// m = -inf, l = 0 (its output was not written and takes no part); one of NaN scores l = NaN.
+__device__ __forceinline__ void part_load8(const float *p, float (&x)[8]) { load8(p, x); }
+__device__ __forceinline__ void part_load8(const _Float16 *p, float (&x)[8]) {
+  typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+  const f16x8_t v = *reinterpret_cast<const f16x8_t *>(p);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
+}
+__device__ __forceinline__ float slot_factor(float4 ml, float M) {  // 0: takes no part
+  if (ml.y == 0.f) return 0.f;
+  return M == -INFINITY ? 1.f : exp2f(ml.x - M);  // (no maximum: all scores NaN)
+}
+__device__ __forceinline__ float merged_lse(float M, float l) {
+  if (l == 0.f) return -INFINITY;
+  return (M == -INFINITY ? 0.f : M * 0.6931471805599453f) + logf(l);
+}
+
+// Few slots: a thread has 8 dims of a pair and requests all slots at once.
+constexpr int MERGE_FEW = 4;
+template <typename TS, typename TP>
+__global__ __launch_bounds__(256) void k_shared_merge_few(SharedBatch s, int slots, int hq, int hd,
+                                                          const TP *__restrict__ part_o,
+                                                          const float4 *__restrict__ part_ml,
+                                                          TS *__restrict__ out,
+                                                          float *__restrict__ lse) {
+  const int per = hd >> 3;
+  const size_t id = (size_t)blockIdx.x * 256 + threadIdx.x, item = id / per;
+  const int e0 = (int)(id - item * per) * 8;
+  if (item >= (size_t)shared_live(s) * hq) return;
   const size_t stride = (size_t)s.n_rows * hq;
-  float m = -INFINITY, l = 0.f, a[8];
+  float4 ml[MERGE_FEW];
+  float x[MERGE_FEW][8];
+#pragma unroll
+  for (int u = 0; u < MERGE_FEW; ++u)
+    if (u < slots) {
+      ml[u] = part_ml[u * stride + item];
+      part_load8(part_o + (u * stride + item) * hd + e0, x[u]);
+    }
+  float M = -INFINITY, l = 0.f, a[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) a[i] = 0.f;
-  if (live) {
-    for (int u = g; u < slots; u += GROUPS) {
-      const float2 ml = part_ml[u * stride + item];
-      if (ml.y == 0.f) continue;
-      float x[8];
-      load8(part_o + (u * stride + item) * hd + e0, x);
-      const float m_new = fmaxf(m, ml.x), off = m_new == -INFINITY ? 0.f : m_new;
-      const float wa = exp2f(m - off), wb = exp2f(ml.x - off);
-      l = wa * l + wb * ml.y;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) a[i] = wa * a[i] + wb * x[i];
-      m = m_new;
+  for (int u = 0; u < MERGE_FEW; ++u)
+    if (u < slots) M = fmaxf(M, ml[u].x);
+#pragma unroll
+  for (int u = 0; u < MERGE_FEW; ++u)
+    if (u < slots) {
+      const float w = slot_factor(ml[u], M);
+      if (w == 0.f) continue;
+      l = fmaf(w, ml[u].y, l);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) a[i] = fmaf(w * ml[u].z, x[u][i], a[i]);
     }
-  }
-  if (GROUPS > 1) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s_a[tid * 9 + i] = a[i];
-    s_a[tid * 9 + 8] = l;
-    s_m[tid] = m;
-    __syncthreads();
-    if (g != 0 || !live) return;
-    for (int q = 1; q < GROUPS; ++q) {
-      const int o = tid + q * per;
-      const float m2 = s_m[o], l2 = s_a[o * 9 + 8];
-      if (l2 == 0.f) continue;
-      const float m_new = fmaxf(m, m2), off = m_new == -INFINITY ? 0.f : m_new;
-      const float wa = exp2f(m - off), wb = exp2f(m2 - off);
-      l = wa * l + wb * l2;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) a[i] = wa * a[i] + wb * s_a[o * 9 + i];
-      m = m_new;
-    }
-  } else if (!live) {
-    return;
-  }
   const float inv = l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll
   for (int i = 0; i < 8; ++i) a[i] *= inv;
   store8(out + item * hd + e0, a);
-  if (lse && e0 == 0)
-    lse[item] = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m * 0.6931471805599453f) + logf(l);
+  if (lse && e0 == 0) lse[item] = merged_lse(M, l);
+}
+
+// Many slots: block = one pair. Its threads have a slot's (m, l, f) each, for the maximum, the
+// factors and their sum; then 256 / (hd / 8) teams of hd / 8 threads take the slots in turn, four
+// outputs requested at a time, and are added in order through LDS.
+constexpr int MERGE_SLOTS = 1024;  // the most slots
+template <typename TS, typename TP, int HD>
+__global__ __launch_bounds__(256) void k_shared_merge(SharedBatch s, int slots, int hq,
+                                                      const TP *__restrict__ part_o,
+                                                      const float4 *__restrict__ part_ml,
+                                                      TS *__restrict__ out,
+                                                      float *__restrict__ lse) {
+  constexpr int PER = HD / 8, TEAMS = 256 / PER;
+  __shared__ float s_w[MERGE_SLOTS];
+  __shared__ float s_a[TEAMS][HD];
+  __shared__ float s_m[4], s_l[4];
+  const int tid = threadIdx.x, wave = tid >> 6;
+  const size_t item = blockIdx.x, stride = (size_t)s.n_rows * hq;
+  if (item >= (size_t)shared_live(s) * hq) return;
+  float4 ml[MERGE_SLOTS / 256];
+  float M = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int i = 0; i < MERGE_SLOTS / 256; ++i) {
+    const int u = tid + 256 * i;
+    if (256 * i < slots) {
+      ml[i] = u < slots ? part_ml[u * stride + item] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+      M = fmaxf(M, ml[i].x);
+    }
+  }
+  M = wave_max(M);
+  if ((tid & 63) == 0) s_m[wave] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+#pragma unroll
+  for (int i = 0; i < MERGE_SLOTS / 256; ++i) {
+    const int u = tid + 256 * i;
+    if (u < slots) {
+      const float w = slot_factor(ml[i], M);
+      if (w != 0.f) l = fmaf(w, ml[i].y, l);
+      s_w[u] = w == 0.f ? 0.f : w * ml[i].z;
+    }
+  }
+  l = wave_sum(l);
+  if ((tid & 63) == 0) s_l[wave] = l;
+  __syncthreads();
+  l = ((s_l[0] + s_l[1]) + s_l[2]) + s_l[3];
+  const int e0 = (tid % PER) * 8, team = tid / PER;
+  float a[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a[i] = 0.f;
+  for (int u0 = team; u0 < slots; u0 += 4 * TEAMS) {
+    float x[4][8], w[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int u = u0 + q * TEAMS;
+      w[q] = u < slots ? s_w[u] : 0.f;
+      part_load8(part_o + (min(u, slots - 1) * stride + item) * HD + e0, x[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (w[q] != 0.f) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a[i] = fmaf(w[q], x[q][i], a[i]);
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s_a[team][e0 + i] = a[i];
+  __syncthreads();
+  if (tid < HD) {
+    float o = s_a[0][tid];
+#pragma unroll
+    for (int q = 1; q < TEAMS; ++q) o += s_a[q][tid];
+    store1(out + item * HD + tid, l == 0.f ? 0.f : o / l);
+  }
+  if (lse && tid == 0) lse[item] = merged_lse(M, l);
 }
 
 __device__ __forceinline__ bool odd_f32(float x) {
@@ -399,7 +492,7 @@ __global__ __launch_bounds__(256, 2) void k_shared_f32(
     SharedBatch s, SharedPlan p, const float *__restrict__ Q, const float *__restrict__ Kp,
     const float *__restrict__ Vp, const float *__restrict__ Ko, const float *__restrict__ Vo,
     int hq, int hkv, float scale_log2, float *__restrict__ out, float *__restrict__ lse,
-    float *__restrict__ part_o, float2 *__restrict__ part_ml) {
+    float *__restrict__ part_o, float4 *__restrict__ part_ml) {
   constexpr int C = HD / 16, NW = 4;
   __shared__ float s_o[NW][HD][17];
   __shared__ float s_m[NW][16], s_l[NW][16];
@@ -417,7 +510,8 @@ __global__ __launch_bounds__(256, 2) void k_shared_f32(
   const int k1 = shared_seen(it, it.r0 + last / G), all_see = shared_seen(it, it.r0 + it.v0 / G);
   if (k1 <= it.k0 && p.slots > 1) {
     if (tid < 16 && valid)
-      part_ml[((size_t)it.slot * s.n_rows + r) * hq + head] = make_float2(-INFINITY, 0.f);
+      part_ml[((size_t)it.slot * s.n_rows + r) * hq + head] =
+          make_float4(-INFINITY, 0.f, 1.f, 0.f);
     return;
   }
   if (tid == 0) s_odd = 0;
@@ -553,7 +647,7 @@ __global__ __launch_bounds__(256, 2) void k_shared_f32(
       const size_t prow = (size_t)it.slot * s.n_rows * hq + row;
 #pragma unroll
       for (int c = 0; c < HD / 64; ++c) part_o[prow * HD + 64 * c + lane] = so[c];
-      if (lane == 0) part_ml[prow] = make_float2(mm, sl);
+      if (lane == 0) part_ml[prow] = make_float4(mm, sl, 1.f, 0.f);
     } else {
       const float inv = sl == 0.f ? 0.f : 1.0f / sl;
 #pragma unroll
@@ -825,7 +919,7 @@ static SharedPlan shared_plan(const SharedBatch &s, int hq, int hkv, int dtype) 
   auto cut = [&](long long items, int keys, int *pieces, int *piece_keys) {
     const int kt = (keys + SH_TILE - 1) / SH_TILE;
     long long want = items ? std::max(1LL, blocks / items) : 1;
-    want = std::min<long long>(want, std::max(1, kt / 2));
+    want = std::min<long long>(want, std::min(MERGE_SLOTS / 2, std::max(1, kt / 2)));
     const int per = kt ? (int)((kt + want - 1) / want) : 1;
     *piece_keys = per * SH_TILE;
     *pieces = (kt + per - 1) / per;
@@ -840,7 +934,8 @@ static SharedPlan shared_plan(const SharedBatch &s, int hq, int hkv, int dtype) 
 size_t shared_part_floats(const SharedBatch &s, int hq, int hkv, int hd, int dtype) {
   if (s.n_rows == 0) return 0;
   const SharedPlan p = shared_plan(s, hq, hkv, dtype);
-  return p.slots > 1 ? (size_t)p.slots * s.n_rows * hq * (hd + 2) : 0;
+  const size_t items = (size_t)p.slots * s.n_rows * hq;
+  return p.slots > 1 ? items * (dtype == AKVS_BF16 ? hd / 2 : hd) + items * 4 : 0;
 }
 
 template <typename TS, int HD>
@@ -852,7 +947,9 @@ static hipError_t shared_attention(const SharedBatch &s, const void *q, const vo
   TS *O = reinterpret_cast<TS *>(out);
   SharedPlan p = shared_plan(s, hq, hkv, dtype);
   const size_t items = (size_t)s.n_rows * hq;
-  float2 *ml = reinterpret_cast<float2 *>(part + p.slots * items * HD);
+  typedef typename std::conditional<sizeof(TS) == 2, _Float16, float>::type TP;
+  float4 *ml = reinterpret_cast<float4 *>(part);  // (m, l, f) of every slot, then the outputs
+  TP *po = reinterpret_cast<TP *>(ml + p.slots * items);
   size_t blocks = p.prefix_blocks + (size_t)s.n_req * p.chunks * p.o_tiles * hkv;
   if (blocks == 0) {  // no key at all: one item without keys writes the rows' zeros
     p.splits = p.slots = 1;
@@ -863,20 +960,18 @@ static hipError_t shared_attention(const SharedBatch &s, const void *q, const vo
   const float scale = 1.4426950408889634f / sqrtf((float)HD);
   if constexpr (sizeof(TS) == 2)
     hipLaunchKernelGGL(k_shared_bf16<HD>, g, b, 0, st, s, p, x(q), x(kp), x(vp), x(ko), x(vo), hq,
-                       hkv, scale, O, lse, part, ml);
+                       hkv, scale, O, lse, po, ml);
   else
     hipLaunchKernelGGL(k_shared_f32<HD>, g, b, 0, st, s, p, x(q), x(kp), x(vp), x(ko), x(vo), hq,
-                       hkv, scale, O, lse, part, ml);
+                       hkv, scale, O, lse, po, ml);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.slots <= 1) return e;
-  const int teams = 256 / (HD / 8);
-#define AKVS_MERGE(G_)                                                                         \
-  hipLaunchKernelGGL((k_shared_merge<TS, G_>), dim3((unsigned)((items * G_ + teams - 1) / teams)), \
-                     b, 0, st, s, p.slots, hq, HD, part, ml, O, lse)
-  if (p.slots >= 12) AKVS_MERGE(16);
-  else if (p.slots >= 4) AKVS_MERGE(4);
-  else AKVS_MERGE(1);
-#undef AKVS_MERGE
+  if (p.slots <= MERGE_FEW)
+    hipLaunchKernelGGL((k_shared_merge_few<TS, TP>), dim3((unsigned)((items * (HD / 8) + 255) / 256)),
+                       b, 0, st, s, p.slots, hq, HD, po, ml, O, lse);
+  else
+    hipLaunchKernelGGL((k_shared_merge<TS, TP, HD>), dim3((unsigned)items), b, 0, st, s, p.slots, hq,
+                       po, ml, O, lse);
   return hipGetLastError();
 }
 
