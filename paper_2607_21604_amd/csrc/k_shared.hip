@@ -6,6 +6,7 @@
 // keys into chunks; each is a work item of its own, all items run in one launch and leave
 // (output, maximum, sum) partials that a second launch merges.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "kernels.h"
@@ -901,31 +902,62 @@ __global__ __launch_bounds__(256) void k_weight_parts(const float *__restrict__ 
   w[i] = (prev ? prev[i] : 0.f) + sum;
 }
 
-// Items of a call. bf16 tiles have 32, 64 or 128 pairs (see k_shared_bf16), fp32 ones 16. Each
-// side's key ranges are cut into pieces until there are two blocks a compute unit, pieces of
-// two key tiles (fp32: of two tiles for each wave) at least.
-static SharedPlan shared_plan(const SharedBatch &s, int hq, int hkv, int dtype) {
+// Items of a call. bf16 tiles have 32, 64 or 128 pairs (see k_shared_bf16), fp32 ones 16; two
+// blocks share a compute unit. Own keys go in chunks of two key tiles at least (their lengths
+// are known on the device alone: most of the room for them may be empty). The prefix is cut
+// into the number of splits whose estimated end is the earliest, in units of a key tile's time
+// in a block: blocks that fit the chip together end with the longest of them; else they end
+// with the average load and the last short block, and no sooner than the rounds of whole
+// prefix blocks. A block costs FIXED tiles beside its keys, and each split's partials cost a
+// write and a read.
+//   16 rows over 16128 keys of 40/8 heads, 128 blocks of own keys: 384 prefix blocks 23 us, 504
+//   27 us (own blocks wait for a place); 116 fp32 rows over 2055 keys of 28/4: 232 blocks 56 us,
+//   464 43 us.
+static SharedPlan shared_plan(const SharedBatch &s, int hq, int hkv, int hd, int dtype) {
+  constexpr double FIXED = 4, BYTES = 6.4e6;  // BYTES: partials moved in a tile's time
   SharedPlan p{};
   const int G = hq / hkv, blocks = 2 * gemm_cu_count();
   const bool bf = dtype == AKVS_BF16;
   auto tile_pairs = [&](long long pairs) {
     return !bf ? 16 : pairs > 64 ? 128 : pairs > 32 ? 64 : 32;
   };
+  auto tiles_of = [](long long n, int per) { return (int)((n + per - 1) / per); };
   const long long pp = (long long)s.n_rows * G, op = (long long)s.rows_max * G;
   p.p_pairs = tile_pairs(pp);
-  p.p_tiles = (int)((pp + p.p_pairs - 1) / p.p_pairs);
+  p.p_tiles = tiles_of(pp, p.p_pairs);
   p.o_pairs = tile_pairs(op);
-  p.o_tiles = (int)((op + p.o_pairs - 1) / p.o_pairs);
-  auto cut = [&](long long items, int keys, int *pieces, int *piece_keys) {
-    const int kt = (keys + SH_TILE - 1) / SH_TILE;
-    long long want = items ? std::max(1LL, blocks / items) : 1;
-    want = std::min<long long>(want, std::min(MERGE_SLOTS / 2, std::max(1, kt / 2)));
-    const int per = kt ? (int)((kt + want - 1) / want) : 1;
+  p.o_tiles = tiles_of(op, p.o_pairs);
+  auto cut = [&](long long n, int kt, int *pieces, int *piece_keys) {
+    n = std::max(1LL, std::min<long long>(n, std::min(MERGE_SLOTS / 2, kt / 2)));
+    const int per = kt ? (int)((kt + n - 1) / n) : 1;
     *piece_keys = per * SH_TILE;
     *pieces = (kt + per - 1) / per;
   };
-  cut((long long)p.p_tiles * hkv, s.prefix_len, &p.splits, &p.split_keys);
-  cut((long long)s.n_req * p.o_tiles * hkv, s.own_rows, &p.chunks, &p.chunk_keys);
+  const long long o_items = s.own_rows ? (long long)s.n_req * p.o_tiles * hkv : 0;
+  cut(o_items ? blocks / o_items : 1, tiles_of(s.own_rows, SH_TILE), &p.chunks, &p.chunk_keys);
+  const double o_blocks = (double)o_items * p.chunks, o_time = p.chunk_keys / SH_TILE + FIXED;
+  const long long items = (long long)p.p_tiles * hkv;
+  const int kt = tiles_of(s.prefix_len, SH_TILE);
+  const double move = (double)s.n_rows * hq * hd * 4 / BYTES;  // of one split's partials
+  auto end = [&](long long n) {
+    const double time = (double)kt / n + FIXED, count = (double)items * n;
+    double t = std::max(time, o_blocks > 0 ? o_time : 0.);
+    if (count + o_blocks > blocks)
+      t = std::max((count * time + o_blocks * o_time) / blocks + std::min(time, o_time),
+                   std::ceil(count / blocks) * time);
+    return t + move * n;
+  };
+  long long best = 1;
+  const long long most = std::max(1, std::min(MERGE_SLOTS / 2, kt / 2));
+  auto consider = [&](long long n) {
+    n = std::max(1LL, std::min(n, most));
+    if (end(n) < end(best)) best = n;
+  };
+  if (items && kt) {
+    consider((long long)((blocks - o_blocks) / items));
+    for (int rounds = 1; rounds <= 8; ++rounds) consider((long long)rounds * blocks / items);
+  }
+  cut(best, kt, &p.splits, &p.split_keys);
   p.prefix_blocks = p.splits * p.p_tiles * hkv;
   p.slots = p.splits + p.chunks;
   return p;
@@ -933,7 +965,7 @@ static SharedPlan shared_plan(const SharedBatch &s, int hq, int hkv, int dtype) 
 
 size_t shared_part_floats(const SharedBatch &s, int hq, int hkv, int hd, int dtype) {
   if (s.n_rows == 0) return 0;
-  const SharedPlan p = shared_plan(s, hq, hkv, dtype);
+  const SharedPlan p = shared_plan(s, hq, hkv, hd, dtype);
   const size_t items = (size_t)p.slots * s.n_rows * hq;
   return p.slots > 1 ? items * (dtype == AKVS_BF16 ? hd / 2 : hd) + items * 4 : 0;
 }
@@ -945,7 +977,7 @@ static hipError_t shared_attention(const SharedBatch &s, const void *q, const vo
                                    hipStream_t st) {
   auto x = [](const void *a) { return reinterpret_cast<const TS *>(a); };
   TS *O = reinterpret_cast<TS *>(out);
-  SharedPlan p = shared_plan(s, hq, hkv, dtype);
+  SharedPlan p = shared_plan(s, hq, hkv, HD, dtype);
   const size_t items = (size_t)s.n_rows * hq;
   typedef typename std::conditional<sizeof(TS) == 2, _Float16, float>::type TP;
   float4 *ml = reinterpret_cast<float4 *>(part);  // (m, l, f) of every slot, then the outputs
