@@ -906,15 +906,16 @@ __global__ __launch_bounds__(256) void k_weight_parts(const float *__restrict__ 
 // blocks share a compute unit. Own keys go in chunks of two key tiles at least (their lengths
 // are known on the device alone: most of the room for them may be empty). The prefix is cut
 // into the number of splits whose estimated end is the earliest, in units of a key tile's time
-// in a block: blocks that fit the chip together end with the longest of them; else they end
-// with the average load and the last short block, and no sooner than the rounds of whole
-// prefix blocks. A block costs FIXED tiles beside its keys, and each split's partials cost a
-// write and a read.
-//   16 rows over 16128 keys of 40/8 heads, 128 blocks of own keys: 384 prefix blocks 23 us, 504
-//   27 us (own blocks wait for a place); 116 fp32 rows over 2055 keys of 28/4: 232 blocks 56 us,
-//   464 43 us.
+// in a block that has its unit for itself (1.85 us): blocks that fit the chip together end with
+// the longest of them; else they end with the average load and half a short block, and no
+// sooner than the rounds of whole prefix blocks. A block costs 4 tiles beside its keys; where
+// blocks share units 7, and 1.3 for a tile; each split's partials cost a write and a read.
+//   16 rows over 4096 / 8192 / 16384 / 32768 / 65536 keys of 40/8 heads, attention alone: 11.8 /
+//   16.1 / 23.4 / 46.5 / 85.8 us with 256 prefix blocks, 12.8 / 20.4 / 24.8 / 39.8 / 62.3 with 512;
+//   with 128 blocks of own keys and 16128, 256 to 384 prefix blocks 23 us, 504 27 us (own blocks
+//   wait for a place); 116 fp32 rows over 2055 keys of 28/4 heads: 232 blocks 56 us, 464 43 us.
 static SharedPlan shared_plan(const SharedBatch &s, int hq, int hkv, int hd, int dtype) {
-  constexpr double FIXED = 4, BYTES = 6.4e6;  // BYTES: partials moved in a tile's time
+  constexpr double BYTES = 7.4e6;  // partials moved in a tile's time
   SharedPlan p{};
   const int G = hq / hkv, blocks = 2 * gemm_cu_count();
   const bool bf = dtype == AKVS_BF16;
@@ -935,27 +936,31 @@ static SharedPlan shared_plan(const SharedBatch &s, int hq, int hkv, int hd, int
   };
   const long long o_items = s.own_rows ? (long long)s.n_req * p.o_tiles * hkv : 0;
   cut(o_items ? blocks / o_items : 1, tiles_of(s.own_rows, SH_TILE), &p.chunks, &p.chunk_keys);
-  const double o_blocks = (double)o_items * p.chunks, o_time = p.chunk_keys / SH_TILE + FIXED;
+  const double o_blocks = (double)o_items * p.chunks;
   const long long items = (long long)p.p_tiles * hkv;
   const int kt = tiles_of(s.prefix_len, SH_TILE);
   const double move = (double)s.n_rows * hq * hd * 4 / BYTES;  // of one split's partials
   auto end = [&](long long n) {
-    const double time = (double)kt / n + FIXED, count = (double)items * n;
-    double t = std::max(time, o_blocks > 0 ? o_time : 0.);
+    const double count = (double)items * n;
+    const bool share = count + o_blocks > blocks / 2;
+    auto time = [&](double tiles) { return share ? 1.3 * tiles + 7 : tiles + 4; };
+    const double pt = time((double)kt / n), ot = o_blocks > 0 ? time(p.chunk_keys / SH_TILE) : 0;
+    double t = std::max(pt, ot);
     if (count + o_blocks > blocks)
-      t = std::max((count * time + o_blocks * o_time) / blocks + std::min(time, o_time),
-                   std::ceil(count / blocks) * time);
+      t = std::max((count * pt + o_blocks * ot) / blocks + 0.5 * std::min(pt, ot),
+                   std::ceil(count / blocks) * pt);
     return t + move * n;
   };
   long long best = 1;
   const long long most = std::max(1, std::min(MERGE_SLOTS / 2, kt / 2));
-  auto consider = [&](long long n) {
-    n = std::max(1LL, std::min(n, most));
-    if (end(n) < end(best)) best = n;
+  auto consider = [&](double n) {
+    const long long k = std::max(1LL, std::min((long long)n, most));
+    if (end(k) < end(best)) best = k;
   };
   if (items && kt) {
-    consider((long long)((blocks - o_blocks) / items));
-    for (int rounds = 1; rounds <= 8; ++rounds) consider((long long)rounds * blocks / items);
+    consider((blocks / 2 - o_blocks) / items);
+    consider((blocks - o_blocks) / items);
+    for (int rounds = 1; rounds <= 8; ++rounds) consider((double)rounds * blocks / items);
   }
   cut(best, kt, &p.splits, &p.split_keys);
   p.prefix_blocks = p.splits * p.p_tiles * hkv;
