@@ -145,14 +145,31 @@ __global__ __launch_bounds__(256, 2) void k_shared_bf16(
     for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;  // (l_run: of this lane's half of the keys)
 
+  // Chunk i of a thread is 16 bytes of key row tid / CPK + i * (256 / CPK) of a tile: a fixed
+  // offset from the tile's first key, whose address is the same for all threads.
   u32x4_t kreg[NCH], vreg[NCH];
-  auto load = [&](int key0) __attribute__((always_inline)) {  // keys past k1 re-read the last
+  const uint32_t row_bytes = hkv * HD * 2;
+  const uint32_t off0 = tid / CPK * row_bytes + tid % CPK * 16;
+  const size_t start = (it.base * hkv + it.kvh) * (HD * 2);
+  auto load = [&](int key0) __attribute__((always_inline)) {
+    const char *kt = reinterpret_cast<const char *>(K) + start + (size_t)key0 * row_bytes;
+    const char *vt = reinterpret_cast<const char *>(V) + start + (size_t)key0 * row_bytes;
+    const int end = k1 - 1 - key0;  // the range's last key, which keys past it re-read
+    if (end >= SH_TILE - 1) {
 #pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      const int c = tid + 256 * i, kr = c / CPK, e0 = (c % CPK) * 8;
-      const size_t at = ((it.base + min(key0 + kr, k1 - 1)) * hkv + it.kvh) * HD + e0;
-      kreg[i] = *reinterpret_cast<const u32x4_t *>(K + at);
-      vreg[i] = *reinterpret_cast<const u32x4_t *>(V + at);
+      for (int i = 0; i < NCH; ++i) {
+        const uint32_t off = off0 + i * (256 / CPK) * row_bytes;
+        kreg[i] = *reinterpret_cast<const u32x4_t *>(kt + off);
+        vreg[i] = *reinterpret_cast<const u32x4_t *>(vt + off);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        const uint32_t off =
+            min(tid / CPK + i * (256 / CPK), end) * row_bytes + tid % CPK * 16;
+        kreg[i] = *reinterpret_cast<const u32x4_t *>(kt + off);
+        vreg[i] = *reinterpret_cast<const u32x4_t *>(vt + off);
+      }
     }
   };
   // Values that some pair of the tile must not see take part with probability 0, and 0 * inf is
