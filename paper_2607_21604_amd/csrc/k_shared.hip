@@ -617,12 +617,10 @@ __global__ __launch_bounds__(256, 2) void k_shared_f32(
     fetch(t0, key0);
     while (true) {  // the next tile (the last key where there is none) is in flight meanwhile
       fetch(t1, key0 + STEP);
-      __builtin_amdgcn_sched_barrier(0);  // (requested before the products wait for theirs)
       attend(t0, key0);
       key0 += STEP;
       if (key0 >= k1) break;
       fetch(t0, key0 + STEP);
-      __builtin_amdgcn_sched_barrier(0);
       attend(t1, key0);
       key0 += STEP;
       if (key0 >= k1) break;
@@ -927,17 +925,18 @@ __global__ __launch_bounds__(256) void k_weight_parts(const float *__restrict__ 
 // Items of a call. bf16 tiles have 32, 64 or 128 pairs (see k_shared_bf16), fp32 ones 16; two
 // blocks share a compute unit. Own keys go in chunks of two key tiles at least (their lengths
 // are known on the device alone: most of the room for them may be empty). The prefix is cut
-// into the number of splits whose estimated end is the earliest, in units of a key tile's time
-// in a block that has its unit for itself (1.85 us): blocks that fit the chip together end with
-// the longest of them; else they end with the average load and half a short block, and no
-// sooner than the rounds of whole prefix blocks. A block costs 4 tiles beside its keys; where
-// blocks share units 7, and 1.3 for a tile; each split's partials cost a write and a read.
-//   16 rows over 4096 / 8192 / 16384 / 32768 / 65536 keys of 40/8 heads, attention alone: 11.8 /
-//   16.1 / 23.4 / 46.5 / 85.8 us with 256 prefix blocks, 12.8 / 20.4 / 24.8 / 39.8 / 62.3 with 512;
-//   with 128 blocks of own keys and 16128, 256 to 384 prefix blocks 23 us, 504 27 us (own blocks
-//   wait for a place); 116 fp32 rows over 2055 keys of 28/4 heads: 232 blocks 56 us, 464 43 us.
+// into the number of splits whose estimated end is the earliest, in units of the time that a
+// block alone on its unit takes for a key tile (1.75 us): such a block takes 4.3 + its tiles, one
+// that shares its unit 7.5 + 1.7 times them. Blocks that fit the chip together end with the
+// longest of them; else whole rounds of prefix blocks, the rest of them, and the own keys'
+// blocks that had no place follow each other. Each split's partials cost a write and a read.
+//   16 rows over 4096 / 8192 / 16384 / 32768 / 65536 keys of 40/8 heads, this launch alone: 256
+//   prefix blocks 11.1 / 14.6 / 21.0 / 34.9 / 62.7 us, 512 of them - / 19.6 / 23.3 / 37.1 / 60.8;
+//   with 128 blocks of own keys and 16128 keys 256 prefix blocks are 4 us faster than 504 (own
+//   blocks wait for a place). 1320 rows over 16128 (416 tiles of pairs): 597 us with one split,
+//   556 with three. 116 fp32 rows over 2055 keys of 28/4 heads: 56 us with two, 43 with four.
 static SharedPlan shared_plan(const SharedBatch &s, int hq, int hkv, int hd, int dtype) {
-  constexpr double BYTES = 7.4e6;  // partials moved in a tile's time
+  constexpr double BYTES = 7e6;  // partials moved in a tile's time
   SharedPlan p{};
   const int G = hq / hkv, blocks = 2 * gemm_cu_count();
   const bool bf = dtype == AKVS_BF16;
@@ -963,14 +962,21 @@ static SharedPlan shared_plan(const SharedBatch &s, int hq, int hkv, int hd, int
   const int kt = tiles_of(s.prefix_len, SH_TILE);
   const double move = (double)s.n_rows * hq * hd * 4 / BYTES;  // of one split's partials
   auto end = [&](long long n) {
-    const double count = (double)items * n;
-    const bool share = count + o_blocks > blocks / 2;
-    auto time = [&](double tiles) { return share ? 1.3 * tiles + 7 : tiles + 4; };
-    const double pt = time((double)kt / n), ot = o_blocks > 0 ? time(p.chunk_keys / SH_TILE) : 0;
-    double t = std::max(pt, ot);
-    if (count + o_blocks > blocks)
-      t = std::max((count * pt + o_blocks * ot) / blocks + 0.5 * std::min(pt, ot),
-                   std::ceil(count / blocks) * pt);
+    auto alone = [](double tiles) { return tiles + 4.3; };
+    auto shared = [](double tiles) { return 1.7 * tiles + 7.5; };
+    const double tiles = (double)kt / n, own = p.chunk_keys / SH_TILE;
+    const long long count = items * n, all = count + (long long)o_blocks;
+    double t;
+    if (all <= blocks / 2) {
+      t = std::max(alone(tiles), o_blocks > 0 ? alone(own) : 0);
+    } else if (all <= blocks) {
+      t = std::max(shared(tiles), o_blocks > 0 ? shared(own) : 0);
+    } else {
+      const long long rest = count % blocks;
+      t = count / blocks * shared(tiles);
+      if (rest) t += rest <= blocks / 2 && count > blocks ? alone(tiles) : shared(tiles);
+      if (o_blocks > 0) t += shared(own) * std::max(1.0, o_blocks / blocks);
+    }
     return t + move * n;
   };
   long long best = 1;
