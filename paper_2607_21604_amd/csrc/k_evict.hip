@@ -4,23 +4,24 @@
 
 namespace akvs {
 
-// Order of the weights as unsigned numbers: a NaN smallest, then -inf .. +inf, -0 as +0.
+// Order of the weights as unsigned numbers: 1 for a NaN, then -inf .. +inf, -0 as +0. (0 is
+// left for keys that are no candidates: -inf maps to 0x007fffff.)
 __device__ __forceinline__ uint32_t weight_key(float w) {
-  const uint32_t u = __float_as_uint(w);
-  if (w != w) return 0u;
-  if (u == 0x80000000u) return 0x80000000u;
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  const uint32_t u = __float_as_uint(w + 0.f);  // (-0 + 0 = +0)
+  const uint32_t k = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+  return w != w ? 1u : k;
 }
 
-// Block = one KV head of one sequence, NW waves; wave w has the keys [w * per, (w + 1) * per), in
-// registers where a lane's are at most R (R = 0: read again from cache in each pass). The
-// smallest kept candidate T is found a digit at a time (11, 11 and 10 bits): a histogram in LDS
-// of the candidates that agree with T so far, its counts summed from the top by all threads, and
-// the bin in which the count reaches what is wanted. Then each wave lists its kept keys in
-// order; of the keys equal to T the first are kept. Bound by its dozen barriers and the LDS
-// round trips between them.
+// Block = one KV head of one sequence, NW waves; wave w has the keys [w * per, (w + 1) * per), R
+// of a lane's at a time in registers (ONE: all of them, read once). The smallest kept candidate
+// T is found a digit at a time (11, 11 and 10 bits): a histogram in LDS of the candidates that
+// agree with T so far, its counts summed from the top by all threads, and the bin in which the
+// count reaches what is wanted. Then each wave lists its kept keys in order; of the keys equal
+// to T the first are kept. Short sequences are bound by a dozen barriers and the LDS round
+// trips between them (6 us at 300 keys, 11 at 4516), long ones by the instructions per key on
+// one compute unit; neither depends on how many heads there are up to 256.
 constexpr int EV_BINS = 2048;
-template <int NW, int R>
+template <int NW, int R, bool ONE>
 __global__ __launch_bounds__(NW * 64) void k_evict_select(const float *__restrict__ weights,
                                                           EvictArgs a, int hkv,
                                                           int32_t *__restrict__ keep,
@@ -37,32 +38,39 @@ __global__ __launch_bounds__(NW * 64) void k_evict_select(const float *__restric
   const int n = a.lens ? min(max(a.lens[seq], 0), a.n_keys) : a.n_keys;
   const int kept = min(n, a.n_keep);
   const bool all = n <= a.n_keep;
-  // candidates [c0, c1), of which `want` are kept; the keys beside them are kept
-  const int c0 = a.n_first, c1 = n - a.n_recent, want = a.n_keep - a.n_first - a.n_recent;
+  // candidates [c0, c1), of which `want` are kept; the keys beside them are kept, as is every key
+  // where there are no more than may be
+  const int want = a.n_keep - a.n_first - a.n_recent;
+  const int c0 = all ? n : a.n_first, c1 = all ? n : n - a.n_recent;
   const int steps = (n + T_ - 1) / T_, b0 = wave * steps * 64, b1 = min(b0 + steps * 64, n);
-  float reg[R ? R : 1];
-  if (R) {
+  uint32_t key[R];  // 0: no candidate
+  auto read = [&](int s0) __attribute__((always_inline)) {
+    float x[R];
 #pragma unroll
     for (int i = 0; i < R; ++i)
-      if (i < steps) reg[i] = w[min(b0 + i * 64 + lane, max(n - 1, 0))];
-  }
-  // f(step, key index, weight) over this wave's keys (indices from b1 on: none)
+      if (s0 + i < steps) x[i] = w[min(b0 + (s0 + i) * 64 + lane, n - 1)];
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+      if (s0 + i < steps) {
+        const int j = b0 + (s0 + i) * 64 + lane;
+        key[i] = j >= c0 && j < min(c1, b1) ? weight_key(x[i]) : 0u;
+      }
+  };
+  if (ONE) read(0);
+  // f(key index, key) over this wave's keys (indices from b1 on: none)
   auto each = [&](auto &&f) __attribute__((always_inline)) {
-    if (R) {
+    for (int s0 = 0; s0 < (ONE ? 1 : steps); s0 += R) {
+      if (!ONE) read(s0);
 #pragma unroll
       for (int i = 0; i < R; ++i)
-        if (i < steps) f(b0 + i * 64 + lane, reg[i]);
-    } else {
-      for (int i = 0; i < steps; ++i) {
-        const int j = b0 + i * 64 + lane;
-        f(j, w[min(j, n - 1)]);
-      }
+        if (s0 + i < steps) f(b0 + (s0 + i) * 64 + lane, key[i]);
     }
   };
-  uint32_t T = 0;
+  uint32_t T = 0xffffffffu;  // (no candidate is kept)
   int eq_take = 0;
   if (!all && want > 0) {
     int left = want;  // how many of the candidates that agree with T are kept
+    T = 0;
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
       const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
@@ -70,11 +78,8 @@ __global__ __launch_bounds__(NW * 64) void k_evict_select(const float *__restric
 #pragma unroll
       for (int i = 0; i < PER_T; ++i) hist[t + i * T_] = 0;
       __syncthreads();
-      each([&](int j, float x) {
-        const uint32_t u = weight_key(x);
-        // (a shift by 32 is none: the first pass takes all)
-        const bool agree = pass == 0 || (u >> (shift + bits)) == (T >> (shift + bits));
-        if (j >= c0 && j < min(c1, b1) && agree)
+      each([&](int, uint32_t u) {
+        if (u != 0 && (pass == 0 || ((u ^ T) >> (shift + bits)) == 0))
           atomicAdd(&hist[(u >> shift) & ((1u << bits) - 1)], 1);
       });
       __syncthreads();
@@ -109,19 +114,12 @@ __global__ __launch_bounds__(NW * 64) void k_evict_select(const float *__restric
     }
     eq_take = left;
   }
-  // 2: kept, 1: equal to T, 0: evicted
-  auto sort_of = [&](int j, float x) {
-    if (j >= b1) return 0;
-    if (all || j < c0 || j >= c1) return 2;
-    if (want <= 0) return 0;
-    const uint32_t u = weight_key(x);
-    return u > T ? 2 : u == T ? 1 : 0;
-  };
+  // kept without comparison: the keys beside the candidates
+  auto beside = [&](int j) { return j < b1 && (j < c0 || j >= c1); };
   int gt = 0, eq = 0;
-  each([&](int j, float x) {
-    const int k = sort_of(j, x);
-    gt += __popcll(__ballot(k == 2));
-    eq += __popcll(__ballot(k == 1));
+  each([&](int j, uint32_t u) {
+    gt += __popcll(__ballot(u > T || beside(j)));
+    eq += __popcll(__ballot(u == T));
   });
   if (lane == 0) {
     s_gt[wave] = gt;
@@ -134,15 +132,14 @@ __global__ __launch_bounds__(NW * 64) void k_evict_select(const float *__restric
     eqs += s_eq[v];
   }
   const unsigned long long below = (1ull << lane) - 1;
-  each([&](int j, float x) {
-    const int k = sort_of(j, x);
-    const unsigned long long e = __ballot(k == 1);
-    const bool take = k == 2 || (k == 1 && eqs + __popcll(e & below) < eq_take);
+  each([&](int j, uint32_t u) {
+    const unsigned long long e = __ballot(u == T);
+    const bool take = u > T || beside(j) || (u == T && eqs + __popcll(e & below) < eq_take);
     const unsigned long long m = __ballot(take);
     if (take) {
       const int i = at + __popcll(m & below);
       keep[i] = j;
-      if (w_out) w_out[i] = x;
+      if (w_out) w_out[i] = w[j];
     }
     at += __popcll(m);
     eqs += __popcll(e);
@@ -203,13 +200,13 @@ __global__ __launch_bounds__(256) void k_evict_gather(const u32x4_t *__restrict_
 hipError_t launch_evict_select(const float *weights, const EvictArgs &a, int hkv, int32_t *keep,
                                float *w_out, hipStream_t s) {
   const dim3 g((unsigned)(a.n_seq * hkv));
-#define AKVS_SELECT(NW_, R_)                                                                  \
-  hipLaunchKernelGGL((k_evict_select<NW_, R_>), g, dim3(NW_ * 64), 0, s, weights, a, hkv, keep, \
-                     w_out)
-  if (a.n_keys <= 2048) AKVS_SELECT(4, 8);
-  else if (a.n_keys <= 8192) AKVS_SELECT(16, 8);
-  else if (a.n_keys <= 32768) AKVS_SELECT(16, 32);
-  else AKVS_SELECT(16, 0);
+#define AKVS_SELECT(NW_, R_, ONE_)                                                              \
+  hipLaunchKernelGGL((k_evict_select<NW_, R_, ONE_>), g, dim3(NW_ * 64), 0, s, weights, a, hkv, \
+                     keep, w_out)
+  if (a.n_keys <= 2048) AKVS_SELECT(4, 8, true);
+  else if (a.n_keys <= 8192) AKVS_SELECT(16, 8, true);
+  else if (a.n_keys <= 32768) AKVS_SELECT(16, 32, true);
+  else AKVS_SELECT(16, 32, false);
 #undef AKVS_SELECT
   return hipGetLastError();
 }
