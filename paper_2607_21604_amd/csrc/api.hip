@@ -1665,8 +1665,11 @@ static akvs_status check_shared(const akvs_model_cfg *m, const akvs_shared_cfg *
           "without row_start every request has rows_max rows: n_rows %d is not %d * %d", c->n_rows,
           c->n_req, c->rows_max);
   REQUIRE(c->own_len || c->own_rows == 0, AKVS_EINVAL, "own_rows %d needs own_len", c->own_rows);
-  *s = {c->n_req,    c->n_rows,    c->rows_max, c->prefix_len,
-        c->own_rows, c->row_start, c->own_len};
+  const int rows_max = std::min(c->rows_max, std::max(c->n_rows, 1));
+  const long long tiles = ((long long)rows_max * (m->n_q_heads / m->n_kv_heads) + 15) / 16;
+  REQUIRE(tiles * c->n_req * m->n_kv_heads < (1LL << 30), AKVS_ESHAPE,
+          "batch too large: %d requests of up to %d rows", c->n_req, rows_max);
+  *s = {c->n_req, c->n_rows, rows_max, c->prefix_len, c->own_rows, c->row_start, c->own_len};
   return AKVS_OK;
 }
 
@@ -1784,7 +1787,8 @@ static akvs_status check_evict(const akvs_model_cfg *m, const akvs_evict_cfg *c,
         c->n_keep,  c->dst_rows ? c->dst_rows : c->n_keep,
         c->n_first, c->n_recent, c->lens};
   REQUIRE(a->n_seq < (1 << 16) && a->src_rows < (1 << 28) && a->dst_rows < (1 << 28) &&
-              (long long)a->n_seq * a->n_keep * m->n_kv_heads < (1LL << 31),
+              (long long)a->n_seq * a->n_keep * m->n_kv_heads < (1LL << 31) &&
+              (long long)a->n_keep * m->n_kv_heads * m->head_dim * es_of(m->dtype) < (1LL << 36),
           AKVS_ESHAPE, "too large");
   return AKVS_OK;
 }

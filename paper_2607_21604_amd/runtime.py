@@ -88,6 +88,153 @@ class Engine:
             s += n
         return kc, vc
 
+    # ---- a batch over one shared context ----------------------------------------------------
+
+    def _need(self, name: str, x, shape, dtype=None):
+        """A contiguous tensor of this shape (None: any size) and type on this engine's device."""
+        dtype = self.dtype if dtype is None else dtype
+        ok = x.dtype == dtype and x.dim() == len(shape) and x.is_contiguous() and all(
+            a == b for a, b in zip(x.shape, shape) if b is not None)
+        if not ok or x.device.type != self.device.type:
+            raise ValueError(f"{name}: need a contiguous {dtype} tensor "
+                             f"[{']['.join('n' if b is None else str(b) for b in shape)}] on "
+                             f"{self.device.type}, got {x.dtype} {tuple(x.shape)} on {x.device.type}")
+        return x
+
+    def qk_norm_rope(self, q, k, v, positions, q_norm, k_norm, rope, k_cache=None, v_cache=None,
+                     kv_rows=None, q_out=None):
+        """Per-head norms and rotation of new tokens' queries [n][Hq*hd] and keys [n][Hkv*hd]
+        (columns of a packed projection, or dense), their values copied: queries to q_out
+        [n][Hq][hd], keys and values to the rows kv_rows (int32 [n]) of k_cache / v_cache
+        [rows][Hkv][hd], or, without caches, to new tensors row by row. q_norm / k_norm [hd] or
+        None; rope: akvs_rope_table output. Returns (q_out, k, v)."""
+        sh, n = self.shape, int(q.shape[0])
+        for name, x, heads in (("q", q, sh.n_q_heads), ("k", k, sh.n_kv_heads),
+                               ("v", v, sh.n_kv_heads)):
+            if x.dtype != self.dtype or x.shape[0] != n or x[0:1].numel() not in (
+                    0, heads * sh.head_dim):
+                raise ValueError(f"{name}: need {n} {self.dtype} rows of {heads * sh.head_dim}")
+        self._need("positions", positions, (n,), torch.int32)
+        for name, x in (("q_norm", q_norm), ("k_norm", k_norm)):
+            if x is not None:
+                self._need(name, x, (sh.head_dim,))
+        self._need("rope", rope, (None, sh.head_dim // 2, 2), torch.float32)
+        if (k_cache is None) != (v_cache is None) or (k_cache is None and kv_rows is not None):
+            raise ValueError("k_cache, v_cache and kv_rows go together")
+        if k_cache is None:
+            k_cache = torch.empty((n, sh.n_kv_heads, sh.head_dim), dtype=self.dtype,
+                                  device=self.device)
+            v_cache = torch.empty_like(k_cache)
+        self._need("k_cache", k_cache, (None, sh.n_kv_heads, sh.head_dim))
+        self._need("v_cache", v_cache, tuple(k_cache.shape))
+        if kv_rows is not None:
+            self._need("kv_rows", kv_rows, (n,), torch.int32)
+        if q_out is None:
+            q_out = torch.empty((n, sh.n_q_heads, sh.head_dim), dtype=self.dtype,
+                                device=self.device)
+        self._need("q_out", q_out, (n, sh.n_q_heads, sh.head_dim))
+        akvs.akvs_qk_norm_rope(q, k, v, n, positions, q_norm, k_norm, self.m, rope,
+                               int(rope.shape[0]), kv_rows, int(k_cache.shape[0]), q_out, k_cache,
+                               v_cache)
+        return q_out, k_cache, v_cache
+
+    def _shared(self, q, k_prefix, k_own, own_len, row_start, rows_max):
+        """The batch that these tensors describe."""
+        sh, n = self.shape, int(q.shape[0])
+        self._need("q", q, (n, sh.n_q_heads, sh.head_dim))
+        self._need("k_prefix", k_prefix, (None, sh.n_kv_heads, sh.head_dim))
+        cap = 0
+        if k_own is not None:
+            self._need("k_own", k_own, (None, None, sh.n_kv_heads, sh.head_dim))
+            cap = int(k_own.shape[1])
+        if row_start is not None:
+            B = int(row_start.numel()) - 1
+        elif k_own is not None:
+            B = int(k_own.shape[0])
+        else:
+            B = 1
+        if k_own is not None and int(k_own.shape[0]) != B:
+            raise ValueError(f"k_own holds {int(k_own.shape[0])} requests, row_start {B}")
+        if cap:
+            if own_len is None:
+                raise ValueError("k_own needs own_len")
+            self._need("own_len", own_len, (B,), torch.int32)
+        if rows_max is None:
+            if row_start is None and n % max(B, 1):
+                raise ValueError(f"{n} rows of {B} requests need row_start")
+            rows_max = n if row_start is not None else n // max(B, 1)
+        return akvs.shared_cfg(B, n, max(int(rows_max), 1), int(k_prefix.shape[0]), cap, row_start,
+                               own_len if cap else None)
+
+    def shared_attention(self, q, k_prefix, v_prefix, k_own=None, v_own=None, own_len=None,
+                         row_start=None, rows_max=None, out=None, lse=None):
+        """Attention of a batch's rows q [n][Hq][hd] over a shared prefix [P][Hkv][hd] (one layer)
+        and each request's own keys [B][rows][Hkv][hd], the first own_len (int32 [B]) of them,
+        which end with the rows' own. row_start (int32 [B + 1]): the requests' rows (None: equally
+        many each); rows_max: the most of one request (None: all). Returns (out, lse)."""
+        c = self._shared(q, k_prefix, k_own, own_len, row_start, rows_max)
+        self._need("v_prefix", v_prefix, tuple(k_prefix.shape))
+        if (k_own is None) != (v_own is None):
+            raise ValueError("k_own and v_own go together")
+        if v_own is not None:
+            self._need("v_own", v_own, tuple(k_own.shape))
+        if out is None:
+            out = torch.empty_like(q)
+        if lse is None:
+            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=self.device)
+        self._need("out", out, tuple(q.shape))
+        self._need("lse", lse, tuple(q.shape[:2]), torch.float32)
+        ws = self.workspace(akvs.akvs_shared_workspace_size(self.m, c))
+        akvs.akvs_shared_attention(q, c, k_prefix, v_prefix, k_own, v_own, self.m, out, lse, ws)
+        return out, lse
+
+    def attention_weights(self, q, lse, k_prefix, k_own=None, own_len=None, row_start=None,
+                          rows_max=None, w_prefix=None, w_own=None):
+        """Adds the attention weights that the rows of a shared_attention call gave its keys to
+        w_prefix [Hkv][P] and (with k_own) w_own [B][Hkv][rows], fp32, made from 0 where they are
+        None. Returns (w_prefix, w_own)."""
+        c = self._shared(q, k_prefix, k_own, own_len, row_start, rows_max)
+        self._need("lse", lse, tuple(q.shape[:2]), torch.float32)
+        hkv = self.shape.n_kv_heads
+        shapes = [(hkv, c.prefix_len), (c.n_req, hkv, c.own_rows) if k_own is not None else None]
+        prev, w = [w_prefix, w_own], [w_prefix, w_own]
+        for i, shape in enumerate(shapes):
+            if w[i] is None and shape is not None:
+                w[i] = torch.empty(shape, dtype=torch.float32, device=self.device)
+            elif w[i] is not None:
+                if shape is None:
+                    raise ValueError("w_own needs k_own")
+                self._need(("w_prefix", "w_own")[i], w[i], shape, torch.float32)
+        ws = self.workspace(akvs.akvs_shared_workspace_size(self.m, c))
+        akvs.akvs_attention_weights(q, lse, c, k_prefix, k_own, self.m, prev[0], w[0], prev[1],
+                                    w[1], ws)
+        return w[0], w[1]
+
+    def evict_cache(self, k, v, weights, n_keep: int, n_first: int = 0, n_recent: int = 0,
+                    lens=None, dst_rows: int = 0):
+        """Caches [S][rows][Hkv][hd] cut to n_keep keys per sequence and KV head by weights
+        [S][Hkv][n]: the first n_first, the last n_recent and those of largest weight. lens
+        (int32 [S]): keys per sequence (None: n). The new caches have dst_rows (0: n_keep) rows,
+        zero past the kept ones. Returns (keep, k, v, weights, lens)."""
+        sh = self.shape
+        self._need("weights", weights, (None, sh.n_kv_heads, None), torch.float32)
+        S, n = int(weights.shape[0]), int(weights.shape[2])
+        self._need("k", k, (S, None, sh.n_kv_heads, sh.head_dim))
+        self._need("v", v, tuple(k.shape))
+        if int(k.shape[1]) < n:
+            raise ValueError(f"k holds {int(k.shape[1])} rows of {n} keys")
+        if lens is not None:
+            self._need("lens", lens, (S,), torch.int32)
+        c = akvs.evict_cfg(S, n, n_keep, n_first, n_recent, int(k.shape[1]), dst_rows, lens)
+        rows, dev = max(dst_rows, n_keep), self.device
+        keep = torch.empty((S, sh.n_kv_heads, n_keep), dtype=torch.int32, device=dev)
+        k_out = torch.zeros((S, rows, sh.n_kv_heads, sh.head_dim), dtype=self.dtype, device=dev)
+        v_out = torch.zeros_like(k_out)
+        w_out = torch.empty((S, sh.n_kv_heads, rows), dtype=torch.float32, device=dev)
+        lens_out = torch.empty(S, dtype=torch.int32, device=dev)
+        akvs.akvs_evict_cache(k, v, weights, c, self.m, keep, k_out, v_out, w_out, lens_out)
+        return keep, k_out, v_out, w_out, lens_out
+
     def reuse_prefill(self, tokens: torch.Tensor, chunk_lens: Sequence[int], query_len: int,
                       k_cache: torch.Tensor, v_cache: torch.Tensor, refresh=(1, 5),
                       check_layer: int = 1, flags: int = 0, k_meta=None, v_meta=None,

@@ -618,3 +618,115 @@ def test_decoding_over_a_context_that_is_cut(hq, hkv, hd, dt):
             akvs.akvs_evict_cache(ko, vo, wo, e, m, idx, k2, v2, w2, lens)
             assert lens.tolist() == [min(x, 8) for x in ln]
             ko, vo, wo = k2, v2, w2
+
+
+class _Shape:
+    def __init__(self, hq, hkv, hd, dt):
+        self.n_layers, self.d_model, self.ffn_dim, self.vocab = 1, 256, 256, 64
+        self.n_q_heads, self.n_kv_heads, self.head_dim = hq, hkv, hd
+        self.rope_theta, self.rms_eps = 1e4, 1e-6
+        self.dtype = "f32" if dt == F32 else "bf16"
+
+
+@pytest.mark.parametrize("hq,hkv,hd,dt", [(28, 4, 128, BF), (4, 2, 64, F32)])
+def test_engine_methods_are_the_entry_points(hq, hkv, hd, dt):
+    """The engine's methods give what the entry points give on the same tensors, over one
+    workspace that grows between calls."""
+    from paper_2607_21604_amd.runtime import Engine
+    eng = Engine(_Shape(hq, hkv, hd, dt), {"layers": [{k: torch.zeros(8, device=DEV) for k in (
+        "attn_norm", "w_qkv", "w_o", "mlp_norm", "w_gate_up", "w_down")}]}, DEV)
+    b = Batch(hq, hkv, hd, dt, 300, [2, 1, 7], [5, 1, 20], own_rows=24, seed=201)
+    tab, pos = rope(400, hd), ints(np.arange(b.n) + 300)
+    qkv = randn(202, b.n, (hq + 2 * hkv) * hd, dt=dt)
+    x = qkv.split([hq * hd, hkv * hd, hkv * hd], dim=1)
+    g = randn(203, hd, dt=dt)
+    slots = ints(np.concatenate([np.arange(n) + ln - n + 24 * i for i, (n, ln) in
+                                 enumerate(zip(b.rows, b.own_len))]))
+    q, k, v = eng.qk_norm_rope(*x, pos, g, g, tab, b.ko.view(-1, hkv, hd), b.vo.view(-1, hkv, hd),
+                               slots)
+    assert k.data_ptr() == b.ko.data_ptr()
+    q2, k2, v2 = eng.qk_norm_rope(*x, pos, g, g, tab)
+    assert torch.equal(q, q2) and torch.equal(k[slots.long()], k2) and torch.equal(v[slots.long()], v2)
+    b.q = q
+    b.attend()
+    b.check()
+    ln, st = ints(b.own_len), ints(b.start)
+    out, lse = eng.shared_attention(q, b.kp, b.vp, b.ko, b.vo, ln, st, 7)
+    assert torch.equal(out, b.out) and torch.equal(lse, b.lse)
+    wp, wo = eng.attention_weights(q, lse, b.kp, b.ko, ln, st)
+    ep, eo = weigh(b, False, 201)
+    assert torch.allclose(wp, ep, rtol=1e-5, atol=0) and torch.allclose(wo, eo, rtol=1e-5, atol=0)
+    wp2, _ = eng.attention_weights(q, lse, b.kp, w_prefix=wp.clone())
+    assert torch.allclose(wp2, 2 * wp, rtol=1e-5, atol=0)
+    o1, _ = eng.shared_attention(q[:3], b.kp, b.vp)
+    o2, _ = eng.shared_attention(q[:3], b.kp[:200].contiguous(), b.vp[:200].contiguous(),
+                                 b.kp[200:][None], b.vp[200:][None], ints([100]), ints([0, 3]))
+    assert o1.shape == o2.shape
+    keep, k, v, w, n = eng.evict_cache(b.ko, b.vo, wo, 4, 1, 2, ln, 24)
+    for i, own in enumerate(b.own_len):
+        for h in range(hkv):
+            want = ref.evict(wo[i, h, :own].tolist(), own, 4, 1, 2)
+            assert keep[i, h, :len(want)].tolist() == want and int(n[i]) == len(want)
+            assert torch.equal(k[i, :len(want), h], b.ko[i, want, h])
+            assert torch.equal(w[i, h, :len(want)], wo[i, h, want])
+
+
+# ---- many rows, long ranges: every split of the work ------------------------------------------
+
+def big_reference(b):
+    """As ref.attention, request by request in 64 bits on the GPU."""
+    G, P = b.hq // b.hkv, b.P
+    outs, lses, masses, reaches = [], [], [], []
+    wp = torch.zeros((b.hkv, P), dtype=torch.float64, device=DEV)
+    far = torch.zeros_like(wp)
+    for i, (n, ln) in enumerate(zip(b.rows, b.own_len)):
+        if n == 0:
+            continue
+        r0 = b.start[i]
+        k = torch.cat((b.kp, b.ko[i, :ln])).double().permute(1, 0, 2)
+        v = torch.cat((b.vp, b.vo[i, :ln])).double().permute(1, 0, 2)
+        q = b.q[r0:r0 + n].double().view(n, b.hkv, G, b.hd).permute(1, 0, 2, 3)
+        q = q.reshape(b.hkv, n * G, b.hd)
+        sc = torch.matmul(q, k.transpose(1, 2).contiguous()) / math.sqrt(b.hd)
+        reach = torch.matmul(q.abs(), k.abs().transpose(1, 2).contiguous()) / math.sqrt(b.hd)
+        seen = torch.arange(n, device=DEV).repeat_interleave(G) + P + ln - n + 1
+        sc = sc.masked_fill(torch.arange(P + ln, device=DEV)[None] >= seen[:, None], -math.inf)
+        lse = torch.logsumexp(sc, -1)
+        p = torch.exp(sc - lse[..., None])
+        rows = lambda t: t.view(b.hkv, n, G, -1).permute(1, 0, 2, 3).reshape(n, b.hq, -1)  # noqa: E731
+        outs.append(rows(torch.matmul(p, v)))
+        masses.append(rows(torch.matmul(p, v.abs())))
+        lses.append(rows(lse[..., None])[..., 0])
+        reaches.append(rows(reach.amax(-1, keepdim=True))[..., 0])
+        wp += p[..., :P].sum(1)
+        far += (p[..., :P] * (1 + reach[..., :P] + lse.abs()[..., None])).sum(1)
+    return torch.cat(outs), torch.cat(lses), torch.cat(masses), torch.cat(reaches), wp, far
+
+
+@pytest.mark.parametrize("hq,hkv,hd,dt,prefix,rows,own", [
+    (8, 8, 128, BF, 2100, [1] * 2100, [1] * 2100),       # two key tiles a wave in the weights
+    (40, 8, 128, BF, 1999, [120, 9, 77, 128, 100], [121, 100, 80, 300, 100]),
+    (12, 2, 64, BF, 4111, [64, 1, 50], [64, 1, 700]),
+    (16, 16, 64, BF, 3000, [700, 800], [700, 801]),
+    (28, 4, 128, F32, 1100, [30, 1, 64], [30, 200, 64]),
+    (8, 8, 64, F32, 1030, [1] * 1030, [2] * 1030),
+    (24, 8, 128, BF, 40000, [1, 1], [1, 3000])])
+def test_every_split(hq, hkv, hd, dt, prefix, rows, own):
+    """Sizes at which the prefix and the rows are cut in each way there is."""
+    b = Batch(hq, hkv, hd, dt, prefix, rows, own, seed=301)
+    b.attend()
+    out, lse, mass, reach, wp, far = big_reference(b)
+    keys = prefix + b.cap
+    err = (b.lse.double() - lse).abs()
+    assert bool((err <= ref.lse_bound(lse, reach, hd, keys)).all())
+    err = (b.out.double() - out).abs()
+    tol = ref.out_bound(out, mass, reach, hd, keys, dt)
+    assert bool((err <= tol).all()), float((err - tol).max())
+    c = b.cfg()
+    w = torch.empty((hkv, prefix), device=DEV)
+    akvs.akvs_attention_weights(b.q, b.lse, c, b.kp, b.ko, b.m, None, w, None, None, b.ws(c))
+    err = (w.double() - wp).abs()
+    # (by the kernel's own lse, off by lse_bound)
+    tol = ref.weights_bound(wp, far, hd, b.n * (hq // hkv)) + float(
+        ref.lse_bound(lse, reach, hd, keys).max()) * wp
+    assert bool((err <= tol).all()), float((err - tol).max())

@@ -33,6 +33,7 @@ SHARED = [
     (dict(prefix_len=1 << 28), akvs.AKVS_ESHAPE),
     (dict(n_req=1 << 10, n_rows=1 << 10, own_rows=1 << 22), akvs.AKVS_ESHAPE),
     (dict(n_rows=1 << 24, row_start=A), akvs.AKVS_ESHAPE),
+    (dict(n_req=1 << 18, n_rows=1 << 20, rows_max=1 << 20, row_start=A), akvs.AKVS_ESHAPE),
 ]
 
 
@@ -88,6 +89,14 @@ def test_null_and_misaligned_pointers(lib):
     assert lib.akvs_attention_weights(*bad) == akvs.AKVS_EINVAL
 
 
+def test_rows_max_above_the_rows_is_the_rows(lib):
+    """A batch that says more rows per request than there are asks for no more workspace."""
+    m = model()
+    a, b = (akvs.akvs_shared_workspace_size(m, shared(n_rows=6, row_start=A, rows_max=r))
+            for r in (6, 1 << 30))
+    assert a == b > 0
+
+
 def test_workspace(lib):
     for kw in (dict(), dict(prefix_len=8000), dict(own_rows=3000), dict(n_req=64, n_rows=64)):
         m, c = model(), shared(**kw)
@@ -105,7 +114,7 @@ def test_workspace(lib):
     (dict(n_keep=0), akvs.AKVS_EINVAL), (dict(n_first=-1), akvs.AKVS_EINVAL),
     (dict(n_recent=-1), akvs.AKVS_EINVAL), (dict(n_first=6, n_recent=5), akvs.AKVS_EINVAL),
     (dict(src_rows=99), akvs.AKVS_ESHAPE), (dict(dst_rows=9), akvs.AKVS_ESHAPE),
-    (dict(n_seq=1 << 17), akvs.AKVS_ESHAPE), (dict(n_first=1 << 30, n_recent=1 << 30), akvs.AKVS_EINVAL)])
+    (dict(n_seq=1 << 17), akvs.AKVS_ESHAPE), (dict(n_keep=1 << 27, n_seq=1), akvs.AKVS_ESHAPE), (dict(n_first=1 << 30, n_recent=1 << 30), akvs.AKVS_EINVAL)])
 def test_invalid_evictions(lib, kw, status):
     d = dict(n_seq=2, n_keys=100, src_rows=0, n_keep=10, dst_rows=0, n_first=0, n_recent=0, lens=None)
     d.update(kw)
@@ -175,3 +184,61 @@ def test_binding_refuses_wrong_tables_and_rows():
         akvs.rows_ptr(x[:, :, :8])
     with pytest.raises(ValueError):
         akvs.rows_ptr(x.transpose(0, 1))
+
+
+class _Shape:
+    n_layers, d_model, n_q_heads, n_kv_heads, head_dim, ffn_dim, vocab = 1, 256, 6, 2, 64, 256, 64
+    rope_theta, rms_eps, dtype = 1e4, 1e-6, "bf16"
+
+
+@pytest.fixture(scope="module")
+def engine(lib):
+    from paper_2607_21604_amd.runtime import Engine
+    w = {k: torch.zeros(8) for k in ("attn_norm", "w_qkv", "w_o", "mlp_norm", "w_gate_up", "w_down")}
+    return Engine(_Shape, {"layers": [w]}, "cpu")
+
+
+def bf(*shape):
+    return torch.zeros(shape, dtype=torch.bfloat16)
+
+
+def i32(*v):
+    return torch.tensor(v, dtype=torch.int32)
+
+
+def test_engine_refuses_wrong_tensors(engine):
+    """Shapes and types that the C entries cannot see are refused by the engine's methods."""
+    q, kp, ko, ln = bf(3, 6, 64), bf(10, 2, 64), bf(3, 8, 2, 64), i32(1, 2, 3)
+    for args in ((q.float(), kp, kp), (q, kp.float(), kp), (q, kp, bf(9, 2, 64)),
+                 (q, kp, kp, ko, None, ln), (q, kp, kp, ko, bf(3, 7, 2, 64), ln),
+                 (q, kp, kp, ko, ko), (q, kp, kp, ko, ko, i32(1, 2)),
+                 (q, kp, kp, ko, ko, ln.long()), (q, kp, kp, ko, ko, ln, i32(0, 1, 3)),
+                 (bf(4, 6, 64), kp, kp, ko, ko, ln), (q.transpose(1, 2), kp, kp)):
+        with pytest.raises(ValueError):
+            engine.shared_attention(*args)
+    with pytest.raises(ValueError):
+        engine.shared_attention(q, kp, kp, out=bf(2, 6, 64))
+    lse = torch.zeros(3, 6)
+    for kw in (dict(lse=lse.double()), dict(w_prefix=torch.zeros(2, 9)),
+               dict(w_own=torch.zeros(3, 2, 8)), dict(k_own=ko, own_len=ln, w_own=torch.zeros(3, 2, 7))):
+        a = dict(lse=lse)
+        a.update(kw)
+        with pytest.raises(ValueError):
+            engine.attention_weights(q, a.pop("lse"), kp, **a)
+    k, w = bf(2, 30, 2, 64), torch.zeros(2, 2, 30)
+    for args in ((k.float(), k, w, 5), (k, bf(2, 29, 2, 64), w, 5), (k, k, w.double(), 5),
+                 (k, k, torch.zeros(2, 3, 30), 5), (k, k, w, 5, 0, 0, i32(1)),
+                 (bf(2, 20, 2, 64), bf(2, 20, 2, 64), w, 5)):
+        with pytest.raises(ValueError):
+            engine.evict_cache(*args)
+    rope, pos = torch.zeros(5, 32, 2), i32(0, 1, 2)
+    for args in ((q, bf(3, 128), bf(3, 127), pos, None, None, rope),
+                 (q.float(), bf(3, 128), bf(3, 128), pos, None, None, rope),
+                 (q, bf(3, 128), bf(2, 128), pos, None, None, rope),
+                 (q, bf(3, 128), bf(3, 128), pos.long(), None, None, rope),
+                 (q, bf(3, 128), bf(3, 128), pos, bf(63), None, rope),
+                 (q, bf(3, 128), bf(3, 128), pos, None, None, rope, bf(9, 2, 64)),
+                 (q, bf(3, 128), bf(3, 128), pos, None, None, rope, None, None, pos),
+                 (q, bf(3, 128), bf(3, 128), pos, None, None, torch.zeros(5, 64, 2))):
+        with pytest.raises(ValueError):
+            engine.qk_norm_rope(*args)
