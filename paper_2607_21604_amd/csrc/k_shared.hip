@@ -35,22 +35,27 @@ struct SharedPlan {
   int p_pairs, p_tiles, splits, split_keys, prefix_blocks;  // pairs of a tile, tiles, ..
   int o_pairs, o_tiles, chunks, chunk_keys;
   int slots;  // partials per (row, head): splits + chunks
+  bool whole;  // no prefix items: a request's items take the prefix's keys, then its own
 };
 constexpr int SH_TILE = 64;  // keys of an LDS tile
 
-// The item that a block serves: `pairs` pairs from v0 of rows [r0, r1), keys [k0, k1) of (K, V) rows from
-// `base`. own = -1: prefix (every row sees all of it), else the request's own keys.
+// The item that a block serves: `pairs` pairs from v0 of rows [r0, r1), keys [k0, k1). own = -1:
+// the prefix's keys, which every row sees; else the request's own, rows from `base` of their
+// tensors. A whole item numbers its keys so that tiles hold one kind: [0, first) are the
+// prefix's, own key j is shift + j, shift the next multiple of a tile (else both are 0).
 struct SharedItem {
-  int kvh, r0, r1, v0, pairs, k0, k1, slot, own;
+  int kvh, r0, r1, v0, pairs, k0, k1, slot, own, first, shift;
   size_t base;
 };
+template <bool WHOLE>
 __device__ __forceinline__ bool shared_item(const SharedBatch &s, const SharedPlan &p, int hkv,
                                             int G, SharedItem &it) {
   int id = blockIdx.x;
-  const bool prefix = id < p.prefix_blocks;
-  if (!prefix) id -= p.prefix_blocks;
+  const bool prefix = !WHOLE && id < p.prefix_blocks;
+  if (!WHOLE && !prefix) id -= p.prefix_blocks;
   it.kvh = id % hkv;
   id /= hkv;
+  it.first = it.shift = 0;
   if (prefix) {
     const int tile = id % p.p_tiles, split = id / p.p_tiles;
     it.pairs = p.p_pairs;
@@ -74,13 +79,18 @@ __device__ __forceinline__ bool shared_item(const SharedBatch &s, const SharedPl
     it.k1 = min(it.own, it.k0 + p.chunk_keys);
     it.slot = p.splits + chunk;
     it.base = (size_t)b * s.own_rows;
+    if (WHOLE) {
+      it.first = s.prefix_len;
+      it.shift = (s.prefix_len + SH_TILE - 1) / SH_TILE * SH_TILE;
+      it.k1 = it.own > 0 ? it.shift + it.own : it.first;
+    }
   }
   return it.v0 < (it.r1 - it.r0) * G;
 }
-// Keys that row r (of the item's rows) sees.
+// The end of the keys that row r (of the item's rows) sees.
 __device__ __forceinline__ int shared_seen(const SharedItem &it, int r) {
-  if (it.own < 0) return it.k1;
-  return min(max(it.own - (it.r1 - r) + 1, 0), it.k1);
+  const int own = it.own - (it.r1 - r) + 1;
+  return it.own < 0 ? it.k1 : own > 0 ? min(it.shift + own, it.k1) : it.first;
 }
 
 __device__ __forceinline__ bool odd_bf16(uint32_t lo16) { return (lo16 & 0x7f80u) == 0x7f80u; }
@@ -93,7 +103,7 @@ __device__ __forceinline__ bool odd_bf16(uint32_t lo16) { return (lo16 & 0x7f80u
 // layout of O^T = V^T P^T; V^T comes from row-major rows by the transposing LDS read. Softmax
 // statistics and outputs are fp32; the probabilities are rounded to bf16 for the second
 // product (the matrix cores' type), their sum is not.
-template <int HD>
+template <int HD, bool WHOLE>
 __global__ __launch_bounds__(256, 2) void k_shared_bf16(
     SharedBatch s, SharedPlan p, const bf16_t *__restrict__ Q, const bf16_t *__restrict__ Kp,
     const bf16_t *__restrict__ Vp, const bf16_t *__restrict__ Ko, const bf16_t *__restrict__ Vo,
@@ -108,7 +118,7 @@ __global__ __launch_bounds__(256, 2) void k_shared_bf16(
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hi = lane >> 5;
   const int G = hq / hkv;
   SharedItem it;
-  if (!shared_item(s, p, hkv, G, it)) return;
+  if (!shared_item<WHOLE>(s, p, hkv, G, it)) return;
   const bf16_t *K = it.own < 0 ? Kp : Ko, *V = it.own < 0 ? Vp : Vo;
   // this wave's pairs and its share of a tile's two 32-key halves
   const int groups = it.pairs >> 5;
@@ -150,11 +160,13 @@ __global__ __launch_bounds__(256, 2) void k_shared_bf16(
   u32x4_t kreg[NCH], vreg[NCH];
   const uint32_t row_bytes = hkv * HD * 2;
   const uint32_t off0 = tid / CPK * row_bytes + tid % CPK * 16;
-  const size_t start = (it.base * hkv + it.kvh) * (HD * 2);
   auto load = [&](int key0) __attribute__((always_inline)) {
-    const char *kt = reinterpret_cast<const char *>(K) + start + (size_t)key0 * row_bytes;
-    const char *vt = reinterpret_cast<const char *>(V) + start + (size_t)key0 * row_bytes;
-    const int end = k1 - 1 - key0;  // the range's last key, which keys past it re-read
+    const bool pre = WHOLE && key0 < it.shift;
+    const size_t at = pre ? key0 : it.base + key0 - it.shift;
+    const size_t start = at * row_bytes + it.kvh * (HD * 2);
+    const char *kt = reinterpret_cast<const char *>(pre ? Kp : K) + start;
+    const char *vt = reinterpret_cast<const char *>(pre ? Vp : V) + start;
+    const int end = (pre ? it.first : k1) - 1 - key0;  // the last key, which keys past it re-read
     if (end >= SH_TILE - 1) {
 #pragma unroll
       for (int i = 0; i < NCH; ++i) {
@@ -177,11 +189,12 @@ __global__ __launch_bounds__(256, 2) void k_shared_bf16(
   // added at the end.
   auto store = [&](int key0, int buf) __attribute__((always_inline)) {
     bf16_t *ks = s_kv + buf * (KB + VB), *vs = ks + KB;
-    const bool some_hidden = key0 + SH_TILE > all_see;
+    const int all = WHOLE && key0 < it.shift ? it.first : all_see;
+    const bool some_hidden = key0 + SH_TILE > all;
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
       const int c = tid + 256 * i, kr = c / CPK, e0 = (c % CPK) * 8;
-      if (some_hidden && key0 + kr >= all_see) {
+      if (some_hidden && key0 + kr >= all) {
         bool odd = false;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -238,8 +251,9 @@ __global__ __launch_bounds__(256, 2) void k_shared_bf16(
           __builtin_memcpy(&vf[t][db], &x0, 8);
           __builtin_memcpy(reinterpret_cast<char *>(&vf[t][db]) + 8, &x1, 8);
         }
-      if (sk0 + 32 > all_see) {
-        const int lim = seen - (sk0 + hi * 4);
+      const bool pre = WHOLE && key0 < it.shift;
+      if (sk0 + 32 > (pre ? it.first : all_see)) {
+        const int lim = (pre ? it.first : seen) - (sk0 + hi * 4);
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           if ((i >> 2) * 8 + (i & 3) >= lim) sc[i] = -INFINITY;
@@ -305,8 +319,8 @@ __global__ __launch_bounds__(256, 2) void k_shared_bf16(
   }
   if (!valid) return;
   if (s_odd) {  // values left out above that this pair sees
-    for (int k = max(it.k0, all_see); k < seen; ++k) {
-      const bf16_t *vr = V + ((it.base + k) * hkv + it.kvh) * HD + hi * 4;
+    for (int k = max(max(it.k0, it.shift), all_see); k < seen; ++k) {
+      const bf16_t *vr = V + ((it.base + k - it.shift) * hkv + it.kvh) * HD + hi * 4;
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -508,7 +522,7 @@ __device__ __forceinline__ bool odd_f32(float x) {
 // registers, a tile ahead. Scores are formed transposed: lane l holds the scores of pair l % 16
 // at keys 4 (l / 16) + 0..3 of the tile, the operand layout of O^T = V^T P^T as it is; row
 // l % 16 of V^T block c stands for dim (l % 16) * C + c, so that a lane's values are contiguous.
-template <int HD>
+template <int HD, bool WHOLE>
 __global__ __launch_bounds__(256, 2) void k_shared_f32(
     SharedBatch s, SharedPlan p, const float *__restrict__ Q, const float *__restrict__ Kp,
     const float *__restrict__ Vp, const float *__restrict__ Ko, const float *__restrict__ Vo,
@@ -521,7 +535,7 @@ __global__ __launch_bounds__(256, 2) void k_shared_f32(
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int lr = lane & 15, lg = lane >> 4, G = hq / hkv;
   SharedItem it;
-  if (!shared_item(s, p, hkv, G, it)) return;
+  if (!shared_item<WHOLE>(s, p, hkv, G, it)) return;
   const float *K = it.own < 0 ? Kp : Ko, *V = it.own < 0 ? Vp : Vo;
   const int n_pairs = (it.r1 - it.r0) * G, v = it.v0 + lr;
   const bool valid = v < n_pairs;
@@ -551,14 +565,19 @@ __global__ __launch_bounds__(256, 2) void k_shared_f32(
     f32x4_t k[C];
     float v[4][C];
   };
-  auto fetch = [&](Tile &t, int key0) __attribute__((always_inline)) {  // past k1: the last key
-    const float *k = K + ((it.base + min(key0 + lr, k1 - 1)) * hkv + it.kvh) * HD + lg * 4;
+  // keys past the last one re-read it
+  auto fetch = [&](Tile &t, int key0) __attribute__((always_inline)) {
+    const bool pre = WHOLE && key0 < it.shift;
+    const float *kb = pre ? Kp : K, *vb = pre ? Vp : V;
+    const int end = (pre ? it.first : k1) - 1;
+    const size_t base = pre ? 0 : it.base - it.shift;  // (wraps; key + base does not)
+    const float *k = kb + ((base + min(key0 + lr, end)) * hkv + it.kvh) * HD + lg * 4;
 #pragma unroll
     for (int c = 0; c < C; ++c) t.k[c] = *reinterpret_cast<const f32x4_t *>(k + 16 * c);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float *x =
-          V + ((it.base + min(key0 + lg * 4 + e, k1 - 1)) * hkv + it.kvh) * HD + lr * C;
+          vb + ((base + min(key0 + lg * 4 + e, end)) * hkv + it.kvh) * HD + lr * C;
 #pragma unroll
       for (int c = 0; c < C; c += 4)
         *reinterpret_cast<f32x4_t *>(&t.v[e][c]) = *reinterpret_cast<const f32x4_t *>(x + c);
@@ -574,14 +593,16 @@ __global__ __launch_bounds__(256, 2) void k_shared_f32(
         s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(t.k[c][e + 1], qf[c][e + 1], s1, 0, 0, 0);
       }
     f32x4_t x = s0 + s1;
+    const bool pre = WHOLE && key0 < it.shift;
+    const int see = pre ? it.first : seen, all = pre ? it.first : all_see;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      x[e] = key0 + lg * 4 + e < seen ? x[e] * scale_log2 : -INFINITY;
-    if (key0 + 16 > all_see) {  // a hidden value that is not finite must not meet p = 0
+      x[e] = key0 + lg * 4 + e < see ? x[e] * scale_log2 : -INFINITY;
+    if (key0 + 16 > all) {  // a hidden value that is not finite must not meet p = 0
       bool odd = false;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (key0 + lg * 4 + e >= all_see) {
+        if (key0 + lg * 4 + e >= all) {
 #pragma unroll
           for (int c = 0; c < C; ++c)
             if (odd_f32(t.v[e][c])) {
@@ -656,8 +677,8 @@ __global__ __launch_bounds__(256, 2) void k_shared_f32(
     }
     if (s_odd) {  // values left out above that this pair sees
       const int end = shared_seen(it, ri);
-      for (int k = max(it.k0, all_see); k < end; ++k) {
-        const float *x = V + ((it.base + k) * hkv + it.kvh) * HD + lane;
+      for (int k = max(max(it.k0, it.shift), all_see); k < end; ++k) {
+        const float *x = V + ((it.base + k - it.shift) * hkv + it.kvh) * HD + lane;
 #pragma unroll
         for (int c = 0; c < HD / 64; ++c)
           if (odd_f32(x[64 * c])) so[c] += x[64 * c];
@@ -930,6 +951,10 @@ __global__ __launch_bounds__(256) void k_weight_parts(const float *__restrict__ 
 // that shares its unit 7.5 + 1.7 times them. Blocks that fit the chip together end with the
 // longest of them; else whole rounds of prefix blocks, the rest of them, and the own keys'
 // blocks that had no place follow each other. Each split's partials cost a write and a read.
+// Up to five tiles of prefix and own keys together, each request's blocks take both (whole) and
+// there is nothing to merge: 16 requests over 60 / 190 / 320 / 450 keys and up to 64 own of 28/4
+// heads 7.9 / 10.0 / 12.0 / 15.9 us whole, 10.8 / 13.8 / 14.0 / 13.3 in pieces (fp32, 4 heads of 64:
+// 6.9 / 8.5 / 10.1 / 13.0 and 9.3 / 11.0 / 11.0 / 11.2).
 //   16 rows over 4096 / 8192 / 16384 / 32768 / 65536 keys of 40/8 heads, this launch alone: 256
 //   prefix blocks 11.1 / 14.6 / 21.0 / 34.9 / 62.7 us, 512 of them - / 19.6 / 23.3 / 37.1 / 60.8;
 //   with 128 blocks of own keys and 16128 keys 256 prefix blocks are 4 us faster than 504 (own
@@ -957,6 +982,13 @@ static SharedPlan shared_plan(const SharedBatch &s, int hq, int hkv, int hd, int
   };
   const long long o_items = s.own_rows ? (long long)s.n_req * p.o_tiles * hkv : 0;
   cut(o_items ? blocks / o_items : 1, tiles_of(s.own_rows, SH_TILE), &p.chunks, &p.chunk_keys);
+  const int ot = tiles_of(s.own_rows, SH_TILE);
+  p.whole = s.prefix_len > 0 && o_items > 0 && o_items <= blocks &&
+            tiles_of(s.prefix_len, SH_TILE) + ot <= 5;
+  if (p.whole) {
+    p.chunks = p.slots = 1;
+    return p;
+  }
   const double o_blocks = (double)o_items * p.chunks;
   const long long items = (long long)p.p_tiles * hkv;
   const int kt = tiles_of(s.prefix_len, SH_TILE);
@@ -977,7 +1009,7 @@ static SharedPlan shared_plan(const SharedBatch &s, int hq, int hkv, int hd, int
       if (rest) t += rest <= blocks / 2 && count > blocks ? alone(tiles) : shared(tiles);
       if (o_blocks > 0) t += shared(own) * std::max(1.0, o_blocks / blocks);
     }
-    return t + move * n;
+    return t + move * n + (n + p.chunks > 1 ? 3 : 0);
   };
   long long best = 1;
   const long long most = std::max(1, std::min(MERGE_SLOTS / 2, kt / 2));
@@ -1023,12 +1055,17 @@ static hipError_t shared_attention(const SharedBatch &s, const void *q, const vo
   }
   const dim3 g((unsigned)blocks), b(256);
   const float scale = 1.4426950408889634f / sqrtf((float)HD);
-  if constexpr (sizeof(TS) == 2)
-    hipLaunchKernelGGL(k_shared_bf16<HD>, g, b, 0, st, s, p, x(q), x(kp), x(vp), x(ko), x(vo), hq,
-                       hkv, scale, O, lse, po, ml);
-  else
-    hipLaunchKernelGGL(k_shared_f32<HD>, g, b, 0, st, s, p, x(q), x(kp), x(vp), x(ko), x(vo), hq,
-                       hkv, scale, O, lse, po, ml);
+#define AKVS_ATTEND(KERNEL_)                                                                      \
+  hipLaunchKernelGGL(KERNEL_, g, b, 0, st, s, p, x(q), x(kp), x(vp), x(ko), x(vo), hq, hkv, scale, O, \
+                     lse, po, ml)
+  if constexpr (sizeof(TS) == 2) {
+    if (p.whole) AKVS_ATTEND((k_shared_bf16<HD, true>));
+    else AKVS_ATTEND((k_shared_bf16<HD, false>));
+  } else {
+    if (p.whole) AKVS_ATTEND((k_shared_f32<HD, true>));
+    else AKVS_ATTEND((k_shared_f32<HD, false>));
+  }
+#undef AKVS_ATTEND
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.slots <= 1) return e;
   if (p.slots <= MERGE_FEW)
