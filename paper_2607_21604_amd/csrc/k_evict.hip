@@ -5,7 +5,8 @@
 namespace akvs {
 
 // Order of the weights as unsigned numbers: 1 for a NaN, then -inf .. +inf, -0 as +0. (0 is
-// left for keys that are no candidates: -inf maps to 0x007fffff.)
+// left for what is no key and 0xffffffff for keys that are kept without comparison: -inf maps to
+// 0x007fffff, +inf to 0xff800000.)
 __device__ __forceinline__ uint32_t weight_key(float w) {
   const uint32_t u = __float_as_uint(w + 0.f);  // (-0 + 0 = +0)
   const uint32_t k = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
@@ -28,8 +29,8 @@ __global__ __launch_bounds__(NW * 64) void k_evict_select(const float *__restric
                                                           float *__restrict__ w_out) {
   constexpr int T_ = NW * 64, PER_T = EV_BINS / T_;
   __shared__ int hist[EV_BINS];
-  __shared__ int s_wave[NW], s_pick[2];
-  __shared__ int s_gt[NW], s_eq[NW];
+  __shared__ __attribute__((aligned(16))) int s_wave[NW], s_gt[NW], s_eq[NW];
+  __shared__ int s_pick[2];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int seq = blockIdx.x / hkv;
   const float *w = weights + (size_t)blockIdx.x * a.n_keys;
@@ -43,7 +44,7 @@ __global__ __launch_bounds__(NW * 64) void k_evict_select(const float *__restric
   const int want = a.n_keep - a.n_first - a.n_recent;
   const int c0 = all ? n : a.n_first, c1 = all ? n : n - a.n_recent;
   const int steps = (n + T_ - 1) / T_, b0 = wave * steps * 64, b1 = min(b0 + steps * 64, n);
-  uint32_t key[R];  // 0: no candidate
+  uint32_t key[R];
   auto read = [&](int s0) __attribute__((always_inline)) {
     float x[R];
 #pragma unroll
@@ -53,7 +54,8 @@ __global__ __launch_bounds__(NW * 64) void k_evict_select(const float *__restric
     for (int i = 0; i < R; ++i)
       if (s0 + i < steps) {
         const int j = b0 + (s0 + i) * 64 + lane;
-        key[i] = j >= c0 && j < min(c1, b1) ? weight_key(x[i]) : 0u;
+        key[i] = j >= c0 && j < c1 ? weight_key(x[i]) : 0xffffffffu;
+        if (j >= b1) key[i] = 0u;
       }
   };
   if (ONE) read(0);
@@ -66,7 +68,7 @@ __global__ __launch_bounds__(NW * 64) void k_evict_select(const float *__restric
         if (s0 + i < steps) f(b0 + (s0 + i) * 64 + lane, key[i]);
     }
   };
-  uint32_t T = 0xffffffffu;  // (no candidate is kept)
+  uint32_t T = 0xfffffffeu;  // (no candidate is kept)
   int eq_take = 0;
   if (!all && want > 0) {
     int left = want;  // how many of the candidates that agree with T are kept
@@ -79,7 +81,8 @@ __global__ __launch_bounds__(NW * 64) void k_evict_select(const float *__restric
       for (int i = 0; i < PER_T; ++i) hist[t + i * T_] = 0;
       __syncthreads();
       each([&](int, uint32_t u) {
-        if (u != 0 && (pass == 0 || ((u ^ T) >> (shift + bits)) == 0))
+        // (what is no candidate agrees with no T but the smallest)
+        if (pass == 0 ? u - 1 < 0xfffffffeu : (u ^ T) < (1u << (shift + bits)) && u != 0)
           atomicAdd(&hist[(u >> shift) & ((1u << bits) - 1)], 1);
       });
       __syncthreads();
@@ -98,8 +101,11 @@ __global__ __launch_bounds__(NW * 64) void k_evict_select(const float *__restric
       }
       if (lane == 63) s_wave[wave] = upto;
       __syncthreads();
-      int above = upto - mine;
-      for (int v = 0; v < wave; ++v) above += s_wave[v];
+      int above = upto - mine, before[NW];
+#pragma unroll
+      for (int v = 0; v < NW; ++v) before[v] = s_wave[v];
+#pragma unroll
+      for (int v = 0; v < NW; ++v) above += v < wave ? before[v] : 0;
 #pragma unroll
       for (int i = 0; i < PER_T; ++i) {
         if (above < left && above + h[i] >= left) {  // (one bin of one thread)
@@ -114,35 +120,49 @@ __global__ __launch_bounds__(NW * 64) void k_evict_select(const float *__restric
     }
     eq_take = left;
   }
-  // kept without comparison: the keys beside the candidates
-  auto beside = [&](int j) { return j < b1 && (j < c0 || j >= c1); };
   int gt = 0, eq = 0;
-  each([&](int j, uint32_t u) {
-    gt += __popcll(__ballot(u > T || beside(j)));
-    eq += __popcll(__ballot(u == T));
+  each([&](int, uint32_t u) {
+    gt += u > T;
+    eq += u == T;
   });
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    gt += __shfl_xor(gt, o, 64);
+    eq += __shfl_xor(eq, o, 64);
+  }
   if (lane == 0) {
     s_gt[wave] = gt;
     s_eq[wave] = eq;
   }
   __syncthreads();
   int at = 0, eqs = 0;  // kept keys and keys equal to T before this wave's
-  for (int v = 0; v < wave; ++v) {
-    at += s_gt[v] + min(s_eq[v], max(eq_take - eqs, 0));
-    eqs += s_eq[v];
+  int gts[NW], es[NW];
+#pragma unroll
+  for (int v = 0; v < NW; ++v) {
+    gts[v] = s_gt[v];
+    es[v] = s_eq[v];
   }
-  const unsigned long long below = (1ull << lane) - 1;
+#pragma unroll
+  for (int v = 0; v < NW; ++v)
+    if (v < wave) {
+      at += gts[v] + min(es[v], max(eq_take - eqs, 0));
+      eqs += es[v];
+    }
   each([&](int j, uint32_t u) {
+    unsigned long long m = __ballot(u > T);
     const unsigned long long e = __ballot(u == T);
-    const bool take = u > T || beside(j) || (u == T && eqs + __popcll(e & below) < eq_take);
-    const unsigned long long m = __ballot(take);
+    bool take = u > T;
+    if (e) {  // (few steps have one)
+      take |= u == T && eqs + (int)__popcll(e & ((1ull << lane) - 1)) < eq_take;
+      m = __ballot(take);
+      eqs += __popcll(e);
+    }
     if (take) {
-      const int i = at + __popcll(m & below);
+      const int i = at + (int)__popcll(m & ((1ull << lane) - 1));
       keep[i] = j;
       if (w_out) w_out[i] = w[j];
     }
     at += __popcll(m);
-    eqs += __popcll(e);
   });
   for (int i = kept + t; i < a.n_keep; i += T_) keep[i] = -1;
   if (w_out)
@@ -195,15 +215,14 @@ __global__ __launch_bounds__(256) void k_evict_gather(const u32x4_t *__restrict_
     }
 }
 
-// Few keys: four waves (barriers of 4 waves cost less than of 16, and short sequences have few
-// keys a lane either way).
+// Few keys: eight waves (300 / 1500 keys 5.2 / 7.1 us, with four 5.7 / 8.5, with sixteen 6.4 / 7.9).
 hipError_t launch_evict_select(const float *weights, const EvictArgs &a, int hkv, int32_t *keep,
                                float *w_out, hipStream_t s) {
   const dim3 g((unsigned)(a.n_seq * hkv));
 #define AKVS_SELECT(NW_, R_, ONE_)                                                              \
   hipLaunchKernelGGL((k_evict_select<NW_, R_, ONE_>), g, dim3(NW_ * 64), 0, s, weights, a, hkv, \
                      keep, w_out)
-  if (a.n_keys <= 2048) AKVS_SELECT(4, 8, true);
+  if (a.n_keys <= 2048) AKVS_SELECT(8, 4, true);
   else if (a.n_keys <= 8192) AKVS_SELECT(16, 8, true);
   else if (a.n_keys <= 32768) AKVS_SELECT(16, 32, true);
   else AKVS_SELECT(16, 32, false);
