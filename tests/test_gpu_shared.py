@@ -438,6 +438,26 @@ def test_qk_norm_rope_extremes():
     assert bool(torch.isfinite(ko).all())
 
 
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("eps", [0.0, 1e-6])
+def test_qk_norm_of_squares_that_leave_the_range(dt, eps):
+    """Rows of 1e25 and, without an eps, of 1e-25: their squares are no fp32 numbers, their
+    norms are; next to ordinary rows of the same wave."""
+    m = model(4, 2, 128, dt)
+    m.rms_eps = eps
+    tab, n = rope(8, 128), 5
+    q, k = randn(1, n, 4, 128, dt=dt), randn(2, n, 2, 128, dt=dt)
+    q[1] *= 1e25
+    q[3] *= 1e25 if eps else 1e-25
+    g = randn(3, 128, dt=dt)
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    akvs.akvs_qk_norm_rope(q, k, None, n, ints(np.arange(n)), g, g, m, tab, 8, None, n, qo, ko, None)
+    cs = tab.cpu()[np.arange(n)]
+    for got, x in ((qo, q), (ko, k)):
+        want, mags = ref.norm_rope(x, g, cs[..., 0], cs[..., 1], eps)
+        close_rotated(got, want, mags, dt)
+
+
 # ---- eviction -------------------------------------------------------------------------------
 
 class Evict:
