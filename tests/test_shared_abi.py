@@ -90,11 +90,15 @@ def test_null_and_misaligned_pointers(lib):
 
 
 def test_rows_max_above_the_rows_is_the_rows(lib):
-    """A batch that says more rows per request than there are asks for no more workspace."""
+    """A batch that says more rows per request than there are asks for no more workspace.
+    (A short context is taken whole and needs none; a long one is split.)"""
     m = model()
-    a, b = (akvs.akvs_shared_workspace_size(m, shared(n_rows=6, row_start=A, rows_max=r))
-            for r in (6, 1 << 30))
-    assert a == b > 0
+    for prefix in (100, 8000):
+        a, b = (akvs.akvs_shared_workspace_size(m, shared(n_rows=6, row_start=A, rows_max=r,
+                                                          prefix_len=prefix))
+                for r in (6, 1 << 30))
+        assert a == b
+        assert (a > 0) == (prefix == 8000)
 
 
 def test_workspace(lib):
