@@ -139,7 +139,7 @@ typedef struct akvs_shared_cfg {
   int32_t own_rows;     /* rows per request of k_own / v_own, >= 0 (0: none)                 */
   const int32_t *row_start; /* device [B + 1], from 0, ascending, <= n_rows: request b has rows
                                row_start[b] .. row_start[b + 1] - 1, at most rows_max of them.
-                               NULL: every request has rows_max (n_rows = B * rows_max)        */
+                               NULL: every request has rows_max (n_rows = B * rows_max, or 0)  */
   const int32_t *own_len;   /* device [B]: own keys, 0 .. own_rows (NULL where own_rows = 0)  */
 } akvs_shared_cfg;
 

@@ -1661,11 +1661,11 @@ static akvs_status check_shared(const akvs_model_cfg *m, const akvs_shared_cfg *
               (long long)c->n_req * c->own_rows < (1LL << 31) && c->own_rows < (1 << 28) &&
               (long long)c->n_rows * m->n_q_heads < (1LL << 30),
           AKVS_ESHAPE, "batch too large");
-  REQUIRE(c->row_start || (long long)c->n_req * c->rows_max == c->n_rows, AKVS_ESHAPE,
-          "without row_start every request has rows_max rows: n_rows %d is not %d * %d", c->n_rows,
-          c->n_req, c->rows_max);
+  REQUIRE(c->row_start || c->n_rows == 0 || (long long)c->n_req * c->rows_max == c->n_rows,
+          AKVS_ESHAPE, "without row_start every request has rows_max rows: n_rows %d is not %d * %d",
+          c->n_rows, c->n_req, c->rows_max);
   REQUIRE(c->own_len || c->own_rows == 0, AKVS_EINVAL, "own_rows %d needs own_len", c->own_rows);
-  const int rows_max = std::min(c->rows_max, std::max(c->n_rows, 1));
+  const int rows_max = std::min(c->rows_max, c->n_rows);  // (no rows: none of any request)
   const long long tiles = ((long long)rows_max * (m->n_q_heads / m->n_kv_heads) + 15) / 16;
   REQUIRE(tiles * c->n_req * m->n_kv_heads < (1LL << 30), AKVS_ESHAPE,
           "batch too large: %d requests of up to %d rows", c->n_req, rows_max);
@@ -1690,6 +1690,7 @@ akvs_status akvs_qk_norm_rope(const void *q, int64_t ldq, const void *k, int64_t
   REQUIRE((long long)n_rows * (hqw + 2 * kvw) < (1LL << 40), AKVS_ESHAPE, "too large");
   REQUIRE(kv_rows || n_kv_rows >= n_rows, AKVS_EINVAL,
           "n_kv_rows %d < n_rows %d without kv_rows", n_kv_rows, n_rows);
+  if (n_rows == 0) return AKVS_OK;
   REQUIRE(q && k && positions && rope && q_out && k_out, AKVS_EINVAL, "NULL argument");
   REQUIRE((v == nullptr) == (v_out == nullptr), AKVS_EINVAL, "v and v_out go together");
   REQUIRE(aligned16(q) && aligned16(k) && aligned16(v) && aligned16(q_norm) &&

@@ -111,8 +111,8 @@ class Engine:
         sh, n = self.shape, int(q.shape[0])
         for name, x, heads in (("q", q, sh.n_q_heads), ("k", k, sh.n_kv_heads),
                                ("v", v, sh.n_kv_heads)):
-            if x.dtype != self.dtype or x.shape[0] != n or x[0:1].numel() not in (
-                    0, heads * sh.head_dim):
+            if x.dtype != self.dtype or x.device.type != self.device.type or x.shape[0] != n or (
+                    n and x[0].numel() != heads * sh.head_dim):
                 raise ValueError(f"{name}: need {n} {self.dtype} rows of {heads * sh.head_dim}")
         self._need("positions", positions, (n,), torch.int32)
         for name, x in (("q_norm", q_norm), ("k_norm", k_norm)):
@@ -148,6 +148,7 @@ class Engine:
             self._need("k_own", k_own, (None, None, sh.n_kv_heads, sh.head_dim))
             cap = int(k_own.shape[1])
         if row_start is not None:
+            self._need("row_start", row_start, (None,), torch.int32)
             B = int(row_start.numel()) - 1
         elif k_own is not None:
             B = int(k_own.shape[0])

@@ -122,6 +122,31 @@ def test_rows_that_see_no_key(hq, hkv, hd, dt):
     assert bool((b.out[:4] == 0).all()) and bool((b.lse[:4] == -math.inf).all())
 
 
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_no_keys_and_no_rows(dt):
+    """Neither a prefix nor own caches: zeros; no rows: nothing happens, weights stay."""
+    m = model(4, 2, 64, dt)
+    q = randn(3, 5, 4, 64, dt=dt)
+    out, lse = torch.full_like(q, 7.0), torch.full((5, 4), 7.0, device=DEV)
+    akvs.akvs_shared_attention(q, akvs.shared_cfg(5, 5, 1, 0), None, None, None, None, m, out, lse)
+    assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+    k, ko = randn(4, 70, 2, 64, dt=dt), randn(5, 3, 9, 2, 64, dt=dt)
+    ln = ints([1, 9, 0])
+    none, nol = q[:0], lse[:0]
+    for c in (akvs.shared_cfg(3, 0, 1, 70, 9, None, ln),
+              akvs.shared_cfg(3, 0, 4, 70, 9, ints([0, 0, 0, 0]), ln)):
+        assert akvs.akvs_shared_workspace_size(m, c) == 0
+        akvs.akvs_shared_attention(none, c, k, k, ko, ko, m, none, nol)
+        w0, o0 = randn(6, 2, 70), randn(7, 3, 2, 9)
+        w, o = torch.empty_like(w0), torch.empty_like(o0)
+        akvs.akvs_attention_weights(none, nol, c, k, ko, m, w0, w, o0, o)
+        assert torch.equal(w, w0) and torch.equal(o, o0)
+        akvs.akvs_attention_weights(none, nol, c, k, ko, m, None, w, None, o)
+        assert not w.any() and not o.any()
+    akvs.akvs_qk_norm_rope(none, none, None, 0, ln, None, None, m, rope(4, 64), 4, None, 0, none,
+                           none, None)
+
+
 @pytest.mark.parametrize("hq,hkv,hd,dt", [(24, 8, 128, BF), (6, 2, 64, BF), (4, 2, 128, F32)])
 def test_prefix_alone(hq, hkv, hd, dt):
     """No own caches at all."""
@@ -161,12 +186,13 @@ def test_large_scores(hq, hkv, hd, dt):
 
 @pytest.mark.parametrize("hq,hkv,hd,dt", [(24, 8, 128, BF), (6, 2, 64, BF), (4, 2, 128, F32)])
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
-def test_hidden_values_that_are_not_finite(hq, hkv, hd, dt, bad):
+@pytest.mark.parametrize("prefix", [40, 600])  # (requests' blocks whole, or in pieces)
+def test_hidden_values_that_are_not_finite(hq, hkv, hd, dt, bad, prefix):
     """A key and a value that the last row of a request alone sees are not finite: the rows
     before it are as if they were not there, the last one is not finite, other requests'
     rows are untouched. (Keys of +-inf: the scores are infinite or NaN.)"""
     def batch():
-        return Batch(hq, hkv, hd, dt, 40, [4, 2, 1], [20, 30, 5], seed=61)
+        return Batch(hq, hkv, hd, dt, prefix, [4, 2, 1], [20, 30, 5], seed=61)
     b = batch()
     b.attend()
     b.check()
