@@ -565,9 +565,10 @@ __global__ __launch_bounds__(256, 2) void k_shared_f32(
     f32x4_t k[C];
     float v[4][C];
   };
-  // keys past the last one re-read it
+  // keys past the last one re-read it (where no own key is seen it is the prefix's: own rows
+  // before `shift` do not exist)
   auto fetch = [&](Tile &t, int key0) __attribute__((always_inline)) {
-    const bool pre = WHOLE && key0 < it.shift;
+    const bool pre = WHOLE && (key0 < it.shift || k1 == it.first);
     const float *kb = pre ? Kp : K, *vb = pre ? Vp : V;
     const int end = (pre ? it.first : k1) - 1;
     const size_t base = pre ? 0 : it.base - it.shift;  // (wraps; key + base does not)

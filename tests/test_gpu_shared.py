@@ -122,6 +122,16 @@ def test_rows_that_see_no_key(hq, hkv, hd, dt):
     assert bool((b.out[:4] == 0).all()) and bool((b.lse[:4] == -math.inf).all())
 
 
+@pytest.mark.parametrize("prefix", [1, 16, 60, 64, 130, 250])
+@pytest.mark.parametrize("hq,hkv,hd,dt", [(4, 2, 64, F32), (4, 2, 128, F32), (6, 2, 128, BF)])
+def test_short_prefix_and_no_own_keys(hq, hkv, hd, dt, prefix):
+    """The first request has room for own keys and none there (its rows see the prefix alone);
+    the last key of the prefix stands for what is read ahead."""
+    b = Batch(hq, hkv, hd, dt, prefix, [1, 1, 2], [0, 5, 0], own_rows=16, seed=83)
+    b.attend()
+    b.check()
+
+
 @pytest.mark.parametrize("dt", [BF, F32])
 def test_no_keys_and_no_rows(dt):
     """Neither a prefix nor own caches: zeros; no rows: nothing happens, weights stay."""
