@@ -1657,9 +1657,12 @@ static akvs_status check_shared(const akvs_model_cfg *m, const akvs_shared_cfg *
           c->n_req);
   REQUIRE(c->n_rows >= 0 && c->rows_max >= 1 && c->prefix_len >= 0 && c->own_rows >= 0,
           AKVS_EINVAL, "need n_rows, prefix_len, own_rows >= 0 and rows_max >= 1");
+  // (a launch has fewer than 2^32 threads, so fewer than 2^24 blocks of 256: of pairs by 16, of
+  // own keys by 64)
   REQUIRE(c->n_rows < (1 << 24) && c->prefix_len < (1 << 28) &&
               (long long)c->n_req * c->own_rows < (1LL << 31) && c->own_rows < (1 << 28) &&
-              (long long)c->n_rows * m->n_q_heads < (1LL << 30),
+              (long long)c->n_rows * m->n_q_heads < (1LL << 27) &&
+              ((long long)c->own_rows + 63) / 64 * c->n_req * m->n_kv_heads < (1LL << 23),
           AKVS_ESHAPE, "batch too large");
   REQUIRE(c->row_start || c->n_rows == 0 || (long long)c->n_req * c->rows_max == c->n_rows,
           AKVS_ESHAPE, "without row_start every request has rows_max rows: n_rows %d is not %d * %d",
@@ -1667,7 +1670,7 @@ static akvs_status check_shared(const akvs_model_cfg *m, const akvs_shared_cfg *
   REQUIRE(c->own_len || c->own_rows == 0, AKVS_EINVAL, "own_rows %d needs own_len", c->own_rows);
   const int rows_max = std::min(c->rows_max, c->n_rows);  // (no rows: none of any request)
   const long long tiles = ((long long)rows_max * (m->n_q_heads / m->n_kv_heads) + 15) / 16;
-  REQUIRE(tiles * c->n_req * m->n_kv_heads < (1LL << 30), AKVS_ESHAPE,
+  REQUIRE(tiles * c->n_req * m->n_kv_heads < (1LL << 23), AKVS_ESHAPE,
           "batch too large: %d requests of up to %d rows", c->n_req, rows_max);
   *s = {c->n_req, c->n_rows, rows_max, c->prefix_len, c->own_rows, c->row_start, c->own_len};
   return AKVS_OK;
@@ -1687,7 +1690,8 @@ akvs_status akvs_qk_norm_rope(const void *q, int64_t ldq, const void *k, int64_t
   const long long es = (long long)es_of(m->dtype);
   REQUIRE(n_rows >= 0 && n_kv_rows >= 0 && rope_rows >= 1, AKVS_EINVAL,
           "need n_rows, n_kv_rows >= 0 and rope_rows >= 1");
-  REQUIRE((long long)n_rows * (hqw + 2 * kvw) < (1LL << 40), AKVS_ESHAPE, "too large");
+  REQUIRE((long long)n_rows * (hqw + 2 * kvw) < (1LL << 35), AKVS_ESHAPE,
+          "too large");  // (16 elements a thread, fewer than 2^32 of them)
   REQUIRE(kv_rows || n_kv_rows >= n_rows, AKVS_EINVAL,
           "n_kv_rows %d < n_rows %d without kv_rows", n_kv_rows, n_rows);
   if (n_rows == 0) return AKVS_OK;

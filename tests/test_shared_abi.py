@@ -34,6 +34,10 @@ SHARED = [
     (dict(n_req=1 << 10, n_rows=1 << 10, own_rows=1 << 22), akvs.AKVS_ESHAPE),
     (dict(n_rows=1 << 24, row_start=A), akvs.AKVS_ESHAPE),
     (dict(n_req=1 << 18, n_rows=1 << 20, rows_max=1 << 20, row_start=A), akvs.AKVS_ESHAPE),
+    # launches of 2^32 threads or more
+    (dict(n_req=1, n_rows=1 << 23, rows_max=1 << 23), akvs.AKVS_ESHAPE),
+    (dict(n_req=1 << 16, n_rows=1 << 10, rows_max=1 << 10, row_start=A), akvs.AKVS_ESHAPE),
+    (dict(n_req=1 << 18, n_rows=1 << 18, own_rows=1 << 12), akvs.AKVS_ESHAPE),
 ]
 
 
@@ -99,6 +103,13 @@ def test_rows_max_above_the_rows_is_the_rows(lib):
                 for r in (6, 1 << 30))
         assert a == b
         assert (a > 0) == (prefix == 8000)
+
+
+def test_norms_of_too_many_rows(lib):
+    for n in (1 << 23, (1 << 31) - 1):
+        m = model()
+        assert lib.akvs_qk_norm_rope(A, 4096, A, 4096, A, 4096, n, A, A, A, ctypes.byref(m), A, 10,
+                                     None, n, A, A, A, None) == akvs.AKVS_ESHAPE
 
 
 def test_workspace(lib):
