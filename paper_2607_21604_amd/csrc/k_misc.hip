@@ -371,7 +371,7 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope(QkNorm a) {
       const float v = fmaf(ss, 1.0f / hd, a.eps);
       rs = rsqrtf(v);
       rs += 0.5 * rs * (1.0 - (double)v * rs * rs);  // (one Newton step)
-      if (__ballot(!(v > 1e-30f && v < 1e38f))) {  // squares that leave fp32's range
+      if (!(v > 1e-30f && v < 1e38f)) {  // squares that leave fp32's range (a head's lanes agree)
         double wide = 0.0;
 #pragma unroll
         for (int i = 0; i < 8; ++i)

@@ -473,6 +473,31 @@ def test_qk_norm_rope_extremes():
     ko[4, 1] = 0
     assert bool(torch.isfinite(ko).all())
 
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_qk_norm_of_a_head_beside_others(dt):
+    """A token's heads come out the same bits alone, among others, and among others whose
+    squares leave fp32's range."""
+    m, n = model(6, 2, 128, dt), 33
+    x = [randn(40 + i, n, h, 128, dt=dt) for i, h in enumerate((6, 2, 2))]
+    gain, table, pos = randn(44, 128, dt=dt), rope(n, 128), torch.arange(n, device=DEV).int()
+
+    def run(q, k, v, pos):
+        out = [torch.empty_like(t) for t in (q, k, v)]
+        akvs.akvs_qk_norm_rope(q, k, v, len(q), pos, gain, gain, m, table, n, None, len(q), *out)
+        return out
+    whole = run(*x, pos)
+    odd = [t.clone() for t in x]
+    for t in odd:
+        t[1::2] *= 1e-25
+        t[:, 1] *= 1e25
+    beside = run(*odd, pos)
+    for r in (0, 2, 32):
+        alone = run(*(t[r:r + 1].contiguous() for t in x), pos[r:r + 1].contiguous())
+        for a, w, o in zip(alone, whole, beside):
+            assert torch.equal(a[0], w[r])
+            assert torch.equal(a[0, 0], o[r, 0]) and torch.equal(a[0, 2:], o[r, 2:])
+
+
 
 @pytest.mark.parametrize("dt", [BF, F32])
 @pytest.mark.parametrize("eps", [0.0, 1e-6])
