@@ -99,7 +99,21 @@ class Engine:
             raise ValueError(f"{name}: need a contiguous {dtype} tensor "
                              f"[{']['.join('n' if b is None else str(b) for b in shape)}] on "
                              f"{self.device.type}, got {x.dtype} {tuple(x.shape)} on {x.device.type}")
+        self._here(name, x)
         return x
+
+    def _here(self, name: str, x):
+        """Calls run on the current device's current stream: tensors of another are refused."""
+        if x.is_cuda and x.device.index != torch.cuda.current_device():
+            raise ValueError(f"{name} is on {x.device}, the current device is "
+                             f"cuda:{torch.cuda.current_device()}")
+
+    def _scratch(self, nbytes: int):
+        """Workspace of one call over a shared context, from torch's pool of the current stream
+        (or of the graph under capture): calls on two streams and captured graphs share none."""
+        if nbytes == 0:
+            return None
+        return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
 
     def qk_norm_rope(self, q, k, v, positions, q_norm, k_norm, rope, k_cache=None, v_cache=None,
                      kv_rows=None, q_out=None):
@@ -114,6 +128,7 @@ class Engine:
             if x.dtype != self.dtype or x.device.type != self.device.type or x.shape[0] != n or (
                     n and x[0].numel() != heads * sh.head_dim):
                 raise ValueError(f"{name}: need {n} {self.dtype} rows of {heads * sh.head_dim}")
+            self._here(name, x)
         self._need("positions", positions, (n,), torch.int32)
         for name, x in (("q_norm", q_norm), ("k_norm", k_norm)):
             if x is not None:
@@ -185,7 +200,7 @@ class Engine:
             lse = torch.empty(q.shape[:2], dtype=torch.float32, device=self.device)
         self._need("out", out, tuple(q.shape))
         self._need("lse", lse, tuple(q.shape[:2]), torch.float32)
-        ws = self.workspace(akvs.akvs_shared_workspace_size(self.m, c))
+        ws = self._scratch(akvs.akvs_shared_workspace_size(self.m, c))
         akvs.akvs_shared_attention(q, c, k_prefix, v_prefix, k_own, v_own, self.m, out, lse, ws)
         return out, lse
 
@@ -206,7 +221,7 @@ class Engine:
                 if shape is None:
                     raise ValueError("w_own needs k_own")
                 self._need(("w_prefix", "w_own")[i], w[i], shape, torch.float32)
-        ws = self.workspace(akvs.akvs_shared_workspace_size(self.m, c))
+        ws = self._scratch(akvs.akvs_shared_workspace_size(self.m, c))
         akvs.akvs_attention_weights(q, lse, c, k_prefix, k_own, self.m, prev[0], w[0], prev[1],
                                     w[1], ws)
         return w[0], w[1]

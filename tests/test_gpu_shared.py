@@ -752,6 +752,60 @@ def test_engine_methods_are_the_entry_points(hq, hkv, hd, dt):
             assert torch.equal(w[i, h, :len(want)], wo[i, h, want])
 
 
+def test_engine_in_two_graphs():
+    """Two captured calls of one engine, replayed on two streams at once after larger eager
+    calls took and gave back memory, give what they gave eagerly."""
+    from paper_2607_21604_amd.runtime import Engine
+    eng = Engine(_Shape(8, 2, 128, BF), {"layers": [{k: torch.zeros(8, device=DEV) for k in (
+        "attn_norm", "w_qkv", "w_o", "mlp_norm", "w_gate_up", "w_down")}]}, DEV)
+    P = 6000
+    kp, vp = randn(1, P, 2, 128, dt=BF), randn(2, P, 2, 128, dt=BF)
+    qs = [randn(3 + i, 4, 8, 128, dt=BF) for i in range(2)]
+
+    def run(q):
+        out, lse = eng.shared_attention(q, kp, vp)
+        return (out, lse) + eng.attention_weights(q, lse, kp)[:1]
+    want = [[t.clone() for t in run(q)] for q in qs]
+    torch.cuda.synchronize()
+    graphs, got = [], []
+    for q in qs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            got.append(run(q))
+        graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in qs]
+    for _ in range(3):
+        run(randn(9, 300, 8, 128, dt=BF))
+        junk = [torch.full((1 << 20,), 255, dtype=torch.uint8, device=DEV) for _ in range(8)]
+        for x in got:
+            for t in x:
+                t.zero_()
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for x, w in zip(got, want):
+            assert all(torch.equal(a, b) for a, b in zip(x, w))
+        assert all(bool((j == 255).all()) for j in junk)
+
+
+def test_engine_refuses_another_device(monkeypatch):
+    """Tensors that are not on the current device (here: said to be another) are refused."""
+    from paper_2607_21604_amd.runtime import Engine
+    eng = Engine(_Shape(8, 2, 128, BF), {"layers": [{k: torch.zeros(8, device=DEV) for k in (
+        "attn_norm", "w_qkv", "w_o", "mlp_norm", "w_gate_up", "w_down")}]}, DEV)
+    q, kp = randn(1, 2, 8, 128, dt=BF), randn(2, 9, 2, 128, dt=BF)
+    lse, w = torch.zeros(2, 8, device=DEV), torch.zeros(1, 2, 9, device=DEV)
+    pos, table = ints([0, 1]), rope(4, 128)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for call in (lambda: eng.shared_attention(q, kp, kp), lambda: eng.attention_weights(q, lse, kp),
+                 lambda: eng.evict_cache(kp[None], kp[None], w, 3),
+                 lambda: eng.qk_norm_rope(q, kp[:2], kp[:2], pos, None, None, table)):
+        with pytest.raises(ValueError, match="current device"):
+            call()
+
+
 # ---- many rows, long ranges: every split of the work ------------------------------------------
 
 def big_reference(b):
