@@ -465,7 +465,9 @@ akvs_status akvs_attention_weights(const void *q, const float *lse, const akvs_s
                                    float *w_prefix, const float *w_own_prev, float *w_own,
                                    void *ws, size_t ws_bytes, hipStream_t stream);
 
-/* Workspace bytes of akvs_evict_cache (needed where `keep` is NULL); 0 if invalid. */
+/* Workspace bytes of akvs_evict_cache; 0 if invalid. It is needed where `keep` is NULL; with
+ * `keep` it may be NULL or smaller, and lets the call split long sequences over blocks (the
+ * same result). */
 size_t akvs_evict_workspace_size(const akvs_model_cfg *m, const akvs_evict_cfg *c);
 
 /* Eviction by accumulated weight: per sequence of n keys and per KV head, the first n_first

@@ -1803,12 +1803,16 @@ static bool overlap(const void *a, size_t na, const void *b, size_t nb) {
   return x < y + nb && y < x + na;
 }
 
+static size_t keep_bytes(const EvictArgs &a, const akvs_model_cfg *m) {
+  return align256((size_t)a.n_seq * m->n_kv_heads * a.n_keep * sizeof(int32_t));
+}
+
 extern "C" {
 
 size_t akvs_evict_workspace_size(const akvs_model_cfg *m, const akvs_evict_cfg *c) {
   EvictArgs a;
   if (check_evict(m, c, &a) != AKVS_OK) return 0;
-  return align256((size_t)a.n_seq * m->n_kv_heads * a.n_keep * sizeof(int32_t));
+  return keep_bytes(a, m) + align256(evict_scratch_bytes(a, m->n_kv_heads));
 }
 
 akvs_status akvs_evict_cache(const void *k, const void *v, const float *weights,
@@ -1838,8 +1842,10 @@ akvs_status akvs_evict_cache(const void *k, const void *v, const float *weights,
   REQUIRE(keep || (ws && ws_bytes >= need), AKVS_ENOSPACE, "workspace %zu < %zu bytes", ws_bytes,
           need);
   if (!keep) keep = reinterpret_cast<int32_t *>(ws);
-  LAUNCH(AKVS_K_SELECT,
-         launch_evict_select(weights, a, m->n_kv_heads, keep, weights_out, stream));
+  const bool split = ws && ws_bytes >= need && evict_scratch_bytes(a, m->n_kv_heads) > 0;
+  void *scratch = split ? reinterpret_cast<char *>(ws) + keep_bytes(a, m) : nullptr;
+  LAUNCH(AKVS_K_SELECT, launch_evict_select(weights, a, m->n_kv_heads, keep, weights_out, scratch,
+                                            stream));
   LAUNCH(AKVS_K_OTHER, launch_evict_gather(k, v, a, m->n_kv_heads,
                                            (int)(m->head_dim * es_of(m->dtype)), keep, k_out,
                                            v_out, lens_out, stream));

@@ -226,8 +226,11 @@ struct EvictArgs {
   int n_seq, n_keys, src_rows, n_keep, dst_rows, n_first, n_recent;
   const int32_t *lens;
 };
+// scratch (evict_scratch_bytes, 16-byte aligned; nullptr: one block a head) lets it split long
+// sequences.
 hipError_t launch_evict_select(const float *weights, const EvictArgs &a, int hkv, int32_t *keep,
-                               float *w_out, hipStream_t s);
+                               float *w_out, void *scratch, hipStream_t s);
+size_t evict_scratch_bytes(const EvictArgs &a, int hkv);  // 0: it would not split
 // Kept rows of k and v (k null: none) and, with lens_out, the kept lengths.
 hipError_t launch_evict_gather(const void *k, const void *v, const EvictArgs &a, int hkv,
                                int row_bytes, const int32_t *keep, void *k_out, void *v_out,

@@ -248,7 +248,8 @@ class Engine:
         v_out = torch.zeros_like(k_out)
         w_out = torch.empty((S, sh.n_kv_heads, rows), dtype=torch.float32, device=dev)
         lens_out = torch.empty(S, dtype=torch.int32, device=dev)
-        akvs.akvs_evict_cache(k, v, weights, c, self.m, keep, k_out, v_out, w_out, lens_out)
+        ws = self._scratch(akvs.akvs_evict_workspace_size(self.m, c))
+        akvs.akvs_evict_cache(k, v, weights, c, self.m, keep, k_out, v_out, w_out, lens_out, ws)
         return keep, k_out, v_out, w_out, lens_out
 
     def reuse_prefill(self, tokens: torch.Tensor, chunk_lens: Sequence[int], query_len: int,

@@ -608,6 +608,69 @@ def test_evict_long_sequence():
         assert torch.equal(e.ko[0, :, h], e.k[0, torch.from_numpy(want).to(DEV), h])
 
 
+@pytest.mark.parametrize("keys,keep,first,recent,lens", [
+    (32769, 1, 0, 0, None), (32769, 32768, 0, 0, None), (36865, 6000, 4, 64, None),
+    (40000, 4000, 3, 100, [40000, 4097, 0]), (40000, 4000, 0, 0, [3999, 4001, 1]),
+    (40000, 50000, 1, 2, None), (70001, 900, 450, 450, None), (300_001, 40_000, 5, 77, None),
+    (1_000_001, 30_000, 0, 5, None)])
+def test_evict_split_over_blocks(keys, keep, first, recent, lens):
+    """With a workspace long sequences are split over blocks: the definition's keys, and the same
+    without one. Head 0 has few distinct weights, head 1 one value and NaN, head 2 all kinds."""
+    S = len(lens) if lens else 1
+    e = Evict(3, 64, BF, S, keys, keep, first, recent, dst=keep + 3, lens=lens, seed=keys)
+    e.w[:, 0] = (e.w[:, 0] * 4).floor()
+    e.w[:, 1] = torch.where(e.w[:, 1] < 0.5, torch.full_like(e.w[:, 1], 0.25), math.nan)
+    size = akvs.akvs_evict_workspace_size(e.m, e.cfg)
+    assert size > S * 3 * keep * 4 + 255
+    ws = torch.full((size,), 255, dtype=torch.uint8, device=DEV)
+    e.run()
+    alone = [x.clone() for x in (e.keep, e.ko, e.vo, e.wo, e.lo)]
+    for x in (e.keep, e.wo, e.lo):
+        x.fill_(-9)
+    e.run(ws=ws)
+    for got, want in zip((e.keep, e.ko, e.vo, e.wo, e.lo), alone):
+        assert torch.equal(got.view(torch.int32) if got.dtype == F32 else got,
+                           want.view(torch.int32) if want.dtype == F32 else want)
+    w = e.w.cpu().numpy()
+    for s in range(S):
+        n = lens[s] if lens else keys
+        for h in range(3):
+            want = np.arange(n)
+            if n > keep:
+                mid = np.arange(first, n - recent)
+                x = np.where(np.isnan(w[s, h, mid]), -np.inf, w[s, h, mid])  # (no -inf among them)
+                best = mid[np.argsort(-x, kind="stable")[:keep - first - recent]]
+                want = np.concatenate((np.arange(first), np.sort(best), np.arange(n - recent, n)))
+            got = e.keep[s, h].cpu().numpy()
+            assert np.array_equal(got[:len(want)], want) and (got[len(want):] == -1).all()
+            assert not e.wo[s, h, len(want):].any()
+
+
+def test_evict_split_in_the_workspace_and_from_a_graph():
+    """Kept indices in the workspace beside the split's, captured, and replayed over new weights
+    between eager calls that use it too."""
+    e = Evict(2, 64, BF, 1, 50_000, 5000, 4, 64, seed=5)
+    ws = torch.empty(akvs.akvs_evict_workspace_size(e.m, e.cfg), dtype=torch.uint8, device=DEV)
+
+    def run():
+        akvs.akvs_evict_cache(e.k, e.v, e.w, e.cfg, e.m, None, e.ko, e.vo, e.wo, e.lo, ws)
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for seed in (1, 2, 3):
+        e.w.copy_(randn(seed, *e.w.shape).square())
+        e.run()
+        want = [x.clone() for x in (e.ko, e.vo, e.wo, e.lo)]
+        for x in (e.ko, e.vo, e.wo, e.lo):
+            x.zero_()
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip((e.ko, e.vo, e.wo, e.lo), want))
+
+
 def test_evict_outputs_left_out():
     """Selection alone; the kept indices in the workspace."""
     e = Evict(4, 128, BF, 3, 500, 90, 4, 20, seed=17)
