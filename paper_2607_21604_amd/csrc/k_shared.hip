@@ -745,7 +745,7 @@ struct WeightPlan {
 
 // NK: key tiles of a wave. Two halve the LDS reads of a pair tile, which bound long walks.
 template <typename TS, int HD, int NK>
-__global__ __launch_bounds__(256) void k_attn_weights(SharedBatch s, WeightPlan p,
+__global__ __launch_bounds__(256, 2) void k_attn_weights(SharedBatch s, WeightPlan p,
                                                       const TS *__restrict__ Q,
                                                       const float *__restrict__ lse,
                                                       const TS *__restrict__ Kp,
