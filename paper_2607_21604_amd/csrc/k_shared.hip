@@ -737,10 +737,11 @@ struct WeightTile<float> {  // 16 x 16
 };
 
 // Blocks [0, prefix_blocks): (part, key block, KV head), part: a share of the pair tiles, whose
-// sums go to a buffer of their own where there are several; then (request, key block, KV head)
-// of the own keys.
+// sums go to a buffer of their own where there are several; then (request, key block, part of
+// the request's tiles, KV head) of the own keys.
 struct WeightPlan {
-  int nk, parts, part_pairs, key_blocks, prefix_blocks, own_blocks;
+  int nk, parts, part_pairs, key_blocks, prefix_blocks;
+  int own_parts, own_pairs, own_blocks;  // own_blocks: of keys
 };
 
 // NK: key tiles of a wave. Two halve the LDS reads of a pair tile, which bound long walks.
@@ -783,6 +784,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_weights(SharedBatch s, WeightPl
     v0 = part * p.part_pairs;
     n_pairs = min(r1 * G, v0 + p.part_pairs);
   } else {
+    const int part = id % p.own_parts;
+    id /= p.own_parts;
     const int b = id / p.own_blocks;
     kb = id - b * p.own_blocks;
     shared_rows(s, b, r0, r1);
@@ -791,8 +794,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_weights(SharedBatch s, WeightPl
     K = Ko + (size_t)b * s.own_rows * hkv * HD;
     const size_t o = ((size_t)b * hkv + kvh) * n_all;
     prev = wo_prev ? wo_prev + o : nullptr;
-    w = wo + o;
-    n_pairs = (r1 - r0) * G;
+    w = wo + (size_t)part * s.n_req * hkv * n_all + o;
+    v0 = part * p.own_pairs;
+    n_pairs = min((r1 - r0) * G, v0 + p.own_pairs);
   }
   constexpr int KEYS = NK * W::KEYS;  // of a wave
   const int j0 = kb * 4 * KEYS, j = j0 + wave * KEYS + li;
@@ -903,8 +907,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_weights(SharedBatch s, WeightPl
       }
     };
     // Loads run two tiles ahead, in registers, and are made whether or not there is a tile: a
-    // block alone on its compute unit is else bound by their latency (2 requests of 98 rows
-    // over 506 keys of 40/8 heads: see the figures below).
+    // block alone on its compute unit is else bound by their latency (16 rows over 16128 keys of
+    // 40/8 heads 11.3 -> 10.9 us).
     Tile a, b;
     load(a);
     load(b);
@@ -934,14 +938,24 @@ __global__ __launch_bounds__(256, 2) void k_attn_weights(SharedBatch s, WeightPl
   }
 }
 
-// w = prev + the parts' sums in order.
-__global__ __launch_bounds__(256) void k_weight_parts(const float *__restrict__ part, int parts,
-                                                      size_t n, const float *prev, float *w) {
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n) return;
-  float sum = part[i];
-  for (int q = 1; q < parts; ++q) sum += part[q * n + i];
-  w[i] = (prev ? prev[i] : 0.f) + sum;
+// w = prev + the parts' sums in order: n weights of the prefix, n_own of the own keys.
+struct WeightSum {
+  const float *part, *prev;
+  float *w;
+  int parts;
+  size_t n;
+};
+// Blocks [0, blocks) are the prefix's, then the own keys'.
+__device__ __forceinline__ void sum_parts(const WeightSum &x, size_t i) {
+  if (i >= x.n) return;
+  float sum = x.part[i];
+  for (int q = 1; q < x.parts; ++q) sum += x.part[q * x.n + i];
+  x.w[i] = (x.prev ? x.prev[i] : 0.f) + sum;
+}
+__global__ __launch_bounds__(256) void k_weight_parts(WeightSum shared, int blocks, WeightSum own) {
+  const int id = blockIdx.x;
+  if (id < blocks) sum_parts(shared, (size_t)id * 256 + threadIdx.x);
+  else sum_parts(own, (size_t)(id - blocks) * 256 + threadIdx.x);
 }
 
 // Items of a call. bf16 tiles have 32, 64 or 128 pairs (see k_shared_bf16), fp32 ones 16; two
@@ -1090,36 +1104,57 @@ hipError_t launch_shared_attention(const SharedBatch &s, const void *q, const vo
 #undef AKVS_SHARED
 }
 
-// Two key tiles a wave share a pair tile's staging and LDS reads, but a block then takes 192
-// registers (two a compute unit) and 256 keys: taken where the prefix makes two such blocks a
-// unit by parts of eight tiles (1070 rows over 4516 keys of 24/8 heads: 58 us with one, 49 with
-// two; 195 rows over 506 keys of 40/8 heads: 19 and 25). The pairs go in parts while the keys
-// alone do not fill the units, at least four tiles each.
+// Two key tiles a wave share a pair tile's staging and LDS reads, but a block then has 256 keys and
+// its unit three blocks of 166 registers: taken where the prefix makes two such blocks a unit by
+// parts of eight tiles (1070 rows over 4516 keys of 24/8 heads: 57 us with two, 63 with one; 600
+// over 16128 of 40/8 127 and 140; 195 over 506 of 40/8 24 and 18). The pairs go in parts while the
+// keys alone do not fill the units, at least four tiles each. So do a request's over its own keys,
+// eight tiles each, or its one block walks them all: 256 rows over 9000 keys and up to 128 own of
+// 28/4 heads 73 us whole, 35 in parts as long as the prefix's, 33 by eight; 1800 rows of 8 requests
+// over 2000 92, 55 and 49 (up to 16 blocks a unit: most of the room may be empty).
 template <typename TS>
 static WeightPlan weight_plan(const SharedBatch &s, int hq, int hkv, bool prefix, bool own) {
   typedef WeightTile<TS> W;
   WeightPlan p;
   const int cus = gemm_cu_count();
-  const int tiles = (int)(((long long)s.n_rows * (hq / hkv) + W::PAIRS - 1) / W::PAIRS);
+  auto tiles_of = [&](long long rows) {
+    return (int)((rows * (hq / hkv) + W::PAIRS - 1) / W::PAIRS);
+  };
+  const int tiles = tiles_of(s.n_rows), own_tiles = tiles_of(s.rows_max);
   const long long wide = (s.prefix_len + 8 * W::KEYS - 1) / (8 * W::KEYS);
   p.nk = wide * hkv * (tiles / 8) >= 2 * cus ? 2 : 1;
   const int keys = 4 * W::KEYS * p.nk;
-  p.key_blocks = prefix ? (s.prefix_len + keys - 1) / keys : 0;
-  p.own_blocks = own ? (s.own_rows + keys - 1) / keys : 0;
+  p.key_blocks = (s.prefix_len + keys - 1) / keys;
+  p.own_blocks = (s.own_rows + keys - 1) / keys;
   const long long blocks = std::max(1LL, (long long)p.key_blocks * hkv);
   long long parts = std::max(1LL, (p.nk == 2 ? 2LL : 4LL) * cus / blocks);
   parts = std::min<long long>(parts, std::max(1, tiles / 4));
   const int per = tiles ? (int)((tiles + parts - 1) / parts) : 1;
   p.parts = tiles ? (tiles + per - 1) / per : 1;
   p.part_pairs = per * W::PAIRS;
-  p.prefix_blocks = p.parts * p.key_blocks * hkv;
+  const int walk = std::max(4, std::min(per, 8));
+  const long long own_most = 16LL * cus / std::max(1LL, (long long)s.n_req * p.own_blocks * hkv);
+  const int own_parts =
+      (int)std::max(1LL, std::min<long long>((own_tiles + walk - 1) / walk, own_most));
+  const int own_per = std::max(1, (own_tiles + own_parts - 1) / own_parts);
+  p.own_parts = std::max(1, (own_tiles + own_per - 1) / own_per);
+  p.own_pairs = own_per * W::PAIRS;
+  p.prefix_blocks = prefix ? p.parts * p.key_blocks * hkv : 0;
+  if (!own) p.own_blocks = 0;
   return p;
 }
 
+static size_t own_weights(const SharedBatch &s, int hkv) {
+  return (size_t)s.n_req * hkv * s.own_rows;
+}
+// Floats of the prefix's parts, then of the own keys', where there are several.
+static size_t prefix_part_floats(const SharedBatch &s, const WeightPlan &p, int hkv) {
+  return p.parts > 1 ? (size_t)p.parts * hkv * s.prefix_len : 0;
+}
 size_t weight_part_floats(const SharedBatch &s, int hq, int hkv, int dtype) {
   const WeightPlan p = dtype == AKVS_BF16 ? weight_plan<bf16_t>(s, hq, hkv, true, true)
                                           : weight_plan<float>(s, hq, hkv, true, true);
-  return p.parts > 1 ? (size_t)p.parts * hkv * s.prefix_len : 0;
+  return prefix_part_floats(s, p, hkv) + (p.own_parts > 1 ? p.own_parts * own_weights(s, hkv) : 0);
 }
 
 template <typename TS>
@@ -1128,15 +1163,17 @@ static hipError_t attention_weights(const SharedBatch &s, const void *q, const f
                                     const float *wp_prev, float *wp, const float *wo_prev,
                                     float *wo, float *part, hipStream_t st) {
   const WeightPlan p = weight_plan<TS>(s, hq, hkv, wp != nullptr, wo != nullptr);
-  const size_t blocks = p.prefix_blocks + (size_t)s.n_req * p.own_blocks * hkv;
+  const size_t blocks = p.prefix_blocks + (size_t)s.n_req * p.own_blocks * p.own_parts * hkv;
   if (blocks == 0) return hipSuccess;
   const bool split = p.parts > 1 && p.prefix_blocks > 0;
+  const bool own_split = p.own_parts > 1 && p.own_blocks > 0;
+  float *own_part = part + prefix_part_floats(s, p, hkv);
   const float scale = 1.4426950408889634f / sqrtf((float)hd);
   auto x = [](const void *a) { return reinterpret_cast<const TS *>(a); };
 #define AKVS_WEIGHTS(HD_, NK_)                                                                 \
   hipLaunchKernelGGL((k_attn_weights<TS, HD_, NK_>), dim3((unsigned)blocks), dim3(256), 0, st, s, p, \
                      x(q), lse, x(kp), x(ko), hq, hkv, scale, split ? nullptr : wp_prev,        \
-                     split ? part : wp, wo_prev, wo)
+                     split ? part : wp, own_split ? nullptr : wo_prev, own_split ? own_part : wo)
   if (hd == 128) {
     if (p.nk == 2) AKVS_WEIGHTS(128, 2); else AKVS_WEIGHTS(128, 1);
   } else {
@@ -1144,10 +1181,12 @@ static hipError_t attention_weights(const SharedBatch &s, const void *q, const f
   }
 #undef AKVS_WEIGHTS
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !split) return e;
-  const size_t n = (size_t)hkv * s.prefix_len;
-  hipLaunchKernelGGL(k_weight_parts, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, part,
-                     p.parts, n, wp_prev, wp);
+  if (e != hipSuccess || !(split || own_split)) return e;
+  const WeightSum shared{part, wp_prev, wp, p.parts, split ? (size_t)hkv * s.prefix_len : 0};
+  const WeightSum own{own_part, wo_prev, wo, p.own_parts, own_split ? own_weights(s, hkv) : 0};
+  const int blocks_shared = (int)((shared.n + 255) / 256), blocks_own = (int)((own.n + 255) / 256);
+  hipLaunchKernelGGL(k_weight_parts, dim3(blocks_shared + blocks_own), dim3(256), 0, st, shared,
+                     blocks_shared, own);
   return hipGetLastError();
 }
 

@@ -362,6 +362,19 @@ def test_weights_of_many_rows(hq, hkv, hd, dt, prefix, rows, own):
     assert abs(total - b.n * hq) < 1e-4 * b.n * hq
 
 
+@pytest.mark.parametrize("hq,hkv,hd,dt", [(28, 4, 128, BF), (4, 2, 64, F32)])
+def test_weights_of_own_keys_in_parts(hq, hkv, hd, dt):
+    """Rows of a request that go in parts over its own keys, beside requests of few rows and of
+    none: added to what was there, and alone (no prefix side) the same bits."""
+    b = Batch(hq, hkv, hd, dt, 70, [90, 2, 0, 41], [91, 200, 4, 41], seed=131)
+    b.attend()
+    _, wo = weigh(b, True, 131)
+    c = b.cfg()
+    alone = randn(131 + 8, b.B, hkv, b.cap).square()
+    akvs.akvs_attention_weights(b.q, b.lse, c, b.kp, b.ko, b.m, None, None, alone, alone, b.ws(c))
+    assert torch.equal(alone, wo)
+
+
 def test_weights_of_rows_that_see_no_key():
     b = Batch(24, 8, 128, BF, 0, [2, 3, 1], [0, 1, 9], own_rows=12, seed=121)
     b.attend()
