@@ -16,8 +16,8 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return w != w ? 1u : k;
 }
 
-// One sequence's keys: [0, n), of which the candidates [c0, c1) are compared and `want` of them kept;
-// the keys beside them are kept, as is every key where there are no more than may be.
+// One sequence's keys: [0, n), of which the candidates [c0, c1) are compared and `want` of them
+// kept; the keys beside them are kept, as is every key where there are no more than may be.
 struct EvictSeq {
   int n, kept, c0, c1, want;
   bool all;
@@ -36,8 +36,8 @@ struct EvictSeq {
 };
 constexpr int EV_BINS = 2048;
 constexpr uint32_t EV_NONE = 0xfffffffeu;  // T where no candidate is kept
-__host__ __device__ constexpr int digit_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
-__host__ __device__ constexpr int digit_bits(int pass) { return pass == 2 ? 10 : 11; }
+constexpr int digit_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
+constexpr int digit_bits(int pass) { return pass == 2 ? 10 : 11; }
 
 // Counts key u, if it is a candidate that agrees with T so far, under its next digit. (What is no
 // candidate agrees with no T but the smallest.)
@@ -379,7 +379,7 @@ size_t evict_scratch_bytes(const EvictArgs &a, int hkv) {
   return (size_t)a.n_seq * hkv * evict_long(a, hkv).chunks * (2 * EV_BINS * 2 + sizeof(int4));
 }
 
-// Few keys: eight waves (300 / 1500 keys 5.2 / 7.1 us, with four 5.7 / 8.5, with sixteen 6.4 / 7.9).
+// Few keys: eight waves (300 / 1500 keys 5.2 / 7.1 us; four 5.7 / 8.5, sixteen 6.4 / 7.9).
 hipError_t launch_evict_select(const float *weights, const EvictArgs &a, int hkv, int32_t *keep,
                                float *w_out, void *scratch, hipStream_t s) {
   const dim3 g((unsigned)(a.n_seq * hkv));
@@ -390,8 +390,8 @@ hipError_t launch_evict_select(const float *weights, const EvictArgs &a, int hkv
     p.hist[0] = reinterpret_cast<uint32_t *>(p.state + items);
     p.hist[1] = p.hist[0] + items * (EV_BINS / 2);
 #define AKVS_STAGE(STAGE_)                                                                        \
-  hipLaunchKernelGGL((k_evict_long<STAGE_>), dim3((unsigned)items), dim3(EVL_NW * 64), 0, s, weights, \
-                     a, p, hkv, keep, w_out)
+  hipLaunchKernelGGL((k_evict_long<STAGE_>), dim3((unsigned)items), dim3(EVL_NW * 64), 0, s,      \
+                     weights, a, p, hkv, keep, w_out)
     AKVS_STAGE(0);
     AKVS_STAGE(1);
     AKVS_STAGE(2);

@@ -103,6 +103,10 @@ __device__ __forceinline__ bool odd_bf16(uint32_t lo16) { return (lo16 & 0x7f80u
 // layout of O^T = V^T P^T; V^T comes from row-major rows by the transposing LDS read. Softmax
 // statistics and outputs are fp32; the probabilities are rounded to bf16 for the second
 // product (the matrix cores' type), their sum is not.
+// Few rows over a long prefix are bound by its bytes (5 rows over 130001 keys of 28/4 heads 61 us
+// with the merge, 4.5 TB/s), over shorter ones by a block's latency, 7.5 us and 1.75 per tile.
+// Many rows are bound by the softmax between the products, which two waves a SIMD hide in part
+// (1328 rows over 16128 keys of 40/8 heads 498 us, 888 TFLOP/s).
 template <int HD, bool WHOLE>
 __global__ __launch_bounds__(256, 2) void k_shared_bf16(
     SharedBatch s, SharedPlan p, const bf16_t *__restrict__ Q, const bf16_t *__restrict__ Kp,
@@ -214,7 +218,8 @@ __global__ __launch_bounds__(256, 2) void k_shared_bf16(
   __syncthreads();
   if (nkt) store(it.k0, 0);
   // vmcnt(0): with the query fragments known to be there, the loop's waits are for keys alone
-  // (without it each product waited for the tile just requested: 32 % of the time of long walks)
+  // (without it each product waited for the tile just requested: 16 rows over 16128 keys of 40/8
+  // heads 26.5 us, 22.7 with it)
   __builtin_amdgcn_s_waitcnt(0x0f70);
   __syncthreads();
   for (int kt = 0; kt < nkt; ++kt) {
@@ -575,6 +580,9 @@ __device__ __forceinline__ bool odd_f32(float x) {
 // registers, a tile ahead. Scores are formed transposed: lane l holds the scores of pair l % 16
 // at keys 4 (l / 16) + 0..3 of the tile, the operand layout of O^T = V^T P^T as it is; row
 // l % 16 of V^T block c stands for dim (l % 16) * C + c, so that a lane's values are contiguous.
+// 85 rows over 2055 keys of 28/4 heads take 43 us: about 10 of a launch do not depend on the keys,
+// and an MFMA takes 18 to 22 ns in the loop (15 in a row) with one or two waves a SIMD. Two pair
+// tiles a wave, which halve the reads from L2, were slower (49 us).
 template <int HD, bool WHOLE>
 __global__ __launch_bounds__(256, 2) void k_shared_f32(
     SharedBatch s, SharedPlan p, const float *__restrict__ Q, const float *__restrict__ Kp,
@@ -761,7 +769,10 @@ __global__ __launch_bounds__(256, 2) void k_shared_f32(
 // over pairs inside the lane, and a key's sum never leaves its column. A wave keeps a tile of
 // keys in registers; the pair tiles pass through LDS for the block's four waves, the next one
 // in flight. (Each wave fetching the queries itself was bound by that: 32 rows of 256 bytes
-// are 32 cache lines an instruction; 1070 rows over 4516 keys of 24/8 heads took 162 us.)
+// are 32 cache lines an instruction; 1171 rows over 4516 keys of 24/8 heads took 162 us, now 49.)
+// Many rows are bound by the instructions of the exponentials and sums between the products and
+// by whole blocks a unit, few by latency and the keys' bytes (16 rows over 16128 keys of 40/8 heads
+// 10.7 us, 3.5 TB/s).
 typedef __attribute__((ext_vector_type(4))) int i32x4_t;
 template <typename TS>
 struct WeightTile;
@@ -1019,15 +1030,16 @@ __global__ __launch_bounds__(256) void k_weight_parts(WeightSum shared, int bloc
 // that shares its unit 7.5 + 1.7 times them. Blocks that fit the chip together end with the
 // longest of them; else whole rounds of prefix blocks, the rest of them, and the own keys'
 // blocks that had no place follow each other. Each split's partials cost a write and a read.
-// Up to five tiles of prefix and own keys together, each request's blocks take both (whole) and
+// Up to six tiles of prefix and own keys together, each request's blocks take both (whole) and
 // there is nothing to merge: 16 requests over 60 / 190 / 320 / 450 keys and up to 64 own of 28/4
-// heads 7.9 / 10.0 / 12.0 / 15.9 us whole, 10.8 / 13.8 / 14.0 / 13.3 in pieces (fp32, 4 heads of 64:
-// 6.9 / 8.5 / 10.1 / 13.0 and 9.3 / 11.0 / 11.0 / 11.2).
+// heads 7.3 / 9.4 / 11.5 / 15.4 us whole, 10.1 / 12.8 / 13.0 / 11.9 in pieces (fp32, 4 heads of
+// 64: 6.2 / 7.9 / 9.5 / 12.5 and 8.5 / 10.1 / 10.1 / 10.1).
 //   16 rows over 4096 / 8192 / 16384 / 32768 / 65536 keys of 40/8 heads, this launch alone: 256
 //   prefix blocks 11.1 / 14.6 / 21.0 / 34.9 / 62.7 us, 512 of them - / 19.6 / 23.3 / 37.1 / 60.8;
 //   with 128 blocks of own keys and 16128 keys 256 prefix blocks are 4 us faster than 504 (own
-//   blocks wait for a place). 1320 rows over 16128 (416 tiles of pairs): 597 us with one split,
-//   556 with three. 116 fp32 rows over 2055 keys of 28/4 heads: 56 us with two, 43 with four.
+//   blocks wait for a place). 1328 rows over 16128 (416 tiles of pairs): 516 us with one split,
+//   491 with three, 511 with four. 85 fp32 rows over 2055 keys of 28/4 heads: 57 us with two, 43
+//   with three, 49 with four.
 static SharedPlan shared_plan(const SharedBatch &s, int hq, int hkv, int hd, int dtype) {
   constexpr double BYTES = 7e6;  // partials moved in a tile's time
   SharedPlan p{};
@@ -1052,7 +1064,7 @@ static SharedPlan shared_plan(const SharedBatch &s, int hq, int hkv, int hd, int
   cut(o_items ? blocks / o_items : 1, tiles_of(s.own_rows, SH_TILE), &p.chunks, &p.chunk_keys);
   const int ot = tiles_of(s.own_rows, SH_TILE);
   p.whole = s.prefix_len > 0 && o_items > 0 && o_items <= blocks &&
-            tiles_of(s.prefix_len, SH_TILE) + ot <= 5;
+            tiles_of(s.prefix_len, SH_TILE) + ot <= 6;
   if (p.whole) {
     p.chunks = p.slots = 1;
     return p;
@@ -1124,8 +1136,8 @@ static hipError_t shared_attention(const SharedBatch &s, const void *q, const vo
   const dim3 g((unsigned)blocks), b(256);
   const float scale = 1.4426950408889634f / sqrtf((float)HD);
 #define AKVS_ATTEND(KERNEL_)                                                                      \
-  hipLaunchKernelGGL(KERNEL_, g, b, 0, st, s, p, x(q), x(kp), x(vp), x(ko), x(vo), hq, hkv, scale, O, \
-                     lse, po, ml)
+  hipLaunchKernelGGL(KERNEL_, g, b, 0, st, s, p, x(q), x(kp), x(vp), x(ko), x(vo), hq, hkv, scale, \
+                     O, lse, po, ml)
   if constexpr (sizeof(TS) == 2) {
     if (p.whole) AKVS_ATTEND((k_shared_bf16<HD, true>));
     else AKVS_ATTEND((k_shared_bf16<HD, false>));
@@ -1136,15 +1148,16 @@ static hipError_t shared_attention(const SharedBatch &s, const void *q, const vo
 #undef AKVS_ATTEND
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.slots <= 1) return e;
-  if (p.slots <= MERGE_FEW)
-    hipLaunchKernelGGL((k_shared_merge_few<TS, TP>), dim3((unsigned)((items * (HD / 8) + 255) / 256)),
-                       b, 0, st, s, p.slots, hq, HD, po, ml, O, lse);
-  else if (p.slots <= MERGE_WAVE)
-    hipLaunchKernelGGL((k_shared_merge_wave<TS, TP, HD>), dim3((unsigned)((items + 3) / 4)), b, 0, st,
-                       s, p.slots, hq, po, ml, O, lse);
-  else
-    hipLaunchKernelGGL((k_shared_merge<TS, TP, HD>), dim3((unsigned)items), b, 0, st, s, p.slots, hq,
-                       po, ml, O, lse);
+  if (p.slots <= MERGE_FEW) {
+    const dim3 gm((unsigned)((items * (HD / 8) + 255) / 256));
+    hipLaunchKernelGGL((k_shared_merge_few<TS, TP>), gm, b, 0, st, s, p.slots, hq, HD, po, ml, O, lse);
+  } else if (p.slots <= MERGE_WAVE) {
+    const dim3 gm((unsigned)((items + 3) / 4));
+    hipLaunchKernelGGL((k_shared_merge_wave<TS, TP, HD>), gm, b, 0, st, s, p.slots, hq, po, ml, O, lse);
+  } else {
+    const dim3 gm((unsigned)items);
+    hipLaunchKernelGGL((k_shared_merge<TS, TP, HD>), gm, b, 0, st, s, p.slots, hq, po, ml, O, lse);
+  }
   return hipGetLastError();
 }
 
@@ -1162,11 +1175,11 @@ hipError_t launch_shared_attention(const SharedBatch &s, const void *q, const vo
 
 // Two key tiles a wave share a pair tile's staging and LDS reads, but a block then has 256 keys and
 // its unit three blocks of 166 registers: taken where the prefix makes two such blocks a unit by
-// parts of eight tiles (1070 rows over 4516 keys of 24/8 heads: 57 us with two, 63 with one; 600
-// over 16128 of 40/8 127 and 140; 195 over 506 of 40/8 24 and 18). The pairs go in parts while the
+// parts of eight tiles (1171 rows over 4516 keys of 24/8 heads: 57 us with two, 63 with one; 584
+// over 16128 of 40/8 127 and 140; 189 over 506 of 40/8 23 and 18). The pairs go in parts while the
 // keys alone do not fill the units, at least four tiles each. So do a request's over its own keys,
-// eight tiles each, or its one block walks them all: 256 rows over 9000 keys and up to 128 own of
-// 28/4 heads 73 us whole, 35 in parts as long as the prefix's, 33 by eight; 1800 rows of 8 requests
+// eight tiles each, or its one block walks them all: 256 rows over 9000 keys and 256 own of
+// 28/4 heads 73 us whole, 35 in parts as long as the prefix's, 33 by eight; 1835 rows of 8 requests
 // over 2000 92, 55 and 49 (up to 16 blocks a unit: most of the room may be empty).
 template <typename TS>
 static WeightPlan weight_plan(const SharedBatch &s, int hq, int hkv, bool prefix, bool own) {
@@ -1227,8 +1240,8 @@ static hipError_t attention_weights(const SharedBatch &s, const void *q, const f
   const float scale = 1.4426950408889634f / sqrtf((float)hd);
   auto x = [](const void *a) { return reinterpret_cast<const TS *>(a); };
 #define AKVS_WEIGHTS(HD_, NK_)                                                                 \
-  hipLaunchKernelGGL((k_attn_weights<TS, HD_, NK_>), dim3((unsigned)blocks), dim3(256), 0, st, s, p, \
-                     x(q), lse, x(kp), x(ko), hq, hkv, scale, split ? nullptr : wp_prev,        \
+  hipLaunchKernelGGL((k_attn_weights<TS, HD_, NK_>), dim3((unsigned)blocks), dim3(256), 0, st, s,  \
+                     p, x(q), lse, x(kp), x(ko), hq, hkv, scale, split ? nullptr : wp_prev,        \
                      split ? part : wp, own_split ? nullptr : wo_prev, own_split ? own_part : wo)
   if (hd == 128) {
     if (p.nk == 2) AKVS_WEIGHTS(128, 2); else AKVS_WEIGHTS(128, 1);
