@@ -1676,6 +1676,11 @@ static akvs_status check_shared(const akvs_model_cfg *m, const akvs_shared_cfg *
   return AKVS_OK;
 }
 
+static bool overlap(const void *a, size_t na, const void *b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
+
 extern "C" {
 
 akvs_status akvs_qk_norm_rope(const void *q, int64_t ldq, const void *k, int64_t ldk,
@@ -1707,6 +1712,25 @@ akvs_status akvs_qk_norm_rope(const void *q, int64_t ldq, const void *k, int64_t
           "row strides too large");
   REQUIRE(ldq * es % 16 == 0 && ldk * es % 16 == 0 && (!v || ldv * es % 16 == 0), AKVS_EINVAL,
           "row strides must be multiples of 16 bytes");
+  // (what is written must be read by the same lanes: the tensor itself, row by row, or elsewhere)
+  const struct {
+    const void *in, *out;
+    long long ld, width, out_rows;
+  } x[3] = {{q, q_out, ldq, hqw, n_rows},
+            {k, k_out, ldk, kvw, kv_rows ? n_kv_rows : n_rows},
+            {v, v_out, ldv, kvw, kv_rows ? n_kv_rows : n_rows}};
+  for (int i = 0; i < 3; ++i)
+    for (int j = 0; j < 3; ++j) {
+      if (!x[i].in || !x[j].in) continue;
+      const bool in_place = i == j && x[i].in == x[i].out && x[i].ld == x[i].width &&
+                            (i == 0 || !kv_rows);
+      const size_t in_bytes = ((n_rows - 1) * x[i].ld + x[i].width) * es;
+      const size_t out_bytes = x[j].out_rows * x[j].width * es;
+      REQUIRE(in_place || !overlap(x[i].in, in_bytes, x[j].out, out_bytes), AKVS_EINVAL,
+              "an output overlaps an input other than its own, dense and without kv_rows");
+      REQUIRE(i >= j || !overlap(x[i].out, x[i].out_rows * x[i].width * es, x[j].out, out_bytes),
+              AKVS_EINVAL, "outputs overlap");
+    }
   const QkNorm a{q,           k,      v,      ldq,          ldk,
                  ldv,         n_rows, m->n_q_heads, m->n_kv_heads, m->head_dim,
                  positions,   q_norm, k_norm, m->rms_eps,   rope,
@@ -1796,11 +1820,6 @@ static akvs_status check_evict(const akvs_model_cfg *m, const akvs_evict_cfg *c,
               (long long)a->n_keep * m->n_kv_heads * m->head_dim * es_of(m->dtype) < (1LL << 36),
           AKVS_ESHAPE, "too large");
   return AKVS_OK;
-}
-
-static bool overlap(const void *a, size_t na, const void *b, size_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + nb && y < x + na;
 }
 
 static size_t keep_bytes(const EvictArgs &a, const akvs_model_cfg *m) {

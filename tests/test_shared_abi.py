@@ -105,6 +105,26 @@ def test_rows_max_above_the_rows_is_the_rows(lib):
         assert (a > 0) == (prefix == 8000)
 
 
+def test_norm_overlaps(lib):
+    """Outputs over inputs other than their own, over each other, and in place where rows lie
+    apart or move."""
+    m, es = model(), 2
+    q, k, v, qo, ko, vo, pos = (1 << 30, 2 << 30, 3 << 30, 4 << 30, 5 << 30, 6 << 30, 7 << 30)
+    base = dict(q=q, ldq=24 * 128, k=k, ldk=8 * 128, v=v, ldv=8 * 128, rows=4, kv=None, n_kv=4,
+                qo=qo, ko=ko, vo=vo)
+    for kw in (dict(qo=k), dict(qo=k - 4 * 24 * 128 * es + 16), dict(ko=q), dict(ko=v), dict(vo=k),
+               dict(ko=qo), dict(vo=ko), dict(ko=qo + 4 * 24 * 128 * es - 16),
+               dict(qo=q + 24 * 128 * es), dict(qo=q, ldq=40 * 128), dict(ko=k, ldk=16 * 128),
+               dict(ko=k, kv=pos), dict(vo=v, kv=pos), dict(ko=v - 8 * 128 * es, kv=pos, n_kv=2),
+               dict(ko=v - 9 * 8 * 128 * es, kv=pos, n_kv=10)):
+        d = dict(base)
+        d.update(kw)
+        assert lib.akvs_qk_norm_rope(
+            d["q"], d["ldq"], d["k"], d["ldk"], d["v"], d["ldv"], d["rows"], pos, None, None,
+            ctypes.byref(m), pos, 10, d["kv"], d["n_kv"], d["qo"], d["ko"], d["vo"],
+            None) == akvs.AKVS_EINVAL, kw
+
+
 def test_norms_of_too_many_rows(lib):
     for n in (1 << 23, (1 << 31) - 1):
         m = model()
