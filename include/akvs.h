@@ -427,7 +427,8 @@ akvs_status akvs_decode_step_noalloc(const int32_t *token, int32_t n_past, const
  * [n_kv_rows][Hkv][hd]; rows that no token names stay as they were. q_out may be q where
  * ldq = Hq * hd (k_out k and v_out v likewise, without kv_rows); no other overlap. v and v_out
  * may both be NULL. Errors: EINVAL (negative sizes, null or misaligned pointers, strides
- * shorter than a row or not of 16 bytes, n_kv_rows < n_rows without kv_rows, overlaps), EHIP. */
+ * shorter than a row or not of 16 bytes, n_kv_rows < n_rows without kv_rows, overlaps),
+ * ESHAPE (too large), EHIP. */
 akvs_status akvs_qk_norm_rope(const void *q, int64_t ldq, const void *k, int64_t ldk,
                               const void *v, int64_t ldv, int32_t n_rows,
                               const int32_t *positions, const void *q_norm, const void *k_norm,
@@ -458,7 +459,7 @@ akvs_status akvs_shared_attention(const void *q, const akvs_shared_cfg *c, const
  * q, lse: as akvs_shared_attention took and left them; w_prefix, w_prefix_prev: device
  * [Hkv][P] fp32; w_own, w_own_prev: [B][Hkv][own_rows] fp32 (keys past own_len keep what they
  * had). A w_*_prev may be its w_* itself, or NULL (0). w_prefix or w_own may be NULL: that
- * side is not formed. A row with lse = -inf gives nothing. */
+ * side is not formed. A row with lse = -inf gives nothing. Errors as above. */
 akvs_status akvs_attention_weights(const void *q, const float *lse, const akvs_shared_cfg *c,
                                    const void *k_prefix, const void *k_own,
                                    const akvs_model_cfg *m, const float *w_prefix_prev,
@@ -479,7 +480,8 @@ size_t akvs_evict_workspace_size(const akvs_model_cfg *m, const akvs_evict_cfg *
  * [S][dst_rows][Hkv][hd], rows past the kept ones stay as they were, no overlap with k or v;
  * k, v, k_out, v_out may all be NULL (selection alone); weights_out (device
  * [S][Hkv][dst_rows] fp32, may be NULL, not `weights`): the kept keys' weights, then 0;
- * lens_out (device [S], may be NULL, may be lens): keys kept. */
+ * lens_out (device [S], may be NULL, may be lens): keys kept.
+ * Errors: EINVAL (sizes, pointers, overlaps) / ESHAPE / ENOSPACE, EHIP. */
 akvs_status akvs_evict_cache(const void *k, const void *v, const float *weights,
                              const akvs_evict_cfg *c, const akvs_model_cfg *m, int32_t *keep,
                              void *k_out, void *v_out, float *weights_out, int32_t *lens_out,
