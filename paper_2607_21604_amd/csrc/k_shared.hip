@@ -142,7 +142,7 @@ __global__ __launch_bounds__(256, 2) void k_shared_bf16(
   const int nkt = k1 > it.k0 ? (k1 - it.k0 + SH_TILE - 1) / SH_TILE : 0;
   const bool writes = valid && (groups == 4 || (works && (wave & 1) == 0));
   if (nkt == 0 && p.slots > 1) {
-    if (writes && hi == 0) part_ml[prow] = make_float4(-INFINITY, 0.f, 1.f, 0.f);
+    if (writes && hi == 0) part_ml[prow] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
     return;
   }
 
@@ -381,8 +381,10 @@ __global__ __launch_bounds__(256, 2) void k_shared_bf16(
 // out = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s over a pair's slots, M = max m_s. A slot
 // holds (m, l, f) and its output over f: fp32 values with f = 1, or fp16 with f a power of two
 // that brings the largest to [2^14, 2^15). fp16 carries 11 bits of a slot's large values, three
-// more than the bf16 result keeps, at half the traffic of fp32. A slot without a key holds
-// m = -inf, l = 0 (its output was not written and takes no part); one of NaN scores l = NaN.
+// more than the bf16 result keeps, at half the traffic of fp32. A slot whose keys the pair's tile
+// does not reach holds f = 0: its output was not written and takes no part. Every other slot
+// counts whatever its weight is, so that what is NaN in one (m = -inf, l = NaN where all scores
+// are NaN) is NaN in the result, as where the keys are not split.
 __device__ __forceinline__ void part_load8(const float *p, float (&x)[8]) { load8(p, x); }
 __device__ __forceinline__ void part_load8(const _Float16 *p, float (&x)[8]) {
   typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
@@ -390,9 +392,9 @@ __device__ __forceinline__ void part_load8(const _Float16 *p, float (&x)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
 }
-__device__ __forceinline__ float slot_factor(float4 ml, float M) {  // 0: takes no part
-  if (ml.y == 0.f) return 0.f;
-  return M == -INFINITY ? 1.f : exp2f(ml.x - M);  // (no maximum: all scores NaN)
+__device__ __forceinline__ bool slot_counts(float4 ml) { return ml.z != 0.f; }
+__device__ __forceinline__ float slot_factor(float4 ml, float M) {
+  return M == -INFINITY ? 1.f : exp2f(ml.x - M);  // (no maximum: scores NaN, or no key seen)
 }
 __device__ __forceinline__ float merged_lse(float M, float l) {
   if (l == 0.f) return -INFINITY;
@@ -429,8 +431,8 @@ __global__ __launch_bounds__(256) void k_shared_merge_few(SharedBatch s, int slo
 #pragma unroll
   for (int u = 0; u < MERGE_FEW; ++u)
     if (u < slots) {
+      if (!slot_counts(ml[u])) continue;
       const float w = slot_factor(ml[u], M);
-      if (w == 0.f) continue;
       l = fmaf(w, ml[u].y, l);
 #pragma unroll
       for (int i = 0; i < 8; ++i) a[i] = fmaf(w * ml[u].z, x[u][i], a[i]);
@@ -468,7 +470,8 @@ __global__ __launch_bounds__(256) void k_shared_merge_wave(SharedBatch s, int sl
   };
   request(0);
   const float M = wave_max(ml.x), w = slot_factor(ml, M);
-  const float l = wave_sum(w == 0.f ? 0.f : w * ml.y), wf = w == 0.f ? 0.f : w * ml.z;
+  const float l = wave_sum(slot_counts(ml) ? w * ml.y : 0.f);
+  const float wf = slot_counts(ml) ? w * ml.z : -1.f;  // (-1: takes no part)
   float a[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) a[i] = 0.f;
@@ -478,7 +481,7 @@ __global__ __launch_bounds__(256) void k_shared_merge_wave(SharedBatch s, int sl
     for (int q = 0; q < MERGE_AHEAD; ++q) {
       const int u = u0 + q * TEAMS + team;
       const float wq = __shfl(wf, u & 63, 64);
-      if (u < slots && wq != 0.f) {
+      if (u < slots && !(wq < 0.f)) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) a[i] = fmaf(wq, x[q][i], a[i]);
       }
@@ -530,9 +533,10 @@ __global__ __launch_bounds__(256) void k_shared_merge(SharedBatch s, int slots, 
   for (int i = 0; i < MERGE_SLOTS / 256; ++i) {
     const int u = tid + 256 * i;
     if (u < slots) {
+      const bool counts = slot_counts(ml[i]);
       const float w = slot_factor(ml[i], M);
-      if (w != 0.f) l = fmaf(w, ml[i].y, l);
-      s_w[u] = w == 0.f ? 0.f : w * ml[i].z;
+      if (counts) l = fmaf(w, ml[i].y, l);
+      s_w[u] = counts ? w * ml[i].z : -1.f;  // (-1: takes no part)
     }
   }
   l = wave_sum(l);
@@ -548,12 +552,12 @@ __global__ __launch_bounds__(256) void k_shared_merge(SharedBatch s, int slots, 
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int u = u0 + q * TEAMS;
-      w[q] = u < slots ? s_w[u] : 0.f;
+      w[q] = u < slots ? s_w[u] : -1.f;
       part_load8(part_o + (min(u, slots - 1) * stride + item) * HD + e0, x[q]);
     }
 #pragma unroll
     for (int q = 0; q < 4; ++q)
-      if (w[q] != 0.f) {
+      if (!(w[q] < 0.f)) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) a[i] = fmaf(w[q], x[q][i], a[i]);
       }
@@ -607,7 +611,7 @@ __global__ __launch_bounds__(256, 2) void k_shared_f32(
   if (k1 <= it.k0 && p.slots > 1) {
     if (tid < 16 && valid)
       part_ml[((size_t)it.slot * s.n_rows + r) * hq + head] =
-          make_float4(-INFINITY, 0.f, 1.f, 0.f);
+          make_float4(-INFINITY, 0.f, 0.f, 0.f);
     return;
   }
   if (tid == 0) s_odd = 0;

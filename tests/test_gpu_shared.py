@@ -941,3 +941,86 @@ def test_every_split(hq, hkv, hd, dt, prefix, rows, own):
     tol = ref.weights_bound(wp, far, hd, b.n * (hq // hkv)) + float(
         ref.lse_bound(lse, reach, hd, keys).max()) * wp
     assert bool((err <= tol).all()), float((err - tol).max())
+
+
+# ---- the merge of key splits ------------------------------------------------------------------
+
+def slots_of(b):
+    """(slots, keys of a prefix split) of a batch of few rows whose own keys are one chunk, from
+    the workspace: per slot and (row, head) the outputs (fp32, or fp16 in bf16 models) and four
+    floats."""
+    per_slot = 4 * b.n * b.hq * ((b.hd // 2 if b.dt == BF else b.hd) + 4)
+    slots = akvs.akvs_shared_workspace_size(b.m, b.cfg()) // per_slot
+    tiles = -(-b.P // 64)
+    per = [t for t in range(1, tiles + 1) if -(-tiles // t) == slots - 1]
+    assert len(per) == 1  # (the sizes here are chosen so)
+    return slots, 64 * per[0]
+
+
+# prefixes that are cut into up to 4, up to 32 and more slots (a merge kernel each)
+MERGES = [(448, 2, 4), (5000, 5, 32), (16384, 33, 1024)]
+
+
+@pytest.mark.parametrize("hq,hkv,hd,dt", [(8, 4, 128, BF), (8, 4, 64, BF), (4, 4, 64, F32), (8, 4, 128, F32)])
+@pytest.mark.parametrize("prefix,least,most", MERGES)
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_a_split_of_keys_that_are_not_finite(hq, hkv, hd, dt, prefix, least, most, bad):
+    """Split keys of which one slot holds nothing but keys of NaN (or of +-inf, whose scores with
+    a query of both signs are NaN): its rows are NaN as they are where the keys are not split,
+    all others the bits they were. First a request's only own key, then a split of the prefix in
+    one KV head, then a row's query."""
+    def batch():
+        return Batch(hq, hkv, hd, dt, prefix, [1, 1, 1], [1, 1, 1], seed=401)
+    b, G = batch(), hq // hkv
+    slots, keys = slots_of(b)
+    assert least <= slots <= most, slots
+    b.attend()
+    b.check()
+    out, lse = b.out.clone(), b.lse.clone()
+
+    c = batch()
+    c.ko[1, 0, 2] = bad
+    c.attend()
+    hit = torch.zeros(3, hq, dtype=torch.bool, device=DEV)
+    hit[1, 2 * G:3 * G] = True
+    assert bool(torch.isnan(c.out[hit].float()).all()) and bool(torch.isnan(c.lse[hit]).all())
+    assert torch.equal(c.out[~hit], out[~hit]) and torch.equal(c.lse[~hit], lse[~hit])
+
+    c = batch()
+    c.kp[keys:2 * keys, 1] = bad
+    c.attend()
+    hit = torch.zeros_like(hit)
+    hit[:, G:2 * G] = True
+    assert bool(torch.isnan(c.out[hit].float()).all()) and bool(torch.isnan(c.lse[hit]).all())
+    assert torch.equal(c.out[~hit], out[~hit]) and torch.equal(c.lse[~hit], lse[~hit])
+
+    c = batch()
+    c.q[2] = math.nan
+    c.attend()
+    assert bool(torch.isnan(c.out[2].float()).all()) and bool(torch.isnan(c.lse[2]).all())
+    # (the others keep the definition's bounds; when a pair's running maximum rises goes by all
+    # pairs of its wave, so not their bits)
+    c.q[2], c.out[2], c.lse[2] = b.q[2], out[2], lse[2]
+    c.check()
+
+
+@pytest.mark.parametrize("hq,hkv,hd,dt", [(4, 4, 128, BF), (4, 4, 64, F32)])
+@pytest.mark.parametrize("prefix,least,most", MERGES)
+def test_a_value_of_a_weight_that_underflows(hq, hkv, hd, dt, prefix, least, most):
+    """A request's only own key has a weight of some 2^-280 of a prefix key's, in a slot of its own:
+    the row is that of the prefix alone; a value that is not finite there spoils its dimension
+    (the definition's weight is above 0) and no other."""
+    b = Batch(hq, hkv, hd, dt, prefix, [1, 1], [1, 1], seed=411, q_std=0.0)
+    assert least <= slots_of(b)[0] <= most
+    b.q[..., 0] = 8.0
+    b.kp[..., 0] = 0.0
+    b.ko[0, 0] = 0.0
+    b.ko[0, 0, :, 0] = -25.0 * math.sqrt(hd)  # a score of -200
+    b.attend()
+    b.check()
+    out, lse = b.out.clone(), b.lse.clone()
+    b.vo[0, 0, :, 7] = math.inf
+    b.attend()
+    assert not bool(torch.isfinite(b.out[0, :, 7].float()).any())
+    b.out[0, :, 7] = out[0, :, 7]
+    assert torch.equal(b.out, out) and torch.equal(b.lse, lse)
