@@ -381,10 +381,23 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope(QkNorm a) {
         rs = 1.0 / sqrt(wide * (1.0 / hd) + (double)a.eps);
       }
     }
+    // The products with the gains are exact: fp64 ones in fp32 models; fp32 ones in bf16 models, of a
+    // head that a power of two brings below 1 (|x| rs <= sqrt(hd) < 2^4), which leave fp32's range
+    // only where the result does.
+    constexpr bool exact_f32 = sizeof(TS) == 2;
+    if (exact_f32 && gain) {
+      const int e = __builtin_amdgcn_frexp_exp(rs) - 5;  // (rs in [2^(e + 4), 2^(e + 5)))
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        lo[i] = ldexpf(lo[i], e) * gl[i];
+        hi[i] = ldexpf(hi[i], e) * gh[i];
+      }
+      rs = ldexp(rs, -e);
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      // in bf16 models the products with the gains are exact in fp32
-      const double x = gain ? lo[i] * gl[i] : lo[i], y = gain ? hi[i] * gh[i] : hi[i];
+      const double x = !exact_f32 && gain ? (double)lo[i] * gl[i] : lo[i];
+      const double y = !exact_f32 && gain ? (double)hi[i] * gh[i] : hi[i];
       const double c = cs[2 * i], s = cs[2 * i + 1];
       lo[i] = (float)(rs * (x * c - y * s));
       hi[i] = (float)(rs * (y * c + x * s));

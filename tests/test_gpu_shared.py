@@ -1024,3 +1024,35 @@ def test_a_value_of_a_weight_that_underflows(hq, hkv, hd, dt, prefix, least, mos
     assert not bool(torch.isfinite(b.out[0, :, 7].float()).any())
     b.out[0, :, 7] = out[0, :, 7]
     assert torch.equal(b.out, out) and torch.equal(b.lse, lse)
+
+
+# ---- products with the gains that leave fp32's range -------------------------------------------
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("eps", [0.0, 1e-6])
+def test_qk_norm_of_products_that_leave_the_range(dt, eps, hd):
+    """Values next to the largest number with gains above 1 and, without an eps, next to the
+    smallest normal one with gains below: value times gain is no fp32 number, the normalised
+    head times gain is. Beside ordinary rows of the same wave."""
+    m = model(4, 2, hd, dt)
+    m.rms_eps = eps
+    tab, n = rope(8, hd), 5
+    sign = lambda seed, h: torch.where(randn(seed, n, h, hd) < 0, -1.0, 1.0)  # noqa: E731
+    part = lambda seed, h: 0.5 + 0.5 * randn(seed, n, h, hd).abs().clamp(max=1.0)  # noqa: E731
+    q, k = (sign(i, h) * part(i + 5, h) for i, h in ((1, 4), (2, 2)))
+    for x in (q, k):
+        x[1] *= 3.0e38
+        x[3] *= 3.0e38 if eps else 3.0e-38
+    q, k = q.to(dt), k.to(dt)
+    assert bool(torch.isfinite(q.float()).all()) and bool((q != 0).all())
+    big = randn(3, hd).abs() * 20 + 2
+    small = (randn(4, hd).abs() + 1) * 1e-5
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    cs = tab.cpu()[np.arange(n)]
+    for g in (big.to(dt), small.to(dt)):
+        akvs.akvs_qk_norm_rope(q, k, None, n, ints(np.arange(n)), g, g, m, tab, 8, None, n, qo, ko,
+                               None)
+        for got, x in ((qo, q), (ko, k)):
+            want, mags = ref.norm_rope(x, g, cs[..., 0], cs[..., 1], eps)
+            close_rotated(got, want, mags, dt)
