@@ -447,7 +447,8 @@ size_t akvs_shared_workspace_size(const akvs_model_cfg *m, const akvs_shared_cfg
  * dtype. lse (device [n_rows][Hq] fp32, may be NULL): natural log of the row's sum of
  * exp(score). A row that sees no key gets out 0 and lse -inf. Keys past a row's last one are
  * never part of its result, whatever they hold; rows from row_start[B] on stay as they were.
- * Errors: EINVAL / ESHAPE / ENOSPACE, EHIP. */
+ * out may be q; out, lse and ws overlap nothing else.
+ * Errors: EINVAL (sizes, pointers, overlaps) / ESHAPE / ENOSPACE, EHIP. */
 akvs_status akvs_shared_attention(const void *q, const akvs_shared_cfg *c, const void *k_prefix,
                                   const void *v_prefix, const void *k_own, const void *v_own,
                                   const akvs_model_cfg *m, void *out, float *lse, void *ws,
@@ -458,8 +459,9 @@ akvs_status akvs_shared_attention(const void *q, const akvs_shared_cfg *c, const
  * w[j] = w_prev[j] + sum_r sum_h exp(q.k_j/sqrt(hd) - lse[r][h]), fp32 sums in a fixed order.
  * q, lse: as akvs_shared_attention took and left them; w_prefix, w_prefix_prev: device
  * [Hkv][P] fp32; w_own, w_own_prev: [B][Hkv][own_rows] fp32 (keys past own_len keep what they
- * had). A w_*_prev may be its w_* itself, or NULL (0). w_prefix or w_own may be NULL: that
- * side is not formed. A row with lse = -inf gives nothing. Errors as above. */
+ * had). A w_*_prev may be its w_* itself, or NULL (0); w_prefix, w_own and ws overlap nothing
+ * else. w_prefix or w_own may be NULL: that side is not formed. A row with lse = -inf gives
+ * nothing. Errors as above. */
 akvs_status akvs_attention_weights(const void *q, const float *lse, const akvs_shared_cfg *c,
                                    const void *k_prefix, const void *k_own,
                                    const akvs_model_cfg *m, const float *w_prefix_prev,

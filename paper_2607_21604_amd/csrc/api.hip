@@ -1681,6 +1681,44 @@ static bool overlap(const void *a, size_t na, const void *b, size_t nb) {
   return x < y + nb && y < x + na;
 }
 
+// A buffer of a call: read (INPUT), or written, then the index of the input that it may be itself
+// (an update in place) or NONE.
+struct Buffer {
+  const char *name;
+  const void *p;
+  size_t bytes;
+  int in_place;
+};
+constexpr int INPUT = -2, NONE = -1;
+static akvs_status check_apart(const Buffer *b, int n) {
+  for (int i = 0; i < n; ++i)
+    for (int j = 0; j < n; ++j) {
+      if (i == j || b[i].in_place == INPUT || !b[i].p || !b[j].p || !b[i].bytes || !b[j].bytes)
+        continue;
+      const bool itself = b[i].in_place == j && b[i].p == b[j].p && b[i].bytes == b[j].bytes;
+      REQUIRE(itself || !overlap(b[i].p, b[i].bytes, b[j].p, b[j].bytes), AKVS_EINVAL,
+              "%s overlaps %s", b[i].name, b[j].name);
+    }
+  return AKVS_OK;
+}
+
+// Bytes of the tensors of a batch over one shared context.
+struct SharedBytes {
+  size_t q, lse, prefix, own, row_start, own_len, w_prefix, w_own;
+  SharedBytes(const akvs_model_cfg *m, const SharedBatch &s) {
+    const size_t es = es_of(m->dtype), kv = m->n_kv_heads * m->head_dim * es;
+    const size_t own_keys = (size_t)s.n_req * s.own_rows;
+    q = (size_t)s.n_rows * m->n_q_heads * m->head_dim * es;
+    lse = (size_t)s.n_rows * m->n_q_heads * sizeof(float);
+    prefix = s.prefix_len * kv;
+    own = own_keys * kv;
+    row_start = (s.n_req + 1) * sizeof(int32_t);
+    own_len = s.n_req * sizeof(int32_t);
+    w_prefix = (size_t)s.prefix_len * m->n_kv_heads * sizeof(float);
+    w_own = own_keys * m->n_kv_heads * sizeof(float);
+  }
+};
+
 extern "C" {
 
 akvs_status akvs_qk_norm_rope(const void *q, int64_t ldq, const void *k, int64_t ldk,
@@ -1765,6 +1803,20 @@ akvs_status akvs_shared_attention(const void *q, const akvs_shared_cfg *c, const
   const size_t need = akvs_shared_workspace_size(m, c);
   REQUIRE(need == 0 || (ws && ws_bytes >= need), AKVS_ENOSPACE, "workspace %zu < %zu bytes",
           ws_bytes, need);
+  const SharedBytes n(m, s);
+  // (a row's query is read by the blocks that write the row, before they do, or by a launch before)
+  const Buffer buffers[] = {{"q", q, n.q, INPUT},
+                            {"k_prefix", k_prefix, n.prefix, INPUT},
+                            {"v_prefix", v_prefix, n.prefix, INPUT},
+                            {"k_own", k_own, n.own, INPUT},
+                            {"v_own", v_own, n.own, INPUT},
+                            {"row_start", s.row_start, n.row_start, INPUT},
+                            {"own_len", s.own_len, n.own_len, INPUT},
+                            {"out", out, n.q, 0},
+                            {"lse", lse, n.lse, NONE},
+                            {"ws", ws, need, NONE}};
+  st = check_apart(buffers, 10);
+  if (st) return st;
   LAUNCH(AKVS_K_ATTENTION,
          launch_shared_attention(s, q, k_prefix, v_prefix, k_own, v_own, m->n_q_heads,
                                  m->n_kv_heads, m->head_dim, m->dtype, out, lse,
@@ -1791,6 +1843,21 @@ akvs_status akvs_attention_weights(const void *q, const float *lse, const akvs_s
   const size_t need = akvs_shared_workspace_size(m, c);
   REQUIRE(need == 0 || (ws && ws_bytes >= need), AKVS_ENOSPACE, "workspace %zu < %zu bytes",
           ws_bytes, need);
+  const SharedBytes n(m, s);
+  const size_t prefix = w_prefix ? n.w_prefix : 0, own = w_own ? n.w_own : 0;
+  const Buffer buffers[] = {{"q", q, n.q, INPUT},
+                            {"lse", lse, n.lse, INPUT},
+                            {"k_prefix", k_prefix, w_prefix ? n.prefix : 0, INPUT},
+                            {"k_own", k_own, w_own ? n.own : 0, INPUT},
+                            {"row_start", s.row_start, n.row_start, INPUT},
+                            {"own_len", s.own_len, n.own_len, INPUT},
+                            {"w_prefix_prev", w_prefix_prev, prefix, INPUT},
+                            {"w_own_prev", w_own_prev, own, INPUT},
+                            {"w_prefix", w_prefix, prefix, 6},
+                            {"w_own", w_own, own, 7},
+                            {"ws", ws, need, NONE}};
+  st = check_apart(buffers, 11);
+  if (st) return st;
   LAUNCH(AKVS_K_ATTENTION,
          launch_attention_weights(s, q, lse, k_prefix, k_own, m->n_q_heads, m->n_kv_heads,
                                   m->head_dim, m->dtype, w_prefix_prev, w_prefix, w_own_prev,

@@ -1056,3 +1056,17 @@ def test_qk_norm_of_products_that_leave_the_range(dt, eps, hd):
         for got, x in ((qo, q), (ko, k)):
             want, mags = ref.norm_rope(x, g, cs[..., 0], cs[..., 1], eps)
             close_rotated(got, want, mags, dt)
+
+
+# ---- in place -------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("hq,hkv,hd,dt", [(28, 4, 128, BF), (6, 2, 64, BF), (4, 2, 128, F32)])
+@pytest.mark.parametrize("prefix,own", [(100, 90), (448, 5), (5000, 40), (30000, 1), (500, 0), (100, 0)])
+def test_attention_over_its_queries(hq, hkv, hd, dt, prefix, own):
+    """out may be q: the same bits, whole, split or alone over the prefix."""
+    b = Batch(hq, hkv, hd, dt, prefix, [3, 1, 40], [own] * 3, seed=421)
+    b.attend()
+    out, lse = b.out.clone(), b.lse.clone()
+    b.out = b.q
+    b.attend()
+    assert torch.equal(b.out, out) and torch.equal(b.lse, lse)

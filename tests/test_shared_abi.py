@@ -277,3 +277,70 @@ def test_engine_refuses_wrong_tensors(engine):
                  (q, bf(3, 128), bf(3, 128), pos, None, None, torch.zeros(5, 64, 2))):
         with pytest.raises(ValueError):
             engine.qk_norm_rope(*args)
+
+
+MB = 1 << 20
+
+
+def overlapping(lib, call, args, cases):
+    """Every call with one buffer moved over another is refused and says so."""
+    for name, at in cases:
+        bad = dict(args)
+        bad[name] = at
+        assert call(bad) == akvs.AKVS_EINVAL, (name, at)
+        assert b"overlaps" in lib.akvs_last_error(), (name, at)
+
+
+@pytest.mark.parametrize("prefix,own", [(100, 16), (8000, 16), (8000, 0)])
+def test_attention_overlaps(lib, prefix, own):
+    """Outputs and the workspace over inputs, tables and each other; out over q is q itself or
+    nothing of it."""
+    m, rows = model(24, 8, 128), 4
+    q, kv = rows * 24 * 128 * 2, 8 * 128 * 2
+    a = {n: (16 + 64 * i) * MB for i, n in enumerate(
+        ("q", "kp", "vp", "ko", "vo", "start", "len", "out", "lse", "ws"))}
+    need = akvs.akvs_shared_workspace_size(m, shared(prefix_len=prefix, own_rows=own))
+
+    def call(x):
+        c = shared(prefix_len=prefix, own_rows=own, row_start=x["start"], own_len=x["len"])
+        return lib.akvs_shared_attention(x["q"], ctypes.byref(c), x["kp"], x["vp"], x["ko"], x["vo"],
+                                         ctypes.byref(m), x["out"], x["lse"], x["ws"], need, None)
+    cases = [("out", a["q"] + 16), ("out", a["q"] - 16), ("out", a["kp"]),
+             ("out", a["kp"] - q + 16), ("out", a["vp"] + prefix * kv - 16), ("out", a["start"]),
+             ("out", a["len"]), ("lse", a["q"]), ("lse", a["out"]), ("lse", a["out"] + q - 16),
+             ("lse", a["kp"]), ("lse", a["start"]), ("lse", a["len"] - rows * 24 * 4 + 16)]
+    if own:
+        cases += [("out", a["ko"] + 4 * own * kv - 16), ("lse", a["vo"])]
+    if need:
+        cases += [("ws", a["q"]), ("ws", a["out"] - need + 256), ("ws", a["lse"]), ("ws", a["vp"]),
+                  ("out", a["ws"] + need - 16)]
+    overlapping(lib, call, a, cases)
+
+
+@pytest.mark.parametrize("prefix,own,rows", [(100, 16, 4), (8000, 16, 4), (300, 64, 256)])
+def test_weights_overlaps(lib, prefix, own, rows):
+    """Weights over inputs, tables, each other and each other's earlier ones; a side's earlier
+    weights are its weights or nothing of them."""
+    m = model(24, 8, 128)
+    cfg = dict(prefix_len=prefix, own_rows=own, n_rows=rows, rows_max=rows // 4)
+    wp, wo = 8 * prefix * 4, 4 * 8 * own * 4
+    a = {n: (16 + 64 * i) * MB for i, n in enumerate(
+        ("q", "lse", "kp", "ko", "start", "len", "wp0", "wo0", "wp", "wo", "ws"))}
+    need = akvs.akvs_shared_workspace_size(m, shared(**cfg))
+
+    def call(x):
+        c = shared(row_start=x["start"], own_len=x["len"], **cfg)
+        return lib.akvs_attention_weights(x["q"], x["lse"], ctypes.byref(c), x["kp"], x["ko"],
+                                          ctypes.byref(m), x["wp0"], x["wp"], x["wo0"], x["wo"], x["ws"],
+                                          need, None)
+    cases = [("wp", a["wp0"] + 16), ("wp", a["wp0"] - 16), ("wo", a["wo0"] + 16), ("wp", a["wo0"]),
+             ("wo", a["wp0"]), ("wo", a["wp"]), ("wo", a["wp"] + wp - 16), ("wp", a["wo"] + wo - 16),
+             ("wp", a["q"]), ("wo", a["lse"]), ("wp", a["kp"]), ("wo", a["ko"]), ("wo", a["start"]),
+             ("wp", a["len"] - wp + 16)]
+    if need:
+        cases += [("ws", a["q"]), ("ws", a["wp"] - need + 256), ("ws", a["wo0"]), ("wo", a["ws"])]
+    overlapping(lib, call, a, cases)
+    for side in ("wp", "wo"):  # a side that is not formed
+        b = dict(a)
+        b[side] = b[side + "0"] = None
+        overlapping(lib, call, b, [({"wp": "wo", "wo": "wp"}[side], a["q"])])
