@@ -425,8 +425,8 @@ akvs_status akvs_decode_step_noalloc(const int32_t *token, int32_t n_past, const
  * that takes row r (one outside [0, n_kv_rows), e.g. -1, is written nowhere; rows must be
  * distinct), NULL: row r, n_kv_rows >= n_rows then. q_out: [n_rows][Hq][hd]; k_out, v_out:
  * [n_kv_rows][Hkv][hd]; rows that no token names stay as they were. q_out may be q where
- * ldq = Hq * hd (k_out k and v_out v likewise, without kv_rows); no other overlap. v and v_out
- * may both be NULL. Errors: EINVAL (negative sizes, null or misaligned pointers, strides
+ * ldq = Hq * hd (k_out k and v_out v likewise, without kv_rows); outputs overlap nothing else.
+ * v and v_out may both be NULL. Errors: EINVAL (negative sizes, null or misaligned pointers, strides
  * shorter than a row or not of 16 bytes, n_kv_rows < n_rows without kv_rows, overlaps),
  * ESHAPE (too large), EHIP. */
 akvs_status akvs_qk_norm_rope(const void *q, int64_t ldq, const void *k, int64_t ldk,
@@ -479,10 +479,10 @@ size_t akvs_evict_workspace_size(const akvs_model_cfg *m, const akvs_evict_cfg *
  * and values move to rows 0.. of k_out / v_out as they are (keys keep their rotation).
  * k, v: [S][src_rows][Hkv][hd] model dtype; weights: [S][Hkv][n_keys] fp32; keep (device
  * [S][Hkv][n_keep], may be NULL): indices of the kept keys, -1 past the last; k_out, v_out:
- * [S][dst_rows][Hkv][hd], rows past the kept ones stay as they were, no overlap with k or v;
- * k, v, k_out, v_out may all be NULL (selection alone); weights_out (device
- * [S][Hkv][dst_rows] fp32, may be NULL, not `weights`): the kept keys' weights, then 0;
- * lens_out (device [S], may be NULL, may be lens): keys kept.
+ * [S][dst_rows][Hkv][hd], rows past the kept ones stay as they were; k, v, k_out, v_out may all
+ * be NULL (selection alone); weights_out (device [S][Hkv][dst_rows] fp32, may be NULL): the kept
+ * keys' weights, then 0; lens_out (device [S], may be NULL, may be lens): keys kept. Outputs and
+ * ws overlap nothing else.
  * Errors: EINVAL (sizes, pointers, overlaps) / ESHAPE / ENOSPACE, EHIP. */
 akvs_status akvs_evict_cache(const void *k, const void *v, const float *weights,
                              const akvs_evict_cfg *c, const akvs_model_cfg *m, int32_t *keep,

@@ -1769,6 +1769,18 @@ akvs_status akvs_qk_norm_rope(const void *q, int64_t ldq, const void *k, int64_t
       REQUIRE(i >= j || !overlap(x[i].out, x[i].out_rows * x[i].width * es, x[j].out, out_bytes),
               AKVS_EINVAL, "outputs overlap");
     }
+  const size_t gain_bytes = m->head_dim * es, ints = n_rows * sizeof(int32_t);
+  const size_t kv_bytes = x[1].out_rows * kvw * es;
+  const Buffer tables[] = {{"positions", positions, ints, INPUT},
+                           {"kv_rows", kv_rows, ints, INPUT},
+                           {"q_norm", q_norm, gain_bytes, INPUT},
+                           {"k_norm", k_norm, gain_bytes, INPUT},
+                           {"rope", rope, rope_rows * (size_t)m->head_dim * sizeof(float), INPUT},
+                           {"q_out", q_out, (size_t)(n_rows * hqw * es), NONE},
+                           {"k_out", k_out, kv_bytes, NONE},
+                           {"v_out", v_out, kv_bytes, NONE}};
+  st = check_apart(tables, 8);
+  if (st) return st;
   const QkNorm a{q,           k,      v,      ldq,          ldk,
                  ldv,         n_rows, m->n_q_heads, m->n_kv_heads, m->head_dim,
                  positions,   q_norm, k_norm, m->rms_eps,   rope,
@@ -1915,18 +1927,23 @@ akvs_status akvs_evict_cache(const void *k, const void *v, const float *weights,
               aligned16(k_out) && aligned16(v_out) && aligned16(weights_out) && aligned16(ws),
           AKVS_EINVAL, "misaligned argument");
   const size_t row = (size_t)m->n_kv_heads * m->head_dim * es_of(m->dtype);
-  const size_t from = a.n_seq * (size_t)a.src_rows * row, to = a.n_seq * (size_t)a.dst_rows * row;
-  REQUIRE(!k || (!overlap(k, from, k_out, to) && !overlap(k, from, v_out, to) &&
-                 !overlap(v, from, k_out, to) && !overlap(v, from, v_out, to) &&
-                 !overlap(k_out, to, v_out, to)),
-          AKVS_EINVAL, "k_out / v_out overlap k, v or each other");
-  REQUIRE(!weights_out ||
-              !overlap(weights, (size_t)a.n_seq * m->n_kv_heads * a.n_keys * 4, weights_out,
-                       (size_t)a.n_seq * m->n_kv_heads * a.dst_rows * 4),
-          AKVS_EINVAL, "weights_out overlaps weights");
   const size_t need = akvs_evict_workspace_size(m, c);
   REQUIRE(keep || (ws && ws_bytes >= need), AKVS_ENOSPACE, "workspace %zu < %zu bytes", ws_bytes,
           need);
+  const size_t heads = (size_t)a.n_seq * m->n_kv_heads, from = a.n_seq * (size_t)a.src_rows * row;
+  const size_t to = a.n_seq * (size_t)a.dst_rows * row, lens = a.n_seq * sizeof(int32_t);
+  const Buffer buffers[] = {{"k", k, from, INPUT},
+                            {"v", v, from, INPUT},
+                            {"weights", weights, heads * a.n_keys * sizeof(float), INPUT},
+                            {"lens", a.lens, lens, INPUT},
+                            {"keep", keep, heads * a.n_keep * sizeof(int32_t), NONE},
+                            {"k_out", k_out, to, NONE},
+                            {"v_out", v_out, to, NONE},
+                            {"weights_out", weights_out, heads * a.dst_rows * sizeof(float), NONE},
+                            {"lens_out", lens_out, lens, 3},
+                            {"ws", ws, ws_bytes >= need ? need : 0, NONE}};
+  st = check_apart(buffers, 10);
+  if (st) return st;
   if (!keep) keep = reinterpret_cast<int32_t *>(ws);
   const bool split = ws && ws_bytes >= need && evict_scratch_bytes(a, m->n_kv_heads) > 0;
   void *scratch = split ? reinterpret_cast<char *>(ws) + keep_bytes(a, m) : nullptr;

@@ -344,3 +344,41 @@ def test_weights_overlaps(lib, prefix, own, rows):
         b = dict(a)
         b[side] = b[side + "0"] = None
         overlapping(lib, call, b, [({"wp": "wo", "wo": "wp"}[side], a["q"])])
+
+
+@pytest.mark.parametrize("keys", [100, 40000])
+def test_eviction_overlaps(lib, keys):
+    """Each output and the workspace over inputs and each other; lens_out over lens is lens itself."""
+    m, S, H, keep = model(2, 2, 64), 2, 2, 10
+    e = akvs.evict_cfg(S, keys, keep)
+    a = {n: (16 + 64 * i) * MB for i, n in enumerate(
+        ("k", "v", "w", "lens", "keep", "ko", "vo", "wo", "lo", "ws"))}
+    need = akvs.akvs_evict_workspace_size(m, e)
+
+    def call(x):
+        c = akvs.EvictCfg(S, keys, 0, keep, 0, 0, 0, x["lens"])
+        return lib.akvs_evict_cache(x["k"], x["v"], x["w"], ctypes.byref(c), ctypes.byref(m), x["keep"],
+                                    x["ko"], x["vo"], x["wo"], x["lo"], x["ws"], need, None)
+    n_keep, n_w = S * H * keep * 4, S * H * keys * 4
+    cases = [("keep", a["w"] + n_w - 16), ("keep", a["k"]), ("keep", a["ko"]), ("keep", a["wo"]),
+             ("keep", a["lens"]), ("ko", a["keep"] + n_keep - 16), ("wo", a["w"]), ("wo", a["vo"]),
+             ("wo", a["lens"]), ("lo", a["lens"] + 4), ("lo", a["w"]), ("lo", a["keep"]), ("lo", a["vo"]),
+             ("ws", a["w"]), ("ws", a["keep"] - need + 256), ("ws", a["lens"]), ("vo", a["ws"])]
+    overlapping(lib, call, a, cases)
+    a["keep"] = None
+    overlapping(lib, call, a, [("ws", a["k"]), ("ws", a["wo"] - need + 16)])
+
+
+def test_norm_overlaps_of_tables(lib):
+    """Outputs over positions, rows, gains and the rotary table."""
+    m, n, hd = model(24, 8, 128), 4, 128
+    a = {x: (16 + 64 * i) * MB for i, x in enumerate(
+        ("q", "k", "v", "pos", "gq", "gk", "rope", "rows", "qo", "ko", "vo"))}
+
+    def call(x):
+        return lib.akvs_qk_norm_rope(x["q"], 24 * hd, x["k"], 8 * hd, x["v"], 8 * hd, n, x["pos"],
+                                     x["gq"], x["gk"], ctypes.byref(m), x["rope"], 10, x["rows"], 9,
+                                     x["qo"], x["ko"], x["vo"], None)
+    overlapping(lib, call, a, [(o, a[i]) for o in ("qo", "ko", "vo") for i in
+                               ("pos", "gq", "gk", "rope", "rows")] +
+                [("qo", a["rope"] + 10 * hd * 4 - 16), ("vo", a["pos"] - 9 * 8 * hd * 2 + 16)])
