@@ -444,6 +444,15 @@ __global__ __launch_bounds__(256) void k_shared_merge_few(SharedBatch s, int slo
   if (lse && e0 == 0) lse[item] = merged_lse(M, l);
 }
 
+// Blocks of a merge with a wave or a block per pair: a grid dimension has fewer than 2^32 threads.
+static dim3 merge_grid(size_t blocks) {
+  constexpr size_t WIDE = 1 << 20;
+  return dim3((unsigned)std::min(blocks, WIDE), (unsigned)((blocks + WIDE - 1) / WIDE));
+}
+__device__ __forceinline__ size_t merge_block() {
+  return (size_t)blockIdx.y * gridDim.x + blockIdx.x;
+}
+
 // Up to 32 slots: a wave per pair, its lanes a slot's (m, l, f) each, while HD / 8 lanes take the
 // outputs of a slot and 64 / (HD / 8) slots are read at a time, the first MERGE_AHEAD of a lane
 // requested with the statistics: one round trip to memory and no barrier. Attention of 235 rows
@@ -458,7 +467,7 @@ __global__ __launch_bounds__(256) void k_shared_merge_wave(SharedBatch s, int sl
                                                            float *__restrict__ lse) {
   constexpr int PER = HD / 8, TEAMS = 64 / PER;
   const int lane = threadIdx.x & 63, team = lane / PER, e0 = lane % PER * 8;
-  const size_t item = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6), stride = (size_t)s.n_rows * hq;
+  const size_t item = merge_block() * 4 + (threadIdx.x >> 6), stride = (size_t)s.n_rows * hq;
   if (item >= (size_t)shared_live(s) * hq) return;
   const float4 ml =
       lane < slots ? part_ml[lane * stride + item] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
@@ -513,7 +522,7 @@ __global__ __launch_bounds__(256) void k_shared_merge(SharedBatch s, int slots, 
   __shared__ float s_a[TEAMS][HD];
   __shared__ float s_m[4], s_l[4];
   const int tid = threadIdx.x, wave = tid >> 6;
-  const size_t item = blockIdx.x, stride = (size_t)s.n_rows * hq;
+  const size_t item = merge_block(), stride = (size_t)s.n_rows * hq;
   if (item >= (size_t)shared_live(s) * hq) return;
   float4 ml[MERGE_SLOTS / 256];
   float M = -INFINITY, l = 0.f;
@@ -1156,10 +1165,10 @@ static hipError_t shared_attention(const SharedBatch &s, const void *q, const vo
     const dim3 gm((unsigned)((items * (HD / 8) + 255) / 256));
     hipLaunchKernelGGL((k_shared_merge_few<TS, TP>), gm, b, 0, st, s, p.slots, hq, HD, po, ml, O, lse);
   } else if (p.slots <= MERGE_WAVE) {
-    const dim3 gm((unsigned)((items + 3) / 4));
+    const dim3 gm = merge_grid((items + 3) / 4);
     hipLaunchKernelGGL((k_shared_merge_wave<TS, TP, HD>), gm, b, 0, st, s, p.slots, hq, po, ml, O, lse);
   } else {
-    const dim3 gm((unsigned)items);
+    const dim3 gm = merge_grid(items);
     hipLaunchKernelGGL((k_shared_merge<TS, TP, HD>), gm, b, 0, st, s, p.slots, hq, po, ml, O, lse);
   }
   return hipGetLastError();

@@ -1070,3 +1070,28 @@ def test_attention_over_its_queries(hq, hkv, hd, dt, prefix, own):
     b.out = b.q
     b.attend()
     assert torch.equal(b.out, out) and torch.equal(b.lse, lse)
+
+
+# ---- large row buffers ------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("rows,slots", [(1 << 19, 33), (1 << 21, 5)])
+def test_merges_of_large_row_buffers(rows, slots):
+    """One row of one request, in buffers of so many rows that a block (33 slots) or a wave (5) for
+    each of their heads is 2^32 threads: the row's result, and nothing behind it written."""
+    hq, hkv, hd = 32, 8, 64
+    ws_bytes = 4 * slots * rows * hq * (hd // 2 + 4)
+    if torch.cuda.mem_get_info()[1] < 3 * ws_bytes:
+        pytest.skip("the partials' workspace is too large a part of this card")
+    own = 128 * slots  # (chunks of two key tiles)
+    b = Batch(hq, hkv, hd, BF, 0, [1], [own], seed=431)
+    q = torch.empty((rows, hq, hd), dtype=BF, device=DEV)
+    q[:1] = b.q
+    b.q, b.out = q, torch.full_like(q, 7.0)
+    b.lse = torch.full((rows, hq), 7.0, device=DEV)
+    c = akvs.shared_cfg(1, rows, 1, 0, own, ints([0, 1]), ints([own]))
+    assert akvs.akvs_shared_workspace_size(b.m, c) == ws_bytes
+    ws = torch.empty(ws_bytes, dtype=torch.uint8, device=DEV)
+    akvs.akvs_shared_attention(q, c, None, None, b.ko, b.vo, b.m, b.out, b.lse, ws)
+    b.check()
+    del q, ws, b
+    torch.cuda.empty_cache()
