@@ -1846,6 +1846,8 @@ akvs_status akvs_attention_weights(const void *q, const float *lse, const akvs_s
   if (st) return st;
   REQUIRE((q && lse) || s.n_rows == 0, AKVS_EINVAL, "NULL argument");
   REQUIRE(w_prefix || w_own, AKVS_EINVAL, "neither w_prefix nor w_own is given");
+  REQUIRE(weight_blocks(s, m->n_q_heads, m->n_kv_heads, m->dtype, w_prefix, w_own) < (1 << 24),
+          AKVS_ESHAPE, "prefix too large");  // (fewer than 2^32 threads of 256 a block)
   REQUIRE(k_prefix || s.prefix_len == 0 || !w_prefix, AKVS_EINVAL, "k_prefix is NULL");
   REQUIRE(k_own || s.own_rows == 0 || !w_own, AKVS_EINVAL, "k_own is NULL");
   REQUIRE(aligned16(q) && aligned16(lse) && aligned16(k_prefix) && aligned16(k_own) &&

@@ -1239,13 +1239,22 @@ size_t weight_part_floats(const SharedBatch &s, int hq, int hkv, int dtype) {
   return prefix_part_floats(s, p, hkv) + (p.own_parts > 1 ? p.own_parts * own_weights(s, hkv) : 0);
 }
 
+static size_t weight_blocks(const SharedBatch &s, const WeightPlan &p, int hkv) {
+  return p.prefix_blocks + (size_t)s.n_req * p.own_blocks * p.own_parts * hkv;
+}
+size_t weight_blocks(const SharedBatch &s, int hq, int hkv, int dtype, bool prefix, bool own) {
+  const WeightPlan p = dtype == AKVS_BF16 ? weight_plan<bf16_t>(s, hq, hkv, prefix, own)
+                                          : weight_plan<float>(s, hq, hkv, prefix, own);
+  return weight_blocks(s, p, hkv);
+}
+
 template <typename TS>
 static hipError_t attention_weights(const SharedBatch &s, const void *q, const float *lse,
                                     const void *kp, const void *ko, int hq, int hkv, int hd,
                                     const float *wp_prev, float *wp, const float *wo_prev,
                                     float *wo, float *part, hipStream_t st) {
   const WeightPlan p = weight_plan<TS>(s, hq, hkv, wp != nullptr, wo != nullptr);
-  const size_t blocks = p.prefix_blocks + (size_t)s.n_req * p.own_blocks * p.own_parts * hkv;
+  const size_t blocks = weight_blocks(s, p, hkv);
   if (blocks == 0) return hipSuccess;
   const bool split = p.parts > 1 && p.prefix_blocks > 0;
   const bool own_split = p.own_parts > 1 && p.own_blocks > 0;

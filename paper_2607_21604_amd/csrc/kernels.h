@@ -221,6 +221,8 @@ hipError_t launch_attention_weights(const SharedBatch &s, const void *q, const f
                                     hipStream_t st);
 // floats of `part` (sums of shares of the rows) that launch_attention_weights needs
 size_t weight_part_floats(const SharedBatch &s, int hq, int hkv, int dtype);
+// its blocks, for the sides that are formed
+size_t weight_blocks(const SharedBatch &s, int hq, int hkv, int dtype, bool prefix, bool own);
 // ---- k_evict.hip ----------------------------------------------------------------------
 struct EvictArgs {
   int n_seq, n_keys, src_rows, n_keep, dst_rows, n_first, n_recent;

@@ -382,3 +382,14 @@ def test_norm_overlaps_of_tables(lib):
     overlapping(lib, call, a, [(o, a[i]) for o in ("qo", "ko", "vo") for i in
                                ("pos", "gq", "gk", "rope", "rows")] +
                 [("qo", a["rope"] + 10 * hd * 4 - 16), ("vo", a["pos"] - 9 * 8 * hd * 2 + 16)])
+
+
+def test_weights_of_too_long_a_prefix(lib):
+    """Prefixes within the batch's limits whose keys alone are 2^32 threads."""
+    for m, kw in ((model(8, 8, 64), dict(prefix_len=(1 << 28) - 1)),
+                  (model(32, 32, 64, akvs.AKVS_F32), dict(prefix_len=1 << 25)),
+                  (model(16, 16, 64), dict(prefix_len=(1 << 27) - 64, n_req=64, n_rows=64))):
+        c = shared(**kw)
+        assert akvs.akvs_shared_workspace_size(m, c) > 0
+        assert lib.akvs_attention_weights(A, A, ctypes.byref(c), A, A, ctypes.byref(m), A, A, A, A, A,
+                                          1 << 40, None) == akvs.AKVS_ESHAPE
