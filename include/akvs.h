@@ -426,7 +426,7 @@ akvs_status akvs_decode_step_noalloc(const int32_t *token, int32_t n_past, const
  * distinct), NULL: row r, n_kv_rows >= n_rows then. q_out: [n_rows][Hq][hd]; k_out, v_out:
  * [n_kv_rows][Hkv][hd]; rows that no token names stay as they were. q_out may be q where
  * ldq = Hq * hd (k_out k and v_out v likewise, without kv_rows); outputs overlap nothing else.
- * v and v_out may both be NULL. Errors: EINVAL (negative sizes, null or misaligned pointers, strides
+ * v and v_out may both be NULL, k_out and v_out where n_kv_rows is 0. Errors: EINVAL (negative sizes, null or misaligned pointers, strides
  * shorter than a row or not of 16 bytes, n_kv_rows < n_rows without kv_rows, overlaps),
  * ESHAPE (too large), EHIP. */
 akvs_status akvs_qk_norm_rope(const void *q, int64_t ldq, const void *k, int64_t ldk,
@@ -460,8 +460,8 @@ akvs_status akvs_shared_attention(const void *q, const akvs_shared_cfg *c, const
  * q, lse: as akvs_shared_attention took and left them; w_prefix, w_prefix_prev: device
  * [Hkv][P] fp32; w_own, w_own_prev: [B][Hkv][own_rows] fp32 (keys past own_len keep what they
  * had). A w_*_prev may be its w_* itself, or NULL (0); w_prefix, w_own and ws overlap nothing
- * else. w_prefix or w_own may be NULL: that side is not formed. A row with lse = -inf gives
- * nothing. Errors as above. */
+ * else. w_prefix or w_own may be NULL: that side is not formed (both: where there are no keys).
+ * A row with lse = -inf gives nothing. Errors as above. */
 akvs_status akvs_attention_weights(const void *q, const float *lse, const akvs_shared_cfg *c,
                                    const void *k_prefix, const void *k_own,
                                    const akvs_model_cfg *m, const float *w_prefix_prev,
@@ -480,9 +480,10 @@ size_t akvs_evict_workspace_size(const akvs_model_cfg *m, const akvs_evict_cfg *
  * k, v: [S][src_rows][Hkv][hd] model dtype; weights: [S][Hkv][n_keys] fp32; keep (device
  * [S][Hkv][n_keep], may be NULL): indices of the kept keys, -1 past the last; k_out, v_out:
  * [S][dst_rows][Hkv][hd], rows past the kept ones stay as they were; k, v, k_out, v_out may all
- * be NULL (selection alone); weights_out (device [S][Hkv][dst_rows] fp32, may be NULL): the kept
- * keys' weights, then 0; lens_out (device [S], may be NULL, may be lens): keys kept. Outputs and
- * ws overlap nothing else.
+ * be NULL (selection alone), some where there are no rows to move (src_rows = n_keys = 0);
+ * weights_out (device [S][Hkv][dst_rows] fp32, may be NULL): the kept keys' weights, then 0;
+ * lens_out (device [S], may be NULL, may be lens): keys kept. Outputs and ws overlap nothing
+ * else.
  * Errors: EINVAL (sizes, pointers, overlaps) / ESHAPE / ENOSPACE, EHIP. */
 akvs_status akvs_evict_cache(const void *k, const void *v, const float *weights,
                              const akvs_evict_cfg *c, const akvs_model_cfg *m, int32_t *keep,

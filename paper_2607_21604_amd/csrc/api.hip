@@ -1738,8 +1738,9 @@ akvs_status akvs_qk_norm_rope(const void *q, int64_t ldq, const void *k, int64_t
   REQUIRE(kv_rows || n_kv_rows >= n_rows, AKVS_EINVAL,
           "n_kv_rows %d < n_rows %d without kv_rows", n_kv_rows, n_rows);
   if (n_rows == 0) return AKVS_OK;
-  REQUIRE(q && k && positions && rope && q_out && k_out, AKVS_EINVAL, "NULL argument");
-  REQUIRE((v == nullptr) == (v_out == nullptr), AKVS_EINVAL, "v and v_out go together");
+  REQUIRE(q && k && positions && rope && q_out, AKVS_EINVAL, "NULL argument");
+  REQUIRE(n_kv_rows == 0 || (k_out && (v == nullptr) == (v_out == nullptr)), AKVS_EINVAL,
+          "k_out is NULL, or one of v and v_out");
   REQUIRE(aligned16(q) && aligned16(k) && aligned16(v) && aligned16(q_norm) &&
               aligned16(k_norm) && aligned16(rope) && aligned16(q_out) && aligned16(k_out) &&
               aligned16(v_out),
@@ -1845,7 +1846,8 @@ akvs_status akvs_attention_weights(const void *q, const float *lse, const akvs_s
   akvs_status st = check_shared(m, c, &s);
   if (st) return st;
   REQUIRE((q && lse) || s.n_rows == 0, AKVS_EINVAL, "NULL argument");
-  REQUIRE(w_prefix || w_own, AKVS_EINVAL, "neither w_prefix nor w_own is given");
+  REQUIRE(w_prefix || w_own || (s.prefix_len == 0 && s.own_rows == 0), AKVS_EINVAL,
+          "neither w_prefix nor w_own is given");
   REQUIRE(weight_blocks(s, m->n_q_heads, m->n_kv_heads, m->dtype, w_prefix, w_own) < (1 << 24),
           AKVS_ESHAPE, "prefix too large");  // (fewer than 2^32 threads of 256 a block)
   REQUIRE(k_prefix || s.prefix_len == 0 || !w_prefix, AKVS_EINVAL, "k_prefix is NULL");
@@ -1923,8 +1925,8 @@ akvs_status akvs_evict_cache(const void *k, const void *v, const float *weights,
   akvs_status st = check_evict(m, c, &a);
   if (st) return st;
   REQUIRE(weights || a.n_keys == 0, AKVS_EINVAL, "weights are NULL");
-  REQUIRE((k && v && k_out && v_out) || (!k && !v && !k_out && !v_out), AKVS_EINVAL,
-          "k, v, k_out and v_out go together");
+  REQUIRE((k && v && k_out && v_out) || (!k && !v && !k_out && !v_out) || a.src_rows == 0,
+          AKVS_EINVAL, "k, v, k_out and v_out go together");
   REQUIRE(aligned16(k) && aligned16(v) && aligned16(weights) && aligned16(keep) &&
               aligned16(k_out) && aligned16(v_out) && aligned16(weights_out) && aligned16(ws),
           AKVS_EINVAL, "misaligned argument");

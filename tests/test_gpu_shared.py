@@ -1095,3 +1095,43 @@ def test_merges_of_large_row_buffers(rows, slots):
     b.check()
     del q, ws, b
     torch.cuda.empty_cache()
+
+
+# ---- nothing there yet --------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("hq,hkv,hd,dt", [(28, 4, 128, BF), (4, 2, 64, F32)])
+def test_engine_over_empty_tensors(hq, hkv, hd, dt):
+    """A context without a key, caches without a row, no rows: the engine's methods take them as
+    they take others (an empty tensor has no address)."""
+    from paper_2607_21604_amd.runtime import Engine
+    eng = Engine(_Shape(hq, hkv, hd, dt), {"layers": [{k: torch.zeros(8, device=DEV) for k in (
+        "attn_norm", "w_qkv", "w_o", "mlp_norm", "w_gate_up", "w_down")}]}, DEV)
+    q, none = randn(1, 3, hq, hd, dt=dt), randn(2, 0, hkv, hd, dt=dt)
+    own, ln = randn(3, 3, 0, hkv, hd, dt=dt), ints([0, 0, 0])
+    for more in ((), (own, own, ln)):
+        out, lse = eng.shared_attention(q, none, none, *more)
+        assert not out.any() and bool((lse == -math.inf).all())
+    wp, wo = eng.attention_weights(q, lse, none)
+    assert wp.shape == (hkv, 0) and wo is None
+    wp, wo = eng.attention_weights(q, lse, none, own, ln)
+    assert wp.shape == (hkv, 0) and wo.shape == (3, hkv, 0)
+    k = randn(4, 5, hkv, hd, dt=dt)
+    out, lse = eng.shared_attention(q[:0], k, k)
+    assert out.shape == (0, hq, hd)
+    wp, _ = eng.attention_weights(q[:0], lse, k)
+    assert wp.shape == (hkv, 5) and not wp.any()
+    # nothing to evict from: nothing kept
+    for rows in (0, 4):
+        c = randn(5, 2, rows, hkv, hd, dt=dt)
+        keep, k2, v2, w2, lens = eng.evict_cache(c, c, torch.empty((2, hkv, 0), device=DEV), 3,
+                                                 dst_rows=6)
+        assert bool((keep == -1).all()) and not k2.any() and not v2.any() and not w2.any()
+        assert k2.shape == (2, 6, hkv, hd) and lens.tolist() == [0, 0]
+    # new tokens whose keys are kept nowhere, and no tokens
+    tab, g = rope(8, hd), randn(6, hd, dt=dt)
+    x = [randn(7 + i, 3, h * hd, dt=dt) for i, h in enumerate((hq, hkv, hkv))]
+    want = eng.qk_norm_rope(*x, ints([0, 1, 2]), g, g, tab)[0]
+    got, kc, vc = eng.qk_norm_rope(*x, ints([0, 1, 2]), g, g, tab, none, none, ints([-1, 0, 7]))
+    assert torch.equal(got, want) and kc.shape == vc.shape == (0, hkv, hd)
+    got = eng.qk_norm_rope(*(t[:0] for t in x), ints([]), g, g, tab)
+    assert [t.shape[0] for t in got] == [0, 0, 0]
