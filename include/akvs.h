@@ -426,9 +426,9 @@ akvs_status akvs_decode_step_noalloc(const int32_t *token, int32_t n_past, const
  * distinct), NULL: row r, n_kv_rows >= n_rows then. q_out: [n_rows][Hq][hd]; k_out, v_out:
  * [n_kv_rows][Hkv][hd]; rows that no token names stay as they were. q_out may be q where
  * ldq = Hq * hd (k_out k and v_out v likewise, without kv_rows); outputs overlap nothing else.
- * v and v_out may both be NULL, k_out and v_out where n_kv_rows is 0. Errors: EINVAL (negative sizes, null or misaligned pointers, strides
- * shorter than a row or not of 16 bytes, n_kv_rows < n_rows without kv_rows, overlaps),
- * ESHAPE (too large), EHIP. */
+ * v and v_out may both be NULL, k_out and v_out where n_kv_rows is 0. Errors: EINVAL (negative
+ * sizes, null or misaligned pointers, strides shorter than a row or not of 16 bytes,
+ * n_kv_rows < n_rows without kv_rows, overlaps), ESHAPE (too large), EHIP. */
 akvs_status akvs_qk_norm_rope(const void *q, int64_t ldq, const void *k, int64_t ldk,
                               const void *v, int64_t ldv, int32_t n_rows,
                               const int32_t *positions, const void *q_norm, const void *k_norm,

@@ -5,6 +5,7 @@ Nothing here computes any part of the method; every step runs in the library.
 """
 from __future__ import annotations
 
+import operator
 from typing import Optional, Sequence
 
 import torch
@@ -154,7 +155,8 @@ class Engine:
         return q_out, k_cache, v_cache
 
     def _shared(self, q, k_prefix, k_own, own_len, row_start, rows_max):
-        """The batch that these tensors describe."""
+        """The batch that these tensors describe. A row_start that is no tensor is checked, gives
+        rows_max and is copied to the device."""
         sh, n = self.shape, int(q.shape[0])
         self._need("q", q, (n, sh.n_q_heads, sh.head_dim))
         self._need("k_prefix", k_prefix, (None, sh.n_kv_heads, sh.head_dim))
@@ -162,6 +164,15 @@ class Engine:
         if k_own is not None:
             self._need("k_own", k_own, (None, None, sh.n_kv_heads, sh.head_dim))
             cap = int(k_own.shape[1])
+        if row_start is not None and not torch.is_tensor(row_start):
+            at = [operator.index(x) for x in row_start]
+            rows = [b - a for a, b in zip(at, at[1:])]
+            if not rows or at[0] != 0 or min(rows) < 0 or at[-1] > n:
+                raise ValueError(f"row_start: need ascending rows from 0 to at most {n}")
+            if rows_max is not None and max(rows) > rows_max:
+                raise ValueError(f"row_start holds a request of {max(rows)} rows, rows_max is {rows_max}")
+            rows_max = max(rows)
+            row_start = torch.tensor(at, dtype=torch.int32, device=q.device)
         if row_start is not None:
             self._need("row_start", row_start, (None,), torch.int32)
             B = int(row_start.numel()) - 1
@@ -186,8 +197,11 @@ class Engine:
                          row_start=None, rows_max=None, out=None, lse=None):
         """Attention of a batch's rows q [n][Hq][hd] over a shared prefix [P][Hkv][hd] (one layer)
         and each request's own keys [B][rows][Hkv][hd], the first own_len (int32 [B]) of them,
-        which end with the rows' own. row_start (int32 [B + 1]): the requests' rows (None: equally
-        many each); rows_max: the most of one request (None: all). Returns (out, lse)."""
+        which end with the rows' own. row_start (B + 1 of them): the requests' rows (None: equally
+        many each), a sequence of ints, or (as under capture) an int32 tensor, then with rows_max,
+        the most of one request: without it each request is planned for all rows (768 rows of 256
+        requests over 2000 keys of 28/4 heads 107 us, 55 with it), and many requests of many rows
+        are refused. Returns (out, lse)."""
         c = self._shared(q, k_prefix, k_own, own_len, row_start, rows_max)
         self._need("v_prefix", v_prefix, tuple(k_prefix.shape))
         if (k_own is None) != (v_own is None):
@@ -208,7 +222,7 @@ class Engine:
                           rows_max=None, w_prefix=None, w_own=None):
         """Adds the attention weights that the rows of a shared_attention call gave its keys to
         w_prefix [Hkv][P] and (with k_own) w_own [B][Hkv][rows], fp32, made from 0 where they are
-        None. Returns (w_prefix, w_own)."""
+        None; row_start and rows_max as there. Returns (w_prefix, w_own)."""
         c = self._shared(q, k_prefix, k_own, own_len, row_start, rows_max)
         self._need("lse", lse, tuple(q.shape[:2]), torch.float32)
         hkv = self.shape.n_kv_heads

@@ -1135,3 +1135,21 @@ def test_engine_over_empty_tensors(hq, hkv, hd, dt):
     assert torch.equal(got, want) and kc.shape == vc.shape == (0, hkv, hd)
     got = eng.qk_norm_rope(*(t[:0] for t in x), ints([]), g, g, tab)
     assert [t.shape[0] for t in got] == [0, 0, 0]
+
+
+@pytest.mark.parametrize("hq,hkv,hd,dt", [(28, 4, 128, BF), (4, 2, 64, F32)])
+def test_engine_rows_from_the_host(hq, hkv, hd, dt):
+    """Row starts as a list: the result of the same tensor with its longest request, and of the
+    definition."""
+    from paper_2607_21604_amd.runtime import Engine
+    eng = Engine(_Shape(hq, hkv, hd, dt), {"layers": [{k: torch.zeros(8, device=DEV) for k in (
+        "attn_norm", "w_qkv", "w_o", "mlp_norm", "w_gate_up", "w_down")}]}, DEV)
+    b = Batch(hq, hkv, hd, dt, 700, [2, 0, 1, 7], [5, 3, 1, 20], own_rows=24, seed=441, spare=2)
+    b.attend()
+    b.check()
+    ln, st = ints(b.own_len), [int(x) for x in b.start]
+    got = eng.shared_attention(b.q, b.kp, b.vp, b.ko, b.vo, ln, st, out=b.out.clone(), lse=b.lse.clone())
+    assert torch.equal(got[0], b.out) and torch.equal(got[1], b.lse)
+    got = eng.attention_weights(b.q, b.lse, b.kp, b.ko, ln, st)
+    want = eng.attention_weights(b.q, b.lse, b.kp, b.ko, ln, ints(st), 7)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])

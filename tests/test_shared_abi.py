@@ -393,3 +393,29 @@ def test_weights_of_too_long_a_prefix(lib):
         assert akvs.akvs_shared_workspace_size(m, c) > 0
         assert lib.akvs_attention_weights(A, A, ctypes.byref(c), A, A, ctypes.byref(m), A, A, A, A, A,
                                           1 << 40, None) == akvs.AKVS_ESHAPE
+
+
+def test_engine_takes_rows_from_the_host(engine):
+    """row_start as a sequence: checked, copied, and planned for its longest request, so that a
+    batch of many requests fits that does not with all rows for each."""
+    kp, B = bf(8000, 2, 64), 4096
+    q, ko, ln = bf(3 * B, 6, 64), bf(B, 4, 2, 64), torch.ones(B, dtype=torch.int32)
+    st = [3 * i for i in range(B + 1)]
+    c = engine._shared(q, kp, ko, ln, st, None)
+    t = engine._shared(q, kp, ko, ln, i32(*st), 3)
+    assert c.rows_max == t.rows_max == 3 and c.n_req == t.n_req == B and c.n_rows == t.n_rows
+    assert c._keep[0].tolist() == st and c._keep[0].dtype == torch.int32
+    need = akvs.akvs_shared_workspace_size(engine.m, c)
+    assert need == akvs.akvs_shared_workspace_size(engine.m, t) > 0
+    every = engine._shared(q, kp, ko, ln, i32(*st), None)
+    assert every.rows_max == 3 * B and akvs.akvs_shared_workspace_size(engine.m, every) == 0
+    q = bf(9, 6, 64)
+    assert engine._shared(q, kp, None, None, (0, 0, 5, 5, 8), None).rows_max == 5
+    assert engine._shared(q, kp, None, None, torch.tensor([0, 2, 9]).numpy(), 8).rows_max == 7
+    assert engine._shared(q[:0], kp, None, None, [0, 0], None).rows_max == 1
+    for bad, most in (([0, 5, 4], None), ([1, 5], None), ([0, 10], None), ([0], None), ([], None),
+                      ([0, 4, 9], 4), ([0, -1, 9], None)):
+        with pytest.raises(ValueError, match="row_start"):
+            engine._shared(q, kp, None, None, bad, most)
+    with pytest.raises(TypeError):
+        engine._shared(q, kp, None, None, [0, 4.5], None)
