@@ -258,8 +258,11 @@ class Engine:
         c = akvs.evict_cfg(S, n, n_keep, n_first, n_recent, int(k.shape[1]), dst_rows, lens)
         rows, dev = max(dst_rows, n_keep), self.device
         keep = torch.empty((S, sh.n_kv_heads, n_keep), dtype=torch.int32, device=dev)
-        k_out = torch.zeros((S, rows, sh.n_kv_heads, sh.head_dim), dtype=self.dtype, device=dev)
-        v_out = torch.zeros_like(k_out)
+        k_out = torch.empty((S, rows, sh.n_kv_heads, sh.head_dim), dtype=self.dtype, device=dev)
+        v_out = torch.empty_like(k_out)
+        filled = min(n, n_keep) if lens is None else 0  # (rows that every sequence fills)
+        k_out[:, filled:].zero_()
+        v_out[:, filled:].zero_()
         w_out = torch.empty((S, sh.n_kv_heads, rows), dtype=torch.float32, device=dev)
         lens_out = torch.empty(S, dtype=torch.int32, device=dev)
         ws = self._scratch(akvs.akvs_evict_workspace_size(self.m, c))

@@ -1153,3 +1153,28 @@ def test_engine_rows_from_the_host(hq, hkv, hd, dt):
     got = eng.attention_weights(b.q, b.lse, b.kp, b.ko, ln, st)
     want = eng.attention_weights(b.q, b.lse, b.kp, b.ko, ln, ints(st), 7)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("keys,keep,dst,lens", [(60, 20, 0, None), (60, 20, 33, None), (20, 20, 20, None),
+                                                (12, 20, 25, None), (60, 20, 0, [60, 7]),
+                                                (60, 20, 30, [0, 21])])
+def test_engine_evicts_into_cleared_rows(keys, keep, dst, lens):
+    """New caches hold the kept keys and zeros behind them, also where their memory held other
+    numbers before."""
+    from paper_2607_21604_amd.runtime import Engine
+    eng = Engine(_Shape(4, 2, 64, BF), {"layers": [{k: torch.zeros(8, device=DEV) for k in (
+        "attn_norm", "w_qkv", "w_o", "mlp_norm", "w_gate_up", "w_down")}]}, DEV)
+    k, v = randn(1, 2, keys, 2, 64, dt=BF), randn(2, 2, keys, 2, 64, dt=BF)
+    w = randn(3, 2, 2, keys).square()
+    for _ in range(3):
+        junk = [torch.full((2, max(keep, dst), 2, 64), math.nan, dtype=BF, device=DEV) for _ in range(6)]
+        del junk  # (the pool hands this memory out again)
+        idx, k2, v2, w2, n = eng.evict_cache(k, v, w, keep, 2, 3, None if lens is None else ints(lens), dst)
+        for s in range(2):
+            own = keys if lens is None else lens[s]
+            assert int(n[s]) == min(own, keep)
+            for h in range(2):
+                at = ref.evict(w[s, h, :own].tolist(), own, keep, 2, 3)
+                assert torch.equal(k2[s, :len(at), h], k[s, at, h])
+                assert torch.equal(v2[s, :len(at), h], v[s, at, h])
+            assert not k2[s, min(own, keep):].any() and not v2[s, min(own, keep):].any()
