@@ -443,10 +443,10 @@ size_t akvs_shared_workspace_size(const akvs_model_cfg *m, const akvs_shared_cfg
 /* Attention of a batch's rows over the shared prefix and each request's own keys, scores
  * q.k/sqrt(hd), softmax over both together. Scores, maxima, sums and lse are fp32. bf16 models
  * round the probabilities p to bf16 for their product with the values, and, where the keys are
- * split, a split's outputs to fp16 scaled by a power of two per row and head: out is off by at
- * most (2^-8 + 2^-11) sum p |v| more than its own rounding; fp32 models round nothing else. The
- * prefix is read once for 128 (row, query head) pairs of a KV head, whichever requests they are
- * of (fp32 models: 16).
+ * split, a split's outputs to fp16 scaled by a power of two per row and head: together up to
+ * about (2^-8 + 2^-11) sum p |v| beside the rounding of out itself. fp32 models round neither.
+ * The prefix is read once for 128 (row, query head) pairs of a KV head (fp32 models: 16),
+ * whichever requests they are of; contexts of a few hundred keys once for each request.
  * q: [n_rows][Hq][hd]; k_prefix, v_prefix: [P][Hkv][hd] (e.g. one layer of a reuse prefill's
  * k_corr / v_corr); k_own, v_own: [B][own_rows][Hkv][hd]; out: [n_rows][Hq][hd]; all model
  * dtype. lse (device [n_rows][Hq] fp32, may be NULL): natural log of the row's sum of
