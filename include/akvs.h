@@ -450,8 +450,9 @@ size_t akvs_shared_workspace_size(const akvs_model_cfg *m, const akvs_shared_cfg
  * q: [n_rows][Hq][hd]; k_prefix, v_prefix: [P][Hkv][hd] (e.g. one layer of a reuse prefill's
  * k_corr / v_corr); k_own, v_own: [B][own_rows][Hkv][hd]; out: [n_rows][Hq][hd]; all model
  * dtype. lse (device [n_rows][Hq] fp32, may be NULL): natural log of the row's sum of
- * exp(score). A row that sees no key gets out 0 and lse -inf. Keys past a row's last one are
- * never part of its result, whatever they hold; rows from row_start[B] on stay as they were.
+ * exp(score). A row that sees no key, or whose scores are all -inf, gets out 0 and lse -inf. Keys
+ * past a row's last one are never part of its result, whatever they hold; rows from
+ * row_start[B] on stay as they were.
  * out may be q; out, lse and ws overlap nothing else.
  * Errors: EINVAL (sizes, pointers, overlaps) / ESHAPE / ENOSPACE, EHIP. */
 akvs_status akvs_shared_attention(const void *q, const akvs_shared_cfg *c, const void *k_prefix,

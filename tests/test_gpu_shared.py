@@ -1178,3 +1178,29 @@ def test_engine_evicts_into_cleared_rows(keys, keep, dst, lens):
                 assert torch.equal(k2[s, :len(at), h], k[s, at, h])
                 assert torch.equal(v2[s, :len(at), h], v[s, at, h])
             assert not k2[s, min(own, keep):].any() and not v2[s, min(own, keep):].any()
+
+
+@pytest.mark.parametrize("hq,hkv,hd,dt", [(6, 2, 128, BF), (3, 3, 64, BF), (4, 2, 64, F32)])
+@pytest.mark.parametrize("prefix", [1, 100, 448, 5000, 16384])
+def test_scores_of_minus_infinity(hq, hkv, hd, dt, prefix):
+    """Keys whose scores are -inf weigh nothing: a row that sees others is as without them, one that
+    sees none but them is as one without a key, and gives no weight."""
+    b = Batch(hq, hkv, hd, dt, prefix, [2, 1, 1], [40, 1, 0], own_rows=41, seed=451)
+    b.q[..., 0] = b.q[..., 0].abs() + 1
+    b.kp[..., 0] = -math.inf
+    b.ko[1, 0, :, 0] = -math.inf
+    b.attend()
+    assert not b.out[2:].any() and bool((b.lse[2:] == -math.inf).all())
+    c = Batch(hq, hkv, hd, dt, 0, [2, 1, 1], [40, 1, 0], own_rows=41, seed=451)
+    c.q, c.ko, c.vo = b.q, b.ko, b.vo
+    c.attend()
+    c.out[2:], c.lse[2:] = 0.0, -math.inf
+    c.kp, c.vp, c.own_len = b.kp[:0], b.vp[:0], [40, 0, 0]
+    c.check()
+    c.out, c.lse = b.out, b.lse
+    c.P, c.cap = prefix, 41  # (as many keys in the bound)
+    c.check()
+    wp, wo = torch.empty((hkv, prefix), device=DEV), torch.empty((3, hkv, 41), device=DEV)
+    akvs.akvs_attention_weights(b.q, b.lse, b.cfg(), b.kp, b.ko, b.m, None, wp, None, wo, b.ws(b.cfg()))
+    assert not wp.any() and not wo[1:].any()
+    assert abs(float(wo[0].double().sum()) - 2 * hq) < 1e-4 * 2 * hq
