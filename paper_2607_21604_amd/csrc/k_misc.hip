@@ -316,21 +316,21 @@ hipError_t launch_mfma_busy_loop(int n_blocks, int iters, float *out, hipStream_
 
 // Norms and rotation of query and key heads. A head is one task of hd / 16 neighbouring lanes,
 // each with 8 elements of its lower half and their rotary partners of the upper half, so the
-// pair turns in a lane and only the sum of squares crosses lanes. A value head is a copy. The
-// squares are added in fp32, their root and the rotation are fp64: a stored bf16 query that
-// falls to the other side of a rounding moves every score of its row by 2^-8 of an element.
-// Bound by HBM: 16128 tokens of 40 + 2 x 8 heads of 128 in 91 us, 5.2 TB/s (87 all in fp32, 104
-// all in fp64).
+// pair turns in a lane and only the sum of squares crosses lanes. A value head is a copy. Squares,
+// root and rotation are fp64, so that a stored bf16 value is the definition's: one that falls to
+// the other side of a rounding moves every score of its row by 2^-8 of an element (with squares in
+// fp32 one of 280 000 values did). Bound by HBM: 16128 tokens of 40 + 2 x 8 heads of 128 in 91 us,
+// 5.2 TB/s, where bf16 models' registers are held to eight waves a SIMD (95 with seven); fp32
+// ones would spill (16000 tokens of 28 + 2 x 4 heads 110 us, 269 held to eight).
 template <typename TS, int LPH>
-__global__ __launch_bounds__(256) void k_qk_norm_rope(QkNorm a) {
+__global__ __launch_bounds__(256, sizeof(TS) == 2 ? 8 : 1) void k_qk_norm_rope(QkNorm a) {
   constexpr int half = LPH * 8, hd = 2 * half;
-  const int heads = a.hq + a.hkv * (a.v ? 2 : 1);
-  const long long gid = (long long)blockIdx.x * 256 + threadIdx.x;
-  const long long task = gid / LPH;
-  const int e0 = (int)(gid % LPH) * 8;
+  const unsigned heads = a.hq + a.hkv * (a.v ? 2 : 1);
+  const unsigned task = (blockIdx.x * 256 + threadIdx.x) / LPH;  // (32 bits: fewer than 2^31 threads)
+  const int e0 = threadIdx.x % LPH * 8;
   const long long r = task / heads;
   if (r >= a.n_rows) return;  // (whole groups of LPH lanes)
-  int h = (int)(task - r * heads);
+  int h = (int)(task - (unsigned)r * heads);
   const TS *src;
   TS *dst;
   const TS *gain = nullptr;
@@ -363,22 +363,21 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope(QkNorm a) {
     if (gain) {
       load8(gain + e0, gl);
       load8(gain + e0 + half, gh);
-      float ss = 0.f;
+      double ss = 0.0, sh = 0.0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) ss = fmaf(lo[i], lo[i], fmaf(hi[i], hi[i], ss));
+      for (int i = 0; i < 8; ++i) {
+        ss = fma((double)lo[i], (double)lo[i], ss);
+        sh = fma((double)hi[i], (double)hi[i], sh);
+      }
+      ss += sh;
 #pragma unroll
       for (int o = 1; o < LPH; o <<= 1) ss += __shfl_xor(ss, o, 64);
-      const float v = fmaf(ss, 1.0f / hd, a.eps);
-      rs = rsqrtf(v);
-      rs += 0.5 * rs * (1.0 - (double)v * rs * rs);  // (one Newton step)
-      if (!(v > 1e-30f && v < 1e38f)) {  // squares that leave fp32's range (a head's lanes agree)
-        double wide = 0.0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          wide = fma((double)lo[i], (double)lo[i], fma((double)hi[i], (double)hi[i], wide));
-#pragma unroll
-        for (int o = 1; o < LPH; o <<= 1) wide += __shfl_xor(wide, o, 64);
-        rs = 1.0 / sqrt(wide * (1.0 / hd) + (double)a.eps);
+      const double v = ss * (1.0 / hd) + (double)a.eps;
+      if (v > 1e-30 && v < 1e38) {
+        rs = rsqrtf((float)v);
+        rs += 0.5 * rs * (1.0 - v * rs * rs);  // (one Newton step)
+      } else {
+        rs = 1.0 / sqrt(v);
       }
     }
     // The products with the gains are exact: fp64 ones in fp32 models; fp32 ones in bf16 models, of a

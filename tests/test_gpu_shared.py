@@ -1204,3 +1204,25 @@ def test_scores_of_minus_infinity(hq, hkv, hd, dt, prefix):
     akvs.akvs_attention_weights(b.q, b.lse, b.cfg(), b.kp, b.ko, b.m, None, wp, None, wo, b.ws(b.cfg()))
     assert not wp.any() and not wo[1:].any()
     assert abs(float(wo[0].double().sum()) - 2 * hq) < 1e-4 * 2 * hq
+
+
+# ---- stored values on the definition's side of a rounding ------------------------------------------------
+
+@pytest.mark.parametrize("hq,hkv,hd,std", [(28, 4, 128, 1.7), (24, 8, 128, 0.02), (6, 2, 64, 300.0)])
+def test_stored_queries_are_the_definitions(hq, hkv, hd, std):
+    """bf16 queries and keys are the 64-bit results rounded (through fp32, as a conversion from 64 bits
+    goes), each of some millions: the two sides' 64-bit arithmetic differs by some 2^-45 (the
+    root's Newton step), and a value is that near a rounding's border with a chance of 2^-36."""
+    m, tab, n = model(hq, hkv, hd, BF), rope(3000, hd), 1500 if hd == 128 else 6000
+    q, k = (randn(461 + i, n, h, hd, dt=BF, std=std) for i, h in enumerate((hq, hkv)))
+    gq, gk = (1 + randn(463, hd, std=0.2)).to(BF), randn(465, hd, dt=BF)
+    pos = np.random.default_rng(5).integers(0, 3000, n)
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    akvs.akvs_qk_norm_rope(q, k, None, n, ints(pos), gq, gk, m, tab, 3000, None, n, qo, ko, None)
+    cs = tab[torch.from_numpy(pos).to(DEV)].double()[:, None]
+    for got, x, g in ((qo, q, gq), (ko, k, gk)):
+        x = x.double()
+        x = x / torch.sqrt((x * x).mean(-1, keepdim=True) + float(np.float32(m.rms_eps))) * g.double()
+        lo, hi = x.chunk(2, dim=-1)
+        want = torch.cat((lo * cs[..., 0] - hi * cs[..., 1], hi * cs[..., 0] + lo * cs[..., 1]), -1)
+        assert torch.equal(got, want.float().to(BF)), int((got != want.float().to(BF)).sum())
