@@ -1226,3 +1226,56 @@ def test_stored_queries_are_the_definitions(hq, hkv, hd, std):
         lo, hi = x.chunk(2, dim=-1)
         want = torch.cat((lo * cs[..., 0] - hi * cs[..., 1], hi * cs[..., 0] + lo * cs[..., 1]), -1)
         assert torch.equal(got, want.float().to(BF)), int((got != want.float().to(BF)).sum())
+
+
+@pytest.mark.parametrize("lens", [None, [60, 0, 7]])
+def test_engine_evicts_from_a_graph(lens):
+    """The engine's eviction captured and replayed over new weights, between eager calls and with its
+    outputs spoilt in between: the eager results, zeros behind the kept keys among them."""
+    from paper_2607_21604_amd.runtime import Engine
+    eng = Engine(_Shape(4, 2, 64, BF), {"layers": [{k: torch.zeros(8, device=DEV) for k in (
+        "attn_norm", "w_qkv", "w_o", "mlp_norm", "w_gate_up", "w_down")}]}, DEV)
+    k, v = randn(1, 3, 60, 2, 64, dt=BF), randn(2, 3, 60, 2, 64, dt=BF)
+    w = randn(3, 3, 2, 60).square()
+    ln = None if lens is None else ints(lens)
+
+    def run():
+        return eng.evict_cache(k, v, w, 20, 2, 3, ln, 27)
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    for seed in (4, 5, 6):
+        w.copy_(randn(seed, *w.shape).square())
+        want = [t.clone() for t in run()]
+        for t in got:
+            t.fill_(77)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), seed
+
+
+@pytest.mark.parametrize("prefix", [100, 5000])
+def test_attention_over_its_queries_from_a_graph(prefix):
+    """In place and captured: replayed over fresh queries it gives what separate buffers give."""
+    b = Batch(28, 4, 128, BF, prefix, [1] * 4, [9, 1, 30, 40], seed=471)
+    c, fresh = b.cfg(), [randn(472 + i, *b.q.shape, dt=BF) for i in range(3)]
+    ws = b.ws(c)
+    x = b.q.clone()
+
+    def run(q, out, lse):
+        akvs.akvs_shared_attention(q, c, b.kp, b.vp, b.ko, b.vo, b.m, out, lse, ws)
+    lse = torch.empty_like(b.lse)
+    run(x, x, lse)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(x, x, lse)
+    for q in fresh:
+        run(q, b.out, b.lse)
+        x.copy_(q)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(x, b.out) and torch.equal(lse, b.lse)
