@@ -47,6 +47,12 @@
  *  - corrected / fresh caches [L][T][Hkv][hd], indexed by position.
  *  - rotary table [n_pos][hd/2][2] fp32 (cos, sin) of p * theta^(-2k/hd), rotate-half
  *    pairing of dimension k with k + hd/2.
+ *  - pages of a 4-bit cache (one layer): codes [n_pages][Hkv][page_rows][hd/2] uint8 and meta
+ *    [n_pages][Hkv][page_rows][hd/64][2] fp16 (scale, zero), the codes as in a quantised cache:
+ *    a head's rows of a page are contiguous. Key j of a sequence is row j % page_rows of the
+ *    page that entry j / page_rows of the sequence's table names.
+ *  - 4-bit weights [out][in]: codes [out][in/2] uint8, meta [out][in/64][2] fp16 (what
+ *    akvs_quantize_cache makes of rows of `in` elements).
  */
 #ifndef AKVS_H
 #define AKVS_H
@@ -154,6 +160,49 @@ typedef struct akvs_evict_cfg {
                                 <= n_keep)                                                   */
   const int32_t *lens;  /* device [S]: keys of each sequence, 0 .. n_keys (NULL: n_keys)     */
 } akvs_evict_cfg;
+
+/* One layer's cache of 4-bit codes in pages (layout above). Layers of a model that follow each
+ * other in memory are n_pages pages apart. */
+typedef struct akvs_pages {
+  uint8_t *k, *v;         /* codes                                                           */
+  void *k_meta, *v_meta;  /* (scale, zero) of every 64 elements                              */
+  int32_t n_pages;        /* >= 0 (0: none, pointers may be NULL)                            */
+  int32_t page_rows;      /* keys of a page: 16, 32, 64, 128 or 256                          */
+} akvs_pages;
+
+/* The pages of S sequences, of all layers alike. A page may be named by several sequences: ref
+ * counts them; a page with ref <= 0 is free. Entries that a sequence's length does not reach are
+ * never read. */
+typedef struct akvs_page_table {
+  int32_t n_seq, max_pages;   /* S >= 1; entries of a sequence, >= 1                         */
+  int32_t n_pages, page_rows; /* as in akvs_pages                                            */
+  int32_t *table;             /* device [S][max_pages]                                       */
+  int32_t *len;               /* device [S]: keys of each sequence                           */
+  int32_t *ref;               /* device [n_pages]                                            */
+} akvs_page_table;
+
+/* A batch over sequences in pages (akvs_store_pages, akvs_load_pages, akvs_paged_attention). Rows
+ * are packed request by request as in akvs_shared_cfg; a request's rows are the last keys of its
+ * sequence: row i of its n is key len - n + i, and sees keys 0 .. len - n + i. */
+typedef struct akvs_paged_cfg {
+  int32_t n_req;        /* B >= 1                                                            */
+  int32_t n_rows;       /* rows that q, out, .. hold, >= 0                                   */
+  int32_t rows_max;     /* the most rows of one request, >= 1                                */
+  int32_t n_seq;        /* sequences of `len` and `table`, >= 1                              */
+  int32_t max_pages;    /* entries of a sequence in `table`, >= 1                            */
+  int32_t max_len;      /* no sequence of the batch has more keys (longer ones count as this
+                           long), 0 .. max_pages * page_rows: what calls are planned for     */
+  const int32_t *row_start; /* device [B + 1] as in akvs_shared_cfg, or NULL                 */
+  const int32_t *seq;   /* device [B]: the sequence of each request; NULL: b (B <= n_seq)    */
+  const int32_t *len;   /* device [n_seq]: keys, the rows' own among them                    */
+  const int32_t *table; /* device [n_seq][max_pages]                                         */
+} akvs_paged_cfg;
+
+/* What akvs_w4_product makes of W x. */
+enum {
+  AKVS_W4_STORE = 0,  /* y = W x (+ resid)                                                   */
+  AKVS_W4_SWIGLU = 1  /* y = silu(g) u, g the first half of W x, u the second                */
+};
 
 /* ---- library information ---------------------------------------------------- */
 int32_t akvs_version(void);
@@ -495,6 +544,105 @@ akvs_status akvs_evict_cache(const void *k, const void *v, const float *weights,
                              const akvs_evict_cfg *c, const akvs_model_cfg *m, int32_t *keep,
                              void *k_out, void *v_out, float *weights_out, int32_t *lens_out,
                              void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* ---- decoding from four bits ----------------------------------------------------------------
+ * Caches of many sequences in pages of 4-bit codes (the format of akvs_quantize_cache with bits
+ * 4), which sequences may share, and products with weights in the same format. bf16 models only
+ * (AKVS_EDTYPE). A sequence index, length or page outside its range is as if the sequence were
+ * empty, cut or the page missing: nothing is read or written for it. */
+
+/* Quantises a batch's new keys and values into their pages, with the codes and meta that
+ * akvs_quantize_cache gives them (values past fp16's range are outside the format). k, v:
+ * [n_rows][Hkv][hd] model dtype, row r at r * ldk / ldv elements (each ld * 2 bytes a multiple of
+ * 16); pages that rows go to are named by one sequence of the batch only. Rows past row_start[B]
+ * and rows that are no key of their sequence (more rows than keys) go nowhere. Errors: EINVAL
+ * (sizes, pointers, strides, overlaps) / EDTYPE / EUNSUPPORTED (page_rows) / ESHAPE, EHIP. */
+akvs_status akvs_store_pages(const void *k, int64_t ldk, const void *v, int64_t ldv,
+                             const akvs_paged_cfg *c, const akvs_pages *p,
+                             const akvs_model_cfg *m, hipStream_t stream);
+
+/* The other way: what the pages hold for a batch's rows (any keys at the end of each sequence, all
+ * of them with n = len). k_out, v_out: [n_rows][Hkv][hd] of dtype (F32: scale * code + zero
+ * exactly rounded; BF16), either may be NULL. Rows that are no key of their sequence, or whose page
+ * is missing, are 0; rows past row_start[B] stay as they were. Errors as above. */
+akvs_status akvs_load_pages(const akvs_paged_cfg *c, const akvs_pages *p, const akvs_model_cfg *m,
+                            void *k_out, void *v_out, int32_t dtype, hipStream_t stream);
+
+/* Workspace bytes of akvs_paged_attention over this batch; 0 for an invalid one, or where it
+ * needs none. */
+size_t akvs_paged_workspace_size(const akvs_model_cfg *m, const akvs_paged_cfg *c);
+
+/* Attention of a batch's rows over their sequences' pages, scores q.k/sqrt(hd), softmax. q, out:
+ * [n_rows][Hq][hd] model dtype; lse (device [n_rows][Hq] fp32, may be NULL): natural log of the
+ * row's sum of exp(score). A row that sees no key, or whose scores are all -inf, gets out 0 and
+ * lse -inf. Keys past a row's last one, and what their places in a page hold, are never part of its
+ * result; rows past row_start[B] stay as they were. A missing page's keys and values count as 0
+ * (with n_pages = 0 there are no keys).
+ * out may be q; out, lse and ws overlap nothing else. Errors as above, ENOSPACE. */
+akvs_status akvs_paged_attention(const void *q, const akvs_paged_cfg *c, const akvs_pages *p,
+                                 const akvs_model_cfg *m, void *out, float *lse, void *ws,
+                                 size_t ws_bytes, hipStream_t stream);
+
+/* Sequences dst[i] (device [n], empty ones) become what src[i] are: they share all their pages,
+ * the last one too. A pair is left out where an index is out of range, dst[i] is not empty, is
+ * named as dst by an earlier pair, or is a source of the call. Errors: EINVAL / ESHAPE /
+ * EUNSUPPORTED (page_rows), EHIP. */
+akvs_status akvs_fork_pages(const akvs_page_table *t, int32_t n, const int32_t *src,
+                            const int32_t *dst, hipStream_t stream);
+
+/* Sequences seq[i] (device [n]; one named twice is one) end: their pages' refs are lowered, their
+ * entries are -1 and their lengths 0. Errors as above. */
+akvs_status akvs_free_pages(const akvs_page_table *t, int32_t n, const int32_t *seq,
+                            hipStream_t stream);
+
+/* Workspace bytes of akvs_grow_pages over n sequences and of akvs_compact_pages (n = 0). 0 if
+ * invalid. */
+size_t akvs_pages_workspace_size(const akvs_page_table *t, int32_t n);
+
+/* Room for add[i] >= 0 more keys in sequences seq[i] (device [n] both), whose lengths grow by
+ * that: pages of the lowest free numbers, sequence by sequence in order. A last page that has room
+ * and is shared (ref > 1 before the call) is replaced by a page of the sequence's own, its first
+ * new one: that page's contents are to be copied, as listed in move_src / move_dst (device [n]
+ * int32 each, in order, -1 past the last; akvs_move_pages). served (device [n]): 1, or 0 for a
+ * sequence that stays as it was: an index out of range or named earlier, add[i] < 0, more than
+ * max_pages pages, or no free pages left (one that needs any follows one that could not be served).
+ * counts (device [2]): copies listed, pages taken. Outputs and ws overlap nothing else. Errors as
+ * above, ENOSPACE. */
+akvs_status akvs_grow_pages(const akvs_page_table *t, int32_t n, const int32_t *seq,
+                            const int32_t *add, int32_t *served, int32_t *move_src,
+                            int32_t *move_dst, int32_t *counts, void *ws, size_t ws_bytes,
+                            hipStream_t stream);
+
+/* The pages in use (ref > 0) move to the lowest numbers: of N in use, those from number N on take
+ * the free numbers below N, in ascending order both. move_src, move_dst (device [n_pages] each, -1
+ * past the last): whose contents go where (akvs_move_pages, before the tables are used again);
+ * table_out, ref_out: the tables afterwards, may be t's own; counts (device [2]): moves, N.
+ * Outputs and ws overlap nothing else. Errors as above. */
+akvs_status akvs_compact_pages(const akvs_page_table *t, int32_t *table_out, int32_t *ref_out,
+                               int32_t *move_src, int32_t *move_dst, int32_t *counts, void *ws,
+                               size_t ws_bytes, hipStream_t stream);
+
+/* Copies pages src[i] to pages dst[i] (device), i < min(*n_moves, max_moves) (n_moves: device,
+ * NULL: max_moves of them), in n_layers layers, p being the first. Indices out of range are left
+ * out; no page is both a source and a target, nor a target twice. Errors as above. */
+akvs_status akvs_move_pages(const akvs_pages *p, int32_t n_layers, const akvs_model_cfg *m,
+                            const int32_t *src, const int32_t *dst, int32_t max_moves,
+                            const int32_t *n_moves, hipStream_t stream);
+
+/* Workspace bytes of akvs_w4_product; 0 if invalid, or where it needs none. */
+size_t akvs_w4_workspace_size(int32_t n_rows, int32_t n_out, int32_t n_in);
+
+/* Products of rows with 4-bit weights: (W x)[r][o] = sum_i x[r][i] (scale code + zero)[o][i],
+ * fp32 sums, weights not rounded. x: [n_rows][n_in] of x_dtype (F32 or BF16), row r at r * ldx
+ * elements (ldx * element size a multiple of 16); w, w_meta: n_out rows of n_in, a multiple of 64;
+ * y: [n_rows][n_out] ([n_out / 2] with AKVS_W4_SWIGLU, n_out even) of y_dtype, row r at r * ldy.
+ * resid (fp32, strides as y, may be y; y_dtype F32 and AKVS_W4_STORE only) or NULL. The weights
+ * are read once for 16 rows. y and ws overlap nothing else. Errors: EINVAL (sizes, strides, mode,
+ * pointers, overlaps) / EDTYPE / ESHAPE / ENOSPACE, EHIP. */
+akvs_status akvs_w4_product(const void *x, int64_t ldx, int32_t x_dtype, int32_t n_rows,
+                            const uint8_t *w, const void *w_meta, int32_t n_out, int32_t n_in,
+                            int32_t mode, const float *resid, void *y, int64_t ldy,
+                            int32_t y_dtype, void *ws, size_t ws_bytes, hipStream_t stream);
 
 /* ---- kernel timing -------------------------------------------------------------------
  * akvs_profile_enable(mask): for every kernel class whose bit (1 << class) is set in

@@ -28,6 +28,7 @@ AKVS_F_FRESH_IF_RECOMPUTED = 4
 AKVS_F_NO_PREFIX_RECOMPUTE = 8
 AKVS_F_GIVEN_PROBES = 16
 AKVS_F_PRE_ROPE_OFFSETS = 32
+AKVS_W4_STORE, AKVS_W4_SWIGLU = range(2)
 AKVS_NOALLOC_SCRATCH_BYTES = 32 << 20  # scratch array of akvs_decode_step_noalloc (akvs.h)
 (AKVS_K_GEMM, AKVS_K_ATTENTION, AKVS_K_CORRECTION, AKVS_K_OFFSET, AKVS_K_DIVERGENCE,
  AKVS_K_SELECT, AKVS_K_NORM, AKVS_K_OTHER, AKVS_K_GEMV) = range(9)
@@ -86,6 +87,26 @@ class EvictCfg(ctypes.Structure):
                 ("src_rows", ctypes.c_int32), ("n_keep", ctypes.c_int32),
                 ("dst_rows", ctypes.c_int32), ("n_first", ctypes.c_int32),
                 ("n_recent", ctypes.c_int32), ("lens", ctypes.c_void_p)]
+
+
+class Pages(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_meta", ctypes.c_void_p),
+                ("v_meta", ctypes.c_void_p), ("n_pages", ctypes.c_int32),
+                ("page_rows", ctypes.c_int32)]
+
+
+class PageTable(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("page_rows", ctypes.c_int32),
+                ("table", ctypes.c_void_p), ("len", ctypes.c_void_p), ("ref", ctypes.c_void_p)]
+
+
+class PagedCfg(ctypes.Structure):
+    _fields_ = [("n_req", ctypes.c_int32), ("n_rows", ctypes.c_int32),
+                ("rows_max", ctypes.c_int32), ("n_seq", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("max_len", ctypes.c_int32),
+                ("row_start", ctypes.c_void_p), ("seq", ctypes.c_void_p),
+                ("len", ctypes.c_void_p), ("table", ctypes.c_void_p)]
 
 
 _P = ctypes.c_void_p
@@ -148,6 +169,26 @@ _SIGS = {
                                                     ctypes.POINTER(EvictCfg)]),
     "akvs_evict_cache": (_I, [_P, _P, _P, ctypes.POINTER(EvictCfg), ctypes.POINTER(ModelCfg), _P,
                               _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
+    "akvs_store_pages": (_I, [_P, _L, _P, _L, ctypes.POINTER(PagedCfg), ctypes.POINTER(Pages),
+                              ctypes.POINTER(ModelCfg), _P]),
+    "akvs_load_pages": (_I, [ctypes.POINTER(PagedCfg), ctypes.POINTER(Pages),
+                             ctypes.POINTER(ModelCfg), _P, _P, _I, _P]),
+    "akvs_paged_workspace_size": (ctypes.c_size_t, [ctypes.POINTER(ModelCfg),
+                                                    ctypes.POINTER(PagedCfg)]),
+    "akvs_paged_attention": (_I, [_P, ctypes.POINTER(PagedCfg), ctypes.POINTER(Pages),
+                                  ctypes.POINTER(ModelCfg), _P, _P, _P, ctypes.c_size_t, _P]),
+    "akvs_fork_pages": (_I, [ctypes.POINTER(PageTable), _I, _P, _P, _P]),
+    "akvs_free_pages": (_I, [ctypes.POINTER(PageTable), _I, _P, _P]),
+    "akvs_pages_workspace_size": (ctypes.c_size_t, [ctypes.POINTER(PageTable), _I]),
+    "akvs_grow_pages": (_I, [ctypes.POINTER(PageTable), _I, _P, _P, _P, _P, _P, _P, _P,
+                             ctypes.c_size_t, _P]),
+    "akvs_compact_pages": (_I, [ctypes.POINTER(PageTable), _P, _P, _P, _P, _P, _P,
+                                ctypes.c_size_t, _P]),
+    "akvs_move_pages": (_I, [ctypes.POINTER(Pages), _I, ctypes.POINTER(ModelCfg), _P, _P, _I, _P,
+                             _P]),
+    "akvs_w4_workspace_size": (ctypes.c_size_t, [_I, _I, _I]),
+    "akvs_w4_product": (_I, [_P, _L, _I, _I, _P, _P, _I, _I, _I, _P, _P, _L, _I, _P,
+                             ctypes.c_size_t, _P]),
     "akvs_profile_enable": (_I, [_I]),
     "akvs_profile_read": (_I, [_I, ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_double)]),
     "akvs_mfma_busy_loop": (_I, [_I, _I, _P, _P]),
@@ -280,6 +321,40 @@ def evict_cfg(n_seq, n_keys, n_keep, n_first=0, n_recent=0, src_rows=0, dst_rows
     c = EvictCfg(int(n_seq), int(n_keys), int(src_rows), int(n_keep), int(dst_rows), int(n_first),
                  int(n_recent), int_ptr(lens, n_seq))
     c._keep = lens
+    return c
+
+
+def pages(k, v, k_meta, v_meta) -> Pages:
+    """One layer's pages: codes uint8 [n_pages][Hkv][page_rows][hd/2], meta fp16
+    [n_pages][Hkv][page_rows][hd/64][2]; it holds references to the tensors."""
+    for name, x, dt in (("k", k, torch.uint8), ("v", v, torch.uint8),
+                        ("k_meta", k_meta, torch.float16), ("v_meta", v_meta, torch.float16)):
+        if x.dtype != dt or x.shape[:3] != k.shape[:3]:
+            raise ValueError(f"{name}: need {dt} pages of {tuple(k.shape[:3])} rows")
+    p = Pages(ptr(k), ptr(v), ptr(k_meta), ptr(v_meta), int(k.shape[0]), int(k.shape[2]))
+    p._keep = (k, v, k_meta, v_meta)
+    return p
+
+
+def page_table(table, lens, ref, page_rows) -> PageTable:
+    """The pages of sequences: int32 table [S][max_pages], lens [S], ref [n_pages]; it holds
+    references to the tensors."""
+    if table.dim() != 2:
+        raise ValueError("table: need [sequences][pages]")
+    t = PageTable(int(table.shape[0]), int(table.shape[1]), int(ref.numel()), int(page_rows),
+                  int_ptr(table, 0), int_ptr(lens, table.shape[0]), int_ptr(ref, 0))
+    t._keep = (table, lens, ref)
+    return t
+
+
+def paged_cfg(n_req, n_rows, rows_max, lens, table, max_len, row_start=None, seq=None) -> PagedCfg:
+    """A batch over sequences in pages; it holds references to its device tensors."""
+    if table.dim() != 2:
+        raise ValueError("table: need [sequences][pages]")
+    c = PagedCfg(int(n_req), int(n_rows), int(rows_max), int(table.shape[0]), int(table.shape[1]),
+                 int(max_len), int_ptr(row_start, n_req + 1), int_ptr(seq, n_req),
+                 int_ptr(lens, table.shape[0]), int_ptr(table, 0))
+    c._keep = (row_start, seq, lens, table)
     return c
 
 
@@ -511,6 +586,99 @@ def akvs_evict_cache(k, v, weights, cfg: EvictCfg, m: ModelCfg, keep, k_out, v_o
                                    ctypes.byref(m), ptr(keep), ptr(k_out), ptr(v_out),
                                    ptr(weights_out), ptr(lens_out), ptr(ws), nbytes,
                                    stream_handle(stream)), "akvs_evict_cache")
+
+
+def akvs_store_pages(k, v, cfg: PagedCfg, p: Pages, m: ModelCfg, stream=None):
+    """k, v: rows that may lie apart (views of a packed projection output)."""
+    (pk, ldk), (pv, ldv) = rows_ptr(k), rows_ptr(v)
+    _check(load().akvs_store_pages(pk, ldk, pv, ldv, ctypes.byref(cfg), ctypes.byref(p),
+                                   ctypes.byref(m), stream_handle(stream)), "akvs_store_pages")
+
+
+def akvs_load_pages(cfg: PagedCfg, p: Pages, m: ModelCfg, k_out, v_out, stream=None):
+    _check(load().akvs_load_pages(ctypes.byref(cfg), ctypes.byref(p), ctypes.byref(m), ptr(k_out),
+                                  ptr(v_out), dtype_code(v_out if k_out is None else k_out),
+                                  stream_handle(stream)), "akvs_load_pages")
+
+
+def akvs_paged_workspace_size(m: ModelCfg, cfg: PagedCfg) -> int:
+    return load().akvs_paged_workspace_size(ctypes.byref(m), ctypes.byref(cfg))
+
+
+def akvs_paged_attention(q, cfg: PagedCfg, p: Pages, m: ModelCfg, out, lse=None, ws=None,
+                         stream=None):
+    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check(load().akvs_paged_attention(ptr(q), ctypes.byref(cfg), ctypes.byref(p), ctypes.byref(m),
+                                       ptr(out), ptr(lse), ptr(ws), nbytes, stream_handle(stream)),
+           "akvs_paged_attention")
+
+
+def akvs_fork_pages(t: PageTable, src, dst, stream=None):
+    n = int(dst.numel())
+    _check(load().akvs_fork_pages(ctypes.byref(t), n, int_ptr(src, n), int_ptr(dst, n),
+                                  stream_handle(stream)), "akvs_fork_pages")
+
+
+def akvs_free_pages(t: PageTable, seq, stream=None):
+    n = int(seq.numel())
+    _check(load().akvs_free_pages(ctypes.byref(t), n, int_ptr(seq, n), stream_handle(stream)),
+           "akvs_free_pages")
+
+
+def akvs_pages_workspace_size(t: PageTable, n: int = 0) -> int:
+    return load().akvs_pages_workspace_size(ctypes.byref(t), int(n))
+
+
+def akvs_grow_pages(t: PageTable, seq, add, served, move_src, move_dst, counts, ws, stream=None):
+    n = int(seq.numel())
+    _check(load().akvs_grow_pages(ctypes.byref(t), n, int_ptr(seq, n), int_ptr(add, n),
+                                  int_ptr(served, n), int_ptr(move_src, n), int_ptr(move_dst, n),
+                                  int_ptr(counts, 2), ptr(ws), ws.numel() * ws.element_size(),
+                                  stream_handle(stream)), "akvs_grow_pages")
+
+
+def akvs_compact_pages(t: PageTable, table_out, ref_out, move_src, move_dst, counts, ws,
+                       stream=None):
+    _check(load().akvs_compact_pages(ctypes.byref(t), int_ptr(table_out, t.n_seq * t.max_pages),
+                                     int_ptr(ref_out, t.n_pages), int_ptr(move_src, t.n_pages),
+                                     int_ptr(move_dst, t.n_pages), int_ptr(counts, 2), ptr(ws),
+                                     ws.numel() * ws.element_size(), stream_handle(stream)),
+           "akvs_compact_pages")
+
+
+def akvs_move_pages(p: Pages, n_layers, m: ModelCfg, move_src, move_dst, max_moves, n_moves=None,
+                    stream=None):
+    """n_moves: device int32, its first entry counts (None: max_moves)."""
+    _check(load().akvs_move_pages(ctypes.byref(p), int(n_layers), ctypes.byref(m),
+                                  int_ptr(move_src, max_moves), int_ptr(move_dst, max_moves),
+                                  int(max_moves), int_ptr(n_moves, 1), stream_handle(stream)),
+           "akvs_move_pages")
+
+
+def akvs_w4_workspace_size(n_rows: int, n_out: int, n_in: int) -> int:
+    return load().akvs_w4_workspace_size(int(n_rows), int(n_out), int(n_in))
+
+
+def akvs_w4_product(x, w, w_meta, y, mode: int = AKVS_W4_STORE, resid=None, ws=None, stream=None):
+    """x [n_rows][n_in] and y [n_rows][n_out (/ 2)]: rows that may lie apart; w uint8 [n_out][n_in/2],
+    w_meta fp16 [n_out][n_in/64][2]; resid: as y."""
+    (px, ldx), (py, ldy) = rows_ptr(x), rows_ptr(y)
+    n_out, n_in = int(w.shape[0]), 2 * int(w.shape[1])
+    wide = n_out // 2 if mode == AKVS_W4_SWIGLU else n_out
+    if tuple(x.shape) != (x.shape[0], n_in) or tuple(y.shape) != (x.shape[0], wide):
+        raise ValueError(f"x {tuple(x.shape)} and y {tuple(y.shape)} do not fit weights "
+                         f"[{n_out}][{n_in}]")
+    if (w.dtype, w_meta.dtype) != (torch.uint8, torch.float16) or w_meta.numel() != n_out * n_in // 32:
+        raise ValueError("weights: need uint8 codes and fp16 (scale, zero) of every 64")
+    pr = None
+    if resid is not None:
+        pr, ldr = rows_ptr(resid)
+        if resid.shape != y.shape or ldr != ldy or resid.dtype != torch.float32:
+            raise ValueError("resid: need an fp32 tensor of y's shape and strides")
+    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check(load().akvs_w4_product(px, ldx, dtype_code(x), int(x.shape[0]), ptr(w), ptr(w_meta),
+                                  n_out, n_in, mode, pr, py, ldy, dtype_code(y), ptr(ws), nbytes,
+                                  stream_handle(stream)), "akvs_w4_product")
 
 
 def akvs_profile_enable(class_mask: int):

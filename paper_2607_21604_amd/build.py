@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libakvs.so")
 SOURCES = ["api.hip", "k_misc.hip", "k_reuse.hip", "k_gemm.hip", "k_few.hip", "k_attn.hip", "k_shared.hip",
-           "k_evict.hip", "k_decode.hip"]
+           "k_evict.hip", "k_decode.hip", "k_pages.hip", "k_paged.hip", "k_w4.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 # Packed fp32 instructions are kept out of the generated code on purpose.

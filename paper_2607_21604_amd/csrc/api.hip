@@ -1960,3 +1960,390 @@ akvs_status akvs_evict_cache(const void *k, const void *v, const float *weights,
 }
 
 }  // extern "C"
+
+// ---- decoding from four bits ---------------------------------------------------------------
+
+static akvs_status check_four_bit_model(const akvs_model_cfg *m) {
+  akvs_status st = check_model(m);
+  if (st) return st;
+  REQUIRE(m->dtype == AKVS_BF16, AKVS_EDTYPE, "4-bit pages need a bf16 model");
+  return AKVS_OK;
+}
+
+static akvs_status check_page_rows(int32_t page_rows, int *shift) {
+  for (*shift = 4; *shift <= 8; ++*shift)
+    if (page_rows == 1 << *shift) return AKVS_OK;
+  return fail(AKVS_EUNSUPPORTED, "page_rows %d is not 16, 32, 64, 128 or 256", page_rows);
+}
+
+static akvs_status check_paged(const akvs_model_cfg *m, const akvs_paged_cfg *c, PagedBatch *s) {
+  akvs_status st = check_four_bit_model(m);
+  if (st) return st;
+  REQUIRE(c, AKVS_EINVAL, "paged cfg is NULL");
+  REQUIRE(c->n_req >= 1 && c->n_req <= (1 << 20), AKVS_EINVAL, "n_req %d outside [1, 2^20]",
+          c->n_req);
+  REQUIRE(c->n_rows >= 0 && c->rows_max >= 1 && c->n_seq >= 1 && c->max_pages >= 1 &&
+              c->max_len >= 0,
+          AKVS_EINVAL, "need n_rows, max_len >= 0 and rows_max, n_seq, max_pages >= 1");
+  REQUIRE(c->len && c->table, AKVS_EINVAL, "len or table is NULL");
+  REQUIRE(c->seq || c->n_req <= c->n_seq, AKVS_ESHAPE, "%d requests of %d sequences without seq",
+          c->n_req, c->n_seq);
+  REQUIRE((long long)c->n_seq * c->max_pages < (1LL << 31) && c->max_len < (1 << 28) &&
+              c->n_rows < (1 << 24) && (long long)c->n_rows * m->n_q_heads < (1LL << 24),
+          AKVS_ESHAPE, "batch too large");
+  REQUIRE(c->row_start || c->n_rows == 0 || (long long)c->n_req * c->rows_max == c->n_rows,
+          AKVS_ESHAPE, "without row_start every request has rows_max rows: n_rows %d is not %d * %d",
+          c->n_rows, c->n_req, c->rows_max);
+  *s = {c->n_req,     c->n_rows, std::min(c->rows_max, std::max(c->n_rows, 1)),
+        c->n_seq,     c->max_pages, c->max_len,
+        c->row_start, c->seq,    c->len,
+        c->table};
+  return AKVS_OK;
+}
+
+static akvs_status check_pages(const akvs_model_cfg *m, const akvs_pages *p, PagePool *pool,
+                               size_t *code_bytes, size_t *meta_bytes) {
+  REQUIRE(p, AKVS_EINVAL, "pages are NULL");
+  int shift;
+  akvs_status st = check_page_rows(p->page_rows, &shift);
+  if (st) return st;
+  REQUIRE(p->n_pages >= 0, AKVS_EINVAL, "n_pages %d is negative", p->n_pages);
+  REQUIRE(p->n_pages < (1 << 28), AKVS_ESHAPE, "too many pages");
+  REQUIRE((p->k && p->v && p->k_meta && p->v_meta) || p->n_pages == 0, AKVS_EINVAL,
+          "pages' codes or meta are NULL");
+  REQUIRE(aligned16(p->k) && aligned16(p->v) && aligned16(p->k_meta) && aligned16(p->v_meta),
+          AKVS_EINVAL, "misaligned pages");
+  const size_t rows = ((size_t)p->n_pages << shift) * m->n_kv_heads;
+  *code_bytes = rows * (m->head_dim / 2);
+  *meta_bytes = rows * (m->head_dim / 64) * 4;
+  *pool = {p->k, p->v, reinterpret_cast<uint32_t *>(p->k_meta),
+           reinterpret_cast<uint32_t *>(p->v_meta), p->n_pages, shift};
+  return AKVS_OK;
+}
+
+// A batch over pages: both, and no keys where there are no pages.
+struct PagedCall {
+  PagedBatch s;
+  PagePool p;
+  size_t codes, meta, row_start, seq, len, table;
+};
+static akvs_status check_paged_call(const akvs_model_cfg *m, const akvs_paged_cfg *c,
+                                    const akvs_pages *p, PagedCall *x) {
+  akvs_status st = check_four_bit_model(m);
+  if (!st) st = check_pages(m, p, &x->p, &x->codes, &x->meta);
+  if (!st) st = check_paged(m, c, &x->s);
+  if (st) return st;
+  REQUIRE(c->max_len <= (long long)c->max_pages * p->page_rows, AKVS_ESHAPE,
+          "max_len %d above the keys of %d pages of %d", c->max_len, c->max_pages, p->page_rows);
+  if (x->p.n_pages == 0) x->s.limit = 0;
+  x->row_start = c->row_start ? (c->n_req + 1) * sizeof(int32_t) : 0;
+  x->seq = c->n_req * sizeof(int32_t);
+  x->len = c->n_seq * sizeof(int32_t);
+  x->table = (size_t)c->n_seq * c->max_pages * sizeof(int32_t);
+  return AKVS_OK;
+}
+
+static akvs_status check_table(const akvs_page_table *t, int32_t n, PageTable *x) {
+  REQUIRE(t, AKVS_EINVAL, "page table is NULL");
+  REQUIRE(n >= 0 && t->n_seq >= 1 && t->max_pages >= 1 && t->n_pages >= 0, AKVS_EINVAL,
+          "need n, n_pages >= 0 and n_seq, max_pages >= 1");
+  int shift;
+  akvs_status st = check_page_rows(t->page_rows, &shift);
+  if (st) return st;
+  REQUIRE(t->n_pages < (1 << 28) && t->n_seq < (1 << 24) && n < (1 << 24) &&
+              (long long)t->n_seq * t->max_pages < (1LL << 31) &&
+              (long long)t->max_pages * t->page_rows < (1LL << 31),
+          AKVS_ESHAPE, "page table too large");
+  REQUIRE(t->table && t->len && (t->ref || t->n_pages == 0), AKVS_EINVAL,
+          "table, len or ref is NULL");
+  REQUIRE(aligned16(t->table) && aligned16(t->len) && aligned16(t->ref), AKVS_EINVAL,
+          "misaligned page table");
+  *x = {t->n_seq, t->max_pages, t->n_pages, shift, t->table, t->len, t->ref};
+  return AKVS_OK;
+}
+
+extern "C" {
+
+akvs_status akvs_store_pages(const void *k, int64_t ldk, const void *v, int64_t ldv,
+                             const akvs_paged_cfg *c, const akvs_pages *p,
+                             const akvs_model_cfg *m, hipStream_t stream) {
+  PagedCall x;
+  akvs_status st = check_paged_call(m, c, p, &x);
+  if (st) return st;
+  const long long width = m->n_kv_heads * m->head_dim;
+  if (x.s.n_rows == 0) return AKVS_OK;
+  REQUIRE(k && v, AKVS_EINVAL, "NULL argument");
+  REQUIRE(aligned16(k) && aligned16(v), AKVS_EINVAL, "misaligned argument");
+  REQUIRE(ldk >= width && ldv >= width, AKVS_EINVAL, "row strides shorter than a row");
+  REQUIRE(ldk < (1LL << 31) && ldv < (1LL << 31), AKVS_ESHAPE, "row strides too large");
+  REQUIRE(ldk % 8 == 0 && ldv % 8 == 0, AKVS_EINVAL, "row strides must be multiples of 16 bytes");
+  const size_t kb = ((x.s.n_rows - 1) * ldk + width) * 2, vb = ((x.s.n_rows - 1) * ldv + width) * 2;
+  const Buffer buffers[] = {{"k", k, kb, INPUT},
+                            {"v", v, vb, INPUT},
+                            {"row_start", x.s.row_start, x.row_start, INPUT},
+                            {"seq", x.s.seq, x.seq, INPUT},
+                            {"len", x.s.len, x.len, INPUT},
+                            {"table", x.s.table, x.table, INPUT},
+                            {"pages' k", p->k, x.codes, NONE},
+                            {"pages' v", p->v, x.codes, NONE},
+                            {"pages' k_meta", p->k_meta, x.meta, NONE},
+                            {"pages' v_meta", p->v_meta, x.meta, NONE}};
+  st = check_apart(buffers, 10);
+  if (st) return st;
+  LAUNCH(AKVS_K_OTHER, launch_store_pages(x.s, x.p, k, ldk, v, ldv, m->n_kv_heads, m->head_dim,
+                                          stream));
+  return AKVS_OK;
+}
+
+akvs_status akvs_load_pages(const akvs_paged_cfg *c, const akvs_pages *p, const akvs_model_cfg *m,
+                            void *k_out, void *v_out, int32_t dtype, hipStream_t stream) {
+  PagedCall x;
+  akvs_status st = check_paged_call(m, c, p, &x);
+  if (st) return st;
+  REQUIRE(dtype == AKVS_F32 || dtype == AKVS_BF16, AKVS_EDTYPE, "dtype");
+  REQUIRE(k_out || v_out || x.s.n_rows == 0, AKVS_EINVAL, "neither k_out nor v_out is given");
+  REQUIRE(aligned16(k_out) && aligned16(v_out), AKVS_EINVAL, "misaligned argument");
+  const size_t out = (size_t)x.s.n_rows * m->n_kv_heads * m->head_dim * es_of(dtype);
+  const Buffer buffers[] = {{"row_start", x.s.row_start, x.row_start, INPUT},
+                            {"seq", x.s.seq, x.seq, INPUT},
+                            {"len", x.s.len, x.len, INPUT},
+                            {"table", x.s.table, x.table, INPUT},
+                            {"pages' k", p->k, x.codes, INPUT},
+                            {"pages' v", p->v, x.codes, INPUT},
+                            {"pages' k_meta", p->k_meta, x.meta, INPUT},
+                            {"pages' v_meta", p->v_meta, x.meta, INPUT},
+                            {"k_out", k_out, out, NONE},
+                            {"v_out", v_out, out, NONE}};
+  st = check_apart(buffers, 10);
+  if (st) return st;
+  LAUNCH(AKVS_K_OTHER, launch_load_pages(x.s, x.p, m->n_kv_heads, m->head_dim, k_out, v_out, dtype,
+                                         stream));
+  return AKVS_OK;
+}
+
+size_t akvs_paged_workspace_size(const akvs_model_cfg *m, const akvs_paged_cfg *c) {
+  PagedBatch s;
+  if (check_paged(m, c, &s) != AKVS_OK) return 0;
+  return align256(sizeof(float) *
+                  paged_part_floats(s, m->n_q_heads, m->n_kv_heads, m->head_dim));
+}
+
+akvs_status akvs_paged_attention(const void *q, const akvs_paged_cfg *c, const akvs_pages *p,
+                                 const akvs_model_cfg *m, void *out, float *lse, void *ws,
+                                 size_t ws_bytes, hipStream_t stream) {
+  PagedCall x;
+  akvs_status st = check_paged_call(m, c, p, &x);
+  if (st) return st;
+  REQUIRE((q && out) || x.s.n_rows == 0, AKVS_EINVAL, "NULL argument");
+  REQUIRE(aligned16(q) && aligned16(out) && aligned16(lse) && aligned16(ws), AKVS_EINVAL,
+          "misaligned argument");
+  const size_t need = align256(
+      sizeof(float) * paged_part_floats(x.s, m->n_q_heads, m->n_kv_heads, m->head_dim));
+  REQUIRE(need == 0 || (ws && ws_bytes >= need), AKVS_ENOSPACE, "workspace %zu < %zu bytes",
+          ws_bytes, need);
+  const size_t rows = (size_t)x.s.n_rows * m->n_q_heads;
+  // (a row's query is read by the blocks that write the row, before they do, or by a launch before)
+  const Buffer buffers[] = {{"q", q, rows * m->head_dim * 2, INPUT},
+                            {"row_start", x.s.row_start, x.row_start, INPUT},
+                            {"seq", x.s.seq, x.seq, INPUT},
+                            {"len", x.s.len, x.len, INPUT},
+                            {"table", x.s.table, x.table, INPUT},
+                            {"pages' k", p->k, x.codes, INPUT},
+                            {"pages' v", p->v, x.codes, INPUT},
+                            {"pages' k_meta", p->k_meta, x.meta, INPUT},
+                            {"pages' v_meta", p->v_meta, x.meta, INPUT},
+                            {"out", out, rows * m->head_dim * 2, 0},
+                            {"lse", lse, rows * sizeof(float), NONE},
+                            {"ws", ws, need, NONE}};
+  st = check_apart(buffers, 12);
+  if (st) return st;
+  LAUNCH(AKVS_K_ATTENTION,
+         launch_paged_attention(x.s, x.p, q, m->n_q_heads, m->n_kv_heads, m->head_dim, out, lse,
+                                reinterpret_cast<float *>(ws), stream));
+  return AKVS_OK;
+}
+
+akvs_status akvs_fork_pages(const akvs_page_table *t, int32_t n, const int32_t *src,
+                            const int32_t *dst, hipStream_t stream) {
+  PageTable x;
+  akvs_status st = check_table(t, n, &x);
+  if (st) return st;
+  REQUIRE((src && dst) || n == 0, AKVS_EINVAL, "NULL argument");
+  const size_t ints = n * sizeof(int32_t);
+  const Buffer buffers[] = {
+      {"src", src, ints, INPUT},
+      {"dst", dst, ints, INPUT},
+      {"table", x.table, (size_t)x.n_seq * x.max_pages * sizeof(int32_t), NONE},
+      {"len", x.len, x.n_seq * sizeof(int32_t), NONE},
+      {"ref", x.ref, x.n_pages * sizeof(int32_t), NONE}};
+  st = check_apart(buffers, 5);
+  if (st) return st;
+  LAUNCH(AKVS_K_OTHER, launch_fork_pages(x, n, src, dst, stream));
+  return AKVS_OK;
+}
+
+akvs_status akvs_free_pages(const akvs_page_table *t, int32_t n, const int32_t *seq,
+                            hipStream_t stream) {
+  PageTable x;
+  akvs_status st = check_table(t, n, &x);
+  if (st) return st;
+  REQUIRE(seq || n == 0, AKVS_EINVAL, "NULL argument");
+  const Buffer buffers[] = {
+      {"seq", seq, n * sizeof(int32_t), INPUT},
+      {"table", x.table, (size_t)x.n_seq * x.max_pages * sizeof(int32_t), NONE},
+      {"len", x.len, x.n_seq * sizeof(int32_t), NONE},
+      {"ref", x.ref, x.n_pages * sizeof(int32_t), NONE}};
+  st = check_apart(buffers, 4);
+  if (st) return st;
+  LAUNCH(AKVS_K_OTHER, launch_free_pages(x, n, seq, stream));
+  return AKVS_OK;
+}
+
+size_t akvs_pages_workspace_size(const akvs_page_table *t, int32_t n) {
+  PageTable x;
+  if (check_table(t, n, &x) != AKVS_OK) return 0;
+  return align256(pages_ws_ints(x, n) * sizeof(int32_t));
+}
+
+akvs_status akvs_grow_pages(const akvs_page_table *t, int32_t n, const int32_t *seq,
+                            const int32_t *add, int32_t *served, int32_t *move_src,
+                            int32_t *move_dst, int32_t *counts, void *ws, size_t ws_bytes,
+                            hipStream_t stream) {
+  PageTable x;
+  akvs_status st = check_table(t, n, &x);
+  if (st) return st;
+  REQUIRE((seq && add && served && move_src && move_dst) || n == 0, AKVS_EINVAL, "NULL argument");
+  REQUIRE(counts, AKVS_EINVAL, "counts are NULL");
+  const size_t need = akvs_pages_workspace_size(t, n);
+  REQUIRE(ws && ws_bytes >= need, AKVS_ENOSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
+  REQUIRE(aligned16(ws), AKVS_EINVAL, "misaligned workspace");
+  const size_t ints = n * sizeof(int32_t);
+  const Buffer buffers[] = {
+      {"seq", seq, ints, INPUT},
+      {"add", add, ints, INPUT},
+      {"served", served, ints, NONE},
+      {"move_src", move_src, ints, NONE},
+      {"move_dst", move_dst, ints, NONE},
+      {"counts", counts, 2 * sizeof(int32_t), NONE},
+      {"table", x.table, (size_t)x.n_seq * x.max_pages * sizeof(int32_t), NONE},
+      {"len", x.len, x.n_seq * sizeof(int32_t), NONE},
+      {"ref", x.ref, x.n_pages * sizeof(int32_t), NONE},
+      {"ws", ws, need, NONE}};
+  st = check_apart(buffers, 10);
+  if (st) return st;
+  LAUNCH(AKVS_K_OTHER, launch_grow_pages(x, n, seq, add, served, move_src, move_dst, counts,
+                                         reinterpret_cast<int32_t *>(ws), stream));
+  return AKVS_OK;
+}
+
+akvs_status akvs_compact_pages(const akvs_page_table *t, int32_t *table_out, int32_t *ref_out,
+                               int32_t *move_src, int32_t *move_dst, int32_t *counts, void *ws,
+                               size_t ws_bytes, hipStream_t stream) {
+  PageTable x;
+  akvs_status st = check_table(t, 0, &x);
+  if (st) return st;
+  REQUIRE(table_out && counts && ((ref_out && move_src && move_dst) || x.n_pages == 0),
+          AKVS_EINVAL, "NULL argument");
+  const size_t need = akvs_pages_workspace_size(t, 0);
+  REQUIRE(ws && ws_bytes >= need, AKVS_ENOSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
+  REQUIRE(aligned16(ws), AKVS_EINVAL, "misaligned workspace");
+  const size_t ints = x.n_pages * sizeof(int32_t);
+  const size_t entries = (size_t)x.n_seq * x.max_pages * sizeof(int32_t);
+  const Buffer buffers[] = {{"table", x.table, entries, INPUT},
+                            {"ref", x.ref, ints, INPUT},
+                            {"len", x.len, x.n_seq * sizeof(int32_t), INPUT},
+                            {"table_out", table_out, entries, 0},
+                            {"ref_out", ref_out, ints, 1},
+                            {"move_src", move_src, ints, NONE},
+                            {"move_dst", move_dst, ints, NONE},
+                            {"counts", counts, 2 * sizeof(int32_t), NONE},
+                            {"ws", ws, need, NONE}};
+  st = check_apart(buffers, 9);
+  if (st) return st;
+  LAUNCH(AKVS_K_OTHER, launch_compact_pages(x, table_out, ref_out, move_src, move_dst, counts,
+                                            reinterpret_cast<int32_t *>(ws), stream));
+  return AKVS_OK;
+}
+
+akvs_status akvs_move_pages(const akvs_pages *p, int32_t n_layers, const akvs_model_cfg *m,
+                            const int32_t *src, const int32_t *dst, int32_t max_moves,
+                            const int32_t *n_moves, hipStream_t stream) {
+  akvs_status st = check_four_bit_model(m);
+  PagePool pool;
+  size_t codes, meta;
+  if (!st) st = check_pages(m, p, &pool, &codes, &meta);
+  if (st) return st;
+  REQUIRE(n_layers >= 0 && max_moves >= 0, AKVS_EINVAL, "need n_layers, max_moves >= 0");
+  REQUIRE(n_layers < (1 << 16) && max_moves < (1 << 28), AKVS_ESHAPE, "too large");
+  REQUIRE((src && dst) || max_moves == 0, AKVS_EINVAL, "NULL argument");
+  const size_t ints = max_moves * sizeof(int32_t);
+  const Buffer buffers[] = {{"src", src, ints, INPUT},
+                            {"dst", dst, ints, INPUT},
+                            {"n_moves", n_moves, sizeof(int32_t), INPUT},
+                            {"pages' k", p->k, codes * n_layers, NONE},
+                            {"pages' v", p->v, codes * n_layers, NONE},
+                            {"pages' k_meta", p->k_meta, meta * n_layers, NONE},
+                            {"pages' v_meta", p->v_meta, meta * n_layers, NONE}};
+  st = check_apart(buffers, 7);
+  if (st) return st;
+  LAUNCH(AKVS_K_OTHER, launch_move_pages(pool, n_layers, m->n_kv_heads, m->head_dim, src, dst,
+                                         max_moves, n_moves, stream));
+  return AKVS_OK;
+}
+
+static akvs_status check_w4(int32_t n_rows, int32_t n_out, int32_t n_in) {
+  REQUIRE(n_rows >= 0 && n_out >= 0 && n_in >= 64 && n_in % 64 == 0, AKVS_EINVAL,
+          "need n_rows, n_out >= 0 and n_in a positive multiple of 64");
+  REQUIRE(n_rows < (1 << 24) && n_out < (1 << 24) && n_in < (1 << 24) &&
+              (long long)n_rows * n_out < (1LL << 31),
+          AKVS_ESHAPE, "too large");
+  return AKVS_OK;
+}
+
+size_t akvs_w4_workspace_size(int32_t n_rows, int32_t n_out, int32_t n_in) {
+  if (check_w4(n_rows, n_out, n_in) != AKVS_OK) return 0;
+  return align256(w4_ws_floats(n_rows, n_out, n_in) * sizeof(float));
+}
+
+akvs_status akvs_w4_product(const void *x, int64_t ldx, int32_t x_dtype, int32_t n_rows,
+                            const uint8_t *w, const void *w_meta, int32_t n_out, int32_t n_in,
+                            int32_t mode, const float *resid, void *y, int64_t ldy,
+                            int32_t y_dtype, void *ws, size_t ws_bytes, hipStream_t stream) {
+  akvs_status st = check_w4(n_rows, n_out, n_in);
+  if (st) return st;
+  REQUIRE((x_dtype == AKVS_F32 || x_dtype == AKVS_BF16) &&
+              (y_dtype == AKVS_F32 || y_dtype == AKVS_BF16),
+          AKVS_EDTYPE, "x and y must be F32 or BF16");
+  REQUIRE(mode == AKVS_W4_STORE || mode == AKVS_W4_SWIGLU, AKVS_EINVAL, "mode %d", mode);
+  REQUIRE(mode == AKVS_W4_STORE || n_out % 2 == 0, AKVS_EINVAL, "SWIGLU needs an even n_out");
+  REQUIRE(!resid || (mode == AKVS_W4_STORE && y_dtype == AKVS_F32), AKVS_EINVAL,
+          "resid goes with AKVS_W4_STORE to F32");
+  const int wide = mode == AKVS_W4_SWIGLU ? n_out / 2 : n_out;
+  if (n_rows == 0 || n_out == 0) return AKVS_OK;
+  REQUIRE(x && w && w_meta && y, AKVS_EINVAL, "NULL argument");
+  REQUIRE(aligned16(x) && aligned16(w) && aligned16(w_meta) && aligned16(resid) && aligned16(y) &&
+              aligned16(ws),
+          AKVS_EINVAL, "misaligned argument");
+  const size_t xs = es_of(x_dtype), ys = es_of(y_dtype);
+  REQUIRE(ldx >= n_in && ldy >= wide, AKVS_EINVAL, "row strides shorter than a row");
+  REQUIRE(ldx < (1LL << 31) && ldy < (1LL << 31), AKVS_ESHAPE, "row strides too large");
+  REQUIRE(ldx * xs % 16 == 0, AKVS_EINVAL, "x's row stride must be a multiple of 16 bytes");
+  const size_t need = akvs_w4_workspace_size(n_rows, n_out, n_in);
+  REQUIRE(need == 0 || (ws && ws_bytes >= need), AKVS_ENOSPACE, "workspace %zu < %zu bytes",
+          ws_bytes, need);
+  const size_t yb = ((n_rows - 1) * ldy + wide) * ys;
+  const Buffer buffers[] = {{"x", x, ((n_rows - 1) * ldx + n_in) * xs, INPUT},
+                            {"w", w, (size_t)n_out * (n_in / 2), INPUT},
+                            {"w_meta", w_meta, (size_t)n_out * (n_in / 64) * 4, INPUT},
+                            {"resid", resid, yb, INPUT},
+                            {"y", y, yb, 3},
+                            {"ws", ws, need, NONE}};
+  st = check_apart(buffers, 6);
+  if (st) return st;
+  const W4Args a{x,     ldx,   x_dtype, n_rows, w, reinterpret_cast<const uint32_t *>(w_meta),
+                 n_out, n_in,  mode == AKVS_W4_SWIGLU, resid, y, ldy, y_dtype};
+  LAUNCH(AKVS_K_GEMV, launch_w4(a, reinterpret_cast<float *>(ws), stream));
+  return AKVS_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,617 @@
+// Pages of 4-bit caches: rows in and out, and which page belongs to which sequence.
+#include <algorithm>
+
+#include "kernels.h"
+#include "pages_dev.h"
+#include "quant_dev.h"
+
+namespace akvs {
+
+// ---- rows in and out -------------------------------------------------------------------------
+// Where a row of a batch lies: (page, row of the page); page -1: no key of its sequence, or none
+// of the pool's pages; -2: no row of the batch.
+struct Place {
+  int page, at;
+};
+
+// A block's rows [R0, R0 + n): a thread per request finds those of its rows that are among them.
+// One round trip for batches of up to 256 requests; of more, those before R0's are skipped by a
+// binary search. Ends with a barrier.
+__device__ __forceinline__ void paged_places(const PagedBatch &s, const PagePool &p, int R0, int n,
+                                             Place *places) {
+  const int tid = threadIdx.x, end = min(R0 + n, s.n_rows);
+  auto place = [&](const int32_t *table, int key, int len) {
+    int page = -1;
+    if (key >= 0 && key < len) page = table[key >> p.shift];
+    if (page < 0 || page >= p.n_pages) page = -1;
+    return Place{page, key & ((1 << p.shift) - 1)};
+  };
+  if (!s.row_start) {
+    for (int i = tid; i < n; i += 256) {
+      Place x{-2, 0};
+      if (R0 + i < end) {
+        const int b = (R0 + i) / s.rows_max;
+        int len;
+        const int32_t *table = paged_keys(s, b, len);
+        x = place(table, len - s.rows_max + (R0 + i - b * s.rows_max), len);
+      }
+      places[i] = x;
+    }
+    __syncthreads();
+    return;
+  }
+  for (int i = tid; i < n; i += 256) places[i] = Place{-2, 0};
+  __syncthreads();
+  int b0 = 0;
+  if (s.n_req > 256) {  // the first request that ends past R0
+    int hi = s.n_req;
+    while (b0 < hi) {
+      const int mid = (b0 + hi) >> 1;
+      if (s.row_start[mid + 1] > R0) hi = mid;
+      else b0 = mid + 1;
+    }
+  }
+  for (int base = b0; base < s.n_req; base += 256) {
+    const int b = base + tid;
+    if (b < s.n_req) {
+      int r0, r1, len;
+      paged_rows(s, b, r0, r1);
+      if (r0 < end && r1 > R0) {
+        const int32_t *table = paged_keys(s, b, len);
+        for (int r = max(r0, R0); r < min(r1, end); ++r)
+          places[r - R0] = place(table, len - r1 + r, len);
+      }
+    }
+    if (s.row_start[base] >= end) break;  // (the same for all threads)
+  }
+  __syncthreads();
+}
+
+// A thread has an octet of a row's keys and values each; a block's rows make 4096 octets at most.
+// Bound by the bytes where there are many rows; 16 rows take a launch.
+constexpr int PG_BLOCK_OCTETS = 1024;
+static int rows_per_block(int octets) { return std::max(1, PG_BLOCK_OCTETS / octets); }
+
+template <int HD>
+__global__ __launch_bounds__(256) void k_store_pages(PagedBatch s, PagePool p,
+                                                     const bf16_t *__restrict__ K, long long ldk,
+                                                     const bf16_t *__restrict__ V, long long ldv,
+                                                     int hkv, int rows) {
+  constexpr int OH = HD / 8;  // octets of a head
+  __shared__ Place places[256];
+  const int R0 = blockIdx.x * rows, octets = hkv * OH;
+  paged_places(s, p, R0, rows, places);
+  for (int o = threadIdx.x; o < rows * octets; o += 256) {
+    const int i = o / octets, e = o - i * octets, h = e / OH, c = e % OH;
+    const Place at = places[i];
+    if (at.page < 0) continue;  // (the same for the 8 lanes of a group)
+    const size_t row = (((size_t)at.page * hkv + h) << p.shift) + at.at;
+    float k[8], v[8];
+    load8(K + (R0 + i) * ldk + e * 8, k);
+    load8(V + (R0 + i) * ldv + e * 8, v);
+    uint32_t w, meta;
+    u4_octet(k, w, meta);
+    reinterpret_cast<uint32_t *>(p.k)[row * OH + c] = w;
+    if ((c & 7) == 0) p.k_meta[row * (HD / 64) + c / 8] = meta;
+    u4_octet(v, w, meta);
+    reinterpret_cast<uint32_t *>(p.v)[row * OH + c] = w;
+    if ((c & 7) == 0) p.v_meta[row * (HD / 64) + c / 8] = meta;
+  }
+}
+
+template <int HD, typename TO>
+__device__ __forceinline__ void load_octet(const uint8_t *codes, const uint32_t *meta, size_t row,
+                                           int c, bool there, TO *out) {
+  float x[8];
+  if (there) cache_load8(codes, reinterpret_cast<const _Float16 *>(meta), AKVS_U4G64, row, HD, c * 8, x);
+  else
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = 0.f;
+  store8(out, x);
+}
+
+template <int HD, typename TO>
+__global__ __launch_bounds__(256) void k_load_pages(PagedBatch s, PagePool p, int hkv, int rows,
+                                                    TO *__restrict__ K, TO *__restrict__ V) {
+  constexpr int OH = HD / 8;
+  __shared__ Place places[256];
+  const int R0 = blockIdx.x * rows, octets = hkv * OH;
+  paged_places(s, p, R0, rows, places);
+  for (int o = threadIdx.x; o < rows * octets; o += 256) {
+    const int i = o / octets, e = o - i * octets, h = e / OH, c = e % OH;
+    const Place at = places[i];
+    if (at.page == -2) continue;
+    const bool there = at.page >= 0;
+    const size_t row = (((size_t)max(at.page, 0) * hkv + h) << p.shift) + at.at;
+    const size_t to = ((size_t)(R0 + i) * octets + e) * 8;
+    if (K) load_octet<HD>(p.k, p.k_meta, row, c, there, K + to);
+    if (V) load_octet<HD>(p.v, p.v_meta, row, c, there, V + to);
+  }
+}
+
+hipError_t launch_store_pages(const PagedBatch &s, const PagePool &p, const void *k, long long ldk,
+                              const void *v, long long ldv, int hkv, int hd, hipStream_t st) {
+  if (s.n_rows == 0 || p.n_pages == 0) return hipSuccess;
+  const int rows = std::min(256, rows_per_block(hkv * hd / 8));
+  const dim3 g((s.n_rows + rows - 1) / rows), b(256);
+  auto x = [](const void *a) { return reinterpret_cast<const bf16_t *>(a); };
+  if (hd == 128)
+    hipLaunchKernelGGL(k_store_pages<128>, g, b, 0, st, s, p, x(k), ldk, x(v), ldv, hkv, rows);
+  else
+    hipLaunchKernelGGL(k_store_pages<64>, g, b, 0, st, s, p, x(k), ldk, x(v), ldv, hkv, rows);
+  return hipGetLastError();
+}
+
+hipError_t launch_load_pages(const PagedBatch &s, const PagePool &p, int hkv, int hd, void *k,
+                             void *v, int dtype, hipStream_t st) {
+  if (s.n_rows == 0 || (!k && !v)) return hipSuccess;
+  const int rows = std::min(256, rows_per_block(hkv * hd / 8));
+  const dim3 g((s.n_rows + rows - 1) / rows), b(256);
+#define AKVS_LOAD(HD_, T_)                                                                     \
+  hipLaunchKernelGGL((k_load_pages<HD_, T_>), g, b, 0, st, s, p, hkv, rows,                    \
+                     reinterpret_cast<T_ *>(k), reinterpret_cast<T_ *>(v))
+  if (dtype == AKVS_BF16) {
+    if (hd == 128) AKVS_LOAD(128, bf16_t); else AKVS_LOAD(64, bf16_t);
+  } else {
+    if (hd == 128) AKVS_LOAD(128, float); else AKVS_LOAD(64, float);
+  }
+#undef AKVS_LOAD
+  return hipGetLastError();
+}
+
+// ---- whose pages ---------------------------------------------------------------------------
+// Integers only. Reference counts are changed by integer atomics, whose order does not matter;
+// which page goes where follows from ranks (prefix sums), so that results do not depend on timing.
+
+__device__ __forceinline__ int pages_of(const PageTable &t, int len) {
+  return min((int)(((long long)max(len, 0) + (1 << t.shift) - 1) >> t.shift), t.max_pages);
+}
+__device__ __forceinline__ bool in_pool(const PageTable &t, int id) {
+  return id >= 0 && id < t.n_pages;
+}
+
+// A block per pair.
+__global__ __launch_bounds__(256) void k_fork_pages(PageTable t, int n, const int32_t *src,
+                                                    const int32_t *dst) {
+  const int i = blockIdx.x, a = src[i], b = dst[i];
+  if (a < 0 || a >= t.n_seq || b < 0 || b >= t.n_seq) return;
+  bool out = t.len[b] != 0;
+  for (int j = threadIdx.x; j < n; j += 256) out |= src[j] == b || (j < i && dst[j] == b);
+  if (__syncthreads_or(out)) return;
+  const int len = t.len[a], used = pages_of(t, len);
+  const int32_t *from = t.table + (size_t)a * t.max_pages;
+  int32_t *to = t.table + (size_t)b * t.max_pages;
+  for (int j = threadIdx.x; j < used; j += 256) {
+    const int id = from[j];
+    to[j] = id;
+    if (in_pool(t, id)) atomicAdd(&t.ref[id], 1);
+  }
+  if (threadIdx.x == 0) t.len[b] = max(len, 0);
+}
+
+// A block per sequence.
+__global__ __launch_bounds__(256) void k_free_pages(PageTable t, int n, const int32_t *seq) {
+  const int i = blockIdx.x, a = seq[i];
+  if (a < 0 || a >= t.n_seq) return;
+  bool out = false;
+  for (int j = threadIdx.x; j < i; j += 256) out |= seq[j] == a;
+  if (__syncthreads_or(out)) return;
+  const int used = pages_of(t, t.len[a]);
+  int32_t *mine = t.table + (size_t)a * t.max_pages;
+  for (int j = threadIdx.x; j < used; j += 256) {
+    const int id = mine[j];
+    mine[j] = -1;
+    if (in_pool(t, id)) atomicSub(&t.ref[id], 1);
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) t.len[a] = 0;
+}
+
+// Pages are counted in segments of 4096, 16 a thread.
+constexpr int SEG = 4096, SEG_PER = SEG / 256;
+static int segments(const PageTable &t) { return (t.n_pages + SEG - 1) / SEG; }
+
+__device__ __forceinline__ int wave_sum_int(int x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+  return x;
+}
+__device__ __forceinline__ int block_sum(int x) {  // of 256 threads
+  __shared__ int s[4];
+  x = wave_sum_int(x);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
+  __syncthreads();
+  return s[0] + s[1] + s[2] + s[3];
+}
+// Sum of the threads before this one; total: of all.
+__device__ __forceinline__ int block_scan(int x, int &total) {
+  __shared__ int s[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int y = x;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int z = __shfl_up(y, o, 64);
+    if (lane >= o) y += z;
+  }
+  __syncthreads();
+  if (lane == 63) s[wave] = y;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) before += s[w];
+    total += s[w];
+  }
+  return before + y - x;
+}
+
+// Bit j: page (segment start + 16 thread + j) is in use; pages past the last are not counted in
+// `there`.
+struct SegBits {
+  uint32_t used, there;
+};
+__device__ __forceinline__ SegBits seg_bits(const PageTable &t, int seg) {
+  const int id0 = seg * SEG + threadIdx.x * SEG_PER;
+  SegBits x{0, 0};
+  if (id0 + SEG_PER <= t.n_pages) {
+    const int4 *r = reinterpret_cast<const int4 *>(t.ref + id0);
+#pragma unroll
+    for (int q = 0; q < SEG_PER / 4; ++q) {
+      const int4 v = r[q];
+      x.used |= (uint32_t)(v.x > 0) << (4 * q) | (uint32_t)(v.y > 0) << (4 * q + 1) |
+                (uint32_t)(v.z > 0) << (4 * q + 2) | (uint32_t)(v.w > 0) << (4 * q + 3);
+    }
+    x.there = 0xffffu;
+  } else {
+    for (int j = 0; j < SEG_PER && id0 + j < t.n_pages; ++j) {
+      x.used |= (uint32_t)(t.ref[id0 + j] > 0) << j;
+      x.there |= 1u << j;
+    }
+  }
+  return x;
+}
+// Sum of the counts of segments [0, n).
+__device__ __forceinline__ int seg_before(const int32_t *count, int n) {
+  int x = 0;
+  for (int j = threadIdx.x; j < n; j += 256) x += count[j];
+  return block_sum(x);
+}
+
+// Workspace of akvs_grow_pages (ints): claim [n_seq], ends [n], copies [n], need [n],
+// count [segments], list [n_pages]; of akvs_compact_pages: count, rank [n_pages], refs [n_pages].
+struct GrowWs {
+  int32_t *claim, *ends, *copies, *need, *count, *list;
+};
+static size_t pad4(size_t n) { return (n + 3) & ~(size_t)3; }
+static GrowWs grow_ws(const PageTable &t, int n, int32_t *ws) {
+  GrowWs w;
+  w.claim = ws;
+  w.ends = w.claim + pad4(t.n_seq);
+  w.copies = w.ends + pad4(n);
+  w.need = w.copies + pad4(n);
+  w.count = w.need + pad4(n);
+  w.list = w.count + pad4(segments(t));
+  return w;
+}
+size_t pages_ws_ints(const PageTable &t, int n) {
+  const size_t pages = pad4(t.n_pages), seg = pad4(segments(t));
+  return std::max(pad4(t.n_seq) + 3 * pad4(n) + seg + pages, seg + 2 * pages);
+}
+
+// Block 0: what each sequence needs (pages, and one of them for a copy: bit 30), -1 where it cannot
+// be served, and the sums up to it. The other blocks count the free pages of a segment each.
+constexpr int NEED_COPY = 1 << 30;
+__global__ __launch_bounds__(256) void k_grow_need(PageTable t, int n, const int32_t *seq,
+                                                   const int32_t *add, GrowWs w) {
+  if (blockIdx.x > 0) {
+    const SegBits x = seg_bits(t, blockIdx.x - 1);
+    const int c = block_sum(__popc(x.there & ~x.used));
+    if (threadIdx.x == 0) w.count[blockIdx.x - 1] = c;
+    return;
+  }
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const int a = seq[i];
+    if (a >= 0 && a < t.n_seq) w.claim[a] = 0x7fffffff;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const int a = seq[i];
+    if (a >= 0 && a < t.n_seq) atomicMin(&w.claim[a], i);
+  }
+  __syncthreads();
+  int ends = 0, copies = 0;
+  for (int base = 0; base < n; base += 256) {
+    const int i = base + threadIdx.x;
+    int need = 0, copy = 0;
+    bool ok = false;
+    if (i < n) {
+      const int a = seq[i], more = add[i];
+      // (claim: read past this block's own atomics)
+      ok = a >= 0 && a < t.n_seq && more >= 0 &&
+           __hip_atomic_load(&w.claim[a], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == i;
+      if (ok) {
+        const int rows = 1 << t.shift, old = max(t.len[a], 0);
+        const long long want = ((long long)old + more + rows - 1) >> t.shift;
+        ok = want <= t.max_pages && old + (long long)more <= 0x7fffffff;
+        if (ok && more > 0) {
+          const int have = (int)(((long long)old + rows - 1) >> t.shift);
+          if (old & (rows - 1)) {
+            const int last = t.table[(size_t)a * t.max_pages + (old >> t.shift)];
+            copy = in_pool(t, last) && t.ref[last] > 1;
+          }
+          need = (int)want - have + copy;
+        }
+      }
+    }
+    int tn, tc;
+    const int en = block_scan(need, tn), ec = block_scan(copy, tc);
+    if (i < n) {
+      w.ends[i] = ends + en + need;
+      w.copies[i] = copies + ec + copy;
+      w.need[i] = ok ? need | (copy ? NEED_COPY : 0) : -1;
+    }
+    ends += tn;
+    copies += tc;
+  }
+}
+
+// The free pages that are needed, in ascending order.
+__global__ __launch_bounds__(256) void k_grow_pick(PageTable t, int n, GrowWs w) {
+  const SegBits x = seg_bits(t, blockIdx.x);
+  uint32_t bits = x.there & ~x.used;
+  const int need = w.ends[n - 1], before = seg_before(w.count, blockIdx.x);
+  if (before >= need) return;
+  int total;
+  int rank = before + block_scan(__popc(bits), total);
+  const int id0 = blockIdx.x * SEG + threadIdx.x * SEG_PER;
+  while (bits && rank < need) {
+    const int j = __ffs(bits) - 1;
+    w.list[rank++] = id0 + j;
+    bits &= bits - 1;
+  }
+}
+
+// A wave per sequence; the last block: the totals, and -1 past the last move.
+__global__ __launch_bounds__(256) void k_grow_assign(PageTable t, int n, int segs,
+                                                     const int32_t *seq, const int32_t *add,
+                                                     GrowWs w, int32_t *served, int32_t *move_src,
+                                                     int32_t *move_dst, int32_t *counts) {
+  const int free_pages = seg_before(w.count, segs);
+  auto serves = [&](int i) {
+    const int x = w.need[i];
+    return x >= 0 && ((x & ~NEED_COPY) == 0 || w.ends[i] <= free_pages);
+  };
+  if (blockIdx.x == gridDim.x - 1) {
+    __shared__ int s_moves, s_taken;
+    if (threadIdx.x == 0) s_moves = s_taken = 0;
+    __syncthreads();
+    int moves = 0, taken = 0;
+    for (int i = threadIdx.x; i < n; i += 256)
+      if (serves(i) && (w.need[i] & ~NEED_COPY)) {
+        moves = max(moves, w.copies[i]);
+        taken = max(taken, w.ends[i]);
+      }
+    atomicMax(&s_moves, moves);
+    atomicMax(&s_taken, taken);
+    __syncthreads();
+    moves = s_moves;
+    for (int i = moves + threadIdx.x; i < n; i += 256) move_src[i] = move_dst[i] = -1;
+    if (threadIdx.x == 0) {
+      counts[0] = moves;
+      counts[1] = s_taken;
+    }
+    return;
+  }
+  const int i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (i >= n) return;
+  const bool ok = serves(i);
+  if (lane == 0) served[i] = ok;
+  if (!ok) return;
+  const int a = seq[i], more = add[i], need = w.need[i] & ~NEED_COPY;
+  const bool copy = w.need[i] & NEED_COPY;
+  const int old = max(t.len[a], 0), base = w.ends[i] - need;
+  int32_t *mine = t.table + (size_t)a * t.max_pages;
+  const int have = (int)(((long long)old + (1 << t.shift) - 1) >> t.shift);
+  const int start = copy ? old >> t.shift : have;
+  if (copy && lane == 0) {
+    const int last = mine[start], m = w.copies[i] - 1;
+    move_src[m] = last;
+    move_dst[m] = w.list[base];
+    atomicSub(&t.ref[last], 1);
+  }
+  for (int j = lane; j < need; j += 64) {
+    const int id = w.list[base + j];
+    mine[start + j] = id;
+    t.ref[id] = 1;
+  }
+  if (lane == 0) t.len[a] = old + more;
+}
+
+__global__ __launch_bounds__(256) void k_compact_count(PageTable t, int32_t *count) {
+  const int c = block_sum(__popc(seg_bits(t, blockIdx.x).used));
+  if (threadIdx.x == 0) count[blockIdx.x] = c;
+}
+
+// Ranks: the pages in use from number N (of all in use) on move, the k-th to the k-th free number
+// below N. rank [n_pages] of those that move, -1 of others from N on; refs [moves] theirs.
+__global__ __launch_bounds__(256) void k_compact_rank(PageTable t, int segs, const int32_t *count,
+                                                      int32_t *rank, int32_t *refs,
+                                                      int32_t *move_src, int32_t *move_dst,
+                                                      int32_t *counts) {
+  const int N = seg_before(count, segs), sn = N / SEG;
+  // pages in use below N: whole segments, and those of N's segment before it
+  int below = seg_before(count, min(sn, segs));
+  if (sn < segs) {
+    const int lim = N - (sn * SEG + (int)threadIdx.x * SEG_PER);
+    const uint32_t mask = lim >= SEG_PER ? 0xffffu : lim > 0 ? (1u << lim) - 1 : 0u;
+    below += block_sum(__popc(seg_bits(t, sn).used & mask));
+  }
+  const int moves = N - below;
+  const SegBits x = seg_bits(t, blockIdx.x);
+  int total;
+  int before = seg_before(count, blockIdx.x);
+  before += block_scan(__popc(x.used), total);
+  const int id0 = blockIdx.x * SEG + threadIdx.x * SEG_PER;
+  for (int j = 0; j < SEG_PER && id0 + j < t.n_pages; ++j) {
+    const int id = id0 + j;
+    const bool used = (x.used >> j) & 1;
+    if (id < N) {
+      if (!used) move_dst[id - before] = id;
+    } else {
+      const int k = before - below;
+      rank[id] = used ? k : -1;
+      if (used) {
+        move_src[k] = id;
+        refs[k] = t.ref[id];
+      }
+    }
+    if (id >= moves) {
+      move_src[id] = move_dst[id] = -1;
+    }
+    before += used;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    counts[0] = moves;
+    counts[1] = N;
+  }
+}
+
+// Entries and refs afterwards: blocks [0, entry_blocks) take 256 entries each, the others 256
+// refs. Each value is read by the thread that writes it, so the outputs may be the inputs.
+__global__ __launch_bounds__(256) void k_compact_write(PageTable t, int entry_blocks,
+                                                       const int32_t *rank, const int32_t *refs,
+                                                       const int32_t *move_dst,
+                                                       const int32_t *counts, int32_t *table_out,
+                                                       int32_t *ref_out) {
+  const int N = counts[1];
+  if (blockIdx.x < (unsigned)entry_blocks) {
+    const size_t e = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (e >= (size_t)t.n_seq * t.max_pages) return;
+    const int s = (int)(e / t.max_pages), j = (int)(e - (size_t)s * t.max_pages);
+    int id = t.table[e];
+    if (id >= N && id < t.n_pages && j < pages_of(t, t.len[s]) && rank[id] >= 0)
+      id = move_dst[rank[id]];
+    table_out[e] = id;
+    return;
+  }
+  const int id = (blockIdx.x - entry_blocks) * 256 + threadIdx.x;
+  if (id >= t.n_pages) return;
+  if (id >= N) {
+    ref_out[id] = 0;
+    return;
+  }
+  const int own = t.ref[id];
+  if (own > 0) {
+    ref_out[id] = own;
+    return;
+  }
+  int lo = 0, hi = counts[0] - 1;  // its place among the targets
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (move_dst[mid] < id) lo = mid + 1;
+    else hi = mid;
+  }
+  ref_out[id] = refs[lo];
+}
+
+// Pieces of 16 KB of (move, layer, codes and meta of keys and values), blocks in turn.
+constexpr int MOVE_PIECE = 16384, MOVE_BLOCKS = 2048;
+__global__ __launch_bounds__(256) void k_move_pages(PagePool p, int layers, int code_bytes,
+                                                    int meta_bytes, const int32_t *src,
+                                                    const int32_t *dst, int max_moves,
+                                                    const int32_t *n_moves) {
+  const int moves = n_moves ? min(max(*n_moves, 0), max_moves) : max_moves;
+  const int cp = (code_bytes + MOVE_PIECE - 1) / MOVE_PIECE;
+  const int mp = (meta_bytes + MOVE_PIECE - 1) / MOVE_PIECE;
+  const int per = 2 * (cp + mp);
+  const long long all = (long long)moves * layers * per;
+  for (long long id = blockIdx.x; id < all; id += gridDim.x) {
+    const long long ml = id / per;
+    const int m = (int)(ml / layers), layer = (int)(ml - (long long)m * layers);
+    int piece = (int)(id - ml * per);
+    const int a = src[m], b = dst[m];
+    if (a < 0 || a >= p.n_pages || b < 0 || b >= p.n_pages) continue;
+    const bool meta = piece >= 2 * cp;
+    if (meta) piece -= 2 * cp;
+    const int pieces = meta ? mp : cp, bytes = meta ? meta_bytes : code_bytes;
+    const bool v = piece >= pieces;
+    if (v) piece -= pieces;
+    char *base = meta ? reinterpret_cast<char *>(v ? p.v_meta : p.k_meta)
+                      : reinterpret_cast<char *>(v ? p.v : p.k);
+    base += (size_t)layer * p.n_pages * bytes;
+    const char *from = base + (size_t)a * bytes;
+    char *to = base + (size_t)b * bytes;
+    const int end = min(bytes, (piece + 1) * MOVE_PIECE);
+    u32x4_t x[MOVE_PIECE / 4096];
+#pragma unroll
+    for (int u = 0; u < MOVE_PIECE / 4096; ++u) {
+      const int o = piece * MOVE_PIECE + u * 4096 + threadIdx.x * 16;
+      if (o < end) x[u] = *reinterpret_cast<const u32x4_t *>(from + o);
+    }
+#pragma unroll
+    for (int u = 0; u < MOVE_PIECE / 4096; ++u) {
+      const int o = piece * MOVE_PIECE + u * 4096 + threadIdx.x * 16;
+      if (o < end) *reinterpret_cast<u32x4_t *>(to + o) = x[u];
+    }
+  }
+}
+
+hipError_t launch_fork_pages(const PageTable &t, int n, const int32_t *src, const int32_t *dst,
+                             hipStream_t st) {
+  if (n == 0) return hipSuccess;
+  hipLaunchKernelGGL(k_fork_pages, dim3(n), dim3(256), 0, st, t, n, src, dst);
+  return hipGetLastError();
+}
+
+hipError_t launch_free_pages(const PageTable &t, int n, const int32_t *seq, hipStream_t st) {
+  if (n == 0) return hipSuccess;
+  hipLaunchKernelGGL(k_free_pages, dim3(n), dim3(256), 0, st, t, n, seq);
+  return hipGetLastError();
+}
+
+hipError_t launch_grow_pages(const PageTable &t, int n, const int32_t *seq, const int32_t *add,
+                             int32_t *served, int32_t *move_src, int32_t *move_dst,
+                             int32_t *counts, int32_t *ws, hipStream_t st) {
+  const int segs = segments(t);
+  const GrowWs w = grow_ws(t, n, ws);
+  const dim3 b(256);
+  if (n > 0) {
+    hipLaunchKernelGGL(k_grow_need, dim3(1 + segs), b, 0, st, t, n, seq, add, w);
+    if (segs > 0) hipLaunchKernelGGL(k_grow_pick, dim3(segs), b, 0, st, t, n, w);
+  }
+  hipLaunchKernelGGL(k_grow_assign, dim3((n + 3) / 4 + 1), b, 0, st, t, n, segs, seq, add, w,
+                     served, move_src, move_dst, counts);
+  return hipGetLastError();
+}
+
+hipError_t launch_compact_pages(const PageTable &t, int32_t *table_out, int32_t *ref_out,
+                                int32_t *move_src, int32_t *move_dst, int32_t *counts, int32_t *ws,
+                                hipStream_t st) {
+  const int segs = segments(t);
+  int32_t *count = ws, *rank = count + pad4(segs), *refs = rank + pad4(t.n_pages);
+  const dim3 b(256);
+  if (segs > 0) hipLaunchKernelGGL(k_compact_count, dim3(segs), b, 0, st, t, count);
+  hipLaunchKernelGGL(k_compact_rank, dim3(std::max(segs, 1)), b, 0, st, t, segs, count, rank, refs,
+                     move_src, move_dst, counts);
+  const int entries = (int)(((size_t)t.n_seq * t.max_pages + 255) / 256);
+  hipLaunchKernelGGL(k_compact_write, dim3(entries + (t.n_pages + 255) / 256), b, 0, st, t, entries,
+                     rank, refs, move_dst, counts, table_out, ref_out);
+  return hipGetLastError();
+}
+
+hipError_t launch_move_pages(const PagePool &p, int layers, int hkv, int hd, const int32_t *src,
+                             const int32_t *dst, int max_moves, const int32_t *n_moves,
+                             hipStream_t st) {
+  if (max_moves == 0 || layers == 0 || p.n_pages == 0) return hipSuccess;
+  const int codes = (hkv * hd / 2) << p.shift, meta = (hkv * hd / 64 * 4) << p.shift;
+  const long long per = 2LL * ((codes + MOVE_PIECE - 1) / MOVE_PIECE +
+                               (meta + MOVE_PIECE - 1) / MOVE_PIECE);
+  const long long all = per * max_moves * layers;
+  hipLaunchKernelGGL(k_move_pages, dim3((unsigned)std::min<long long>(all, MOVE_BLOCKS)), dim3(256),
+                     0, st, p, layers, codes, meta, src, dst, max_moves, n_moves);
+  return hipGetLastError();
+}
+
+}  // namespace akvs

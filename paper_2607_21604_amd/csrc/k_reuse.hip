@@ -3,6 +3,7 @@
 #include <algorithm>
 
 #include "kernels.h"
+#include "quant_dev.h"
 
 namespace akvs {
 
@@ -757,27 +758,6 @@ hipError_t launch_correction(CacheLayer cache, const float *mu_k, const float *m
 // per lane, divisions and wave-wide reductions (k_quantize_any below), 60 us here
 // (4.9 TB/s, what a large copy reaches).
 constexpr int QZ_U = 4;
-
-template <int CTRL>
-__device__ __forceinline__ float dpp_f32(float x) {
-  return __int_as_float(
-      __builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, false));
-}
-__device__ __forceinline__ float oct_max(float x) {  // over aligned groups of 8 lanes
-  x = fmaxf(x, dpp_f32<0xB1>(x));    // lane ^ 1
-  x = fmaxf(x, dpp_f32<0x4E>(x));    // lane ^ 2
-  return fmaxf(x, dpp_f32<0x141>(x));  // the two quads of the 8 lanes
-}
-__device__ __forceinline__ float oct_min(float x) {
-  x = fminf(x, dpp_f32<0xB1>(x));
-  x = fminf(x, dpp_f32<0x4E>(x));
-  return fminf(x, dpp_f32<0x141>(x));
-}
-
-// Quotient rounded to an integer code 0..levels (rne), from v = x - zero.
-__device__ __forceinline__ uint32_t int_code(float tq, float levels) {
-  return (uint32_t)(int)fminf(fmaxf(rintf(tq), 0.f), levels);
-}
 
 template <typename TX, int BITS>
 __global__ __launch_bounds__(256) void k_quantize(const TX *__restrict__ x, long long octets,

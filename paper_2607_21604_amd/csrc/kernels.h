@@ -237,6 +237,59 @@ size_t evict_scratch_bytes(const EvictArgs &a, int hkv);  // 0: it would not spl
 hipError_t launch_evict_gather(const void *k, const void *v, const EvictArgs &a, int hkv,
                                int row_bytes, const int32_t *keep, void *k_out, void *v_out,
                                int32_t *lens_out, hipStream_t s);
+// ---- k_pages.hip, k_paged.hip -----------------------------------------------------------
+// A batch over sequences in pages (akvs_paged_cfg); limit: the most keys of a sequence.
+struct PagedBatch {
+  int n_req, n_rows, rows_max, n_seq, max_pages, limit;
+  const int32_t *row_start, *seq, *len, *table;
+};
+// One layer's pages: page_rows = 1 << shift; meta as (scale, zero) pairs of fp16.
+struct PagePool {
+  uint8_t *k, *v;
+  uint32_t *k_meta, *v_meta;
+  int n_pages, shift;
+};
+struct PageTable {
+  int n_seq, max_pages, n_pages, shift;
+  int32_t *table, *len, *ref;
+};
+hipError_t launch_store_pages(const PagedBatch &s, const PagePool &p, const void *k, long long ldk,
+                              const void *v, long long ldv, int hkv, int hd, hipStream_t st);
+hipError_t launch_load_pages(const PagedBatch &s, const PagePool &p, int hkv, int hd, void *k,
+                             void *v, int dtype, hipStream_t st);
+hipError_t launch_fork_pages(const PageTable &t, int n, const int32_t *src, const int32_t *dst,
+                             hipStream_t st);
+hipError_t launch_free_pages(const PageTable &t, int n, const int32_t *seq, hipStream_t st);
+size_t pages_ws_ints(const PageTable &t, int n);
+hipError_t launch_grow_pages(const PageTable &t, int n, const int32_t *seq, const int32_t *add,
+                             int32_t *served, int32_t *move_src, int32_t *move_dst,
+                             int32_t *counts, int32_t *ws, hipStream_t st);
+hipError_t launch_compact_pages(const PageTable &t, int32_t *table_out, int32_t *ref_out,
+                                int32_t *move_src, int32_t *move_dst, int32_t *counts, int32_t *ws,
+                                hipStream_t st);
+hipError_t launch_move_pages(const PagePool &p, int layers, int hkv, int hd, const int32_t *src,
+                             const int32_t *dst, int max_moves, const int32_t *n_moves,
+                             hipStream_t st);
+// floats of `part` that launch_paged_attention needs
+size_t paged_part_floats(const PagedBatch &s, int hq, int hkv, int hd);
+hipError_t launch_paged_attention(const PagedBatch &s, const PagePool &p, const void *q, int hq,
+                                  int hkv, int hd, void *out, float *lse, float *part,
+                                  hipStream_t st);
+// ---- k_w4.hip ---------------------------------------------------------------------------
+struct W4Args {
+  const void *x;
+  long long ldx;
+  int x_dtype, rows;
+  const uint8_t *w;
+  const uint32_t *meta;
+  int n_out, n_in, swiglu;
+  const float *resid;
+  void *y;
+  long long ldy;
+  int y_dtype;
+};
+size_t w4_ws_floats(int rows, int n_out, int n_in);
+hipError_t launch_w4(const W4Args &a, float *ws, hipStream_t st);
 // ---- k_decode.hip -------------------------------------------------------------------
 // Matrix-vector products of one token, y = W x (W [N][K], K a multiple of 8), item i of
 // a launch = one pair of rows, with these epilogues:

@@ -1,0 +1,733 @@
+"""Operators that decode from four bits against their definitions in 64 bits."""
+import math
+import random
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_21604_amd import akvs
+from tests import four_bit_ref as ref
+from tests.gpu_util import DEV
+from tests.libutil import ensure_built
+
+pytestmark = pytest.mark.gpu
+
+BF, F32, F16, U8 = torch.bfloat16, torch.float32, torch.float16, torch.uint8
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    return ensure_built()
+
+
+def model(hq, hkv, hd):
+    return akvs.ModelCfg(1, 256, hq, hkv, hd, 256, 64, 1e4, 1e-6, akvs.AKVS_BF16)
+
+
+def randn(seed, *shape, dt=F32, std=1.0):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return (torch.randn(shape, generator=g) * std).to(dt)
+
+
+def ints(x):
+    return torch.tensor(np.asarray(x), dtype=torch.int32, device=DEV)
+
+
+class Batch:
+    """Sequences in pages and a batch over them. Every place of the pool that no key has holds NaN
+    (scale and zero) and codes of ones; entries of the table past a sequence's keys are wild."""
+
+    def __init__(self, geom, page_rows, lens, rows, seq=None, seed=0, spare=0, max_len=None,
+                 shared=0, std=1.0, q_std=2.0):
+        self.hq, self.hkv, self.hd = geom
+        self.m, self.page = model(*geom), page_rows
+        B = len(rows)
+        self.seq = list(range(B)) if seq is None else list(seq)
+        self.lens, self.rows = list(lens), list(rows)
+        S = len(lens)
+        need = [-(-n // page_rows) for n in lens]
+        same = min([shared] + [n // page_rows for n in lens if n])
+        rng = random.Random(seed)
+        self.n_pages = sum(need) + 2
+        free = list(range(self.n_pages))
+        rng.shuffle(free)
+        wide = max(need + [1]) + 1
+        first = [free.pop() for _ in range(same)]
+        self.table = [[rng.choice([-1, 1 << 30, -(1 << 31), 3]) for _ in range(wide)]
+                      for _ in range(S)]
+        for s in range(S):
+            own = [free.pop() for _ in range(need[s] - (same if need[s] else 0))]
+            self.table[s][:need[s]] = ((first if need[s] else []) + own)[:need[s]]
+        self.start = [0] + list(np.cumsum(rows))
+        self.n = self.start[-1]
+        self.max_len = max(lens + [0]) if max_len is None else max_len
+        shape = (self.n_pages, self.hkv, page_rows)
+        self.pools = []
+        for i in range(2):  # keys, values
+            x = randn(seed + 3 + i, *shape, self.hd, std=std)
+            codes, meta = ref.quantise(x)
+            live = torch.zeros(self.n_pages, page_rows, dtype=torch.bool)
+            for s in range(S):
+                for j in range(lens[s]):
+                    page, at = ref.place(self.table[s], page_rows, self.n_pages, j)
+                    if page >= 0:
+                        live[page, at] = True
+            codes[~live[:, None].expand(shape)] = 255
+            meta[~live[:, None].expand(shape)] = math.nan
+            self.pools.append([codes, meta])
+        self.q = randn(seed + 1, self.n + spare, self.hq, self.hd, dt=BF, std=q_std)
+        self.out = torch.full((self.n + spare, self.hq, self.hd), 7.0, dtype=BF, device=DEV)
+        self.lse = torch.full((self.n + spare, self.hq), 7.0, dtype=F32, device=DEV)
+
+    def upload(self):
+        (k, km), (v, vm) = self.pools
+        self.p = akvs.pages(*(x.to(DEV).contiguous() for x in (k, v, km, vm)))
+        return self.p
+
+    def cfg(self, uniform=False):
+        return akvs.paged_cfg(len(self.rows), self.q.shape[0], max(1, max(self.rows)),
+                              ints(self.lens), ints(self.table), self.max_len,
+                              None if uniform else ints(self.start), ints(self.seq))
+
+    def ws(self, c):
+        n = akvs.akvs_paged_workspace_size(self.m, c)
+        return torch.full((n,), 255, dtype=U8, device=DEV) if n else None
+
+    def attend(self, uniform=False, **kw):
+        c = self.cfg(uniform)
+        self.qd = self.q.to(DEV)
+        akvs.akvs_paged_attention(self.qd, c, self.upload(), self.m, self.out, self.lse, self.ws(c),
+                                  **kw)
+
+    def expect(self):
+        return ref.attention(self.q[:self.n], *self.pools, self.table, self.lens, self.start,
+                             self.seq)
+
+    def check(self, r=None):
+        r = self.expect() if r is None else r
+        got, gl = self.out[:self.n].double().cpu(), self.lse[:self.n].double().cpu()
+        keys = max(self.lens + [1])
+        none = torch.isinf(r["lse"])
+        assert torch.equal(torch.isinf(gl), none)
+        tol = ref.lse_bound(r, self.hd, keys)
+        err = (gl - r["lse"]).abs()
+        assert bool((err <= tol)[~none].all()), float((err - tol)[~none].max())
+        tol, err = ref.out_bound(r, self.hd, keys), (got - r["out"]).abs()
+        assert bool((err <= tol).all()), float((err - tol).max())
+        assert bool((self.out[self.n:] == 7).all()) and bool((self.lse[self.n:] == 7).all())
+
+
+GEOMS = [(28, 4, 128), (40, 8, 128), (20, 1, 128), (34, 1, 128), (16, 8, 64), (8, 8, 64),
+         (35, 1, 64), (3, 3, 128)]
+LENS = [1, 2, 15, 16, 17, 63, 64, 65, 0, 130]
+
+
+@pytest.mark.parametrize("geom", GEOMS)
+@pytest.mark.parametrize("page_rows", [16, 64, 256])
+def test_decode_batch(geom, page_rows):
+    """One row per request, sequences from no key to past several tiles' ends."""
+    b = Batch(geom, page_rows, LENS, [1] * len(LENS), seed=page_rows)
+    b.attend(uniform=True)
+    b.check()
+
+
+@pytest.mark.parametrize("geom", [(28, 4, 128), (16, 8, 64), (35, 1, 64)])
+@pytest.mark.parametrize("page_rows", [32, 128])
+def test_ragged_rows(geom, page_rows):
+    """Requests without rows, with more rows than keys (the first see none), in an order of
+    sequences of their own; rows behind the last request stay as they were."""
+    b = Batch(geom, page_rows, [3, 77, 2, 0, 50, 131, 260], [3, 0, 5, 2, 17, 33],
+              seq=[0, 1, 2, 3, 6, 5], seed=11, spare=3)
+    b.attend()
+    b.check()
+
+
+@pytest.mark.parametrize("geom", [(28, 4, 128), (8, 8, 64), (40, 8, 128)])
+@pytest.mark.parametrize("rows", [[1, 1, 1], [1, 7, 30]])
+def test_long_sequences_are_split(geom, rows):
+    """Sequences long enough for several blocks each, beside a short one; two of them share their
+    first pages."""
+    b = Batch(geom, 64, [1500, 9, 2111], rows, seed=5, shared=20 if rows[1] == 1 else 0)
+    b.attend(uniform=rows[1] == 1)
+    b.check()
+
+
+def test_shared_pages():
+    b = Batch((28, 4, 128), 16, [70, 81, 64, 130], [1, 3, 2, 1], seed=7, shared=4)
+    b.attend()
+    b.check()
+
+
+@pytest.mark.parametrize("geom", [(28, 4, 128), (16, 8, 64)])
+def test_the_smallest_and_largest_scales(geom):
+    """Subnormal scales, groups without spread, values near fp16's largest."""
+    b = Batch(geom, 16, [40, 33], [2, 1], seed=13)
+    for codes, meta in b.pools:
+        live = ~torch.isnan(meta[..., 0])
+        g = torch.Generator()
+        g.manual_seed(1)
+        pick = torch.randint(0, 4, live.shape, generator=g)
+        small, flat = (pick == 0) & live, (pick == 1) & live
+        meta[small] = torch.tensor([6e-8, -3e-7], dtype=F16)
+        meta[flat] = torch.tensor([0.0, 0.75], dtype=F16)
+    vm = b.pools[1][1]
+    vm[(torch.rand(vm.shape[:-1], generator=torch.Generator().manual_seed(2)) < 0.2) &
+       ~torch.isnan(vm[..., 0])] = torch.tensor([8000.0, -60000.0], dtype=F16)
+    b.attend()
+    b.check()
+
+
+def test_large_scores():
+    """Scores of hundreds: one key takes all the weight, wherever it is."""
+    b = Batch((28, 4, 128), 64, [200, 333, 64], [2, 1, 1], seed=17, q_std=40.0)
+    b.attend()
+    b.check()
+
+
+def test_indices_out_of_range():
+    """Sequences that do not exist see no key; lengths past max_len are cut; missing pages' keys
+    and values are 0. Nothing is read outside the pool."""
+    b = Batch((28, 4, 128), 16, [40, 50, 33, 20], [1, 2, 1, 1, 1], seq=[0, 9, -1, 2, 1], seed=19)
+    b.table[0][1] = -1
+    b.table[0][2] = b.n_pages
+    b.table[2][0] = -(1 << 31)
+    b.attend()
+    b.check()
+    assert bool((b.out[1:4] == 0).all()) and bool((b.lse[1:4] == -math.inf).all())
+    b = Batch((28, 4, 128), 16, [40, 50], [1, 1], seed=23, max_len=33)
+    b.attend()
+    b.lens = [33, 33]
+    b.check()
+    b.lens = [-5, 1 << 30]  # the second sequence: 33 keys
+    b.attend()
+    b.lens = [0, 33]
+    b.check()
+
+
+def test_no_pages_and_no_rows():
+    m = model(16, 8, 64)
+    z = lambda *s, dt=U8: torch.zeros(s, dtype=dt, device=DEV)
+    p = akvs.pages(z(0, 8, 16, 32), z(0, 8, 16, 32), z(0, 8, 16, 1, 2, dt=F16),
+                   z(0, 8, 16, 1, 2, dt=F16))
+    q = randn(3, 4, 16, 64, dt=BF).to(DEV)
+    out, lse = torch.full_like(q, 7.0), torch.full((4, 16), 7.0, device=DEV)
+    c = akvs.paged_cfg(2, 4, 2, ints([5, 9]), ints([[0], [1]]), 16)
+    n = akvs.akvs_paged_workspace_size(m, c)
+    akvs.akvs_paged_attention(q, c, p, m, out, lse, torch.empty(n, dtype=U8, device=DEV) if n else None)
+    assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+    k = torch.full((4, 8, 64), 3.0, device=DEV)
+    akvs.akvs_load_pages(c, p, m, k, None)
+    assert bool((k == 0).all())
+    akvs.akvs_store_pages(q[:, :8].contiguous(), q[:, 8:].contiguous(), c, p, m)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("geom", [(28, 4, 128), (16, 8, 64)])
+def test_what_is_not_a_number_reaches_the_rows_that_see_it(geom):
+    """A value (a key) without a number in the middle of a question: the rows before it are as
+    ever, those from it on have none."""
+    for which in (1, 0):
+        b = Batch(geom, 16, [40, 100], [6, 2], seed=29)
+        r = b.expect()  # before the spoilt key
+        page, at = ref.place(b.table[0], 16, b.n_pages, 37)  # rows 0..2 of request 0 do not see it
+        b.pools[which][1][page, :, at] = math.nan
+        b.attend()
+        bad = slice(3, 6)
+        assert bool(torch.isnan(b.out[bad]).all())
+        b.out[bad], b.lse[bad] = 0, 0
+        for x in r:
+            r[x][bad] = 0
+        b.check(r)
+    b = Batch(geom, 16, [40, 100], [6, 2], seed=31)
+    r = b.expect()
+    page, at = ref.place(b.table[0], 16, b.n_pages, 37)
+    b.pools[1][1][page, :, at, :, 1] = math.inf  # zero: every value of the key
+    b.attend()
+    assert bool((b.out[3:6] == math.inf).all())
+    b.out[3:6] = 0
+    for x in r:
+        if x != "lse":
+            r[x][3:6] = 0
+    r["reach"] = torch.ones_like(r["reach"]) * r["reach"].max()
+    b.check(r)
+
+
+def test_in_place_and_without_lse():
+    b = Batch((28, 4, 128), 64, [300, 40], [1, 4], seed=37)
+    b.attend()
+    want = b.out.clone()
+    c, q = b.cfg(), b.qd.clone()
+    akvs.akvs_paged_attention(q, c, b.p, b.m, q, None, b.ws(c))
+    assert torch.equal(q, want)
+
+
+def test_pages_beyond_32_bits():
+    """Codes of more than 4 GiB, the keys at their end."""
+    geom, page, n = (16, 8, 128), 256, 36000
+    m = model(*geom)
+    b = Batch(geom, page, [300, 257], [2, 1], seed=41)
+    far = [n - 1 - i for i in range(b.n_pages)]
+    big = []
+    for codes, meta in b.pools:
+        c = torch.empty((n, 8, page, 64), dtype=U8, device=DEV)
+        t = torch.empty((n, 8, page, 2, 2), dtype=F16, device=DEV)
+        assert c.numel() > 1 << 32
+        for i, f in enumerate(far):
+            c[f], t[f] = codes[i].to(DEV), meta[i].to(DEV)
+        big.append((c, t))
+    r = b.expect()
+    b.table = [[far[x] if 0 <= x < b.n_pages else x for x in row] for row in b.table]
+    p = akvs.pages(big[0][0], big[1][0], big[0][1], big[1][1])
+    c, qd = b.cfg(), b.q.to(DEV)
+    akvs.akvs_paged_attention(qd, c, p, m, b.out, b.lse, b.ws(c))
+    b.check(r)
+    k, v = (randn(i, 3, 8, 128, dt=BF).to(DEV) for i in (1, 2))
+    akvs.akvs_store_pages(k, v, c, p, m)
+    back = torch.empty((3, 8, 128), device=DEV)
+    akvs.akvs_load_pages(c, p, m, None, back)
+    assert torch.equal(back.cpu().double(), ref.values(*ref.quantise(v.cpu())))
+    src, dst = ints([far[0]]), ints([n // 2])
+    akvs.akvs_move_pages(p, 1, m, src, dst, 1)
+    for c, t in big:
+        assert torch.equal(c[n // 2], c[far[0]])
+        assert torch.equal(t[n // 2].view(torch.int16), t[far[0]].view(torch.int16))
+
+
+# ---- rows in and out ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("geom", [(28, 4, 128), (16, 8, 64), (20, 1, 128), (4, 1, 64)])
+@pytest.mark.parametrize("page_rows", [16, 64])
+@pytest.mark.parametrize("rows", [[1] * 6, [3, 0, 40, 1, 6, 17]])
+def test_store_and_load(geom, page_rows, rows):
+    """Rows strided as in a packed projection; the codes are akvs_quantize_cache's, everything else
+    of the pool stays as it was; rows that are no keys are nowhere, and 0 when read."""
+    hq, hkv, hd = geom
+    lens = [5, 30, 45, 1, 3, 100, 9]
+    b = Batch(geom, page_rows, lens, rows, seq=[0, 1, 2, 6, 4, 5], seed=3, spare=2)
+    uniform = rows == [1] * 6
+    if uniform:
+        b.q = b.q[:6]
+    b.upload()
+    n = b.q.shape[0]
+    wide = randn(5, n, 3 * hkv * hd + 16, dt=BF, std=3.0).to(DEV)
+    k, v = wide[:, 8:8 + hkv * hd], wide[:, 16 + hkv * hd:16 + 2 * hkv * hd]
+    before = [x.clone() for x in b.p._keep]
+    akvs.akvs_store_pages(k, v, b.cfg(uniform), b.p, b.m)
+    want = [x.cpu().clone() for x in before]
+    kept = torch.zeros(n, dtype=torch.bool)
+    codes = [ref.quantise(x.contiguous().view(n, hkv, hd).cpu()) for x in (k, v)]
+    for i in range(len(rows)):
+        r0, r1, s = b.start[i], b.start[i + 1], b.seq[i]
+        for r in range(r0, r1):
+            j = lens[s] - r1 + r
+            if j < 0:
+                continue
+            page, at = ref.place(b.table[s], page_rows, b.n_pages, j)
+            kept[r] = True
+            for w, x in ((0, codes[0][0]), (1, codes[1][0]), (2, codes[0][1]), (3, codes[1][1])):
+                want[w][page, :, at] = x[r]
+    assert not bool(kept.all()) or uniform
+    for got, x in zip(b.p._keep, want):
+        got = got.cpu()
+        bits = lambda t: t.contiguous().view(U8)
+        assert torch.equal(bits(got), bits(x))
+    for dt in (F32, BF):
+        out = [torch.full((n, hkv, hd), 7.0, dtype=dt, device=DEV) for _ in range(2)]
+        akvs.akvs_load_pages(b.cfg(uniform), b.p, b.m, *out)
+        for got, c in zip(out, codes):
+            x = ref.values(*c)
+            x[~kept] = 0
+            x[b.n:] = 7
+            assert torch.equal(got.cpu(), x.to(dt))
+    # the library's own quantiser gives the same codes
+    dense = k.contiguous()
+    c2 = torch.empty((n * hkv, hd // 2), dtype=U8, device=DEV)
+    m2 = torch.empty((n * hkv, hd // 64, 2), dtype=F16, device=DEV)
+    akvs.akvs_quantize_cache(dense, n * hkv, hd, 4, c2, m2)
+    assert torch.equal(c2.cpu().view_as(codes[0][0]), codes[0][0])
+
+
+def test_store_many_requests():
+    """More requests than a block has threads, with and without rows."""
+    rng = random.Random(2)
+    rows = [rng.choice([0, 0, 1, 1, 2, 9]) for _ in range(700)]
+    lens = [max(1, n + rng.randint(-1, 20)) for n in rows]
+    b = Batch((8, 1, 64), 16, lens, rows, seed=9, spare=5)
+    b.upload()
+    n = b.q.shape[0]
+    k, v = (randn(i, n, 1, 64, dt=BF).to(DEV) for i in (1, 2))
+    akvs.akvs_store_pages(k, v, b.cfg(), b.p, b.m)
+    kb, vb = (torch.full((n, 1, 64), 7.0, device=DEV) for _ in range(2))
+    akvs.akvs_load_pages(b.cfg(), b.p, b.m, kb, vb)
+    for got, x in ((kb, k), (vb, v)):
+        want = ref.values(*ref.quantise(x.cpu()))
+        for i, nb in enumerate(rows):
+            for r in range(b.start[i], b.start[i + 1]):
+                if lens[i] - nb + r - b.start[i] < 0:
+                    want[r] = 0
+        want[b.n:] = 7
+        assert torch.equal(got.cpu().double(), want)
+
+
+def test_codes_next_to_a_border():
+    """Quotients within a few steps of a half: the codes are those of the divisions."""
+    g = torch.Generator()
+    g.manual_seed(4)
+    n = 512
+    x = torch.empty(n, 1, 64)
+    lo = torch.randn(n, 1, 1, generator=g)
+    step = torch.rand(n, 1, 1, generator=g) + 0.01
+    x[:] = lo + step * (torch.randint(0, 15, (n, 1, 64), generator=g) + 0.5)
+    x[..., 0], x[..., 1] = lo[..., 0], (lo + 15 * step)[..., 0]
+    x = x.to(BF)
+    m = model(4, 1, 64)
+    z = lambda *s, dt=U8: torch.zeros(s, dtype=dt, device=DEV)
+    p = akvs.pages(z(2, 1, 256, 32), z(2, 1, 256, 32), z(2, 1, 256, 1, 2, dt=F16),
+                   z(2, 1, 256, 1, 2, dt=F16))
+    c = akvs.paged_cfg(1, n, n, ints([n]), ints([[1, 0]]), n)
+    akvs.akvs_store_pages(x.to(DEV), x.to(DEV), c, p, m)
+    codes, meta = ref.quantise(x)
+    got = p._keep[0].cpu()
+    assert torch.equal(torch.cat((got[1, 0], got[0, 0])), codes[:, 0])
+
+
+# ---- whose pages ---------------------------------------------------------------------------------
+
+def random_tables(seed, S, page_rows, wide, n_pages, fill=0.6):
+    """Tables of S sequences, some of which share leading pages; a third is empty."""
+    rng = random.Random(seed)
+    free = list(range(n_pages))
+    rng.shuffle(free)
+    table = [[-1] * wide for _ in range(S)]
+    lens, ref_ = [0] * S, [0] * n_pages
+    for s in range(S):
+        if rng.random() < 1 / 3 or len(free) < (1 - fill) * n_pages:
+            continue
+        lens[s] = rng.randint(0, wide * page_rows)
+        need = -(-lens[s] // page_rows)
+        k = 0
+        if s and lens[s - 1] and rng.random() < 0.5:
+            have = -(-lens[s - 1] // page_rows)
+            k = rng.randint(0, min(need, have))
+        if len(free) < need - k:
+            lens[s] = 0
+            continue
+        table[s][:k] = table[s - 1][:k]
+        table[s][k:need] = [free.pop() for _ in range(need - k)]
+        for x in table[s][:need]:
+            ref_[x] += 1
+    return table, lens, ref_
+
+
+class Pool:
+    def __init__(self, table, lens, refs, page_rows):
+        self.want = ref.Tables(table, lens, refs, page_rows)
+        self.table, self.len = ints(table), ints(lens)
+        self.ref = ints(refs) if refs else torch.zeros(0, dtype=torch.int32, device=DEV)
+        self.t = akvs.page_table(self.table, self.len, self.ref, page_rows)
+
+    def check(self):
+        assert self.table.cpu().tolist() == self.want.table
+        assert self.len.cpu().tolist() == self.want.len
+        assert self.ref.cpu().tolist() == self.want.ref
+
+    def ws(self, n):
+        return torch.full((akvs.akvs_pages_workspace_size(self.t, n),), 255, dtype=U8, device=DEV)
+
+    def grow(self, seq, add):
+        n = len(seq)
+        a = [torch.full((n,), -9, dtype=torch.int32, device=DEV) for _ in range(3)]
+        counts = torch.full((2,), -9, dtype=torch.int32, device=DEV)
+        akvs.akvs_grow_pages(self.t, ints(seq), ints(add), *a, counts, self.ws(n))
+        served, moves, want = self.want.grow(list(seq), list(add))
+        pad = [-1] * (n - len(moves))
+        assert a[0].cpu().tolist() == served
+        assert a[1].cpu().tolist() == [x for x, _ in moves] + pad
+        assert a[2].cpu().tolist() == [y for _, y in moves] + pad
+        assert counts.cpu().tolist() == want
+        self.check()
+        return served, moves
+
+    def compact(self, in_place):
+        n = self.ref.numel()
+        tab = self.table if in_place else torch.full_like(self.table, -9)
+        rf = self.ref if in_place else torch.full_like(self.ref, -9)
+        a = [torch.full((n,), -9, dtype=torch.int32, device=DEV) for _ in range(2)]
+        counts = torch.full((2,), -9, dtype=torch.int32, device=DEV)
+        akvs.akvs_compact_pages(self.t, tab, rf, *a, counts, self.ws(0))
+        table, refs, moves, want = self.want.compact()
+        pad = [-1] * (n - len(moves))
+        assert tab.cpu().tolist() == table and rf.cpu().tolist() == refs
+        assert a[0].cpu().tolist() == [x for x, _ in moves] + pad
+        assert a[1].cpu().tolist() == [y for _, y in moves] + pad
+        assert counts.cpu().tolist() == want
+        return moves
+
+
+SIZES = [(1, 16, 1, 1), (5, 16, 3, 9), (40, 32, 9, 200), (300, 16, 40, 5000), (64, 256, 7, 9000)]
+
+
+@pytest.mark.parametrize("S,page_rows,wide,n_pages", SIZES)
+def test_fork_and_free(S, page_rows, wide, n_pages):
+    p = Pool(*random_tables(S, S, page_rows, wide, n_pages), page_rows)
+    rng = random.Random(S)
+    for _ in range(3):
+        n = rng.randint(1, 2 * S)
+        pick = lambda: [rng.randint(-2, S + 1) for _ in range(n)]
+        src, dst = pick(), pick()
+        akvs.akvs_fork_pages(p.t, ints(src), ints(dst))
+        p.want.fork(src, dst)
+        p.check()
+        seq = pick()[:max(1, n // 3)]
+        akvs.akvs_free_pages(p.t, ints(seq), )
+        p.want.free(seq)
+        p.check()
+
+
+@pytest.mark.parametrize("S,page_rows,wide,n_pages", SIZES)
+def test_grow(S, page_rows, wide, n_pages):
+    """Until the pool is full: copies of shared last pages, sequences named twice or out of range,
+    that want too much, or come after the last free page."""
+    p = Pool(*random_tables(S + 1, S, page_rows, wide, n_pages), page_rows)
+    rng = random.Random(S)
+    src = [s for s in range(S) if p.want.len[s]][:max(1, S // 4)]
+    dst = [s for s in range(S) if not p.want.len[s]][:len(src)]
+    if src and dst:
+        akvs.akvs_fork_pages(p.t, ints(src[:len(dst)]), ints(dst))
+        p.want.fork(src[:len(dst)], dst)
+    some = False
+    for _ in range(4):
+        n = rng.randint(1, S + 3)
+        seq = [rng.randint(-1, S) for _ in range(n)]
+        add = [rng.choice([0, 1, 1, 3, page_rows, 5 * page_rows, -1]) for _ in range(n)]
+        served, moves = p.grow(seq, add)
+        some = some or bool(moves)
+    assert some or S < 40
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("S,page_rows,wide,n_pages", SIZES)
+def test_compact(S, page_rows, wide, n_pages, in_place):
+    p = Pool(*random_tables(S + 2, S, page_rows, wide, n_pages, fill=0.4), page_rows)
+    p.compact(in_place)
+
+
+@pytest.mark.parametrize("n_pages", [0, 4096, 8192, 12289])
+def test_compact_at_segment_ends(n_pages):
+    """Pools of whole segments, full, empty, and used in their upper half alone."""
+    table = [[-1]]
+    for refs in ([0] * n_pages, [1] * n_pages,
+                 [int(2 * i >= n_pages) for i in range(n_pages)]):
+        p = Pool(table, [0], refs, 16)
+        p.compact(False)
+        p.grow([0], [1])
+
+
+def test_grow_nothing():
+    p = Pool(*random_tables(3, 6, 16, 4, 20), 16)
+    p.grow([], [])
+    p.grow([0], [0])
+
+
+@pytest.mark.parametrize("hkv,hd,page_rows,layers", [(4, 128, 32, 3), (1, 64, 16, 2), (8, 128, 256, 1)])
+@pytest.mark.parametrize("counted", [True, False])
+def test_move_pages(hkv, hd, page_rows, layers, counted):
+    """In all layers; moves past the count, and indices out of range, are left out."""
+    n = 30
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    pool = [torch.randint(0, 256, (layers, n, hkv, page_rows, w), generator=g, device=DEV, dtype=U8)
+            for w in (hd // 2, hd // 2)]
+    meta = [torch.randint(0, 30000, (layers, n, hkv, page_rows, hd // 64, 2), generator=g,
+                          device=DEV, dtype=torch.int16).view(F16) for _ in range(2)]
+    before = [x.clone() for x in pool + meta]
+    src, dst = [3, 29, 0, -1, 4, 30, 7], [5, 1, 28, 2, 31, 6, 8]
+    p = akvs.pages(pool[0][0], pool[1][0], meta[0][0], meta[1][0])
+    akvs.akvs_move_pages(p, layers, model(hkv, hkv, hd), ints(src), ints(dst), len(src),
+                         ints([6, 99]) if counted else None)
+    for got, x in zip(pool + meta, before):
+        for a, b in list(zip(src, dst))[:6 if counted else 7]:
+            if 0 <= a < n and 0 <= b < n:
+                x[:, b] = x[:, a]
+        assert torch.equal(got.view(torch.int16) if got.dtype == F16 else got,
+                           x.view(torch.int16) if x.dtype == F16 else x)
+
+
+# ---- products ------------------------------------------------------------------------------------
+
+def weights(seed, n_out, n_in):
+    return ref.quantise(randn(seed, n_out, n_in, std=n_in ** -0.5))
+
+
+def rounded(bound, y, dt):
+    return bound + (2.0 ** -8 if dt == BF else 2.0 ** -24) * (y.abs() + bound)
+
+
+SHAPES = [(1, 64, 1), (1, 64, 16), (2, 128, 33), (3, 192, 100), (16, 576, 40), (17, 1024, 65),
+          (33, 320, 48), (64, 2048, 17), (70, 128, 130), (1, 3584, 257), (5, 27648, 24)]
+
+
+@pytest.mark.parametrize("rows,n_in,n_out", SHAPES)
+@pytest.mark.parametrize("xt,yt", [(BF, BF), (BF, F32), (F32, F32), (F32, BF)])
+def test_w4_store(rows, n_in, n_out, xt, yt):
+    """x's and y's rows lie apart; what is between y's rows stays as it was."""
+    codes, meta = weights(rows, n_out, n_in)
+    x = randn(rows + 1, rows, n_in + 24, dt=xt)[:, 8:n_in + 8]
+    y = torch.full((rows, n_out + 5), 7.0, dtype=yt, device=DEV)
+    xd = torch.empty((rows, n_in + 24), dtype=xt, device=DEV)[:, 8:n_in + 8]
+    xd.copy_(x)
+    ws = w4_ws(rows, n_out, n_in)
+    akvs.akvs_w4_product(xd, codes.to(DEV), meta.to(DEV), y[:, :n_out], ws=ws)
+    want, tol = ref.product(x, codes, meta)
+    err = (y[:, :n_out].double().cpu() - want).abs()
+    assert bool((err <= rounded(tol, want, yt)).all()), float((err / rounded(tol, want, yt)).max())
+    assert bool((y[:, n_out:] == 7).all())
+
+
+def w4_ws(rows, n_out, n_in):
+    n = akvs.akvs_w4_workspace_size(rows, n_out, n_in)
+    return torch.full((n,), 255, dtype=U8, device=DEV) if n else None
+
+
+@pytest.mark.parametrize("rows,n_in,n_out", SHAPES)
+@pytest.mark.parametrize("in_place", [False, True])
+def test_w4_residual(rows, n_in, n_out, in_place):
+    codes, meta = weights(rows, n_out, n_in)
+    x, h = randn(3, rows, n_in, dt=BF), randn(4, rows, n_out)
+    hd = h.to(DEV)
+    y = hd if in_place else torch.empty_like(hd)
+    akvs.akvs_w4_product(x.to(DEV), codes.to(DEV), meta.to(DEV), y, resid=hd,
+                         ws=w4_ws(rows, n_out, n_in))
+    want, tol = ref.product(x, codes, meta)
+    want = want + h.double()
+    tol = rounded(tol, want, F32)
+    assert bool(((y.double().cpu() - want).abs() <= tol).all())
+    assert in_place or torch.equal(hd.cpu(), h)
+
+
+@pytest.mark.parametrize("rows,n_in,n_out", [(1, 64, 2), (2, 128, 34), (5, 576, 130), (17, 1024, 66),
+                                             (40, 256, 1000), (1, 5120, 258)])
+@pytest.mark.parametrize("xt,yt", [(BF, BF), (F32, F32)])
+def test_w4_swiglu(rows, n_in, n_out, xt, yt):
+    """silu(g) u: its derivatives are at most 1.1 |u| and |silu(g)|; exponential and reciprocal are
+    off by a few 2^-23."""
+    codes, meta = weights(7, n_out, n_in)
+    x = randn(8, rows, n_in, dt=xt, std=2.0)
+    y = torch.full((rows, n_out // 2), 7.0, dtype=yt, device=DEV)
+    akvs.akvs_w4_product(x.to(DEV), codes.to(DEV), meta.to(DEV), y, akvs.AKVS_W4_SWIGLU,
+                         ws=w4_ws(rows, n_out, n_in))
+    z, tol = ref.product(x, codes, meta)
+    g, u = z.chunk(2, 1)
+    tg, tu = tol.chunk(2, 1)
+    s = g * torch.sigmoid(g)
+    want = s * u
+    tol = 1.1 * tg * (u.abs() + tu) + tu * s.abs() + 2.0 ** -20 * (1 + g.abs()) * want.abs()
+    assert bool(((y.double().cpu() - want).abs() <= rounded(tol, want, yt)).all())
+
+
+def test_w4_extreme_inputs():
+    """A row that is not a number leaves the others alone; huge and tiny rows beside each other."""
+    codes, meta = weights(1, 50, 256)
+    x = randn(2, 5, 256)
+    x[1, 17] = math.nan
+    x[2] *= 1e30
+    x[3] *= 1e-30
+    x[4, 200] = math.inf
+    for dt in (BF, F32):
+        xx = x.to(dt)
+        y = torch.empty(5, 50, device=DEV)
+        akvs.akvs_w4_product(xx.to(DEV), codes.to(DEV), meta.to(DEV), y, ws=w4_ws(5, 50, 256))
+        want, tol = ref.product(xx, codes, meta)
+        for r in (0, 2, 3):
+            assert bool(((y[r].double().cpu() - want[r]).abs() <= rounded(tol, want, F32)[r]).all())
+        assert bool(torch.isnan(y[1]).all()) and not bool(torch.isfinite(y[4]).any())
+
+
+def test_w4_beyond_32_bits():
+    """Weights of more than 2^32 bytes of codes: the last outputs."""
+    n_in, n_out = 64 * 1024, 140000
+    codes = torch.zeros((n_out, n_in // 2), dtype=U8, device=DEV)
+    meta = torch.zeros((n_out, n_in // 64, 2), dtype=F16, device=DEV)
+    assert codes.numel() > 1 << 32
+    c, m = weights(3, 20, n_in)
+    codes[-20:], meta[-20:] = c.to(DEV), m.to(DEV)
+    x = randn(5, 2, n_in, dt=BF)
+    y = torch.empty(2, n_out, device=DEV)
+    akvs.akvs_w4_product(x.to(DEV), codes, meta, y, ws=w4_ws(2, n_out, n_in))
+    want, tol = ref.product(x, c, m)
+    assert bool(((y[:, -20:].double().cpu() - want).abs() <= rounded(tol, want, F32)).all())
+    assert bool((y[:, :-20] == 0).all())
+
+
+# ---- streams and graphs --------------------------------------------------------------------------
+
+def test_another_stream_and_graphs_that_share_a_workspace():
+    """The calls of a decoding step on a stream of its own, captured twice over one workspace (the
+    graphs run one after the other) and replayed with eager work between: the same bits."""
+    geom = (28, 4, 128)
+    b = Batch(geom, 16, [700, 90, 300], [1, 1, 1], seed=43)
+    b.upload()
+    c, qd = b.cfg(True), b.q.to(DEV)
+    ws = b.ws(c)
+    k, v = (randn(i, 3, 4, 128, dt=BF).to(DEV) for i in (1, 2))
+    codes, meta = (x.to(DEV) for x in weights(2, 64, 28 * 128))
+    y = torch.empty(3, 64, device=DEV)
+
+    def step():
+        akvs.akvs_store_pages(k, v, c, b.p, b.m)
+        akvs.akvs_paged_attention(qd, c, b.p, b.m, b.out, b.lse, ws)
+        akvs.akvs_w4_product(b.out.view(3, -1), codes, meta, y, ws=w4_ws(3, 64, 28 * 128))
+
+    step()
+    torch.cuda.synchronize()
+    want = [x.clone() for x in (b.out, b.lse, y)]
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        b.out.zero_()
+        step()
+    s.synchronize()
+    assert all(torch.equal(a, x) for a, x in zip((b.out, b.lse, y), want))
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            step()
+        graphs.append(g)
+    for i in range(4):
+        b.out.fill_(3)
+        y.fill_(3)
+        graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, x) for a, x in zip((b.out, b.lse, y), want))
+        akvs.akvs_paged_attention(qd, c, b.p, b.m, b.out, b.lse, ws)
+        torch.cuda.synchronize()
+
+
+def test_page_calls_captured():
+    """A branching step of the pages in a graph: every replay as the rules say."""
+    p = Pool(*random_tables(5, 40, 16, 12, 400), 16)
+    live = [s for s in range(40) if p.want.len[s]][:5]
+    new = [s for s in range(40) if not p.want.len[s]][:5]
+    src, dst, add = ints(live), ints(new), ints([3, 20, 0, 16, 1])
+    a = [torch.empty(5, dtype=torch.int32, device=DEV) for _ in range(3)]
+    counts, ws = torch.empty(2, dtype=torch.int32, device=DEV), p.ws(5)
+
+    def step():
+        akvs.akvs_free_pages(p.t, dst)
+        akvs.akvs_fork_pages(p.t, src, dst)
+        akvs.akvs_grow_pages(p.t, dst, add, *a, counts, ws)
+
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for _ in range(3):
+        g.replay()
+        p.want.free(new)
+        p.want.fork(live, new)
+        served, moves, want = p.want.grow(new, [3, 20, 0, 16, 1])
+        p.check()
+        assert counts.cpu().tolist() == want and a[0].cpu().tolist() == served
+        src_ = torch.zeros(8, device=DEV).add_(1)  # eager work between the replays
+        torch.cuda.synchronize()
