@@ -510,7 +510,7 @@ __global__ __launch_bounds__(256) void k_shared_merge_wave(SharedBatch s, int sl
 // Many slots: block = one pair. Its threads have a slot's (m, l, f) each, for the maximum, the
 // factors and their sum; then 256 / (hd / 8) teams of hd / 8 threads take the slots in turn, four
 // outputs requested at a time, and are added in order through LDS.
-constexpr int MERGE_SLOTS = 1024;  // the most slots
+static_assert(MERGE_SLOTS % 256 == 0, "a block takes 256 slots at a time");
 template <typename TS, typename TP, int HD>
 __global__ __launch_bounds__(256) void k_shared_merge(SharedBatch s, int slots, int hq,
                                                       const TP *__restrict__ part_o,
@@ -1128,6 +1128,33 @@ size_t shared_part_floats(const SharedBatch &s, int hq, int hkv, int hd, int dty
   return p.slots > 1 ? items * (dtype == AKVS_BF16 ? hd / 2 : hd) + items * 4 : 0;
 }
 
+template <typename TS, typename TP, int HD>
+static hipError_t shared_merge(const SharedBatch &s, int slots, int hq, const TP *po,
+                               const float4 *ml, TS *out, float *lse, hipStream_t st) {
+  const size_t items = (size_t)s.n_rows * hq;
+  const dim3 b(256);
+  if (slots <= MERGE_FEW) {
+    const dim3 gm((unsigned)((items * (HD / 8) + 255) / 256));
+    hipLaunchKernelGGL((k_shared_merge_few<TS, TP>), gm, b, 0, st, s, slots, hq, HD, po, ml, out, lse);
+  } else if (slots <= MERGE_WAVE) {
+    const dim3 gm = merge_grid((items + 3) / 4);
+    hipLaunchKernelGGL((k_shared_merge_wave<TS, TP, HD>), gm, b, 0, st, s, slots, hq, po, ml, out, lse);
+  } else {
+    const dim3 gm = merge_grid(items);
+    hipLaunchKernelGGL((k_shared_merge<TS, TP, HD>), gm, b, 0, st, s, slots, hq, po, ml, out, lse);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_merge_slots(const SharedBatch &s, int slots, int hq, int hd, const void *po,
+                              const void *ml, void *out, float *lse, hipStream_t st) {
+  const _Float16 *o = reinterpret_cast<const _Float16 *>(po);
+  const float4 *m = reinterpret_cast<const float4 *>(ml);
+  bf16_t *O = reinterpret_cast<bf16_t *>(out);
+  return hd == 128 ? shared_merge<bf16_t, _Float16, 128>(s, slots, hq, o, m, O, lse, st)
+                   : shared_merge<bf16_t, _Float16, 64>(s, slots, hq, o, m, O, lse, st);
+}
+
 template <typename TS, int HD>
 static hipError_t shared_attention(const SharedBatch &s, const void *q, const void *kp,
                                    const void *vp, const void *ko, const void *vo, int hq,
@@ -1161,17 +1188,7 @@ static hipError_t shared_attention(const SharedBatch &s, const void *q, const vo
 #undef AKVS_ATTEND
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.slots <= 1) return e;
-  if (p.slots <= MERGE_FEW) {
-    const dim3 gm((unsigned)((items * (HD / 8) + 255) / 256));
-    hipLaunchKernelGGL((k_shared_merge_few<TS, TP>), gm, b, 0, st, s, p.slots, hq, HD, po, ml, O, lse);
-  } else if (p.slots <= MERGE_WAVE) {
-    const dim3 gm = merge_grid((items + 3) / 4);
-    hipLaunchKernelGGL((k_shared_merge_wave<TS, TP, HD>), gm, b, 0, st, s, p.slots, hq, po, ml, O, lse);
-  } else {
-    const dim3 gm = merge_grid(items);
-    hipLaunchKernelGGL((k_shared_merge<TS, TP, HD>), gm, b, 0, st, s, p.slots, hq, po, ml, O, lse);
-  }
-  return hipGetLastError();
+  return shared_merge<TS, TP, HD>(s, p.slots, hq, po, ml, O, lse, st);
 }
 
 hipError_t launch_shared_attention(const SharedBatch &s, const void *q, const void *kp,

@@ -214,6 +214,11 @@ hipError_t launch_shared_attention(const SharedBatch &s, const void *q, const vo
                                    hipStream_t st);
 // floats of `part` (partials of key splits) that launch_shared_attention needs
 size_t shared_part_floats(const SharedBatch &s, int hq, int hkv, int hd, int dtype);
+// bf16 rows from fp16 partials in `slots` key splits (2 .. MERGE_SLOTS), as k_shared_bf16 leaves
+// them: po [slots][n_rows][hq][hd], ml [slots][n_rows][hq] (m, l, f, -); of s the rows alone count.
+constexpr int MERGE_SLOTS = 1024;  // the most slots
+hipError_t launch_merge_slots(const SharedBatch &s, int slots, int hq, int hd, const void *po,
+                              const void *ml, void *out, float *lse, hipStream_t st);
 hipError_t launch_attention_weights(const SharedBatch &s, const void *q, const float *lse,
                                     const void *kp, const void *ko, int hq, int hkv, int hd,
                                     int dtype, const float *wp_prev, float *wp,
