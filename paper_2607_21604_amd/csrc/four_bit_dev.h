@@ -1,0 +1,46 @@
+// Device helpers of the products with 4-bit codes.
+#pragma once
+#include "common.h"
+
+namespace akvs {
+
+typedef __attribute__((ext_vector_type(2))) int i32x2_t;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_t;
+
+// Eight codes as bf16 16 + c, in the order 0, 4, 1, 5, 2, 6, 3, 7.
+__device__ __forceinline__ bf16x8_t codes8(uint32_t w) {
+  const u32x4_t x = {((w << 3) & 0x00780078u) | 0x41804180u, ((w >> 1) & 0x00780078u) | 0x41804180u,
+                     ((w >> 5) & 0x00780078u) | 0x41804180u, ((w >> 9) & 0x00780078u) | 0x41804180u};
+  return __builtin_bit_cast(bf16x8_t, x);
+}
+// Eight bf16 in that order.
+__device__ __forceinline__ bf16x8_t order8(u32x4_t q) {
+  const u32x4_t x = {(q[0] & 0xffffu) | (q[2] << 16), (q[0] >> 16) | (q[2] & 0xffff0000u),
+                     (q[1] & 0xffffu) | (q[3] << 16), (q[1] >> 16) | (q[3] & 0xffff0000u)};
+  return __builtin_bit_cast(bf16x8_t, x);
+}
+__device__ __forceinline__ float scale_of(uint32_t m) {
+  return (float)__builtin_bit_cast(f16x2_t, m)[0];
+}
+__device__ __forceinline__ float zero_of(uint32_t m) {
+  return (float)__builtin_bit_cast(f16x2_t, m)[1];
+}
+
+// The upper half of the wave's a against the lower half of its b.
+__device__ __forceinline__ void swap_halves(uint32_t &a, uint32_t &b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  a = r[0];
+  b = r[1];
+}
+// o[j]: what lane l % 16 of the wave's j-th 16 lanes has, in all lanes.
+__device__ __forceinline__ void spread4(uint32_t v, uint32_t (&o)[4]) {
+  const auto h = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  const auto a = __builtin_amdgcn_permlane16_swap(h[0], h[0], false, false);
+  const auto b = __builtin_amdgcn_permlane16_swap(h[1], h[1], false, false);
+  o[0] = a[0];
+  o[1] = a[1];
+  o[2] = b[0];
+  o[3] = b[1];
+}
+
+}  // namespace akvs

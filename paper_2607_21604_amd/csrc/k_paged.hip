@@ -12,6 +12,7 @@
 #include <cmath>
 #include <type_traits>
 
+#include "four_bit_dev.h"
 #include "kernels.h"
 #include "pages_dev.h"
 
@@ -22,28 +23,6 @@ struct PagedPlan {
   int tiles, chunks, chunk_keys;
 };
 constexpr int PG_TILE = 64;  // keys a wave takes at a time
-
-typedef __attribute__((ext_vector_type(2))) int i32x2_t;
-typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_t;
-
-// Eight codes as bf16 16 + c, in the order 0, 4, 1, 5, 2, 6, 3, 7.
-__device__ __forceinline__ bf16x8_t codes8(uint32_t w) {
-  const u32x4_t x = {((w << 3) & 0x00780078u) | 0x41804180u, ((w >> 1) & 0x00780078u) | 0x41804180u,
-                     ((w >> 5) & 0x00780078u) | 0x41804180u, ((w >> 9) & 0x00780078u) | 0x41804180u};
-  return __builtin_bit_cast(bf16x8_t, x);
-}
-// Eight bf16 in that order.
-__device__ __forceinline__ bf16x8_t order8(u32x4_t q) {
-  const u32x4_t x = {(q[0] & 0xffffu) | (q[2] << 16), (q[0] >> 16) | (q[2] & 0xffff0000u),
-                     (q[1] & 0xffffu) | (q[3] << 16), (q[1] >> 16) | (q[3] & 0xffff0000u)};
-  return __builtin_bit_cast(bf16x8_t, x);
-}
-__device__ __forceinline__ float scale_of(uint32_t m) {
-  return (float)__builtin_bit_cast(f16x2_t, m)[0];
-}
-__device__ __forceinline__ float zero_of(uint32_t m) {
-  return (float)__builtin_bit_cast(f16x2_t, m)[1];
-}
 
 // Block = 4 waves over NP tiles of 16 pairs and one chunk of keys; its waves take the chunk's
 // tiles of 64 keys in turn, each with its own maximum, sum and output, merged through LDS at the
