@@ -26,6 +26,33 @@ __device__ __forceinline__ float zero_of(uint32_t m) {
   return (float)__builtin_bit_cast(f16x2_t, m)[1];
 }
 
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
+// scale * code + zero of eight codes in fp16, rounded once: 1024 + c and 1024 + 16 c are fp16 numbers
+// whose low bits are the nibble, c itself is exact. In the order 0, 4, 1, 5, 2, 6, 3, 7.
+__device__ __forceinline__ f16x8_t values8(uint32_t w, f16x2_t scale, f16x2_t zero) {
+  const f16x2_t down = {(_Float16)-1024.f, (_Float16)-1024.f};
+  const f16x2_t part = {(_Float16)0.0625f, (_Float16)0.0625f};
+  const f16x2_t off = {(_Float16)-64.f, (_Float16)-64.f};
+  union {
+    f16x2_t h[4];
+    f16x8_t v;
+  } x;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t u = w >> (8 * i);
+    const f16x2_t lo = __builtin_bit_cast(f16x2_t, (u & 0x000f000fu) | 0x64006400u) + down;
+    const f16x2_t hi = __builtin_elementwise_fma(
+        __builtin_bit_cast(f16x2_t, (u & 0x00f000f0u) | 0x64006400u), part, off);
+    x.h[2 * i] = __builtin_elementwise_fma(lo, scale, zero);
+    x.h[2 * i + 1] = __builtin_elementwise_fma(hi, scale, zero);
+  }
+  return x.v;
+}
+// Elements of that order in their own.
+__device__ __forceinline__ f16x8_t unorder8(f16x8_t x) {
+  return __builtin_shufflevector(x, x, 0, 2, 4, 6, 1, 3, 5, 7);
+}
+
 // The upper half of the wave's a against the lower half of its b.
 __device__ __forceinline__ void swap_halves(uint32_t &a, uint32_t &b) {
   const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);

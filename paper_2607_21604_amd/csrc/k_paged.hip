@@ -20,7 +20,8 @@ namespace akvs {
 
 // Work items of a call: (request, chunk of its keys, pair tile, KV head), KV heads innermost.
 struct PagedPlan {
-  int tiles, chunks, chunk_keys;
+  int pairs, tiles, chunks, chunk_keys;  // pairs: of a tile
+  bool many;                             // k_paged_many's
 };
 constexpr int PG_TILE = 64;  // keys a wave takes at a time
 
@@ -400,7 +401,6 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(PagedBatch s, PagePool p, 
       const int e = max(__builtin_amdgcn_frexp_expf(big), -100) - 15;
       const float down = ldexpf(1.f, -e);
       const size_t prow = (size_t)chunk * s.n_rows * hq + row;
-      typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
       f16x8_t x;
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] = (_Float16)(a[j] * down);
@@ -418,16 +418,330 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(PagedBatch s, PagePool p, 
   }
 }
 
-static int pair_tiles(const PagedBatch &s, int G, int *np) {
-  const long long pairs = (long long)s.rows_max * G;
-  *np = pairs > 16 ? 2 : 1;
-  return (int)((pairs + 16 * *np - 1) / (16 * *np));
+// Many pairs. Block = 4 waves over 32 * groups pairs (groups 1, 2 or 4) and one chunk of keys. Tiles
+// of 64 keys are turned into fp16 values (rounded once; no key or value of the format lies outside
+// its range) in LDS, from codes loaded two tiles ahead; a wave takes 32 pairs and 32 or 64 of the
+// tile's keys: with 4 groups each wave has a group, with 2 two waves share a group's keys, with
+// 1 two of the waves only load. Scores are formed transposed, S^T = K Q^T (MFMA 32x32x16): lane l
+// holds 16 scores of pair l % 32, the operand layout of O^T = V^T P^T; V^T comes from row-major
+// rows by the transposing LDS read. Queries are fp16 scaled by a power of two per pair, the
+// probabilities fp16 times 2^7, so that what is lost below fp16's smallest is 2^-32 of the
+// largest; statistics and outputs are fp32.
+template <int HD>
+__global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p, PagedPlan plan,
+                                                       const bf16_t *__restrict__ Q, int hq,
+                                                       int hkv, float scale_log2,
+                                                       bf16_t *__restrict__ out,
+                                                       float *__restrict__ lse,
+                                                       _Float16 *__restrict__ part_o,
+                                                       float4 *__restrict__ part_ml) {
+  constexpr int KS = HD / 16, DB = HD / 32, NG = HD / 64, RB = HD / 2;
+  constexpr int WORDS = HD / 32;                   // of codes per thread: 4 threads a row
+  constexpr int KST = HD + 8, VST = HD + 32;       // row strides: fragment reads on all banks
+  constexpr int KB = PG_TILE * KST, VB = PG_TILE * VST;
+  constexpr float P_BITS = 7.f;
+  __shared__ __attribute__((aligned(16))) _Float16 s_kv[2 * (KB + VB)];
+  __shared__ int s_odd;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hi = lane >> 5;
+  const int G = hq / hkv;
+  int id = blockIdx.x;
+  const int h = id % hkv;
+  id /= hkv;
+  const int tile = id % plan.tiles;
+  id /= plan.tiles;
+  const int chunk = id % plan.chunks, b = id / plan.chunks;
+  int r0, r1, len;
+  paged_rows(s, b, r0, r1);
+  const int32_t *table = paged_keys(s, b, len);
+  const int n_pairs = (r1 - r0) * G, v0 = tile * plan.pairs;
+  if (v0 >= n_pairs) return;
+  auto seen_by = [&](int r) { return max(len - r1 + r + 1, 0); };
+  // this wave's pairs and its share of a tile's two 32-key halves
+  const int groups = plan.pairs >> 5;
+  const int group = groups == 4 ? wave : groups == 2 ? wave >> 1 : 0;
+  const bool works = groups > 1 || wave < 2;
+  const int st0 = groups == 4 ? 0 : wave & 1, st_step = groups == 4 ? 1 : 2;
+  const int last = min(n_pairs, v0 + plan.pairs) - 1;
+  const int v = v0 + group * 32 + (lane & 31);
+  const bool valid = v <= last;
+  const int r = r0 + (valid ? v : v0) / G, head = h * G + (valid ? v : v0) % G;
+  const int k0 = chunk * plan.chunk_keys;
+  const int k1 = min(k0 + plan.chunk_keys, seen_by(r0 + last / G));
+  const int all_see = seen_by(r0 + v0 / G), seen = valid ? min(seen_by(r), k1) : 0;
+  const size_t prow = ((size_t)chunk * s.n_rows + r) * hq + head;
+  const int nkt = k1 > k0 ? (k1 - k0 + PG_TILE - 1) / PG_TILE : 0;
+  const bool writes = valid && (groups == 4 || (works && (wave & 1) == 0));
+  if (nkt == 0 && plan.chunks > 1) {
+    if (writes && hi == 0) part_ml[prow] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+    return;
+  }
+
+  // the pair's query, its largest element brought to [2^14, 2^15)
+  f16x8_t qf[KS];
+  float q_scale = scale_log2;
+  {
+    const bf16_t *q = Q + ((size_t)r * hq + head) * HD + hi * 8;
+    float x[KS][8], big = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      load8(q + ks * 16, x[ks]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) big = fmaxf(big, fabsf(x[ks][i]));
+    }
+    big = fmaxf(big, __shfl_xor(big, 32, 64));
+    int e = 0;
+    if (big > 0.f && big < INFINITY) e = max(__builtin_amdgcn_frexp_expf(big), -100) - 15;
+    const float down = ldexpf(1.f, -e);
+    q_scale *= ldexpf(1.f, e);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)  // (in the order of values8, as the keys are)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) qf[ks][i] = (_Float16)(x[ks][(i & 1) * 4 + i / 2] * down);
+  }
+  f32x16_t o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;  // (l_run: of this lane's half of the keys)
+
+  // A thread has a quarter of a row's codes, keys and values.
+  const int krow = tid >> 2, kq = tid & 3;
+  typedef __attribute__((ext_vector_type(WORDS))) uint32_t words_t;
+  struct Codes {
+    words_t k, v;
+    uint32_t km, vm;
+  };
+  const int last_page = (max(k1, 1) - 1) >> p.shift, mask = (1 << p.shift) - 1;
+  auto page_at = [&](int key0) { return table[min((key0 + krow) >> p.shift, last_page)]; };
+  auto load = [&](Codes &c, int key0, int page) __attribute__((always_inline)) {
+    const bool there = page >= 0 && page < p.n_pages, live = there && key0 + krow < k1;
+    const size_t row =
+        (((size_t)(there ? page : 0) * hkv + h) << p.shift) + ((key0 + krow) & mask);
+    c.k = *reinterpret_cast<const words_t *>(p.k + row * RB + kq * (RB / 4));
+    c.v = *reinterpret_cast<const words_t *>(p.v + row * RB + kq * (RB / 4));
+    const uint32_t km = p.k_meta[row * NG + kq * NG / 4], vm = p.v_meta[row * NG + kq * NG / 4];
+    c.km = live ? km : 0u;
+    c.vm = live ? vm : 0u;
+  };
+  // Values that some pair of the tile must not see take part with probability 0, and 0 * inf is
+  // NaN: where such a value is not finite, 0 goes to LDS, and the pairs that do see it get it
+  // added at the end. Pieces of the values are written in an order that differs by row, so that
+  // rows four apart in a bank do not meet.
+  auto store = [&](Codes &c, int key0, int buf) __attribute__((always_inline)) {
+    _Float16 *ks = s_kv + buf * (KB + VB) + krow * KST + kq * (HD / 4), *vs = s_kv + buf * (KB + VB) + KB + krow * VST + kq * (HD / 4);
+    if (key0 + PG_TILE > all_see && key0 + krow >= all_see) {
+      if ((c.vm & 0x7c00u) == 0x7c00u || (c.vm & 0x7c000000u) == 0x7c000000u) {
+        s_odd = 1;
+        c.vm = 0;
+      }
+    }
+    f16x2_t m = __builtin_bit_cast(f16x2_t, c.km);
+    f16x2_t sc = {m[0], m[0]}, z = {m[1], m[1]};
+#pragma unroll
+    for (int j = 0; j < WORDS; ++j)
+      *reinterpret_cast<f16x8_t *>(ks + j * 8) = values8(c.k[j], sc, z);
+    m = __builtin_bit_cast(f16x2_t, c.vm);
+    sc = (f16x2_t){m[0], m[0]};
+    z = (f16x2_t){m[1], m[1]};
+    words_t w = c.v;
+    const int turn = krow & (WORDS - 1);
+#pragma unroll
+    for (int bit = 1; bit < WORDS; bit <<= 1) {
+      words_t u;
+#pragma unroll
+      for (int j = 0; j < WORDS; ++j) u[j] = turn & bit ? w[(j + bit) & (WORDS - 1)] : w[j];
+      w = u;
+    }
+#pragma unroll
+    for (int j = 0; j < WORDS; ++j)
+      *reinterpret_cast<f16x8_t *>(vs + ((j + turn) & (WORDS - 1)) * 8) =
+          unorder8(values8(w[j], sc, z));
+  };
+  if (tid == 0) s_odd = 0;
+  Codes c;
+  int page = 0;
+  if (nkt) {
+    load(c, k0, page_at(k0));
+    page = page_at(k0 + PG_TILE);
+  }
+  __syncthreads();
+  if (nkt) {
+    store(c, k0, 0);
+    load(c, k0 + PG_TILE, page);  // (past the end: its last page again)
+    page = page_at(k0 + 2 * PG_TILE);
+  }
+  __syncthreads();
+  for (int kt = 0; kt < nkt; ++kt) {
+    const int key0 = k0 + kt * PG_TILE;
+    const _Float16 *ks_ = s_kv + (kt & 1) * (KB + VB), *vs_ = ks_ + KB;
+    for (int st = works ? st0 : 2; st < 2; st += st_step) {
+      const int sk0 = key0 + st * 32;
+      if (sk0 >= k1) break;
+      // S^T block: score i is key sk0 + (i / 4) * 8 + hi * 4 + i % 4 of this lane's pair
+      f32x16_t sc;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+      const _Float16 *kr = ks_ + (st * 32 + (lane & 31)) * KST + hi * 8;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+            *reinterpret_cast<const f16x8_t *>(kr + ks * 16), qf[ks], sc, 0, 0, 0);
+      // V^T operand of step t, dims db * 32 + lane % 32: its 8 slots are keys 16 t + 4 hi + 0..3
+      // and the same + 8 of the block
+      f16x8_t vf[2][DB];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          typedef short v4s __attribute__((ext_vector_type(4)));
+          const _Float16 *vb = vs_ + (st * 32 + 16 * t + 4 * hi + ((lane & 15) >> 2)) * VST +
+                               db * 32 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+          const v4s x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) v4s *)(vb));
+          const v4s x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) v4s *)(vb + 8 * VST));
+          __builtin_memcpy(&vf[t][db], &x0, 8);
+          __builtin_memcpy(reinterpret_cast<char *>(&vf[t][db]) + 8, &x1, 8);
+        }
+      if (sk0 + 32 > min(all_see, k1)) {
+        const int lim = seen - (sk0 + hi * 4);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if ((i >> 2) * 8 + (i & 3) >= lim) sc[i] = -INFINITY;
+      }
+      float mx = sc[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[i]);
+      // the running maximum rises only when some score exceeds it by more than 2^8
+      if (__ballot(mx * q_scale > m_run + 8.f)) {
+        const float mp = fmaxf(mx, __shfl_xor(mx, 32, 64)) * q_scale;
+        const float m_new = fmaxf(m_run, mp);
+        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[db] *= alpha;
+        l_run *= alpha;
+        m_run = m_new;
+      }
+      const float m_off = (m_run == -INFINITY ? 0.f : m_run) - P_BITS;  // (no key yet: every p is 0)
+      float pv[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        pv[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], q_scale, -m_off));
+        l_run += pv[i];
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        f16x8_t pb;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) pb[j] = (_Float16)pv[8 * t + j];
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[t][db], pb, o[db], 0, 0, 0);
+      }
+    }
+    if (kt + 1 < nkt) {
+      store(c, key0 + PG_TILE, (kt + 1) & 1);
+      load(c, key0 + 2 * PG_TILE, page);
+      page = page_at(key0 + 3 * PG_TILE);
+    }
+    __syncthreads();
+  }
+  float l = l_run + __shfl_xor(l_run, 32, 64);
+  if (groups < 4) {  // the two waves of a group: the odd one hands over through LDS
+    float *x = reinterpret_cast<float *>(s_kv) + group * (HD / 2 + 2) * 64 + lane;
+    if (works && (wave & 1)) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[(db * 16 + i) * 64] = o[db][i];
+      x[HD / 2 * 64] = m_run;
+      x[(HD / 2 + 1) * 64] = l;
+    }
+    __syncthreads();
+    if (!works || (wave & 1)) return;
+    const float m2 = x[HD / 2 * 64], l2 = x[(HD / 2 + 1) * 64];
+    const float mm = fmaxf(m_run, m2), off = mm == -INFINITY ? 0.f : mm;
+    // a half without a key has m = -inf, l = 0 and o = 0; one of NaN scores l = NaN
+    const float fa = __builtin_amdgcn_exp2f(m_run - off), fb = __builtin_amdgcn_exp2f(m2 - off);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[db][i] = fa * o[db][i] + fb * x[(db * 16 + i) * 64];
+    l = fa * l + fb * l2;
+    m_run = mm;
+  }
+  if (!valid) return;
+  if (s_odd) {  // values left out above that this pair sees
+    for (int k = max(k0, all_see); k < seen; ++k) {
+      const int pg = table[k >> p.shift];
+      if (pg < 0 || pg >= p.n_pages) continue;
+      const size_t row = (((size_t)pg * hkv + h) << p.shift) + (k & mask);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const uint32_t mt = p.v_meta[row * NG + db / 2];
+        const float sv = scale_of(mt), zv = zero_of(mt);
+        if (fabsf(sv) < INFINITY && fabsf(zv) < INFINITY) continue;
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const uint32_t w = *reinterpret_cast<const uint16_t *>(p.v + row * RB + db * 16 + q4 * 4 + hi * 2);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            o[db][4 * q4 + j] += fmaf(sv, (float)((w >> (4 * j)) & 15u), zv);
+        }
+      }
+    }
+  }
+  // o[db][i] is dim db * 32 + (i / 4) * 8 + hi * 4 + i % 4 of the pair
+  if (plan.chunks > 1) {
+    float big = 0.f;  // the pair's largest finite value
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float x = fabsf(o[db][i]);
+        big = x < INFINITY ? fmaxf(big, x) : big;
+      }
+    big = fmaxf(big, __shfl_xor(big, 32, 64));
+    const int e = max(__builtin_amdgcn_frexp_expf(big), -100) - 15;
+    const float down = ldexpf(1.f, -e);
+    _Float16 *po = part_o + prow * HD + hi * 4;
+    typedef _Float16 f16x4_t __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        f16x4_t x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = (_Float16)(o[db][4 * q4 + j] * down);
+        *reinterpret_cast<f16x4_t *>(po + db * 32 + q4 * 8) = x;
+      }
+    if (hi == 0)
+      part_ml[prow] = make_float4(m_run - P_BITS, l, ldexpf(1.f, e), 0.f);
+    return;
+  }
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  bf16_t *orow = out + ((size_t)r * hq + head) * HD + hi * 4;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4)
+      store4(orow + db * 32 + q4 * 8, o[db][4 * q4] * inv, o[db][4 * q4 + 1] * inv,
+             o[db][4 * q4 + 2] * inv, o[db][4 * q4 + 3] * inv);
+  if (lse && hi == 0)
+    lse[(size_t)r * hq + head] =
+        l == 0.f ? -INFINITY
+                 : ((m_run == -INFINITY ? 0.f : m_run) - P_BITS) * 0.6931471805599453f + logf(l);
 }
 
+// Pairs of a request and KV head: up to 16 or 32, one or two tiles of k_paged_few; more, the
+// tiles of k_paged_many.
 static PagedPlan paged_plan(const PagedBatch &s, int hq, int hkv) {
   PagedPlan p;
-  int np;
-  p.tiles = pair_tiles(s, hq / hkv, &np);
+  const long long pairs = (long long)s.rows_max * (hq / hkv);
+  p.pairs = pairs <= 16 ? 16 : pairs <= 32 ? 32 : pairs <= 64 ? 64 : 128;
+  p.many = pairs > 32;
+  p.tiles = (int)((pairs + p.pairs - 1) / p.pairs);
   const long long items = (long long)s.n_req * p.tiles * hkv;
   const int kt = (s.limit + PG_TILE - 1) / PG_TILE;
   // chunks of whole rounds of the block's waves
@@ -451,21 +765,22 @@ hipError_t launch_paged_attention(const PagedBatch &s, const PagePool &p, const 
                                   hipStream_t st) {
   if (s.n_rows == 0) return hipSuccess;
   const PagedPlan plan = paged_plan(s, hq, hkv);
-  int np;
-  pair_tiles(s, hq / hkv, &np);
   const dim3 g((unsigned)((size_t)s.n_req * plan.chunks * plan.tiles * hkv)), b(256);
   const float scale = 1.4426950408889634f / sqrtf((float)hd);
   const bf16_t *Q = reinterpret_cast<const bf16_t *>(q);
   bf16_t *O = reinterpret_cast<bf16_t *>(out);
   float4 *ml = reinterpret_cast<float4 *>(part);  // (m, l, f) of every slot, then the outputs
   _Float16 *po = reinterpret_cast<_Float16 *>(ml + (size_t)plan.chunks * s.n_rows * hq);
-#define AKVS_PAGED(HD_, NP_)                                                                      \
-  hipLaunchKernelGGL((k_paged_few<HD_, NP_>), g, b, 0, st, s, p, plan, Q, hq, hkv, scale, O, lse, \
-                     po, ml)
+#define AKVS_PAGED(...)                                                                          \
+  hipLaunchKernelGGL((__VA_ARGS__), g, b, 0, st, s, p, plan, Q, hq, hkv, scale, O, lse, po, ml)
   if (hd == 128) {
-    if (np == 2) AKVS_PAGED(128, 2); else AKVS_PAGED(128, 1);
+    if (plan.many) AKVS_PAGED(k_paged_many<128>);
+    else if (plan.pairs == 32) AKVS_PAGED(k_paged_few<128, 2>);
+    else AKVS_PAGED(k_paged_few<128, 1>);
   } else {
-    if (np == 2) AKVS_PAGED(64, 2); else AKVS_PAGED(64, 1);
+    if (plan.many) AKVS_PAGED(k_paged_many<64>);
+    else if (plan.pairs == 32) AKVS_PAGED(k_paged_few<64, 2>);
+    else AKVS_PAGED(k_paged_few<64, 1>);
   }
 #undef AKVS_PAGED
   const hipError_t e = hipGetLastError();
