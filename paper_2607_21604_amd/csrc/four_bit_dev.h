@@ -7,10 +7,24 @@ namespace akvs {
 typedef __attribute__((ext_vector_type(2))) int i32x2_t;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_t;
 
-// Eight codes as bf16 16 + c, in the order 0, 4, 1, 5, 2, 6, 3, 7.
-__device__ __forceinline__ bf16x8_t codes8(uint32_t w) {
-  const u32x4_t x = {((w << 3) & 0x00780078u) | 0x41804180u, ((w >> 1) & 0x00780078u) | 0x41804180u,
-                     ((w >> 5) & 0x00780078u) | 0x41804180u, ((w >> 9) & 0x00780078u) | 0x41804180u};
+// (w & mask) | bits in one instruction. It takes one operand from a scalar register, and no constant:
+// written with constants the compiler makes two of it (the other constant in a vector register for
+// good is what this costs).
+struct CodeBits {
+  uint32_t mask, bits;
+};
+__device__ __forceinline__ CodeBits code_bits(uint32_t mask, uint32_t bits) {
+  CodeBits x;
+  asm("s_mov_b32 %0, %1" : "=s"(x.mask) : "i"(mask));
+  asm("v_mov_b32 %0, %1" : "=v"(x.bits) : "i"(bits));
+  return x;
+}
+__device__ __forceinline__ uint32_t and_or(uint32_t w, CodeBits c) { return (w & c.mask) | c.bits; }
+
+// Eight codes as bf16 16 + c, in the order 0, 4, 1, 5, 2, 6, 3, 7; c: bf16_bits().
+__device__ __forceinline__ CodeBits bf16_bits() { return code_bits(0x00780078u, 0x41804180u); }
+__device__ __forceinline__ bf16x8_t codes8(uint32_t w, CodeBits c) {
+  const u32x4_t x = {and_or(w << 3, c), and_or(w >> 1, c), and_or(w >> 5, c), and_or(w >> 9, c)};
   return __builtin_bit_cast(bf16x8_t, x);
 }
 // Eight bf16 in that order.
@@ -29,7 +43,15 @@ __device__ __forceinline__ float zero_of(uint32_t m) {
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
 // scale * code + zero of eight codes in fp16, rounded once: 1024 + c and 1024 + 16 c are fp16 numbers
 // whose low bits are the nibble, c itself is exact. In the order 0, 4, 1, 5, 2, 6, 3, 7.
-__device__ __forceinline__ f16x8_t values8(uint32_t w, f16x2_t scale, f16x2_t zero) {
+struct F16Bits {
+  CodeBits lo, hi;
+};
+__device__ __forceinline__ F16Bits f16_bits() {
+  F16Bits x{code_bits(0x000f000fu, 0x64006400u), code_bits(0x00f000f0u, 0x64006400u)};
+  x.hi.bits = x.lo.bits;
+  return x;
+}
+__device__ __forceinline__ f16x8_t values8(uint32_t w, f16x2_t scale, f16x2_t zero, F16Bits b) {
   const f16x2_t down = {(_Float16)-1024.f, (_Float16)-1024.f};
   const f16x2_t part = {(_Float16)0.0625f, (_Float16)0.0625f};
   const f16x2_t off = {(_Float16)-64.f, (_Float16)-64.f};
@@ -40,9 +62,9 @@ __device__ __forceinline__ f16x8_t values8(uint32_t w, f16x2_t scale, f16x2_t ze
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const uint32_t u = w >> (8 * i);
-    const f16x2_t lo = __builtin_bit_cast(f16x2_t, (u & 0x000f000fu) | 0x64006400u) + down;
+    const f16x2_t lo = __builtin_bit_cast(f16x2_t, and_or(u, b.lo)) + down;
     const f16x2_t hi = __builtin_elementwise_fma(
-        __builtin_bit_cast(f16x2_t, (u & 0x00f000f0u) | 0x64006400u), part, off);
+        __builtin_bit_cast(f16x2_t, and_or(u, b.hi)), part, off);
     x.h[2 * i] = __builtin_elementwise_fma(lo, scale, zero);
     x.h[2 * i + 1] = __builtin_elementwise_fma(hi, scale, zero);
   }

@@ -25,36 +25,41 @@ struct PagedPlan {
 };
 constexpr int PG_TILE = 64;  // keys a wave takes at a time
 
-// Block = 4 waves over NP tiles of 16 pairs and one chunk of keys; its waves take the chunk's
-// tiles of 64 keys in turn, each with its own maximum, sum and output, merged through LDS at the
-// end, so that the loop has no barrier. MFMA 16x16x32, lane l: g = l / 16.
-//   Scores, S^T = K Q^T: row r of key tile T stands for key 16 (r / 4) + 4 T + r % 4, so that lane
-//   l holds the scores of pair l % 16 at keys 16 g .. 16 g + 15; its reduction takes elements
-//   64 group + 16 g + 8 step .. + 7.
-//   Outputs, O^T = V^T P^T: the lane's keys are its part of the reduction; V^T comes from rows in
-//   LDS by the transposing read of 4-bit elements, 16 keys of a dim at once.
-// Loads of the next tile, and its pages' numbers a tile earlier, are in flight meanwhile; 16
-// consecutive keys lie in one page.
-template <int HD, int NP>
-__global__ __launch_bounds__(256, 2) void k_paged_few(PagedBatch s, PagePool p, PagedPlan plan,
-                                                      const bf16_t *__restrict__ Q, int hq, int hkv,
-                                                      float scale_log2, bf16_t *__restrict__ out,
-                                                      float *__restrict__ lse,
-                                                      _Float16 *__restrict__ part_o,
-                                                      float4 *__restrict__ part_ml) {
+// Few pairs. Block = 4 waves over NP tiles of 16 pairs, or one of 16 / NB, and one chunk of keys; its
+// waves take the chunk's tiles of 64 keys in turn, each with its own maximum, sum and output, merged
+// through LDS at the end, so that the loop has no barrier. MFMA 16x16x32, lane l: g = l / 16.
+//   Scores, S^T = K Q^T, 16 keys T = 0..3 of the tile at a time: the lane holds the scores of column
+//   l % 16 at keys 16 T + 4 g .. + 3; the reduction takes elements 64 group + 16 g + 8 step .. + 7.
+//   Outputs, O^T = V^T P^T: a step's reduction takes 16 keys of two T, V^T comes from rows in LDS by
+//   the transposing read of 4-bit elements, 16 keys of a dim at once.
+// Instructions on scores are what bounds it beside the bytes, so columns are not left empty where
+// few pairs leave room (NB > 1): the columns are NB copies of the pairs, and copy T % NB belongs to
+// the keys of T. Queries are 0 in the others' columns, so that NB products add into one accumulator,
+// and so are a copy's probabilities in the others' places of the reduction.
+// Loads of the next tile, and its pages' numbers (scalar: 16 consecutive keys lie in one page) a
+// tile earlier, are in flight meanwhile.
+template <int HD, int NP, int NB>
+__global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
+    PagedBatch s, PagePool p, PagedPlan plan, const bf16_t *__restrict__ Q, int hq, int hkv,
+    float scale_log2, bf16_t *__restrict__ out, float *__restrict__ lse,
+    _Float16 *__restrict__ part_o, float4 *__restrict__ part_ml) {
+  static_assert(NP == 1 || NB == 1, "copies of one tile");
   constexpr int NG = HD / 64, DB = HD / 16;      // groups of a row, blocks of 16 dims
   constexpr int RB = HD / 2;                     // bytes of a row's codes
   constexpr int VST = RB + 16;                   // row stride in LDS: reads on all banks
-  constexpr int NV = PG_TILE * RB / 1024;        // 16-byte chunks of V per lane
-  constexpr int VKEYS = 1024 / RB;               // keys of one such load of the wave
-  constexpr int MST = 16 * NG * 4 + 16;          // of the meta of 16 keys
+  constexpr int VC = RB / 16;                    // 16-byte chunks of a row
+  constexpr int NV = PG_TILE * RB / 1024;        // of these per lane
+  constexpr int VROWS = 64 / VC;                 // rows that a load of the wave takes
+  constexpr int COLS = 16 / NB, PAIRS = NP * COLS, NS = 16 / NB;  // NS: a lane's scores of a tile
   constexpr int OST = HD + 4;
-  constexpr int STAGE = PG_TILE * VST + 8 * MST; // of a wave
+  constexpr int STAGE = PG_TILE * VST + 2 * NG * PG_TILE * 4;  // of a wave
   constexpr int MERGE = 16 * NP * OST * 4;
   constexpr int WAVE_BYTES = (STAGE > MERGE ? STAGE : MERGE);
   __shared__ __attribute__((aligned(16))) char s_mem[4 * WAVE_BYTES];
   __shared__ float s_m[4][16 * NP], s_l[4][16 * NP];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, lr = lane & 15;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, lr = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int copy = lr / COLS;  // (NB = 1: 0)
   const int G = hq / hkv;
   int id = blockIdx.x;
   const int h = id % hkv;
@@ -65,13 +70,13 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(PagedBatch s, PagePool p, 
   int r0, r1, len;
   paged_rows(s, b, r0, r1);
   const int32_t *table = paged_keys(s, b, len);
-  const int n_pairs = (r1 - r0) * G, v0 = tile * 16 * NP;
+  const int n_pairs = (r1 - r0) * G, v0 = tile * PAIRS;
   if (v0 >= n_pairs) return;
   auto seen_by = [&](int r) { return max(len - r1 + r + 1, 0); };
-  const int last = min(n_pairs, v0 + 16 * NP) - 1;
+  const int last = min(n_pairs, v0 + PAIRS) - 1;
   const int k0 = chunk * plan.chunk_keys;
   const int k1 = min(k0 + plan.chunk_keys, seen_by(r0 + last / G));
-  const int all_see = seen_by(r0 + v0 / G);
+  const int all_see = min(seen_by(r0 + v0 / G), k1);
   const bool split = plan.chunks > 1;
   auto place = [&](int v, int &r, int &head) {
     r = r0 + v / G;
@@ -96,15 +101,15 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(PagedBatch s, PagePool p, 
   }
 
   // queries, and their sums over a group's elements
-  bf16x8_t qf[NP][NG][2];
+  bf16x8_t qf[NP][NB][NG][2];
   float qs[NP][NG];
   int seen[NP];
 #pragma unroll
   for (int np = 0; np < NP; ++np) {
-    const int v = v0 + np * 16 + lr;
+    const int v = v0 + np * 16 + lr % COLS;
     int r, head;
     place(min(v, last), r, head);
-    seen[np] = v <= last ? seen_by(r) : 0;
+    seen[np] = v <= last ? min(seen_by(r), k1) : 0;
     const bf16_t *q = Q + ((size_t)r * hq + head) * HD + g * 16;
 #pragma unroll
     for (int gr = 0; gr < NG; ++gr) {
@@ -115,7 +120,9 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(PagedBatch s, PagePool p, 
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           sum += __uint_as_float(x[i] << 16) + __uint_as_float(x[i] & 0xffff0000u);
-        qf[np][gr][st] = order8(x);
+#pragma unroll
+        for (int c = 0; c < NB; ++c)
+          qf[np][c][gr][st] = order8(NB == 1 || copy == c ? x : (u32x4_t){0, 0, 0, 0});
       }
       sum += __shfl_xor(sum, 16, 64);
       qs[np][gr] = sum + __shfl_xor(sum, 32, 64);
@@ -135,111 +142,147 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(PagedBatch s, PagePool p, 
     m_run[np] = -INFINITY;
     l_run[np] = 0.f;
   }
+  // which half of a word of two bf16 (of two groups, or of two keys) goes to which half of the
+  // reduction's places for two T, and which to none: selectors of v_perm_b32
+  auto selector = [&](int st, int half) {
+    const uint32_t from = half ? 0x0302u : 0x0100u;
+    const int T = copy - 2 * st;  // of this lane's copy (NB = 4); NB = 2: T = copy
+    if (NB == 4 && (T < 0 || T > 1)) return 0x0c0c0c0cu;
+    return (NB == 4 ? T : copy) ? (from << 16) | 0x0c0cu : 0x0c0c0000u | from;
+  };
+  uint32_t sel[2][2];
+#pragma unroll
+  for (int st = 0; st < 2; ++st)
+#pragma unroll
+    for (int half = 0; half < 2; ++half) sel[st][half] = selector(st, half);
 
+  const CodeBits cb = bf16_bits();
   char *mem = s_mem + wave * WAVE_BYTES;
-  char *s_km = mem + PG_TILE * VST, *s_vm = s_km + 4 * MST;
-  const int last_page = (k1 - 1) >> p.shift;
+  uint32_t *s_km = reinterpret_cast<uint32_t *>(mem + PG_TILE * VST), *s_vm = s_km + NG * PG_TILE;
+  const int mask = (1 << p.shift) - 1, last_page = (k1 - 1) >> p.shift;
   struct Tile {
     i32x2_t k[4][NG];
     u32x4_t v[NV];
     uint32_t km[NG], vm[NG];
   };
-  // the page of the 16 keys from key0 + 16 g on, clamped into the sequence
-  auto page_at = [&](int key0) { return table[min((key0 + 16 * g) >> p.shift, last_page)]; };
-  auto load = [&](Tile &t, int key0, int page) __attribute__((always_inline)) {
-    const int mask = (1 << p.shift) - 1;
-    const bool there = page >= 0 && page < p.n_pages;
-    const int at = there ? page : 0;
-    // rows of 16 keys of every group, in rows of the pool's heads
-    const size_t mine = (((size_t)at * hkv + h) << p.shift) + ((key0 + 16 * g) & mask);
-    {
-      const bool live = there && key0 + lane < k1;
-      const uint32_t *km = p.k_meta + (mine + lr) * NG, *vm = p.v_meta + (mine + lr) * NG;
+  // (read through scalar registers: nothing writes the table meanwhile)
+  typedef const __attribute__((address_space(4))) int32_t *entries_t;
+  const entries_t entries = (entries_t)(uintptr_t)table;
+  struct Ids {
+    int page[4];
+  };
+  // the pages of the tile's 16 keys each, clamped into the sequence
+  auto pages_at = [&](int key0) __attribute__((always_inline)) {
+    Ids x;
 #pragma unroll
-      for (int gr = 0; gr < NG; ++gr) {
-        t.km[gr] = live ? km[gr] : 0u;
-        t.vm[gr] = live ? vm[gr] : 0u;
+    for (int T = 0; T < 4; ++T) x.page[T] = entries[min((key0 + 16 * T) >> p.shift, last_page)];
+    return x;
+  };
+  auto load = [&](Tile &t, int key0, const Ids &ids) __attribute__((always_inline)) {
+    size_t row[4];  // of the pool's rows of all heads, where 16 keys begin (uniform)
+    bool there[4];
+#pragma unroll
+    for (int T = 0; T < 4; ++T) {
+      there[T] = ids.page[T] >= 0 && ids.page[T] < p.n_pages;
+      row[T] = (((size_t)(there[T] ? ids.page[T] : 0) * hkv + h) << p.shift) +
+               ((key0 + 16 * T) & mask);
+    }
+#pragma unroll
+    for (int T = 0; T < 4; ++T) {
+      const uint8_t *k = p.k + row[T] * RB;
+#pragma unroll
+      for (int gr = 0; gr < NG; ++gr)
+        t.k[T][gr] = *reinterpret_cast<const i32x2_t *>(k + lr * RB + g * 8 + gr * 32);
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {  // (HD 64: the rows of two T in a load)
+      if (VROWS == 16) {
+        t.v[j] = *reinterpret_cast<const u32x4_t *>(p.v + row[j] * RB + lane * 16);
+      } else {
+        const uint8_t *v = p.v + (lane < 32 ? row[2 * j] : row[2 * j + 1]) * RB;
+        t.v[j] = *reinterpret_cast<const u32x4_t *>(v + (lane & 31) * 16);
       }
     }
-    {
-      const int kg = lr >> 2;
-      const int kp = __shfl(at, kg * 16, 64);
-      const size_t row = (((size_t)kp * hkv + h) << p.shift) + ((key0 + 16 * kg) & mask) + (lr & 3);
-      const uint8_t *k = p.k + row * RB + g * 8;
-#pragma unroll
-      for (int T = 0; T < 4; ++T)
-#pragma unroll
-        for (int gr = 0; gr < NG; ++gr)
-          t.k[T][gr] = *reinterpret_cast<const i32x2_t *>(k + T * 4 * RB + gr * 32);
-    }
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      // keys j VKEYS .. of the tile, lane's at lane / (RB / 16)
-      const int key = j * VKEYS + lane / (RB / 16), vg = key >> 4;
-      const int vp = __shfl(at, vg * 16, 64);
-      const size_t row = (((size_t)vp * hkv + h) << p.shift) + ((key0 + key) & mask);
-      t.v[j] = *reinterpret_cast<const u32x4_t *>(p.v + row * RB + lane % (RB / 16) * 16);
-    }
-  };
-  // values and meta to this wave's LDS (its reads of the tile before are done: in order)
-  auto stash = [&](const Tile &t) __attribute__((always_inline)) {
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-      *reinterpret_cast<u32x4_t *>(mem + (j * VKEYS + lane / (RB / 16)) * VST +
-                                   lane % (RB / 16) * 16) = t.v[j];
+    // meta of key `lane`
+    const size_t a = g & 1 ? row[1] : row[0], c = g & 1 ? row[3] : row[2];
+    const bool ta = g & 1 ? there[1] : there[0], tc = g & 1 ? there[3] : there[2];
+    const size_t mine = ((g & 2 ? c : a) + lr) * NG;
+    const bool live = (g & 2 ? tc : ta) && key0 + lane < k1;
 #pragma unroll
     for (int gr = 0; gr < NG; ++gr) {
-      *reinterpret_cast<uint32_t *>(s_km + g * MST + (gr * 16 + lr) * 4) = t.km[gr];
-      *reinterpret_cast<uint32_t *>(s_vm + g * MST + (gr * 16 + lr) * 4) = t.vm[gr];
+      const uint32_t km = p.k_meta[mine + gr], vm = p.v_meta[mine + gr];
+      t.km[gr] = live ? km : 0u;
+      t.vm[gr] = live ? vm : 0u;
+    }
+  };
+  // Values and meta to this wave's LDS (its reads of the tile before are done: in order). Row 16 g +
+  // 4 T + i of the values is key 16 T + 4 g + i.
+  auto stash = [&](const Tile &t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int key = j * VROWS + lane / VC;
+      const int at = 16 * ((key >> 2) & 3) + 4 * (key >> 4) + (key & 3);
+      *reinterpret_cast<u32x4_t *>(mem + at * VST + lane % VC * 16) = t.v[j];
+    }
+#pragma unroll
+    for (int gr = 0; gr < NG; ++gr) {
+      s_km[gr * PG_TILE + lane] = t.km[gr];
+      s_vm[gr * PG_TILE + lane] = t.vm[gr];
     }
     __builtin_amdgcn_wave_barrier();
   };
   auto attend = [&](const Tile &t, int key0) __attribute__((always_inline)) {
-    float sc[NP][16];
+    float sc[NP][NS];
 #pragma unroll
-    for (int T = 0; T < 4; ++T) {
-      u32x4_t km[NG];  // of keys 16 g + 4 T ..
+    for (int u = 0; u < 4 / NB; ++u) {
+      f32x4_t c[NP][NG];
 #pragma unroll
-      for (int gr = 0; gr < NG; ++gr)
-        km[gr] = *reinterpret_cast<const u32x4_t *>(s_km + g * MST + (gr * 16 + 4 * T) * 4);
-      bf16x8_t kf[NG][2];
-#pragma unroll
-      for (int gr = 0; gr < NG; ++gr)
-#pragma unroll
-        for (int st = 0; st < 2; ++st) kf[gr][st] = codes8((uint32_t)t.k[T][gr][st]);
-#pragma unroll
-      for (int np = 0; np < NP; ++np) {
+      for (int np = 0; np < NP; ++np)
 #pragma unroll
         for (int gr = 0; gr < NG; ++gr) {
           const float off = -16.f * qs[np][gr];
-          f32x4_t c = {off, off, off, off};
+          c[np][gr] = (f32x4_t){off, off, off, off};
+        }
 #pragma unroll
-          for (int st = 0; st < 2; ++st)
-            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[gr][st], qf[np][gr][st], c, 0, 0, 0);
+      for (int cp = 0; cp < NB; ++cp)
+#pragma unroll
+        for (int gr = 0; gr < NG; ++gr)
+#pragma unroll
+          for (int st = 0; st < 2; ++st) {
+            const bf16x8_t kf = codes8((uint32_t)t.k[u * NB + cp][gr][st], cb);
+#pragma unroll
+            for (int np = 0; np < NP; ++np)
+              c[np][gr] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[np][cp][gr][st], c[np][gr],
+                                                                  0, 0, 0);
+          }
+#pragma unroll
+      for (int gr = 0; gr < NG; ++gr) {
+        const u32x4_t m = *reinterpret_cast<const u32x4_t *>(s_km + gr * PG_TILE +
+                                                             16 * (u * NB + copy) + 4 * g);
+#pragma unroll
+        for (int np = 0; np < NP; ++np)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint32_t m = km[gr][i];
-            const float base = gr == 0 ? zero_of(m) * qs[np][gr]
-                                       : fmaf(zero_of(m), qs[np][gr], sc[np][4 * T + i]);
-            sc[np][4 * T + i] = fmaf(scale_of(m), c[i], base);
+            float &x = sc[np][4 * u + i];
+            x = fmaf(zero_of(m[i]), qs[np][gr], gr == 0 ? 0.f : x);
+            x = fmaf(scale_of(m[i]), c[np][gr][i], x);
           }
-        }
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    const bool masked = key0 + PG_TILE > min(all_see, k1);
+    const bool masked = key0 + PG_TILE > all_see;
     bf16x8_t pf[NP][NG][2];
 #pragma unroll
     for (int np = 0; np < NP; ++np) {
-      const int lim = min(seen[np], k1) - (key0 + 16 * g);  // of this lane's 16 keys
+      const int lim = seen[np] - (key0 + 16 * copy + 4 * g);  // score 4 u + i: key 16 NB u + i of it
       if (masked) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (i >= lim) sc[np][i] = -INFINITY;
+        for (int i = 0; i < NS; ++i)
+          if ((i >> 2) * 16 * NB + (i & 3) >= lim) sc[np][i] = -INFINITY;
       }
       float mx = sc[np][0];
 #pragma unroll
-      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[np][i]);
+      for (int i = 1; i < NS; ++i) mx = fmaxf(mx, sc[np][i]);
       // the running maximum rises only when some score exceeds it by more than 2^8
       if (__ballot(mx * scale_log2 > m_run[np] + 8.f)) {
         mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
@@ -257,38 +300,65 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(PagedBatch s, PagePool p, 
         m_run[np] = m_new;
       }
       const float m_off = m_run[np] == -INFINITY ? 0.f : m_run[np];  // (no key yet: every p is 0)
-      float pv[16];
+      float pv[NS], ps[NG][NS];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
+      for (int i = 0; i < NS; ++i) {
         pv[i] = __builtin_amdgcn_exp2f(fmaf(sc[np][i], scale_log2, -m_off));
         l_run[np] += pv[i];
       }
 #pragma unroll
       for (int gr = 0; gr < NG; ++gr) {
-        float ps[16];
+        float sum = 0.f;
 #pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) {
-          u32x4_t m = *reinterpret_cast<const u32x4_t *>(s_vm + g * MST + (gr * 16 + 4 * i4) * 4);
+        for (int u = 0; u < NS / 4; ++u) {
+          u32x4_t m = *reinterpret_cast<const u32x4_t *>(s_vm + gr * PG_TILE + 16 * (u * NB + copy) +
+                                                         4 * g);
           if (masked) {  // a hidden key's scale and zero may be anything: 0 times them is not taken
 #pragma unroll
-            for (int j = 0; j < 4; ++j) m[j] = 4 * i4 + j < lim ? m[j] : 0u;
+            for (int j = 0; j < 4; ++j) m[j] = 16 * NB * u + j < lim ? m[j] : 0u;
           }
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const float sv = scale_of(m[j]), p_ = pv[4 * i4 + j];
-            ps[4 * i4 + j] = p_ * sv;
-            zs[np][gr] = fmaf(p_, fmaf(8.f, sv, zero_of(m[j])), zs[np][gr]);
+            const float p_ = pv[4 * u + j];
+            ps[gr][4 * u + j] = p_ * scale_of(m[j]);
+            zs[np][gr] = fmaf(p_, zero_of(m[j]), zs[np][gr]);
+            sum += ps[gr][4 * u + j];
+          }
+        }
+        zs[np][gr] = fmaf(8.f, sum, zs[np][gr]);
+      }
+      // a step's places: (key i of T = 2 st, key i of 2 st + 1), i = 0..3
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        u32x4_t x[NG];
+        if constexpr (NB == 1) {
+#pragma unroll
+          for (int gr = 0; gr < NG; ++gr)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              x[gr][i] = pack_bf2(ps[gr][8 * st + i], ps[gr][8 * st + 4 + i]);
+        } else {
+          const int u = NB == 4 ? 0 : st;
+          if constexpr (NG == 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t w = pack_bf2(ps[0][4 * u + i], ps[1][4 * u + i]);
+              x[0][i] = __builtin_amdgcn_perm(0u, w, sel[st][0]);
+              x[1][i] = __builtin_amdgcn_perm(0u, w, sel[st][1]);
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; i += 2) {
+              const uint32_t w = pack_bf2(ps[0][4 * u + i], ps[0][4 * u + i + 1]);
+              x[0][i] = __builtin_amdgcn_perm(0u, w, sel[st][0]);
+              x[0][i + 1] = __builtin_amdgcn_perm(0u, w, sel[st][1]);
+            }
           }
         }
 #pragma unroll
-        for (int st = 0; st < 2; ++st) {
-          u32x4_t x;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x[i] = pack_bf2(ps[8 * st + i], ps[8 * st + 4 + i]);
-          pf[np][gr][st] = __builtin_bit_cast(bf16x8_t, x);
-        }
-        __builtin_amdgcn_sched_barrier(0);
+        for (int gr = 0; gr < NG; ++gr) pf[np][gr][st] = __builtin_bit_cast(bf16x8_t, x[gr]);
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
     const bf16x8_t one = __builtin_bit_cast(
         bf16x8_t, (u32x4_t){0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
@@ -306,7 +376,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(PagedBatch s, PagePool p, 
           (__attribute__((address_space(3))) i32x2_t *)(mem + lane * VST + db * 8));
 #pragma unroll
       for (int st = 0; st < 2; ++st) {
-        const bf16x8_t vf = codes8((uint32_t)w[st]);
+        const bf16x8_t vf = codes8((uint32_t)w[st], cb);
 #pragma unroll
         for (int np = 0; np < NP; ++np)
           o[np][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[np][db / 4][st], o[np][db], 0,
@@ -320,26 +390,26 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(PagedBatch s, PagePool p, 
   int key0 = k0 + wave * PG_TILE;
   if (key0 < k1) {
     Tile t0, t1;
-    load(t0, key0, page_at(key0));
-    int page = page_at(key0 + STEP);
-    while (true) {
-      const int next = page_at(key0 + 2 * STEP);
+    load(t0, key0, pages_at(key0));
+    Ids ids = pages_at(key0 + STEP);
+    while (true) {  // (past the end: the last page again)
       stash(t0);
-      load(t1, key0 + STEP, page);  // (past the end: its last page again)
+      load(t1, key0 + STEP, ids);
+      ids = pages_at(key0 + 2 * STEP);
       __builtin_amdgcn_sched_barrier(0);
       attend(t0, key0);
       key0 += STEP;
       if (key0 >= k1) break;
-      page = page_at(key0 + 2 * STEP);
       stash(t1);
-      load(t0, key0 + STEP, next);
+      load(t0, key0 + STEP, ids);
+      ids = pages_at(key0 + 2 * STEP);
       __builtin_amdgcn_sched_barrier(0);
       attend(t1, key0);
       key0 += STEP;
       if (key0 >= k1) break;
     }
   }
-  // the waves' parts through LDS: rows of a pair's outputs
+  // the waves' and copies' parts through LDS: rows of a column's outputs
   __syncthreads();
   float *mine = reinterpret_cast<float *>(mem);
 #pragma unroll
@@ -369,18 +439,19 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(PagedBatch s, PagePool p, 
   for (int i = tid / PER; v0 + i <= last; i += 256 / PER) {
     float mm = -INFINITY, l = 0.f, a[8];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) mm = fmaxf(mm, s_m[w][i]);
+    for (int w = 0; w < 4 * NB; ++w) mm = fmaxf(mm, s_m[w / NB][i + w % NB * COLS]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) a[j] = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      // a wave without a key of the pair has l = 0 (m = -inf is also what NaN scores leave, with
+    for (int w = 0; w < 4 * NB; ++w) {
+      // a part without a key of the pair has l = 0 (m = -inf is also what NaN scores leave, with
       // a sum of NaN)
-      const float lw = s_l[w][i];
+      const int c = i + w % NB * COLS;
+      const float lw = s_l[w / NB][c];
       if (lw == 0.f) continue;
-      const float f = mm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(s_m[w][i] - mm);
+      const float f = mm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(s_m[w / NB][c] - mm);
       l = fmaf(f, lw, l);
-      const float *x = reinterpret_cast<const float *>(s_mem + w * WAVE_BYTES) + i * OST + e0;
+      const float *x = reinterpret_cast<const float *>(s_mem + w / NB * WAVE_BYTES) + c * OST + e0;
       float xv[8];
       load8(x, xv);
 #pragma unroll
@@ -507,6 +578,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
 
   // A thread has a quarter of a row's codes, keys and values.
   const int krow = tid >> 2, kq = tid & 3;
+  const F16Bits fb = f16_bits();
   typedef __attribute__((ext_vector_type(WORDS))) uint32_t words_t;
   struct Codes {
     words_t k, v;
@@ -540,7 +612,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
     f16x2_t sc = {m[0], m[0]}, z = {m[1], m[1]};
 #pragma unroll
     for (int j = 0; j < WORDS; ++j)
-      *reinterpret_cast<f16x8_t *>(ks + j * 8) = values8(c.k[j], sc, z);
+      *reinterpret_cast<f16x8_t *>(ks + j * 8) = values8(c.k[j], sc, z, fb);
     m = __builtin_bit_cast(f16x2_t, c.vm);
     sc = (f16x2_t){m[0], m[0]};
     z = (f16x2_t){m[1], m[1]};
@@ -556,7 +628,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
 #pragma unroll
     for (int j = 0; j < WORDS; ++j)
       *reinterpret_cast<f16x8_t *>(vs + ((j + turn) & (WORDS - 1)) * 8) =
-          unorder8(values8(w[j], sc, z));
+          unorder8(values8(w[j], sc, z, fb));
   };
   if (tid == 0) s_odd = 0;
   Codes c;
@@ -739,7 +811,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
 static PagedPlan paged_plan(const PagedBatch &s, int hq, int hkv) {
   PagedPlan p;
   const long long pairs = (long long)s.rows_max * (hq / hkv);
-  p.pairs = pairs <= 16 ? 16 : pairs <= 32 ? 32 : pairs <= 64 ? 64 : 128;
+  p.pairs = pairs <= 4 ? 4 : pairs <= 8 ? 8 : pairs <= 16 ? 16 : pairs <= 32 ? 32 : pairs <= 64 ? 64 : 128;
   p.many = pairs > 32;
   p.tiles = (int)((pairs + p.pairs - 1) / p.pairs);
   const long long items = (long long)s.n_req * p.tiles * hkv;
@@ -773,15 +845,18 @@ hipError_t launch_paged_attention(const PagedBatch &s, const PagePool &p, const 
   _Float16 *po = reinterpret_cast<_Float16 *>(ml + (size_t)plan.chunks * s.n_rows * hq);
 #define AKVS_PAGED(...)                                                                          \
   hipLaunchKernelGGL((__VA_ARGS__), g, b, 0, st, s, p, plan, Q, hq, hkv, scale, O, lse, po, ml)
+#define AKVS_PAGED_HD(HD_)                                   \
+  if (plan.many) AKVS_PAGED(k_paged_many<HD_>);              \
+  else if (plan.pairs == 32) AKVS_PAGED(k_paged_few<HD_, 2, 1>); \
+  else if (plan.pairs == 16) AKVS_PAGED(k_paged_few<HD_, 1, 1>); \
+  else if (plan.pairs == 8) AKVS_PAGED(k_paged_few<HD_, 1, 2>);  \
+  else AKVS_PAGED(k_paged_few<HD_, 1, 4>)
   if (hd == 128) {
-    if (plan.many) AKVS_PAGED(k_paged_many<128>);
-    else if (plan.pairs == 32) AKVS_PAGED(k_paged_few<128, 2>);
-    else AKVS_PAGED(k_paged_few<128, 1>);
+    AKVS_PAGED_HD(128);
   } else {
-    if (plan.many) AKVS_PAGED(k_paged_many<64>);
-    else if (plan.pairs == 32) AKVS_PAGED(k_paged_few<64, 2>);
-    else AKVS_PAGED(k_paged_few<64, 1>);
+    AKVS_PAGED_HD(64);
   }
+#undef AKVS_PAGED_HD
 #undef AKVS_PAGED
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || plan.chunks <= 1) return e;

@@ -96,6 +96,7 @@ __global__ __launch_bounds__(1024, 4) void k_w4_rows(W4Args a, W4X<XP> x, int ld
   f32x4_t y[NW];
 #pragma unroll
   for (int t = 0; t < NW; ++t) y[t] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+  const CodeBits cb = bf16_bits();
   const bf16x8_t m16 = __builtin_bit_cast(
       bf16x8_t, (u32x4_t){0xc180c180u, 0xc180c180u, 0xc180c180u, 0xc180c180u});  // -16
   const int runs = (a.n_in + W4_RUN - 1) / W4_RUN, last_byte = a.n_in / 2 - 16;
@@ -163,7 +164,7 @@ __global__ __launch_bounds__(1024, 4) void k_w4_rows(W4Args a, W4X<XP> x, int ld
             f32x4_t s = off[gr];
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
-              const bf16x8_t wf = codes8(cw[gr][st]);
+              const bf16x8_t wf = codes8(cw[gr][st], cb);
 #pragma unroll
               for (int p = 0; p < XP; ++p)
                 s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[p][gr][st], wf, s, 0, 0, 0);
