@@ -36,9 +36,9 @@ constexpr int PG_TILE = 64;  // keys a wave takes at a time
 // few pairs leave room (NB > 1): the columns are NB copies of the pairs, and copy T % NB belongs to
 // the keys of T. Queries are 0 in the others' columns, so that NB products add into one accumulator,
 // and so are a copy's probabilities in the others' places of the reduction.
-// Loads of the next tile, and its pages' numbers (scalar: 16 consecutive keys lie in one page) a
-// tile earlier, are in flight meanwhile.
-template <int HD, int NP, int NB>
+// Loads of the next tile, and its pages' numbers (scalar: 16 consecutive keys lie in one page, with
+// WIDE pages of 64 rows or more the tile) a tile earlier, are in flight meanwhile.
+template <int HD, int NP, int NB, bool WIDE>
 __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
     PagedBatch s, PagePool p, PagedPlan plan, const bf16_t *__restrict__ Q, int hq, int hkv,
     float scale_log2, bf16_t *__restrict__ out, float *__restrict__ lse,
@@ -168,35 +168,38 @@ __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
   // (read through scalar registers: nothing writes the table meanwhile)
   typedef const __attribute__((address_space(4))) int32_t *entries_t;
   const entries_t entries = (entries_t)(uintptr_t)table;
+  constexpr int NI = WIDE ? 1 : 4;  // pages of a tile at most
   struct Ids {
-    int page[4];
+    int page[NI];
   };
   // the pages of the tile's 16 keys each, clamped into the sequence
   auto pages_at = [&](int key0) __attribute__((always_inline)) {
     Ids x;
 #pragma unroll
-    for (int T = 0; T < 4; ++T) x.page[T] = entries[min((key0 + 16 * T) >> p.shift, last_page)];
+    for (int T = 0; T < NI; ++T) x.page[T] = entries[min((key0 + 16 * T) >> p.shift, last_page)];
     return x;
   };
   auto load = [&](Tile &t, int key0, const Ids &ids) __attribute__((always_inline)) {
-    size_t row[4];  // of the pool's rows of all heads, where 16 keys begin (uniform)
-    bool there[4];
+    size_t row[NI];  // of the pool's rows of all heads, where 16 keys begin (uniform)
+    bool there[NI];
 #pragma unroll
-    for (int T = 0; T < 4; ++T) {
+    for (int T = 0; T < NI; ++T) {
       there[T] = ids.page[T] >= 0 && ids.page[T] < p.n_pages;
       row[T] = (((size_t)(there[T] ? ids.page[T] : 0) * hkv + h) << p.shift) +
                ((key0 + 16 * T) & mask);
     }
 #pragma unroll
     for (int T = 0; T < 4; ++T) {
-      const uint8_t *k = p.k + row[T] * RB;
+      const uint8_t *k = WIDE ? p.k + row[0] * RB + T * 16 * RB : p.k + row[T * (NI - 1) / 3] * RB;
 #pragma unroll
       for (int gr = 0; gr < NG; ++gr)
         t.k[T][gr] = *reinterpret_cast<const i32x2_t *>(k + lr * RB + g * 8 + gr * 32);
     }
 #pragma unroll
     for (int j = 0; j < NV; ++j) {  // (HD 64: the rows of two T in a load)
-      if (VROWS == 16) {
+      if constexpr (WIDE) {
+        t.v[j] = *reinterpret_cast<const u32x4_t *>(p.v + row[0] * RB + j * 1024 + lane * 16);
+      } else if constexpr (VROWS == 16) {
         t.v[j] = *reinterpret_cast<const u32x4_t *>(p.v + row[j] * RB + lane * 16);
       } else {
         const uint8_t *v = p.v + (lane < 32 ? row[2 * j] : row[2 * j + 1]) * RB;
@@ -204,15 +207,25 @@ __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
       }
     }
     // meta of key `lane`
-    const size_t a = g & 1 ? row[1] : row[0], c = g & 1 ? row[3] : row[2];
-    const bool ta = g & 1 ? there[1] : there[0], tc = g & 1 ? there[3] : there[2];
-    const size_t mine = ((g & 2 ? c : a) + lr) * NG;
-    const bool live = (g & 2 ? tc : ta) && key0 + lane < k1;
+    const uint32_t *km = p.k_meta, *vm = p.v_meta;
+    bool live = key0 + lane < k1;
+    if constexpr (WIDE) {
+      km += row[0] * NG + lane * NG;
+      vm += row[0] * NG + lane * NG;
+      live = live && there[0];
+    } else {
+      const size_t a = g & 1 ? row[1] : row[0], c = g & 1 ? row[3] : row[2];
+      const bool ta = g & 1 ? there[1] : there[0], tc = g & 1 ? there[3] : there[2];
+      const size_t mine = ((g & 2 ? c : a) + lr) * NG;
+      km += mine;
+      vm += mine;
+      live = live && (g & 2 ? tc : ta);
+    }
 #pragma unroll
     for (int gr = 0; gr < NG; ++gr) {
-      const uint32_t km = p.k_meta[mine + gr], vm = p.v_meta[mine + gr];
-      t.km[gr] = live ? km : 0u;
-      t.vm[gr] = live ? vm : 0u;
+      const uint32_t a = km[gr], c = vm[gr];
+      t.km[gr] = live ? a : 0u;
+      t.vm[gr] = live ? c : 0u;
     }
   };
   // Values and meta to this wave's LDS (its reads of the tile before are done: in order). Row 16 g +
@@ -320,7 +333,7 @@ __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const float p_ = pv[4 * u + j];
-            ps[gr][4 * u + j] = p_ * scale_of(m[j]);
+            ps[gr][4 * u + j] = fmaf(p_, scale_of(m[j]), 0.f);  // (one mixed instruction)
             zs[np][gr] = fmaf(p_, zero_of(m[j]), zs[np][gr]);
             sum += ps[gr][4 * u + j];
           }
@@ -806,28 +819,51 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
                  : ((m_run == -INFINITY ? 0.f : m_run) - P_BITS) * 0.6931471805599453f + logf(l);
 }
 
-// Pairs of a request and KV head: up to 16 or 32, one or two tiles of k_paged_few; more, the
-// tiles of k_paged_many.
-static PagedPlan paged_plan(const PagedBatch &s, int hq, int hkv) {
+// Pairs of a request and KV head: up to 32 are k_paged_few's, more k_paged_many's. The keys are cut
+// into the number of chunks whose estimated end is the earliest, taking every sequence to be as
+// long as the longest: a block takes FIXED and WALK per tile that it walks (its waves walk a
+// quarter each in k_paged_few), ALONE of that where it has its unit for itself; whole rounds of
+// blocks, and what is left of them, follow each other.
+//   32 requests of 4700 to 16000 keys of 40/8 heads: chunks of 8192 keys (one round) 92 us, of 4096
+//   102, of 16384 99; 3 of 91000 to 122000 of 28/4: 2816 (one round) 40, 2560 (a little more) 50,
+//   1536 45, 6144 46.
+static PagedPlan paged_plan(const PagedBatch &s, int hq, int hkv, int hd) {
   PagedPlan p;
-  const long long pairs = (long long)s.rows_max * (hq / hkv);
+  const int G = hq / hkv;
+  const long long pairs = (long long)s.rows_max * G;
   p.pairs = pairs <= 4 ? 4 : pairs <= 8 ? 8 : pairs <= 16 ? 16 : pairs <= 32 ? 32 : pairs <= 64 ? 64 : 128;
   p.many = pairs > 32;
   p.tiles = (int)((pairs + p.pairs - 1) / p.pairs);
-  const long long items = (long long)s.n_req * p.tiles * hkv;
-  const int kt = (s.limit + PG_TILE - 1) / PG_TILE;
-  // chunks of whole rounds of the block's waves
-  const long long want = std::max(1LL, 4LL * gemm_cu_count() / std::max(1LL, items));
-  const long long most = std::max(1, std::min(MERGE_SLOTS, kt / 8));
-  const int per = kt ? (int)((kt + std::min(want, most) - 1) / std::min(want, most)) : 1;
-  p.chunk_keys = (per + 3) / 4 * 4 * PG_TILE;
+  const double FIXED = 7, WALK = p.many ? 3.3 : 2.55, ALONE = 0.6, MOVED = 5e6;
+  const int kt = (s.limit + PG_TILE - 1) / PG_TILE, unit = p.many ? 1 : 4;
+  const long long slots = gemm_cu_count() * (hd == 64 ? (p.many ? 3LL : 4LL) : 2LL);
+  // (tiles of a request that has fewer rows than another are empty)
+  const double items =
+      hkv * std::min((double)s.n_req * p.tiles, (double)s.n_rows * G / p.pairs + 0.5 * s.n_req);
+  const double moved = (double)s.n_rows * hq * (4 * hd + 32) / MOVED;  // a chunk's partials
+  auto end = [&](long long n) {
+    const double walk = WALK * (double)(((kt + n - 1) / n + unit - 1) / unit);
+    const double count = items * n, rounds = std::floor(count / slots), rest = count - rounds * slots;
+    double t = rounds * (FIXED + walk);
+    if (rest > 0) t += FIXED + walk * (rest <= slots / 2 ? ALONE : 1.0);
+    return t + (n > 1 ? 4 + moved * n : 0);
+  };
+  const long long most = std::max(1, std::min(MERGE_SLOTS, (kt + 3) / 4));
+  long long best = 1;
+  auto consider = [&](double want) {
+    const long long n = std::max(1LL, std::min((long long)want, most));
+    if (end(n) < end(best)) best = n;
+  };
+  for (double rounds : {0.5, 1.0, 2.0, 3.0, 4.0}) consider(rounds * slots / std::max(1.0, items));
+  const int per = kt ? (int)((kt + best - 1) / best) : 1;
+  p.chunk_keys = (per + unit - 1) / unit * unit * PG_TILE;
   p.chunks = std::max(1, (s.limit + p.chunk_keys - 1) / p.chunk_keys);
   return p;
 }
 
 size_t paged_part_floats(const PagedBatch &s, int hq, int hkv, int hd) {
   if (s.n_rows == 0) return 0;
-  const PagedPlan p = paged_plan(s, hq, hkv);
+  const PagedPlan p = paged_plan(s, hq, hkv, hd);
   const size_t items = (size_t)p.chunks * s.n_rows * hq;
   return p.chunks > 1 ? items * (hd / 2) + items * 4 : 0;
 }
@@ -836,7 +872,7 @@ hipError_t launch_paged_attention(const PagedBatch &s, const PagePool &p, const 
                                   int hkv, int hd, void *out, float *lse, float *part,
                                   hipStream_t st) {
   if (s.n_rows == 0) return hipSuccess;
-  const PagedPlan plan = paged_plan(s, hq, hkv);
+  const PagedPlan plan = paged_plan(s, hq, hkv, hd);
   const dim3 g((unsigned)((size_t)s.n_req * plan.chunks * plan.tiles * hkv)), b(256);
   const float scale = 1.4426950408889634f / sqrtf((float)hd);
   const bf16_t *Q = reinterpret_cast<const bf16_t *>(q);
@@ -845,17 +881,27 @@ hipError_t launch_paged_attention(const PagedBatch &s, const PagePool &p, const 
   _Float16 *po = reinterpret_cast<_Float16 *>(ml + (size_t)plan.chunks * s.n_rows * hq);
 #define AKVS_PAGED(...)                                                                          \
   hipLaunchKernelGGL((__VA_ARGS__), g, b, 0, st, s, p, plan, Q, hq, hkv, scale, O, lse, po, ml)
-#define AKVS_PAGED_HD(HD_)                                   \
-  if (plan.many) AKVS_PAGED(k_paged_many<HD_>);              \
-  else if (plan.pairs == 32) AKVS_PAGED(k_paged_few<HD_, 2, 1>); \
-  else if (plan.pairs == 16) AKVS_PAGED(k_paged_few<HD_, 1, 1>); \
-  else if (plan.pairs == 8) AKVS_PAGED(k_paged_few<HD_, 1, 2>);  \
-  else AKVS_PAGED(k_paged_few<HD_, 1, 4>)
-  if (hd == 128) {
-    AKVS_PAGED_HD(128);
-  } else {
-    AKVS_PAGED_HD(64);
+#define AKVS_PAGED_FEW(HD_, NP_, NB_)                            \
+  if (p.shift >= 6) AKVS_PAGED(k_paged_few<HD_, NP_, NB_, true>); \
+  else AKVS_PAGED(k_paged_few<HD_, NP_, NB_, false>)
+#define AKVS_PAGED_HD(HD_)                                 \
+  if (plan.many) {                                         \
+    AKVS_PAGED(k_paged_many<HD_>);                         \
+  } else if (plan.pairs == 32) {                           \
+    AKVS_PAGED_FEW(HD_, 2, 1);                             \
+  } else if (plan.pairs == 16) {                           \
+    AKVS_PAGED_FEW(HD_, 1, 1);                             \
+  } else if (plan.pairs == 8) {                            \
+    AKVS_PAGED_FEW(HD_, 1, 2);                             \
+  } else {                                                 \
+    AKVS_PAGED_FEW(HD_, 1, 4);                             \
   }
+  if (hd == 128) {
+    AKVS_PAGED_HD(128)
+  } else {
+    AKVS_PAGED_HD(64)
+  }
+#undef AKVS_PAGED_FEW
 #undef AKVS_PAGED_HD
 #undef AKVS_PAGED
   const hipError_t e = hipGetLastError();
