@@ -6,6 +6,7 @@
 // weights go to the matrix cores without a rounding, two in an instruction; -16 sum x comes from
 // the matrix cores as well. x in bf16 is taken as it is, in fp32 as three bf16 that add up to it.
 #include <algorithm>
+#include <type_traits>
 
 #include "four_bit_dev.h"
 #include "gemm_dev.h"
@@ -21,48 +22,11 @@ constexpr int W4_RUN = 4 * W4_UNIT; // what a wave takes at a time
 // lane g with elements w4_first(g) .. + 15 of it.
 __device__ __forceinline__ int w4_first(int g) { return ((g & 1) << 5) + ((g >> 1) << 4); }
 
-// x as it is multiplied: the fragment of group elements w4_first(g) + 8 st .., row r.
-template <int XP>
-struct W4X;
-template <>
-struct W4X<1> {
-  const bf16_t *x;
-  __device__ bf16x8_t get(int, size_t at) const {
-    return order8(*reinterpret_cast<const u32x4_t *>(x + at));
-  }
+// How a call is cut: a block has `slice` runs of the reduction (of blockIdx.y), its rows of x in
+// LDS, and waves / wk tiles of outputs, whose runs wk waves share.
+struct W4Plan {
+  int waves, wk, slice, slices, rows;  // rows: of x in the block
 };
-template <>
-struct W4X<3> {  // planes of [rows][n_in], already in the products' order
-  const bf16_t *x;
-  size_t plane;
-  __device__ bf16x8_t get(int p, size_t at) const {
-    return *reinterpret_cast<const bf16x8_t *>(x + p * plane + at);
-  }
-};
-
-// fp32 rows as three bf16 parts (truncated, so that each difference is exact), every 8 elements in
-// the order 0, 4, 1, 5, 2, 6, 3, 7.
-__global__ __launch_bounds__(256) void k_w4_split(const float *__restrict__ x, long long ldx,
-                                                  int rows, int n_in, bf16_t *__restrict__ out) {
-  const int per = n_in / 8;
-  const size_t id = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (id >= (size_t)rows * per) return;
-  const int r = (int)(id / per), e = (int)(id - (size_t)r * per) * 8;
-  float v[8];
-  load8(x + r * ldx + e, v);
-#pragma unroll
-  for (int p = 0; p < 3; ++p) {
-    u32x4_t q;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t a = __float_as_uint(v[2 * i]), b = __float_as_uint(v[2 * i + 1]);
-      q[i] = (a >> 16) | (b & 0xffff0000u);
-      v[2 * i] -= __uint_as_float(a & 0xffff0000u);
-      v[2 * i + 1] -= __uint_as_float(b & 0xffff0000u);
-    }
-    *reinterpret_cast<bf16x8_t *>(out + ((size_t)p * rows + r) * n_in + e) = order8(q);
-  }
-}
 
 __device__ __forceinline__ void w4_put(const W4Args &a, int r, int o, float y) {
   const size_t at = r * a.ldy + o;
@@ -71,18 +35,39 @@ __device__ __forceinline__ void w4_put(const W4Args &a, int r, int o, float y) {
   else reinterpret_cast<float *>(a.y)[at] = y;
 }
 
-// Up to 16 rows. Block: 16 outputs, or NW = 2 of these tiles (with SWIGLU a gate's and an up's);
-// its waves take runs of 512 elements in turn, codes a run ahead, and are summed in order through
-// LDS. MFMA 16x16x32, rows of x as rows, outputs as columns: a lane holds 4 rows of one output,
-// whose scale and zero it has itself.
-template <int NW, int XP, bool SWIGLU>
-__global__ __launch_bounds__(1024, 4) void k_w4_rows(W4Args a, W4X<XP> x, int ldx, int row0) {
-  extern __shared__ float s_y[];  // [waves][NW][16][16 + 1]
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const int g = lane >> 4, lr = lane & 15;
-  const int wide = SWIGLU ? a.n_out / 2 : a.n_out;
-  const int o0 = blockIdx.x * 16 * (SWIGLU ? NW / 2 : NW);
-  const int groups = a.n_in / 64, rows = min(a.rows - row0, 16);
+// fp32 elements as XP = 3 bf16 parts (truncated, so that each difference is exact), bf16 as they are.
+__device__ __forceinline__ u32x4_t w4_part(const bf16_t *, u32x4_t &x, float (&)[8]) { return x; }
+__device__ __forceinline__ u32x4_t w4_part(const float *, u32x4_t &, float (&v)[8]) {
+  u32x4_t q;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t a = __float_as_uint(v[2 * i]), b = __float_as_uint(v[2 * i + 1]);
+    q[i] = (a >> 16) | (b & 0xffff0000u);
+    v[2 * i] -= __uint_as_float(a & 0xffff0000u);
+    v[2 * i + 1] -= __uint_as_float(b & 0xffff0000u);
+  }
+  return q;
+}
+__device__ __forceinline__ void w4_read(const bf16_t *p, u32x4_t &x, float (&)[8]) {
+  x = *reinterpret_cast<const u32x4_t *>(p);
+}
+__device__ __forceinline__ void w4_read(const float *p, u32x4_t &, float (&v)[8]) { load8(p, v); }
+
+// A wave has 16 outputs, or NW tiles of them (with SWIGLU tiles of gate and up in turn), and NX
+// tiles of 16 rows. MFMA 16x16x32, rows of x as rows, outputs as columns: a lane holds 4 rows of
+// one output, whose scale and zero it has itself. x goes to LDS once, every 8 elements in the
+// order of the codes; codes are loaded a run ahead.
+template <int NW, int NX, typename TX, bool SWIGLU>
+__global__ __launch_bounds__(512, 2) void k_w4(W4Args a, W4Plan p, int row0, float *part) {
+  constexpr int XP = std::is_same<TX, float>::value ? 3 : 1;
+  extern __shared__ __attribute__((aligned(16))) char s_x[];  // [XP][rows][slice], then sums
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, lr = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wk = wave % p.wk, wn = wave / p.wk;
+  const int wide = SWIGLU ? a.n_out / 2 : a.n_out, groups = a.n_in / 64;
+  constexpr int TILES = SWIGLU ? NW / 2 : NW;  // of the result
+  const int o0 = (blockIdx.x * (p.waves / p.wk) + wn) * 16 * TILES;
+  const int k0 = blockIdx.y * p.slice * W4_RUN, k1 = min(a.n_in, k0 + p.slice * W4_RUN);
+  const int stride = p.slice * W4_RUN * 2 + 16;  // bytes of a row of x
   const uint8_t *w[NW];
   const uint32_t *meta[NW];
 #pragma unroll
@@ -92,36 +77,60 @@ __global__ __launch_bounds__(1024, 4) void k_w4_rows(W4Args a, W4X<XP> x, int ld
     w[t] = a.w + (size_t)o * (a.n_in / 2);
     meta[t] = a.meta + (size_t)o * groups;
   }
-  const size_t xrow = (size_t)(row0 + min(lr, rows - 1)) * ldx;
-  f32x4_t y[NW];
-#pragma unroll
-  for (int t = 0; t < NW; ++t) y[t] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-  const CodeBits cb = bf16_bits();
-  const bf16x8_t m16 = __builtin_bit_cast(
-      bf16x8_t, (u32x4_t){0xc180c180u, 0xc180c180u, 0xc180c180u, 0xc180c180u});  // -16
-  const int runs = (a.n_in + W4_RUN - 1) / W4_RUN, last_byte = a.n_in / 2 - 16;
-  // codes of unit u of the run; meta of unit g of it, both groups
-  auto codes = [&](int t, int run, int u) __attribute__((always_inline)) {
-    return *reinterpret_cast<const u32x4_t *>(w[t] + min(run * (W4_RUN / 2) + u * 64 + g * 16, last_byte));
+  const int last_byte = a.n_in / 2 - 16;
+  // codes of unit u from element k on; meta of unit g, both groups
+  auto codes = [&](int t, int k, int u) __attribute__((always_inline)) {
+    return *reinterpret_cast<const u32x4_t *>(w[t] + min(k / 2 + u * 64 + g * 16, last_byte));
   };
   struct Meta {
     uint32_t a, b;
   };
-  auto metas = [&](int t, int run) __attribute__((always_inline)) {
-    const int gr = run * 8 + g * 2;
+  auto metas = [&](int t, int k) __attribute__((always_inline)) {
+    const int gr = k / 64 + g * 2;
     return Meta{meta[t][min(gr, groups - 1)], meta[t][min(gr + 1, groups - 1)]};
   };
-  if (wave < runs) {
-    u32x4_t c[NW][4];
-    Meta md[NW];
+  const bool live = o0 < wide;  // (waves past the last output only load x)
+  u32x4_t c[NW][4];
+  Meta md[NW];
+  int k = k0 + wk * W4_RUN;
+  const int step = p.wk * W4_RUN;
+  if (live && k < k1) {
 #pragma unroll
     for (int t = 0; t < NW; ++t) {
-      md[t] = metas(t, wave);
+      md[t] = metas(t, k);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) c[t][u] = codes(t, wave, u);
+      for (int u = 0; u < 4; ++u) c[t][u] = codes(t, k, u);
     }
-    for (int run = wave; run < runs; run += waves) {
-      const int next = min(run + waves, runs - 1);
+  }
+  {
+    const int per = (k1 - k0) / 8;  // octets of a row
+    for (int i = tid; i < p.rows * per; i += blockDim.x) {
+      const int r = i / per, e = i - r * per;
+      u32x4_t x;
+      float v[8];
+      w4_read(reinterpret_cast<const TX *>(a.x) + (row0 + r) * a.ldx + k0 + e * 8, x, v);
+#pragma unroll
+      for (int q = 0; q < XP; ++q)
+        *reinterpret_cast<bf16x8_t *>(s_x + (q * p.rows + r) * stride + e * 16) =
+            order8(w4_part(static_cast<const TX *>(nullptr), x, v));
+    }
+  }
+  f32x4_t y[NW][NX];
+#pragma unroll
+  for (int t = 0; t < NW; ++t)
+#pragma unroll
+    for (int n = 0; n < NX; ++n) y[t][n] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+  const CodeBits cb = bf16_bits();
+  const bf16x8_t m16 = __builtin_bit_cast(
+      bf16x8_t, (u32x4_t){0xc180c180u, 0xc180c180u, 0xc180c180u, 0xc180c180u});  // -16
+  const char *x0[NX];
+#pragma unroll
+  for (int n = 0; n < NX; ++n)
+    x0[n] = s_x + min(n * 16 + lr, p.rows - 1) * stride + w4_first(g) * 2;
+  __syncthreads();
+  if (live) {
+    for (; k < k1; k += step) {
+      const int next = min(k + step, a.n_in - 1) / W4_RUN * W4_RUN;  // (past the end: any)
       uint32_t ma[NW][4], mb[NW][4];
 #pragma unroll
       for (int t = 0; t < NW; ++t) {
@@ -131,106 +140,215 @@ __global__ __launch_bounds__(1024, 4) void k_w4_rows(W4Args a, W4X<XP> x, int ld
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const int k = run * W4_RUN + u * W4_UNIT;
-        if (k >= a.n_in) break;
-        const bool both = k + 64 < a.n_in;
-        bf16x8_t xf[XP][2][2];
-#pragma unroll
-        for (int p = 0; p < XP; ++p)
-#pragma unroll
-          for (int gr = 0; gr < 2; ++gr)
-#pragma unroll
-            for (int st = 0; st < 2; ++st)
-              xf[p][gr][st] = x.get(p, xrow + k + (gr && both ? 64 : 0) + w4_first(g) + st * 8);
-        f32x4_t off[2];
-#pragma unroll
-        for (int gr = 0; gr < 2; ++gr) {
-          off[gr] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int p = 0; p < XP; ++p)
-#pragma unroll
-            for (int st = 0; st < 2; ++st)
-              off[gr] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[p][gr][st], m16, off[gr], 0, 0, 0);
-        }
+        const int ku = k + u * W4_UNIT;
+        if (ku >= k1) break;
+        const bool both = ku + 64 < k1;
+        uint32_t cw[NW][2][2];
 #pragma unroll
         for (int t = 0; t < NW; ++t) {
-          uint32_t cw[2][2] = {{c[t][u][0], c[t][u][1]}, {c[t][u][2], c[t][u][3]}};
-          swap_halves(cw[0][0], cw[1][0]);
-          swap_halves(cw[0][1], cw[1][1]);
+          cw[t][0][0] = c[t][u][0];
+          cw[t][0][1] = c[t][u][1];
+          cw[t][1][0] = c[t][u][2];
+          cw[t][1][1] = c[t][u][3];
+          swap_halves(cw[t][0][0], cw[t][1][0]);
+          swap_halves(cw[t][0][1], cw[t][1][1]);
           c[t][u] = codes(t, next, u);
+        }
 #pragma unroll
-          for (int gr = 0; gr < 2; ++gr) {
-            if (gr && !both) break;
-            f32x4_t s = off[gr];
+        for (int gr = 0; gr < 2; ++gr) {
+          if (gr && !both) break;
+          bf16x8_t wf[NW][2];
 #pragma unroll
-            for (int st = 0; st < 2; ++st) {
-              const bf16x8_t wf = codes8(cw[gr][st], cb);
+          for (int t = 0; t < NW; ++t)
 #pragma unroll
-              for (int p = 0; p < XP; ++p)
-                s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[p][gr][st], wf, s, 0, 0, 0);
+            for (int st = 0; st < 2; ++st) wf[t][st] = codes8(cw[t][gr][st], cb);
+#pragma unroll
+          for (int n = 0; n < NX; ++n) {
+            bf16x8_t xf[XP][2];
+#pragma unroll
+            for (int q = 0; q < XP; ++q)
+#pragma unroll
+              for (int st = 0; st < 2; ++st)
+                xf[q][st] = *reinterpret_cast<const bf16x8_t *>(
+                    x0[n] + q * p.rows * stride + (ku - k0 + gr * 64 + st * 8) * 2);
+            f32x4_t off = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int q = 0; q < XP; ++q)
+#pragma unroll
+              for (int st = 0; st < 2; ++st)
+                off = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[q][st], m16, off, 0, 0, 0);
+#pragma unroll
+            for (int t = 0; t < NW; ++t) {
+              f32x4_t s = off;
+#pragma unroll
+              for (int q = 0; q < XP; ++q)
+#pragma unroll
+                for (int st = 0; st < 2; ++st)
+                  s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[q][st], wf[t][st], s, 0, 0, 0);
+              const uint32_t m = gr ? mb[t][u] : ma[t][u];
+              const float zero = -0.0625f * zero_of(m);
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                y[t][n][i] = fmaf(scale_of(m), s[i], fmaf(zero, off[i], y[t][n][i]));
             }
-            const uint32_t m = gr ? mb[t][u] : ma[t][u];
-            const float scale = scale_of(m), zero = -0.0625f * zero_of(m);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[t][i] = fmaf(scale, s[i], fmaf(zero, off[gr][i], y[t][i]));
           }
         }
       }
     }
   }
-  // y[t][i]: row 4 g + i of output lr of tile t
-  constexpr int ST = 17;
+  // y[t][n][i]: row 16 n + 4 g + i of output lr of tile t
+  if (p.wk > 1) {  // the waves of a tile in order, through LDS
+    constexpr int ST = 17, SIZE = NW * NX * 16 * ST;
+    float *s_y = reinterpret_cast<float *>(s_x + (size_t)XP * p.rows * stride);
+    float *mine = s_y + wave * SIZE;
 #pragma unroll
-  for (int t = 0; t < NW; ++t)
+    for (int t = 0; t < NW; ++t)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s_y[((wave * NW + t) * 16 + 4 * g + i) * ST + lr] = y[t][i];
-  __syncthreads();
-  constexpr int TILES = SWIGLU ? NW / 2 : NW;
-  for (int e = threadIdx.x; e < TILES * 256; e += blockDim.x) {
-    const int t = e >> 8, r = (e >> 4) & 15, c = e & 15, o = o0 + t * 16 + c;
-    if (r >= rows || o >= wide) continue;
-    float s[2] = {0.f, 0.f};
+      for (int n = 0; n < NX; ++n)
 #pragma unroll
-    for (int h = 0; h < (SWIGLU ? 2 : 1); ++h) {
-      const float *p = s_y + ((SWIGLU ? 2 * t + h : t) * 16 + r) * ST + c;
-      for (int v = 0; v < waves; ++v) s[h] += p[v * NW * 16 * ST];
+        for (int i = 0; i < 4; ++i)
+          mine[((t * NX + n) * 16 + 4 * g + i) * ST + lr] = y[t][n][i];
+    __syncthreads();
+    const float *first = s_y + wn * p.wk * SIZE;
+    for (int e = wk * 64 + lane; e < TILES * NX * 256; e += p.wk * 64) {
+      const int t = e / (NX * 256), r = e / 16 % (NX * 16), col = e & 15, o = o0 + t * 16 + col;
+      if (r >= p.rows || o >= wide) continue;
+      float s[2] = {0.f, 0.f};
+#pragma unroll
+      for (int h = 0; h < (SWIGLU ? 2 : 1); ++h) {
+        const float *q = first + ((SWIGLU ? 2 * t + h : t) * NX * 16 + r) * ST + col;
+        for (int v = 0; v < p.wk; ++v) s[h] += q[v * SIZE];
+      }
+      if (part) {
+#pragma unroll
+        for (int h = 0; h < (SWIGLU ? 2 : 1); ++h)
+          part[((size_t)blockIdx.y * p.rows + r) * a.n_out + o + h * wide] = s[h];
+      } else {
+        w4_put(a, row0 + r, o, SWIGLU ? silu(s[0]) * s[1] : s[0]);
+      }
     }
-    w4_put(a, row0 + r, o, SWIGLU ? silu(s[0]) * s[1] : s[0]);
+    return;
+  }
+#pragma unroll
+  for (int t = 0; t < TILES; ++t) {
+    const int o = o0 + t * 16 + lr;
+    if (o >= wide) continue;
+#pragma unroll
+    for (int n = 0; n < NX; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = n * 16 + 4 * g + i;
+        if (r >= p.rows) continue;
+        const float s = y[SWIGLU ? 2 * t : t][n][i], u = SWIGLU ? y[SWIGLU ? 2 * t + 1 : 0][n][i] : 0.f;
+        if (part) {
+          float *q = part + ((size_t)blockIdx.y * p.rows + r) * a.n_out + o;
+          q[0] = s;
+          if (SWIGLU) q[wide] = u;
+        } else {
+          w4_put(a, row0 + r, o, SWIGLU ? silu(s) * u : s);
+        }
+      }
   }
 }
 
-static size_t w4_planes(int rows, int n_in) { return 3 * (size_t)rows * n_in; }
-
-size_t w4_ws_floats(int rows, int n_out, int n_in) { return (w4_planes(rows, n_in) + 1) / 2; }
-
-template <int XP>
-static hipError_t w4_rows(const W4Args &a, const W4X<XP> &x, long long ldx, hipStream_t st) {
+// The slices' sums in order, and what is made of them.
+__global__ __launch_bounds__(256) void k_w4_sum(W4Args a, int slices, int rows, int row0,
+                                                const float *__restrict__ part) {
   const int wide = a.swiglu ? a.n_out / 2 : a.n_out;
-  const int runs = (a.n_in + W4_RUN - 1) / W4_RUN;
-  const int waves = std::max(1, std::min(8, runs));
-  for (int row0 = 0; row0 < a.rows; row0 += 16) {
-    const int nw = a.swiglu ? 2 : 1;
-    const dim3 g((wide + 15) / 16), b(64 * waves);
-    const size_t lds = waves * nw * 16 * 17 * sizeof(float);
-    if (a.swiglu)
-      hipLaunchKernelGGL((k_w4_rows<2, XP, true>), g, b, lds, st, a, x, (int)ldx, row0);
-    else
-      hipLaunchKernelGGL((k_w4_rows<1, XP, false>), g, b, lds, st, a, x, (int)ldx, row0);
+  const size_t id = (size_t)blockIdx.x * 256 + threadIdx.x, all = (size_t)rows * a.n_out;
+  if (id >= (size_t)rows * wide) return;
+  const int r = (int)(id / wide), o = (int)(id - (size_t)r * wide);
+  const float *p = part + (size_t)r * a.n_out + o;
+  float s = 0.f, u = 0.f;
+  for (int q = 0; q < slices; ++q) s += p[q * all];
+  if (a.swiglu) {
+    for (int q = 0; q < slices; ++q) u += p[q * all + wide];
+    s = silu(s) * u;
   }
+  w4_put(a, row0 + r, o, s);
+}
+
+// Rows in one read of the weights.
+static int w4_most_rows(int parts) { return parts == 1 ? 64 : 32; }
+static int w4_nw(int rows, bool swiglu) { return swiglu || rows > 16 ? 2 : 1; }
+
+// x's rows of a slice fill at most half a unit's LDS; runs are shared by waves while tiles are too
+// few to fill the units.
+static W4Plan w4_plan(int rows, int n_out, int n_in, bool swiglu, int parts) {
+  constexpr int LDS = 72 << 10, WAVES = 8;
+  W4Plan p;
+  p.rows = std::min(rows, w4_most_rows(parts));
+  const int runs = (n_in + W4_RUN - 1) / W4_RUN;
+  const int most = std::max(1, (LDS / (p.rows * parts) - 16) / (W4_RUN * 2));
+  p.slices = (runs + most - 1) / most;
+  p.slice = (runs + p.slices - 1) / p.slices;
+  p.slices = (runs + p.slice - 1) / p.slice;
+  const int per = 16 * w4_nw(rows, swiglu);
+  const long long tiles = (n_out + per - 1) / per;
+  const long long want = 8LL * gemm_cu_count() / std::max(1LL, tiles * p.slices);
+  p.wk = (int)std::max(1LL, std::min<long long>({want, p.slice, WAVES}));
+  const int rounds = (p.slice + p.wk - 1) / p.wk;
+  p.wk = (p.slice + rounds - 1) / rounds;  // as few waves as take these rounds
+  p.waves = WAVES / p.wk * p.wk;
+  return p;
+}
+
+static size_t w4_part_floats(const W4Plan &p, int n_out) {
+  return p.slices > 1 ? (size_t)p.slices * p.rows * n_out : 0;
+}
+
+size_t w4_ws_floats(int rows, int n_out, int n_in) {
+  if (rows == 0 || n_out == 0) return 0;
+  size_t n = 0;
+  for (int parts : {1, 3})
+    for (bool swiglu : {false, true})
+      n = std::max(n, w4_part_floats(w4_plan(rows, n_out, n_in, swiglu, parts), n_out));
+  return n;
+}
+
+template <int NW, int NX, typename TX, bool SWIGLU>
+static hipError_t w4_launch(const W4Args &a, const W4Plan &p, int row0, float *part,
+                            hipStream_t st) {
+  constexpr int XP = std::is_same<TX, float>::value ? 3 : 1;
+  const int per = 16 * (SWIGLU ? NW / 2 : NW) * (p.waves / p.wk);
+  const int wide = SWIGLU ? a.n_out / 2 : a.n_out;
+  const dim3 g((wide + per - 1) / per, p.slices), b(64 * p.waves);
+  const size_t lds = (size_t)XP * p.rows * (p.slice * W4_RUN * 2 + 16) +
+                     (p.wk > 1 ? p.waves * NW * NX * 16 * 17 * sizeof(float) : 0);
+  hipLaunchKernelGGL((k_w4<NW, NX, TX, SWIGLU>), g, b, lds, st, a, p, row0, part);
   return hipGetLastError();
+}
+
+template <typename TX, bool SWIGLU>
+static hipError_t w4_rows(const W4Args &a, const W4Plan &p, int row0, float *part, hipStream_t st) {
+  if (p.rows <= 16) return w4_launch<SWIGLU ? 2 : 1, 1, TX, SWIGLU>(a, p, row0, part, st);
+  if constexpr (std::is_same<TX, bf16_t>::value) {
+    if (p.rows > 32 && p.rows <= 48) return w4_launch<2, 3, TX, SWIGLU>(a, p, row0, part, st);
+    if (p.rows > 48) return w4_launch<2, 4, TX, SWIGLU>(a, p, row0, part, st);
+  }
+  return w4_launch<2, 2, TX, SWIGLU>(a, p, row0, part, st);
 }
 
 hipError_t launch_w4(const W4Args &a, float *ws, hipStream_t st) {
   if (a.rows == 0 || a.n_out == 0) return hipSuccess;
-  if (a.x_dtype == AKVS_BF16)
-    return w4_rows<1>(a, {reinterpret_cast<const bf16_t *>(a.x)}, a.ldx, st);
-  bf16_t *planes = reinterpret_cast<bf16_t *>(ws);
-  const size_t octets = (size_t)a.rows * (a.n_in / 8);
-  hipLaunchKernelGGL(k_w4_split, dim3((unsigned)((octets + 255) / 256)), dim3(256), 0, st,
-                     reinterpret_cast<const float *>(a.x), a.ldx, a.rows, a.n_in, planes);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  return w4_rows<3>(a, {planes, (size_t)a.rows * a.n_in}, a.n_in, st);
+  const bool bf = a.x_dtype == AKVS_BF16;
+  W4Plan p = w4_plan(a.rows, a.n_out, a.n_in, a.swiglu, bf ? 1 : 3);
+  float *part = p.slices > 1 ? ws : nullptr;
+  const int most = p.rows;
+  for (int row0 = 0; row0 < a.rows; row0 += most) {
+    p.rows = std::min(most, a.rows - row0);
+    hipError_t e = bf ? (a.swiglu ? w4_rows<bf16_t, true>(a, p, row0, part, st)
+                                  : w4_rows<bf16_t, false>(a, p, row0, part, st))
+                      : (a.swiglu ? w4_rows<float, true>(a, p, row0, part, st)
+                                  : w4_rows<float, false>(a, p, row0, part, st));
+    if (e != hipSuccess) return e;
+    if (!part) continue;
+    const size_t n = (size_t)p.rows * (a.swiglu ? a.n_out / 2 : a.n_out);
+    hipLaunchKernelGGL(k_w4_sum, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, a, p.slices,
+                       p.rows, row0, part);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace akvs
