@@ -2302,7 +2302,11 @@ static akvs_status check_w4(int32_t n_rows, int32_t n_out, int32_t n_in) {
 
 size_t akvs_w4_workspace_size(int32_t n_rows, int32_t n_out, int32_t n_in) {
   if (check_w4(n_rows, n_out, n_in) != AKVS_OK) return 0;
-  return align256(w4_ws_floats(n_rows, n_out, n_in) * sizeof(float));
+  size_t n = 0;
+  for (const bool swiglu : {false, true})
+    for (const int32_t x_dtype : {AKVS_F32, AKVS_BF16})
+      n = std::max(n, w4_ws_floats(n_rows, n_out, n_in, swiglu, x_dtype));
+  return align256(n * sizeof(float));
 }
 
 akvs_status akvs_w4_product(const void *x, int64_t ldx, int32_t x_dtype, int32_t n_rows,
@@ -2328,7 +2332,8 @@ akvs_status akvs_w4_product(const void *x, int64_t ldx, int32_t x_dtype, int32_t
   REQUIRE(ldx >= n_in && ldy >= wide, AKVS_EINVAL, "row strides shorter than a row");
   REQUIRE(ldx < (1LL << 31) && ldy < (1LL << 31), AKVS_ESHAPE, "row strides too large");
   REQUIRE(ldx * xs % 16 == 0, AKVS_EINVAL, "x's row stride must be a multiple of 16 bytes");
-  const size_t need = akvs_w4_workspace_size(n_rows, n_out, n_in);
+  const size_t need =
+      w4_ws_floats(n_rows, n_out, n_in, mode == AKVS_W4_SWIGLU, x_dtype) * sizeof(float);
   REQUIRE(need == 0 || (ws && ws_bytes >= need), AKVS_ENOSPACE, "workspace %zu < %zu bytes",
           ws_bytes, need);
   const size_t yb = ((n_rows - 1) * ldy + wide) * ys;

@@ -3,14 +3,17 @@
 // y = x W^T with W = scale c + zero per group of 64: for each group
 //   sum x w = scale (sum x (16 + c) - 16 sum x) + zero sum x,
 // where a nibble c put into the upper mantissa bits of a bf16 of 16 is 16 + c, exactly, so that the
-// weights go to the matrix cores without a rounding, two in an instruction; -16 sum x comes from
-// the matrix cores as well. x in bf16 is taken as it is, in fp32 as three bf16 that add up to it.
+// weights go to the matrix cores without a rounding, two in an instruction. A group's sum x is
+// formed once, in fp32; sum zero sum x over the groups is a matrix product of its own, 1 / 64 as
+// long. x in bf16 is taken as it is, in fp32 as three bf16 that add up to it.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "four_bit_dev.h"
 #include "gemm_dev.h"
 #include "kernels.h"
+#include "quant_dev.h"
 
 namespace akvs {
 
@@ -52,14 +55,25 @@ __device__ __forceinline__ void w4_read(const bf16_t *p, u32x4_t &x, float (&)[8
   x = *reinterpret_cast<const u32x4_t *>(p);
 }
 __device__ __forceinline__ void w4_read(const float *p, u32x4_t &, float (&v)[8]) { load8(p, v); }
+__device__ __forceinline__ float octet_sum(const bf16_t *, const u32x4_t &x, const float (&)[8]) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    s += __uint_as_float(x[i] << 16) + __uint_as_float(x[i] & 0xffff0000u);
+  return s;
+}
+__device__ __forceinline__ float octet_sum(const float *, const u32x4_t &, const float (&v)[8]) {
+  return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+}
 
 // A wave has 16 outputs, or NW tiles of them (with SWIGLU tiles of gate and up in turn), and NX
 // tiles of 16 rows. MFMA 16x16x32, rows of x as rows, outputs as columns: a lane holds 4 rows of
 // one output, whose scale and zero it has itself. x goes to LDS once, every 8 elements in the
 // order of the codes; codes are loaded a run ahead.
 template <int NW, int NX, typename TX, bool SWIGLU>
-__global__ __launch_bounds__(512, 2) void k_w4(W4Args a, W4Plan p, int row0, float *part) {
+__global__ __launch_bounds__(768, 3) void k_w4(W4Args a, W4Plan p, int row0, float *part) {
   constexpr int XP = std::is_same<TX, float>::value ? 3 : 1;
+  constexpr bool UNITS_WHOLE = NX == 1 && NW == 1;
   extern __shared__ __attribute__((aligned(16))) char s_x[];  // [XP][rows][slice], then sums
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, lr = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wk = wave % p.wk, wn = wave / p.wk;
@@ -94,6 +108,9 @@ __global__ __launch_bounds__(512, 2) void k_w4(W4Args a, W4Plan p, int row0, flo
   Meta md[NW];
   int k = k0 + wk * W4_RUN;
   const int step = p.wk * W4_RUN;
+  // -16 times the sums of x over groups, [group][16 NX rows]; rows past the last are the last one's
+  constexpr int XR = 16 * NX;
+  float *s_sum = reinterpret_cast<float *>(s_x + (size_t)XP * p.rows * stride);
   if (live && k < k1) {
 #pragma unroll
     for (int t = 0; t < NW; ++t) {
@@ -102,17 +119,42 @@ __global__ __launch_bounds__(512, 2) void k_w4(W4Args a, W4Plan p, int row0, flo
       for (int u = 0; u < 4; ++u) c[t][u] = codes(t, k, u);
     }
   }
-  {
-    const int per = (k1 - k0) / 8;  // octets of a row
-    for (int i = tid; i < p.rows * per; i += blockDim.x) {
-      const int r = i / per, e = i - r * per;
-      u32x4_t x;
-      float v[8];
-      w4_read(reinterpret_cast<const TX *>(a.x) + (row0 + r) * a.ldx + k0 + e * 8, x, v);
+  {  // x, its octets row by row, BATCH of a thread requested at a time
+    constexpr int BATCH = XP == 1 ? 8 : 4;
+    const int per = (k1 - k0) / 8, total = p.rows * per, threads = p.waves * 64;
+    const int rows_on = threads / per, on = threads % per;  // of a thread's next octet
+    int r = tid / per, e = tid % per;
+    for (int i = tid; i < total; i += BATCH * threads) {
+      u32x4_t x[BATCH];
+      float v[BATCH][8];
+      int at_r[BATCH], at_e[BATCH];
 #pragma unroll
-      for (int q = 0; q < XP; ++q)
-        *reinterpret_cast<bf16x8_t *>(s_x + (q * p.rows + r) * stride + e * 16) =
-            order8(w4_part(static_cast<const TX *>(nullptr), x, v));
+      for (int b = 0; b < BATCH; ++b) {
+        at_r[b] = r;
+        at_e[b] = e;
+        r += rows_on;
+        e += on;
+        if (e >= per) {
+          e -= per;
+          ++r;
+        }
+        if (i + b * threads < total)
+          w4_read(reinterpret_cast<const TX *>(a.x) + (row0 + at_r[b]) * a.ldx + k0 + at_e[b] * 8,
+                  x[b], v[b]);
+      }
+#pragma unroll
+      for (int b = 0; b < BATCH; ++b) {
+        if (i + b * threads >= total) break;  // (the same for the 8 lanes of a group)
+        float sum = octet_sum(static_cast<const TX *>(nullptr), x[b], v[b]);
+#pragma unroll
+        for (int q = 0; q < XP; ++q)
+          *reinterpret_cast<bf16x8_t *>(s_x + (q * p.rows + at_r[b]) * stride + at_e[b] * 16) =
+              order8(w4_part(static_cast<const TX *>(nullptr), x[b], v[b]));
+        sum = -16.f * oct_sum(sum);
+        if ((lane & 7) == 0)
+          for (int row = at_r[b]; row < (at_r[b] == p.rows - 1 ? XR : at_r[b] + 1); ++row)
+            s_sum[at_e[b] / 8 * XR + row] = sum;
+      }
     }
   }
   f32x4_t y[NW][NX];
@@ -121,12 +163,47 @@ __global__ __launch_bounds__(512, 2) void k_w4(W4Args a, W4Plan p, int row0, flo
 #pragma unroll
     for (int n = 0; n < NX; ++n) y[t][n] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
   const CodeBits cb = bf16_bits();
-  const bf16x8_t m16 = __builtin_bit_cast(
-      bf16x8_t, (u32x4_t){0xc180c180u, 0xc180c180u, 0xc180c180u, 0xc180c180u});  // -16
   const char *x0[NX];
 #pragma unroll
   for (int n = 0; n < NX; ++n)
     x0[n] = s_x + min(n * 16 + lr, p.rows - 1) * stride + w4_first(g) * 2;
+  // sum zero sum x over a run's eight groups: lane g has the zeros of two, in two bf16 parts (11
+  // bits), and takes the sums in three; 2 x 2 places of its eight for each part of the sums
+  auto zeros = [&](int k) __attribute__((always_inline)) {
+    const int gr = (k - k0) / 64 + g * 2;
+    const bool in0 = k + g * 128 < k1, in1 = k + g * 128 + 64 < k1;
+    bf16x8_t zf[NW];
+#pragma unroll
+    for (int t = 0; t < NW; ++t) {
+      const float za = in0 ? -0.0625f * zero_of(md[t].a) : 0.f;
+      const float zb = in1 ? -0.0625f * zero_of(md[t].b) : 0.f;
+      const uint32_t a = __float_as_uint(za), b = __float_as_uint(zb);
+      const uint32_t hi = (a >> 16) | (b & 0xffff0000u);
+      const uint32_t lo = (__float_as_uint(za - __uint_as_float(a & 0xffff0000u)) >> 16) |
+                          (__float_as_uint(zb - __uint_as_float(b & 0xffff0000u)) & 0xffff0000u);
+      zf[t] = __builtin_bit_cast(bf16x8_t, (u32x4_t){hi, lo, hi, lo});
+    }
+#pragma unroll
+    for (int n = 0; n < NX; ++n) {
+      float v[2] = {in0 ? s_sum[gr * XR + n * 16 + lr] : 0.f,
+                    in1 ? s_sum[(gr + 1) * XR + n * 16 + lr] : 0.f};
+      uint32_t q[3];
+#pragma unroll
+      for (int e = 0; e < 3; ++e) {
+        const uint32_t a = __float_as_uint(v[0]), b = __float_as_uint(v[1]);
+        q[e] = (a >> 16) | (b & 0xffff0000u);
+        v[0] -= __uint_as_float(a & 0xffff0000u);
+        v[1] -= __uint_as_float(b & 0xffff0000u);
+      }
+      const bf16x8_t x01 = __builtin_bit_cast(bf16x8_t, (u32x4_t){q[0], q[0], q[1], q[1]});
+      const bf16x8_t x2 = __builtin_bit_cast(bf16x8_t, (u32x4_t){q[2], q[2], 0u, 0u});
+#pragma unroll
+      for (int t = 0; t < NW; ++t) {
+        y[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x01, zf[t], y[t][n], 0, 0, 0);
+        y[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x2, zf[t], y[t][n], 0, 0, 0);
+      }
+    }
+  };
   __syncthreads();
   if (live) {
     for (; k < k1; k += step) {
@@ -136,70 +213,72 @@ __global__ __launch_bounds__(512, 2) void k_w4(W4Args a, W4Plan p, int row0, flo
       for (int t = 0; t < NW; ++t) {
         spread4(md[t].a, ma[t]);
         spread4(md[t].b, mb[t]);
-        md[t] = metas(t, next);
       }
+      zeros(k);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int ku = k + u * W4_UNIT;
-        if (ku >= k1) break;
-        const bool both = ku + 64 < k1;
-        uint32_t cw[NW][2][2];
+      for (int t = 0; t < NW; ++t) md[t] = metas(t, next);
+      // (whole runs without a branch, so that LDS reads go ahead of the products)
+      auto units = [&](auto whole) __attribute__((always_inline)) {
+        constexpr bool WHOLE = decltype(whole)::value;
 #pragma unroll
-        for (int t = 0; t < NW; ++t) {
-          cw[t][0][0] = c[t][u][0];
-          cw[t][0][1] = c[t][u][1];
-          cw[t][1][0] = c[t][u][2];
-          cw[t][1][1] = c[t][u][3];
-          swap_halves(cw[t][0][0], cw[t][1][0]);
-          swap_halves(cw[t][0][1], cw[t][1][1]);
-          c[t][u] = codes(t, next, u);
-        }
+        for (int u = 0; u < 4; ++u) {
+          const int ku = k + u * W4_UNIT;
+          if (!WHOLE && ku >= k1) break;
+          const bool both = WHOLE || ku + 64 < k1;
+          uint32_t cw[NW][2][2];
 #pragma unroll
-        for (int gr = 0; gr < 2; ++gr) {
-          if (gr && !both) break;
-          bf16x8_t wf[NW][2];
+          for (int t = 0; t < NW; ++t) {
+            cw[t][0][0] = c[t][u][0];
+            cw[t][0][1] = c[t][u][1];
+            cw[t][1][0] = c[t][u][2];
+            cw[t][1][1] = c[t][u][3];
+            swap_halves(cw[t][0][0], cw[t][1][0]);
+            swap_halves(cw[t][0][1], cw[t][1][1]);
+            c[t][u] = codes(t, next, u);
+          }
 #pragma unroll
-          for (int t = 0; t < NW; ++t)
+          for (int gr = 0; gr < 2; ++gr) {
+            if (gr && !both) break;
+            bf16x8_t wf[NW][2];
 #pragma unroll
-            for (int st = 0; st < 2; ++st) wf[t][st] = codes8(cw[t][gr][st], cb);
+            for (int t = 0; t < NW; ++t)
 #pragma unroll
-          for (int n = 0; n < NX; ++n) {
-            bf16x8_t xf[XP][2];
+              for (int st = 0; st < 2; ++st) wf[t][st] = codes8(cw[t][gr][st], cb);
 #pragma unroll
-            for (int q = 0; q < XP; ++q)
-#pragma unroll
-              for (int st = 0; st < 2; ++st)
-                xf[q][st] = *reinterpret_cast<const bf16x8_t *>(
-                    x0[n] + q * p.rows * stride + (ku - k0 + gr * 64 + st * 8) * 2);
-            f32x4_t off = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int q = 0; q < XP; ++q)
-#pragma unroll
-              for (int st = 0; st < 2; ++st)
-                off = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[q][st], m16, off, 0, 0, 0);
-#pragma unroll
-            for (int t = 0; t < NW; ++t) {
-              f32x4_t s = off;
+            for (int n = 0; n < NX; ++n) {
+              bf16x8_t xf[XP][2];
 #pragma unroll
               for (int q = 0; q < XP; ++q)
 #pragma unroll
                 for (int st = 0; st < 2; ++st)
-                  s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[q][st], wf[t][st], s, 0, 0, 0);
-              const uint32_t m = gr ? mb[t][u] : ma[t][u];
-              const float zero = -0.0625f * zero_of(m);
+                  xf[q][st] = *reinterpret_cast<const bf16x8_t *>(
+                      x0[n] + q * p.rows * stride + (ku - k0 + gr * 64 + st * 8) * 2);
+              const f32x4_t off = *reinterpret_cast<const f32x4_t *>(
+                  s_sum + ((ku - k0) / 64 + gr) * XR + n * 16 + 4 * g);
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                y[t][n][i] = fmaf(scale_of(m), s[i], fmaf(zero, off[i], y[t][n][i]));
+              for (int t = 0; t < NW; ++t) {
+                f32x4_t s = off;
+#pragma unroll
+                for (int q = 0; q < XP; ++q)
+#pragma unroll
+                  for (int st = 0; st < 2; ++st)
+                    s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[q][st], wf[t][st], s, 0, 0, 0);
+                const uint32_t m = gr ? mb[t][u] : ma[t][u];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[t][n][i] = fmaf(scale_of(m), s[i], y[t][n][i]);
+              }
             }
           }
         }
-      }
+      };
+      if (UNITS_WHOLE && k + W4_RUN <= k1) units(std::true_type{});
+      else units(std::false_type{});
     }
   }
   // y[t][n][i]: row 16 n + 4 g + i of output lr of tile t
   if (p.wk > 1) {  // the waves of a tile in order, through LDS
     constexpr int ST = 17, SIZE = NW * NX * 16 * ST;
-    float *s_y = reinterpret_cast<float *>(s_x + (size_t)XP * p.rows * stride);
+    float *s_y = s_sum + p.slice * (W4_RUN / 64) * XR;
     float *mine = s_y + wave * SIZE;
 #pragma unroll
     for (int t = 0; t < NW; ++t)
@@ -251,7 +330,18 @@ __global__ __launch_bounds__(512, 2) void k_w4(W4Args a, W4Plan p, int row0, flo
   }
 }
 
-// The slices' sums in order, and what is made of them.
+// The slices' sums in order, and what is made of them. Eight of them are requested at a time.
+__device__ __forceinline__ float w4_slices(const float *p, size_t all, int slices) {
+  float s = 0.f;
+  for (int q0 = 0; q0 < slices; q0 += 8) {
+    float x[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) x[q] = p[min(q0 + q, slices - 1) * all];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) s += q0 + q < slices ? x[q] : 0.f;
+  }
+  return s;
+}
 __global__ __launch_bounds__(256) void k_w4_sum(W4Args a, int slices, int rows, int row0,
                                                 const float *__restrict__ part) {
   const int wide = a.swiglu ? a.n_out / 2 : a.n_out;
@@ -259,12 +349,8 @@ __global__ __launch_bounds__(256) void k_w4_sum(W4Args a, int slices, int rows, 
   if (id >= (size_t)rows * wide) return;
   const int r = (int)(id / wide), o = (int)(id - (size_t)r * wide);
   const float *p = part + (size_t)r * a.n_out + o;
-  float s = 0.f, u = 0.f;
-  for (int q = 0; q < slices; ++q) s += p[q * all];
-  if (a.swiglu) {
-    for (int q = 0; q < slices; ++q) u += p[q * all + wide];
-    s = silu(s) * u;
-  }
+  float s = w4_slices(p, all, slices);
+  if (a.swiglu) s = silu(s) * w4_slices(p + wide, all, slices);
   w4_put(a, row0 + r, o, s);
 }
 
@@ -272,38 +358,74 @@ __global__ __launch_bounds__(256) void k_w4_sum(W4Args a, int slices, int rows, 
 static int w4_most_rows(int parts) { return parts == 1 ? 64 : 32; }
 static int w4_nw(int rows, bool swiglu) { return swiglu || rows > 16 ? 2 : 1; }
 
-// x's rows of a slice fill at most half a unit's LDS; runs are shared by waves while tiles are too
-// few to fill the units.
+// LDS of a block: x, its sums, and with shared tiles their parts.
+static size_t w4_lds(const W4Plan &p, int nw, int parts) {
+  const int nx = (p.rows + 15) / 16;
+  return (size_t)parts * p.rows * (p.slice * W4_RUN * 2 + 16) +
+         p.slice * (W4_RUN / 64) * 16 * nx * sizeof(float) +
+         (p.wk > 1 ? p.waves * nw * nx * 16 * 17 * sizeof(float) : 0);
+}
+
+// The cut (slices of the reduction, waves of a block, waves that share a tile) whose estimated end is
+// the earliest, in us: a block takes FIXED for its x and its first codes, then its waves' runs at the
+// rate of a unit's instructions or of its share of the memory, whichever is slower, and 1 at least;
+// whole rounds of resident blocks follow each other; slices take another launch.
+//   1 row 3584 -> 4608: 4 of 8 waves a tile 6.9 us, 8 of 8 7.4, 4 of 4 7.4, 2 of 4 7.9, 1 of 4 10.1.
+//   5 rows 5120 -> 55296 (SWIGLU): a wave a tile 36, two 36, blocks of 4 waves 38, 2 slices 40.
+//   33 rows 27648 -> 5120: 18 slices in blocks of 12 waves (one round) 36, of 8 47, 27 slices 47, 54 58.
 static W4Plan w4_plan(int rows, int n_out, int n_in, bool swiglu, int parts) {
-  constexpr int LDS = 72 << 10, WAVES = 8;
-  W4Plan p;
+  constexpr double FIXED = 4, CYCLES = 1300, BYTES = 5.2e6;  // a unit's cycles, all bytes, per us
+  constexpr size_t LDS = 160 << 10;
+  W4Plan p, best;
   p.rows = std::min(rows, w4_most_rows(parts));
-  const int runs = (n_in + W4_RUN - 1) / W4_RUN;
-  const int most = std::max(1, (LDS / (p.rows * parts) - 16) / (W4_RUN * 2));
-  p.slices = (runs + most - 1) / most;
-  p.slice = (runs + p.slices - 1) / p.slices;
-  p.slices = (runs + p.slice - 1) / p.slice;
-  const int per = 16 * w4_nw(rows, swiglu);
-  const long long tiles = (n_out + per - 1) / per;
-  const long long want = 8LL * gemm_cu_count() / std::max(1LL, tiles * p.slices);
-  p.wk = (int)std::max(1LL, std::min<long long>({want, p.slice, WAVES}));
-  const int rounds = (p.slice + p.wk - 1) / p.wk;
-  p.wk = (p.slice + rounds - 1) / rounds;  // as few waves as take these rounds
-  p.waves = WAVES / p.wk * p.wk;
-  return p;
+  const int nw = w4_nw(rows, swiglu), nx = (p.rows + 15) / 16;
+  const int runs = (n_in + W4_RUN - 1) / W4_RUN, cus = gemm_cu_count();
+  const long long tiles = (n_out + 16 * nw - 1) / (16 * nw);
+  // resident waves of a SIMD (by registers), and cycles of a run's instructions
+  const int occ = nx == 1 && (nw == 1 || parts == 1) ? 4 : 3;
+  const double cycles = 4 * (4.0 * (8 + 31 * nw + 9 * nx * nw) + 16.0 * 4 * nx * nw * parts);
+  double least = 1e30;
+  int tried = 0;
+  for (int slices = 1; slices <= runs && tried < 4;) {
+    p.slice = (runs + slices - 1) / slices;
+    p.slices = (runs + p.slice - 1) / p.slice;
+    bool fits = false;
+    for (int waves : {4, 8, 12})
+      for (int wk : {1, 2, 4, 8}) {
+        if (waves % wk || (wk > 1 && wk > p.slice)) continue;
+        p.waves = waves;
+        p.wk = wk;
+        const size_t lds = w4_lds(p, nw, parts);
+        if (lds > LDS) continue;
+        fits = true;
+        const int each = std::max(1, (int)std::min<size_t>(LDS / lds, occ * 4 / waves));
+        const long long blocks = (tiles * wk + waves - 1) / waves * p.slices;
+        const double rounds = std::ceil((double)blocks / (cus * each));
+        const double resident = std::min<double>(each, std::ceil((double)blocks / cus)) * waves;
+        const double run = std::max(
+            {1.0, cycles * std::max(1.0, resident / 4) / CYCLES,
+             resident * std::min<double>(cus, blocks) * nw * 16 * W4_RUN * 0.5625 / BYTES});
+        const double walk = (p.slice + wk - 1) / wk * run;
+        const double t = rounds * (FIXED + walk) + (wk > 1 ? 0.5 : 0) +
+                         (p.slices > 1 ? 4 + 1e-6 * p.slices * p.rows * n_out : 0);
+        if (t < least) {
+          least = t;
+          best = p;
+        }
+      }
+    tried += fits;
+    slices = p.slice > 1 ? (runs + p.slice - 2) / (p.slice - 1) : runs + 1;
+  }
+  return best;
 }
 
 static size_t w4_part_floats(const W4Plan &p, int n_out) {
   return p.slices > 1 ? (size_t)p.slices * p.rows * n_out : 0;
 }
 
-size_t w4_ws_floats(int rows, int n_out, int n_in) {
+size_t w4_ws_floats(int rows, int n_out, int n_in, bool swiglu, int x_dtype) {
   if (rows == 0 || n_out == 0) return 0;
-  size_t n = 0;
-  for (int parts : {1, 3})
-    for (bool swiglu : {false, true})
-      n = std::max(n, w4_part_floats(w4_plan(rows, n_out, n_in, swiglu, parts), n_out));
-  return n;
+  return w4_part_floats(w4_plan(rows, n_out, n_in, swiglu, x_dtype == AKVS_BF16 ? 1 : 3), n_out);
 }
 
 template <int NW, int NX, typename TX, bool SWIGLU>
@@ -313,8 +435,7 @@ static hipError_t w4_launch(const W4Args &a, const W4Plan &p, int row0, float *p
   const int per = 16 * (SWIGLU ? NW / 2 : NW) * (p.waves / p.wk);
   const int wide = SWIGLU ? a.n_out / 2 : a.n_out;
   const dim3 g((wide + per - 1) / per, p.slices), b(64 * p.waves);
-  const size_t lds = (size_t)XP * p.rows * (p.slice * W4_RUN * 2 + 16) +
-                     (p.wk > 1 ? p.waves * NW * NX * 16 * 17 * sizeof(float) : 0);
+  const size_t lds = w4_lds(p, NW, XP);
   hipLaunchKernelGGL((k_w4<NW, NX, TX, SWIGLU>), g, b, lds, st, a, p, row0, part);
   return hipGetLastError();
 }

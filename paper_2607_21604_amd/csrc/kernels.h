@@ -293,7 +293,8 @@ struct W4Args {
   long long ldy;
   int y_dtype;
 };
-size_t w4_ws_floats(int rows, int n_out, int n_in);
+// floats of `ws` that launch_w4 needs
+size_t w4_ws_floats(int rows, int n_out, int n_in, bool swiglu, int x_dtype);
 hipError_t launch_w4(const W4Args &a, float *ws, hipStream_t st);
 // ---- k_decode.hip -------------------------------------------------------------------
 // Matrix-vector products of one token, y = W x (W [N][K], K a multiple of 8), item i of

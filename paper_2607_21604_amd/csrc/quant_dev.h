@@ -20,6 +20,11 @@ __device__ __forceinline__ float oct_min(float x) {
   x = fminf(x, dpp_f32<0x4E>(x));
   return fminf(x, dpp_f32<0x141>(x));
 }
+__device__ __forceinline__ float oct_sum(float x) {
+  x += dpp_f32<0xB1>(x);
+  x += dpp_f32<0x4E>(x);
+  return x + dpp_f32<0x141>(x);
+}
 
 // Quotient rounded to an integer code 0..levels (rne), from v = x - zero.
 __device__ __forceinline__ uint32_t int_code(float tq, float levels) {
