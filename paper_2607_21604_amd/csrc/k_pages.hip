@@ -67,10 +67,16 @@ __device__ __forceinline__ void paged_places(const PagedBatch &s, const PagePool
   __syncthreads();
 }
 
-// A thread has an octet of a row's keys and values each; a block's rows make 4096 octets at most.
-// Bound by the bytes where there are many rows; 16 rows take a launch.
-constexpr int PG_BLOCK_OCTETS = 1024;
-static int rows_per_block(int octets) { return std::max(1, PG_BLOCK_OCTETS / octets); }
+// An item is an octet of a row's keys and values both; a block's rows make 1024 of them at most, a
+// thread has those that are 256 apart. Few rows take blocks of one item a thread, whose loads are
+// made before the row's place is known: 16 rows are bound by round trips to memory (request ->
+// sequence -> length, table -> page), many rows by their bytes (16128 rows of 8 heads of 128: 28 us
+// to store, 4.7 TB/s, 28 to load as fp32, 6.0 TB/s).
+constexpr int PG_ITEMS = 4;  // of a thread, at most
+static int rows_per_block(int n_rows, int items) {
+  const int most = std::max(1, PG_ITEMS * 256 / items), least = std::max(1, 256 / items);
+  return std::min(256, std::max(least, std::min(most, n_rows / (2 * gemm_cu_count()))));
+}
 
 template <int HD>
 __global__ __launch_bounds__(256) void k_store_pages(PagedBatch s, PagePool p,
@@ -79,16 +85,21 @@ __global__ __launch_bounds__(256) void k_store_pages(PagedBatch s, PagePool p,
                                                      int hkv, int rows) {
   constexpr int OH = HD / 8;  // octets of a head
   __shared__ Place places[256];
-  const int R0 = blockIdx.x * rows, octets = hkv * OH;
+  const int R0 = blockIdx.x * rows, octets = hkv * OH, n = min(rows, s.n_rows - R0) * octets;
+  float k[8], v[8];
+  auto read = [&](int o) {
+    const int i = o / octets, e = o - i * octets;
+    load8(K + (R0 + i) * ldk + e * 8, k);
+    load8(V + (R0 + i) * ldv + e * 8, v);
+  };
+  if ((int)threadIdx.x < n) read(threadIdx.x);
   paged_places(s, p, R0, rows, places);
-  for (int o = threadIdx.x; o < rows * octets; o += 256) {
+  for (int o = threadIdx.x; o < n; o += 256) {
     const int i = o / octets, e = o - i * octets, h = e / OH, c = e % OH;
+    if (o >= 256) read(o);
     const Place at = places[i];
     if (at.page < 0) continue;  // (the same for the 8 lanes of a group)
     const size_t row = (((size_t)at.page * hkv + h) << p.shift) + at.at;
-    float k[8], v[8];
-    load8(K + (R0 + i) * ldk + e * 8, k);
-    load8(V + (R0 + i) * ldv + e * 8, v);
     uint32_t w, meta;
     u4_octet(k, w, meta);
     reinterpret_cast<uint32_t *>(p.k)[row * OH + c] = w;
@@ -102,37 +113,33 @@ __global__ __launch_bounds__(256) void k_store_pages(PagedBatch s, PagePool p,
 template <int HD, typename TO>
 __device__ __forceinline__ void load_octet(const uint8_t *codes, const uint32_t *meta, size_t row,
                                            int c, bool there, TO *out) {
-  float x[8];
-  if (there) cache_load8(codes, reinterpret_cast<const _Float16 *>(meta), AKVS_U4G64, row, HD, c * 8, x);
-  else
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = 0.f;
+  float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if (there)
+    cache_load8(codes, reinterpret_cast<const _Float16 *>(meta), AKVS_U4G64, row, HD, c * 8, x);
   store8(out, x);
 }
-
 template <int HD, typename TO>
 __global__ __launch_bounds__(256) void k_load_pages(PagedBatch s, PagePool p, int hkv, int rows,
                                                     TO *__restrict__ K, TO *__restrict__ V) {
   constexpr int OH = HD / 8;
   __shared__ Place places[256];
-  const int R0 = blockIdx.x * rows, octets = hkv * OH;
+  const int R0 = blockIdx.x * rows, octets = hkv * OH, n = min(rows, s.n_rows - R0) * octets;
   paged_places(s, p, R0, rows, places);
-  for (int o = threadIdx.x; o < rows * octets; o += 256) {
+  for (int o = threadIdx.x; o < n; o += 256) {
     const int i = o / octets, e = o - i * octets, h = e / OH, c = e % OH;
     const Place at = places[i];
     if (at.page == -2) continue;
-    const bool there = at.page >= 0;
     const size_t row = (((size_t)max(at.page, 0) * hkv + h) << p.shift) + at.at;
     const size_t to = ((size_t)(R0 + i) * octets + e) * 8;
-    if (K) load_octet<HD>(p.k, p.k_meta, row, c, there, K + to);
-    if (V) load_octet<HD>(p.v, p.v_meta, row, c, there, V + to);
+    if (K) load_octet<HD>(p.k, p.k_meta, row, c, at.page >= 0, K + to);
+    if (V) load_octet<HD>(p.v, p.v_meta, row, c, at.page >= 0, V + to);
   }
 }
 
 hipError_t launch_store_pages(const PagedBatch &s, const PagePool &p, const void *k, long long ldk,
                               const void *v, long long ldv, int hkv, int hd, hipStream_t st) {
   if (s.n_rows == 0 || p.n_pages == 0) return hipSuccess;
-  const int rows = std::min(256, rows_per_block(hkv * hd / 8));
+  const int rows = rows_per_block(s.n_rows, hkv * hd / 8);
   const dim3 g((s.n_rows + rows - 1) / rows), b(256);
   auto x = [](const void *a) { return reinterpret_cast<const bf16_t *>(a); };
   if (hd == 128)
@@ -145,7 +152,7 @@ hipError_t launch_store_pages(const PagedBatch &s, const PagePool &p, const void
 hipError_t launch_load_pages(const PagedBatch &s, const PagePool &p, int hkv, int hd, void *k,
                              void *v, int dtype, hipStream_t st) {
   if (s.n_rows == 0 || (!k && !v)) return hipSuccess;
-  const int rows = std::min(256, rows_per_block(hkv * hd / 8));
+  const int rows = rows_per_block(s.n_rows, hkv * hd / 8);
   const dim3 g((s.n_rows + rows - 1) / rows), b(256);
 #define AKVS_LOAD(HD_, T_)                                                                     \
   hipLaunchKernelGGL((k_load_pages<HD_, T_>), g, b, 0, st, s, p, hkv, rows,                    \
@@ -207,8 +214,8 @@ __global__ __launch_bounds__(256) void k_free_pages(PageTable t, int n, const in
   if (threadIdx.x == 0) t.len[a] = 0;
 }
 
-// Pages are counted in segments of 4096, 16 a thread.
-constexpr int SEG = 4096, SEG_PER = SEG / 256;
+// Pages are counted in segments of 1024, 4 a thread.
+constexpr int SEG_PER = 4, SEG = SEG_PER * 256;
 static int segments(const PageTable &t) { return (t.n_pages + SEG - 1) / SEG; }
 
 __device__ __forceinline__ int wave_sum_int(int x) {
@@ -247,7 +254,7 @@ __device__ __forceinline__ int block_scan(int x, int &total) {
   return before + y - x;
 }
 
-// Bit j: page (segment start + 16 thread + j) is in use; pages past the last are not counted in
+// Bit j: page (segment start + 4 thread + j) is in use; pages past the last are not counted in
 // `there`.
 struct SegBits {
   uint32_t used, there;
@@ -256,14 +263,10 @@ __device__ __forceinline__ SegBits seg_bits(const PageTable &t, int seg) {
   const int id0 = seg * SEG + threadIdx.x * SEG_PER;
   SegBits x{0, 0};
   if (id0 + SEG_PER <= t.n_pages) {
-    const int4 *r = reinterpret_cast<const int4 *>(t.ref + id0);
-#pragma unroll
-    for (int q = 0; q < SEG_PER / 4; ++q) {
-      const int4 v = r[q];
-      x.used |= (uint32_t)(v.x > 0) << (4 * q) | (uint32_t)(v.y > 0) << (4 * q + 1) |
-                (uint32_t)(v.z > 0) << (4 * q + 2) | (uint32_t)(v.w > 0) << (4 * q + 3);
-    }
-    x.there = 0xffffu;
+    const int4 v = *reinterpret_cast<const int4 *>(t.ref + id0);
+    x.used = (uint32_t)(v.x > 0) | (uint32_t)(v.y > 0) << 1 | (uint32_t)(v.z > 0) << 2 |
+             (uint32_t)(v.w > 0) << 3;
+    x.there = 15u;
   } else {
     for (int j = 0; j < SEG_PER && id0 + j < t.n_pages; ++j) {
       x.used |= (uint32_t)(t.ref[id0 + j] > 0) << j;
@@ -445,7 +448,7 @@ __global__ __launch_bounds__(256) void k_compact_rank(PageTable t, int segs, con
   int below = seg_before(count, min(sn, segs));
   if (sn < segs) {
     const int lim = N - (sn * SEG + (int)threadIdx.x * SEG_PER);
-    const uint32_t mask = lim >= SEG_PER ? 0xffffu : lim > 0 ? (1u << lim) - 1 : 0u;
+    const uint32_t mask = lim >= SEG_PER ? 15u : lim > 0 ? (1u << lim) - 1 : 0u;
     below += block_sum(__popc(seg_bits(t, sn).used & mask));
   }
   const int moves = N - below;

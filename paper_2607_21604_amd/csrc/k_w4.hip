@@ -28,7 +28,7 @@ __device__ __forceinline__ int w4_first(int g) { return ((g & 1) << 5) + ((g >> 
 // How a call is cut: a block has `slice` runs of the reduction (of blockIdx.y), its rows of x in
 // LDS, and waves / wk tiles of outputs, whose runs wk waves share.
 struct W4Plan {
-  int waves, wk, slice, slices, rows;  // rows: of x in the block
+  int nw, waves, wk, slice, slices, rows;  // nw: tiles of a wave; rows: of x in the block
 };
 
 __device__ __forceinline__ void w4_put(const W4Args &a, int r, int o, float y) {
@@ -356,14 +356,12 @@ __global__ __launch_bounds__(256) void k_w4_sum(W4Args a, int slices, int rows, 
 
 // Rows in one read of the weights.
 static int w4_most_rows(int parts) { return parts == 1 ? 64 : 32; }
-static int w4_nw(int rows, bool swiglu) { return swiglu || rows > 16 ? 2 : 1; }
-
 // LDS of a block: x, its sums, and with shared tiles their parts.
-static size_t w4_lds(const W4Plan &p, int nw, int parts) {
+static size_t w4_lds(const W4Plan &p, int parts) {
   const int nx = (p.rows + 15) / 16;
   return (size_t)parts * p.rows * (p.slice * W4_RUN * 2 + 16) +
          p.slice * (W4_RUN / 64) * 16 * nx * sizeof(float) +
-         (p.wk > 1 ? p.waves * nw * nx * 16 * 17 * sizeof(float) : 0);
+         (p.wk > 1 ? p.waves * p.nw * nx * 16 * 17 * sizeof(float) : 0);
 }
 
 // The cut (slices of the reduction, waves of a block, waves that share a tile) whose estimated end is
@@ -378,41 +376,45 @@ static W4Plan w4_plan(int rows, int n_out, int n_in, bool swiglu, int parts) {
   constexpr size_t LDS = 160 << 10;
   W4Plan p, best;
   p.rows = std::min(rows, w4_most_rows(parts));
-  const int nw = w4_nw(rows, swiglu), nx = (p.rows + 15) / 16;
+  const int nx = (p.rows + 15) / 16;
   const int runs = (n_in + W4_RUN - 1) / W4_RUN, cus = gemm_cu_count();
-  const long long tiles = (n_out + 16 * nw - 1) / (16 * nw);
-  // resident waves of a SIMD (by registers), and cycles of a run's instructions
-  const int occ = nx == 1 && (nw == 1 || parts == 1) ? 4 : 3;
-  const double cycles = 4 * (4.0 * (8 + 31 * nw + 9 * nx * nw) + 16.0 * 4 * nx * nw * parts);
   double least = 1e30;
   int tried = 0;
   for (int slices = 1; slices <= runs && tried < 4;) {
     p.slice = (runs + slices - 1) / slices;
     p.slices = (runs + p.slice - 1) / p.slice;
     bool fits = false;
-    for (int waves : {4, 8, 12})
-      for (int wk : {1, 2, 4, 8}) {
-        if (waves % wk || (wk > 1 && wk > p.slice)) continue;
-        p.waves = waves;
-        p.wk = wk;
-        const size_t lds = w4_lds(p, nw, parts);
-        if (lds > LDS) continue;
-        fits = true;
-        const int each = std::max(1, (int)std::min<size_t>(LDS / lds, occ * 4 / waves));
-        const long long blocks = (tiles * wk + waves - 1) / waves * p.slices;
-        const double rounds = std::ceil((double)blocks / (cus * each));
-        const double resident = std::min<double>(each, std::ceil((double)blocks / cus)) * waves;
-        const double run = std::max(
-            {1.0, cycles * std::max(1.0, resident / 4) / CYCLES,
-             resident * std::min<double>(cus, blocks) * nw * 16 * W4_RUN * 0.5625 / BYTES});
-        const double walk = (p.slice + wk - 1) / wk * run;
-        const double t = rounds * (FIXED + walk) + (wk > 1 ? 0.5 : 0) +
-                         (p.slices > 1 ? 4 + 1e-6 * p.slices * p.rows * n_out : 0);
-        if (t < least) {
-          least = t;
-          best = p;
+    for (int nw : {1, 2}) {
+      if (swiglu ? nw == 1 : nw == 2 && nx == 1) continue;
+      const long long tiles = (n_out + 16 * nw - 1) / (16 * nw);
+      // resident waves of a SIMD (by registers), and cycles of a run's instructions
+      const int occ = nx == 1 && (nw == 1 || parts == 1) ? 4 : 3;
+      const double cycles = 4 * (4.0 * (8 + 31 * nw + 9 * nx * nw) + 16.0 * 4 * nx * nw * parts);
+      for (int waves : {4, 8, 12})
+        for (int wk : {1, 2, 4, 8}) {
+          if (waves % wk || (wk > 1 && wk > p.slice)) continue;
+          p.nw = nw;
+          p.waves = waves;
+          p.wk = wk;
+          const size_t lds = w4_lds(p, parts);
+          if (lds > LDS) continue;
+          fits = true;
+          const int each = std::max(1, (int)std::min<size_t>(LDS / lds, occ * 4 / waves));
+          const long long blocks = (tiles * wk + waves - 1) / waves * p.slices;
+          const double rounds = std::ceil((double)blocks / (cus * each));
+          const double resident = std::min<double>(each, std::ceil((double)blocks / cus)) * waves;
+          const double run = std::max(
+              {1.0, cycles * std::max(1.0, resident / 4) / CYCLES,
+               resident * std::min<double>(cus, blocks) * nw * 16 * W4_RUN * 0.5625 / BYTES});
+          const double walk = (p.slice + wk - 1) / wk * run;
+          const double t = rounds * (FIXED + walk) + (wk > 1 ? 0.5 : 0) +
+                           (p.slices > 1 ? 4 + 1e-6 * p.slices * p.rows * n_out : 0);
+          if (t < least) {
+            least = t;
+            best = p;
+          }
         }
-      }
+    }
     tried += fits;
     slices = p.slice > 1 ? (runs + p.slice - 2) / (p.slice - 1) : runs + 1;
   }
@@ -435,17 +437,27 @@ static hipError_t w4_launch(const W4Args &a, const W4Plan &p, int row0, float *p
   const int per = 16 * (SWIGLU ? NW / 2 : NW) * (p.waves / p.wk);
   const int wide = SWIGLU ? a.n_out / 2 : a.n_out;
   const dim3 g((wide + per - 1) / per, p.slices), b(64 * p.waves);
-  const size_t lds = w4_lds(p, NW, XP);
+  const size_t lds = w4_lds(p, XP);
   hipLaunchKernelGGL((k_w4<NW, NX, TX, SWIGLU>), g, b, lds, st, a, p, row0, part);
   return hipGetLastError();
 }
 
 template <typename TX, bool SWIGLU>
 static hipError_t w4_rows(const W4Args &a, const W4Plan &p, int row0, float *part, hipStream_t st) {
-  if (p.rows <= 16) return w4_launch<SWIGLU ? 2 : 1, 1, TX, SWIGLU>(a, p, row0, part, st);
+  const int nx = (p.rows + 15) / 16;
+  if (nx == 1) return w4_launch<SWIGLU ? 2 : 1, 1, TX, SWIGLU>(a, p, row0, part, st);
+  if constexpr (!SWIGLU) {
+    if (p.nw == 1) {
+      if constexpr (std::is_same<TX, bf16_t>::value) {
+        if (nx == 3) return w4_launch<1, 3, TX, false>(a, p, row0, part, st);
+        if (nx == 4) return w4_launch<1, 4, TX, false>(a, p, row0, part, st);
+      }
+      return w4_launch<1, 2, TX, false>(a, p, row0, part, st);
+    }
+  }
   if constexpr (std::is_same<TX, bf16_t>::value) {
-    if (p.rows > 32 && p.rows <= 48) return w4_launch<2, 3, TX, SWIGLU>(a, p, row0, part, st);
-    if (p.rows > 48) return w4_launch<2, 4, TX, SWIGLU>(a, p, row0, part, st);
+    if (nx == 3) return w4_launch<2, 3, TX, SWIGLU>(a, p, row0, part, st);
+    if (nx == 4) return w4_launch<2, 4, TX, SWIGLU>(a, p, row0, part, st);
   }
   return w4_launch<2, 2, TX, SWIGLU>(a, p, row0, part, st);
 }
@@ -458,6 +470,7 @@ hipError_t launch_w4(const W4Args &a, float *ws, hipStream_t st) {
   const int most = p.rows;
   for (int row0 = 0; row0 < a.rows; row0 += most) {
     p.rows = std::min(most, a.rows - row0);
+    if (p.rows <= 16 && !a.swiglu) p.nw = 1;  // (the last rows of many)
     hipError_t e = bf ? (a.swiglu ? w4_rows<bf16_t, true>(a, p, row0, part, st)
                                   : w4_rows<bf16_t, false>(a, p, row0, part, st))
                       : (a.swiglu ? w4_rows<float, true>(a, p, row0, part, st)
