@@ -27,6 +27,10 @@ __device__ __forceinline__ bf16x8_t codes8(uint32_t w, CodeBits c) {
   const u32x4_t x = {and_or(w << 3, c), and_or(w >> 1, c), and_or(w >> 5, c), and_or(w >> 9, c)};
   return __builtin_bit_cast(bf16x8_t, x);
 }
+// Two fp16, rounded to nearest even.
+__device__ __forceinline__ uint32_t pack_half2(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){a, b}, f16x2_t));
+}
 // Eight bf16 in that order.
 __device__ __forceinline__ bf16x8_t order8(u32x4_t q) {
   const u32x4_t x = {(q[0] & 0xffffu) | (q[2] << 16), (q[0] >> 16) | (q[2] & 0xffff0000u),
@@ -36,13 +40,17 @@ __device__ __forceinline__ bf16x8_t order8(u32x4_t q) {
 __device__ __forceinline__ float scale_of(uint32_t m) {
   return (float)__builtin_bit_cast(f16x2_t, m)[0];
 }
+// |scale| as the fp16 it is, whose order is that of the integers; 0 where it is not finite.
+__device__ __forceinline__ uint32_t scale_bits(uint32_t m) {
+  const uint32_t x = m & 0x7fffu;
+  return x < 0x7c00u ? x : 0u;
+}
 __device__ __forceinline__ float zero_of(uint32_t m) {
   return (float)__builtin_bit_cast(f16x2_t, m)[1];
 }
 
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
-// scale * code + zero of eight codes in fp16, rounded once: 1024 + c and 1024 + 16 c are fp16 numbers
-// whose low bits are the nibble, c itself is exact. In the order 0, 4, 1, 5, 2, 6, 3, 7.
+// 1024 + c and 1024 + 16 c are fp16 numbers whose low bits are the nibble where it lies.
 struct F16Bits {
   CodeBits lo, hi;
 };
@@ -51,7 +59,14 @@ __device__ __forceinline__ F16Bits f16_bits() {
   x.hi.bits = x.lo.bits;
   return x;
 }
-__device__ __forceinline__ f16x8_t values8(uint32_t w, f16x2_t scale, f16x2_t zero, F16Bits b) {
+// Eight codes as fp16 1024 + c (nibbles 0, 4, 2, 6) and 1024 + 16 c (1, 5, 3, 7), in that order of
+// pairs: 0, 4, 1, 5, 2, 6, 3, 7.
+__device__ __forceinline__ f16x8_t raw8(uint32_t w, F16Bits b) {
+  const u32x4_t x = {and_or(w, b.lo), and_or(w, b.hi), and_or(w >> 8, b.lo), and_or(w >> 8, b.hi)};
+  return __builtin_bit_cast(f16x8_t, x);
+}
+// Eight codes as fp16, exactly, in that order.
+__device__ __forceinline__ f16x8_t exact8(uint32_t w, F16Bits b) {
   const f16x2_t down = {(_Float16)-1024.f, (_Float16)-1024.f};
   const f16x2_t part = {(_Float16)0.0625f, (_Float16)0.0625f};
   const f16x2_t off = {(_Float16)-64.f, (_Float16)-64.f};
@@ -59,15 +74,23 @@ __device__ __forceinline__ f16x8_t values8(uint32_t w, f16x2_t scale, f16x2_t ze
     f16x2_t h[4];
     f16x8_t v;
   } x;
+  x.v = raw8(w, b);
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint32_t u = w >> (8 * i);
-    const f16x2_t lo = __builtin_bit_cast(f16x2_t, and_or(u, b.lo)) + down;
-    const f16x2_t hi = __builtin_elementwise_fma(
-        __builtin_bit_cast(f16x2_t, and_or(u, b.hi)), part, off);
-    x.h[2 * i] = __builtin_elementwise_fma(lo, scale, zero);
-    x.h[2 * i + 1] = __builtin_elementwise_fma(hi, scale, zero);
+  for (int i = 0; i < 4; i += 2) {
+    x.h[i] = x.h[i] + down;
+    x.h[i + 1] = __builtin_elementwise_fma(x.h[i + 1], part, off);
   }
+  return x.v;
+}
+// scale * code + zero in fp16, rounded once.
+__device__ __forceinline__ f16x8_t values8(uint32_t w, f16x2_t scale, f16x2_t zero, F16Bits b) {
+  union {
+    f16x2_t h[4];
+    f16x8_t v;
+  } x;
+  x.v = exact8(w, b);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x.h[i] = __builtin_elementwise_fma(x.h[i], scale, zero);
   return x.v;
 }
 // Elements of that order in their own.

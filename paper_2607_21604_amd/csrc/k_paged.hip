@@ -1,13 +1,14 @@
 // Attention over sequences in pages of 4-bit codes.
 //
 // The (row, query head) pairs of a request that read one KV head are the columns of a matrix, as in
-// the attention over a shared context. Codes go to the matrix cores as they are: a nibble c put
-// into the upper mantissa bits of a bf16 of 16 is 16 + c, exactly, in one instruction for two, and
-// with (scale s, zero z) of a group of 64 elements outside the products
-//   q.k   = sum_groups s (sum q (16 + c) - 16 sum q) + z sum q
-//   sum p v = sum p s (16 + c) - 24 sum p s + sum p (z + 8 s)
-// (p s rounded to bf16 in the first two sums, which together hold p s (c - 8), about as large as
-// the values' deviations; the last one in fp32). Scores hold no rounded operand.
+// the attention over a shared context. Codes go to the matrix cores as they are, with (scale s,
+// zero z) of a group of 64 elements outside the products,
+//   q.k   = sum_groups s (sum q c) + z sum q
+//   sum p v = sum (p s) (c - 8) + sum p (z + 8 s),
+// so that scores hold no rounded operand, and the rounding of p s to fp16 meets what a value
+// differs from its group's middle by. A nibble put into the mantissa of a constant is that constant
+// plus the code, exactly, in one instruction for two; the constants' share is taken off by the
+// matrix cores as well.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -128,15 +129,17 @@ __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
       qs[np][gr] = sum + __shfl_xor(sum, 32, 64);
     }
   }
-  f32x4_t o[NP][DB], ones[NP][NG];  // ones: the sums of the rounded p s, in every element
-  float zs[NP][NG], m_run[NP], l_run[NP];  // (zs, l_run: of this lane's keys)
+  // o: of p s 2^-e (1024 + c), share: what of it is not p s 2^-e (c - 8), in every element; zs, l_run:
+  // of this lane's keys
+  f32x4_t o[NP][DB], share[NP][NG];
+  float zs[NP][NG], m_run[NP], l_run[NP];
 #pragma unroll
   for (int np = 0; np < NP; ++np) {
 #pragma unroll
     for (int db = 0; db < DB; ++db) o[np][db] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int gr = 0; gr < NG; ++gr) {
-      ones[np][gr] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+      share[np][gr] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
       zs[np][gr] = 0.f;
     }
     m_run[np] = -INFINITY;
@@ -157,6 +160,12 @@ __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
     for (int half = 0; half < 2; ++half) sel[st][half] = selector(st, half);
 
   const CodeBits cb = bf16_bits();
+  const F16Bits fb = f16_bits();
+  // p s is fp16 times 2^(P_BITS - e), 2^e being at least the largest scale so far: up to 2^15; what is
+  // lost below fp16's smallest is 2^-32 of the largest (2^-28 at every other key)
+  constexpr float P_BITS = 7.f;
+  uint32_t top = 0;  // the largest scale's bits, and e
+  int e_run = -40;
   char *mem = s_mem + wave * WAVE_BYTES;
   uint32_t *s_km = reinterpret_cast<uint32_t *>(mem + PG_TILE * VST), *s_vm = s_km + NG * PG_TILE;
   const int mask = (1 << p.shift) - 1, last_page = (k1 - 1) >> p.shift;
@@ -231,6 +240,23 @@ __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
   // Values and meta to this wave's LDS (its reads of the tile before are done: in order). Row 16 g +
   // 4 T + i of the values is key 16 T + 4 g + i.
   auto stash = [&](const Tile &t) __attribute__((always_inline)) {
+    uint32_t big = scale_bits(t.vm[0]);  // (infinities and NaN count as nothing)
+    if constexpr (NG == 2) big = max(big, scale_bits(t.vm[1]));
+    if (__ballot(big > top)) {
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) big = max(big, (uint32_t)__shfl_xor((int)big, d, 64));
+      top = big;
+      const int e = max((int)(big >> 10) - 14, -14);  // scale < 2^e
+      const float down = ldexpf(1.f, e_run - max(e, e_run));
+      e_run = max(e, e_run);
+#pragma unroll
+      for (int np = 0; np < NP; ++np) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[np][db] *= down;
+#pragma unroll
+        for (int gr = 0; gr < NG; ++gr) share[np][gr] *= down;
+      }
+    }
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int key = j * VROWS + lane / VC;
@@ -284,7 +310,7 @@ __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
       __builtin_amdgcn_sched_barrier(0);
     }
     const bool masked = key0 + PG_TILE > all_see;
-    bf16x8_t pf[NP][NG][2];
+    f16x8_t pf[NP][NG][2];
 #pragma unroll
     for (int np = 0; np < NP; ++np) {
       const int lim = seen[np] - (key0 + 16 * copy + 4 * g);  // score 4 u + i: key 16 NB u + i of it
@@ -306,22 +332,25 @@ __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
         for (int db = 0; db < DB; ++db) o[np][db] *= alpha;
 #pragma unroll
         for (int gr = 0; gr < NG; ++gr) {
-          ones[np][gr] *= alpha;
+          share[np][gr] *= alpha;
           zs[np][gr] *= alpha;
         }
         l_run[np] *= alpha;
         m_run[np] = m_new;
       }
-      const float m_off = m_run[np] == -INFINITY ? 0.f : m_run[np];  // (no key yet: every p is 0)
+      const float m_off =
+          (m_run[np] == -INFINITY ? 0.f : m_run[np]) - P_BITS;  // (no key yet: every p is 0)
       float pv[NS], ps[NG][NS];
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
         pv[i] = __builtin_amdgcn_exp2f(fmaf(sc[np][i], scale_log2, -m_off));
         l_run[np] += pv[i];
       }
+      // (odd places of the reduction have 16 times the code)
+      const float down[2] = {ldexpf(1.f, -e_run), ldexpf(1.f, -e_run - 4)};
 #pragma unroll
       for (int gr = 0; gr < NG; ++gr) {
-        float sum = 0.f;
+        float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int u = 0; u < NS / 4; ++u) {
           u32x4_t m = *reinterpret_cast<const u32x4_t *>(s_vm + gr * PG_TILE + 16 * (u * NB + copy) +
@@ -333,12 +362,14 @@ __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const float p_ = pv[4 * u + j];
-            ps[gr][4 * u + j] = fmaf(p_, scale_of(m[j]), 0.f);  // (one mixed instruction)
+            // (one mixed instruction each)
+            ps[gr][4 * u + j] = fmaf(p_ * down[j & 1], scale_of(m[j]), 0.f);
             zs[np][gr] = fmaf(p_, zero_of(m[j]), zs[np][gr]);
-            sum += ps[gr][4 * u + j];
+            sum[j & 1] += ps[gr][4 * u + j];
           }
         }
-        zs[np][gr] = fmaf(8.f, sum, zs[np][gr]);
+        // 8 sum p s
+        zs[np][gr] = fmaf(ldexpf(8.f, e_run), fmaf(16.f, sum[1], sum[0]), zs[np][gr]);
       }
       // a step's places: (key i of T = 2 st, key i of 2 st + 1), i = 0..3
 #pragma unroll
@@ -349,51 +380,52 @@ __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
           for (int gr = 0; gr < NG; ++gr)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              x[gr][i] = pack_bf2(ps[gr][8 * st + i], ps[gr][8 * st + 4 + i]);
+              x[gr][i] = pack_half2(ps[gr][8 * st + i], ps[gr][8 * st + 4 + i]);
         } else {
           const int u = NB == 4 ? 0 : st;
           if constexpr (NG == 2) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const uint32_t w = pack_bf2(ps[0][4 * u + i], ps[1][4 * u + i]);
+              const uint32_t w = pack_half2(ps[0][4 * u + i], ps[1][4 * u + i]);
               x[0][i] = __builtin_amdgcn_perm(0u, w, sel[st][0]);
               x[1][i] = __builtin_amdgcn_perm(0u, w, sel[st][1]);
             }
           } else {
 #pragma unroll
             for (int i = 0; i < 4; i += 2) {
-              const uint32_t w = pack_bf2(ps[0][4 * u + i], ps[0][4 * u + i + 1]);
+              const uint32_t w = pack_half2(ps[0][4 * u + i], ps[0][4 * u + i + 1]);
               x[0][i] = __builtin_amdgcn_perm(0u, w, sel[st][0]);
               x[0][i + 1] = __builtin_amdgcn_perm(0u, w, sel[st][1]);
             }
           }
         }
 #pragma unroll
-        for (int gr = 0; gr < NG; ++gr) pf[np][gr][st] = __builtin_bit_cast(bf16x8_t, x[gr]);
+        for (int gr = 0; gr < NG; ++gr) pf[np][gr][st] = __builtin_bit_cast(f16x8_t, x[gr]);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    const bf16x8_t one = __builtin_bit_cast(
-        bf16x8_t, (u32x4_t){0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+    // 1024 + 8 and, of a 16th, 1024 + 128
+    const f16x8_t rest = __builtin_bit_cast(
+        f16x8_t, (u32x4_t){0x64086408u, 0x64806480u, 0x64086408u, 0x64806480u});
 #pragma unroll
     for (int np = 0; np < NP; ++np)
 #pragma unroll
       for (int gr = 0; gr < NG; ++gr)
 #pragma unroll
         for (int st = 0; st < 2; ++st)
-          ones[np][gr] =
-              __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, pf[np][gr][st], ones[np][gr], 0, 0, 0);
+          share[np][gr] =
+              __builtin_amdgcn_mfma_f32_16x16x32_f16(rest, pf[np][gr][st], share[np][gr], 0, 0, 0);
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
       const i32x2_t w = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
           (__attribute__((address_space(3))) i32x2_t *)(mem + lane * VST + db * 8));
 #pragma unroll
       for (int st = 0; st < 2; ++st) {
-        const bf16x8_t vf = codes8((uint32_t)w[st], cb);
+        const f16x8_t vf = raw8((uint32_t)w[st], fb);
 #pragma unroll
         for (int np = 0; np < NP; ++np)
-          o[np][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[np][db / 4][st], o[np][db], 0,
-                                                              0, 0);
+          o[np][db] =
+              __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[np][db / 4][st], o[np][db], 0, 0, 0);
       }
       if (db & 1) __builtin_amdgcn_sched_barrier(0);
     }
@@ -435,14 +467,17 @@ __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
       float z = zs[np][gr];
       z += __shfl_xor(z, 16, 64);
       z += __shfl_xor(z, 32, 64);
-      z = fmaf(-24.f, ones[np][gr][0], z);
+      const float up = ldexpf(1.f, e_run), sh = share[np][gr][0];
 #pragma unroll
-      for (int db = 4 * gr; db < 4 * gr + 4; ++db)
-        *reinterpret_cast<f32x4_t *>(mine + (np * 16 + lr) * OST + db * 16 + 4 * g) =
-            o[np][db] + (f32x4_t){z, z, z, z};
+      for (int db = 4 * gr; db < 4 * gr + 4; ++db) {
+        f32x4_t x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = fmaf(o[np][db][i] - sh, up, z);
+        *reinterpret_cast<f32x4_t *>(mine + (np * 16 + lr) * OST + db * 16 + 4 * g) = x;
+      }
     }
     if (g == 0) {
-      s_m[wave][np * 16 + lr] = m_run[np];
+      s_m[wave][np * 16 + lr] = m_run[np] - P_BITS;
       s_l[wave][np * 16 + lr] = l;
     }
   }
@@ -503,8 +538,9 @@ __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
 }
 
 // Many pairs. Block = 4 waves over 32 * groups pairs (groups 1, 2 or 4) and one chunk of keys. Tiles
-// of 64 keys are turned into fp16 values (rounded once; no key or value of the format lies outside
-// its range) in LDS, from codes loaded two tiles ahead; a wave takes 32 pairs and 32 or 64 of the
+// of 64 keys are put into LDS as fp16, from codes loaded two tiles ahead: the keys' codes, exactly,
+// whose scales and zeros the scores get after the products; the values themselves, rounded once (no
+// value of the format lies outside fp16's range); a wave takes 32 pairs and 32 or 64 of the
 // tile's keys: with 4 groups each wave has a group, with 2 two waves share a group's keys, with
 // 1 two of the waves only load. Scores are formed transposed, S^T = K Q^T (MFMA 32x32x16): lane l
 // holds 16 scores of pair l % 32, the operand layout of O^T = V^T P^T; V^T comes from row-major
@@ -525,6 +561,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
   constexpr int KB = PG_TILE * KST, VB = PG_TILE * VST;
   constexpr float P_BITS = 7.f;
   __shared__ __attribute__((aligned(16))) _Float16 s_kv[2 * (KB + VB)];
+  __shared__ __attribute__((aligned(16))) uint32_t s_km[2][NG][PG_TILE];
   __shared__ int s_odd;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hi = lane >> 5;
   const int G = hq / hkv;
@@ -562,7 +599,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
 
   // the pair's query, its largest element brought to [2^14, 2^15)
   f16x8_t qf[KS];
-  float q_scale = scale_log2;
+  float q_scale = scale_log2, qs[NG];  // qs: its sums over the groups' elements
   {
     const bf16_t *q = Q + ((size_t)r * hq + head) * HD + hi * 8;
     float x[KS][8], big = 0.f;
@@ -578,7 +615,16 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
     const float down = ldexpf(1.f, -e);
     q_scale *= ldexpf(1.f, e);
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)  // (in the order of values8, as the keys are)
+    for (int gr = 0; gr < NG; ++gr) {
+      float sum = 0.f;
+#pragma unroll
+      for (int ks = 4 * gr; ks < 4 * gr + 4; ++ks)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += x[ks][i] * down;
+      qs[gr] = sum + __shfl_xor(sum, 32, 64);
+    }
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)  // (in the order of exact8, as the keys are)
 #pragma unroll
       for (int i = 0; i < 8; ++i) qf[ks][i] = (_Float16)(x[ks][(i & 1) * 4 + i / 2] * down);
   }
@@ -621,14 +667,11 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
         c.vm = 0;
       }
     }
-    f16x2_t m = __builtin_bit_cast(f16x2_t, c.km);
-    f16x2_t sc = {m[0], m[0]}, z = {m[1], m[1]};
 #pragma unroll
     for (int j = 0; j < WORDS; ++j)
-      *reinterpret_cast<f16x8_t *>(ks + j * 8) = values8(c.k[j], sc, z, fb);
-    m = __builtin_bit_cast(f16x2_t, c.vm);
-    sc = (f16x2_t){m[0], m[0]};
-    z = (f16x2_t){m[1], m[1]};
+      *reinterpret_cast<f16x8_t *>(ks + j * 8) = exact8(c.k[j], fb);
+    if ((kq & (4 / NG - 1)) == 0) s_km[buf][kq * NG / 4][krow] = c.km;
+    const f16x2_t m = __builtin_bit_cast(f16x2_t, c.vm), sc = {m[0], m[0]}, z = {m[1], m[1]};
     words_t w = c.v;
     const int turn = krow & (WORDS - 1);
 #pragma unroll
@@ -664,14 +707,29 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
       const int sk0 = key0 + st * 32;
       if (sk0 >= k1) break;
       // S^T block: score i is key sk0 + (i / 4) * 8 + hi * 4 + i % 4 of this lane's pair
-      f32x16_t sc;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+      f32x16_t acc[NG], sc;
       const _Float16 *kr = ks_ + (st * 32 + (lane & 31)) * KST + hi * 8;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-        sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-            *reinterpret_cast<const f16x8_t *>(kr + ks * 16), qf[ks], sc, 0, 0, 0);
+      for (int gr = 0; gr < NG; ++gr) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[gr][i] = 0.f;
+#pragma unroll
+        for (int ks = 4 * gr; ks < 4 * gr + 4; ++ks)
+          acc[gr] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+              *reinterpret_cast<const f16x8_t *>(kr + ks * 16), qf[ks], acc[gr], 0, 0, 0);
+      }
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4)
+#pragma unroll
+        for (int gr = 0; gr < NG; ++gr) {
+          const u32x4_t m = *reinterpret_cast<const u32x4_t *>(
+              &s_km[kt & 1][gr][st * 32 + i4 * 8 + hi * 4]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float base = fmaf(zero_of(m[j]), qs[gr], gr == 0 ? 0.f : sc[4 * i4 + j]);
+            sc[4 * i4 + j] = fmaf(scale_of(m[j]), acc[gr][4 * i4 + j], base);
+          }
+        }
       // V^T operand of step t, dims db * 32 + lane % 32: its 8 slots are keys 16 t + 4 hi + 0..3
       // and the same + 8 of the block
       f16x8_t vf[2][DB];

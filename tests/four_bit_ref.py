@@ -48,13 +48,14 @@ def keys_of(pages, table, n):
 
 
 def attention(q, k_pages, v_pages, table, lens, row_start, seq):
-    """dict of out, lse and, per output, what its bound is made of. All tensors on the CPU."""
+    """dict of out, lse and, per output, what its bound is made of (top: at least the largest scale of
+    a value of the sequence). All tensors on the CPU."""
     n, hq, hd = q.shape
     hkv = k_pages[0].shape[1]
     G = hq // hkv
     q = q.double()
     r = {"out": torch.full((n, hq, hd), math.nan, dtype=torch.float64)}
-    for x in ("mass", "coarse", "fine"):
+    for x in ("mass", "coarse", "fine", "top"):
         r[x] = torch.zeros(n, hq, hd, dtype=torch.float64)
     r["lse"] = torch.full((n, hq), math.nan, dtype=torch.float64)
     r["reach"] = torch.zeros(n, hq, dtype=torch.float64)
@@ -81,32 +82,35 @@ def attention(q, k_pages, v_pages, table, lens, row_start, seq):
             r["mass"][i] = (p * x.abs()).sum(0)
             r["coarse"][i] = (p * up(vs).abs() * (up(vc) - 8).abs()).sum(0)
             r["fine"][i] = (p * (40 * up(vs).abs() + up(vz).abs())).sum(0)
+            r["top"][i] = vs.nan_to_num(0, 0, 0).abs().max() + r["mass"][i].nan_to_num(0, 0, 0).max()
             r["reach"][i] = (q[i].abs()[None] * (60 * s.abs() + z.abs())).sum(-1).max(0).values \
                 / math.sqrt(hd)
     return r
 
 
 def score_bound(reach, hd):
-    """Error of a score formed in 32 bits from codes: with x = scale (c - 8) + (zero + 8 scale), c
-    taken as 16 + c less 24, at most 64 products of q and up to 31, and 24 times q's sum, are
-    added per group (66 roundings of up to 55 sum |q|), q's sum itself (64 roundings) is multiplied
-    with 24 scale and zero + 8 scale; scaling, the groups' sum and the logarithm's base are 8 more.
-    reach = sum |q| (60 scale + |zero|): 66 * 55 + 64 * 32 + 8 * 23 = 5862 scale < 100 * 60, and
-    72 |zero| < 100."""
+    """Error of a score formed in 32 bits from codes: x = scale (c + 16) + (zero - 16 scale) with codes
+    taken as 16 + c (or c), at most 64 products of q and up to 31, and 16 times q's sum, are added
+    per group (66 roundings of up to 47 sum |q|), q's sum itself (64 roundings) is multiplied with 16
+    scale and zero; scaling, the groups' sum and the logarithm's base are 8 more. reach = sum |q|
+    (60 scale + |zero|): 66 * 47 + 64 * 16 + 8 * 31 = 4374 scale < 100 * 60, 72 |zero| < 100."""
     return 100 * EPS * reach
 
 
 def out_bound(r, hd, keys):
     """|kernel - definition| of an output. Scores off by d change each probability by a factor
-    within e^+-d, numerator and denominator both; exponentials 2^-22; sums of `keys` terms in 32
-    bits add keys * 2^-24 of what is added: p (16 + c) scale and 24 p scale, p (zero + 8 scale)
-    (fine). p scale is rounded to bf16 for its product with the codes, less 8 (2^-8 coarse; the same
-    numbers are taken for the 24), split keys' outputs to fp16 of their largest (2^-11), and the
-    result to bf16."""
+    within e^+-d, numerator and denominator both; exponentials 2^-22. fp16 rounds (2^-11 each) either
+    p scale, which meets the code less 8 (coarse; the constant's share is taken of the rounded
+    numbers), or p and the value (mass twice), then split keys' outputs. What lies below fp16's
+    smallest is lost, 2^-25 of p scale 2^(7 - e) / 16 at worst with 2^e at most twice the largest
+    scale, times a code of at most 8 from the middle: 2^-25 2^-7 16 8 2 = 2^-24 of the largest scale
+    a key; 2^-32 of a value for p. Sums of `keys` terms in 32 bits add keys * 2^-24 of what is added:
+    p scale (1024 + c) and its share (2100 scale: fine has 40, so 53 of it). The result is rounded
+    to bf16."""
     d = 2 * (score_bound(r["reach"], hd)[..., None] + 2.0 ** -22)
-    tol = (d + 2 * (keys + 24) * EPS) * (r["fine"] + r["mass"]) + 1e-30
-    tol = tol + (2.0 ** -8 * r["coarse"] + 2.0 ** -11 * (r["mass"] + r["coarse"])) * (1 + d)
-    tol = tol + 2.0 ** -24 * r["mass"].amax(-1, keepdim=True)
+    tol = d * r["mass"] + (keys + 24) * EPS * (53 * r["fine"] + r["mass"]) + 1e-30
+    tol = tol + 2.0 ** -11 * (2 * r["coarse"] + 3 * r["mass"]) * (1 + d)
+    tol = tol + keys * 2.0 ** -24 * r["top"]
     return tol + 2.0 ** -8 * (r["out"].abs() + tol)
 
 
