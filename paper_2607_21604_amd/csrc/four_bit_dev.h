@@ -93,11 +93,6 @@ __device__ __forceinline__ f16x8_t values8(uint32_t w, f16x2_t scale, f16x2_t ze
   for (int i = 0; i < 4; ++i) x.h[i] = __builtin_elementwise_fma(x.h[i], scale, zero);
   return x.v;
 }
-// Elements of that order in their own.
-__device__ __forceinline__ f16x8_t unorder8(f16x8_t x) {
-  return __builtin_shufflevector(x, x, 0, 2, 4, 6, 1, 3, 5, 7);
-}
-
 // The upper half of the wave's a against the lower half of its b.
 __device__ __forceinline__ void swap_halves(uint32_t &a, uint32_t &b) {
   const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);

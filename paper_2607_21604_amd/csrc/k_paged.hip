@@ -547,7 +547,7 @@ __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
 // rows by the transposing LDS read. Queries are fp16 scaled by a power of two per pair, the
 // probabilities fp16 times 2^7, so that what is lost below fp16's smallest is 2^-32 of the
 // largest; statistics and outputs are fp32.
-template <int HD>
+template <int HD, bool WIDE>
 __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p, PagedPlan plan,
                                                        const bf16_t *__restrict__ Q, int hq,
                                                        int hkv, float scale_log2,
@@ -597,9 +597,9 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
     return;
   }
 
-  // the pair's query, its largest element brought to [2^14, 2^15)
-  f16x8_t qf[KS];
-  float q_scale = scale_log2, qs[NG];  // qs: its sums over the groups' elements
+  // the pair's query, its largest element brought to [2^7, 2^8)
+  f16x8_t qf[KS], qz;  // qz: the sum over group hi's elements in three fp16 parts, for its zeros
+  float q_scale = scale_log2;
   {
     const bf16_t *q = Q + ((size_t)r * hq + head) * HD + hi * 8;
     float x[KS][8], big = 0.f;
@@ -611,17 +611,23 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
     }
     big = fmaxf(big, __shfl_xor(big, 32, 64));
     int e = 0;
-    if (big > 0.f && big < INFINITY) e = max(__builtin_amdgcn_frexp_expf(big), -100) - 15;
+    if (big > 0.f && big < INFINITY) e = max(__builtin_amdgcn_frexp_expf(big), -100) - 8;
     const float down = ldexpf(1.f, -e);
     q_scale *= ldexpf(1.f, e);
+    float sums[2] = {0.f, 0.f};
 #pragma unroll
     for (int gr = 0; gr < NG; ++gr) {
-      float sum = 0.f;
 #pragma unroll
       for (int ks = 4 * gr; ks < 4 * gr + 4; ++ks)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += x[ks][i] * down;
-      qs[gr] = sum + __shfl_xor(sum, 32, 64);
+        for (int i = 0; i < 8; ++i) sums[gr] += x[ks][i] * down;
+      sums[gr] += __shfl_xor(sums[gr], 32, 64);
+    }
+    float rest = hi ? sums[1] : sums[0];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      qz[i] = i < 3 ? (_Float16)rest : (_Float16)0.f;
+      rest -= (float)qz[i];
     }
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)  // (in the order of exact8, as the keys are)
@@ -644,17 +650,28 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
     uint32_t km, vm;
   };
   const int last_page = (max(k1, 1) - 1) >> p.shift, mask = (1 << p.shift) - 1;
-  auto page_at = [&](int key0) { return table[min((key0 + krow) >> p.shift, last_page)]; };
+  // (WIDE: the tile lies in one page, whose number is read through scalar registers: nothing writes
+  // the table meanwhile)
+  typedef const __attribute__((address_space(4))) int32_t *entries_t;
+  const entries_t entries = (entries_t)(uintptr_t)table;
+  auto page_at = [&](int key0) {
+    if constexpr (WIDE) return entries[min(key0 >> p.shift, last_page)];
+    else return table[min((key0 + krow) >> p.shift, last_page)];
+  };
   auto load = [&](Codes &c, int key0, int page) __attribute__((always_inline)) {
     const bool there = page >= 0 && page < p.n_pages, live = there && key0 + krow < k1;
-    const size_t row =
-        (((size_t)(there ? page : 0) * hkv + h) << p.shift) + ((key0 + krow) & mask);
-    c.k = *reinterpret_cast<const words_t *>(p.k + row * RB + kq * (RB / 4));
-    c.v = *reinterpret_cast<const words_t *>(p.v + row * RB + kq * (RB / 4));
-    const uint32_t km = p.k_meta[row * NG + kq * NG / 4], vm = p.v_meta[row * NG + kq * NG / 4];
+    // rows of the pool's heads: where the tile begins (or this thread's row), and from there
+    const size_t base = (((size_t)(there ? page : 0) * hkv + h) << p.shift) +
+                        ((key0 + (WIDE ? 0 : krow)) & mask);
+    const int row = WIDE ? krow : 0;
+    c.k = *reinterpret_cast<const words_t *>(p.k + base * RB + row * RB + kq * (RB / 4));
+    c.v = *reinterpret_cast<const words_t *>(p.v + base * RB + row * RB + kq * (RB / 4));
+    const uint32_t km = (p.k_meta + base * NG)[row * NG + kq * NG / 4];
+    const uint32_t vm = (p.v_meta + base * NG)[row * NG + kq * NG / 4];
     c.km = live ? km : 0u;
     c.vm = live ? vm : 0u;
   };
+  // Dims are in LDS in the order of values8, 0 4 1 5 2 6 3 7 of every 8, until the end.
   // Values that some pair of the tile must not see take part with probability 0, and 0 * inf is
   // NaN: where such a value is not finite, 0 goes to LDS, and the pairs that do see it get it
   // added at the end. Pieces of the values are written in an order that differs by row, so that
@@ -683,8 +700,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
     }
 #pragma unroll
     for (int j = 0; j < WORDS; ++j)
-      *reinterpret_cast<f16x8_t *>(vs + ((j + turn) & (WORDS - 1)) * 8) =
-          unorder8(values8(w[j], sc, z, fb));
+      *reinterpret_cast<f16x8_t *>(vs + ((j + turn) & (WORDS - 1)) * 8) = values8(w[j], sc, z, fb);
   };
   if (tid == 0) s_odd = 0;
   Codes c;
@@ -708,6 +724,14 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
       if (sk0 >= k1) break;
       // S^T block: score i is key sk0 + (i / 4) * 8 + hi * 4 + i % 4 of this lane's pair
       f32x16_t acc[NG], sc;
+      {  // zeros times the query's sums
+        const uint32_t m = s_km[kt & 1][hi & (NG - 1)][st * 32 + (lane & 31)];
+        const uint32_t z = (m >> 16) | (m & 0xffff0000u);
+        f16x8_t zf = __builtin_bit_cast(f16x8_t, (u32x4_t){z, z & 0xffffu, 0u, 0u});
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+        sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(zf, qz, sc, 0, 0, 0);
+      }
       const _Float16 *kr = ks_ + (st * 32 + (lane & 31)) * KST + hi * 8;
 #pragma unroll
       for (int gr = 0; gr < NG; ++gr) {
@@ -725,10 +749,8 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
           const u32x4_t m = *reinterpret_cast<const u32x4_t *>(
               &s_km[kt & 1][gr][st * 32 + i4 * 8 + hi * 4]);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float base = fmaf(zero_of(m[j]), qs[gr], gr == 0 ? 0.f : sc[4 * i4 + j]);
-            sc[4 * i4 + j] = fmaf(scale_of(m[j]), acc[gr][4 * i4 + j], base);
-          }
+          for (int j = 0; j < 4; ++j)
+            sc[4 * i4 + j] = fmaf(scale_of(m[j]), acc[gr][4 * i4 + j], sc[4 * i4 + j]);
         }
       // V^T operand of step t, dims db * 32 + lane % 32: its 8 slots are keys 16 t + 4 hi + 0..3
       // and the same + 8 of the block
@@ -814,6 +836,21 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
     l = fa * l + fb * l2;
     m_run = mm;
   }
+  // o[db][i] becomes dim db * 32 + (i / 4) * 8 + hi * 4 + i % 4 of the pair (all lanes take part)
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {
+      uint32_t x[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = __float_as_uint(o[db][4 * q4 + j]);
+      swap_halves(x[0], x[1]);
+      swap_halves(x[2], x[3]);
+      o[db][4 * q4] = __uint_as_float(x[0]);
+      o[db][4 * q4 + 1] = __uint_as_float(x[2]);
+      o[db][4 * q4 + 2] = __uint_as_float(x[1]);
+      o[db][4 * q4 + 3] = __uint_as_float(x[3]);
+    }
   if (!valid) return;
   if (s_odd) {  // values left out above that this pair sees
     for (int k = max(k0, all_see); k < seen; ++k) {
@@ -835,7 +872,6 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
       }
     }
   }
-  // o[db][i] is dim db * 32 + (i / 4) * 8 + hi * 4 + i % 4 of the pair
   if (plan.chunks > 1) {
     float big = 0.f;  // the pair's largest finite value
 #pragma unroll
@@ -944,7 +980,8 @@ hipError_t launch_paged_attention(const PagedBatch &s, const PagePool &p, const 
   else AKVS_PAGED(k_paged_few<HD_, NP_, NB_, false>)
 #define AKVS_PAGED_HD(HD_)                                 \
   if (plan.many) {                                         \
-    AKVS_PAGED(k_paged_many<HD_>);                         \
+    if (p.shift >= 6) AKVS_PAGED(k_paged_many<HD_, true>); \
+    else AKVS_PAGED(k_paged_many<HD_, false>);             \
   } else if (plan.pairs == 32) {                           \
     AKVS_PAGED_FEW(HD_, 2, 1);                             \
   } else if (plan.pairs == 16) {                           \
