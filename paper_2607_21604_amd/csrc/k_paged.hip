@@ -19,7 +19,10 @@
 
 namespace akvs {
 
-// Work items of a call: (request, chunk of its keys, pair tile, KV head), KV heads innermost.
+// Work items of a call: (pair tile, chunk of its keys, request, KV head), KV heads innermost. The
+// device deals blocks out to its parts in turn, so the items that may be empty, the last tiles and
+// chunks, are outermost: with them inside, a power of two of them leaves all of the empty ones to
+// the same part (6 requests of up to 4 tiles: half of the device idle, 123 us against 101).
 struct PagedPlan {
   int pairs, tiles, chunks, chunk_keys;  // pairs: of a tile
   bool many;                             // k_paged_many's
@@ -65,9 +68,9 @@ __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
   int id = blockIdx.x;
   const int h = id % hkv;
   id /= hkv;
-  const int tile = id % plan.tiles;
-  id /= plan.tiles;
-  const int chunk = id % plan.chunks, b = id / plan.chunks;
+  const int b = id % s.n_req;
+  id /= s.n_req;
+  const int chunk = id % plan.chunks, tile = id / plan.chunks;
   int r0, r1, len;
   paged_rows(s, b, r0, r1);
   const int32_t *table = paged_keys(s, b, len);
@@ -568,21 +571,21 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
   int id = blockIdx.x;
   const int h = id % hkv;
   id /= hkv;
-  const int tile = id % plan.tiles;
-  id /= plan.tiles;
-  const int chunk = id % plan.chunks, b = id / plan.chunks;
+  const int b = id % s.n_req;
+  id /= s.n_req;
+  const int chunk = id % plan.chunks, tile = id / plan.chunks;
   int r0, r1, len;
   paged_rows(s, b, r0, r1);
   const int32_t *table = paged_keys(s, b, len);
   const int n_pairs = (r1 - r0) * G, v0 = tile * plan.pairs;
   if (v0 >= n_pairs) return;
   auto seen_by = [&](int r) { return max(len - r1 + r + 1, 0); };
+  const int last = min(n_pairs, v0 + plan.pairs) - 1;
   // this wave's pairs and its share of a tile's two 32-key halves
-  const int groups = plan.pairs >> 5;
+  const int groups = last - v0 >= 64 ? 4 : last - v0 >= 32 ? 2 : 1;
   const int group = groups == 4 ? wave : groups == 2 ? wave >> 1 : 0;
   const bool works = groups > 1 || wave < 2;
   const int st0 = groups == 4 ? 0 : wave & 1, st_step = groups == 4 ? 1 : 2;
-  const int last = min(n_pairs, v0 + plan.pairs) - 1;
   const int v = v0 + group * 32 + (lane & 31);
   const bool valid = v <= last;
   const int r = r0 + (valid ? v : v0) / G, head = h * G + (valid ? v : v0) % G;
@@ -595,6 +598,43 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
   if (nkt == 0 && plan.chunks > 1) {
     if (writes && hi == 0) part_ml[prow] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
     return;
+  }
+
+  // A thread has a quarter of a row's codes, keys and values.
+  const int krow = tid >> 2, kq = tid & 3;
+  const F16Bits fb = f16_bits();
+  typedef __attribute__((ext_vector_type(WORDS))) uint32_t words_t;
+  struct Codes {
+    words_t k, v;
+    uint32_t km, vm;
+  };
+  const int last_page = (max(k1, 1) - 1) >> p.shift, mask = (1 << p.shift) - 1;
+  // (WIDE: the tile lies in one page, whose number is read through scalar registers: nothing writes
+  // the table meanwhile)
+  typedef const __attribute__((address_space(4))) int32_t *entries_t;
+  const entries_t entries = (entries_t)(uintptr_t)table;
+  auto page_at = [&](int key0) {
+    if constexpr (WIDE) return entries[min(key0 >> p.shift, last_page)];
+    else return table[min((key0 + krow) >> p.shift, last_page)];
+  };
+  auto load = [&](Codes &c, int key0, int page) __attribute__((always_inline)) {
+    const bool there = page >= 0 && page < p.n_pages, live = there && key0 + krow < k1;
+    // rows of the pool's heads: where the tile begins (or this thread's row), and from there
+    const size_t base = (((size_t)(there ? page : 0) * hkv + h) << p.shift) +
+                        ((key0 + (WIDE ? 0 : krow)) & mask);
+    const int row = WIDE ? krow : 0;
+    c.k = *reinterpret_cast<const words_t *>(p.k + base * RB + row * RB + kq * (RB / 4));
+    c.v = *reinterpret_cast<const words_t *>(p.v + base * RB + row * RB + kq * (RB / 4));
+    const uint32_t km = (p.k_meta + base * NG)[row * NG + kq * NG / 4];
+    const uint32_t vm = (p.v_meta + base * NG)[row * NG + kq * NG / 4];
+    c.km = live ? km : 0u;
+    c.vm = live ? vm : 0u;
+  };
+  Codes c;
+  int page = 0;
+  if (nkt) {
+    load(c, k0, page_at(k0));
+    page = page_at(k0 + PG_TILE);
   }
 
   // the pair's query, its largest element brought to [2^7, 2^8)
@@ -641,36 +681,6 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
     for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;  // (l_run: of this lane's half of the keys)
 
-  // A thread has a quarter of a row's codes, keys and values.
-  const int krow = tid >> 2, kq = tid & 3;
-  const F16Bits fb = f16_bits();
-  typedef __attribute__((ext_vector_type(WORDS))) uint32_t words_t;
-  struct Codes {
-    words_t k, v;
-    uint32_t km, vm;
-  };
-  const int last_page = (max(k1, 1) - 1) >> p.shift, mask = (1 << p.shift) - 1;
-  // (WIDE: the tile lies in one page, whose number is read through scalar registers: nothing writes
-  // the table meanwhile)
-  typedef const __attribute__((address_space(4))) int32_t *entries_t;
-  const entries_t entries = (entries_t)(uintptr_t)table;
-  auto page_at = [&](int key0) {
-    if constexpr (WIDE) return entries[min(key0 >> p.shift, last_page)];
-    else return table[min((key0 + krow) >> p.shift, last_page)];
-  };
-  auto load = [&](Codes &c, int key0, int page) __attribute__((always_inline)) {
-    const bool there = page >= 0 && page < p.n_pages, live = there && key0 + krow < k1;
-    // rows of the pool's heads: where the tile begins (or this thread's row), and from there
-    const size_t base = (((size_t)(there ? page : 0) * hkv + h) << p.shift) +
-                        ((key0 + (WIDE ? 0 : krow)) & mask);
-    const int row = WIDE ? krow : 0;
-    c.k = *reinterpret_cast<const words_t *>(p.k + base * RB + row * RB + kq * (RB / 4));
-    c.v = *reinterpret_cast<const words_t *>(p.v + base * RB + row * RB + kq * (RB / 4));
-    const uint32_t km = (p.k_meta + base * NG)[row * NG + kq * NG / 4];
-    const uint32_t vm = (p.v_meta + base * NG)[row * NG + kq * NG / 4];
-    c.km = live ? km : 0u;
-    c.vm = live ? vm : 0u;
-  };
   // Dims are in LDS in the order of values8, 0 4 1 5 2 6 3 7 of every 8, until the end.
   // Values that some pair of the tile must not see take part with probability 0, and 0 * inf is
   // NaN: where such a value is not finite, 0 goes to LDS, and the pairs that do see it get it
@@ -703,12 +713,6 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
       *reinterpret_cast<f16x8_t *>(vs + ((j + turn) & (WORDS - 1)) * 8) = values8(w[j], sc, z, fb);
   };
   if (tid == 0) s_odd = 0;
-  Codes c;
-  int page = 0;
-  if (nkt) {
-    load(c, k0, page_at(k0));
-    page = page_at(k0 + PG_TILE);
-  }
   __syncthreads();
   if (nkt) {
     store(c, k0, 0);
@@ -719,6 +723,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
   for (int kt = 0; kt < nkt; ++kt) {
     const int key0 = k0 + kt * PG_TILE;
     const _Float16 *ks_ = s_kv + (kt & 1) * (KB + VB), *vs_ = ks_ + KB;
+    __builtin_amdgcn_s_setprio(1);
     for (int st = works ? st0 : 2; st < 2; st += st_step) {
       const int sk0 = key0 + st * 32;
       if (sk0 >= k1) break;
@@ -805,6 +810,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
           o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[t][db], pb, o[db], 0, 0, 0);
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     if (kt + 1 < nkt) {
       store(c, key0 + PG_TILE, (kt + 1) & 1);
       load(c, key0 + 2 * PG_TILE, page);
@@ -920,7 +926,8 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
 // blocks, and what is left of them, follow each other.
 //   32 requests of 4700 to 16000 keys of 40/8 heads: chunks of 8192 keys (one round) 92 us, of 4096
 //   102, of 16384 99; 3 of 91000 to 122000 of 28/4: 2816 (one round) 40, 2560 (a little more) 50,
-//   1536 45, 6144 46.
+//   1536 45, 6144 46; 16 of 3000 to 9000 with 30 pairs each: 3072 keys 94, 4096 66, 8192 115; 16 of
+//   3000 to 19000 with 16 pairs of heads of 64: 3200 (3 blocks a unit) 38, 2432 (4) 32.
 static PagedPlan paged_plan(const PagedBatch &s, int hq, int hkv, int hd) {
   PagedPlan p;
   const int G = hq / hkv;
@@ -928,9 +935,13 @@ static PagedPlan paged_plan(const PagedBatch &s, int hq, int hkv, int hd) {
   p.pairs = pairs <= 4 ? 4 : pairs <= 8 ? 8 : pairs <= 16 ? 16 : pairs <= 32 ? 32 : pairs <= 64 ? 64 : 128;
   p.many = pairs > 32;
   p.tiles = (int)((pairs + p.pairs - 1) / p.pairs);
-  const double FIXED = 7, WALK = p.many ? 3.3 : 2.55, ALONE = 0.6, MOVED = 5e6;
+  const bool single = p.pairs == 32 && hd == 128;  // (registers for one block a unit)
+  const double FIXED = 7, WALK = p.many ? 3.3 : single ? 3.5 : 2.55, ALONE = single ? 1.0 : 0.6,
+               MOVED = 5e6;
   const int kt = (s.limit + PG_TILE - 1) / PG_TILE, unit = p.many ? 1 : 4;
-  const long long slots = gemm_cu_count() * (hd == 64 ? (p.many ? 3LL : 4LL) : 2LL);
+  // (heads of 64, up to 16 pairs: 3 blocks fit a unit, and some are empty)
+  const long long slots =
+      gemm_cu_count() * (single ? 1LL : hd == 128 || p.pairs == 32 ? 2LL : p.many ? 3LL : 4LL);
   // (tiles of a request that has fewer rows than another are empty)
   const double items =
       hkv * std::min((double)s.n_req * p.tiles, (double)s.n_rows * G / p.pairs + 0.5 * s.n_req);
