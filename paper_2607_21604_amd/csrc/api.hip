@@ -2134,6 +2134,9 @@ akvs_status akvs_paged_attention(const void *q, const akvs_paged_cfg *c, const a
   PagedCall x;
   akvs_status st = check_paged_call(m, c, p, &x);
   if (st) return st;
+  REQUIRE(x.s.n_rows == 0 ||
+              paged_blocks(x.s, m->n_q_heads, m->n_kv_heads, m->head_dim) < (1LL << 24),
+          AKVS_ESHAPE, "too many requests of up to %d rows", c->rows_max);
   REQUIRE((q && out) || x.s.n_rows == 0, AKVS_EINVAL, "NULL argument");
   REQUIRE(aligned16(q) && aligned16(out) && aligned16(lse) && aligned16(ws), AKVS_EINVAL,
           "misaligned argument");

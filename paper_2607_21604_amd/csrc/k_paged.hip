@@ -973,6 +973,11 @@ size_t paged_part_floats(const PagedBatch &s, int hq, int hkv, int hd) {
   return p.chunks > 1 ? items * (hd / 2) + items * 4 : 0;
 }
 
+long long paged_blocks(const PagedBatch &s, int hq, int hkv, int hd) {
+  const PagedPlan p = paged_plan(s, hq, hkv, hd);
+  return (long long)s.n_req * p.chunks * p.tiles * hkv;
+}
+
 hipError_t launch_paged_attention(const PagedBatch &s, const PagePool &p, const void *q, int hq,
                                   int hkv, int hd, void *out, float *lse, float *part,
                                   hipStream_t st) {

@@ -380,7 +380,9 @@ static W4Plan w4_plan(int rows, int n_out, int n_in, bool swiglu, int parts) {
   const int runs = (n_in + W4_RUN - 1) / W4_RUN, cus = gemm_cu_count();
   double least = 1e30;
   int tried = 0;
-  for (int slices = 1; slices <= runs && tried < 4;) {
+  // (from about as few slices as their x leaves in LDS)
+  const int held = std::max<int>(1, LDS / ((size_t)parts * p.rows * W4_RUN * 2));
+  for (int slices = (runs + held - 1) / held; slices <= runs && tried < 4;) {
     p.slice = (runs + slices - 1) / slices;
     p.slices = (runs + p.slice - 1) / p.slice;
     bool fits = false;

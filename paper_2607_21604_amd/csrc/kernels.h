@@ -277,6 +277,8 @@ hipError_t launch_move_pages(const PagePool &p, int layers, int hkv, int hd, con
                              hipStream_t st);
 // floats of `part` that launch_paged_attention needs
 size_t paged_part_floats(const PagedBatch &s, int hq, int hkv, int hd);
+// Blocks of a call; a launch takes fewer than 2^24 (2^32 threads).
+long long paged_blocks(const PagedBatch &s, int hq, int hkv, int hd);
 hipError_t launch_paged_attention(const PagedBatch &s, const PagePool &p, const void *q, int hq,
                                   int hkv, int hd, void *out, float *lse, float *part,
                                   hipStream_t st);

@@ -144,6 +144,16 @@ def test_load_arguments(lib):
     assert lib.akvs_load_pages(*args) == akvs.AKVS_EINVAL
 
 
+@pytest.mark.parametrize("kw", [
+    dict(n_req=1 << 16, n_rows=1 << 16, rows_max=1 << 16),  # 2^16 requests of up to 4096 tiles
+    dict(n_req=1 << 20, n_rows=(1 << 24) // 28 - 1, rows_max=400, max_len=640),
+])
+def test_attention_of_too_many_blocks(lib, kw):
+    c = cfg(row_start=FAR[13], **kw)
+    assert lib.akvs_paged_attention(FAR[4], by(c), by(pages()), by(model()), FAR[5], FAR[6], FAR[7],
+                                    1 << 39, None) == akvs.AKVS_ESHAPE
+
+
 def test_attention_arguments(lib):
     m, c, p = by(model()), by(cfg()), by(pages())
     ok = [FAR[4], c, p, m, FAR[5], FAR[6], FAR[7], 1 << 39, None]
