@@ -154,16 +154,8 @@ class Engine:
                                v_cache)
         return q_out, k_cache, v_cache
 
-    def _shared(self, q, k_prefix, k_own, own_len, row_start, rows_max):
-        """The batch that these tensors describe. A row_start that is no tensor is checked, gives
-        rows_max and is copied to the device."""
-        sh, n = self.shape, int(q.shape[0])
-        self._need("q", q, (n, sh.n_q_heads, sh.head_dim))
-        self._need("k_prefix", k_prefix, (None, sh.n_kv_heads, sh.head_dim))
-        cap = 0
-        if k_own is not None:
-            self._need("k_own", k_own, (None, None, sh.n_kv_heads, sh.head_dim))
-            cap = int(k_own.shape[1])
+    def _row_start(self, n, row_start, rows_max, device):
+        """A row_start that is no tensor is checked, gives rows_max and is copied to the device."""
         if row_start is not None and not torch.is_tensor(row_start):
             at = [operator.index(x) for x in row_start]
             rows = [b - a for a, b in zip(at, at[1:])]
@@ -172,7 +164,19 @@ class Engine:
             if rows_max is not None and max(rows) > rows_max:
                 raise ValueError(f"row_start holds a request of {max(rows)} rows, rows_max is {rows_max}")
             rows_max = max(rows)
-            row_start = torch.tensor(at, dtype=torch.int32, device=q.device)
+            row_start = torch.tensor(at, dtype=torch.int32, device=device)
+        return row_start, rows_max
+
+    def _shared(self, q, k_prefix, k_own, own_len, row_start, rows_max):
+        """The batch that these tensors describe."""
+        sh, n = self.shape, int(q.shape[0])
+        self._need("q", q, (n, sh.n_q_heads, sh.head_dim))
+        self._need("k_prefix", k_prefix, (None, sh.n_kv_heads, sh.head_dim))
+        cap = 0
+        if k_own is not None:
+            self._need("k_own", k_own, (None, None, sh.n_kv_heads, sh.head_dim))
+            cap = int(k_own.shape[1])
+        row_start, rows_max = self._row_start(n, row_start, rows_max, q.device)
         if row_start is not None:
             self._need("row_start", row_start, (None,), torch.int32)
             B = int(row_start.numel()) - 1
@@ -268,6 +272,34 @@ class Engine:
         ws = self._scratch(akvs.akvs_evict_workspace_size(self.m, c))
         akvs.akvs_evict_cache(k, v, weights, c, self.m, keep, k_out, v_out, w_out, lens_out, ws)
         return keep, k_out, v_out, w_out, lens_out
+
+    def w4_product(self, x, codes, meta, swiglu: bool = False, resid=None, y=None, y_dtype=None):
+        """x [rows][n_in] (rows may lie apart) times 4-bit weights (quantize_weight), to y
+        [rows][n_out], or with swiglu silu(gate) * up [rows][n_out / 2] of weights whose first half
+        of rows is the gate's; resid (fp32) is added, y may be resid. A y that is not given is
+        made, of y_dtype (the engine's; fp32 with resid). Returns y."""
+        self._need("codes", codes, (None, None), torch.uint8)
+        n_out, n_in = int(codes.shape[0]), 2 * int(codes.shape[1])
+        self._need("meta", meta, (n_out, n_in // 64, 2), torch.float16)
+        if x.dim() != 2:
+            raise ValueError("x: need [rows][n_in]")
+        if resid is not None and (swiglu or (y_dtype if y is None else y.dtype) not in (
+                None, torch.float32)):
+            raise ValueError("resid goes with an fp32 y, without swiglu")
+        if y is None:
+            if y_dtype is None:
+                y_dtype = torch.float32 if resid is not None else self.dtype
+            y = torch.empty((x.shape[0], n_out // 2 if swiglu else n_out), dtype=y_dtype,
+                            device=self.device)
+        for name, t in (("x", x), ("y", y), ("resid", resid)):
+            if t is not None:
+                if t.device.type != self.device.type:
+                    raise ValueError(f"{name} is on {t.device}, not on {self.device.type}")
+                self._here(name, t)
+        ws = self._scratch(akvs.akvs_w4_workspace_size(int(x.shape[0]), n_out, n_in))
+        akvs.akvs_w4_product(x, codes, meta, y,
+                             akvs.AKVS_W4_SWIGLU if swiglu else akvs.AKVS_W4_STORE, resid, ws)
+        return y
 
     def reuse_prefill(self, tokens: torch.Tensor, chunk_lens: Sequence[int], query_len: int,
                       k_cache: torch.Tensor, v_cache: torch.Tensor, refresh=(1, 5),
@@ -375,6 +407,171 @@ def quantize_cache(x: torch.Tensor, bits: int):
     meta = torch.empty(x.shape[:-1] + (hd // 64, 2), dtype=torch.float16, device=x.device)
     akvs.akvs_quantize_cache(x.contiguous(), rows, hd, bits, codes, meta)
     return codes, meta
+
+
+def quantize_weight(w: torch.Tensor):
+    """4-bit copy of a weight [n_out][n_in] (n_in a multiple of 64) for Engine.w4_product:
+    codes uint8 [n_out][n_in / 2], meta fp16 [n_out][n_in / 64][2] (scale, zero)."""
+    if w.dim() != 2 or w.shape[1] % 64:
+        raise ValueError(f"w: need [n_out][n_in], n_in a multiple of 64, got {tuple(w.shape)}")
+    return quantize_cache(w, 4)
+
+
+class PagedCache:
+    """Keys and values of many sequences, in pages of 4-bit codes that sequences may share: pools
+    of all the engine's layers and one table of pages (akvs_pages, akvs_page_table). Everything is
+    allocated here, once: the methods that follow run on the current stream without a host
+    synchronisation and can be captured. Sequences (`seq`, `src`, `dst`) are given as ints, which
+    are checked and copied to the device, or (as under capture) as an int32 tensor, whose entries
+    out of range the device leaves out."""
+
+    def __init__(self, engine: Engine, n_seq: int, max_len: int, n_pages: int, page_rows: int = 64):
+        if min(n_seq, max_len) < 1 or n_pages < 0 or page_rows not in (16, 32, 64, 128, 256):
+            raise ValueError("need n_seq, max_len >= 1, n_pages >= 0 and pages of 16 to 256 rows")
+        sh, dev = engine.shape, engine.device
+        self.engine, self.page_rows, self.n_seq = engine, page_rows, n_seq
+        max_pages = -(-max_len // page_rows)
+        self.max_len = max_pages * page_rows  # keys a sequence can have
+        rows = (engine.n_layers, n_pages, sh.n_kv_heads, page_rows)
+        self.k, self.v = (torch.zeros(rows + (sh.head_dim // 2,), dtype=torch.uint8, device=dev)
+                          for _ in range(2))
+        self.k_meta, self.v_meta = (torch.zeros(rows + (sh.head_dim // 64, 2), dtype=torch.float16,
+                                                device=dev) for _ in range(2))
+        self.table = torch.full((n_seq, max_pages), -1, dtype=torch.int32, device=dev)
+        self.len = torch.zeros(n_seq, dtype=torch.int32, device=dev)
+        self.ref = torch.zeros(n_pages, dtype=torch.int32, device=dev)
+        self.t = akvs.page_table(self.table, self.len, self.ref, page_rows)
+        self.layers = [akvs.pages(*x) for x in zip(self.k, self.v, self.k_meta, self.v_meta)]
+
+    def _layer(self, layer):
+        if not 0 <= layer < len(self.layers):
+            raise ValueError(f"layer {layer} of {len(self.layers)}")
+        self.engine._here("the cache", self.table)
+        return self.layers[layer]
+
+    def _seq(self, name, seq):
+        if not torch.is_tensor(seq):
+            seq = [operator.index(x) for x in seq]
+            if any(not 0 <= x < self.n_seq for x in seq):
+                raise ValueError(f"{name}: need sequences of 0 to {self.n_seq - 1}")
+            seq = torch.tensor(seq, dtype=torch.int32, device=self.engine.device)
+        self.engine._here("the cache", self.table)
+        return self.engine._need(name, seq, (None,), torch.int32)
+
+    def _ints(self, n):
+        return torch.empty(n, dtype=torch.int32, device=self.engine.device)
+
+    def batch(self, n_rows: int, seq=None, row_start=None, rows_max=None, max_len=None):
+        """A batch of n_rows new or last rows of sequences seq (None: of all, in order), request
+        by request; row_start and rows_max as in Engine.shared_attention. max_len: the most keys
+        that a sequence of the batch has when it runs (None: what the cache has room for), which
+        calls are planned for; longer sequences are cut to it. It stays valid while the sequences
+        grow within it."""
+        eng = self.engine
+        if max_len is None:
+            max_len = self.max_len
+        if not 0 <= max_len <= self.max_len:
+            raise ValueError(f"max_len {max_len} outside 0 to {self.max_len}")
+        row_start, rows_max = eng._row_start(n_rows, row_start, rows_max, eng.device)
+        if seq is not None:
+            seq = self._seq("seq", seq)
+            B = int(seq.numel())
+        else:
+            B = self.n_seq if row_start is None else int(row_start.numel()) - 1
+        if B < 1:
+            raise ValueError("a batch of no request")
+        if row_start is not None:
+            eng._need("row_start", row_start, (B + 1,), torch.int32)
+        elif n_rows % B:
+            raise ValueError(f"{n_rows} rows of {B} requests need row_start")
+        if rows_max is None:
+            rows_max = n_rows if row_start is not None else n_rows // B
+        return akvs.paged_cfg(B, n_rows, max(int(rows_max), 1), self.len, self.table, max_len,
+                              row_start, seq)
+
+    def store(self, layer: int, k, v, batch):
+        """New keys and values [rows][Hkv*hd] (columns of a packed projection, or dense
+        [rows][Hkv][hd]) of a batch, whose sequences have grown by them (grow), into one layer's
+        pages. Sequences of the batch must not share the pages that the rows go to: pages that
+        grow gave them are their own."""
+        sh, eng = self.engine.shape, self.engine
+        p = self._layer(layer)
+        for name, x in (("k", k), ("v", v)):
+            if x.dtype != eng.dtype or x.device.type != eng.device.type or (
+                    int(x.shape[0]) != batch.n_rows or
+                    (batch.n_rows and x[0].numel() != sh.n_kv_heads * sh.head_dim)):
+                raise ValueError(f"{name}: need {batch.n_rows} {eng.dtype} rows of "
+                                 f"{sh.n_kv_heads * sh.head_dim}")
+            eng._here(name, x)
+        akvs.akvs_store_pages(k, v, batch, p, eng.m)
+
+    def load(self, layer: int, batch, dtype=None):
+        """What one layer's pages hold for a batch's rows, the last keys of its sequences: (k, v)
+        [rows][Hkv][hd] of dtype (the engine's; torch.float32: scale * code + zero). Rows of no
+        request are 0."""
+        sh, eng = self.engine.shape, self.engine
+        p = self._layer(layer)
+        k = torch.zeros((batch.n_rows, sh.n_kv_heads, sh.head_dim), dtype=dtype or eng.dtype,
+                        device=eng.device)
+        v = torch.zeros_like(k)
+        akvs.akvs_load_pages(batch, p, eng.m, k, v)
+        return k, v
+
+    def attention(self, layer: int, q, batch, out=None, lse=None):
+        """Attention of a batch's rows q [rows][Hq][hd] over their sequences' keys in one layer,
+        each row up to its own key. out may be q. Returns (out, lse)."""
+        sh, eng = self.engine.shape, self.engine
+        p = self._layer(layer)
+        eng._need("q", q, (batch.n_rows, sh.n_q_heads, sh.head_dim))
+        if out is None:
+            out = torch.empty_like(q)
+        if lse is None:
+            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=eng.device)
+        eng._need("out", out, tuple(q.shape))
+        eng._need("lse", lse, tuple(q.shape[:2]), torch.float32)
+        ws = eng._scratch(akvs.akvs_paged_workspace_size(eng.m, batch))
+        akvs.akvs_paged_attention(q, batch, p, eng.m, out, lse, ws)
+        return out, lse
+
+    def fork(self, src, dst):
+        """Empty sequences dst become what src are: they share all pages, until one grows."""
+        src, dst = self._seq("src", src), self._seq("dst", dst)
+        if src.numel() != dst.numel():
+            raise ValueError(f"{src.numel()} sources of {dst.numel()} sequences")
+        akvs.akvs_fork_pages(self.t, src, dst)
+
+    def free(self, seq):
+        """Sequences end; pages that no other has are free."""
+        akvs.akvs_free_pages(self.t, self._seq("seq", seq))
+
+    def grow(self, seq, add):
+        """Room for add keys more (an int for all, ints, or an int32 tensor) in every sequence of
+        seq, with a copy, in all layers, of a last page that is shared. Returns served (int32 per
+        sequence: 1, or 0 where there is no room and the sequence stays as it was)."""
+        seq = self._seq("seq", seq)
+        n, eng = int(seq.numel()), self.engine
+        if not torch.is_tensor(add):
+            add = [operator.index(x) for x in (add if hasattr(add, "__len__") else [add] * n)]
+            if any(x < 0 for x in add):
+                raise ValueError("add: need numbers >= 0")
+            add = torch.tensor(add, dtype=torch.int32, device=eng.device)
+        eng._need("add", add, (n,), torch.int32)
+        served, src, dst, counts = self._ints(n), self._ints(n), self._ints(n), self._ints(2)
+        ws = eng._scratch(akvs.akvs_pages_workspace_size(self.t, n))
+        akvs.akvs_grow_pages(self.t, seq, add, served, src, dst, counts, ws)
+        akvs.akvs_move_pages(self.layers[0], len(self.layers), eng.m, src, dst, n, counts)
+        return served
+
+    def compact(self):
+        """The pages in use move to the lowest numbers, in all layers. Returns counts (int32:
+        pages moved, pages in use)."""
+        eng, n = self.engine, int(self.ref.numel())
+        eng._here("the cache", self.table)
+        src, dst, counts = self._ints(n), self._ints(n), self._ints(2)
+        ws = eng._scratch(akvs.akvs_pages_workspace_size(self.t, 0))
+        akvs.akvs_compact_pages(self.t, self.table, self.ref, src, dst, counts, ws)
+        akvs.akvs_move_pages(self.layers[0], len(self.layers), eng.m, src, dst, n, counts)
+        return counts
 
 
 class BatchGraph:
