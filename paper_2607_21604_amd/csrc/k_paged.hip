@@ -29,8 +29,7 @@ struct PagedPlan {
 };
 constexpr int PG_TILE = 64;  // keys a wave takes at a time
 
-// Few pairs. Block = 4 waves over NP tiles of 16 pairs, or one of 16 / NB, and one chunk of keys; its
-// waves take the chunk's tiles of 64 keys in turn, each with its own maximum, sum and output, merged
+// Few pairs. Block = 4 waves over a tile of 16 / NB pairs and one chunk of keys; its waves take the chunk's tiles of 64 keys in turn, each with its own maximum, sum and output, merged
 // through LDS at the end, so that the loop has no barrier. MFMA 16x16x32, lane l: g = l / 16.
 //   Scores, S^T = K Q^T, 16 keys T = 0..3 of the tile at a time: the lane holds the scores of column
 //   l % 16 at keys 16 T + 4 g .. + 3; the reduction takes elements 64 group + 16 g + 8 step .. + 7.
@@ -42,25 +41,24 @@ constexpr int PG_TILE = 64;  // keys a wave takes at a time
 // and so are a copy's probabilities in the others' places of the reduction.
 // Loads of the next tile, and its pages' numbers (scalar: 16 consecutive keys lie in one page, with
 // WIDE pages of 64 rows or more the tile) a tile earlier, are in flight meanwhile.
-template <int HD, int NP, int NB, bool WIDE>
-__global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
+template <int HD, int NB, bool WIDE>
+__global__ __launch_bounds__(256, 2) void k_paged_few(
     PagedBatch s, PagePool p, PagedPlan plan, const bf16_t *__restrict__ Q, int hq, int hkv,
     float scale_log2, bf16_t *__restrict__ out, float *__restrict__ lse,
     _Float16 *__restrict__ part_o, float4 *__restrict__ part_ml) {
-  static_assert(NP == 1 || NB == 1, "copies of one tile");
   constexpr int NG = HD / 64, DB = HD / 16;      // groups of a row, blocks of 16 dims
   constexpr int RB = HD / 2;                     // bytes of a row's codes
   constexpr int VST = RB + 16;                   // row stride in LDS: reads on all banks
   constexpr int VC = RB / 16;                    // 16-byte chunks of a row
   constexpr int NV = PG_TILE * RB / 1024;        // of these per lane
   constexpr int VROWS = 64 / VC;                 // rows that a load of the wave takes
-  constexpr int COLS = 16 / NB, PAIRS = NP * COLS, NS = 16 / NB;  // NS: a lane's scores of a tile
+  constexpr int COLS = 16 / NB, NS = 16 / NB;  // NS: a lane's scores of a tile
   constexpr int OST = HD + 4;
   constexpr int STAGE = PG_TILE * VST + 2 * NG * PG_TILE * 4;  // of a wave
-  constexpr int MERGE = 16 * NP * OST * 4;
+  constexpr int MERGE = 16 * OST * 4;
   constexpr int WAVE_BYTES = (STAGE > MERGE ? STAGE : MERGE);
   __shared__ __attribute__((aligned(16))) char s_mem[4 * WAVE_BYTES];
-  __shared__ float s_m[4][16 * NP], s_l[4][16 * NP];
+  __shared__ float s_m[4][16], s_l[4][16];
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, lr = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int copy = lr / COLS;  // (NB = 1: 0)
@@ -74,10 +72,10 @@ __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
   int r0, r1, len;
   paged_rows(s, b, r0, r1);
   const int32_t *table = paged_keys(s, b, len);
-  const int n_pairs = (r1 - r0) * G, v0 = tile * PAIRS;
+  const int n_pairs = (r1 - r0) * G, v0 = tile * COLS;
   if (v0 >= n_pairs) return;
   auto seen_by = [&](int r) { return max(len - r1 + r + 1, 0); };
-  const int last = min(n_pairs, v0 + PAIRS) - 1;
+  const int last = min(n_pairs, v0 + COLS) - 1;
   const int k0 = chunk * plan.chunk_keys;
   const int k1 = min(k0 + plan.chunk_keys, seen_by(r0 + last / G));
   const int all_see = min(seen_by(r0 + v0 / G), k1);
@@ -105,49 +103,43 @@ __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
   }
 
   // queries, and their sums over a group's elements
-  bf16x8_t qf[NP][NB][NG][2];
-  float qs[NP][NG];
-  int seen[NP];
+  bf16x8_t qf[NB][NG][2];
+  float qs[NG];
+  int seen;
+  const int v = v0 + lr % COLS;
+  int r, head;
+  place(min(v, last), r, head);
+  seen = v <= last ? min(seen_by(r), k1) : 0;
+  const bf16_t *q = Q + ((size_t)r * hq + head) * HD + g * 16;
 #pragma unroll
-  for (int np = 0; np < NP; ++np) {
-    const int v = v0 + np * 16 + lr % COLS;
-    int r, head;
-    place(min(v, last), r, head);
-    seen[np] = v <= last ? min(seen_by(r), k1) : 0;
-    const bf16_t *q = Q + ((size_t)r * hq + head) * HD + g * 16;
+  for (int gr = 0; gr < NG; ++gr) {
+    float sum = 0.f;
 #pragma unroll
-    for (int gr = 0; gr < NG; ++gr) {
-      float sum = 0.f;
+    for (int st = 0; st < 2; ++st) {
+      const u32x4_t x = *reinterpret_cast<const u32x4_t *>(q + gr * 64 + st * 8);
 #pragma unroll
-      for (int st = 0; st < 2; ++st) {
-        const u32x4_t x = *reinterpret_cast<const u32x4_t *>(q + gr * 64 + st * 8);
+      for (int i = 0; i < 4; ++i)
+        sum += __uint_as_float(x[i] << 16) + __uint_as_float(x[i] & 0xffff0000u);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          sum += __uint_as_float(x[i] << 16) + __uint_as_float(x[i] & 0xffff0000u);
-#pragma unroll
-        for (int c = 0; c < NB; ++c)
-          qf[np][c][gr][st] = order8(NB == 1 || copy == c ? x : (u32x4_t){0, 0, 0, 0});
-      }
-      sum += __shfl_xor(sum, 16, 64);
-      qs[np][gr] = sum + __shfl_xor(sum, 32, 64);
+      for (int c = 0; c < NB; ++c)
+        qf[c][gr][st] = order8(NB == 1 || copy == c ? x : (u32x4_t){0, 0, 0, 0});
     }
+    sum += __shfl_xor(sum, 16, 64);
+    qs[gr] = sum + __shfl_xor(sum, 32, 64);
   }
   // o: of p s 2^-e (1024 + c), share: what of it is not p s 2^-e (c - 8), in every element; zs, l_run:
   // of this lane's keys
-  f32x4_t o[NP][DB], share[NP][NG];
-  float zs[NP][NG], m_run[NP], l_run[NP];
+  f32x4_t o[DB], share[NG];
+  float zs[NG], m_run, l_run;
 #pragma unroll
-  for (int np = 0; np < NP; ++np) {
+  for (int db = 0; db < DB; ++db) o[db] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int db = 0; db < DB; ++db) o[np][db] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int gr = 0; gr < NG; ++gr) {
-      share[np][gr] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-      zs[np][gr] = 0.f;
-    }
-    m_run[np] = -INFINITY;
-    l_run[np] = 0.f;
+  for (int gr = 0; gr < NG; ++gr) {
+    share[gr] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+    zs[gr] = 0.f;
   }
+  m_run = -INFINITY;
+  l_run = 0.f;
   // which half of a word of two bf16 (of two groups, or of two keys) goes to which half of the
   // reduction's places for two T, and which to none: selectors of v_perm_b32
   auto selector = [&](int st, int half) {
@@ -253,12 +245,9 @@ __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
       const float down = ldexpf(1.f, e_run - max(e, e_run));
       e_run = max(e, e_run);
 #pragma unroll
-      for (int np = 0; np < NP; ++np) {
+      for (int db = 0; db < DB; ++db) o[db] *= down;
 #pragma unroll
-        for (int db = 0; db < DB; ++db) o[np][db] *= down;
-#pragma unroll
-        for (int gr = 0; gr < NG; ++gr) share[np][gr] *= down;
-      }
+      for (int gr = 0; gr < NG; ++gr) share[gr] *= down;
     }
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -274,17 +263,15 @@ __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
     __builtin_amdgcn_wave_barrier();
   };
   auto attend = [&](const Tile &t, int key0) __attribute__((always_inline)) {
-    float sc[NP][NS];
+    float sc[NS];
 #pragma unroll
     for (int u = 0; u < 4 / NB; ++u) {
-      f32x4_t c[NP][NG];
+      f32x4_t c[NG];
 #pragma unroll
-      for (int np = 0; np < NP; ++np)
-#pragma unroll
-        for (int gr = 0; gr < NG; ++gr) {
-          const float off = -16.f * qs[np][gr];
-          c[np][gr] = (f32x4_t){off, off, off, off};
-        }
+      for (int gr = 0; gr < NG; ++gr) {
+        const float off = -16.f * qs[gr];
+        c[gr] = (f32x4_t){off, off, off, off};
+      }
 #pragma unroll
       for (int cp = 0; cp < NB; ++cp)
 #pragma unroll
@@ -292,132 +279,122 @@ __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
 #pragma unroll
           for (int st = 0; st < 2; ++st) {
             const bf16x8_t kf = codes8((uint32_t)t.k[u * NB + cp][gr][st], cb);
-#pragma unroll
-            for (int np = 0; np < NP; ++np)
-              c[np][gr] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[np][cp][gr][st], c[np][gr],
-                                                                  0, 0, 0);
+            c[gr] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[cp][gr][st], c[gr], 0, 0, 0);
           }
 #pragma unroll
       for (int gr = 0; gr < NG; ++gr) {
         const u32x4_t m = *reinterpret_cast<const u32x4_t *>(s_km + gr * PG_TILE +
                                                              16 * (u * NB + copy) + 4 * g);
 #pragma unroll
-        for (int np = 0; np < NP; ++np)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float &x = sc[np][4 * u + i];
-            x = fmaf(zero_of(m[i]), qs[np][gr], gr == 0 ? 0.f : x);
-            x = fmaf(scale_of(m[i]), c[np][gr][i], x);
-          }
+        for (int i = 0; i < 4; ++i) {
+          float &x = sc[4 * u + i];
+          x = fmaf(zero_of(m[i]), qs[gr], gr == 0 ? 0.f : x);
+          x = fmaf(scale_of(m[i]), c[gr][i], x);
+        }
       }
       __builtin_amdgcn_sched_barrier(0);
     }
     const bool masked = key0 + PG_TILE > all_see;
-    f16x8_t pf[NP][NG][2];
+    f16x8_t pf[NG][2];
+    const int lim = seen - (key0 + 16 * copy + 4 * g);  // score 4 u + i: key 16 NB u + i of it
+    if (masked) {
 #pragma unroll
-    for (int np = 0; np < NP; ++np) {
-      const int lim = seen[np] - (key0 + 16 * copy + 4 * g);  // score 4 u + i: key 16 NB u + i of it
-      if (masked) {
+      for (int i = 0; i < NS; ++i)
+        if ((i >> 2) * 16 * NB + (i & 3) >= lim) sc[i] = -INFINITY;
+    }
+    float mx = sc[0];
 #pragma unroll
-        for (int i = 0; i < NS; ++i)
-          if ((i >> 2) * 16 * NB + (i & 3) >= lim) sc[np][i] = -INFINITY;
-      }
-      float mx = sc[np][0];
+    for (int i = 1; i < NS; ++i) mx = fmaxf(mx, sc[i]);
+    // the running maximum rises only when some score exceeds it by more than 2^8
+    if (__ballot(mx * scale_log2 > m_run + 8.f)) {
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * scale_log2;
+      const float m_new = fmaxf(m_run, mx);
+      const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
 #pragma unroll
-      for (int i = 1; i < NS; ++i) mx = fmaxf(mx, sc[np][i]);
-      // the running maximum rises only when some score exceeds it by more than 2^8
-      if (__ballot(mx * scale_log2 > m_run[np] + 8.f)) {
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * scale_log2;
-        const float m_new = fmaxf(m_run[np], mx);
-        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[np] - m_new);
-#pragma unroll
-        for (int db = 0; db < DB; ++db) o[np][db] *= alpha;
-#pragma unroll
-        for (int gr = 0; gr < NG; ++gr) {
-          share[np][gr] *= alpha;
-          zs[np][gr] *= alpha;
-        }
-        l_run[np] *= alpha;
-        m_run[np] = m_new;
-      }
-      const float m_off =
-          (m_run[np] == -INFINITY ? 0.f : m_run[np]) - P_BITS;  // (no key yet: every p is 0)
-      float pv[NS], ps[NG][NS];
-#pragma unroll
-      for (int i = 0; i < NS; ++i) {
-        pv[i] = __builtin_amdgcn_exp2f(fmaf(sc[np][i], scale_log2, -m_off));
-        l_run[np] += pv[i];
-      }
-      // (odd places of the reduction have 16 times the code)
-      const float down[2] = {ldexpf(1.f, -e_run), ldexpf(1.f, -e_run - 4)};
+      for (int db = 0; db < DB; ++db) o[db] *= alpha;
 #pragma unroll
       for (int gr = 0; gr < NG; ++gr) {
-        float sum[2] = {0.f, 0.f};
-#pragma unroll
-        for (int u = 0; u < NS / 4; ++u) {
-          u32x4_t m = *reinterpret_cast<const u32x4_t *>(s_vm + gr * PG_TILE + 16 * (u * NB + copy) +
-                                                         4 * g);
-          if (masked) {  // a hidden key's scale and zero may be anything: 0 times them is not taken
-#pragma unroll
-            for (int j = 0; j < 4; ++j) m[j] = 16 * NB * u + j < lim ? m[j] : 0u;
-          }
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float p_ = pv[4 * u + j];
-            // (one mixed instruction each)
-            ps[gr][4 * u + j] = fmaf(p_ * down[j & 1], scale_of(m[j]), 0.f);
-            zs[np][gr] = fmaf(p_, zero_of(m[j]), zs[np][gr]);
-            sum[j & 1] += ps[gr][4 * u + j];
-          }
-        }
-        // 8 sum p s
-        zs[np][gr] = fmaf(ldexpf(8.f, e_run), fmaf(16.f, sum[1], sum[0]), zs[np][gr]);
+        share[gr] *= alpha;
+        zs[gr] *= alpha;
       }
-      // a step's places: (key i of T = 2 st, key i of 2 st + 1), i = 0..3
-#pragma unroll
-      for (int st = 0; st < 2; ++st) {
-        u32x4_t x[NG];
-        if constexpr (NB == 1) {
-#pragma unroll
-          for (int gr = 0; gr < NG; ++gr)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              x[gr][i] = pack_half2(ps[gr][8 * st + i], ps[gr][8 * st + 4 + i]);
-        } else {
-          const int u = NB == 4 ? 0 : st;
-          if constexpr (NG == 2) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t w = pack_half2(ps[0][4 * u + i], ps[1][4 * u + i]);
-              x[0][i] = __builtin_amdgcn_perm(0u, w, sel[st][0]);
-              x[1][i] = __builtin_amdgcn_perm(0u, w, sel[st][1]);
-            }
-          } else {
-#pragma unroll
-            for (int i = 0; i < 4; i += 2) {
-              const uint32_t w = pack_half2(ps[0][4 * u + i], ps[0][4 * u + i + 1]);
-              x[0][i] = __builtin_amdgcn_perm(0u, w, sel[st][0]);
-              x[0][i + 1] = __builtin_amdgcn_perm(0u, w, sel[st][1]);
-            }
-          }
-        }
-#pragma unroll
-        for (int gr = 0; gr < NG; ++gr) pf[np][gr][st] = __builtin_bit_cast(f16x8_t, x[gr]);
-      }
-      __builtin_amdgcn_sched_barrier(0);
+      l_run *= alpha;
+      m_run = m_new;
     }
+    const float m_off =
+        (m_run == -INFINITY ? 0.f : m_run) - P_BITS;  // (no key yet: every p is 0)
+    float pv[NS], ps[NG][NS];
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      pv[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], scale_log2, -m_off));
+      l_run += pv[i];
+    }
+    // (odd places of the reduction have 16 times the code)
+    const float down[2] = {ldexpf(1.f, -e_run), ldexpf(1.f, -e_run - 4)};
+#pragma unroll
+    for (int gr = 0; gr < NG; ++gr) {
+      float sum[2] = {0.f, 0.f};
+#pragma unroll
+      for (int u = 0; u < NS / 4; ++u) {
+        u32x4_t m = *reinterpret_cast<const u32x4_t *>(s_vm + gr * PG_TILE + 16 * (u * NB + copy) +
+                                                       4 * g);
+        if (masked) {  // a hidden key's scale and zero may be anything: 0 times them is not taken
+#pragma unroll
+          for (int j = 0; j < 4; ++j) m[j] = 16 * NB * u + j < lim ? m[j] : 0u;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float p_ = pv[4 * u + j];
+          // (one mixed instruction each)
+          ps[gr][4 * u + j] = fmaf(p_ * down[j & 1], scale_of(m[j]), 0.f);
+          zs[gr] = fmaf(p_, zero_of(m[j]), zs[gr]);
+          sum[j & 1] += ps[gr][4 * u + j];
+        }
+      }
+      // 8 sum p s
+      zs[gr] = fmaf(ldexpf(8.f, e_run), fmaf(16.f, sum[1], sum[0]), zs[gr]);
+    }
+    // a step's places: (key i of T = 2 st, key i of 2 st + 1), i = 0..3
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+      u32x4_t x[NG];
+      if constexpr (NB == 1) {
+#pragma unroll
+        for (int gr = 0; gr < NG; ++gr)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            x[gr][i] = pack_half2(ps[gr][8 * st + i], ps[gr][8 * st + 4 + i]);
+      } else {
+        const int u = NB == 4 ? 0 : st;
+        if constexpr (NG == 2) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t w = pack_half2(ps[0][4 * u + i], ps[1][4 * u + i]);
+            x[0][i] = __builtin_amdgcn_perm(0u, w, sel[st][0]);
+            x[1][i] = __builtin_amdgcn_perm(0u, w, sel[st][1]);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; i += 2) {
+            const uint32_t w = pack_half2(ps[0][4 * u + i], ps[0][4 * u + i + 1]);
+            x[0][i] = __builtin_amdgcn_perm(0u, w, sel[st][0]);
+            x[0][i + 1] = __builtin_amdgcn_perm(0u, w, sel[st][1]);
+          }
+        }
+      }
+#pragma unroll
+      for (int gr = 0; gr < NG; ++gr) pf[gr][st] = __builtin_bit_cast(f16x8_t, x[gr]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
     // 1024 + 8 and, of a 16th, 1024 + 128
     const f16x8_t rest = __builtin_bit_cast(
         f16x8_t, (u32x4_t){0x64086408u, 0x64806480u, 0x64086408u, 0x64806480u});
 #pragma unroll
-    for (int np = 0; np < NP; ++np)
+    for (int gr = 0; gr < NG; ++gr)
 #pragma unroll
-      for (int gr = 0; gr < NG; ++gr)
-#pragma unroll
-        for (int st = 0; st < 2; ++st)
-          share[np][gr] =
-              __builtin_amdgcn_mfma_f32_16x16x32_f16(rest, pf[np][gr][st], share[np][gr], 0, 0, 0);
+      for (int st = 0; st < 2; ++st)
+        share[gr] =
+            __builtin_amdgcn_mfma_f32_16x16x32_f16(rest, pf[gr][st], share[gr], 0, 0, 0);
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
       const i32x2_t w = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
@@ -425,10 +402,8 @@ __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
 #pragma unroll
       for (int st = 0; st < 2; ++st) {
         const f16x8_t vf = raw8((uint32_t)w[st], fb);
-#pragma unroll
-        for (int np = 0; np < NP; ++np)
-          o[np][db] =
-              __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[np][db / 4][st], o[np][db], 0, 0, 0);
+        o[db] =
+            __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[db / 4][st], o[db], 0, 0, 0);
       }
       if (db & 1) __builtin_amdgcn_sched_barrier(0);
     }
@@ -460,29 +435,26 @@ __global__ __launch_bounds__(256, NP == 1 || HD == 64 ? 2 : 1) void k_paged_few(
   // the waves' and copies' parts through LDS: rows of a column's outputs
   __syncthreads();
   float *mine = reinterpret_cast<float *>(mem);
+  float l = l_run;
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
 #pragma unroll
-  for (int np = 0; np < NP; ++np) {
-    float l = l_run[np];
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
+  for (int gr = 0; gr < NG; ++gr) {
+    float z = zs[gr];
+    z += __shfl_xor(z, 16, 64);
+    z += __shfl_xor(z, 32, 64);
+    const float up = ldexpf(1.f, e_run), sh = share[gr][0];
 #pragma unroll
-    for (int gr = 0; gr < NG; ++gr) {
-      float z = zs[np][gr];
-      z += __shfl_xor(z, 16, 64);
-      z += __shfl_xor(z, 32, 64);
-      const float up = ldexpf(1.f, e_run), sh = share[np][gr][0];
+    for (int db = 4 * gr; db < 4 * gr + 4; ++db) {
+      f32x4_t x;
 #pragma unroll
-      for (int db = 4 * gr; db < 4 * gr + 4; ++db) {
-        f32x4_t x;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = fmaf(o[np][db][i] - sh, up, z);
-        *reinterpret_cast<f32x4_t *>(mine + (np * 16 + lr) * OST + db * 16 + 4 * g) = x;
-      }
+      for (int i = 0; i < 4; ++i) x[i] = fmaf(o[db][i] - sh, up, z);
+      *reinterpret_cast<f32x4_t *>(mine + lr * OST + db * 16 + 4 * g) = x;
     }
-    if (g == 0) {
-      s_m[wave][np * 16 + lr] = m_run[np] - P_BITS;
-      s_l[wave][np * 16 + lr] = l;
-    }
+  }
+  if (g == 0) {
+    s_m[wave][lr] = m_run - P_BITS;
+    s_l[wave][lr] = l;
   }
   __syncthreads();
   constexpr int PER = HD / 8;  // lanes of a pair
@@ -919,29 +891,33 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
                  : ((m_run == -INFINITY ? 0.f : m_run) - P_BITS) * 0.6931471805599453f + logf(l);
 }
 
-// Pairs of a request and KV head: up to 32 are k_paged_few's, more k_paged_many's. The keys are cut
-// into the number of chunks whose estimated end is the earliest, taking every sequence to be as
-// long as the longest: a block takes FIXED and WALK per tile that it walks (its waves walk a
-// quarter each in k_paged_few), ALONE of that where it has its unit for itself; whole rounds of
-// blocks, and what is left of them, follow each other.
+// Pairs of a request and KV head: up to 48 are k_paged_few's, in tiles of up to 16 of which each reads
+// the codes (the second from the caches), more k_paged_many's.
+//   16 requests of 3000 to 9000 keys, 40/8 heads: 30 pairs 62 us in two tiles, 73 in one of 32 (256
+//   registers, one block a unit), 81 by k_paged_many; 40 pairs 69 in three and 82; 60 pairs 92 in four
+//   and 83.
+// Up to 8 pairs are there twice, up to 4 of heads of 64 four times (at 128 the queries' copies leave
+// no registers: 32 requests with 3 pairs each 54 us twice, 73 four times; heads of 64, 2 pairs, 57
+// and 53).
+// The keys are cut into the number of chunks whose estimated end is the earliest, taking every
+// sequence to be as long as the longest: a block takes FIXED and WALK per tile that it walks (its
+// waves walk a quarter each in k_paged_few), ALONE of that where it has its unit for itself; whole
+// rounds of blocks, and what is left of them, follow each other.
 //   32 requests of 4700 to 16000 keys of 40/8 heads: chunks of 8192 keys (one round) 92 us, of 4096
 //   102, of 16384 99; 3 of 91000 to 122000 of 28/4: 2816 (one round) 40, 2560 (a little more) 50,
-//   1536 45, 6144 46; 16 of 3000 to 9000 with 30 pairs each: 3072 keys 94, 4096 66, 8192 115; 16 of
-//   3000 to 19000 with 16 pairs of heads of 64: 3200 (3 blocks a unit) 38, 2432 (4) 32.
+//   1536 45, 6144 46; 16 of 3000 to 19000 with 16 pairs of heads of 64: 3200 (3 blocks a unit) 38,
+//   2432 (4) 32.
 static PagedPlan paged_plan(const PagedBatch &s, int hq, int hkv, int hd) {
   PagedPlan p;
   const int G = hq / hkv;
   const long long pairs = (long long)s.rows_max * G;
-  p.pairs = pairs <= 4 ? 4 : pairs <= 8 ? 8 : pairs <= 16 ? 16 : pairs <= 32 ? 32 : pairs <= 64 ? 64 : 128;
-  p.many = pairs > 32;
+  p.pairs = pairs <= 4 && hd == 64 ? 4 : pairs <= 8 ? 8 : pairs <= 48 ? 16 : pairs <= 64 ? 64 : 128;
+  p.many = pairs > 48;
   p.tiles = (int)((pairs + p.pairs - 1) / p.pairs);
-  const bool single = p.pairs == 32 && hd == 128;  // (registers for one block a unit)
-  const double FIXED = 7, WALK = p.many ? 3.3 : single ? 3.5 : 2.55, ALONE = single ? 1.0 : 0.6,
-               MOVED = 5e6;
+  const double FIXED = 7, WALK = p.many ? 3.3 : 2.55, ALONE = 0.6, MOVED = 5e6;
   const int kt = (s.limit + PG_TILE - 1) / PG_TILE, unit = p.many ? 1 : 4;
-  // (heads of 64, up to 16 pairs: 3 blocks fit a unit, and some are empty)
-  const long long slots =
-      gemm_cu_count() * (single ? 1LL : hd == 128 || p.pairs == 32 ? 2LL : p.many ? 3LL : 4LL);
+  // (k_paged_few, heads of 64: 3 blocks fit a unit, and some are empty)
+  const long long slots = gemm_cu_count() * (hd == 128 ? 2LL : p.many ? 3LL : 4LL);
   // (tiles of a request that has fewer rows than another are empty)
   const double items =
       hkv * std::min((double)s.n_req * p.tiles, (double)s.n_rows * G / p.pairs + 0.5 * s.n_req);
@@ -991,26 +967,24 @@ hipError_t launch_paged_attention(const PagedBatch &s, const PagePool &p, const 
   _Float16 *po = reinterpret_cast<_Float16 *>(ml + (size_t)plan.chunks * s.n_rows * hq);
 #define AKVS_PAGED(...)                                                                          \
   hipLaunchKernelGGL((__VA_ARGS__), g, b, 0, st, s, p, plan, Q, hq, hkv, scale, O, lse, po, ml)
-#define AKVS_PAGED_FEW(HD_, NP_, NB_)                            \
-  if (p.shift >= 6) AKVS_PAGED(k_paged_few<HD_, NP_, NB_, true>); \
-  else AKVS_PAGED(k_paged_few<HD_, NP_, NB_, false>)
+#define AKVS_PAGED_FEW(HD_, NB_)                            \
+  if (p.shift >= 6) AKVS_PAGED(k_paged_few<HD_, NB_, true>); \
+  else AKVS_PAGED(k_paged_few<HD_, NB_, false>)
 #define AKVS_PAGED_HD(HD_)                                 \
   if (plan.many) {                                         \
     if (p.shift >= 6) AKVS_PAGED(k_paged_many<HD_, true>); \
     else AKVS_PAGED(k_paged_many<HD_, false>);             \
-  } else if (plan.pairs == 32) {                           \
-    AKVS_PAGED_FEW(HD_, 2, 1);                             \
   } else if (plan.pairs == 16) {                           \
-    AKVS_PAGED_FEW(HD_, 1, 1);                             \
+    AKVS_PAGED_FEW(HD_, 1);                                \
   } else if (plan.pairs == 8) {                            \
-    AKVS_PAGED_FEW(HD_, 1, 2);                             \
-  } else {                                                 \
-    AKVS_PAGED_FEW(HD_, 1, 4);                             \
+    AKVS_PAGED_FEW(HD_, 2);                                \
   }
   if (hd == 128) {
     AKVS_PAGED_HD(128)
   } else {
-    AKVS_PAGED_HD(64)
+    AKVS_PAGED_HD(64) else {
+      AKVS_PAGED_FEW(64, 4);
+    }
   }
 #undef AKVS_PAGED_FEW
 #undef AKVS_PAGED_HD
