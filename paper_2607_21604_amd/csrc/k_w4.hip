@@ -25,11 +25,14 @@ constexpr int W4_RUN = 4 * W4_UNIT; // what a wave takes at a time
 // lane g with elements w4_first(g) .. + 15 of it.
 __device__ __forceinline__ int w4_first(int g) { return ((g & 1) << 5) + ((g >> 1) << 4); }
 
-// How a call is cut: a block has `slice` runs of the reduction (of blockIdx.y), its rows of x in
-// LDS, and waves / wk tiles of outputs, whose runs wk waves share.
+// How a call is cut: a block has `slice` runs of the reduction (of blockIdx.y), its rows of x in LDS
+// for `held` of them at a time, and waves / wk tiles of outputs, whose runs wk waves share.
 struct W4Plan {
-  int nw, waves, wk, slice, slices, rows;  // nw: tiles of a wave; rows: of x in the block
+  int nw, waves, wk, slice, held, slices, rows;  // nw: tiles of a wave; rows: of x in the block
 };
+
+// Octets of x that a thread requests at a time on their way to LDS; parts: of an element.
+constexpr int w4_batch(int parts) { return parts == 1 ? 8 : 4; }
 
 __device__ __forceinline__ void w4_put(const W4Args &a, int r, int o, float y) {
   const size_t at = r * a.ldy + o;
@@ -74,14 +77,14 @@ template <int NW, int NX, typename TX, bool SWIGLU>
 __global__ __launch_bounds__(768, 3) void k_w4(W4Args a, W4Plan p, int row0, float *part) {
   constexpr int XP = std::is_same<TX, float>::value ? 3 : 1;
   constexpr bool UNITS_WHOLE = NX == 1 && NW == 1;
-  extern __shared__ __attribute__((aligned(16))) char s_x[];  // [XP][rows][slice], then sums
+  extern __shared__ __attribute__((aligned(16))) char s_x[];  // [XP][rows][held], then sums
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, lr = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wk = wave % p.wk, wn = wave / p.wk;
   const int wide = SWIGLU ? a.n_out / 2 : a.n_out, groups = a.n_in / 64;
   constexpr int TILES = SWIGLU ? NW / 2 : NW;  // of the result
   const int o0 = (blockIdx.x * (p.waves / p.wk) + wn) * 16 * TILES;
   const int k0 = blockIdx.y * p.slice * W4_RUN, k1 = min(a.n_in, k0 + p.slice * W4_RUN);
-  const int stride = p.slice * W4_RUN * 2 + 16;  // bytes of a row of x
+  const int stride = p.held * W4_RUN * 2 + 16;  // bytes of a row of x
   const uint8_t *w[NW];
   const uint32_t *meta[NW];
 #pragma unroll
@@ -119,9 +122,10 @@ __global__ __launch_bounds__(768, 3) void k_w4(W4Args a, W4Plan p, int row0, flo
       for (int u = 0; u < 4; ++u) c[t][u] = codes(t, k, u);
     }
   }
-  {  // x, its octets row by row, BATCH of a thread requested at a time
-    constexpr int BATCH = XP == 1 ? 8 : 4;
-    const int per = (k1 - k0) / 8, total = p.rows * per, threads = p.waves * 64;
+  // x from element kb to ke, its octets row by row, BATCH of a thread requested at a time
+  auto stage = [&](int kb, int ke) __attribute__((always_inline)) {
+    constexpr int BATCH = w4_batch(XP);
+    const int per = (ke - kb) / 8, total = p.rows * per, threads = p.waves * 64;
     const int rows_on = threads / per, on = threads % per;  // of a thread's next octet
     int r = tid / per, e = tid % per;
     for (int i = tid; i < total; i += BATCH * threads) {
@@ -139,7 +143,7 @@ __global__ __launch_bounds__(768, 3) void k_w4(W4Args a, W4Plan p, int row0, flo
           ++r;
         }
         if (i + b * threads < total)
-          w4_read(reinterpret_cast<const TX *>(a.x) + (row0 + at_r[b]) * a.ldx + k0 + at_e[b] * 8,
+          w4_read(reinterpret_cast<const TX *>(a.x) + (row0 + at_r[b]) * a.ldx + kb + at_e[b] * 8,
                   x[b], v[b]);
       }
 #pragma unroll
@@ -156,7 +160,7 @@ __global__ __launch_bounds__(768, 3) void k_w4(W4Args a, W4Plan p, int row0, flo
             s_sum[at_e[b] / 8 * XR + row] = sum;
       }
     }
-  }
+  };
   f32x4_t y[NW][NX];
 #pragma unroll
   for (int t = 0; t < NW; ++t)
@@ -169,8 +173,8 @@ __global__ __launch_bounds__(768, 3) void k_w4(W4Args a, W4Plan p, int row0, flo
     x0[n] = s_x + min(n * 16 + lr, p.rows - 1) * stride + w4_first(g) * 2;
   // sum zero sum x over a run's eight groups: lane g has the zeros of two, in two bf16 parts (11
   // bits), and takes the sums in three; 2 x 2 places of its eight for each part of the sums
-  auto zeros = [&](int k) __attribute__((always_inline)) {
-    const int gr = (k - k0) / 64 + g * 2;
+  auto zeros = [&](int k, int kb) __attribute__((always_inline)) {
+    const int gr = (k - kb) / 64 + g * 2;
     const bool in0 = k + g * 128 < k1, in1 = k + g * 128 + 64 < k1;
     bf16x8_t zf[NW];
 #pragma unroll
@@ -204,17 +208,23 @@ __global__ __launch_bounds__(768, 3) void k_w4(W4Args a, W4Plan p, int row0, flo
       }
     }
   };
-  __syncthreads();
-  if (live) {
-    for (; k < k1; k += step) {
-      const int next = min(k + step, a.n_in - 1) / W4_RUN * W4_RUN;  // (past the end: any)
+  for (int kb = k0; kb < k1; kb += p.held * W4_RUN) {
+    const int ke = min(k1, kb + p.held * W4_RUN);
+    if (kb > k0) __syncthreads();  // (x of the runs before is read)
+    stage(kb, ke);
+    __syncthreads();
+    if (!live) continue;
+    for (k = kb + wk * W4_RUN; k < ke; k += step) {
+      // the next run of this wave, maybe of the next x; none: any
+      const int then = k + step < ke ? k + step : ke + wk * W4_RUN;
+      const int next = min(then, a.n_in - 1) / W4_RUN * W4_RUN;
       uint32_t ma[NW][4], mb[NW][4];
 #pragma unroll
       for (int t = 0; t < NW; ++t) {
         spread4(md[t].a, ma[t]);
         spread4(md[t].b, mb[t]);
       }
-      zeros(k);
+      zeros(k, kb);
 #pragma unroll
       for (int t = 0; t < NW; ++t) md[t] = metas(t, next);
       // (whole runs without a branch, so that LDS reads go ahead of the products)
@@ -237,7 +247,7 @@ __global__ __launch_bounds__(768, 3) void k_w4(W4Args a, W4Plan p, int row0, flo
           }
           // (the two halves of a line one right after the other: 5 rows 5120 -> 55296 from memory
           // 48 us a unit at a time, 42 in pairs)
-          if ((u & 1) && k + step < k1) {
+          if ((u & 1) && then < k1) {
 #pragma unroll
             for (int t = 0; t < NW; ++t) {
               c[t][u - 1] = codes(t, next, u - 1);
@@ -260,9 +270,9 @@ __global__ __launch_bounds__(768, 3) void k_w4(W4Args a, W4Plan p, int row0, flo
 #pragma unroll
                 for (int st = 0; st < 2; ++st)
                   xf[q][st] = *reinterpret_cast<const bf16x8_t *>(
-                      x0[n] + q * p.rows * stride + (ku - k0 + gr * 64 + st * 8) * 2);
+                      x0[n] + q * p.rows * stride + (ku - kb + gr * 64 + st * 8) * 2);
               const f32x4_t off = *reinterpret_cast<const f32x4_t *>(
-                  s_sum + ((ku - k0) / 64 + gr) * XR + n * 16 + 4 * g);
+                  s_sum + ((ku - kb) / 64 + gr) * XR + n * 16 + 4 * g);
 #pragma unroll
               for (int t = 0; t < NW; ++t) {
                 f32x4_t s = off;
@@ -286,7 +296,7 @@ __global__ __launch_bounds__(768, 3) void k_w4(W4Args a, W4Plan p, int row0, flo
   // y[t][n][i]: row 16 n + 4 g + i of output lr of tile t
   if (p.wk > 1) {  // the waves of a tile in order, through LDS
     constexpr int ST = 17, SIZE = NW * NX * 16 * ST;
-    float *s_y = s_sum + p.slice * (W4_RUN / 64) * XR;
+    float *s_y = s_sum + p.held * (W4_RUN / 64) * XR;
     float *mine = s_y + wave * SIZE;
 #pragma unroll
     for (int t = 0; t < NW; ++t)
@@ -367,68 +377,103 @@ static int w4_most_rows(int parts) { return parts == 1 ? 64 : 32; }
 // LDS of a block: x, its sums, and with shared tiles their parts.
 static size_t w4_lds(const W4Plan &p, int parts) {
   const int nx = (p.rows + 15) / 16;
-  return (size_t)parts * p.rows * (p.slice * W4_RUN * 2 + 16) +
-         p.slice * (W4_RUN / 64) * 16 * nx * sizeof(float) +
+  return (size_t)parts * p.rows * (p.held * W4_RUN * 2 + 16) +
+         p.held * (W4_RUN / 64) * 16 * nx * sizeof(float) +
          (p.wk > 1 ? p.waves * p.nw * nx * 16 * 17 * sizeof(float) : 0);
 }
 
-// The cut (slices of the reduction, waves of a block, waves that share a tile) whose estimated end is
-// the earliest, in us: a block takes FIXED for its x and its first codes, then its waves' runs at the
-// rate of a unit's instructions or of its share of the memory, whichever is slower, and 1 at least;
-// whole rounds of resident blocks follow each other; slices take another launch.
+// The cut (slices of the reduction, runs whose x is held, waves of a block, waves that share a tile)
+// whose estimated end is the earliest, in us: a block takes FIXED, STAGE and a TRIP to memory for every
+// batch of the x that it takes in, then its waves' runs at the rate of a unit's instructions or of its
+// share of the memory, whichever is slower, and 1 at least; whole rounds of resident blocks follow each
+// other; slices take another launch. Few outputs are sliced, to fill the device; many are not, their
+// blocks take x in turns: no partial sums.
 //   1 row 3584 -> 4608: 4 of 8 waves a tile 6.9 us, 8 of 8 7.4, 4 of 4 7.4, 2 of 4 7.9, 1 of 4 10.1.
-//   5 rows 5120 -> 55296 (SWIGLU): a wave a tile 36, two 36, blocks of 4 waves 38, 2 slices 40.
+//   5 rows 5120 -> 55296 (SWIGLU): a wave a tile 41, two 41, blocks of 4 waves 43, 2 slices 46.
+//   64 rows 5120 -> 55296 (SWIGLU): x of 2 runs in 5 turns 83, in 5 slices 101.
+//   17 rows 5120 -> 7168: 4 slices in blocks of 8 waves 14, of 4 waves with two tiles each 20, 2
+//   turns of 5 runs 25.
 //   33 rows 27648 -> 5120: 18 slices in blocks of 12 waves (one round) 36, of 8 47, 27 slices 47, 54 58.
-static W4Plan w4_plan(int rows, int n_out, int n_in, bool swiglu, int parts) {
-  constexpr double FIXED = 4, CYCLES = 1300, BYTES = 5.2e6;  // a unit's cycles, all bytes, per us
+static W4Plan w4_make_plan(int rows, int n_out, int n_in, bool swiglu, int parts, int cus) {
+  constexpr double FIXED = 2.5, STAGE = 1, TRIP = 1.2, CYCLES = 1300, BYTES = 5.2e6;
   constexpr size_t LDS = 160 << 10;
   W4Plan p, best;
   p.rows = std::min(rows, w4_most_rows(parts));
   const int nx = (p.rows + 15) / 16;
-  const int runs = (n_in + W4_RUN - 1) / W4_RUN, cus = gemm_cu_count();
+  const int runs = (n_in + W4_RUN - 1) / W4_RUN;
+  const size_t run_lds = (size_t)parts * p.rows * W4_RUN * 2 + (W4_RUN / 64) * 16 * nx * sizeof(float);
   double least = 1e30;
-  int tried = 0;
-  // (from about as few slices as their x leaves in LDS)
-  const int held = std::max<int>(1, LDS / ((size_t)parts * p.rows * W4_RUN * 2));
-  for (int slices = (runs + held - 1) / held; slices <= runs && tried < 4;) {
+  auto consider = [&](int slices) {
     p.slice = (runs + slices - 1) / slices;
     p.slices = (runs + p.slice - 1) / p.slice;
-    bool fits = false;
     for (int nw : {1, 2}) {
       if (swiglu ? nw == 1 : nw == 2 && nx == 1) continue;
+      p.nw = nw;
       const long long tiles = (n_out + 16 * nw - 1) / (16 * nw);
       // resident waves of a SIMD (by registers), and cycles of a run's instructions
       const int occ = nx == 1 && (nw == 1 || parts == 1) ? 4 : 3;
       const double cycles = 4 * (4.0 * (8 + 31 * nw + 9 * nx * nw) + 16.0 * 4 * nx * nw * parts);
-      for (int waves : {4, 8, 12})
+      for (int waves : {8, 4, 12})  // (8 where the estimate is the same)
         for (int wk : {1, 2, 4, 8}) {
           if (waves % wk || (wk > 1 && wk > p.slice)) continue;
-          p.nw = nw;
           p.waves = waves;
           p.wk = wk;
-          const size_t lds = w4_lds(p, parts);
-          if (lds > LDS) continue;
-          fits = true;
-          const int each = std::max(1, (int)std::min<size_t>(LDS / lds, occ * 4 / waves));
-          const long long blocks = (tiles * wk + waves - 1) / waves * p.slices;
-          const double rounds = std::ceil((double)blocks / (cus * each));
-          const double resident = std::min<double>(each, std::ceil((double)blocks / cus)) * waves;
-          const double run = std::max(
-              {1.0, cycles * std::max(1.0, resident / 4) / CYCLES,
-               resident * std::min<double>(cus, blocks) * nw * 16 * W4_RUN * 0.5625 / BYTES});
-          const double walk = (p.slice + wk - 1) / wk * run;
-          const double t = rounds * (FIXED + walk) + (wk > 1 ? 0.5 : 0) +
-                           (p.slices > 1 ? 4 + 1e-6 * p.slices * p.rows * n_out : 0);
-          if (t < least) {
-            least = t;
-            best = p;
+          p.held = 0;
+          const size_t rest = w4_lds(p, parts);  // beside the x and sums of held runs
+          for (int share : {1, 2}) {             // blocks of a unit that LDS is for
+            if (rest + run_lds > LDS / share) break;
+            const int most = (int)std::min<size_t>(p.slice, (LDS / share - rest) / run_lds);
+            const int times = (p.slice + most - 1) / most;
+            p.held = (p.slice + times - 1) / times;
+            if (p.held < wk) continue;  // (a wave has a run of every x)
+            const size_t lds = rest + p.held * run_lds;
+            const int each = std::max(1, (int)std::min<size_t>(LDS / lds, occ * 4 / waves));
+            const long long blocks = (tiles * wk + waves - 1) / waves * p.slices;
+            const double rounds = std::ceil((double)blocks / (cus * each));
+            const double resident = std::min<double>(each, std::ceil((double)blocks / cus)) * waves;
+            const double run = std::max(
+                {1.0, cycles * std::max(1.0, resident / 4) / CYCLES,
+                 resident * std::min<double>(cus, blocks) * nw * 16 * W4_RUN * 0.5625 / BYTES});
+            // (x's octets, w4_batch of a thread requested at a time)
+            const int threads = waves * 64 * w4_batch(parts);
+            const double stage =
+                STAGE + TRIP * ((p.rows * p.held * (W4_RUN / 8) + threads - 1) / threads);
+            const double walk = (p.slice + wk - 1) / wk * run;
+            const double t = rounds * (FIXED + times * stage + walk) + (wk > 1 ? 0.5 : 0) +
+                             (p.slices > 1 ? 4 + 1e-6 * p.slices * p.rows * n_out : 0);
+            if (t < least) {
+              least = t;
+              best = p;
+            }
+            if (times == 1) break;
           }
         }
     }
-    tried += fits;
+  };
+  // the fewest slices, and from about as few as their x is held whole
+  const int whole = (int)std::max<size_t>(1, LDS / run_lds);
+  int slices = 1;
+  for (int n = 0; n < 8 && slices <= runs; ++n) {
+    if (n == 4) slices = std::max(slices, (runs + whole - 1) / whole);
+    consider(slices);
     slices = p.slice > 1 ? (runs + p.slice - 2) / (p.slice - 1) : runs + 1;
   }
   return best;
+}
+
+// The same, kept per thread for the sizes that come again (1.5 us of a call's 8 otherwise).
+static W4Plan w4_plan(int rows, int n_out, int n_in, bool swiglu, int parts) {
+  struct Known {
+    int rows, n_out, n_in, kind, cus;
+    W4Plan plan;
+  };
+  thread_local Known known[64] = {};
+  rows = std::min(rows, w4_most_rows(parts));  // (what the plan is of)
+  const int kind = 2 * parts + swiglu, cus = gemm_cu_count();
+  Known &k = known[(rows * 7u + n_out / 16 * 3u + n_in / 64 * 5u + kind) % 64];
+  if (k.rows != rows || k.n_out != n_out || k.n_in != n_in || k.kind != kind || k.cus != cus)
+    k = {rows, n_out, n_in, kind, cus, w4_make_plan(rows, n_out, n_in, swiglu, parts, cus)};
+  return k.plan;
 }
 
 static size_t w4_part_floats(const W4Plan &p, int n_out) {

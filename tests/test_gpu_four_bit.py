@@ -627,6 +627,26 @@ def test_w4_swiglu(rows, n_in, n_out, xt, yt):
     assert bool(((y.double().cpu() - want).abs() <= rounded(tol, want, yt)).all())
 
 
+@pytest.mark.parametrize("rows,n_out,xt,swiglu", [(48, 16390, BF, False), (20, 24006, F32, False),
+                                                  (48, 24006, BF, True)])
+def test_w4_of_wide_weights(rows, n_out, xt, swiglu):
+    """Many outputs of some rows, whose x enters in turns; the last turn and run are short ones."""
+    n_in = 1600
+    codes, meta = weights(rows, n_out, n_in)
+    x = randn(9, rows, n_in, dt=xt)
+    y = torch.full((rows, n_out // 2 if swiglu else n_out), 7.0, dtype=F32, device=DEV)
+    akvs.akvs_w4_product(x.to(DEV), codes.to(DEV), meta.to(DEV), y,
+                         akvs.AKVS_W4_SWIGLU if swiglu else akvs.AKVS_W4_STORE,
+                         ws=w4_ws(rows, n_out, n_in))
+    want, tol = ref.product(x, codes, meta)
+    if swiglu:
+        (g, u), (tg, tu) = want.chunk(2, 1), tol.chunk(2, 1)
+        s = g * torch.sigmoid(g)
+        want = s * u
+        tol = 1.1 * tg * (u.abs() + tu) + tu * s.abs() + 2.0 ** -20 * (1 + g.abs()) * want.abs()
+    assert bool(((y.double().cpu() - want).abs() <= rounded(tol, want, F32)).all())
+
+
 def test_w4_extreme_inputs():
     """A row that is not a number leaves the others alone; huge and tiny rows beside each other."""
     codes, meta = weights(1, 50, 256)
