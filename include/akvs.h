@@ -643,9 +643,9 @@ size_t akvs_w4_workspace_size(int32_t n_rows, int32_t n_out, int32_t n_in);
  * elements (ldx * element size a multiple of 16); w, w_meta: n_out rows of n_in, a multiple of 64;
  * y: [n_rows][n_out] ([n_out / 2] with AKVS_W4_SWIGLU, n_out even) of y_dtype, row r at r * ldy.
  * resid (fp32, strides as y, may be y; y_dtype F32 and AKVS_W4_STORE only) or NULL. The weights
- * are read once for 64 rows (x in F32: 32). A row of x that holds an infinity may give NaN. y and ws
- * overlap nothing else. Errors: EINVAL (sizes, strides, mode, pointers, overlaps) / EDTYPE / ESHAPE /
- * ENOSPACE, EHIP. */
+ * are read once for 64 rows (x in F32: 32). A row of x that holds an infinity, or
+ * elements above 2^116, may give NaN. y and ws overlap nothing else. Errors: EINVAL (sizes, strides,
+ * mode, pointers, overlaps) / EDTYPE / ESHAPE / ENOSPACE, EHIP. */
 akvs_status akvs_w4_product(const void *x, int64_t ldx, int32_t x_dtype, int32_t n_rows,
                             const uint8_t *w, const void *w_meta, int32_t n_out, int32_t n_in,
                             int32_t mode, const float *resid, void *y, int64_t ldy,

@@ -154,6 +154,20 @@ def test_long_sequences_are_split(geom, rows):
     b.check()
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("pairs", [4, 5, 8, 9, 16, 17, 32, 48, 49, 64, 65, 96, 128, 129])
+def test_pairs_of_a_head_where_the_form_changes(pairs, hd):
+    """As many rows of one head, beside requests of fewer, one of them short; then in place."""
+    b = Batch((1, 1, hd), 32, [333, 40, 9, 700], [pairs, 1, min(pairs, 12), (pairs + 1) // 2],
+              seed=pairs)
+    b.attend()
+    b.check()
+    q = b.qd.clone()
+    c = b.cfg()
+    akvs.akvs_paged_attention(q, c, b.p, b.m, q, b.lse, b.ws(c))
+    assert torch.equal(q, b.out)
+
+
 def test_shared_pages():
     b = Batch((28, 4, 128), 16, [70, 81, 64, 130], [1, 3, 2, 1], seed=7, shared=4)
     b.attend()
@@ -466,7 +480,8 @@ class Pool:
         return moves
 
 
-SIZES = [(1, 16, 1, 1), (5, 16, 3, 9), (40, 32, 9, 200), (300, 16, 40, 5000), (64, 256, 7, 9000)]
+SIZES = [(1, 16, 1, 1), (5, 16, 3, 9), (40, 32, 9, 200), (300, 16, 40, 5000), (64, 256, 7, 9000),
+         (700, 16, 9, 3000)]
 
 
 @pytest.mark.parametrize("S,page_rows,wide,n_pages", SIZES)
@@ -628,7 +643,7 @@ def test_w4_swiglu(rows, n_in, n_out, xt, yt):
 
 
 @pytest.mark.parametrize("rows,n_out,xt,swiglu", [(48, 16390, BF, False), (20, 24006, F32, False),
-                                                  (48, 24006, BF, True)])
+                                                  (48, 24006, BF, True), (70, 16390, BF, False)])
 def test_w4_of_wide_weights(rows, n_out, xt, swiglu):
     """Many outputs of some rows, whose x enters in turns; the last turn and run are short ones."""
     n_in = 1600
