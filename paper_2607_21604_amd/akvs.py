@@ -663,22 +663,23 @@ def akvs_w4_product(x, w, w_meta, y, mode: int = AKVS_W4_STORE, resid=None, ws=N
     """x [n_rows][n_in] and y [n_rows][n_out (/ 2)]: rows that may lie apart; w uint8 [n_out][n_in/2],
     w_meta fp16 [n_out][n_in/64][2]; resid: as y."""
     (px, ldx), (py, ldy) = rows_ptr(x), rows_ptr(y)
-    n_out, n_in = int(w.shape[0]), 2 * int(w.shape[1])
-    wide = n_out // 2 if mode == AKVS_W4_SWIGLU else n_out
-    if tuple(x.shape) != (x.shape[0], n_in) or tuple(y.shape) != (x.shape[0], wide):
-        raise ValueError(f"x {tuple(x.shape)} and y {tuple(y.shape)} do not fit weights "
+    xs, (n_out, n_in) = x.shape, w.shape
+    n_rows, n_in = xs[0], 2 * n_in
+    if xs != (n_rows, n_in) or y.shape != (n_rows, n_out // 2 if mode == AKVS_W4_SWIGLU else n_out):
+        raise ValueError(f"x {tuple(xs)} and y {tuple(y.shape)} do not fit weights "
                          f"[{n_out}][{n_in}]")
-    if (w.dtype, w_meta.dtype) != (torch.uint8, torch.float16) or w_meta.numel() != n_out * n_in // 32:
+    if w.dtype != torch.uint8 or w_meta.dtype != torch.float16 or (
+            w_meta.numel() != n_out * n_in // 32):
         raise ValueError("weights: need uint8 codes and fp16 (scale, zero) of every 64")
     pr = None
     if resid is not None:
         pr, ldr = rows_ptr(resid)
         if resid.shape != y.shape or ldr != ldy or resid.dtype != torch.float32:
             raise ValueError("resid: need an fp32 tensor of y's shape and strides")
-    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
-    _check(load().akvs_w4_product(px, ldx, dtype_code(x), int(x.shape[0]), ptr(w), ptr(w_meta),
-                                  n_out, n_in, mode, pr, py, ldy, dtype_code(y), ptr(ws), nbytes,
-                                  stream_handle(stream)), "akvs_w4_product")
+    _check(load().akvs_w4_product(px, ldx, dtype_code(x), n_rows, ptr(w), ptr(w_meta), n_out, n_in,
+                                  mode, pr, py, ldy, dtype_code(y), ptr(ws),
+                                  0 if ws is None else ws.nbytes, stream_handle(stream)),
+           "akvs_w4_product")
 
 
 def akvs_profile_enable(class_mask: int):
