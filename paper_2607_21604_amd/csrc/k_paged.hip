@@ -24,10 +24,72 @@ namespace akvs {
 // chunks, are outermost: with them inside, a power of two of them leaves all of the empty ones to
 // the same part (6 requests of up to 4 tiles: half of the device idle, 123 us against 101).
 struct PagedPlan {
-  int pairs, tiles, chunks, chunk_keys;  // pairs: of a tile
+  int pairs, tiles, chunks, chunk_keys;  // pairs: of a tile; chunk_keys: at most
+  int slots;                             // blocks of a head at a time; 0: chunk_keys is the cut
   bool many;                             // k_paged_many's
 };
 constexpr int PG_TILE = 64;  // keys a wave takes at a time
+
+// Sum (MAX: largest, of numbers >= 0) over a wave by DPP: rows of 16, then each row's last to the next.
+template <bool MAX>
+__device__ __forceinline__ float wave_all(float x) {
+  auto step = [&](auto ctrl, auto rows) __attribute__((always_inline)) {
+    const float y = __int_as_float(__builtin_amdgcn_update_dpp(
+        0, __float_as_int(x), decltype(ctrl)::value, decltype(rows)::value, 0xf, true));
+    x = MAX ? fmaxf(x, y) : x + y;
+  };
+  using std::integral_constant;
+  step(integral_constant<int, 0x111>(), integral_constant<int, 0xf>());  // row_shr 1, 2, 4, 8
+  step(integral_constant<int, 0x112>(), integral_constant<int, 0xf>());
+  step(integral_constant<int, 0x114>(), integral_constant<int, 0xf>());
+  step(integral_constant<int, 0x118>(), integral_constant<int, 0xf>());
+  step(integral_constant<int, 0x142>(), integral_constant<int, 0xa>());  // row_bcast 15, 31
+  step(integral_constant<int, 0x143>(), integral_constant<int, 0xc>());
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+
+// Request b's rows, keys and table, and the keys of a chunk. Where the plan leaves it open, that is
+// the least for which the requests' own lengths, a lane each, make one round of blocks, tried at 1 to
+// 7/4 of an even share and cut into no more than the plan's chunks; the same in all blocks of a call.
+// It costs 0.6 to 1.5 us, and makes up for a max_len far above the lengths, as captured calls have it:
+//   8 requests of 3000 to 4000 keys, 28/4 heads: 14.2 us for any max_len; by the plan's cut 13.8 for a
+//   max_len of 4000, 16.3 for 16000, 33 for 64000. 6 questions of 9 to 96 rows over 2000 to 8192 keys,
+//   40/8 heads: 77 us, 103 for a max_len of 131000; 94 and 257. (32 requests in two chunks each gain 1
+//   of 36: k_paged_few has the plan's cut below 8 chunks.)
+__device__ __forceinline__ const int32_t *paged_request(const PagedBatch &s, const PagedPlan &plan,
+                                                        int G, int b, int &r0, int &r1, int &len,
+                                                        int &chunk_keys) {
+  chunk_keys = plan.chunk_keys;
+  if (plan.slots == 0) {
+    paged_rows(s, b, r0, r1);
+    return paged_keys(s, b, len);
+  }
+  const int lane = threadIdx.x & 63, mine = min(lane, s.n_req - 1);
+  const int q = s.seq ? s.seq[mine] : mine;
+  paged_rows(s, mine, r0, r1);
+  paged_keys(s, mine, len);
+  const float tiles = lane < s.n_req ? (float)(((r1 - r0) * G + plan.pairs - 1) / plan.pairs) : 0.f;
+  const int kt = tiles > 0.f ? (len + PG_TILE - 1) / PG_TILE : 0;
+  const float work = wave_all<false>(tiles * kt);
+  const int most = (int)wave_all<true>((float)kt);
+  const int unit = plan.many ? 1 : 4, least = (most + plan.chunks - 1) / plan.chunks;
+  int c = plan.chunk_keys / PG_TILE;
+  for (int f = 4; f <= 7; ++f) {
+    int t = max(max((int)(work * f / (4 * plan.slots)) + 1, least), 2);
+    t = (t + unit - 1) / unit * unit;
+    if (t >= c) break;
+    if (wave_all<false>(tiles * (float)((kt + t - 1) / t)) <= (float)plan.slots) {
+      c = t;
+      break;
+    }
+  }
+  chunk_keys = max(c, least) * PG_TILE;
+  r0 = __builtin_amdgcn_readlane(r0, b);
+  r1 = __builtin_amdgcn_readlane(r1, b);
+  len = __builtin_amdgcn_readlane(len, b);
+  const int own = __builtin_amdgcn_readlane(q, b);
+  return s.table + (own >= 0 && own < s.n_seq ? (size_t)own * s.max_pages : 0);
+}
 
 // Few pairs. Block = 4 waves over a tile of 16 / NB pairs and one chunk of keys; its waves take the chunk's tiles of 64 keys in turn, each with its own maximum, sum and output, merged
 // through LDS at the end, so that the loop has no barrier. MFMA 16x16x32, lane l: g = l / 16.
@@ -72,15 +134,14 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(
   const int b = id % s.n_req;
   id /= s.n_req;
   const int chunk = id % plan.chunks, tile = id / plan.chunks;
-  int r0, r1, len;
-  paged_rows(s, b, r0, r1);
-  const int32_t *table = paged_keys(s, b, len);
+  int r0, r1, len, chunk_keys;
+  const int32_t *table = paged_request(s, plan, G, b, r0, r1, len, chunk_keys);
   const int n_pairs = (r1 - r0) * G, v0 = tile * COLS;
   if (v0 >= n_pairs) return;
   auto seen_by = [&](int r) { return max(len - r1 + r + 1, 0); };
   const int last = min(n_pairs, v0 + COLS) - 1;
-  const int k0 = chunk * plan.chunk_keys;
-  const int k1 = min(k0 + plan.chunk_keys, seen_by(r0 + last / G));
+  const int k0 = chunk * chunk_keys;
+  const int k1 = min(k0 + chunk_keys, seen_by(r0 + last / G));
   const int all_see = min(seen_by(r0 + v0 / G), k1);
   const bool split = plan.chunks > 1;
   auto place = [&](int v, int &r, int &head) {
@@ -552,9 +613,8 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
   const int b = id % s.n_req;
   id /= s.n_req;
   const int chunk = id % plan.chunks, tile = id / plan.chunks;
-  int r0, r1, len;
-  paged_rows(s, b, r0, r1);
-  const int32_t *table = paged_keys(s, b, len);
+  int r0, r1, len, chunk_keys;
+  const int32_t *table = paged_request(s, plan, G, b, r0, r1, len, chunk_keys);
   const int n_pairs = (r1 - r0) * G, v0 = tile * plan.pairs;
   if (v0 >= n_pairs) return;
   auto seen_by = [&](int r) { return max(len - r1 + r + 1, 0); };
@@ -567,8 +627,8 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
   const int v = v0 + group * 32 + (lane & 31);
   const bool valid = v <= last;
   const int r = r0 + (valid ? v : v0) / G, head = h * G + (valid ? v : v0) % G;
-  const int k0 = chunk * plan.chunk_keys;
-  const int k1 = min(k0 + plan.chunk_keys, seen_by(r0 + last / G));
+  const int k0 = chunk * chunk_keys;
+  const int k1 = min(k0 + chunk_keys, seen_by(r0 + last / G));
   const int all_see = seen_by(r0 + v0 / G), seen = valid ? min(seen_by(r), k1) : 0;
   const size_t prow = ((size_t)chunk * s.n_rows + r) * hq + head;
   const int nkt = k1 > k0 ? (k1 - k0 + PG_TILE - 1) / PG_TILE : 0;
@@ -945,6 +1005,9 @@ static PagedPlan paged_plan(const PagedBatch &s, int hq, int hkv, int hd) {
   const int per = kt ? (int)((kt + best - 1) / best) : 1;
   p.chunk_keys = (per + unit - 1) / unit * unit * PG_TILE;
   p.chunks = std::max(1, (s.limit + p.chunk_keys - 1) / p.chunk_keys);
+  // the cut is made anew of the lengths, by k_paged_many in up to half as many chunks more
+  p.slots = s.n_req <= 64 && (p.many ? p.chunks > 1 : p.chunks >= 8) ? (int)(slots / hkv) : 0;
+  if (p.slots && p.many) p.chunks = (int)std::min(most, (p.chunks * 3LL + 1) / 2);
   return p;
 }
 

@@ -168,6 +168,18 @@ def test_pairs_of_a_head_where_the_form_changes(pairs, hd):
     assert torch.equal(q, b.out)
 
 
+@pytest.mark.parametrize("geom", [(28, 4, 128), (16, 8, 64)])
+@pytest.mark.parametrize("rows", [[1, 1, 1, 1], [1, 9, 60, 2]])
+def test_a_far_larger_max_len(geom, rows):
+    """Room for many more keys than the sequences have, which are cut by their own lengths."""
+    b = Batch(geom, 64, [2900, 0, 1333, 40], rows, seq=[3, 2, 0, 1], seed=51)
+    for r in b.table:
+        r += [-1] * (1500 - len(r))
+    b.max_len = 1500 * 64
+    b.attend()
+    b.check()
+
+
 def test_shared_pages():
     b = Batch((28, 4, 128), 16, [70, 81, 64, 130], [1, 3, 2, 1], seed=7, shared=4)
     b.attend()
