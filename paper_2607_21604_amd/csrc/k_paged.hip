@@ -586,7 +586,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(
 // rows by the transposing LDS read. Queries are fp16 scaled by a power of two per pair, the
 // probabilities fp16 times 2^7, so that what is lost below fp16's smallest is 2^-32 of the
 // largest; statistics and outputs are fp32.
-//   6 questions of 39 to 92 rows over 3155 to 8115 keys, 40/8 heads: 98 us, 340 TFLOP/s. The matrix
+//   6 questions of 39 to 92 rows over 3155 to 8115 keys, 40/8 heads: 97 us, 345 TFLOP/s. The matrix
 //   cores are busy a sixth of that, the vector unit a third, LDS a fifth: two waves a SIMD wait for
 //   each other's steps, and the longest question's blocks for nobody.
 template <int HD, bool WIDE>

@@ -403,7 +403,7 @@ __device__ __forceinline__ float merged_lse(float M, float l) {
 
 // Few slots: a thread has 8 dims of a pair and requests all slots at once.
 constexpr int MERGE_FEW = 4;
-template <typename TS, typename TP>
+template <typename TS, typename TP, int FEW>
 __global__ __launch_bounds__(256) void k_shared_merge_few(SharedBatch s, int slots, int hq, int hd,
                                                           const TP *__restrict__ part_o,
                                                           const float4 *__restrict__ part_ml,
@@ -414,10 +414,10 @@ __global__ __launch_bounds__(256) void k_shared_merge_few(SharedBatch s, int slo
   const int e0 = (int)(id - item * per) * 8;
   if (item >= (size_t)shared_live(s) * hq) return;
   const size_t stride = (size_t)s.n_rows * hq;
-  float4 ml[MERGE_FEW];
-  float x[MERGE_FEW][8];
+  float4 ml[FEW];
+  float x[FEW][8];
 #pragma unroll
-  for (int u = 0; u < MERGE_FEW; ++u)
+  for (int u = 0; u < FEW; ++u)
     if (u < slots) {
       ml[u] = part_ml[u * stride + item];
       part_load8(part_o + (u * stride + item) * hd + e0, x[u]);
@@ -426,10 +426,10 @@ __global__ __launch_bounds__(256) void k_shared_merge_few(SharedBatch s, int slo
 #pragma unroll
   for (int i = 0; i < 8; ++i) a[i] = 0.f;
 #pragma unroll
-  for (int u = 0; u < MERGE_FEW; ++u)
+  for (int u = 0; u < FEW; ++u)
     if (u < slots) M = fmaxf(M, ml[u].x);
 #pragma unroll
-  for (int u = 0; u < MERGE_FEW; ++u)
+  for (int u = 0; u < FEW; ++u)
     if (u < slots) {
       if (!slot_counts(ml[u])) continue;
       const float w = slot_factor(ml[u], M);
@@ -1130,12 +1130,20 @@ size_t shared_part_floats(const SharedBatch &s, int hq, int hkv, int hd, int dty
 
 template <typename TS, typename TP, int HD>
 static hipError_t shared_merge(const SharedBatch &s, int slots, int hq, const TP *po,
-                               const float4 *ml, TS *out, float *lse, hipStream_t st) {
+                               const float4 *ml, TS *out, float *lse, hipStream_t st, int eight = 0) {
   const size_t items = (size_t)s.n_rows * hq;
   const dim3 b(256);
+  const dim3 gf((unsigned)((items * (HD / 8) + 255) / 256));
+  if constexpr (sizeof(TP) == 2) {
+    if (slots > MERGE_FEW && slots <= eight) {
+      hipLaunchKernelGGL((k_shared_merge_few<TS, TP, 8>), gf, b, 0, st, s, slots, hq, HD, po, ml, out,
+                         lse);
+      return hipGetLastError();
+    }
+  }
   if (slots <= MERGE_FEW) {
-    const dim3 gm((unsigned)((items * (HD / 8) + 255) / 256));
-    hipLaunchKernelGGL((k_shared_merge_few<TS, TP>), gm, b, 0, st, s, slots, hq, HD, po, ml, out, lse);
+    hipLaunchKernelGGL((k_shared_merge_few<TS, TP, MERGE_FEW>), gf, b, 0, st, s, slots, hq, HD, po, ml,
+                       out, lse);
   } else if (slots <= MERGE_WAVE) {
     const dim3 gm = merge_grid((items + 3) / 4);
     hipLaunchKernelGGL((k_shared_merge_wave<TS, TP, HD>), gm, b, 0, st, s, slots, hq, po, ml, out, lse);
@@ -1151,8 +1159,10 @@ hipError_t launch_merge_slots(const SharedBatch &s, int slots, int hq, int hd, c
   const _Float16 *o = reinterpret_cast<const _Float16 *>(po);
   const float4 *m = reinterpret_cast<const float4 *>(ml);
   bf16_t *O = reinterpret_cast<bf16_t *>(out);
-  return hd == 128 ? shared_merge<bf16_t, _Float16, 128>(s, slots, hq, o, m, O, lse, st)
-                   : shared_merge<bf16_t, _Float16, 64>(s, slots, hq, o, m, O, lse, st);
+  // (many pairs in up to 8 slots: 13200 in 6 take 6.5 us so, 8.6 with a wave each)
+  const int eight = (size_t)s.n_rows * hq >= 4096 ? 8 : 0;
+  return hd == 128 ? shared_merge<bf16_t, _Float16, 128>(s, slots, hq, o, m, O, lse, st, eight)
+                   : shared_merge<bf16_t, _Float16, 64>(s, slots, hq, o, m, O, lse, st, eight);
 }
 
 template <typename TS, int HD>
