@@ -397,60 +397,91 @@ __global__ __launch_bounds__(256) void k_grow_pick(PageTable t, int n, GrowWs w)
   grow_list(bits, blockIdx.x, rank, need, w.list);
 }
 
-// A wave per sequence; the last block: the totals, and -1 past the last move.
+// A wave per sequence; the last block: the totals, and -1 past the last move. All that a wave needs is
+// requested before the free pages are counted, which decides whether its sequence is served.
 __global__ __launch_bounds__(256) void k_grow_assign(PageTable t, int n, int segs,
                                                      const int32_t *seq, const int32_t *add,
                                                      GrowWs w, int32_t *served, int32_t *move_src,
                                                      int32_t *move_dst, int32_t *counts) {
-  const int free_pages = seg_before(w.count, segs);
-  auto serves = [&](int i) {
-    const int x = w.need[i];
-    return x >= 0 && ((x & ~NEED_COPY) == 0 || w.ends[i] <= free_pages);
+  auto serves = [&](int need, int ends, int free_pages) {
+    return need >= 0 && ((need & ~NEED_COPY) == 0 || ends <= free_pages);
   };
   if (blockIdx.x == gridDim.x - 1) {
-    __shared__ int s_moves, s_taken;
-    if (threadIdx.x == 0) s_moves = s_taken = 0;
-    __syncthreads();
+    __shared__ int s_moves[4], s_taken[4];
+    int i = threadIdx.x, x = -1, e = 0, c = 0;
+    auto read = [&]() {
+      x = w.need[i];
+      e = w.ends[i];
+      c = w.copies[i];
+    };
+    if (i < n) read();
+    const int free_pages = seg_before(w.count, segs);
     int moves = 0, taken = 0;
-    for (int i = threadIdx.x; i < n; i += 256)
-      if (serves(i) && (w.need[i] & ~NEED_COPY)) {
-        moves = max(moves, w.copies[i]);
-        taken = max(taken, w.ends[i]);
+    while (i < n) {
+      if (serves(x, e, free_pages) && (x & ~NEED_COPY)) {
+        moves = max(moves, c);
+        taken = max(taken, e);
       }
-    atomicMax(&s_moves, moves);
-    atomicMax(&s_taken, taken);
+      i += 256;
+      if (i < n) read();
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      moves = max(moves, __shfl_xor(moves, d, 64));
+      taken = max(taken, __shfl_xor(taken, d, 64));
+    }
+    if ((threadIdx.x & 63) == 0) {
+      s_moves[threadIdx.x >> 6] = moves;
+      s_taken[threadIdx.x >> 6] = taken;
+    }
     __syncthreads();
-    moves = s_moves;
+    moves = max(max(s_moves[0], s_moves[1]), max(s_moves[2], s_moves[3]));
+    taken = max(max(s_taken[0], s_taken[1]), max(s_taken[2], s_taken[3]));
     for (int i = moves + threadIdx.x; i < n; i += 256) move_src[i] = move_dst[i] = -1;
     if (threadIdx.x == 0) {
       counts[0] = moves;
-      counts[1] = s_taken;
+      counts[1] = taken;
     }
     return;
   }
   const int i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  int x = -1, ends = 0, copies = 0, more = 0, old = 0, last = 0, first = 0;
+  int32_t *mine = nullptr;
+  if (i < n) {
+    const int a = seq[i];
+    x = w.need[i];
+    ends = w.ends[i];
+    copies = w.copies[i];
+    more = add[i];
+    if (x >= 0) {  // (a is a sequence)
+      old = max(t.len[a], 0);
+      mine = t.table + (size_t)a * t.max_pages;
+      if (x & NEED_COPY) last = mine[old >> t.shift];
+      const int need = x & ~NEED_COPY, at = ends - need + lane;
+      if (lane < need && at < t.n_pages) first = w.list[at];
+    }
+  }
+  const int free_pages = seg_before(w.count, segs);
   if (i >= n) return;
-  const bool ok = serves(i);
+  const bool ok = serves(x, ends, free_pages);
   if (lane == 0) served[i] = ok;
   if (!ok) return;
-  const int a = seq[i], more = add[i], need = w.need[i] & ~NEED_COPY;
-  const bool copy = w.need[i] & NEED_COPY;
-  const int old = max(t.len[a], 0), base = w.ends[i] - need;
-  int32_t *mine = t.table + (size_t)a * t.max_pages;
+  const int need = x & ~NEED_COPY, base = ends - need;
+  const bool copy = x & NEED_COPY;
   const int have = (int)(((long long)old + (1 << t.shift) - 1) >> t.shift);
   const int start = copy ? old >> t.shift : have;
   if (copy && lane == 0) {
-    const int last = mine[start], m = w.copies[i] - 1;
+    const int m = copies - 1;
     move_src[m] = last;
-    move_dst[m] = w.list[base];
+    move_dst[m] = first;
     atomicSub(&t.ref[last], 1);
   }
   for (int j = lane; j < need; j += 64) {
-    const int id = w.list[base + j];
+    const int id = j < 64 ? first : w.list[base + j];
     mine[start + j] = id;
     t.ref[id] = 1;
   }
-  if (lane == 0) t.len[a] = old + more;
+  if (lane == 0) t.len[seq[i]] = old + more;
 }
 
 __global__ __launch_bounds__(256) void k_compact_count(PageTable t, int32_t *count) {
