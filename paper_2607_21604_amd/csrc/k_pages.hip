@@ -283,8 +283,8 @@ __device__ __forceinline__ int seg_before(const int32_t *count, int n) {
 }
 
 // The same from the pages themselves: of a few segments a launch less.
-//   64 branches end, begin again and grow over 1500 pages: 29.3 us with a launch for the counts, 26.3 without;
-//   1500 pages move together in 3 layers: 50.6 and 49.0.
+//   192 branches end, begin again and grow, three segments: 29.3 us with a launch for the counts, 26.3
+//   without; 1500 pages move together in 3 layers: 50.6 and 49.0.
 constexpr int FEW_SEGS = 8;
 __device__ __forceinline__ uint32_t seg_pages(const PageTable &t, int seg, bool used) {
   const SegBits x = seg_bits(t, seg);
