@@ -91,8 +91,9 @@ __device__ __forceinline__ const int32_t *paged_request(const PagedBatch &s, con
   return s.table + (own >= 0 && own < s.n_seq ? (size_t)own * s.max_pages : 0);
 }
 
-// Few pairs. Block = 4 waves over a tile of 16 / NB pairs and one chunk of keys; its waves take the chunk's tiles of 64 keys in turn, each with its own maximum, sum and output, merged
-// through LDS at the end, so that the loop has no barrier. MFMA 16x16x32, lane l: g = l / 16.
+// Few pairs. Block = 4 waves over a tile of 16 / NB pairs and one chunk of keys; its waves take the
+// chunk's tiles of 64 keys in turn, each with its own maximum, sum and output, merged through LDS at
+// the end, so that the loop has no barrier. MFMA 16x16x32, lane l: g = l / 16.
 //   Scores, S^T = K Q^T, 16 keys T = 0..3 of the tile at a time: the lane holds the scores of column
 //   l % 16 at keys 16 T + 4 g .. + 3; the reduction takes elements 64 group + 16 g + 8 step .. + 7.
 //   Outputs, O^T = V^T P^T: a step's reduction takes 16 keys of two T, V^T comes from rows in LDS by
@@ -725,7 +726,8 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
   // added at the end. Pieces of the values are written in an order that differs by row, so that
   // rows four apart in a bank do not meet.
   auto store = [&](Codes &c, int key0, int buf) __attribute__((always_inline)) {
-    _Float16 *ks = s_kv + buf * (KB + VB) + krow * KST + kq * (HD / 4), *vs = s_kv + buf * (KB + VB) + KB + krow * VST + kq * (HD / 4);
+    _Float16 *ks = s_kv + buf * (KB + VB) + krow * KST + kq * (HD / 4);
+    _Float16 *vs = s_kv + buf * (KB + VB) + KB + krow * VST + kq * (HD / 4);
     if (key0 + PG_TILE > all_see && key0 + krow >= all_see) {
       if ((c.vm & 0x7c00u) == 0x7c00u || (c.vm & 0x7c000000u) == 0x7c000000u) {
         s_odd = 1;
@@ -908,7 +910,8 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
         if (fabsf(sv) < INFINITY && fabsf(zv) < INFINITY) continue;
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) {
-          const uint32_t w = *reinterpret_cast<const uint16_t *>(p.v + row * RB + db * 16 + q4 * 4 + hi * 2);
+          const uint32_t w =
+              *reinterpret_cast<const uint16_t *>(p.v + row * RB + db * 16 + q4 * 4 + hi * 2);
 #pragma unroll
           for (int j = 0; j < 4; ++j)
             o[db][4 * q4 + j] += fmaf(sv, (float)((w >> (4 * j)) & 15u), zv);

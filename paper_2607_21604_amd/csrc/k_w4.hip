@@ -397,7 +397,8 @@ static size_t w4_lds(const W4Plan &p, int parts) {
 //   64 rows 5120 -> 55296 (SWIGLU): x of 2 runs in 5 turns 83, in 5 slices 101.
 //   17 rows 5120 -> 7168: 4 slices in blocks of 8 waves 14, of 4 waves with two tiles each 20, 2
 //   turns of 5 runs 25.
-//   33 rows 27648 -> 5120: 18 slices in blocks of 12 waves (one round) 36, of 8 47, 27 slices 47, 54 58.
+//   33 rows 27648 -> 5120: 18 slices in blocks of 12 waves (one round) 36, of 8 47, 27 slices 47, 54
+//   58.
 static W4Plan w4_make_plan(int rows, int n_out, int n_in, bool swiglu, int parts, int cus) {
   constexpr double FIXED = 2.5, STAGE = 1, TRIP = 1.2, CYCLES = 1300, BYTES = 5.2e6;
   constexpr size_t LDS = 160 << 10;

@@ -48,7 +48,8 @@ def test_sizes_of_a_cache(engine, args):
 
 def test_layout(cache):
     assert cache.max_len == 112 and tuple(cache.table.shape) == (5, 7)
-    assert tuple(cache.k.shape) == (2, 12, 2, 16, 32) and tuple(cache.v_meta.shape) == (2, 12, 2, 16, 1, 2)
+    assert tuple(cache.k.shape) == (2, 12, 2, 16, 32)
+    assert tuple(cache.v_meta.shape) == (2, 12, 2, 16, 1, 2)
     assert bool((cache.table == -1).all()) and not cache.len.any() and not cache.ref.any()
     a, b = cache.layers
     assert b.k == a.k + 12 * 2 * 16 * 32 and b.v_meta == a.v_meta + 12 * 2 * 16 * 4
@@ -64,7 +65,8 @@ def test_batches(cache):
     assert (c.n_req, c.rows_max) == (2, 7)
     for args in ((9,), (4, [0, 1, 2]), (4, [0, 5]), (4, [-1, 0]), (4, i32(0, 1).long()),
                  (4, [0, 1], [0, 2]), (4, [0, 1], [0, 3, 5]), (4, [0, 1], i32(0, 2)),
-                 (4, [0, 1], [0, 1, 4], 2), (5, [0], None, None, 113), (5, [0], None, None, -1), (0, []), (0, [], [0])):
+                 (4, [0, 1], [0, 1, 4], 2), (5, [0], None, None, 113),
+                 (5, [0], None, None, -1), (0, []), (0, [], [0])):
         with pytest.raises(ValueError):
             cache.batch(*args)
 
