@@ -778,3 +778,40 @@ def test_page_calls_captured():
         assert counts.cpu().tolist() == want and a[0].cpu().tolist() == served
         src_ = torch.zeros(8, device=DEV).add_(1)  # eager work between the replays
         torch.cuda.synchronize()
+
+
+# ---- long walks, many pairs, many requests ------------------------------------------------------
+
+@pytest.mark.parametrize("geom,n_req", [((4, 1, 64), 1024), ((4, 1, 128), 512), ((16, 1, 128), 512)])
+@pytest.mark.parametrize("q_std", [0.05, 1.0])
+def test_long_even_attention_in_one_block(geom, n_req, q_std):
+    """Requests that read the same 65536 keys, a block each, with fairly even weights, so that the
+    result is far smaller than what is added up. Root mean square of the error, relative to the
+    results': rounding to bf16 is off by up to 2^-8 of a value, evenly spread (2^-8 / sqrt 3); p scale
+    in fp16 by up to 2^-11 each, independent of each other, which is at most twice as much of the sum
+    of its codes less their middle as of the result (2 2^-11 / sqrt 3 in quadrature); the rest is left
+    to the sums in 32 bits: as much as a fifth of the bf16 result's rounding, whatever the number of
+    keys."""
+    (hq, hkv, hd), keys, page = geom, 65536, 256
+    m, n = model(*geom), keys // page
+    pools = [ref.quantise(randn(i, n, hkv, page, hd)) for i in (1, 2)]
+    (k, km), (v, vm) = ([x.to(DEV) for x in p] for p in pools)
+    order = torch.randperm(n, generator=torch.Generator().manual_seed(3))
+    q = randn(4, n_req, hq, hd, dt=BF, std=q_std)
+    c = akvs.paged_cfg(n_req, n_req, 1, ints([keys]), ints(order[None]), keys, None,
+                       ints([0] * n_req))
+    assert akvs.akvs_paged_workspace_size(m, c) == 0  # (one chunk)
+    out = torch.empty((n_req, hq, hd), dtype=BF, device=DEV)
+    lse = torch.empty((n_req, hq), device=DEV)
+    akvs.akvs_paged_attention(q.to(DEV), c, akvs.pages(k, v, km, vm), m, out, lse)
+    x, y = (ref.values(*(z.index_select(0, order.to(DEV)) for z in p)).flatten(0, 2)
+            for p in ((k, km), (v, vm)))
+    for i in range(0, n_req, 64):
+        sc = q[i:i + 64].to(DEV).double().view(-1, hd) @ x.T.contiguous() / math.sqrt(hd)
+        want = torch.softmax(sc, 1) @ y
+        got = out[i:i + 64].double().view(-1, hd)
+        tol = 2.0 ** -8 * math.sqrt((1 + 0.2 ** 2) / 3 + (2 * 2.0 ** -3) ** 2 / 3)
+        err = ((got - want).square().mean() / want.square().mean()).sqrt()
+        assert float(err) <= tol
+        err = (lse[i:i + 64].double().flatten() - torch.logsumexp(sc, 1)).abs().max()
+        assert float(err) <= 1e-4
