@@ -179,6 +179,9 @@ typedef struct akvs_page_table {
   int32_t *table;             /* device [S][max_pages]                                       */
   int32_t *len;               /* device [S]: keys of each sequence                           */
   int32_t *ref;               /* device [n_pages]                                            */
+  int32_t *grown;             /* device [S], or NULL: 0 for a sequence that the last
+                                 akvs_grow_pages of it could not serve, 1 for others (ones
+                                 at first); akvs_free_pages and akvs_fork_pages make it 1    */
 } akvs_page_table;
 
 /* A batch over sequences in pages (akvs_store_pages, akvs_load_pages, akvs_paged_attention). Rows
@@ -196,6 +199,8 @@ typedef struct akvs_paged_cfg {
   const int32_t *seq;   /* device [B]: the sequence of each request; NULL: b (B <= n_seq)    */
   const int32_t *len;   /* device [n_seq]: keys, the rows' own among them                    */
   const int32_t *table; /* device [n_seq][max_pages]                                         */
+  const int32_t *grown; /* device [n_seq], or NULL: akvs_store_pages stores no rows of
+                           sequences with 0 (akvs_page_table's); the others do not read it   */
 } akvs_paged_cfg;
 
 /* What akvs_w4_product makes of W x. */
@@ -554,8 +559,9 @@ akvs_status akvs_evict_cache(const void *k, const void *v, const float *weights,
 /* Quantises a batch's new keys and values into their pages, with the codes and meta that
  * akvs_quantize_cache gives them (values past fp16's range are outside the format). k, v:
  * [n_rows][Hkv][hd] model dtype, row r at r * ldk / ldv elements (each ld * 2 bytes a multiple of
- * 16); pages that rows go to are named by one sequence of the batch only. Rows past row_start[B]
- * and rows that are no key of their sequence (more rows than keys) go nowhere. Errors: EINVAL
+ * 16); pages that rows go to are named by one sequence of the batch only. Rows past row_start[B],
+ * rows that are no key of their sequence (more rows than keys) and rows of a sequence that could not
+ * grow by them (grown) go nowhere: without `grown` they would be taken for its last keys of before. Errors: EINVAL
  * (sizes, pointers, strides, overlaps) / EDTYPE / EUNSUPPORTED (page_rows) / ESHAPE, EHIP. */
 akvs_status akvs_store_pages(const void *k, int64_t ldk, const void *v, int64_t ldv,
                              const akvs_paged_cfg *c, const akvs_pages *p,
@@ -610,7 +616,8 @@ size_t akvs_pages_workspace_size(const akvs_page_table *t, int32_t n);
  * new one: that page's contents are to be copied, as listed in move_src / move_dst (device [n]
  * int32 each, in order, -1 past the last; akvs_move_pages). served (device [n]): 1, or 0 for a
  * sequence that stays as it was: an index out of range or named earlier, add[i] < 0, more than
- * max_pages pages, or no free pages left (one that needs any follows one that could not be served).
+ * max_pages pages, or no free pages left (one that needs any follows one that could not be served);
+ * grown has the same of every sequence named, of its first entry.
  * counts (device [2]): copies listed, pages taken. Outputs and ws overlap nothing else. Errors as
  * above, ENOSPACE. */
 akvs_status akvs_grow_pages(const akvs_page_table *t, int32_t n, const int32_t *seq,

@@ -98,7 +98,8 @@ class Pages(ctypes.Structure):
 class PageTable(ctypes.Structure):
     _fields_ = [("n_seq", ctypes.c_int32), ("max_pages", ctypes.c_int32),
                 ("n_pages", ctypes.c_int32), ("page_rows", ctypes.c_int32),
-                ("table", ctypes.c_void_p), ("len", ctypes.c_void_p), ("ref", ctypes.c_void_p)]
+                ("table", ctypes.c_void_p), ("len", ctypes.c_void_p), ("ref", ctypes.c_void_p),
+                ("grown", ctypes.c_void_p)]
 
 
 class PagedCfg(ctypes.Structure):
@@ -106,7 +107,8 @@ class PagedCfg(ctypes.Structure):
                 ("rows_max", ctypes.c_int32), ("n_seq", ctypes.c_int32),
                 ("max_pages", ctypes.c_int32), ("max_len", ctypes.c_int32),
                 ("row_start", ctypes.c_void_p), ("seq", ctypes.c_void_p),
-                ("len", ctypes.c_void_p), ("table", ctypes.c_void_p)]
+                ("len", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("grown", ctypes.c_void_p)]
 
 
 _P = ctypes.c_void_p
@@ -336,25 +338,27 @@ def pages(k, v, k_meta, v_meta) -> Pages:
     return p
 
 
-def page_table(table, lens, ref, page_rows) -> PageTable:
-    """The pages of sequences: int32 table [S][max_pages], lens [S], ref [n_pages]; it holds
-    references to the tensors."""
+def page_table(table, lens, ref, page_rows, grown=None) -> PageTable:
+    """The pages of sequences: int32 table [S][max_pages], lens [S], ref [n_pages], grown [S]; it
+    holds references to the tensors."""
     if table.dim() != 2:
         raise ValueError("table: need [sequences][pages]")
     t = PageTable(int(table.shape[0]), int(table.shape[1]), int(ref.numel()), int(page_rows),
-                  int_ptr(table, 0), int_ptr(lens, table.shape[0]), int_ptr(ref, 0))
-    t._keep = (table, lens, ref)
+                  int_ptr(table, 0), int_ptr(lens, table.shape[0]), int_ptr(ref, 0),
+                  int_ptr(grown, table.shape[0]))
+    t._keep = (table, lens, ref, grown)
     return t
 
 
-def paged_cfg(n_req, n_rows, rows_max, lens, table, max_len, row_start=None, seq=None) -> PagedCfg:
+def paged_cfg(n_req, n_rows, rows_max, lens, table, max_len, row_start=None, seq=None,
+              grown=None) -> PagedCfg:
     """A batch over sequences in pages; it holds references to its device tensors."""
     if table.dim() != 2:
         raise ValueError("table: need [sequences][pages]")
     c = PagedCfg(int(n_req), int(n_rows), int(rows_max), int(table.shape[0]), int(table.shape[1]),
                  int(max_len), int_ptr(row_start, n_req + 1), int_ptr(seq, n_req),
-                 int_ptr(lens, table.shape[0]), int_ptr(table, 0))
-    c._keep = (row_start, seq, lens, table)
+                 int_ptr(lens, table.shape[0]), int_ptr(table, 0), int_ptr(grown, table.shape[0]))
+    c._keep = (row_start, seq, lens, table, grown)
     return c
 
 

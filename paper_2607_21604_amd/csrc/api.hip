@@ -1997,7 +1997,7 @@ static akvs_status check_paged(const akvs_model_cfg *m, const akvs_paged_cfg *c,
   *s = {c->n_req,     c->n_rows, std::min(c->rows_max, std::max(c->n_rows, 1)),
         c->n_seq,     c->max_pages, c->max_len,
         c->row_start, c->seq,    c->len,
-        c->table};
+        c->table,     nullptr};
   return AKVS_OK;
 }
 
@@ -2056,9 +2056,9 @@ static akvs_status check_table(const akvs_page_table *t, int32_t n, PageTable *x
           AKVS_ESHAPE, "page table too large");
   REQUIRE(t->table && t->len && (t->ref || t->n_pages == 0), AKVS_EINVAL,
           "table, len or ref is NULL");
-  REQUIRE(aligned16(t->table) && aligned16(t->len) && aligned16(t->ref), AKVS_EINVAL,
-          "misaligned page table");
-  *x = {t->n_seq, t->max_pages, t->n_pages, shift, t->table, t->len, t->ref};
+  REQUIRE(aligned16(t->table) && aligned16(t->len) && aligned16(t->ref) && aligned16(t->grown),
+          AKVS_EINVAL, "misaligned page table");
+  *x = {t->n_seq, t->max_pages, t->n_pages, shift, t->table, t->len, t->ref, t->grown};
   return AKVS_OK;
 }
 
@@ -2072,6 +2072,7 @@ akvs_status akvs_store_pages(const void *k, int64_t ldk, const void *v, int64_t 
   if (st) return st;
   const long long width = m->n_kv_heads * m->head_dim;
   if (x.s.n_rows == 0) return AKVS_OK;
+  x.s.grown = c->grown;
   REQUIRE(k && v, AKVS_EINVAL, "NULL argument");
   REQUIRE(aligned16(k) && aligned16(v), AKVS_EINVAL, "misaligned argument");
   REQUIRE(ldk >= width && ldv >= width, AKVS_EINVAL, "row strides shorter than a row");
@@ -2084,11 +2085,12 @@ akvs_status akvs_store_pages(const void *k, int64_t ldk, const void *v, int64_t 
                             {"seq", x.s.seq, x.seq, INPUT},
                             {"len", x.s.len, x.len, INPUT},
                             {"table", x.s.table, x.table, INPUT},
+                            {"grown", x.s.grown, x.len, INPUT},
                             {"pages' k", p->k, x.codes, NONE},
                             {"pages' v", p->v, x.codes, NONE},
                             {"pages' k_meta", p->k_meta, x.meta, NONE},
                             {"pages' v_meta", p->v_meta, x.meta, NONE}};
-  st = check_apart(buffers, 10);
+  st = check_apart(buffers, 11);
   if (st) return st;
   LAUNCH(AKVS_K_OTHER, launch_store_pages(x.s, x.p, k, ldk, v, ldv, m->n_kv_heads, m->head_dim,
                                           stream));
@@ -2178,8 +2180,9 @@ akvs_status akvs_fork_pages(const akvs_page_table *t, int32_t n, const int32_t *
       {"dst", dst, ints, INPUT},
       {"table", x.table, (size_t)x.n_seq * x.max_pages * sizeof(int32_t), NONE},
       {"len", x.len, x.n_seq * sizeof(int32_t), NONE},
+      {"grown", x.grown, x.n_seq * sizeof(int32_t), NONE},
       {"ref", x.ref, x.n_pages * sizeof(int32_t), NONE}};
-  st = check_apart(buffers, 5);
+  st = check_apart(buffers, 6);
   if (st) return st;
   LAUNCH(AKVS_K_OTHER, launch_fork_pages(x, n, src, dst, stream));
   return AKVS_OK;
@@ -2195,8 +2198,9 @@ akvs_status akvs_free_pages(const akvs_page_table *t, int32_t n, const int32_t *
       {"seq", seq, n * sizeof(int32_t), INPUT},
       {"table", x.table, (size_t)x.n_seq * x.max_pages * sizeof(int32_t), NONE},
       {"len", x.len, x.n_seq * sizeof(int32_t), NONE},
+      {"grown", x.grown, x.n_seq * sizeof(int32_t), NONE},
       {"ref", x.ref, x.n_pages * sizeof(int32_t), NONE}};
-  st = check_apart(buffers, 4);
+  st = check_apart(buffers, 5);
   if (st) return st;
   LAUNCH(AKVS_K_OTHER, launch_free_pages(x, n, seq, stream));
   return AKVS_OK;
@@ -2230,9 +2234,10 @@ akvs_status akvs_grow_pages(const akvs_page_table *t, int32_t n, const int32_t *
       {"counts", counts, 2 * sizeof(int32_t), NONE},
       {"table", x.table, (size_t)x.n_seq * x.max_pages * sizeof(int32_t), NONE},
       {"len", x.len, x.n_seq * sizeof(int32_t), NONE},
+      {"grown", x.grown, x.n_seq * sizeof(int32_t), NONE},
       {"ref", x.ref, x.n_pages * sizeof(int32_t), NONE},
       {"ws", ws, need, NONE}};
-  st = check_apart(buffers, 10);
+  st = check_apart(buffers, 11);
   if (st) return st;
   LAUNCH(AKVS_K_OTHER, launch_grow_pages(x, n, seq, add, served, move_src, move_dst, counts,
                                          reinterpret_cast<int32_t *>(ws), stream));

@@ -20,6 +20,15 @@ struct Place {
 __device__ __forceinline__ void paged_places(const PagedBatch &s, const PagePool &p, int R0, int n,
                                              Place *places) {
   const int tid = threadIdx.x, end = min(R0 + n, s.n_rows);
+  // A request's table and keys: no keys where its sequence could not grow by these rows.
+  auto keys_of = [&](int b, int &len) {
+    const int32_t *table = paged_keys(s, b, len);
+    if (s.grown) {
+      const int q = s.seq ? s.seq[b] : b;
+      if (q >= 0 && q < s.n_seq && s.grown[q] == 0) len = 0;
+    }
+    return table;
+  };
   auto place = [&](const int32_t *table, int key, int len) {
     int page = -1;
     if (key >= 0 && key < len) page = table[key >> p.shift];
@@ -32,7 +41,7 @@ __device__ __forceinline__ void paged_places(const PagedBatch &s, const PagePool
       if (R0 + i < end) {
         const int b = (R0 + i) / s.rows_max;
         int len;
-        const int32_t *table = paged_keys(s, b, len);
+        const int32_t *table = keys_of(b, len);
         x = place(table, len - s.rows_max + (R0 + i - b * s.rows_max), len);
       }
       places[i] = x;
@@ -57,7 +66,7 @@ __device__ __forceinline__ void paged_places(const PagedBatch &s, const PagePool
       int r0, r1, len;
       paged_rows(s, b, r0, r1);
       if (r0 < end && r1 > R0) {
-        const int32_t *table = paged_keys(s, b, len);
+        const int32_t *table = keys_of(b, len);
         for (int r = max(r0, R0); r < min(r1, end); ++r)
           places[r - R0] = place(table, len - r1 + r, len);
       }
@@ -193,7 +202,10 @@ __global__ __launch_bounds__(256) void k_fork_pages(PageTable t, int n, const in
     to[j] = id;
     if (in_pool(t, id)) atomicAdd(&t.ref[id], 1);
   }
-  if (threadIdx.x == 0) t.len[b] = max(len, 0);
+  if (threadIdx.x == 0) {
+    t.len[b] = max(len, 0);
+    if (t.grown) t.grown[b] = 1;
+  }
 }
 
 // A block per sequence.
@@ -211,7 +223,10 @@ __global__ __launch_bounds__(256) void k_free_pages(PageTable t, int n, const in
     if (in_pool(t, id)) atomicSub(&t.ref[id], 1);
   }
   __syncthreads();
-  if (threadIdx.x == 0) t.len[a] = 0;
+  if (threadIdx.x == 0) {
+    t.len[a] = 0;
+    if (t.grown) t.grown[a] = 1;
+  }
 }
 
 // Pages are counted in segments of 1024, 4 a thread.
@@ -446,9 +461,10 @@ __global__ __launch_bounds__(256) void k_grow_assign(PageTable t, int n, int seg
   }
   const int i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   int x = -1, ends = 0, copies = 0, more = 0, old = 0, last = 0, first = 0;
-  int32_t *mine = nullptr;
+  int32_t *mine = nullptr, *grown = nullptr;
   if (i < n) {
     const int a = seq[i];
+    if (t.grown && a >= 0 && a < t.n_seq && w.claim[a] == i) grown = t.grown + a;
     x = w.need[i];
     ends = w.ends[i];
     copies = w.copies[i];
@@ -464,7 +480,10 @@ __global__ __launch_bounds__(256) void k_grow_assign(PageTable t, int n, int seg
   const int free_pages = seg_before(w.count, segs);
   if (i >= n) return;
   const bool ok = serves(x, ends, free_pages);
-  if (lane == 0) served[i] = ok;
+  if (lane == 0) {
+    served[i] = ok;
+    if (grown) *grown = ok;
+  }
   if (!ok) return;
   const int need = x & ~NEED_COPY, base = ends - need;
   const bool copy = x & NEED_COPY;

@@ -243,10 +243,11 @@ hipError_t launch_evict_gather(const void *k, const void *v, const EvictArgs &a,
                                int row_bytes, const int32_t *keep, void *k_out, void *v_out,
                                int32_t *lens_out, hipStream_t s);
 // ---- k_pages.hip, k_paged.hip -----------------------------------------------------------
-// A batch over sequences in pages (akvs_paged_cfg); limit: the most keys of a sequence.
+// A batch over sequences in pages (akvs_paged_cfg); limit: the most keys of a sequence; grown: where
+// rows are stored, else NULL.
 struct PagedBatch {
   int n_req, n_rows, rows_max, n_seq, max_pages, limit;
-  const int32_t *row_start, *seq, *len, *table;
+  const int32_t *row_start, *seq, *len, *table, *grown;
 };
 // One layer's pages: page_rows = 1 << shift; meta as (scale, zero) pairs of fp16.
 struct PagePool {
@@ -256,7 +257,7 @@ struct PagePool {
 };
 struct PageTable {
   int n_seq, max_pages, n_pages, shift;
-  int32_t *table, *len, *ref;
+  int32_t *table, *len, *ref, *grown;
 };
 hipError_t launch_store_pages(const PagedBatch &s, const PagePool &p, const void *k, long long ldk,
                               const void *v, long long ldv, int hkv, int hd, hipStream_t st);

@@ -440,7 +440,8 @@ class PagedCache:
         self.table = torch.full((n_seq, max_pages), -1, dtype=torch.int32, device=dev)
         self.len = torch.zeros(n_seq, dtype=torch.int32, device=dev)
         self.ref = torch.zeros(n_pages, dtype=torch.int32, device=dev)
-        self.t = akvs.page_table(self.table, self.len, self.ref, page_rows)
+        self.grown = torch.ones(n_seq, dtype=torch.int32, device=dev)
+        self.t = akvs.page_table(self.table, self.len, self.ref, page_rows, self.grown)
         self.layers = [akvs.pages(*x) for x in zip(self.k, self.v, self.k_meta, self.v_meta)]
 
     def _layer(self, layer):
@@ -487,13 +488,14 @@ class PagedCache:
         if rows_max is None:
             rows_max = n_rows if row_start is not None else n_rows // B
         return akvs.paged_cfg(B, n_rows, max(int(rows_max), 1), self.len, self.table, max_len,
-                              row_start, seq)
+                              row_start, seq, self.grown)
 
     def store(self, layer: int, k, v, batch):
         """New keys and values [rows][Hkv*hd] (columns of a packed projection, or dense
         [rows][Hkv][hd]) of a batch, whose sequences have grown by them (grow), into one layer's
-        pages. Sequences of the batch must not share the pages that the rows go to: pages that
-        grow gave them are their own."""
+        pages. A sequence that its last grow could not serve gets none of them: it stays as it was,
+        also under capture. Sequences of the batch must not share the pages that the rows go to:
+        pages that grow gave them are their own."""
         sh, eng = self.engine.shape, self.engine
         p = self._layer(layer)
         for name, x in (("k", k), ("v", v)):
@@ -547,7 +549,8 @@ class PagedCache:
     def grow(self, seq, add):
         """Room for add keys more (an int for all, ints, or an int32 tensor) in every sequence of
         seq, with a copy, in all layers, of a last page that is shared. Returns served (int32 per
-        sequence: 1, or 0 where there is no room and the sequence stays as it was)."""
+        sequence: 1, or 0 where there is no room and the sequence stays as it was, through the
+        batch's store too, until another grow serves it)."""
         seq = self._seq("seq", seq)
         n, eng = int(seq.numel()), self.engine
         if not torch.is_tensor(add):

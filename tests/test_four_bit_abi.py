@@ -306,3 +306,23 @@ def test_wrappers_check_their_tensors(lib):
             akvs.akvs_w4_product(x, w, wm, y, **kw)
     with pytest.raises(ValueError, match="weights"):
         akvs.akvs_w4_product(x, w, wm[:5], torch.zeros(2, 6))
+
+
+def test_the_marks_of_sequences_without_room(lib):
+    """`grown` lies apart from what a call writes, at an aligned address."""
+    E, m = akvs.AKVS_EINVAL, by(model())
+    for t in (table(grown=FAR[8] + 4), table(grown=FAR[0] + 16), table(grown=FAR[2] + 16),
+              table(grown=FAR[4])):
+        assert lib.akvs_fork_pages(by(t), 1, FAR[4], FAR[5], None) == E
+        assert lib.akvs_free_pages(by(t), 1, FAR[4], None) == E
+        assert lib.akvs_grow_pages(by(t), 1, FAR[4], FAR[5], FAR[6], FAR[7], FAR[9], FAR[10],
+                                   FAR[11], 1 << 39, None) == E
+    for x in (FAR[0], FAR[3] + 16):
+        assert lib.akvs_store_pages(FAR[4], 1024, FAR[5], 1024, by(cfg(grown=x)), by(pages()), m,
+                                    None) == E
+    lens, tab = torch.zeros(4, dtype=torch.int32), torch.zeros(4, 5, dtype=torch.int32)
+    for bad in (lens[:3], lens.long()):
+        with pytest.raises(ValueError, match="int32"):
+            akvs.page_table(tab, lens, torch.zeros(3, dtype=torch.int32), 16, bad)
+        with pytest.raises(ValueError, match="int32"):
+            akvs.paged_cfg(2, 2, 1, lens, tab, 16, grown=bad)

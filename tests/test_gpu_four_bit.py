@@ -818,3 +818,36 @@ def test_long_even_attention_in_one_block(geom, n_req, q_std):
         err = (lse[i:i + 64].double().flatten() - torch.logsumexp(sc, 1)).abs()
         reach = q[i:i + 64].to(DEV).double().view(-1, hd).abs() @ spread / math.sqrt(hd)
         assert bool((err <= ref.score_bound(reach, hd) + (keys + 16) * ref.EPS + 2.0 ** -22).all())
+
+
+@pytest.mark.parametrize("S,page_rows,wide,n_pages", SIZES)
+def test_marks_of_sequences_without_room(S, page_rows, wide, n_pages):
+    """grown: what served has of a sequence's first entry; sequences that end, or that branches are
+    made of, are as good as new."""
+    p = Pool(*random_tables(S + 1, S, page_rows, wide, n_pages), page_rows)
+    marks = ints([1] * S)
+    p.t = akvs.page_table(p.table, p.len, p.ref, page_rows, marks)
+    want, rng = [1] * S, random.Random(S)
+    for _ in range(3):
+        n = rng.randint(1, S + 3)
+        seq = [rng.randint(-1, S) for _ in range(n)]
+        add = [rng.choice([0, 1, page_rows, 5 * page_rows, -1]) for _ in range(n)]
+        served, _ = p.grow(seq, add)
+        for i, (a, ok) in enumerate(zip(seq, served)):
+            if 0 <= a < S and a not in seq[:i]:
+                want[a] = ok
+        assert marks.cpu().tolist() == want
+        gone = [rng.randint(-1, S) for _ in range(max(1, n // 3))]
+        akvs.akvs_free_pages(p.t, ints(gone))
+        p.want.free(gone)
+        src = [rng.randint(-1, S) for _ in range(n)]
+        dst = [rng.randint(-1, S) for _ in range(n)]
+        empty = [x == 0 for x in p.want.len]
+        akvs.akvs_fork_pages(p.t, ints(src), ints(dst))
+        p.want.fork(src, dst)
+        for a in gone + [b for a, b in zip(src, dst)
+                         if 0 <= a < S and 0 <= b < S and empty[b] and b not in src]:
+            if 0 <= a < S:
+                want[a] = 1
+        p.check()
+        assert marks.cpu().tolist() == want

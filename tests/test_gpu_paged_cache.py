@@ -224,3 +224,86 @@ def test_a_captured_step():
         want = eager.run(seq, [1] * n, 60 + t, check=False)
         assert torch.equal(y, want)
         assert torch.equal(d.cache.table, eager.cache.table)
+
+
+def test_tokens_of_a_sequence_without_room_are_stored_nowhere():
+    """What grow could not serve stays as it was through the step that follows, in its own pages and
+    in those that others share, until a grow serves it; eager, then captured."""
+    d = Decoder(5, 64, 6, 16)
+    c, n = d.cache, HKV * HD
+    assert d.grow([0, 3], [40, 20]) == [1, 1]
+    d.run([0, 3], [40, 20], 1)
+    d.fork([0, 0], [1, 2])  # 3 pages of three sequences, the last of them not full; one page is left
+    pools = (c.k, c.v, c.k_meta, c.v_meta)
+    k, v = (randn(i, 3, n).to(DEV, BF) for i in (5, 6))
+    batch = c.batch(3, [1, 0, 3])
+    seq = torch.tensor([1, 0, 3], dtype=torch.int32, device=DEV)
+    add = torch.ones(3, dtype=torch.int32, device=DEV)
+
+    def step():
+        served = c.grow(seq, add)
+        for i in range(2):
+            c.store(i, k, v, batch)
+        return served
+
+    def check(before, served, want):
+        assert served.tolist() == want
+        d.check_tables()
+        after = [x.clone() for x in pools]
+        for x, y in zip(after, before):  # all but the rows that went in are as before
+            for b, (a, ok) in enumerate(zip((1, 0, 3), want)):
+                if ok:
+                    j = d.want.len[a] - 1
+                    page = d.want.table[a][j // 16]
+                    assert not torch.equal(x[:, page, :, j % 16], y[:, page, :, j % 16])
+                    if page in moved:
+                        x[:, page] = y[:, page]
+                    x[:, page, :, j % 16] = y[:, page, :, j % 16]
+            assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+    # the copy for sequence 1 takes the last page; 0, whose page 2 shares, gets none; 3 has room
+    # (one that needs no page is served)
+    before = [x.clone() for x in pools]
+    got = step()
+    want, moves, _ = d.want.grow([1, 0, 3], [1, 1, 1])
+    moved = [b for _, b in moves]
+    assert want == [1, 0, 1]
+    check(before, got, want)
+    before = [x.clone() for x in pools]
+    got = step()
+    want, moves, _ = d.want.grow([1, 0, 3], [1, 1, 1])
+    moved = []
+    assert want == [1, 0, 1] and not moves
+    check(before, got, want)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = step()
+    for t in range(3):
+        if t == 2:  # then there is room
+            c.free([2])
+            d.want.free([2])
+        k.copy_(randn(20 + t, 3, n))
+        before = [x.clone() for x in pools]
+        g.replay()
+        torch.cuda.synchronize()
+        want, moves, _ = d.want.grow([1, 0, 3], [1, 1, 1])
+        assert want == [1, int(t == 2), 1] and not moves
+        check(before, got, want)
+
+
+@pytest.mark.parametrize("ends", [[0], [0, 1]])
+def test_a_sequence_without_room_begins_anew(ends):
+    """One that never had room becomes a branch, ended before or not: its tokens are stored."""
+    d = Decoder(3, 64, 2, 16)
+    c = d.cache
+    assert d.grow([0, 1], [17, 16]) == [1, 0]
+    k, v = (randn(i, 1, HKV * HD).to(DEV, BF) for i in (5, 6))
+    c.free(ends)
+    d.want.free(ends)
+    d.grow([2], 5)
+    d.fork([2], [1])
+    c.store(0, k, v, c.batch(1, [1]))  # (sequence 2 has the same page)
+    back = c.load(0, c.batch(1, [2]), F32)
+    for x, y in zip(back, (k, v)):
+        want = ref.values(*ref.quantise(y.view(1, HKV, HD).cpu()))
+        assert torch.equal(x.cpu(), want.float())
