@@ -251,6 +251,13 @@ def rows_ptr(t: torch.Tensor):
     return t.data_ptr(), stride[0] if shape[0] > 1 else width
 
 
+def need_rows(name: str, t: torch.Tensor, n: int, width: int, dtype: torch.dtype):
+    """Refuses a tensor that is not `n` rows or more, of `width` elements of this type."""
+    if t.dtype != dtype or t.shape[0] < n or t.numel() != t.shape[0] * width:
+        raise ValueError(f"{name}: need {n} {dtype} rows of {width}, got {t.dtype} "
+                         f"{tuple(t.shape)}")
+
+
 # The current stream's handle without building a torch.cuda.Stream object for it (3.1 us a
 # call, of the 9 us of a step entry's wrapper; 0.3 us this way), where this torch has it.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -600,6 +607,11 @@ def akvs_store_pages(k, v, cfg: PagedCfg, p: Pages, m: ModelCfg, stream=None):
 
 
 def akvs_load_pages(cfg: PagedCfg, p: Pages, m: ModelCfg, k_out, v_out, stream=None):
+    """k_out, v_out: one type, a row each of the batch's (either may be None)."""
+    width, dtype = m.n_kv_heads * m.head_dim, (v_out if k_out is None else k_out).dtype
+    for name, x in (("k_out", k_out), ("v_out", v_out)):
+        if x is not None:
+            need_rows(name, x, cfg.n_rows, width, dtype)
     _check(load().akvs_load_pages(ctypes.byref(cfg), ctypes.byref(p), ctypes.byref(m), ptr(k_out),
                                   ptr(v_out), dtype_code(v_out if k_out is None else k_out),
                                   stream_handle(stream)), "akvs_load_pages")

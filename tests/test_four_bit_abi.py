@@ -326,3 +326,20 @@ def test_the_marks_of_sequences_without_room(lib):
             akvs.page_table(tab, lens, torch.zeros(3, dtype=torch.int32), 16, bad)
         with pytest.raises(ValueError, match="int32"):
             akvs.paged_cfg(2, 2, 1, lens, tab, 16, grown=bad)
+
+
+def test_loading_checks_its_outputs(lib):
+    """Both of one type and as many rows as the batch's: nothing is written past their ends."""
+    m, F, B = model(), torch.float32, torch.bfloat16
+    c = akvs.paged_cfg(2, 5, 3, torch.zeros(4, dtype=torch.int32),
+                       torch.zeros(4, 5, dtype=torch.int32), 16,
+                       row_start=torch.zeros(3, dtype=torch.int32))
+    k = torch.zeros(3, 8, 16, 64, dtype=torch.uint8)
+    meta = torch.zeros(3, 8, 16, 2, 2, dtype=torch.float16)
+    p = akvs.pages(k, k.clone(), meta, meta.clone())
+    rows = lambda n, dt, hd=128: torch.zeros(n, 8, hd, dtype=dt)
+    for a, b in ((rows(5, F), rows(5, B)), (rows(5, B), rows(5, F)), (rows(4, F), rows(5, F)),
+                 (rows(5, F), rows(4, F)), (None, rows(4, B)), (rows(5, B, 64), None),
+                 (rows(5, F), rows(5, F, 64))):
+        with pytest.raises(ValueError, match="out"):
+            akvs.akvs_load_pages(c, p, m, a, b)
