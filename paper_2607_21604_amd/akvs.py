@@ -336,13 +336,27 @@ def evict_cfg(n_seq, n_keys, n_keep, n_first=0, n_recent=0, src_rows=0, dst_rows
 def pages(k, v, k_meta, v_meta) -> Pages:
     """One layer's pages: codes uint8 [n_pages][Hkv][page_rows][hd/2], meta fp16
     [n_pages][Hkv][page_rows][hd/64][2]; it holds references to the tensors."""
-    for name, x, dt in (("k", k, torch.uint8), ("v", v, torch.uint8),
-                        ("k_meta", k_meta, torch.float16), ("v_meta", v_meta, torch.float16)):
-        if x.dtype != dt or x.shape[:3] != k.shape[:3]:
-            raise ValueError(f"{name}: need {dt} pages of {tuple(k.shape[:3])} rows")
+    if k.dim() != 4 or k.shape[3] % 32:
+        raise ValueError("k: need [pages][KV heads][rows][hd / 2] codes")
+    groups = tuple(k.shape[:3]) + (k.shape[3] // 32, 2)
+    for name, x, dt, shape in (("k", k, torch.uint8, k.shape), ("v", v, torch.uint8, k.shape),
+                               ("k_meta", k_meta, torch.float16, groups),
+                               ("v_meta", v_meta, torch.float16, groups)):
+        if x.dtype != dt or x.shape != shape:
+            raise ValueError(f"{name}: need {dt} pages {tuple(shape)}, got {x.dtype} "
+                             f"{tuple(x.shape)}")
     p = Pages(ptr(k), ptr(v), ptr(k_meta), ptr(v_meta), int(k.shape[0]), int(k.shape[2]))
     p._keep = (k, v, k_meta, v_meta)
+    p._heads = (int(k.shape[1]), 2 * int(k.shape[3]))
     return p
+
+
+def fit_model(p: Pages, m: ModelCfg):
+    """Refuses pages() of other KV heads than the model's."""
+    heads = getattr(p, "_heads", None)
+    if heads is not None and heads != (m.n_kv_heads, m.head_dim):
+        raise ValueError(f"pages of {heads[0]} heads of {heads[1]}, the model has "
+                         f"{m.n_kv_heads} of {m.head_dim}")
 
 
 def page_table(table, lens, ref, page_rows, grown=None) -> PageTable:
@@ -601,6 +615,7 @@ def akvs_evict_cache(k, v, weights, cfg: EvictCfg, m: ModelCfg, keep, k_out, v_o
 
 def akvs_store_pages(k, v, cfg: PagedCfg, p: Pages, m: ModelCfg, stream=None):
     """k, v: rows that may lie apart (views of a packed projection output)."""
+    fit_model(p, m)
     (pk, ldk), (pv, ldv) = rows_ptr(k), rows_ptr(v)
     _check(load().akvs_store_pages(pk, ldk, pv, ldv, ctypes.byref(cfg), ctypes.byref(p),
                                    ctypes.byref(m), stream_handle(stream)), "akvs_store_pages")
@@ -608,6 +623,7 @@ def akvs_store_pages(k, v, cfg: PagedCfg, p: Pages, m: ModelCfg, stream=None):
 
 def akvs_load_pages(cfg: PagedCfg, p: Pages, m: ModelCfg, k_out, v_out, stream=None):
     """k_out, v_out: one type, a row each of the batch's (either may be None)."""
+    fit_model(p, m)
     width, dtype = m.n_kv_heads * m.head_dim, (v_out if k_out is None else k_out).dtype
     for name, x in (("k_out", k_out), ("v_out", v_out)):
         if x is not None:
@@ -623,6 +639,7 @@ def akvs_paged_workspace_size(m: ModelCfg, cfg: PagedCfg) -> int:
 
 def akvs_paged_attention(q, cfg: PagedCfg, p: Pages, m: ModelCfg, out, lse=None, ws=None,
                          stream=None):
+    fit_model(p, m)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
     _check(load().akvs_paged_attention(ptr(q), ctypes.byref(cfg), ctypes.byref(p), ctypes.byref(m),
                                        ptr(out), ptr(lse), ptr(ws), nbytes, stream_handle(stream)),
@@ -665,6 +682,7 @@ def akvs_compact_pages(t: PageTable, table_out, ref_out, move_src, move_dst, cou
 def akvs_move_pages(p: Pages, n_layers, m: ModelCfg, move_src, move_dst, max_moves, n_moves=None,
                     stream=None):
     """n_moves: device int32, its first entry counts (None: max_moves)."""
+    fit_model(p, m)
     _check(load().akvs_move_pages(ctypes.byref(p), int(n_layers), ctypes.byref(m),
                                   int_ptr(move_src, max_moves), int_ptr(move_dst, max_moves),
                                   int(max_moves), int_ptr(n_moves, 1), stream_handle(stream)),

@@ -343,3 +343,29 @@ def test_loading_checks_its_outputs(lib):
                  (rows(5, F), rows(5, F, 64))):
         with pytest.raises(ValueError, match="out"):
             akvs.akvs_load_pages(c, p, m, a, b)
+
+
+def test_pages_fit_the_model(lib):
+    """Codes and meta of one width, the model's, and of its KV heads: no call reads past them."""
+    u8, f16 = torch.uint8, torch.float16
+    k, meta = torch.zeros(3, 8, 16, 64, dtype=u8), torch.zeros(3, 8, 16, 2, 2, dtype=f16)
+    thin, one = torch.zeros(3, 8, 16, 32, dtype=u8), torch.zeros(3, 8, 16, 1, 2, dtype=f16)
+    for args in ((k, thin, meta, meta), (k, k, one, meta), (k, k, meta, one), (k, k, meta, meta[..., 0]),
+                 (thin, thin, meta, meta), (k[..., :48].contiguous(),) * 2 + (meta,) * 2,
+                 (k[:, 0].contiguous(),) * 2 + (meta[:, 0].contiguous(),) * 2):
+        with pytest.raises(ValueError):
+            akvs.pages(*args)
+    c = akvs.paged_cfg(2, 2, 1, torch.zeros(4, dtype=torch.int32),
+                       torch.zeros(4, 5, dtype=torch.int32), 16)
+    for args, m in (((thin, thin, one, one), model()), ((k, k, meta, meta), model(hd=64)),
+                    ((k, k, meta, meta), model(hq=16, hkv=16)), ((k, k, meta, meta), model(hkv=4))):
+        p = akvs.pages(*args)
+        rows = torch.zeros(2, m.n_kv_heads, m.head_dim, dtype=torch.bfloat16)
+        q = torch.zeros(2, m.n_q_heads, m.head_dim, dtype=torch.bfloat16)
+        moves = torch.zeros(2, dtype=torch.int32)
+        for call in (lambda: akvs.akvs_store_pages(rows, rows.clone(), c, p, m),
+                     lambda: akvs.akvs_load_pages(c, p, m, rows, rows.clone()),
+                     lambda: akvs.akvs_paged_attention(q, c, p, m, q.clone()),
+                     lambda: akvs.akvs_move_pages(p, 1, m, moves, moves.clone(), 2)):
+            with pytest.raises(ValueError, match="pages"):
+                call()
