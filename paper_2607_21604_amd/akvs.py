@@ -616,6 +616,9 @@ def akvs_evict_cache(k, v, weights, cfg: EvictCfg, m: ModelCfg, keep, k_out, v_o
 def akvs_store_pages(k, v, cfg: PagedCfg, p: Pages, m: ModelCfg, stream=None):
     """k, v: rows that may lie apart (views of a packed projection output)."""
     fit_model(p, m)
+    width = m.n_kv_heads * m.head_dim
+    need_rows("k", k, cfg.n_rows, width, torch.bfloat16)
+    need_rows("v", v, cfg.n_rows, width, torch.bfloat16)
     (pk, ldk), (pv, ldv) = rows_ptr(k), rows_ptr(v)
     _check(load().akvs_store_pages(pk, ldk, pv, ldv, ctypes.byref(cfg), ctypes.byref(p),
                                    ctypes.byref(m), stream_handle(stream)), "akvs_store_pages")
@@ -640,6 +643,11 @@ def akvs_paged_workspace_size(m: ModelCfg, cfg: PagedCfg) -> int:
 def akvs_paged_attention(q, cfg: PagedCfg, p: Pages, m: ModelCfg, out, lse=None, ws=None,
                          stream=None):
     fit_model(p, m)
+    n, width = cfg.n_rows, m.n_q_heads * m.head_dim
+    need_rows("q", q, n, width, torch.bfloat16)
+    need_rows("out", out, n, width, torch.bfloat16)
+    if lse is not None:
+        need_rows("lse", lse, n, m.n_q_heads, torch.float32)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
     _check(load().akvs_paged_attention(ptr(q), ctypes.byref(cfg), ctypes.byref(p), ctypes.byref(m),
                                        ptr(out), ptr(lse), ptr(ws), nbytes, stream_handle(stream)),

@@ -369,3 +369,27 @@ def test_pages_fit_the_model(lib):
                      lambda: akvs.akvs_move_pages(p, 1, m, moves, moves.clone(), 2)):
             with pytest.raises(ValueError, match="pages"):
                 call()
+
+
+def test_storing_and_attending_check_their_rows(lib):
+    """As many rows as the batch's, of the model's type and width."""
+    m, F, B = model(), torch.float32, torch.bfloat16
+    c = akvs.paged_cfg(2, 5, 3, torch.zeros(4, dtype=torch.int32),
+                       torch.zeros(4, 5, dtype=torch.int32), 16,
+                       row_start=torch.zeros(3, dtype=torch.int32))
+    k = torch.zeros(3, 8, 16, 64, dtype=torch.uint8)
+    meta = torch.zeros(3, 8, 16, 2, 2, dtype=torch.float16)
+    p = akvs.pages(k, k.clone(), meta, meta.clone())
+    z = lambda *s, dt=B: torch.zeros(s, dtype=dt)
+    ok = z(5, 8, 128)
+    for x in (z(4, 8, 128), z(5, 8, 64), z(5, 8, 128, dt=F), z(5, 512)):
+        for args in ((x, ok), (ok, x)):
+            with pytest.raises(ValueError, match="^[kv]:"):
+                akvs.akvs_store_pages(*args, c, p, m)
+    q, out, lse = z(5, 24, 128), z(5, 24, 128), z(5, 24, dt=F)
+    for bad, name in ((z(4, 24, 128), "q"), (z(5, 24, 128, dt=F), "q"), (z(4, 24, 128), "out"),
+                      (z(5, 24, 128, dt=F), "out"), (z(4, 24, dt=F), "lse"), (z(5, 24), "lse")):
+        a = dict(q=q, out=out, lse=lse)
+        a[name] = bad
+        with pytest.raises(ValueError, match=name + ":"):
+            akvs.akvs_paged_attention(a["q"], c, p, m, a["out"], a["lse"])
