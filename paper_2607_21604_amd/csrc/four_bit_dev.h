@@ -49,6 +49,12 @@ __device__ __forceinline__ float zero_of(uint32_t m) {
   return (float)__builtin_bit_cast(f16x2_t, m)[1];
 }
 
+// Whether scale * code + zero may lie past fp16's range, or is no number: true at |scale| > 2^11 or
+// |zero| > 2^15 (fp16 in the order of integers, both at once).
+__device__ __forceinline__ bool wide_values(uint32_t m) {
+  return (((m & 0x7fff7fffu) + 0x07ff17ffu) & 0x80008000u) != 0;
+}
+
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_t;
 // 1024 + c and 1024 + 16 c are fp16 numbers whose low bits are the nibble where it lies.
 struct F16Bits {

@@ -590,8 +590,8 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(
 
 // Many pairs. Block = 4 waves over 32 * groups pairs (groups 1, 2 or 4) and one chunk of keys. Tiles
 // of 64 keys are put into LDS as fp16, from codes loaded two tiles ahead: the keys' codes, exactly,
-// whose scales and zeros the scores get after the products; the values themselves, rounded once (no
-// value of the format lies outside fp16's range); a wave takes 32 pairs and 32 or 64 of the
+// whose scales and zeros the scores get after the products; the values themselves, rounded once (those
+// that may lie outside fp16's range apart); a wave takes 32 pairs and 32 or 64 of the
 // tile's keys: with 4 groups each wave has a group, with 2 two waves share a group's keys, with
 // 1 two of the waves only load. Scores are formed transposed, S^T = K Q^T (MFMA 32x32x16): lane l
 // holds 16 scores of pair l % 32, the operand layout of O^T = V^T P^T; V^T comes from row-major
@@ -733,17 +733,16 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
 
   // Dims are in LDS in the order of values8, 0 4 1 5 2 6 3 7 of every 8, until the end.
   // Values that some pair of the tile must not see take part with probability 0, and 0 * inf is
-  // NaN: where such a value is not finite, 0 goes to LDS, and the pairs that do see it get it
-  // added at the end. Pieces of the values are written in an order that differs by row, so that
-  // rows four apart in a bank do not meet.
+  // NaN; and scale and zero may make a value past fp16's range, which only 32 bits hold. Where a
+  // group's scale or zero lets that be, 0 goes to LDS, and the pairs that see it get it added at the
+  // end. Pieces of the values are written in an order that differs by row, so that rows four apart
+  // in a bank do not meet.
   auto store = [&](Codes &c, int key0, int buf) __attribute__((always_inline)) {
     _Float16 *ks = s_kv + buf * (KB + VB) + krow * KST + kq * (HD / 4);
     _Float16 *vs = s_kv + buf * (KB + VB) + KB + krow * VST + kq * (HD / 4);
-    if (key0 + PG_TILE > all_see && key0 + krow >= all_see) {
-      if ((c.vm & 0x7c00u) == 0x7c00u || (c.vm & 0x7c000000u) == 0x7c000000u) {
-        s_odd = 1;
-        c.vm = 0;
-      }
+    if (wide_values(c.vm)) {
+      s_odd = 1;
+      c.vm = 0;
     }
 #pragma unroll
     for (int j = 0; j < WORDS; ++j)
@@ -909,23 +908,48 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
       o[db][4 * q4 + 3] = __uint_as_float(x[3]);
     }
   if (!valid) return;
-  if (s_odd) {  // values left out above that this pair sees
-    for (int k = max(k0, all_see); k < seen; ++k) {
+  if (s_odd) {  // values left out above that this pair sees: finite ones by their probability
+    for (int k = k0; k < seen; ++k) {
       const int pg = table[k >> p.shift];
       if (pg < 0 || pg >= p.n_pages) continue;
       const size_t row = (((size_t)pg * hkv + h) << p.shift) + (k & mask);
+      bool any = false;
+      for (int gr = 0; gr < NG; ++gr) any |= wide_values(p.v_meta[row * NG + gr]);
+      if (!any) continue;
+      float s = 0.f;
+      for (int gr = 0; gr < NG; ++gr) {
+        const bf16_t *q = Q + ((size_t)r * hq + head) * HD + gr * 64;
+        const uint8_t *kc = p.k + row * RB + gr * 32;
+        float qc = 0.f, q1 = 0.f;
+        for (int e = 0; e < 64; e += 8) {
+          float x[8];
+          load8(q + e, x);
+          const uint32_t w = *reinterpret_cast<const uint32_t *>(kc + e / 2);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            qc = fmaf(x[j], (float)((w >> (4 * j)) & 15u), qc);
+            q1 += x[j];
+          }
+        }
+        const uint32_t mt = p.k_meta[row * NG + gr];
+        s += fmaf(scale_of(mt), qc, zero_of(mt) * q1);
+      }
+      const float pk = __builtin_amdgcn_exp2f(
+          fmaf(s, scale_log2, P_BITS - (m_run == -INFINITY ? 0.f : m_run)));
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
         const uint32_t mt = p.v_meta[row * NG + db / 2];
+        if (!wide_values(mt)) continue;
         const float sv = scale_of(mt), zv = zero_of(mt);
-        if (fabsf(sv) < INFINITY && fabsf(zv) < INFINITY) continue;
+        const float f = fabsf(sv) < INFINITY && fabsf(zv) < INFINITY ? pk : 1.f;
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) {
           const uint32_t w =
               *reinterpret_cast<const uint16_t *>(p.v + row * RB + db * 16 + q4 * 4 + hi * 2);
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            o[db][4 * q4 + j] += fmaf(sv, (float)((w >> (4 * j)) & 15u), zv);
+            o[db][4 * q4 + j] =
+                fmaf(f, fmaf(sv, (float)((w >> (4 * j)) & 15u), zv), o[db][4 * q4 + j]);
         }
       }
     }

@@ -88,6 +88,51 @@ def attention(q, k_pages, v_pages, table, lens, row_start, seq):
     return r
 
 
+def attention_by_heads(q, k_pages, v_pages, table, lens, row_start, seq):
+    """What attention() gives, a request's KV head at a time: for many rows or keys."""
+    n, hq, hd = q.shape
+    hkv = k_pages[0].shape[1]
+    G = hq // hkv
+    r = {"out": torch.full((n, hq, hd), math.nan, dtype=torch.float64)}
+    for x in ("mass", "coarse", "fine", "top"):
+        r[x] = torch.zeros(n, hq, hd, dtype=torch.float64)
+    r["lse"] = torch.full((n, hq), math.nan, dtype=torch.float64)
+    r["reach"] = torch.zeros(n, hq, dtype=torch.float64)
+    for b in range(len(row_start) - 1):
+        r0, r1, sq = int(row_start[b]), int(row_start[b + 1]), int(seq[b])
+        ln = int(lens[sq]) if 0 <= sq < len(lens) else 0
+        if r1 == r0:
+            continue
+        if ln == 0:
+            r["out"][r0:r1], r["lse"][r0:r1] = 0.0, -math.inf
+            continue
+        at = [place(table[sq], k_pages[0].shape[2], k_pages[0].shape[0], j) for j in range(ln)]
+        page, row = (torch.tensor(x) for x in zip(*at))
+        there = (page >= 0)[:, None]
+        seen = (torch.arange(ln - r1 + r0, ln) + 1).clamp(min=0)
+        hidden = (torch.arange(ln)[None] >= seen[:, None]).repeat_interleave(G, 0)
+        none = (seen == 0).repeat_interleave(G)
+        for h in range(hkv):
+            (kc, ks, kz), (vc, vs, vz) = (
+                [torch.where(there, x, 0.0) for x in parts(p[0][page.clamp(min=0), h, row],
+                                                           p[1][page.clamp(min=0), h, row])]
+                for p in (k_pages, v_pages))
+            rows, heads = slice(r0, r1), slice(h * G, (h + 1) * G)
+            qh = q[rows, heads].double().reshape(-1, hd)
+            sc = (qh @ (ks * kc + kz).T / math.sqrt(hd)).masked_fill(hidden, -math.inf)
+            lse = torch.logsumexp(sc, 1)
+            p = torch.exp(sc - torch.where(none, 0.0, lse)[:, None])
+            reach = (qh.abs() @ (60 * ks.abs() + kz.abs()).T / math.sqrt(hd)).masked_fill(hidden, 0)
+            mass = p @ (vs * vc + vz).abs()
+            big = torch.where(none[:, None], 0.0, mass).max(-1, keepdim=True).values
+            for name, x in (("out", p @ (vs * vc + vz)), ("lse", lse), ("mass", mass),
+                            ("coarse", p @ (vs.abs() * (vc - 8).abs())),
+                            ("fine", p @ (40 * vs.abs() + vz.abs())), ("reach", reach.max(1).values),
+                            ("top", (vs.abs().max() + big).expand_as(mass))):
+                r[name][rows, heads] = x.view(r[name][rows, heads].shape)
+    return r
+
+
 def score_bound(reach, hd):
     """Error of a score formed in 32 bits from codes: x = scale (c + 16) + (zero - 16 scale) with codes
     taken as 16 + c (or c), at most 64 products of q and up to 31, and 16 times q's sum, are added

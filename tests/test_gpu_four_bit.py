@@ -851,3 +851,23 @@ def test_marks_of_sequences_without_room(S, page_rows, wide, n_pages):
                 want[a] = 1
         p.check()
         assert marks.cpu().tolist() == want
+
+
+@pytest.mark.parametrize("geom,rows", [((28, 4, 128), [9, 2]), ((16, 8, 64), [30, 2]),
+                                       ((28, 4, 128), [6, 2])])
+@pytest.mark.parametrize("page_rows", [16, 64])
+@pytest.mark.parametrize("split", [False, True])
+def test_values_past_fp16s_range(geom, rows, page_rows, split):
+    """Finite scales and zeros whose values are not: a row that does not see such a key is as ever,
+    one that does has the definition's result, in the forms of many pairs and of few."""
+    lens = [1400 if split else 140, 1100 if split else 100]
+    n = rows[0]
+    for key in (lens[0] - n + 2, 70):
+        b = Batch(geom, page_rows, lens, rows, seed=83)
+        page, at = ref.place(b.table[0], page_rows, b.n_pages, key)
+        b.pools[1][1][page, :, at] = torch.tensor([8000.0, 60000.0], dtype=F16)
+        b.pools[1][1][page, 0, at, 0] = torch.tensor([-65504.0, -65504.0], dtype=F16)
+        page, at = ref.place(b.table[1], page_rows, b.n_pages, 99)  # (one group of two)
+        b.pools[1][1][page, :, at, -1] = torch.tensor([3000.0, -65000.0], dtype=F16)
+        b.attend()
+        b.check(ref.attention_by_heads(b.q[:b.n], *b.pools, b.table, b.lens, b.start, b.seq))
