@@ -154,7 +154,16 @@ class Engine:
                                v_cache)
         return q_out, k_cache, v_cache
 
-    def _row_start(self, n, row_start, rows_max, device):
+    def _ints_of(self, values):
+        """An int32 tensor of Python ints, without a wait for the device: through pinned memory,
+        which torch keeps until the copy is done. A captured copy would read it at every replay."""
+        cuda = self.device.type == "cuda"
+        if cuda and torch.cuda.is_current_stream_capturing():
+            raise ValueError("a call under capture takes device tensors, not lists")
+        x = torch.tensor(values, dtype=torch.int32, pin_memory=cuda)
+        return x.to(self.device, non_blocking=True) if cuda else x
+
+    def _row_start(self, n, row_start, rows_max):
         """A row_start that is no tensor is checked, gives rows_max and is copied to the device."""
         if row_start is not None and not torch.is_tensor(row_start):
             at = [operator.index(x) for x in row_start]
@@ -164,7 +173,7 @@ class Engine:
             if rows_max is not None and max(rows) > rows_max:
                 raise ValueError(f"row_start holds a request of {max(rows)} rows, rows_max is {rows_max}")
             rows_max = max(rows)
-            row_start = torch.tensor(at, dtype=torch.int32, device=device)
+            row_start = self._ints_of(at)
         return row_start, rows_max
 
     def _shared(self, q, k_prefix, k_own, own_len, row_start, rows_max):
@@ -176,7 +185,7 @@ class Engine:
         if k_own is not None:
             self._need("k_own", k_own, (None, None, sh.n_kv_heads, sh.head_dim))
             cap = int(k_own.shape[1])
-        row_start, rows_max = self._row_start(n, row_start, rows_max, q.device)
+        row_start, rows_max = self._row_start(n, row_start, rows_max)
         if row_start is not None:
             self._need("row_start", row_start, (None,), torch.int32)
             B = int(row_start.numel()) - 1
@@ -455,7 +464,7 @@ class PagedCache:
             seq = [operator.index(x) for x in seq]
             if any(not 0 <= x < self.n_seq for x in seq):
                 raise ValueError(f"{name}: need sequences of 0 to {self.n_seq - 1}")
-            seq = torch.tensor(seq, dtype=torch.int32, device=self.engine.device)
+            seq = self.engine._ints_of(seq)
         self.engine._here("the cache", self.table)
         return self.engine._need(name, seq, (None,), torch.int32)
 
@@ -473,7 +482,7 @@ class PagedCache:
             max_len = self.max_len
         if not 0 <= max_len <= self.max_len:
             raise ValueError(f"max_len {max_len} outside 0 to {self.max_len}")
-        row_start, rows_max = eng._row_start(n_rows, row_start, rows_max, eng.device)
+        row_start, rows_max = eng._row_start(n_rows, row_start, rows_max)
         if seq is not None:
             seq = self._seq("seq", seq)
             B = int(seq.numel())
@@ -554,10 +563,12 @@ class PagedCache:
         seq = self._seq("seq", seq)
         n, eng = int(seq.numel()), self.engine
         if not torch.is_tensor(add):
-            add = [operator.index(x) for x in (add if hasattr(add, "__len__") else [add] * n)]
+            each = hasattr(add, "__len__")
+            add = [operator.index(x) for x in (add if each else [add])]
             if any(x < 0 for x in add):
                 raise ValueError("add: need numbers >= 0")
-            add = torch.tensor(add, dtype=torch.int32, device=eng.device)
+            add = eng._ints_of(add) if each else torch.full((n,), add[0], dtype=torch.int32,
+                                                             device=eng.device)
         eng._need("add", add, (n,), torch.int32)
         served, src, dst, counts = self._ints(n), self._ints(n), self._ints(n), self._ints(2)
         ws = eng._scratch(akvs.akvs_pages_workspace_size(self.t, n))

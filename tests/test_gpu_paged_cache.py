@@ -307,3 +307,43 @@ def test_a_sequence_without_room_begins_anew(ends):
     for x, y in zip(back, (k, v)):
         want = ref.values(*ref.quantise(y.view(1, HKV, HD).cpu()))
         assert torch.equal(x.cpu(), want.float())
+
+
+def test_calls_with_lists_do_not_wait_for_the_device():
+    """Lists and numbers are copied without a wait."""
+    d = Decoder(4, 64, 8, 16)
+    x, c = randn(1, 3, HKV * HD).to(DEV, BF), d.cache
+    torch.cuda.synchronize()
+    torch.cuda.set_sync_debug_mode("error")
+    try:
+        served = c.grow([0, 3], [20, 3])
+        c.fork([0], [1])
+        c.grow([0, 1, 3], 1)
+        batch = c.batch(3, [0, 1, 3], [0, 1, 2, 3])
+        c.store(1, x, x, batch)
+        c.free([3])
+        c.free([])
+        c.compact()
+    finally:
+        torch.cuda.set_sync_debug_mode("default")
+    assert served.tolist() == [1, 1] and c.len.tolist() == [21, 21, 0, 0]
+
+
+def test_lists_are_refused_under_capture():
+    """A replay would read a list's copy from memory that is another's by then."""
+    c = Decoder(4, 64, 8, 16).cache
+    ids = torch.tensor([0, 3], dtype=torch.int32, device=DEV)
+    for call in (lambda: c.grow([0], 1), lambda: c.grow(ids, [1, 2]), lambda: c.free([1]),
+                 lambda: c.batch(2, [0, 3]), lambda: c.batch(2, ids, [0, 1, 2])):
+        g = torch.cuda.CUDAGraph()
+        with pytest.raises(ValueError, match="capture"):
+            with torch.cuda.graph(g):
+                ids.add_(0)
+                call()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        served = c.grow(ids, 2)
+    for t in range(3):
+        g.replay()
+        torch.cuda.synchronize()
+        assert served.tolist() == [1, 1] and c.len.tolist() == [2 + 2 * t, 0, 0, 2 + 2 * t]
