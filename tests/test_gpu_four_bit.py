@@ -871,3 +871,159 @@ def test_values_past_fp16s_range(geom, rows, page_rows, split):
         b.pools[1][1][page, :, at, -1] = torch.tensor([3000.0, -65000.0], dtype=F16)
         b.attend()
         b.check(ref.attention_by_heads(b.q[:b.n], *b.pools, b.table, b.lens, b.start, b.seq))
+
+# ---- forms that a batch's own sizes choose --------------------------------------------------------
+# More than 48 (row, query head) pairs of a KV head and request take k_paged_many, the others
+# k_paged_few; products of 17 rows or more take k_w4 with one or two tiles of outputs a wave.
+
+MANY = [((28, 4, 128), [9, 2]), ((16, 8, 64), [30, 2])]  # 63 and 60 pairs of a KV head
+
+
+def chunks(b, c):
+    """Parts that the keys are cut into: each has 16 bytes and an fp16 output of every pair."""
+    n = akvs.akvs_paged_workspace_size(b.m, c)
+    return n // (b.q.shape[0] * b.hq * (16 + 2 * b.hd)) if n else 1
+
+
+@pytest.mark.parametrize("geom,rows", MANY)
+def test_what_is_not_a_number_in_many_pairs(geom, rows):
+    """Keys and values without a number, and infinite zeros, where some rows of a question see them
+    and others do not, and where all do."""
+    n = rows[0]
+    for which, what in ((1, 0), (0, 0), (1, 1)):
+        for key in (40 - n + 2, 20):
+            b = Batch(geom, 16, [40, 100], rows, seed=71 + which)
+            r = b.expect()
+            page, at = ref.place(b.table[0], 16, b.n_pages, key)
+            if what:
+                b.pools[which][1][page, :, at, :, 1] = math.inf
+            else:
+                b.pools[which][1][page, :, at] = math.nan
+            b.attend()
+            bad = slice(max(key - (40 - n), 0), n)
+            hit = (b.out == math.inf) if what else torch.isnan(b.out)
+            assert bool(hit[bad].all())
+            b.out[bad] = 0
+            if not what:
+                b.lse[bad] = 0
+            for x in r:
+                if not what or x not in ("lse", "reach"):
+                    r[x][bad] = 0
+            b.check(r)
+
+
+@pytest.mark.parametrize("geom,rows", MANY)
+def test_missing_pages_and_lengths_in_many_pairs(geom, rows):
+    """As test_indices_out_of_range: sequences that do not exist, missing pages, lengths cut."""
+    n = rows[0]
+    b = Batch(geom, 16, [40, 50, 133, 20], [2, n, 1, n, 3], seq=[0, 9, -1, 2, 1], seed=19)
+    b.table[0][1] = -1
+    b.table[0][2] = b.n_pages
+    b.table[2][0] = b.table[2][7] = -(1 << 31)
+    b.attend()
+    b.check()
+    assert bool((b.out[2:3 + n] == 0).all()) and bool((b.lse[2:3 + n] == -math.inf).all())
+    for page in (16, 64):
+        b = Batch(geom, page, [40, 50], [n, n - 1], seed=23, max_len=33)
+        b.attend()
+        b.lens = [33, 33]
+        b.check()
+        b.lens = [-5, 1 << 30]
+        b.attend()
+        b.lens = [0, 33]
+        b.check()
+
+
+@pytest.mark.parametrize("geom,rows", MANY)
+def test_large_scores_in_many_pairs(geom, rows):
+    """Scores of hundreds; queries whose elements lie far apart within a row (down to 2^-24 of its
+    largest they are taken exactly)."""
+    b = Batch(geom, 64, [200, 333], rows, seed=17, q_std=40.0)
+    b.attend()
+    b.check()
+    b = Batch(geom, 32, [200, 333], rows, seed=18)
+    e = torch.randint(0, 13, b.q.shape, generator=torch.Generator().manual_seed(3))
+    b.q = (b.q.float() * torch.exp2(-e.float())).to(BF)
+    b.q[3:] *= 1e-6
+    b.attend()
+    b.check()
+
+
+@pytest.mark.parametrize("geom,rows", MANY)
+def test_the_smallest_and_largest_scales_in_many_pairs(geom, rows):
+    b = Batch(geom, 16, [40, 133], rows, seed=13)
+    for codes, meta in b.pools:
+        live = ~torch.isnan(meta[..., 0])
+        pick = torch.randint(0, 4, live.shape, generator=torch.Generator().manual_seed(1))
+        meta[(pick == 0) & live] = torch.tensor([6e-8, -3e-7], dtype=F16)
+        meta[(pick == 1) & live] = torch.tensor([0.0, 0.75], dtype=F16)
+    vm = b.pools[1][1]
+    vm[(torch.rand(vm.shape[:-1], generator=torch.Generator().manual_seed(2)) < 0.2) &
+       ~torch.isnan(vm[..., 0])] = torch.tensor([8000.0, -60000.0], dtype=F16)
+    b.attend()
+    b.check()
+
+
+@pytest.mark.parametrize("geom,rows,lens,n_req,many,parts", [
+    # up to eight parts of 4096 pairs or more: the merge with a thread per eight dims
+    ((40, 8, 128), [96, 40, 9], [1850, 1400, 500], 3, True, (5, 8)),
+    ((16, 8, 64), [200, 64, 9], [1850, 1400, 500], 3, True, (5, 8)),
+    # more than 64 requests: the cut is the host's
+    ((20, 1, 128), [3], [1500, 900, 1, 1300], 70, True, (2, 1024)),
+    ((20, 1, 128), [1], [3000, 900, 0, 2600], 70, False, (2, 1024)),
+    ((8, 1, 64), [2], [3000, 900, 0, 2600], 70, False, (2, 1024)),
+])
+def test_many_requests_and_pairs_in_parts(geom, rows, lens, n_req, many, parts):
+    b = Batch(geom, 64, lens, [rows[i % len(rows)] for i in range(n_req)],
+              seq=[i % len(lens) for i in range(n_req)], seed=61)
+    c = b.cfg()
+    assert (max(b.rows) * b.hq // b.hkv > 48) == many
+    assert parts[0] <= chunks(b, c) <= parts[1]
+    assert parts[1] > 8 or b.n * b.hq >= 4096
+    b.attend()
+    b.check(ref.attention_by_heads(b.q[:b.n], *b.pools, b.table, b.lens, b.start, b.seq))
+
+
+@pytest.mark.parametrize("rows,n_in,n_out,xt", [
+    # two tiles of outputs a wave, sliced or not, of two, three and four tiles of rows, of fp32 rows,
+    # and the last rows of many
+    (33, 27648, 5120, BF), (17, 16384, 8208, BF), (17, 2048, 40000, BF), (50, 27648, 5120, BF),
+    (64, 5120, 16400, BF), (64 + 37, 27648, 5120, BF), (64 + 7, 5120, 16400, BF),
+    (32, 27648, 5120, F32), (17, 5120, 16400, F32), (32 + 20, 4096, 20000, F32)])
+@pytest.mark.parametrize("add", [False, True])
+def test_w4_of_several_tiles_a_wave(rows, n_in, n_out, xt, add):
+    """Weights of 40 (or 16) rows over and over: each of their outputs is the same."""
+    few = 40 if n_out % 40 == 0 else 16
+    codes, meta = weights(rows, few, n_in)
+    x = randn(5, rows, n_in, dt=xt)
+    h = randn(6, rows, n_out) if add else None
+    y = torch.full((rows, n_out), 7.0, device=DEV)
+    again = n_out // few
+    akvs.akvs_w4_product(x.to(DEV), codes.to(DEV).repeat(again, 1), meta.to(DEV).repeat(again, 1, 1),
+                         y, resid=h.to(DEV) if add else None, ws=w4_ws(rows, n_out, n_in))
+    want, tol = ref.product(x, codes, meta)
+    want, tol = want.repeat(1, again), tol.repeat(1, again)
+    if add:
+        want = want + h.double()
+    assert bool(((y.double().cpu() - want).abs() <= rounded(tol, want, F32)).all())
+
+
+@pytest.mark.parametrize("rows,n_in,n_out", [(64, 256, 1000), (49, 960, 4096), (64, 5120, 55296),
+                                             (64 + 50, 320, 260)])
+def test_w4_swiglu_of_four_tiles_of_rows(rows, n_in, n_out):
+    """As above: gate and up rows of a few outputs over and over."""
+    few = 1000 if n_out == 1000 else 26 if n_out == 260 else 64
+    codes, meta = weights(7, few, n_in)
+    half = n_out // 2
+    take = torch.cat([torch.arange(half) % (few // 2), few // 2 + torch.arange(half) % (few // 2)])
+    x = randn(8, rows, n_in, dt=BF, std=2.0)
+    y = torch.full((rows, half), 7.0, device=DEV)
+    akvs.akvs_w4_product(x.to(DEV), codes.to(DEV)[take.to(DEV)], meta.to(DEV)[take.to(DEV)], y,
+                         akvs.AKVS_W4_SWIGLU, ws=w4_ws(rows, n_out, n_in))
+    z, tol = ref.product(x, codes, meta)
+    (g, u), (tg, tu) = z.chunk(2, 1), tol.chunk(2, 1)
+    s = g * torch.sigmoid(g)
+    want = s * u
+    tol = 1.1 * tg * (u.abs() + tu) + tu * s.abs() + 2.0 ** -20 * (1 + g.abs()) * want.abs()
+    want, tol = want[:, take[:half]], tol[:, take[:half]]
+    assert bool(((y.double().cpu() - want).abs() <= rounded(tol, want, F32)).all())
