@@ -239,23 +239,24 @@ def int_ptr(t: Optional[torch.Tensor], least: int):
     return ptr(t)
 
 
-def rows_ptr(t: torch.Tensor):
+def rows_ptr(t: torch.Tensor, name: str = "", n: int = 0, of: int = 0):
     """(pointer, elements between rows) of rows that are dense but may lie apart, as the
-    columns of a packed projection output do."""
+    columns of a packed projection output do. With `of`: n bf16 rows or more of that width."""
     shape, stride = t.shape, t.stride()
     width = 1
     for i in range(len(shape) - 1, 0, -1):
         if stride[i] != width and shape[i] != 1:
             raise ValueError("each row must be contiguous")
         width *= shape[i]
+    if of and (shape[0] < n or width != of or t.dtype != torch.bfloat16):
+        raise ValueError(f"{name}: need {n} bf16 rows of {of}, got {t.dtype} {tuple(shape)}")
     return t.data_ptr(), stride[0] if shape[0] > 1 else width
 
 
-def need_rows(name: str, t: torch.Tensor, n: int, width: int, dtype: torch.dtype):
-    """Refuses a tensor that is not `n` rows or more, of `width` elements of this type."""
-    if t.dtype != dtype or t.shape[0] < n or t.numel() != t.shape[0] * width:
-        raise ValueError(f"{name}: need {n} {dtype} rows of {width}, got {t.dtype} "
-                         f"{tuple(t.shape)}")
+def need_bytes(name: str, t: torch.Tensor, n: int, dtype: torch.dtype):
+    """Refuses a tensor of another type, or of fewer than n bytes."""
+    if t.dtype != dtype or t.nbytes < n:
+        raise ValueError(f"{name}: need {n} bytes of {dtype}, got {t.dtype} {tuple(t.shape)}")
 
 
 # The current stream's handle without building a torch.cuda.Stream object for it (3.1 us a
@@ -616,10 +617,8 @@ def akvs_evict_cache(k, v, weights, cfg: EvictCfg, m: ModelCfg, keep, k_out, v_o
 def akvs_store_pages(k, v, cfg: PagedCfg, p: Pages, m: ModelCfg, stream=None):
     """k, v: rows that may lie apart (views of a packed projection output)."""
     fit_model(p, m)
-    width = m.n_kv_heads * m.head_dim
-    need_rows("k", k, cfg.n_rows, width, torch.bfloat16)
-    need_rows("v", v, cfg.n_rows, width, torch.bfloat16)
-    (pk, ldk), (pv, ldv) = rows_ptr(k), rows_ptr(v)
+    n, width = cfg.n_rows, m.n_kv_heads * m.head_dim
+    (pk, ldk), (pv, ldv) = rows_ptr(k, "k", n, width), rows_ptr(v, "v", n, width)
     _check(load().akvs_store_pages(pk, ldk, pv, ldv, ctypes.byref(cfg), ctypes.byref(p),
                                    ctypes.byref(m), stream_handle(stream)), "akvs_store_pages")
 
@@ -627,10 +626,11 @@ def akvs_store_pages(k, v, cfg: PagedCfg, p: Pages, m: ModelCfg, stream=None):
 def akvs_load_pages(cfg: PagedCfg, p: Pages, m: ModelCfg, k_out, v_out, stream=None):
     """k_out, v_out: one type, a row each of the batch's (either may be None)."""
     fit_model(p, m)
-    width, dtype = m.n_kv_heads * m.head_dim, (v_out if k_out is None else k_out).dtype
-    for name, x in (("k_out", k_out), ("v_out", v_out)):
-        if x is not None:
-            need_rows(name, x, cfg.n_rows, width, dtype)
+    first = v_out if k_out is None else k_out
+    n = cfg.n_rows * m.n_kv_heads * m.head_dim * first.itemsize
+    need_bytes("k_out" if k_out is not None else "v_out", first, n, first.dtype)
+    if k_out is not None and v_out is not None:
+        need_bytes("v_out", v_out, n, k_out.dtype)
     _check(load().akvs_load_pages(ctypes.byref(cfg), ctypes.byref(p), ctypes.byref(m), ptr(k_out),
                                   ptr(v_out), dtype_code(v_out if k_out is None else k_out),
                                   stream_handle(stream)), "akvs_load_pages")
@@ -643,11 +643,11 @@ def akvs_paged_workspace_size(m: ModelCfg, cfg: PagedCfg) -> int:
 def akvs_paged_attention(q, cfg: PagedCfg, p: Pages, m: ModelCfg, out, lse=None, ws=None,
                          stream=None):
     fit_model(p, m)
-    n, width = cfg.n_rows, m.n_q_heads * m.head_dim
-    need_rows("q", q, n, width, torch.bfloat16)
-    need_rows("out", out, n, width, torch.bfloat16)
+    n = cfg.n_rows * m.n_q_heads
+    need_bytes("q", q, n * m.head_dim * 2, torch.bfloat16)
+    need_bytes("out", out, n * m.head_dim * 2, torch.bfloat16)
     if lse is not None:
-        need_rows("lse", lse, n, m.n_q_heads, torch.float32)
+        need_bytes("lse", lse, n * 4, torch.float32)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
     _check(load().akvs_paged_attention(ptr(q), ctypes.byref(cfg), ctypes.byref(p), ctypes.byref(m),
                                        ptr(out), ptr(lse), ptr(ws), nbytes, stream_handle(stream)),
