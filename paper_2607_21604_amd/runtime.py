@@ -154,16 +154,17 @@ class Engine:
                                v_cache)
         return q_out, k_cache, v_cache
 
-    def _ints_of(self, values):
-        """An int32 tensor of Python ints, without a wait for the device: through pinned memory,
-        which torch keeps until the copy is done. A captured copy would read it at every replay."""
+    def _ints_of(self, values, keep=False):
+        """An int32 tensor of Python ints for calls on the current stream, without a wait for the
+        device: through pinned memory, which torch keeps until the copy is done (a captured copy would
+        read it at every replay). keep: for later calls on any stream, after a wait for the copy."""
         cuda = self.device.type == "cuda"
         if cuda and torch.cuda.is_current_stream_capturing():
             raise ValueError("a call under capture takes device tensors, not lists")
         x = torch.tensor(values, dtype=torch.int32, pin_memory=cuda)
-        return x.to(self.device, non_blocking=True) if cuda else x
+        return x.to(self.device, non_blocking=not keep) if cuda else x
 
-    def _row_start(self, n, row_start, rows_max):
+    def _row_start(self, n, row_start, rows_max, keep=False):
         """A row_start that is no tensor is checked, gives rows_max and is copied to the device."""
         if row_start is not None and not torch.is_tensor(row_start):
             at = [operator.index(x) for x in row_start]
@@ -173,7 +174,7 @@ class Engine:
             if rows_max is not None and max(rows) > rows_max:
                 raise ValueError(f"row_start holds a request of {max(rows)} rows, rows_max is {rows_max}")
             rows_max = max(rows)
-            row_start = self._ints_of(at)
+            row_start = self._ints_of(at, keep)
         return row_start, rows_max
 
     def _shared(self, q, k_prefix, k_own, own_len, row_start, rows_max):
@@ -430,9 +431,10 @@ class PagedCache:
     """Keys and values of many sequences, in pages of 4-bit codes that sequences may share: pools
     of all the engine's layers and one table of pages (akvs_pages, akvs_page_table). Everything is
     allocated here, once: the methods that follow run on the current stream without a host
-    synchronisation and can be captured. Sequences (`seq`, `src`, `dst`) are given as ints, which
-    are checked and copied to the device, or (as under capture) as an int32 tensor, whose entries
-    out of range the device leaves out."""
+    synchronisation and can be captured, but for a batch of ints, which may be used on any stream and
+    waits for their copy. Sequences (`seq`, `src`, `dst`) are given as ints, which are checked and
+    copied to the device, or (as under capture) as an int32 tensor, whose entries out of range the
+    device leaves out."""
 
     def __init__(self, engine: Engine, n_seq: int, max_len: int, n_pages: int, page_rows: int = 64):
         if min(n_seq, max_len) < 1 or n_pages < 0 or page_rows not in (16, 32, 64, 128, 256):
@@ -459,12 +461,12 @@ class PagedCache:
         self.engine._here("the cache", self.table)
         return self.layers[layer]
 
-    def _seq(self, name, seq):
+    def _seq(self, name, seq, keep=False):
         if not torch.is_tensor(seq):
             seq = [operator.index(x) for x in seq]
             if any(not 0 <= x < self.n_seq for x in seq):
                 raise ValueError(f"{name}: need sequences of 0 to {self.n_seq - 1}")
-            seq = self.engine._ints_of(seq)
+            seq = self.engine._ints_of(seq, keep)
         self.engine._here("the cache", self.table)
         return self.engine._need(name, seq, (None,), torch.int32)
 
@@ -482,9 +484,9 @@ class PagedCache:
             max_len = self.max_len
         if not 0 <= max_len <= self.max_len:
             raise ValueError(f"max_len {max_len} outside 0 to {self.max_len}")
-        row_start, rows_max = eng._row_start(n_rows, row_start, rows_max)
+        row_start, rows_max = eng._row_start(n_rows, row_start, rows_max, keep=True)
         if seq is not None:
-            seq = self._seq("seq", seq)
+            seq = self._seq("seq", seq, keep=True)
             B = int(seq.numel())
         else:
             B = self.n_seq if row_start is None else int(row_start.numel()) - 1

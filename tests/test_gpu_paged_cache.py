@@ -313,13 +313,13 @@ def test_calls_with_lists_do_not_wait_for_the_device():
     """Lists and numbers are copied without a wait."""
     d = Decoder(4, 64, 8, 16)
     x, c = randn(1, 3, HKV * HD).to(DEV, BF), d.cache
+    batch = c.batch(3, [0, 1, 3], [0, 1, 2, 3])
     torch.cuda.synchronize()
     torch.cuda.set_sync_debug_mode("error")
     try:
         served = c.grow([0, 3], [20, 3])
         c.fork([0], [1])
         c.grow([0, 1, 3], 1)
-        batch = c.batch(3, [0, 1, 3], [0, 1, 2, 3])
         c.store(1, x, x, batch)
         c.free([3])
         c.free([])
@@ -327,6 +327,27 @@ def test_calls_with_lists_do_not_wait_for_the_device():
     finally:
         torch.cuda.set_sync_debug_mode("default")
     assert served.tolist() == [1, 1] and c.len.tolist() == [21, 21, 0, 0]
+
+
+def test_a_batch_of_lists_is_used_on_another_stream():
+    """Made while the current stream is busy, used at once on one that does not wait for it."""
+    d, own = Decoder(4, 64, 8, 16), Decoder(4, 64, 8, 16)
+    x = randn(1, 3, HKV * HD).to(DEV, BF)
+    for e in (d, own):
+        e.grow([0, 1, 3], 1)
+        e.cache.store(1, x, x, e.cache.batch(3, [0, 1, 3]))
+    big = torch.ones(1 << 28, device=DEV)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for i in range(4):
+        for _ in range(30):
+            big.mul_(1.0)
+        batch = d.cache.batch(3, [3, 0, 1], [0, 1, 2, 3])
+        with torch.cuda.stream(side):
+            got = d.cache.load(1, batch, F32)
+        side.synchronize()
+        want = own.cache.load(1, own.cache.batch(3, [3, 0, 1]), F32)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
 def test_lists_are_refused_under_capture():
