@@ -93,6 +93,7 @@ class Pages(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_meta", ctypes.c_void_p),
                 ("v_meta", ctypes.c_void_p), ("n_pages", ctypes.c_int32),
                 ("page_rows", ctypes.c_int32)]
+    _heads = None  # (KV heads, head dim) where pages() made it
 
 
 class PageTable(ctypes.Structure):
@@ -354,8 +355,8 @@ def pages(k, v, k_meta, v_meta) -> Pages:
 
 def fit_model(p: Pages, m: ModelCfg):
     """Refuses pages() of other KV heads than the model's."""
-    heads = getattr(p, "_heads", None)
-    if heads is not None and heads != (m.n_kv_heads, m.head_dim):
+    heads = p._heads
+    if heads and (heads[0] != m.n_kv_heads or heads[1] != m.head_dim):
         raise ValueError(f"pages of {heads[0]} heads of {heads[1]}, the model has "
                          f"{m.n_kv_heads} of {m.head_dim}")
 
@@ -628,7 +629,8 @@ def akvs_load_pages(cfg: PagedCfg, p: Pages, m: ModelCfg, k_out, v_out, stream=N
     fit_model(p, m)
     first = v_out if k_out is None else k_out
     n = cfg.n_rows * m.n_kv_heads * m.head_dim * first.itemsize
-    need_bytes("k_out" if k_out is not None else "v_out", first, n, first.dtype)
+    if first.nbytes < n:
+        need_bytes("k_out" if k_out is not None else "v_out", first, n, first.dtype)
     if k_out is not None and v_out is not None:
         need_bytes("v_out", v_out, n, k_out.dtype)
     _check(load().akvs_load_pages(ctypes.byref(cfg), ctypes.byref(p), ctypes.byref(m), ptr(k_out),
@@ -643,11 +645,13 @@ def akvs_paged_workspace_size(m: ModelCfg, cfg: PagedCfg) -> int:
 def akvs_paged_attention(q, cfg: PagedCfg, p: Pages, m: ModelCfg, out, lse=None, ws=None,
                          stream=None):
     fit_model(p, m)
-    n = cfg.n_rows * m.n_q_heads
-    need_bytes("q", q, n * m.head_dim * 2, torch.bfloat16)
-    need_bytes("out", out, n * m.head_dim * 2, torch.bfloat16)
+    pairs = cfg.n_rows * m.n_q_heads
+    n = 2 * pairs * m.head_dim
+    if q.nbytes < n or out.nbytes < n or not q.dtype is out.dtype is torch.bfloat16:
+        need_bytes("q", q, n, torch.bfloat16)
+        need_bytes("out", out, n, torch.bfloat16)
     if lse is not None:
-        need_bytes("lse", lse, n * 4, torch.float32)
+        need_bytes("lse", lse, 4 * pairs, torch.float32)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
     _check(load().akvs_paged_attention(ptr(q), ctypes.byref(cfg), ctypes.byref(p), ctypes.byref(m),
                                        ptr(out), ptr(lse), ptr(ws), nbytes, stream_handle(stream)),

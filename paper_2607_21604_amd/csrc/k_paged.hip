@@ -52,10 +52,10 @@ __device__ __forceinline__ float wave_all(float x) {
 // the least for which the requests' own lengths, a lane each, make one round of blocks, tried at 1 to
 // 7/4 of an even share and cut into no more than the plan's chunks; the same in all blocks of a call.
 // It costs 0.6 to 1.5 us, and makes up for a max_len far above the lengths, as captured calls have it:
-//   8 requests of 3000 to 4000 keys, 28/4 heads: 14.2 us for any max_len; by the plan's cut 13.8 for a
-//   max_len of 4000, 16.3 for 16000, 33 for 64000. 6 questions of 9 to 96 rows over 2000 to 8192 keys,
-//   40/8 heads: 77 us, 103 for a max_len of 131000; 94 and 257. (32 requests in two chunks each gain 1
-//   of 36: k_paged_few has the plan's cut below 8 chunks.)
+//   8 requests of 3000 to 4000 keys, 28/4 heads: 15.0 us for any max_len; by the plan's cut 14.6 for a
+//   max_len of 4000, 16.7 for 16000, 33 for 64000. 6 questions of 39 to 92 rows over 3155 to 8115 keys,
+//   40/8 heads: 100 us, 107 for a max_len of 131000; 102 and 307. (32 requests of 4500 to 8128 keys in
+//   two chunks each are as fast either way: k_paged_few has the plan's cut below 8 chunks.)
 __device__ __forceinline__ const int32_t *paged_request(const PagedBatch &s, const PagedPlan &plan,
                                                         int G, int b, int &r0, int &r1, int &len,
                                                         int &chunk_keys) {
@@ -599,8 +599,8 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(
 // probabilities fp16 times 2^7, so that what is lost below fp16's smallest is 2^-32 of the
 // largest; statistics and outputs are fp32.
 //   6 questions of 39 to 92 rows over 3155 to 8115 keys, 40/8 heads: 97 us, 345 TFLOP/s. The matrix
-//   cores are busy a sixth of that, the vector unit a third, LDS a fifth: two waves a SIMD wait for
-//   each other's steps, and the longest question's blocks for nobody.
+//   cores are busy 0.16 of that, the vector unit 0.32, LDS 0.21, at 1.1 waves a SIMD of the 2 that fit:
+//   they wait for each other's steps, and the longest question's blocks for nobody.
 template <int HD, bool WIDE>
 __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p, PagedPlan plan,
                                                        const bf16_t *__restrict__ Q, int hq,
