@@ -587,9 +587,9 @@ size_t akvs_paged_workspace_size(const akvs_model_cfg *m, const akvs_paged_cfg *
  * Scores are formed of q and the codes in fp32 (rows_max * Hq / Hkv above 48: of q scaled into fp16
  * by a power of two, which is exact for elements down to 2^-24 of the row's largest). Probabilities
  * are rounded to fp16, with a value's scale or beside the value rounded to fp16 (fp32 where scale and
- * zero lead past fp16's range); outputs of parts of the keys to fp16 scaled by a power of two; sums and
- * statistics are fp32: 65536 keys of even weights lose no more than the bf16 result's own rounding. A
- * query with an infinity may give NaN in its own row.
+ * zero lead past fp16's range); sums, of parts of the keys too, and statistics are fp32: 65536 keys of
+ * even weights lose no more than the bf16 result's own rounding. A query with an infinity may give NaN
+ * in its own row.
  * out may be q; out, lse and ws overlap nothing else. Errors as above, ENOSPACE. */
 akvs_status akvs_paged_attention(const void *q, const akvs_paged_cfg *c, const akvs_pages *p,
                                  const akvs_model_cfg *m, void *out, float *lse, void *ws,

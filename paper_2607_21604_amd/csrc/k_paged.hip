@@ -29,6 +29,9 @@ struct PagedPlan {
   bool many;                             // k_paged_many's
 };
 constexpr int PG_TILE = 64;  // keys a wave takes at a time
+// Parts of the keys leave their outputs in fp32: parts may cancel, and fp16 (scaled by a power of two)
+// keeps 11 bits of each. 13200 pairs in 6 parts are merged in 8.8 us, in fp16 in 6.4, after a launch
+// that takes 92.6 and 94.7, fp16 having to find the largest value first.
 
 // Sum (MAX: largest, of numbers >= 0) over a wave by DPP: rows of 16, then each row's last to the next.
 template <bool MAX>
@@ -111,7 +114,7 @@ template <int HD, int NB, bool WIDE>
 __global__ __launch_bounds__(256, 2) void k_paged_few(
     PagedBatch s, PagePool p, PagedPlan plan, const bf16_t *__restrict__ Q, int hq, int hkv,
     float scale_log2, bf16_t *__restrict__ out, float *__restrict__ lse,
-    _Float16 *__restrict__ part_o, float4 *__restrict__ part_ml) {
+    float *__restrict__ part_o, float4 *__restrict__ part_ml) {
   constexpr int NG = HD / 64, DB = HD / 16;      // groups of a row, blocks of 16 dims
   constexpr int RB = HD / 2;                     // bytes of a row's codes
   constexpr int VST = RB + 16;                   // row stride in LDS: reads on all banks
@@ -559,23 +562,10 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(
     int r, head;
     place(v0 + i, r, head);
     const size_t row = (size_t)r * hq + head;
-    if (split) {  // fp16 scaled by a power of two, as the merge takes them
-      float big = 0.f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float x = fabsf(a[j]);
-        big = x < INFINITY ? fmaxf(big, x) : big;
-      }
-#pragma unroll
-      for (int d = 1; d < PER; d <<= 1) big = fmaxf(big, __shfl_xor(big, d, 64));
-      const int e = max(__builtin_amdgcn_frexp_expf(big), -100) - 15;
-      const float down = ldexpf(1.f, -e);
+    if (split) {
       const size_t prow = (size_t)chunk * s.n_rows * hq + row;
-      f16x8_t x;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = (_Float16)(a[j] * down);
-      *reinterpret_cast<f16x8_t *>(part_o + prow * HD + e0) = x;
-      if (e0 == 0) part_ml[prow] = make_float4(mm, l, ldexpf(1.f, e), 0.f);
+      store8(part_o + prow * HD + e0, a);
+      if (e0 == 0) part_ml[prow] = make_float4(mm, l, 1.f, 0.f);
     } else {
       const float inv = l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll
@@ -607,7 +597,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
                                                        int hkv, float scale_log2,
                                                        bf16_t *__restrict__ out,
                                                        float *__restrict__ lse,
-                                                       _Float16 *__restrict__ part_o,
+                                                       float *__restrict__ part_o,
                                                        float4 *__restrict__ part_ml) {
   constexpr int KS = HD / 16, DB = HD / 32, NG = HD / 64, RB = HD / 2;
   constexpr int WORDS = HD / 32;                   // of codes per thread: 4 threads a row
@@ -955,30 +945,14 @@ __global__ __launch_bounds__(256, 2) void k_paged_many(PagedBatch s, PagePool p,
     }
   }
   if (plan.chunks > 1) {
-    float big = 0.f;  // the pair's largest finite value
+    float *po = part_o + prow * HD + hi * 4;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float x = fabsf(o[db][i]);
-        big = x < INFINITY ? fmaxf(big, x) : big;
-      }
-    big = fmaxf(big, __shfl_xor(big, 32, 64));
-    const int e = max(__builtin_amdgcn_frexp_expf(big), -100) - 15;
-    const float down = ldexpf(1.f, -e);
-    _Float16 *po = part_o + prow * HD + hi * 4;
-    typedef _Float16 f16x4_t __attribute__((ext_vector_type(4)));
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) {
-        f16x4_t x;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = (_Float16)(o[db][4 * q4 + j] * down);
-        *reinterpret_cast<f16x4_t *>(po + db * 32 + q4 * 8) = x;
-      }
-    if (hi == 0)
-      part_ml[prow] = make_float4(m_run - P_BITS, l, ldexpf(1.f, e), 0.f);
+      for (int q4 = 0; q4 < 4; ++q4)
+        *reinterpret_cast<float4 *>(po + db * 32 + q4 * 8) = make_float4(
+            o[db][4 * q4], o[db][4 * q4 + 1], o[db][4 * q4 + 2], o[db][4 * q4 + 3]);
+    if (hi == 0) part_ml[prow] = make_float4(m_run - P_BITS, l, 1.f, 0.f);
     return;
   }
   const float inv = l == 0.f ? 0.f : 1.0f / l;
@@ -1018,14 +992,15 @@ static PagedPlan paged_plan(const PagedBatch &s, int hq, int hkv, int hd) {
   p.pairs = pairs <= 4 && hd == 64 ? 4 : pairs <= 8 ? 8 : pairs <= 48 ? 16 : pairs <= 64 ? 64 : 128;
   p.many = pairs > 48;
   p.tiles = (int)((pairs + p.pairs - 1) / p.pairs);
-  const double FIXED = 7, WALK = p.many ? 3.3 : 2.55, ALONE = 0.6, MOVED = 5e6;
+  // (MOVED: bytes of the partials in a us, most of them to and from the caches)
+  const double FIXED = 7, WALK = p.many ? 3.3 : 2.55, ALONE = 0.6, MOVED = 1e7;
   const int kt = (s.limit + PG_TILE - 1) / PG_TILE, unit = p.many ? 1 : 4;
   // (k_paged_few, heads of 64: 3 blocks fit a unit, and some are empty)
   const long long slots = gemm_cu_count() * (hd == 128 ? 2LL : p.many ? 3LL : 4LL);
   // (tiles of a request that has fewer rows than another are empty)
   const double items =
       hkv * std::min((double)s.n_req * p.tiles, (double)s.n_rows * G / p.pairs + 0.5 * s.n_req);
-  const double moved = (double)s.n_rows * hq * (4 * hd + 32) / MOVED;  // a chunk's partials
+  const double moved = (double)s.n_rows * hq * (8 * hd + 32) / MOVED;  // a chunk's partials
   auto end = [&](long long n) {
     const double walk = WALK * (double)(((kt + n - 1) / n + unit - 1) / unit);
     const double count = items * n, rounds = std::floor(count / slots), rest = count - rounds * slots;
@@ -1053,7 +1028,7 @@ size_t paged_part_floats(const PagedBatch &s, int hq, int hkv, int hd) {
   if (s.n_rows == 0) return 0;
   const PagedPlan p = paged_plan(s, hq, hkv, hd);
   const size_t items = (size_t)p.chunks * s.n_rows * hq;
-  return p.chunks > 1 ? items * (hd / 2) + items * 4 : 0;
+  return p.chunks > 1 ? items * hd + items * 4 : 0;
 }
 
 long long paged_blocks(const PagedBatch &s, int hq, int hkv, int hd) {
@@ -1071,7 +1046,7 @@ hipError_t launch_paged_attention(const PagedBatch &s, const PagePool &p, const 
   const bf16_t *Q = reinterpret_cast<const bf16_t *>(q);
   bf16_t *O = reinterpret_cast<bf16_t *>(out);
   float4 *ml = reinterpret_cast<float4 *>(part);  // (m, l, f) of every slot, then the outputs
-  _Float16 *po = reinterpret_cast<_Float16 *>(ml + (size_t)plan.chunks * s.n_rows * hq);
+  float *po = reinterpret_cast<float *>(ml + (size_t)plan.chunks * s.n_rows * hq);
 #define AKVS_PAGED(...)                                                                          \
   hipLaunchKernelGGL((__VA_ARGS__), g, b, 0, st, s, p, plan, Q, hq, hkv, scale, O, lse, po, ml)
 #define AKVS_PAGED_FEW(HD_, NB_)                            \

@@ -1134,12 +1134,10 @@ static hipError_t shared_merge(const SharedBatch &s, int slots, int hq, const TP
   const size_t items = (size_t)s.n_rows * hq;
   const dim3 b(256);
   const dim3 gf((unsigned)((items * (HD / 8) + 255) / 256));
-  if constexpr (sizeof(TP) == 2) {
-    if (slots > MERGE_FEW && slots <= eight) {
-      hipLaunchKernelGGL((k_shared_merge_few<TS, TP, 8>), gf, b, 0, st, s, slots, hq, HD, po, ml, out,
-                         lse);
-      return hipGetLastError();
-    }
+  if (slots > MERGE_FEW && slots <= eight) {
+    hipLaunchKernelGGL((k_shared_merge_few<TS, TP, 8>), gf, b, 0, st, s, slots, hq, HD, po, ml, out,
+                       lse);
+    return hipGetLastError();
   }
   if (slots <= MERGE_FEW) {
     hipLaunchKernelGGL((k_shared_merge_few<TS, TP, MERGE_FEW>), gf, b, 0, st, s, slots, hq, HD, po, ml,
@@ -1156,13 +1154,13 @@ static hipError_t shared_merge(const SharedBatch &s, int slots, int hq, const TP
 
 hipError_t launch_merge_slots(const SharedBatch &s, int slots, int hq, int hd, const void *po,
                               const void *ml, void *out, float *lse, hipStream_t st) {
-  const _Float16 *o = reinterpret_cast<const _Float16 *>(po);
+  const float *o = reinterpret_cast<const float *>(po);
   const float4 *m = reinterpret_cast<const float4 *>(ml);
   bf16_t *O = reinterpret_cast<bf16_t *>(out);
-  // (many pairs in up to 8 slots: 13200 in 6 take 6.5 us so, 8.6 with a wave each)
+  // (many pairs in up to 8 slots: 13200 in 6 take 8.8 us so, 9.5 with a wave each)
   const int eight = (size_t)s.n_rows * hq >= 4096 ? 8 : 0;
-  return hd == 128 ? shared_merge<bf16_t, _Float16, 128>(s, slots, hq, o, m, O, lse, st, eight)
-                   : shared_merge<bf16_t, _Float16, 64>(s, slots, hq, o, m, O, lse, st, eight);
+  return hd == 128 ? shared_merge<bf16_t, float, 128>(s, slots, hq, o, m, O, lse, st, eight)
+                   : shared_merge<bf16_t, float, 64>(s, slots, hq, o, m, O, lse, st, eight);
 }
 
 template <typename TS, int HD>

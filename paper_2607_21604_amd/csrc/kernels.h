@@ -214,8 +214,9 @@ hipError_t launch_shared_attention(const SharedBatch &s, const void *q, const vo
                                    hipStream_t st);
 // floats of `part` (partials of key splits) that launch_shared_attention needs
 size_t shared_part_floats(const SharedBatch &s, int hq, int hkv, int hd, int dtype);
-// bf16 rows from fp16 partials in `slots` key splits (2 .. MERGE_SLOTS), as k_shared_bf16 leaves
-// them: po [slots][n_rows][hq][hd], ml [slots][n_rows][hq] (m, l, f, -); of s the rows alone count.
+// bf16 rows from fp32 partials in `slots` key splits (2 .. MERGE_SLOTS): po [slots][n_rows][hq][hd],
+// ml [slots][n_rows][hq] (m, l, f = 1 or, where a split has no key of the row, 0, -); of s the rows
+// alone count.
 constexpr int MERGE_SLOTS = 1024;  // the most slots
 hipError_t launch_merge_slots(const SharedBatch &s, int slots, int hq, int hd, const void *po,
                               const void *ml, void *out, float *lse, hipStream_t st);

@@ -880,9 +880,9 @@ MANY = [((28, 4, 128), [9, 2]), ((16, 8, 64), [30, 2])]  # 63 and 60 pairs of a 
 
 
 def chunks(b, c):
-    """Parts that the keys are cut into: each has 16 bytes and an fp16 output of every pair."""
+    """Parts that the keys are cut into: each has 16 bytes and an fp32 output of every pair."""
     n = akvs.akvs_paged_workspace_size(b.m, c)
-    return n // (b.q.shape[0] * b.hq * (16 + 2 * b.hd)) if n else 1
+    return n // (b.q.shape[0] * b.hq * (16 + 4 * b.hd)) if n else 1
 
 
 @pytest.mark.parametrize("geom,rows", MANY)
@@ -1027,3 +1027,23 @@ def test_w4_swiglu_of_four_tiles_of_rows(rows, n_in, n_out):
     tol = 1.1 * tg * (u.abs() + tu) + tu * s.abs() + 2.0 ** -20 * (1 + g.abs()) * want.abs()
     want, tol = want[:, take[:half]], tol[:, take[:half]]
     assert bool(((y.double().cpu() - want).abs() <= rounded(tol, want, F32)).all())
+
+
+@pytest.mark.parametrize("geom,rows", MANY + [((28, 4, 128), [1, 2]), ((8, 8, 64), [2, 1])])
+def test_parts_that_cancel(geom, rows):
+    """Even weights over values of 1024 + c, then of -1024 + c. A probability is 2^7 and a value below
+    2^11 in size, all of them whole: sums over 3000 keys are multiples of 2^7 below 2^7 2^22, exact in 32
+    bits, whatever their order. The result, about 7, has the rounding to bf16 and those of the
+    reciprocal and the product with it."""
+    b = Batch(geom, 64, [3000, 2900], rows, seed=91)
+    b.q[:] = 0
+    codes, meta = b.pools[1]
+    for s in range(2):
+        for j in range(b.lens[s]):
+            page, at = ref.place(b.table[s], 64, b.n_pages, j)
+            meta[page, :, at] = torch.tensor([1.0, 1024.0 if 2 * j < b.lens[s] else -1024.0], dtype=F16)
+    assert chunks(b, b.cfg()) > 1
+    b.attend()
+    want = ref.attention_by_heads(b.q, *b.pools, b.table, b.lens, b.start, b.seq)["out"]
+    tol = (2.0 ** -8 + 2.0 ** -22) * want.abs()
+    assert bool(((b.out.double().cpu() - want).abs() <= tol).all())
